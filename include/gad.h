@@ -348,6 +348,30 @@ const char* gad_last_error(const gad_ctx* ctx);
  * context: at most 16 blocks of 16 KB and two of 8 MB in a process. */
 void gad_destroy(gad_ctx* ctx);
 
+/* ---- operators of an output head: they need no context, and work on device memory of the caller --------------------------------
+ * Element types of their matrices (sums and statistics are fp32 whatever the type): */
+#define GAD_F32 0
+#define GAD_F16 1
+#define GAD_BF16 2
+
+/* Layer norm over the columns of x [rows x cols] (row stride ldx elements, at least cols; 0 = every row is the first):
+ *   mean_i, rstd_i = 1 / sqrt(mean((x_i - mean_i)^2) + eps),  y = (x - mean) rstd gamma + beta.
+ * gamma, beta [cols] in param_dtype (that of x, or GAD_F32); NULL means 1 and 0.  mean, rstd [rows] are what the backward pass needs.
+ * Outputs must not overlap inputs.  Enqueued on `stream`; nothing waits. */
+int gad_layer_norm(const void* x, int64_t ldx, int64_t rows, int32_t cols, int32_t dtype, const void* gamma,
+                   const void* beta, int32_t param_dtype, float eps, void* y, int64_t ldy, float* mean, float* rstd,
+                   void* stream);
+
+/* Its backward pass.  With h = (x - mean) rstd and g = dy gamma:
+ *   dx = rstd (g - mean(g) - h mean(g h)) in x's type,  dgamma = sum over rows of dy h,  dbeta = sum over rows of dy, in
+ * param_dtype.  dgamma and dbeta may be NULL; with both NULL no workspace is needed.  The sums over rows are taken in an order
+ * that depends on the sizes alone, so equal calls give equal bits.  workspace: device, 16-byte aligned. */
+int gad_layer_norm_backward_workspace_bytes(int64_t rows, int32_t cols, size_t* bytes);
+int gad_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t rows, int32_t cols,
+                            int32_t dtype, const void* gamma, int32_t param_dtype, const float* mean, const float* rstd,
+                            void* dx, int64_t lddx, void* dgamma, void* dbeta, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
 /* Frees the pinned host memory that the library keeps and no context or call is using. */
 int gad_release_pinned(void);
 

@@ -1,0 +1,421 @@
+// Layer norm over the columns of a matrix, forward and backward:
+//   mu_i = mean_c x_ic,  r_i = 1 / sqrt(mean_c (x_ic - mu_i)^2 + eps),  h = (x - mu) r,  y = h gamma + beta;
+//   with g = dy gamma:  dx = r (g - mean_c g - h mean_c (g h)),  dgamma = sum_i dy h,  dbeta = sum_i dy.
+// Both are bound by HBM: forward reads x and writes y, backward reads dy and x and writes dx, once.  A row is held in the registers of one
+// warp (up to 1024 two-byte or 512 four-byte values) or of one block, so that nothing is read twice; sums are fp32 and every statistic is taken from the
+// registers in two passes (a thread's own mean and squared deviations, joined pairwise), which loses nothing to a large mean.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "gad_internal.h"
+#include "half_types.cuh"
+
+namespace gad {
+
+namespace {
+
+// Blocks of the backward pass at most, each with a partial sum of dgamma and dbeta: four on every SM.
+constexpr int kNormBlocks = 592;
+
+// gamma / beta in fp32 or in the matrix's own type; null is 1 or 0.
+template <class T, int VEC>
+__device__ __forceinline__ void load_param(const void* p, bool fp32, int c, int cols, float none, float (&v)[VEC]) {
+    if (!p) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[j] = none;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        if (c + j >= cols) v[j] = 0.f;
+        else v[j] = fp32 ? reinterpret_cast<const float*>(p)[c + j] : to_float(reinterpret_cast<const T*>(p)[c + j]);
+    }
+}
+
+template <int WPR> struct RowGroup {   // WPR warps share a row; a block has several rows only with one warp each
+    static constexpr int kRows = WPR == 1 ? 4 : 1;
+    static constexpr int kThreads = 32 * WPR * kRows;
+};
+
+// A row's sum over its WPR warps.  `slot` alternates between two places, so that one barrier a call is enough.
+template <int WPR, int NS>
+__device__ __forceinline__ void row_sum(float (&v)[NS], float* sm, int slot) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < NS; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    if constexpr (WPR > 1) {
+        float* at = sm + slot * NS * WPR;
+        const int w = threadIdx.x >> 5;
+        if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i) at[i * WPR + w] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < WPR; ++k) s += at[i * WPR + k];
+            v[i] = s;
+        }
+    }
+}
+
+// NV vectors of VEC values a thread hold a row: vector k of thread t starts at column (k * threads + t) * VEC.
+template <class T, int VEC, int NV, int WPR>
+__global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* __restrict__ x, long long ldx, long long rows, int cols, const void* __restrict__ gamma,
+                                                                       const void* __restrict__ beta, bool p32, float eps, T* __restrict__ y, long long ldy,
+                                                                       float* __restrict__ mean, float* __restrict__ rstd) {
+    constexpr int TPR = 32 * WPR;
+    __shared__ float sm[2 * WPR];
+    const int t = threadIdx.x % TPR;
+    const long long r = (long long)blockIdx.x * RowGroup<WPR>::kRows + threadIdx.x / TPR;
+    if (r >= rows) return;                       // (a whole warp, or a whole block)
+    float v[NV][VEC];
+    const T* xr = x + r * ldx;
+    float s[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = (k * TPR + t) * VEC;
+        load_vec<T, VEC>(xr, c, cols, v[k]);     // zeros behind the last column
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) s[0] += v[k][j];
+    }
+    row_sum<WPR, 1>(s, sm, 0);
+    const float mu = s[0] / (float)cols;
+    float q[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = (k * TPR + t) * VEC;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            if (c + j < cols) { const float d = v[k][j] - mu; q[0] = fmaf(d, d, q[0]); }
+    }
+    row_sum<WPR, 1>(q, sm, 1);
+    const float rs = 1.f / sqrtf(q[0] / (float)cols + eps);
+    T* yr = y + r * ldy;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int c = (k * TPR + t) * VEC;
+        if (c >= cols) continue;
+        float g[VEC], b[VEC];
+        load_param<T, VEC>(gamma, p32, c, cols, 1.f, g);
+        load_param<T, VEC>(beta, p32, c, cols, 0.f, b);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[k][j] = fmaf((v[k][j] - mu) * rs, g[j], b[j]);
+        store_vec<T, VEC>(yr, c, cols, v[k]);
+    }
+    if (t == 0) { mean[r] = mu; rstd[r] = rs; }
+}
+
+// Rows longer than a block's registers hold: read three times, from L2 as long as they fit it.
+template <class T>
+__global__ void __launch_bounds__(1024) norm_long_kernel(const T* __restrict__ x, long long ldx, int cols, const void* __restrict__ gamma, const void* __restrict__ beta,
+                                                         bool p32, float eps, T* __restrict__ y, long long ldy, float* __restrict__ mean, float* __restrict__ rstd) {
+    __shared__ float sm[2 * 32];
+    const long long r = blockIdx.x;
+    const T* xr = x + r * ldx;
+    float s[1] = {0.f};
+    for (int c = threadIdx.x; c < cols; c += 1024) s[0] += to_float(xr[c]);
+    row_sum<32, 1>(s, sm, 0);
+    const float mu = s[0] / (float)cols;
+    float q[1] = {0.f};
+    for (int c = threadIdx.x; c < cols; c += 1024) { const float d = to_float(xr[c]) - mu; q[0] = fmaf(d, d, q[0]); }
+    row_sum<32, 1>(q, sm, 1);
+    const float rs = 1.f / sqrtf(q[0] / (float)cols + eps);
+    for (int c = threadIdx.x; c < cols; c += 1024) {
+        float g[1], b[1];
+        load_param<T, 1>(gamma, p32, c, cols, 1.f, g);
+        load_param<T, 1>(beta, p32, c, cols, 0.f, b);
+        y[r * ldy + c] = from_float<T>(fmaf((to_float(xr[c]) - mu) * rs, g[0], b[0]));
+    }
+    if (threadIdx.x == 0) { mean[r] = mu; rstd[r] = rs; }
+}
+
+// Every block takes rows blockIdx, blockIdx + gridDim ... (several at once where a row is a warp's) and keeps the sums of dy h and dy of its
+// columns in registers; they go to partial[block][2][cols], which norm_columns_kernel adds up in block order.
+template <class T, int VEC, int NV, int WPR>
+__global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, long long rows,
+                                                                                int cols, const void* __restrict__ gamma, bool p32, const float* __restrict__ mean,
+                                                                                const float* __restrict__ rstd, T* __restrict__ dx, long long lddx, float* __restrict__ partial) {
+    constexpr int TPR = 32 * WPR, ROWS = RowGroup<WPR>::kRows;
+    __shared__ float sm[2 * 2 * WPR];
+    extern __shared__ float cs[];                // with several rows a block: [2][cols]
+    const int t = threadIdx.x % TPR;
+    float ag[NV][VEC], ab[NV][VEC], g[NV][VEC];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        load_param<T, VEC>(gamma, p32, (k * TPR + t) * VEC, cols, 1.f, g[k]);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) ag[k][j] = ab[k][j] = 0.f;
+    }
+    const float inv = 1.f / (float)cols;
+    int slot = 0;
+    for (long long r = (long long)blockIdx.x * ROWS + threadIdx.x / TPR; r < rows; r += (long long)gridDim.x * ROWS, slot ^= 1) {
+        const float mu = mean[r], rs = rstd[r];
+        float d[NV][VEC], h[NV][VEC], s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TPR + t) * VEC;
+            load_vec<T, VEC>(dy + r * lddy, c, cols, d[k]);
+            load_vec<T, VEC>(x + r * ldx, c, cols, h[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                h[k][j] = (h[k][j] - mu) * rs;   // (behind the last column d = 0: adds nothing)
+                ag[k][j] = fmaf(d[k][j], h[k][j], ag[k][j]);
+                ab[k][j] += d[k][j];
+                d[k][j] *= g[k][j];
+                s[0] += d[k][j];
+                s[1] = fmaf(d[k][j], h[k][j], s[1]);
+            }
+        row_sum<WPR, 2>(s, sm, slot);
+        const float m0 = s[0] * inv, m1 = s[1] * inv;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TPR + t) * VEC;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) d[k][j] = (d[k][j] - m0 - h[k][j] * m1) * rs;
+            if (c < cols) store_vec<T, VEC>(dx + r * lddx, c, cols, d[k]);
+        }
+    }
+    if (!partial) return;
+    float* out = partial + (long long)blockIdx.x * 2 * cols;
+    if constexpr (ROWS == 1) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TPR + t) * VEC;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (c + j < cols) { out[c + j] = ag[k][j]; out[cols + c + j] = ab[k][j]; }
+        }
+    } else {
+        for (int w = 0; w < ROWS; ++w) {          // warp by warp, in order
+            if (threadIdx.x / TPR == w) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int c = (k * TPR + t) * VEC;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (c + j < cols) {
+                            cs[c + j] = w ? cs[c + j] + ag[k][j] : ag[k][j];
+                            cs[cols + c + j] = w ? cs[cols + c + j] + ab[k][j] : ab[k][j];
+                        }
+                }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < 2 * cols; c += RowGroup<WPR>::kThreads) out[c] = cs[c];
+    }
+}
+
+// Long rows: dx by a block a row, read twice.
+template <class T>
+__global__ void __launch_bounds__(1024) norm_backward_long_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, int cols,
+                                                                  const void* __restrict__ gamma, bool p32, const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                                  T* __restrict__ dx, long long lddx) {
+    __shared__ float sm[2 * 2 * 32];
+    const long long r = blockIdx.x;
+    const float mu = mean[r], rs = rstd[r], inv = 1.f / (float)cols;
+    float s[2] = {0.f, 0.f}, g[1];
+    for (int c = threadIdx.x; c < cols; c += 1024) {
+        load_param<T, 1>(gamma, p32, c, cols, 1.f, g);
+        const float d = to_float(dy[r * lddy + c]) * g[0];
+        s[0] += d;
+        s[1] = fmaf(d, (to_float(x[r * ldx + c]) - mu) * rs, s[1]);
+    }
+    row_sum<32, 2>(s, sm, 0);
+    const float m0 = s[0] * inv, m1 = s[1] * inv;
+    for (int c = threadIdx.x; c < cols; c += 1024) {
+        load_param<T, 1>(gamma, p32, c, cols, 1.f, g);
+        dx[r * lddx + c] = from_float<T>((to_float(dy[r * lddy + c]) * g[0] - m0 - (to_float(x[r * ldx + c]) - mu) * rs * m1) * rs);
+    }
+}
+// ... and their column sums: a block has 32 columns and every gridDim.y-th eight rows.
+template <class T>
+__global__ void __launch_bounds__(256) norm_long_columns_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, long long rows, int cols,
+                                                                const float* __restrict__ mean, const float* __restrict__ rstd, float* __restrict__ partial) {
+    __shared__ float sm[2][8][32];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+    float ag = 0.f, ab = 0.f;
+    if (c < cols)
+        for (long long r = (long long)blockIdx.y * 8 + w; r < rows; r += 8ll * gridDim.y) {
+            const float d = to_float(dy[r * lddy + c]);
+            ag = fmaf(d, (to_float(x[r * ldx + c]) - mean[r]) * rstd[r], ag);
+            ab += d;
+        }
+    sm[0][w][threadIdx.x & 31] = ag;
+    sm[1][w][threadIdx.x & 31] = ab;
+    __syncthreads();
+    if (w < 2 && c < cols) {
+        float s = 0.f;
+        for (int i = 0; i < 8; ++i) s += sm[w][i][threadIdx.x & 31];
+        partial[((long long)blockIdx.y * 2 + w) * cols + c] = s;
+    }
+}
+
+// dgamma, dbeta [2 x cols] = the blocks' partial sums, in block order: 32 columns a block, each of its eight warps a run of blocks.
+template <class T>
+__global__ void __launch_bounds__(256) norm_columns_kernel(const float* __restrict__ partial, int nblocks, int cols, bool p32, void* __restrict__ dgamma, void* __restrict__ dbeta) {
+    __shared__ float sm[8][32];
+    const int i = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+    const int per = (nblocks + 7) / 8, lo = min(nblocks, w * per), hi = min(nblocks, lo + per);
+    float s = 0.f;
+    if (i < 2 * cols)
+        for (int b = lo; b < hi; ++b) s += partial[(long long)b * 2 * cols + i];
+    sm[w][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (w || i >= 2 * cols) return;
+    s = 0.f;
+    for (int k = 0; k < 8; ++k) s += sm[k][threadIdx.x & 31];
+    void* out = i < cols ? dgamma : dbeta;
+    const int c = i < cols ? i : i - cols;
+    if (!out) return;
+    if (p32) reinterpret_cast<float*>(out)[c] = s;
+    else reinterpret_cast<T*>(out)[c] = from_float<T>(s);
+}
+
+bool wide_rows(const void* p, int64_t ld, size_t size) { return ((uintptr_t)p & 15) == 0 && (ld * size) % 16 == 0; }
+
+struct NormCall {
+    const void *x, *gamma, *beta;
+    int64_t ldx, rows;
+    int cols;
+    bool p32;
+    float eps;
+    void* y;
+    int64_t ldy;
+    float *mean, *rstd;
+};
+
+template <class T, int VEC, int NV, int WPR>
+void norm_go(const NormCall& a, cudaStream_t s) {
+    const int64_t blocks = (a.rows + RowGroup<WPR>::kRows - 1) / RowGroup<WPR>::kRows;
+    norm_kernel<T, VEC, NV, WPR><<<(unsigned)blocks, RowGroup<WPR>::kThreads, 0, s>>>((const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.beta, a.p32, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
+}
+template <class T>
+void norm_pick(const NormCall& a, cudaStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    if (wide_rows(a.x, a.ldx, sizeof(T)) && wide_rows(a.y, a.ldy, sizeof(T))) {
+        const int n = (a.cols + V - 1) / V;
+        if (n <= 32) return norm_go<T, V, 1, 1>(a, s);
+        if (n <= 64) return norm_go<T, V, 2, 1>(a, s);
+        if (n <= 128) return norm_go<T, V, 4, 1>(a, s);
+        if (n <= 256) return norm_go<T, V, 2, 4>(a, s);
+        if (n <= 512) return norm_go<T, V, 2, 8>(a, s);
+        if (n <= 1024) return norm_go<T, V, 4, 8>(a, s);
+        if (n <= 2048) return norm_go<T, V, 4, 16>(a, s);
+        if (n <= 4096) return norm_go<T, V, 4, 32>(a, s);
+    } else {
+        if (a.cols <= 128) return norm_go<T, 1, 4, 1>(a, s);
+        if (a.cols <= 1024) return norm_go<T, 1, 8, 4>(a, s);
+        if (a.cols <= 2048) return norm_go<T, 1, 8, 8>(a, s);
+        if (a.cols <= 8192) return norm_go<T, 1, 16, 16>(a, s);
+    }
+    norm_long_kernel<T><<<(unsigned)a.rows, 1024, 0, s>>>((const T*)a.x, a.ldx, a.cols, a.gamma, a.beta, a.p32, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
+}
+
+struct NormBackCall {
+    const void *dy, *x, *gamma;
+    int64_t lddy, ldx, rows;
+    int cols;
+    bool p32;
+    const float *mean, *rstd;
+    void* dx;
+    int64_t lddx;
+    void *dgamma, *dbeta;
+    float* partial;
+};
+
+template <class T, int VEC, int NV, int WPR>
+int norm_back_go(const NormBackCall& a, cudaStream_t s) {
+    constexpr int ROWS = RowGroup<WPR>::kRows;
+    const int blocks = (int)std::min<int64_t>((a.rows + ROWS - 1) / ROWS, kNormBlocks);
+    norm_backward_kernel<T, VEC, NV, WPR><<<(unsigned)blocks, RowGroup<WPR>::kThreads, ROWS > 1 ? 8 * (size_t)a.cols : 0, s>>>(
+        (const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.p32, a.mean, a.rstd, (T*)a.dx, a.lddx, a.partial);
+    return blocks;
+}
+template <class T>
+int norm_back_rows(const NormBackCall& a, cudaStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    if (wide_rows(a.x, a.ldx, sizeof(T)) && wide_rows(a.dy, a.lddy, sizeof(T)) && wide_rows(a.dx, a.lddx, sizeof(T))) {
+        const int n = (a.cols + V - 1) / V;
+        if (n <= 32) return norm_back_go<T, V, 1, 1>(a, s);
+        if (n <= 64) return norm_back_go<T, V, 2, 1>(a, s);
+        if (n <= 128) return norm_back_go<T, V, 1, 4>(a, s);
+        if (n <= 256) return norm_back_go<T, V, 1, 8>(a, s);
+        if (n <= 512) return norm_back_go<T, V, 2, 8>(a, s);
+        if (n <= 1024) return norm_back_go<T, V, 2, 16>(a, s);
+        if (n <= 2048) return norm_back_go<T, V, 2, 32>(a, s);
+    } else {
+        if (a.cols <= 128) return norm_back_go<T, 1, 4, 1>(a, s);
+        if (a.cols <= 1024) return norm_back_go<T, 1, 8, 4>(a, s);
+        if (a.cols <= 2048) return norm_back_go<T, 1, 8, 8>(a, s);
+        if (a.cols <= 8192) return norm_back_go<T, 1, 16, 16>(a, s);
+    }
+    norm_backward_long_kernel<T><<<(unsigned)a.rows, 1024, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.cols, a.gamma, a.p32, a.mean, a.rstd, (T*)a.dx, a.lddx);
+    const int blocks = (int)std::min<int64_t>((a.rows + 7) / 8, 64);
+    if (a.partial) {
+        norm_long_columns_kernel<T><<<dim3((unsigned)((a.cols + 31) / 32), (unsigned)blocks), 256, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.rows, a.cols, a.mean, a.rstd, a.partial);
+        ++g_kernel_launches;
+    }
+    return blocks;
+}
+template <class T>
+void norm_back_pick(const NormBackCall& a, cudaStream_t s) {
+    const int blocks = a.rows > 0 ? norm_back_rows<T>(a, s) : 0;
+    if (a.rows > 0) ++g_kernel_launches;
+    if (!a.dgamma && !a.dbeta) return;
+    norm_columns_kernel<T><<<(unsigned)((2ll * a.cols + 31) / 32), 256, 0, s>>>(a.partial, blocks, a.cols, a.p32, a.dgamma, a.dbeta);
+    ++g_kernel_launches;
+}
+
+bool norm_sizes_ok(int64_t rows, int32_t cols, int32_t dtype, int32_t param_dtype) {
+    return rows >= 0 && rows < ((int64_t)1 << 31) && cols >= 1 && cols <= (1 << 29) && dtype >= GAD_F32 && dtype <= GAD_BF16 && (param_dtype == dtype || param_dtype == GAD_F32);
+}
+
+}  // namespace
+}  // namespace gad
+
+extern "C" int gad_layer_norm(const void* x, int64_t ldx, int64_t rows, int32_t cols, int32_t dtype, const void* gamma, const void* beta, int32_t param_dtype, float eps,
+                              void* y, int64_t ldy, float* mean, float* rstd, void* stream) {
+    using namespace gad;
+    if (!norm_sizes_ok(rows, cols, dtype, param_dtype) || !(eps >= 0.f)) return GAD_ERR_ARG;
+    if (rows == 0) return GAD_OK;
+    if (!x || !y || !mean || !rstd || (ldx && ldx < cols) || ldy < cols) return GAD_ERR_ARG;
+    const NormCall a{x, gamma, beta, ldx, rows, cols, param_dtype == GAD_F32, eps, y, ldy, mean, rstd};
+    const cudaStream_t s = (cudaStream_t)stream;
+    if (dtype == GAD_F32) norm_pick<float>(a, s);
+    else if (dtype == GAD_F16) norm_pick<__half>(a, s);
+    else norm_pick<__nv_bfloat16>(a, s);
+    ++g_kernel_launches;
+    return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
+}
+
+extern "C" int gad_layer_norm_backward_workspace_bytes(int64_t rows, int32_t cols, size_t* bytes) {
+    if (!bytes || rows < 0 || cols < 1) return GAD_ERR_ARG;
+    *bytes = (size_t)std::min<int64_t>(rows, gad::kNormBlocks) * 2 * (size_t)cols * sizeof(float);
+    return GAD_OK;
+}
+
+extern "C" int gad_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t rows, int32_t cols, int32_t dtype, const void* gamma,
+                                       int32_t param_dtype, const float* mean, const float* rstd, void* dx, int64_t lddx, void* dgamma, void* dbeta, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+    using namespace gad;
+    if (!norm_sizes_ok(rows, cols, dtype, param_dtype)) return GAD_ERR_ARG;
+    if (rows > 0 && (!dy || !x || !mean || !rstd || !dx || (lddy && lddy < cols) || (ldx && ldx < cols) || lddx < cols)) return GAD_ERR_ARG;
+    size_t need = 0;
+    gad_layer_norm_backward_workspace_bytes(rows, cols, &need);
+    if ((dgamma || dbeta) && need > 0 && (!workspace || workspace_bytes < need)) return GAD_ERR_OOM;
+    const NormBackCall a{dy, x, gamma, lddy, ldx, rows, cols, param_dtype == GAD_F32, mean, rstd, dx, lddx, dgamma, dbeta, dgamma || dbeta ? (float*)workspace : nullptr};
+    const cudaStream_t s = (cudaStream_t)stream;
+    if (dtype == GAD_F32) norm_back_pick<float>(a, s);
+    else if (dtype == GAD_F16) norm_back_pick<__half>(a, s);
+    else norm_back_pick<__nv_bfloat16>(a, s);
+    return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
+}
