@@ -372,6 +372,51 @@ int gad_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t
                             void* dx, int64_t lddx, void* dgamma, void* dbeta, void* workspace, size_t workspace_bytes,
                             void* stream);
 
+/* Loss of an output layer z = H W^T + b over many classes, and its gradients, without keeping z (rows x classes): softmax cross
+ * entropy against labels (k = 0), or distillation from the k largest logits of a teacher (k > 0).  With q_i = softmax(teacher_i / T)
+ * over the slots of row i that are used:
+ *   k = 0:  l_i = log sum_v exp(z_iv) - z_{i, label}
+ *   k > 0:  l_i = a (that, where the row has a label) + (1 - a) T^2 sum_j q_ij (log q_ij - log softmax(z_i / T)_{c_ij})
+ *           (a = hard_weight where labels are given, else 0)
+ *   loss = scale * sum_i w_i l_i, divided by the number of rows that count with `mean`.
+ * A row counts if it has a label (>= 0) and a > 0, or a used slot (target_classes >= 0) and a < 1.  Rows that do not count get loss and dH of zero
+ * whatever H, teacher and weight hold there, and add nothing to dW and db.  If no row counts the loss and all gradients are zero.  A class named twice
+ * in a row's slots has the sum of both.  A label or slot of `classes` or more makes that row's loss, and the whole, NaN.
+ * A bias of -inf takes a class out (its W row must be finite).
+ * Gradients are those of `loss`, in dtype; any of dH, dW, db may be NULL (db needs a bias).  fp32 matrices are multiplied to fp32
+ * accuracy (24-bit operands in three parts); with fp16 and bfloat16 the softmax's gradient is rounded to that type, and row weights
+ * should lie within 2^20 of the largest one in fp16.  Equal calls give equal bits. */
+typedef struct {
+    int32_t dtype;                 /* of H, W, bias, dH, dW, db: GAD_F32, GAD_F16, GAD_BF16                 */
+    int32_t cols, classes;         /* D and V                                                               */
+    int64_t rows;                  /* N                                                                     */
+    const void* H; int64_t ldh;    /* [rows x cols], row stride in elements (0: every row is the first)      */
+    const void* W; int64_t ldw;    /* [classes x cols]                                                      */
+    const void* bias;              /* [classes] or NULL                                                     */
+    const void* labels;            /* [rows] or NULL (k = 0 needs them)                                     */
+    int32_t label_bytes;           /* 4: int32, 8: int64                                                    */
+    int32_t k;                     /* slots a row, at most 1024; 0: no teacher                              */
+    const void* target_classes;    /* [rows x k], int32 or int64                                            */
+    int32_t target_bytes;
+    int32_t teacher_dtype;
+    const void* teacher;           /* [rows x k] logits                                                     */
+    float temperature, hard_weight; /* T in 1e-3 .. 1e3, a in 0 .. 1                                       */
+    const float* row_weights;      /* [rows] or NULL: 1                                                     */
+    float scale;
+    int32_t mean;
+    float* loss;                   /* device [1]                                                            */
+    float* row_loss;               /* device [rows]: l_i                                                    */
+    void* dH; int64_t lddh;
+    void* dW; int64_t lddw;
+    void* db;
+    int32_t* status;               /* device [1]: 0, or the code of a bounded wait that ran out (the other outputs are then undefined) */
+} gad_class_loss_args;
+
+/* Device workspace of gad_class_loss (256-byte aligned), at most about 0.5 GB for the gradients of a piece of the classes beside copies of H (and of W where it is
+ * fp32 or its rows do not start on 16 bytes).  Depends on sizes, types, strides, which pointers are NULL, and W's alignment.  Host-only. */
+int gad_class_loss_workspace_bytes(const gad_class_loss_args* args, size_t* bytes);
+int gad_class_loss(const gad_class_loss_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Frees the pinned host memory that the library keeps and no context or call is using. */
 int gad_release_pinned(void);
 

@@ -29,6 +29,7 @@ SYMBOLS = (
     "gad_consensus_apply", "gad_export_params", "gad_get_train_counts", "gad_augment_workspace_bytes", "gad_augment",
     "gad_augment_last_error", "gad_debug_expire_wait", "gad_default_params", "gad_check_store", "gad_release_pinned",
     "gad_layer_norm", "gad_layer_norm_backward_workspace_bytes", "gad_layer_norm_backward",
+    "gad_class_loss_workspace_bytes", "gad_class_loss",
 )
 
 

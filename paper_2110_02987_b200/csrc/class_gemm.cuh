@@ -1,0 +1,415 @@
+// The matrix product of the output head: C [M x N] = A B^T over 16-bit operands with fp32 accumulators, by pairs of CTAs on tcgen05, and what
+// the loss does with a finished tile.  Used by class_loss.cu for
+//   kStats     z = H W^T + b, not kept: per row the largest value, the sum(s) of the softmax and the product with the row's targets
+//   kGrad      z again, turned into G = d loss / d z and rounded to the operand type (fp32: into three parts)
+//   kOut       dH = G W and dW = G^T H, scaled and rounded to the result's type
+//   kPartial   the same as fp32 sums of a share of the reduction, for join_parts_kernel
+#pragma once
+
+#include <cuda.h>
+
+#include "gad_internal.h"
+#include "half_types.cuh"
+#include "tc_common.cuh"
+
+namespace gad {
+
+namespace {
+
+constexpr int CT_M = 256, CT_H = 128, CT_K = 64;            // rows of a pair's tile, of a CTA's share, reduction per ring stage
+constexpr int CT_OPERAND = CT_H * CT_K * 2;                 // 16 KiB
+constexpr int CT_STAGE = 2 * CT_OPERAND;                    // A | B
+constexpr int CT_STAGES = 6;
+constexpr int CT_RING = CT_STAGES * CT_STAGE;
+constexpr int CT_EPI_WARPS = 8, CT_EPI_WARP0 = 2;           // two per quarter of the tensor-memory lanes, half of the columns each
+constexpr int CT_THREADS = 32 * (CT_EPI_WARP0 + CT_EPI_WARPS);
+constexpr int CT_BIAS = CT_EPI_WARPS * 128 * 4;             // a draining warp's biases
+constexpr int CT_SMEM = CT_RING + 1024 + 256 + CT_BIAS;
+constexpr int CT_TMEM = 512;                                // two accumulators of 256 columns
+
+enum TileUse { kStats, kGrad, kOut, kPartial };
+
+// An operand of the product: a matrix [parts][rows][inner] behind a TMA descriptor.  K-major: inner is the reduction; MN-major: rows are.
+struct TileArgs {
+    int M, N;                  // result
+    int tiles_m, tiles_n, width;   // tiles of 256 x width (128 or 256)
+    int nkb;                   // 64-blocks of the reduction
+    int splits, kb_split;      // shares of it, blocks a share
+    int group;                 // row tiles that are gone through together, for the L2
+    int pairs;                 // products of operand parts: 1, or 6 for operands in three parts
+    int b_row0;                // first row of B (MN-major: added to the reduction, K-major: to the column)
+    int bf16;                  // operand type: 1 bfloat16, 0 fp16
+    int32_t* err;
+    // kStats, kGrad
+    const void* bias;          // [classes] in the caller's type, or null
+    int bias_type;
+    int col0, classes;         // first class of the piece; all of them
+    float sc, inv_t;           // log2(e) (/ T with one softmax), 1 / T of the second
+    const int2* targets;       // [M x ntargets] (class, weight), classes ascending
+    int ntargets;
+    float4* stats;             // [2 tiles_n x M]
+    const float4* rowc;        // [M] coefficients of the softmaxes, their log2 sums
+    const float4* rowk;        // [M] .w = weight of the row
+    const float* scal;         // [0] scale of G, [1] factor of the results
+    void* C;                   // kGrad: G [parts][M x ldc]; kOut, kPartial: the result
+    long long ldc, part_stride;
+    int accumulate;            // kPartial: add to what is there
+};
+
+// Products of operand parts, the smallest first, so that what an addition to the accumulator cuts off is small for as long as possible.
+__device__ __forceinline__ void part_pair(int p, int pairs, int& a, int& b) {
+    if (pairs == 1) { a = b = 0; return; }
+    a = (0x012010 >> (4 * (5 - p))) & 15;     // 0 1 2 0 1 0
+    b = (0x210100 >> (4 * (5 - p))) & 15;     // 2 1 0 1 0 0
+}
+
+// Shared-memory descriptors: K-major as smem_desc; MN-major (16-bit): blocks of 64 values of the M or N axis (128 bytes, 64 reduction rows: 8 KiB apart),
+// groups of eight reduction rows 1024 bytes apart.
+template <bool MN>
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
+    if (!MN) return smem_desc(saddr);
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(8192 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+// This warp's 32 tensor-memory lanes x 32 columns, complete on return.
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
+        "%23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        "tcgen05.wait::ld.sync.aligned;\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]),
+          "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// v[c] for a c that is not known to the compiler, by halving.
+__device__ __forceinline__ float pick(const float (&v)[32], int c) {
+    float a[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) a[j] = (c & 16) ? v[j + 16] : v[j];
+#pragma unroll
+    for (int w = 8; w > 0; w >>= 1)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < w) a[j] = (c & w) ? a[j + w] : a[j];
+    return a[0];
+}
+
+// The bfloat16 parts of a value: x = hi + mid + lo, each the nearest to what is left (a finite value stays finite).
+__device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
+    __nv_bfloat16 h = __float2bfloat16_rn(x);
+    if (__hisinf(h) && !isinf(x)) h = __ushort_as_bfloat16((unsigned short)(0x7F7F | (__float_as_uint(x) >> 31 << 15)));
+    const float r = x - __bfloat162float(h);
+    p[0] = h;
+    p[1] = __float2bfloat16_rn(r);
+    p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
+}
+
+// 32 values of a row, to columns c0 .. of a result row that ends at `cols`.
+template <class T>
+__device__ __forceinline__ void store32(T* row, int c0, int cols, bool wide, const float (&v)[32]) {
+    constexpr int V = 16 / sizeof(T);
+    if (wide && c0 + 32 <= cols) {
+#pragma unroll
+        for (int j = 0; j < 32; j += V) {
+            union { uint4 u; T e[V]; } w;
+#pragma unroll
+            for (int i = 0; i < V; ++i) w.e[i] = from_float<T>(v[j + i]);
+            *reinterpret_cast<uint4*>(row + c0 + j) = w.u;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (c0 + j < cols) row[c0 + j] = from_float<T>(v[j]);
+    }
+}
+
+struct TileAt { int m, n, split; };
+__device__ __forceinline__ TileAt tile_at(const TileArgs& a, long long u) {
+    const long long tiles = (long long)a.tiles_m * a.tiles_n;
+    TileAt t;
+    t.split = (int)(u / tiles);
+    const long long i = u - t.split * tiles, per = (long long)a.group * a.tiles_n;
+    const int g = (int)(i / per), first = g * a.group, rows = min(a.group, a.tiles_m - first);
+    const int r = (int)(i - g * per);
+    t.m = first + r % rows;
+    t.n = r / rows;
+    return t;
+}
+
+// USE as above; A_MN, B_MN: operand is MN-major; T: type of the result (kGrad: float = three bfloat16 parts); NL: softmaxes (temperatures) at once.
+template <int USE, bool A_MN, bool B_MN, class T, int NL>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(CT_THREADS, 1)
+class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ TileArgs a) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;   // the same in both CTAs
+    uint8_t* sm = smem_raw + pad;
+    const uint32_t sm_addr = raw_addr + pad;
+    const uint32_t rank = cluster_rank();
+    const uint32_t bars = sm_addr + CT_RING;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (CT_STAGES + s); };
+    auto pfull = [&](int s) { return bars + 8u * (2 * CT_STAGES + s); };     // leader: the other CTA's stage is full
+    auto tfull = [&](int i) { return bars + 8u * (3 * CT_STAGES + i); };
+    auto tempty = [&](int i) { return bars + 8u * (3 * CT_STAGES + 2 + i); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + CT_RING + 8 * (3 * CT_STAGES + 4));
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < CT_STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); mbar_init(pfull(s), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(tfull(i), 1); mbar_init(tempty(i), 2 * CT_EPI_WARPS); }
+        *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) tmem_alloc2(smem_u32(tmem_slot), CT_TMEM);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();           // the peer's barriers exist before anything arrives at them
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = *tmem_slot;
+
+    const int ncl = gridDim.x >> 1, half_w = a.width / 2;
+    const long long units = (long long)a.tiles_m * a.tiles_n * a.splits;
+    auto blocks_of = [&](int split, int& kb0) {
+        kb0 = split * a.kb_split;
+        return min(a.kb_split, a.nkb - kb0);
+    };
+
+    if (warp == 0 && lane == 0) {
+        // ---------------- TMA producer: this CTA's rows of A and half of the rows of B, 64 of the reduction at a time ----------------
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
+            const TileAt t = tile_at(a, u);
+            const int ra = t.m * CT_M + (int)rank * CT_H, rb = t.n * a.width + (int)rank * half_w;
+            int kb0;
+            const int nkb = blocks_of(t.split, kb0);
+            for (int p = 0; p < a.pairs && ok; ++p) {
+                int za, zb;
+                part_pair(p, a.pairs, za, zb);
+                for (int kb = kb0; kb < kb0 + nkb; ++kb) {
+                    if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, 31))) break;
+                    mbar_expect_tx(full(stage), (uint32_t)(CT_H + half_w) * (CT_K * 2));
+                    const uint32_t base = sm_addr + stage * CT_STAGE;
+                    if (A_MN) {
+                        tma_load_3d(base, &tmA, ra, kb * CT_K, za, full(stage));
+                        tma_load_3d(base + 8192, &tmA, ra + 64, kb * CT_K, za, full(stage));
+                    } else {
+                        tma_load_3d(base, &tmA, kb * CT_K, ra, za, full(stage));
+                    }
+                    if (B_MN) {
+                        for (int j = 0; j < half_w; j += 64) tma_load_3d(base + CT_OPERAND + j * 128, &tmB, rb + j, a.b_row0 + kb * CT_K, zb, full(stage));
+                    } else {
+                        tma_load_3d(base + CT_OPERAND, &tmB, kb * CT_K, a.b_row0 + rb, zb, full(stage));
+                    }
+                    if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 1 && rank == 1) {
+        // ---------------- the other CTA's stages: the leader is told of each ----------------
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (long long u = blockIdx.x >> 1; u < units && ok && lane == 0; u += ncl) {
+            int kb0;
+            const int steps = blocks_of(tile_at(a, u).split, kb0) * a.pairs;
+            for (int i = 0; i < steps; ++i) {
+                if (!(ok = mbar_wait(full(stage), phase, abort_flag, a.err, 34))) break;
+                mbar_arrive_leader(pfull(stage));
+                if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer (leader of the pair): the whole warp runs the loop, one elected lane issues ----------------
+        int stage = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        const uint32_t idesc = instr_desc_f16(a.width, CT_M) | (a.bf16 ? (1u << 7) | (1u << 10) : 0u) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+        constexpr uint32_t stepA = A_MN ? 128 : 2, stepB = B_MN ? 128 : 2;    // 16 values of the reduction: 16 rows of 128 bytes, or 32 bytes of a row
+        bool ok = true;
+        for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
+            int kb0;
+            const int steps = blocks_of(tile_at(a, u).split, kb0) * a.pairs;
+            if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 32)))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t d = tmem_base + (uint32_t)(acc * 256);
+            for (int i = 0; i < steps; ++i) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag, a.err, 33) && mbar_wait<true>(pfull(stage), phase, abort_flag, a.err, 35)))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t base = sm_addr + stage * CT_STAGE;
+                const uint64_t da = operand_desc<A_MN>(base), db = operand_desc<B_MN>(base + CT_OPERAND);
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_pair(d, da + stepA * ks, db + stepB * ks, idesc, (i | ks) != 0 ? 1u : 0u);
+                    mma_commit2(empty(stage));                    // in both CTAs
+                    if (i == steps - 1) mma_commit2(tfull(acc));
+                }
+                __syncwarp();
+                if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
+            }
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+    } else if (warp >= CT_EPI_WARP0) {
+        // ---------------- drain: this warp's 32 rows (a row a lane) x half of the tile's columns ----------------
+        const int ew = warp - CT_EPI_WARP0, q = warp & 3, half = ew >> 2;
+        float* bias = reinterpret_cast<float*>(sm + CT_RING + 256) + ew * 128;
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        float gscale = 1.f, factor = 1.f;
+        if (USE == kGrad) gscale = a.scal[0];
+        if (USE == kOut) factor = a.scal[1];
+        const bool wide = ((uintptr_t)a.C & 15) == 0 && (a.ldc * sizeof(T)) % 16 == 0;
+        for (long long u = blockIdx.x >> 1; u < units; u += ncl) {
+            const TileAt t = tile_at(a, u);
+            const int row = t.m * CT_M + (int)rank * CT_H + q * 32 + lane;
+            const bool rv = row < a.M;
+            const int tile_c = t.n * a.width + half * half_w;               // first column of this warp, in the piece
+            float m2 = -INFINITY, s1 = 0.f, s2 = 0.f, dot = 0.f, fw = 0.f, fa = 0.f, fb = 0.f;
+            float4 rc = make_float4(0.f, 0.f, 0.f, 0.f);
+            int e = 0, next = INT_MAX;
+            const int2* tg = nullptr;
+            if (USE == kStats || USE == kGrad) {
+                __syncwarp();                                               // the previous tile's biases have been read
+                for (int j = lane; j < half_w; j += 32) {
+                    const int c = a.col0 + tile_c + j;
+                    float b = c < a.classes ? 0.f : -INFINITY;              // columns that are no class carry no weight
+                    if (a.bias && c < a.classes)
+                        b = a.bias_type == GAD_F32 ? reinterpret_cast<const float*>(a.bias)[c]
+                            : a.bias_type == GAD_F16 ? to_float(reinterpret_cast<const __half*>(a.bias)[c]) : to_float(reinterpret_cast<const __nv_bfloat16*>(a.bias)[c]);
+                    bias[j] = b * a.sc;
+                }
+                __syncwarp();
+                if (rv) {
+                    tg = a.targets + (long long)row * a.ntargets;
+                    int hi = a.ntargets;                                    // the first target at or behind this warp's columns
+                    while (e < hi) {
+                        const int mid = (e + hi) >> 1;
+                        if (tg[mid].x < a.col0 + tile_c) e = mid + 1; else hi = mid;
+                    }
+                    if (e < a.ntargets) next = tg[e].x;
+                    if (USE == kGrad) {
+                        rc = a.rowc[row];
+                        fw = a.rowk[row].w * gscale;
+                        fa = rc.x * fw;
+                        fb = rc.y * fw;
+                    }
+                }
+            }
+            if (!__all_sync(0xffffffffu, mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 36))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            for (int c0 = 0; c0 < half_w; c0 += 32) {
+                float v[32];
+                __syncwarp();
+                tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * 256 + half * half_w + c0), v);
+                const int gc = a.col0 + tile_c + c0;                        // class of v[0]
+                if (USE == kStats) {
+                    float most = m2;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        v[j] = fmaf(v[j], a.sc, bias[c0 + j]);
+                        most = fmaxf(most, v[j]);
+                    }
+                    const float base = most == -INFINITY ? 0.f : most;      // nothing but masked classes so far: all terms are zero
+                    s1 *= exp2_fast(m2 - base);
+                    if (NL == 2) s2 *= exp2_fast((m2 - base) * a.inv_t);
+                    m2 = most;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        s1 += exp2_fast(v[j] - base);
+                        if (NL == 2) s2 += exp2_fast((v[j] - base) * a.inv_t);
+                    }
+                    while (next < gc + 32) {
+                        dot = fmaf(__int_as_float(tg[e].y), pick(v, next - gc), dot);
+                        next = ++e < a.ntargets ? tg[e].x : INT_MAX;
+                    }
+                } else if (USE == kGrad) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const float z = fmaf(v[j], a.sc, bias[c0 + j]);
+                        v[j] = fw == 0.f ? 0.f : fa * exp2_fast(z - rc.z);
+                        if (NL == 2) v[j] += fw == 0.f ? 0.f : fb * exp2_fast(fmaf(z, a.inv_t, -rc.w));
+                    }
+                    while (next < gc + 32) {
+                        const int at = next - gc;
+                        const float w = fw * __int_as_float(tg[e].y);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] -= j == at ? w : 0.f;
+                        next = ++e < a.ntargets ? tg[e].x : INT_MAX;
+                    }
+                    if (rv) {
+                        if constexpr (sizeof(T) == 4) {                     // three bfloat16 parts
+                            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.C) + (long long)row * a.ldc + tile_c + c0;
+#pragma unroll
+                            for (int j = 0; j < 32; j += 8) {
+                                union { uint4 u; __nv_bfloat16 h[8]; } w[3];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    __nv_bfloat16 p3[3];
+                                    split3(v[j + i], p3);
+#pragma unroll
+                                    for (int k = 0; k < 3; ++k) w[k].h[i] = p3[k];
+                                }
+#pragma unroll
+                                for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(out + k * a.part_stride + j) = w[k].u;
+                            }
+                        } else {
+                            store32<T>(reinterpret_cast<T*>(a.C) + (long long)row * a.ldc, tile_c + c0, INT_MAX, true, v);   // (rows of G are padded to whole tiles)
+                        }
+                    }
+                } else if (rv && tile_c + c0 < a.N) {
+                    if (USE == kOut) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= factor;
+                        store32<T>(reinterpret_cast<T*>(a.C) + (long long)row * a.ldc, tile_c + c0, a.N, wide, v);
+                    } else {
+                        float* out = reinterpret_cast<float*>(a.C) + t.split * a.part_stride + (long long)row * a.ldc;
+                        if (a.accumulate) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (tile_c + c0 + j < a.N) v[j] += out[tile_c + c0 + j];
+                        }
+                        store32<float>(out, tile_c + c0, a.N, wide, v);
+                    }
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive_leader_tmem(tempty(acc));
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            if (USE == kStats && rv) a.stats[(long long)(2 * t.n + half) * a.M + row] = make_float4(m2, s1, s2, dot);
+        }
+    }
+
+    // Tear-down.  After a time-out, give loads that may still be in flight a bounded chance to land before the shared memory is
+    // released.  Neither CTA leaves while the other may still read its operands or arrive at its barriers.
+    __syncthreads();
+    if (*abort_flag && threadIdx.x == 0)
+        for (int s = 0; s < CT_STAGES; ++s)
+            for (uint32_t i = 0; i < 4096u; ++i)
+                if (mbar_try_wait(full(s), 0) || mbar_try_wait(full(s), 1)) break;
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();
+    if (warp == 0) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        tmem_dealloc2(tmem_base, CT_TMEM);
+    }
+}
+
+}  // namespace
+
+}  // namespace gad

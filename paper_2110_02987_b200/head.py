@@ -1,4 +1,5 @@
-"""Operators of an output head on CUDA tensors the caller owns (no context): layer norm and its backward pass.
+"""Operators of an output head on CUDA tensors the caller owns (no context): layer norm and its backward pass, the softmax cross entropy
+of an output layer with many classes, and distillation from a teacher's top logits.
 
 Like the rest of the binding this is argument checking and marshalling; the work is the library's kernels (``include/gad.h``).
 Every call enqueues on ``stream`` (default: torch's current stream of the tensors' device) and does not wait.  Outputs and
@@ -8,11 +9,21 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+from typing import NamedTuple, Optional
 
 from .binding import GAD_OK, GadError, load
 
 _DTYPES = {}     # torch dtype -> GAD_F32 / GAD_F16 / GAD_BF16, filled on first use (torch is imported late, as in the rest of the binding)
 _lib = None
+
+
+class _ClassLossArgs(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("cols", C.c_int32), ("classes", C.c_int32), ("rows", C.c_int64), ("H", C.c_void_p), ("ldh", C.c_int64),
+                ("W", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p), ("labels", C.c_void_p), ("label_bytes", C.c_int32), ("k", C.c_int32),
+                ("target_classes", C.c_void_p), ("target_bytes", C.c_int32), ("teacher_dtype", C.c_int32), ("teacher", C.c_void_p),
+                ("temperature", C.c_float), ("hard_weight", C.c_float), ("row_weights", C.c_void_p), ("scale", C.c_float), ("mean", C.c_int32),
+                ("loss", C.c_void_p), ("row_loss", C.c_void_p), ("dH", C.c_void_p), ("lddh", C.c_int64), ("dW", C.c_void_p), ("lddw", C.c_int64),
+                ("db", C.c_void_p), ("status", C.c_void_p)]
 
 
 def _load():
@@ -24,6 +35,8 @@ def _load():
         L.gad_layer_norm.argtypes = [vp, i64, i64, i32, i32, vp, vp, i32, f32, vp, i64, vp, vp, vp]
         L.gad_layer_norm_backward_workspace_bytes.argtypes = [i64, i32, C.POINTER(C.c_size_t)]
         L.gad_layer_norm_backward.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp, C.c_size_t, vp]
+        L.gad_class_loss_workspace_bytes.argtypes = [C.POINTER(_ClassLossArgs), C.POINTER(C.c_size_t)]
+        L.gad_class_loss.argtypes = [C.POINTER(_ClassLossArgs), vp, C.c_size_t, vp]
         _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
         _lib = L
     return _lib
@@ -151,3 +164,97 @@ def layer_norm_backward(dy, x, mean, rstd, gamma=None, *, param_grads=True, stre
                                       dgamma.data_ptr() if param_grads else None, dbeta.data_ptr() if param_grads else None,
                                       ws.data_ptr() if param_grads else None, nbytes.value, st.cuda_stream), "gad_layer_norm_backward")
     return dx, dgamma, dbeta
+
+
+class ClassLoss(NamedTuple):
+    """What ``class_loss`` and ``distill_loss`` return.  ``loss`` float32 [1]; ``row_loss`` float32 [rows]; the gradients in the type of H,
+    or None where not asked for; ``status`` int32 [1], zero unless a wait inside a kernel ran out."""
+    loss: "object"
+    row_loss: "object"
+    dH: Optional["object"]
+    dW: Optional["object"]
+    db: Optional["object"]
+    status: "object"
+
+    def check(self):
+        """Waits for the result; raises GAD_ERR_DEVICE_TIMEOUT if a bounded wait ran out, GAD_ERR_NONFINITE if the loss is not finite."""
+        code = int(self.status.item())
+        if code:
+            raise GadError(-7, "wait %d ran out" % code)
+        if not bool(self.loss.isfinite().item()):
+            raise GadError(-6, "the loss is not finite")
+        return self
+
+
+def _indices(t, name, shape, device):
+    """Checks contiguous int32 / int64 indices; returns (address, bytes of one)."""
+    import torch
+    if not (t.is_cuda and t.device == device and t.dtype in (torch.int32, torch.int64) and tuple(t.shape) == shape and t.is_contiguous()):
+        raise GadError(-1, "%s must be a contiguous int32 or int64 tensor of shape %s on the same device" % (name, list(shape)))
+    return t.data_ptr(), t.element_size()
+
+
+def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, row_weights, mean, scale, grads, stream):
+    import torch
+    L = _load()
+    ldh = _matrix(H, "H")
+    N, D = H.shape
+    dev, dt = H.device, H.dtype
+    ldw = _matrix(W, "W", dev)
+    V = W.shape[0]
+    if W.dtype is not dt or W.shape[1] != D:
+        raise GadError(-1, "W must have H's type and number of columns")
+    if V < 1 or (V > 1 and ldw == 0):
+        raise GadError(-1, "W must have a row for every class")
+    b = _vector(bias, "bias", V, (dt,), dev)
+    w = _vector(row_weights, "row_weights", N, (torch.float32,), dev)
+    lab, lab_bytes = _indices(labels, "labels", (N,), dev) if labels is not None else (None, 4)
+    k, tc, tc_bytes, te, te_type = 0, None, 4, None, 0
+    if classes is not None:
+        if classes.dim() != 2 or classes.shape[1] < 1:
+            raise GadError(-1, "classes must be rows x k, k of 1 and more")
+        k = classes.shape[1]
+        tc, tc_bytes = _indices(classes, "classes", (N, k), dev)
+        if not (teacher.is_cuda and teacher.device == dev and teacher.dtype in _DTYPES and tuple(teacher.shape) == (N, k) and teacher.is_contiguous()):
+            raise GadError(-1, "teacher must be a contiguous floating tensor of the shape of classes on the same device")
+        te, te_type = teacher.data_ptr(), _DTYPES[teacher.dtype]
+    want = {"H", "W", "b"} if grads is True else set() if not grads else set(grads)
+    if not want <= {"H", "W", "b"}:
+        raise GadError(-1, "grads is True, False or some of H, W and b")
+    with _on(dev, stream) as st:
+        out = torch.empty(N + 1, dtype=torch.float32, device=dev)
+        status = torch.empty(1, dtype=torch.int32, device=dev)
+        dH = torch.empty((N, D), dtype=dt, device=dev) if "H" in want else None
+        dW = torch.empty((V, D), dtype=dt, device=dev) if "W" in want else None
+        db = torch.empty(V, dtype=dt, device=dev) if "b" in want and b is not None else None
+        at = out.data_ptr()
+        a = _ClassLossArgs(_DTYPES[dt], D, V, N, H.data_ptr(), ldh, W.data_ptr(), ldw, b, lab, lab_bytes, k, tc, tc_bytes, te_type, te, temperature,
+                           hard_weight, w, scale, 1 if mean else 0, at + 4 * N, at, dH.data_ptr() if dH is not None else None, D,
+                           dW.data_ptr() if dW is not None else None, D, db.data_ptr() if db is not None else None, status.data_ptr())
+        nbytes = C.c_size_t(0)
+        _ck(L.gad_class_loss_workspace_bytes(C.byref(a), C.byref(nbytes)), "gad_class_loss")
+        ws = torch.empty(nbytes.value, dtype=torch.uint8, device=dev)     # (torch's blocks start on 512 bytes)
+        _ck(L.gad_class_loss(C.byref(a), ws.data_ptr(), nbytes.value, st.cuda_stream), "gad_class_loss")
+    return ClassLoss(out[N:], out[:N], dH, dW, db, status)
+
+
+def class_loss(H, W, labels, *, bias=None, row_weights=None, mean=True, scale=1.0, grads=True, stream=None):
+    """gad_class_loss with labels: softmax cross entropy of the output layer z = H W^T + bias over many classes, without keeping z.
+
+    H [rows x cols] and W [classes x cols] float32, float16 or bfloat16 (both the same), any row stride; labels int32 / int64 [rows], below
+    zero: the row does not count; bias [classes] in the same type, -inf takes a class out.
+    loss = scale * sum_i row_weights_i row_loss_i, with ``mean`` divided by the number of rows that count.
+    grads: True, False, or some of "H", "W", "b" as a string or set.  Returns a ``ClassLoss``."""
+    if labels is None:
+        raise GadError(-1, "labels are needed")
+    return _class_loss(H, W, labels, None, None, 1.0, 1.0, bias, row_weights, mean, scale, grads, stream)
+
+
+def distill_loss(H, W, classes, teacher, *, temperature=1.0, labels=None, hard_weight=0.0, bias=None, row_weights=None, mean=True, scale=1.0,
+                 grads=True, stream=None):
+    """gad_class_loss with a teacher: classes int32 / int64 [rows x k] (below zero: the slot is unused) and its logits there, ``teacher``
+    [rows x k] of any of the three types, k of 1 to 1024.  With q = softmax(teacher / T) over the used slots of a row and z as in ``class_loss``,
+    row_loss = (1 - hard_weight) T^2 sum q (log q - log softmax(z / T)) + hard_weight * cross entropy against ``labels`` (where given)."""
+    if classes is None or teacher is None:
+        raise GadError(-1, "classes and teacher are needed")
+    return _class_loss(H, W, labels, classes, teacher, temperature, hard_weight if labels is not None else 0.0, bias, row_weights, mean, scale, grads, stream)
