@@ -24,7 +24,8 @@ constexpr int CT_RING = CT_STAGES * CT_STAGE;
 constexpr int CT_EPI_WARPS = 8, CT_EPI_WARP0 = 2;           // two per quarter of the tensor-memory lanes, half of the columns each
 constexpr int CT_THREADS = 32 * (CT_EPI_WARP0 + CT_EPI_WARPS);
 constexpr int CT_BIAS = CT_EPI_WARPS * 128 * 4;             // a draining warp's biases
-constexpr int CT_SMEM = CT_RING + 1024 + 256 + CT_BIAS;
+constexpr int CT_STAGING = CT_EPI_WARPS * 2048;             // and 64 bytes of each of its rows on their way out
+constexpr int CT_SMEM = CT_RING + 1024 + 256 + CT_BIAS + CT_STAGING;
 constexpr int CT_TMEM = 512;                                // two accumulators of 256 columns
 
 enum TileUse { kStats, kGrad, kOut, kPartial };
@@ -37,6 +38,7 @@ struct TileArgs {
     int splits, kb_split;      // shares of it, blocks a share
     int group;                 // row tiles that are gone through together, for the L2
     int pairs;                 // products of operand parts: 1, or 6 for operands in three parts
+    int chunk;                 // ADD_UP: ring stages that are summed in tensor memory before the sum moves to registers
     int b_row0;                // first row of B (MN-major: added to the reduction, K-major: to the column)
     int bf16;                  // operand type: 1 bfloat16, 0 fp16
     int32_t* err;
@@ -54,6 +56,7 @@ struct TileArgs {
     void* C;                   // kGrad: G [parts][M x ldc]; kOut, kPartial: the result
     long long ldc, part_stride;
     int accumulate;            // kPartial: add to what is there
+    float* colsum;             // kGrad: [8 tiles_m][ldc] column sums of 32 rows each, or null
 };
 
 // Products of operand parts, the smallest first, so that what an addition to the accumulator cuts off is small for as long as possible.
@@ -116,23 +119,89 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
     p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
 }
 
-// 32 values of a row, to columns c0 .. of a result row that ends at `cols`.
-template <class T>
-__device__ __forceinline__ void store32(T* row, int c0, int cols, bool wide, const float (&v)[32]) {
-    constexpr int V = 16 / sizeof(T);
-    if (wide && c0 + 32 <= cols) {
+// Rows leave through shared memory, 64 bytes of each of a warp's 32 rows at a time: written from registers they would go out as 32 separate 16-byte (or,
+// where rows do not start on 16 bytes, one-element) stores, each half a sector or less (G of 8192 x 4096 in three parts: 168 us, as whole sectors
+// 82).  Units of 16 bytes are swizzled by the row, so neither side has bank conflicts.
+__device__ __forceinline__ uint8_t* staged(uint8_t* buf, int row, int unit) { return buf + row * 64 + ((unit ^ ((row >> 1) & 3)) << 4); }
+
+// GB: bytes of a store, a divisor of every row's address.
+template <int GB, class T, bool ADD>
+__device__ __forceinline__ void copy_out(uint8_t* buf, int lane, T* __restrict__ out, long long ld, int rows, int cols) {
+    constexpr int PER = 64 / GB, ROWS = 32 / PER, E = GB / sizeof(T);
+    const int g = lane % PER, e0 = g * E;
+    if (e0 >= cols) return;
 #pragma unroll
-        for (int j = 0; j < 32; j += V) {
-            union { uint4 u; T e[V]; } w;
+    for (int r = lane / PER; r < 32; r += ROWS) {
+        if (r >= rows) break;
+        union { T e[E]; uint4 u4; uint2 u2; uint32_t u1; uint16_t h; } w;
+        const uint8_t* src = staged(buf, r, (g * GB) >> 4) + ((g * GB) & 15);
+        if constexpr (GB == 16) w.u4 = *reinterpret_cast<const uint4*>(src);
+        else if constexpr (GB == 8) w.u2 = *reinterpret_cast<const uint2*>(src);
+        else if constexpr (GB == 4) w.u1 = *reinterpret_cast<const uint32_t*>(src);
+        else w.h = *reinterpret_cast<const uint16_t*>(src);
+        T* at = out + r * ld + e0;
+        if (E == 1 || e0 + E <= cols) {
+            if constexpr (ADD) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) w.e[i] = from_float<T>(v[j + i]);
-            *reinterpret_cast<uint4*>(row + c0 + j) = w.u;
+                for (int i = 0; i < E; ++i) w.e[i] += at[i];
+            }
+            if constexpr (GB == 16) *reinterpret_cast<uint4*>(at) = w.u4;
+            else if constexpr (GB == 8) *reinterpret_cast<uint2*>(at) = w.u2;
+            else if constexpr (GB == 4) *reinterpret_cast<uint32_t*>(at) = w.u1;
+            else *reinterpret_cast<uint16_t*>(at) = w.h;
+        } else {
+            for (int i = 0; i < E && e0 + i < cols; ++i) {
+                if constexpr (ADD) w.e[i] += at[i];
+                at[i] = w.e[i];
+            }
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (c0 + j < cols) row[c0 + j] = from_float<T>(v[j]);
     }
+}
+// The largest store every row of a matrix allows.
+__device__ __forceinline__ int store_bytes(const void* p, long long ld_bytes) {
+    const unsigned long long m = (unsigned long long)p | (unsigned long long)ld_bytes;
+    return m % 16 == 0 ? 16 : m % 8 == 0 ? 8 : m % 4 == 0 ? 4 : 2;
+}
+// A lane's 32 values (a row each) to out[row of the warp][0 .. 32), at most `cols` columns of `rows` rows.
+template <class T, bool ADD = false>
+__device__ __forceinline__ void drain_rows(uint8_t* buf, int lane, const float (&v)[32], T* __restrict__ out, long long ld, int rows, int cols, int bytes) {
+    constexpr int PER = 64 / sizeof(T);           // columns a time
+#pragma unroll
+    for (int c = 0; c < 32; c += PER) {
+        if (c >= cols) break;
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            union { uint4 u; T e[16 / sizeof(T)]; } w;
+#pragma unroll
+            for (int i = 0; i < 16 / (int)sizeof(T); ++i) w.e[i] = from_float<T>(v[c + k * (16 / sizeof(T)) + i]);
+            *reinterpret_cast<uint4*>(staged(buf, lane, k)) = w.u;
+        }
+        __syncwarp();
+        if (bytes == 16) copy_out<16, T, ADD>(buf, lane, out + c, ld, rows, cols - c);
+        else if (bytes == 8) copy_out<8, T, ADD>(buf, lane, out + c, ld, rows, cols - c);
+        else if (bytes == 4 || sizeof(T) == 4) copy_out<4, T, ADD>(buf, lane, out + c, ld, rows, cols - c);
+        else copy_out<sizeof(T) == 4 ? 4 : 2, T, ADD>(buf, lane, out + c, ld, rows, cols - c);
+    }
+}
+
+// Sum over the warp's lanes of every one of 32 values: lane c gets that of v[c].
+__device__ __forceinline__ float column_sums(const float (&v)[32], int lane) {
+    float a[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const float keep = (lane & 16) ? v[j + 16] : v[j], give = (lane & 16) ? v[j] : v[j + 16];
+        a[j] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+    }
+#pragma unroll
+    for (int w = 8; w > 0; w >>= 1)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < w) {
+                const float keep = (lane & w) ? a[j + w] : a[j], give = (lane & w) ? a[j] : a[j + w];
+                a[j] = keep + __shfl_xor_sync(0xffffffffu, give, w);
+            }
+    return a[0];
 }
 
 struct TileAt { int m, n, split; };
@@ -149,7 +218,10 @@ __device__ __forceinline__ TileAt tile_at(const TileArgs& a, long long u) {
 }
 
 // USE as above; A_MN, B_MN: operand is MN-major; T: type of the result (kGrad: float = three bfloat16 parts); NL: softmaxes (temperatures) at once.
-template <int USE, bool A_MN, bool B_MN, class T, int NL>
+// ADD_UP: the tensor core cuts its accumulator off at every addition (it does not round), half a step a time and always towards zero: long reductions lose
+// 5e-9 of their value per 16 terms (128 000 x 4096 logits of one row: loss off by 1.3e-6).  Where a result is wanted to fp32 accuracy the
+// reduction is cut into chunks whose sums the draining threads add up in registers.
+template <int USE, bool A_MN, bool B_MN, class T, int NL, bool ADD_UP>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(CT_THREADS, 1)
 class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ TileArgs a) {
     extern __shared__ uint8_t smem_raw[];
@@ -174,12 +246,14 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    pdl_next();
     if (warp == 0) tmem_alloc2(smem_u32(tmem_slot), CT_TMEM);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     cluster_sync();           // the peer's barriers exist before anything arrives at them
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = *tmem_slot;
+    pdl_wait();
 
     const int ncl = gridDim.x >> 1, half_w = a.width / 2;
     const long long units = (long long)a.tiles_m * a.tiles_n * a.splits;
@@ -244,35 +318,41 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
             int kb0;
             const int steps = blocks_of(tile_at(a, u).split, kb0) * a.pairs;
-            if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 32)))) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t d = tmem_base + (uint32_t)(acc * 256);
+            int left = 0;                                          // stages until this accumulator is full
             for (int i = 0; i < steps; ++i) {
+                const bool first = left == 0;
+                if (first) {
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 32)))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    left = ADD_UP ? min(a.chunk, steps - i) : steps;
+                }
+                const uint32_t d = tmem_base + (uint32_t)(acc * 256);
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag, a.err, 33) && mbar_wait<true>(pfull(stage), phase, abort_flag, a.err, 35)))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t base = sm_addr + stage * CT_STAGE;
                 const uint64_t da = operand_desc<A_MN>(base), db = operand_desc<B_MN>(base + CT_OPERAND);
                 if (elect_one()) {
 #pragma unroll
-                    for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_pair(d, da + stepA * ks, db + stepB * ks, idesc, (i | ks) != 0 ? 1u : 0u);
+                    for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_pair(d, da + stepA * ks, db + stepB * ks, idesc, !first || ks != 0 ? 1u : 0u);
                     mma_commit2(empty(stage));                    // in both CTAs
-                    if (i == steps - 1) mma_commit2(tfull(acc));
+                    if (left == 1) mma_commit2(tfull(acc));
                 }
                 __syncwarp();
                 if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
+                if (--left == 0 && ++acc == 2) { acc = 0; acc_phase ^= 1u; }
             }
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
     } else if (warp >= CT_EPI_WARP0) {
         // ---------------- drain: this warp's 32 rows (a row a lane) x half of the tile's columns ----------------
         const int ew = warp - CT_EPI_WARP0, q = warp & 3, half = ew >> 2;
         float* bias = reinterpret_cast<float*>(sm + CT_RING + 256) + ew * 128;
+        uint8_t* buf = sm + CT_RING + 256 + CT_BIAS + ew * 2048;
         int acc = 0;
         uint32_t acc_phase = 0;
         float gscale = 1.f, factor = 1.f;
         if (USE == kGrad) gscale = a.scal[0];
         if (USE == kOut) factor = a.scal[1];
-        const bool wide = ((uintptr_t)a.C & 15) == 0 && (a.ldc * sizeof(T)) % 16 == 0;
+        const int bytes = USE == kOut || USE == kPartial ? store_bytes(a.C, a.ldc * (long long)sizeof(T)) : 16;
         for (long long u = blockIdx.x >> 1; u < units; u += ncl) {
             const TileAt t = tile_at(a, u);
             const int row = t.m * CT_M + (int)rank * CT_H + q * 32 + lane;
@@ -309,12 +389,9 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     }
                 }
             }
-            if (!__all_sync(0xffffffffu, mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 36))) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int c0 = 0; c0 < half_w; c0 += 32) {
-                float v[32];
-                __syncwarp();
-                tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * 256 + half * half_w + c0), v);
+            const int row0 = t.m * CT_M + (int)rank * CT_H + q * 32, rows = a.M - row0;   // this warp's rows
+            // 32 finished values of this thread's row, from column c0 of the warp's columns on
+            const auto take = [&](int c0, float (&v)[32]) {
                 const int gc = a.col0 + tile_c + c0;                        // class of v[0]
                 if (USE == kStats) {
                     float most = m2;
@@ -350,46 +427,84 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                         for (int j = 0; j < 32; ++j) v[j] -= j == at ? w : 0.f;
                         next = ++e < a.ntargets ? tg[e].x : INT_MAX;
                     }
-                    if (rv) {
-                        if constexpr (sizeof(T) == 4) {                     // three bfloat16 parts
-                            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.C) + (long long)row * a.ldc + tile_c + c0;
+                    __syncwarp();
+                    if (a.colsum) a.colsum[(long long)(t.m * 8 + (int)rank * 4 + q) * a.ldc + tile_c + c0 + lane] = column_sums(v, lane);
+                    if constexpr (sizeof(T) == 4) {                         // three bfloat16 parts
+                        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.C) + (long long)row0 * a.ldc + tile_c + c0;
 #pragma unroll
-                            for (int j = 0; j < 32; j += 8) {
-                                union { uint4 u; __nv_bfloat16 h[8]; } w[3];
+                        for (int k = 0; k < 3; ++k) {
+                            float p[32];
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    __nv_bfloat16 p3[3];
-                                    split3(v[j + i], p3);
-#pragma unroll
-                                    for (int k = 0; k < 3; ++k) w[k].h[i] = p3[k];
-                                }
-#pragma unroll
-                                for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(out + k * a.part_stride + j) = w[k].u;
+                            for (int j = 0; j < 32; ++j) {
+                                p[j] = v[j];
+                                v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
                             }
-                        } else {
-                            store32<T>(reinterpret_cast<T*>(a.C) + (long long)row * a.ldc, tile_c + c0, INT_MAX, true, v);   // (rows of G are padded to whole tiles)
+                            drain_rows<__nv_bfloat16>(buf, lane, p, out + k * a.part_stride, a.ldc, rows, 32, 16);
                         }
+                    } else {
+                        drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, 32, 16);
                     }
-                } else if (rv && tile_c + c0 < a.N) {
+                } else if (tile_c + c0 < a.N) {
                     if (USE == kOut) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] *= factor;
-                        store32<T>(reinterpret_cast<T*>(a.C) + (long long)row * a.ldc, tile_c + c0, a.N, wide, v);
+                        drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, a.N - tile_c - c0, bytes);
                     } else {
-                        float* out = reinterpret_cast<float*>(a.C) + t.split * a.part_stride + (long long)row * a.ldc;
-                        if (a.accumulate) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (tile_c + c0 + j < a.N) v[j] += out[tile_c + c0 + j];
-                        }
-                        store32<float>(out, tile_c + c0, a.N, wide, v);
+                        float* out = reinterpret_cast<float*>(a.C) + t.split * a.part_stride + (long long)row0 * a.ldc + tile_c + c0;
+                        if (a.accumulate) drain_rows<float, true>(buf, lane, v, out, a.ldc, rows, a.N - tile_c - c0, bytes);
+                        else drain_rows<float>(buf, lane, v, out, a.ldc, rows, a.N - tile_c - c0, bytes);
                     }
                 }
+            };
+            const uint32_t tm_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * half_w);
+            const auto release = [&]() {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_leader_tmem(tempty(acc));
+                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            };
+            bool ok = true;
+            const auto wait_full = [&]() {
+                ok = __all_sync(0xffffffffu, mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 36));
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                return ok;
+            };
+            if constexpr (ADD_UP) {
+                int kb0;
+                const int chunks = (blocks_of(t.split, kb0) * a.pairs + a.chunk - 1) / a.chunk;
+                if (chunks > 1) {
+                    float sum[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
+                    for (int i = 0; i < chunks; ++i) {
+                        if (!wait_full()) break;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            if (32 * c >= half_w) break;
+                            float v[32];
+                            tmem_ld32(tm_row + (uint32_t)(acc * 256 + 32 * c), v);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+                        }
+                        if (i < chunks - 1) release();
+                    }
+                    if (!ok) break;
+                    // the sums take the place of the last chunk, and are taken from there block by block: held in registers beside what follows they would spill
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (32 * c < half_w) tmem_st_32x32b_x32(tm_row + (uint32_t)(acc * 256 + 32 * c), sum[c]);
+                    tmem_wait_st();
+                } else if (!wait_full()) break;
+            } else if (!wait_full()) break;
+            for (int c0 = 0; c0 < half_w; c0 += 32) {
+                float v[32];
+                __syncwarp();
+                tmem_ld32(tm_row + (uint32_t)(acc * 256 + c0), v);
+                take(c0, v);
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive_leader_tmem(tempty(acc));
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            release();
             if (USE == kStats && rv) a.stats[(long long)(2 * t.n + half) * a.M + row] = make_float4(m2, s1, s2, dot);
         }
     }

@@ -38,7 +38,20 @@ template <class T>
 __device__ __forceinline__ void pack_row(const T* __restrict__ src, int cols, bool keep, void* dst, int64_t at, int64_t part_stride, int t, int threads) {
     if constexpr (sizeof(T) == 4) {
         __nv_bfloat16* d = reinterpret_cast<__nv_bfloat16*>(dst) + at;
-        for (int c = t; c < cols; c += threads) {
+        const int n4 = ((uintptr_t)src & 15) == 0 ? cols >> 2 : 0;
+        for (int c = t; c < n4; c += threads) {
+            const float4 x = keep ? reinterpret_cast<const float4*>(src)[c] : make_float4(0.f, 0.f, 0.f, 0.f);
+            __nv_bfloat16 p[4][3];
+            split3(x.x, p[0]); split3(x.y, p[1]); split3(x.z, p[2]); split3(x.w, p[3]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                union { uint2 u; __nv_bfloat16 h[4]; } w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w.h[i] = p[i][k];
+                *reinterpret_cast<uint2*>(d + k * part_stride + 4 * c) = w.u;
+            }
+        }
+        for (int c = 4 * n4 + t; c < cols; c += threads) {
             __nv_bfloat16 p[3];
             split3(keep ? src[c] : 0.f, p);
             for (int k = 0; k < 3; ++k) d[k * part_stride + c] = p[k];
@@ -66,7 +79,26 @@ struct RowArgs {
     int2* targets; int ntargets;
     float4* rowk;
     int32_t* status;
+    int64_t rows;
+    unsigned* ticket;
 };
+
+// Labels alone: a warp a row.
+template <class T>
+__global__ void __launch_bounds__(256) class_label_rows_kernel(const RowArgs a) {
+    const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    pdl_next();
+    if (blockIdx.x == 0 && threadIdx.x == 0) { *a.status = 0; *a.ticket = 0u; }
+    if (r >= a.rows) return;
+    const int64_t y = load_index(a.labels, a.label_bytes, r);
+    const bool counts = y >= 0, bad = y >= a.classes;
+    if (lane == 0) {
+        a.targets[r] = make_int2(counts && !bad ? (int)y : INT_MAX, __float_as_int(counts && !bad ? 1.f : 0.f));
+        a.rowk[r] = make_float4(counts ? 1.f : 0.f, 0.f, bad ? NAN : 0.f, counts ? (a.weights ? a.weights[r] : 1.f) : 0.f);
+    }
+    pack_row<T>(reinterpret_cast<const T*>(a.H) + r * a.ldh, a.cols, counts, a.Hp, r * a.ldp, a.part_stride, lane, 32);
+}
 
 // A block a row.  rowk = (coefficient of lse(z), of lse(z / T), sum of q log q with its factor, weight of the row); a row without target: (0, 0, 0, 0).
 template <class T>
@@ -78,7 +110,8 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
     __shared__ int bad, soft_any;
     const int64_t r = blockIdx.x;
     const int t = threadIdx.x, lane = t & 31, w = t >> 5;
-    if (t == 0) { bad = 0; soft_any = 0; if (r == 0) *a.status = 0; }
+    pdl_next();
+    if (t == 0) { bad = 0; soft_any = 0; if (r == 0) { *a.status = 0; *a.ticket = 0u; } }
     __syncthreads();
     float most = -INFINITY;
     for (int j = t; j < a.k; j += kRowThreads) {
@@ -148,121 +181,165 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
 template <class T>
 __global__ void __launch_bounds__(256) class_pack_kernel(const T* __restrict__ W, int64_t ldw, int rows, int cols, void* Wp, int64_t ldp, int64_t part_stride) {
     const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    pdl_next();
+    pdl_wait();
     if (r < rows) pack_row<T>(W + r * ldw, cols, true, Wp, r * ldp, part_stride, threadIdx.x & 31, 32);
 }
 
-// The parts of a row's statistics joined: a block has 32 rows, each of its warps every eighth part.
+// What a block of class_finish_kernel adds to the loss: sum of weighted row losses, the largest coefficient of G, counted rows.
+struct LossShare { double sum; float most; int n; };
+constexpr int kFinishRows = 8;
+
+// The parts of a row's statistics joined (a block has 8 rows, 32 threads each, every 32nd part a thread; joined pairwise in a fixed order), and in the block that
+// comes last the loss and what the gradients are multiplied with.  scal[0]: a power of two that brings the largest coefficient of G to 2^14 .. 2^15;
+// [1]: scale / counted rows / that.
 template <int NL>
 __global__ void __launch_bounds__(256) class_finish_kernel(const float4* __restrict__ stats, int parts, int rows, const float4* __restrict__ rowk, float sc, float inv_t, float hard_t,
-                                                           float4* __restrict__ rowc, float* __restrict__ row_loss) {
-    __shared__ float4 sm[8][32];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, r = blockIdx.x * 32 + lane;
-    float m = -INFINITY, s1 = 0.f, s2 = 0.f, dot = 0.f;
-    const auto join = [&](const float4& v) {
-        const float most = fmaxf(m, v.x), base = most == -INFINITY ? 0.f : most;
-        s1 = s1 * exp2f(m - base) + v.y * exp2f(v.x - base);
-        if (NL == 2) s2 = s2 * exp2f((m - base) * inv_t) + v.z * exp2f((v.x - base) * inv_t);
-        m = most;
-        dot += v.w;
+                                                           float4* __restrict__ rowc, float* __restrict__ row_loss, LossShare* shares, unsigned* ticket, float scale, int mean,
+                                                           float* __restrict__ scal, float* __restrict__ loss) {
+    __shared__ float4 sm[8][kFinishRows];
+    __shared__ bool last;
+    __shared__ LossShare smt[8];
+    const int rl = threadIdx.x % kFinishRows, lane = threadIdx.x & 31, w = threadIdx.x >> 5, r = blockIdx.x * kFinishRows + rl;
+    pdl_next();
+    pdl_wait();
+    after_wait(stats);
+    after_wait(rowk);
+    const float4 none = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    const auto join = [&](const float4& u, const float4& v) {
+        const float most = fmaxf(u.x, v.x), base = most == -INFINITY ? 0.f : most;
+        float4 o;
+        o.x = most;
+        o.y = u.y * exp2f(u.x - base) + v.y * exp2f(v.x - base);
+        o.z = NL == 2 ? u.z * exp2f((u.x - base) * inv_t) + v.z * exp2f((v.x - base) * inv_t) : 0.f;
+        o.w = u.w + v.w;
+        return o;
     };
+    float4 at = none;
     if (r < rows)
-        for (int p = w; p < parts; p += 8) join(stats[(int64_t)p * rows + r]);
-    sm[w][lane] = make_float4(m, s1, s2, dot);
+        for (int p = threadIdx.x / kFinishRows; p < parts; p += 128) {
+            float4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = p + 32 * i < parts ? stats[(int64_t)(p + 32 * i) * rows + r] : none;
+            at = join(at, join(join(v[0], v[1]), join(v[2], v[3])));
+        }
+#pragma unroll
+    for (int o = kFinishRows; o < 32; o <<= 1) {
+        const float4 v = make_float4(__shfl_xor_sync(0xffffffffu, at.x, o), __shfl_xor_sync(0xffffffffu, at.y, o), __shfl_xor_sync(0xffffffffu, at.z, o), __shfl_xor_sync(0xffffffffu, at.w, o));
+        at = lane & o ? join(v, at) : join(at, v);
+    }
+    if (lane < kFinishRows) sm[w][lane] = at;
     __syncthreads();
-    if (w || r >= rows) return;
-    m = -INFINITY; s1 = s2 = dot = 0.f;
-    for (int i = 0; i < 8; ++i) join(sm[i][lane]);
-    const float4 k = rowk[r];
-    // in log2: of the (first) softmax, whose logits were scaled by sc, and of the second
-    const float l1 = m + log2f(s1), l2 = NL == 2 ? m * inv_t + log2f(s2) : l1;
-    const float ln2 = 0.693147181f;
-    const bool counts = k.x > 0.f || k.y > 0.f;
-    // cancellation of lse and z is that of the result: both are sums of the same rounded logits
-    row_loss[r] = counts ? k.x * (l1 * ln2) + k.y * (l2 * ln2) + k.z - dot / sc : 0.f;
-    if (!rowc) return;
-    // gradient: a p + (1 - a) T p^T; with one softmax both coefficients are its
-    const float a = k.x, b = hard_t > 0.f ? k.y / hard_t : 0.f;
-    rowc[r] = NL == 2 ? make_float4(a, b, l1, l2) : make_float4(a + b, 0.f, l1, 0.f);
-}
-
-// loss, and what the gradients are multiplied with.  scal[0]: a power of two that brings the largest coefficient of G to 2^14 .. 2^15; [1]: scale / counted rows / that.
-__global__ void __launch_bounds__(1024) class_total_kernel(const float4* __restrict__ rowk, const float4* __restrict__ rowc, const float* __restrict__ row_loss, int rows, float scale,
-                                                           int mean, float* __restrict__ scal, float* __restrict__ loss) {
-    __shared__ double sm[32];
-    __shared__ float smc[32];
-    __shared__ int smn[32];
-    double s = 0.0;
-    float most = 0.f;
-    int n = 0;
-    for (int r = threadIdx.x; r < rows; r += 1024) {
-        const float4 k = rowk[r];
-        if (!(k.x > 0.f || k.y > 0.f)) continue;
-        ++n;
-        s += (double)k.w * (double)row_loss[r];
-        if (rowc) most = fmaxf(most, fabsf(k.w) * (rowc[r].x + rowc[r].y));
+    if (w == 0) {
+        LossShare mine{0.0, 0.f, 0};
+        if (lane < kFinishRows && r < rows) {
+            at = sm[0][lane];
+            for (int i = 1; i < 8; ++i) at = join(at, sm[i][lane]);
+            const float4 k = rowk[r];
+            // in log2: of the (first) softmax, whose logits were scaled by sc, and of the second
+            const float l1 = at.x + log2f(at.y), l2 = NL == 2 ? at.x * inv_t + log2f(at.z) : l1;
+            const float ln2 = 0.693147181f;
+            const bool counts = k.x > 0.f || k.y > 0.f;
+            const float l = counts ? k.x * (l1 * ln2) + k.y * (l2 * ln2) + k.z - at.w / sc : 0.f;
+            row_loss[r] = l;
+            // gradient: a p + (1 - a) T p^T; with one softmax both coefficients are its
+            const float a = k.x, b = k.y / hard_t;
+            if (rowc) rowc[r] = NL == 2 ? make_float4(a, b, l1, l2) : make_float4(a + b, 0.f, l1, 0.f);
+            if (counts) { mine.sum = (double)k.w * (double)l; mine.most = fabsf(k.w) * (a + b); mine.n = 1; }
+        }
+#pragma unroll
+        for (int o = 1; o < kFinishRows; o <<= 1) {
+            mine.sum += __shfl_xor_sync(0xffffffffu, mine.sum, o);
+            mine.most = fmaxf(mine.most, __shfl_xor_sync(0xffffffffu, mine.most, o));
+            mine.n += __shfl_xor_sync(0xffffffffu, mine.n, o);
+        }
+        if (lane == 0) {
+            shares[blockIdx.x] = mine;
+            __threadfence();
+            last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+        }
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    LossShare all{0.0, 0.f, 0};
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += 256) {
+        const double s = __ldcg(&shares[i].sum);
+        all.sum += s;
+        all.most = fmaxf(all.most, __ldcg(&shares[i].most));
+        all.n += __ldcg(&shares[i].n);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        s += __shfl_xor_sync(0xffffffffu, s, o);
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        n += __shfl_xor_sync(0xffffffffu, n, o);
+        all.sum += __shfl_xor_sync(0xffffffffu, all.sum, o);
+        all.most = fmaxf(all.most, __shfl_xor_sync(0xffffffffu, all.most, o));
+        all.n += __shfl_xor_sync(0xffffffffu, all.n, o);
     }
-    if ((threadIdx.x & 31) == 0) { sm[threadIdx.x >> 5] = s; smc[threadIdx.x >> 5] = most; smn[threadIdx.x >> 5] = n; }
+    if (lane == 0) smt[w] = all;
     __syncthreads();
     if (threadIdx.x) return;
-    s = 0.0; most = 0.f; n = 0;
-    for (int i = 0; i < 32; ++i) { s += sm[i]; most = fmaxf(most, smc[i]); n += smn[i]; }
-    const double f = mean ? (n ? (double)scale / n : 0.0) : (double)scale;
-    loss[0] = (float)(f * s);
-    const int e = most > 0.f && most < INFINITY ? 14 - ilogbf(most) : 0;
+    all = smt[0];
+    for (int i = 1; i < 8; ++i) { all.sum += smt[i].sum; all.most = fmaxf(all.most, smt[i].most); all.n += smt[i].n; }
+    const double f = mean ? (all.n ? (double)scale / all.n : 0.0) : (double)scale;
+    loss[0] = (float)(f * all.sum);
+    const int e = all.most > 0.f && all.most < INFINITY ? 14 - ilogbf(all.most) : 0;
     scal[0] = ldexpf(1.f, max(-100, min(100, e)));
     scal[1] = (float)(f / (double)scal[0]);
 }
 
-// result = factor x the sum of the shares, in order.
-template <class T>
-__global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ part, int splits, int64_t part_stride, int cols, const float* __restrict__ scal, T* __restrict__ out, int64_t ld) {
-    const int64_t r = blockIdx.y;
-    const float f = scal[1];
-    for (int c = blockIdx.x * 256 + threadIdx.x; c < cols; c += gridDim.x * 256) {
-        float s = 0.f;
-        for (int i = 0; i < splits; ++i) s += part[i * part_stride + r * cols + c];
-        out[r * ld + c] = from_float<T>(f * s);
+// result [rows x cols] = factor x the sum of the shares, in order; VEC columns a thread.
+template <class T, int VEC>
+__global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ part, int splits, int64_t part_stride, int64_t rows, int cols, const float* __restrict__ scal,
+                                                         T* __restrict__ out, int64_t ld) {
+    pdl_next();
+    pdl_wait();
+    after_wait(part);
+    after_wait(scal);
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC;
+    if (i >= rows * cols) return;
+    const int64_t r = i / cols;
+    const int c = (int)(i - r * cols);
+    float s[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) s[j] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) {
+        const float* p = part + k * part_stride + i;
+        if constexpr (VEC == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(p);
+            s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+        } else s[0] += *p;
     }
+    const float f = scal[1];
+    union { T e[VEC]; uint4 u4; uint2 u2; } w;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) w.e[j] = from_float<T>(f * s[j]);
+    T* o = out + r * ld + c;
+    if constexpr (VEC == 4 && sizeof(T) == 4) *reinterpret_cast<uint4*>(o) = w.u4;
+    else if constexpr (VEC == 4) *reinterpret_cast<uint2*>(o) = w.u2;
+    else *o = w.e[0];
 }
 
-// db of a piece: column sums of G, a block 64 classes, rows in the order of its 32 row lanes.
+// db of a piece from the column sums of 32 rows each that the drain of G leaves: 32 classes a block, each of its eight warps a run of them, in order.
 template <class T>
-__global__ void __launch_bounds__(256) class_bias_kernel(const void* __restrict__ G, int64_t ld, int64_t part_stride, int rows, int classes, const float* __restrict__ scal, T* __restrict__ db) {
-    __shared__ float sm[32][65];
-    const int cx = (threadIdx.x & 7) * 8, ry = threadIdx.x >> 3, c0 = blockIdx.x * 64 + cx;    // (rows of G are padded to 128 classes)
-    float s[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = 0.f;
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    for (int64_t r = ry; r < rows; r += 32)
-#pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p) {
-            if constexpr (sizeof(T) == 4) {
-                float v[8];
-                load_vec<__nv_bfloat16, 8>(reinterpret_cast<const __nv_bfloat16*>(G) + p * part_stride + r * ld, c0, INT_MAX, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] += v[j];
-            } else {
-                float v[8];
-                load_vec<T, 8>(reinterpret_cast<const T*>(G) + r * ld, c0, INT_MAX, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] += v[j];
-            }
-        }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sm[ry][cx + j] = s[j];
+__global__ void __launch_bounds__(256) class_bias_kernel(const float* __restrict__ colsum, int64_t ld, int n, int classes, const float* __restrict__ scal, T* __restrict__ db) {
+    __shared__ float sm[8][32];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+    const int per = (n + 7) / 8, lo = min(n, w * per), hi = min(n, lo + per);
+    float s = 0.f;
+    pdl_next();
+    pdl_wait();
+    after_wait(colsum);
+    after_wait(scal);
+    if (c < classes)
+#pragma unroll 8
+        for (int i = lo; i < hi; ++i) s += colsum[i * ld + c];
+    sm[w][threadIdx.x & 31] = s;
     __syncthreads();
-    const int c = blockIdx.x * 64 + threadIdx.x;
-    if (threadIdx.x >= 64 || c >= classes) return;
-    float t = 0.f;
-    for (int i = 0; i < 32; ++i) t += sm[i][threadIdx.x];
-    db[c] = from_float<T>(t * scal[1]);
+    if (w || c >= classes) return;
+    s = 0.f;
+    for (int k = 0; k < 8; ++k) s += sm[k][threadIdx.x & 31];
+    db[c] = from_float<T>(s * scal[1]);
 }
 
 template <class T>
@@ -281,6 +358,26 @@ Cut cut_reduction(int64_t tiles, int nkb) {
     const int kb = (int)((nkb + want - 1) / want);
     return {(nkb + kb - 1) / kb, kb};
 }
+// Kernels of one call follow each other by programmatic dependent launch: each comes up while the one in front ends and waits (pdl_wait) before it touches
+// memory.  The first waits for all that is in front of it on the stream.
+template <class... P, class... Args>
+cudaError_t chain(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t s, bool first, Args&&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = first ? 0 : 1;
+    ++g_kernel_launches;
+    return cudaLaunchKernelEx(&cfg, kernel, P(std::forward<Args>(args))...);
+}
+template <class T>
+cudaError_t join_parts(const float* part, int splits, int64_t part_stride, int64_t rows, int cols, const float* scal, T* out, int64_t ld, cudaStream_t s) {
+    const bool wide = cols % 4 == 0 && ld % 4 == 0 && ((uintptr_t)out & (4 * sizeof(T) - 1)) == 0;
+    const int64_t n = rows * cols, per = wide ? 1024 : 256;
+    return chain(wide ? join_parts_kernel<T, 4> : join_parts_kernel<T, 1>, dim3((unsigned)((n + per - 1) / per)), 256, 0, s, false, part, splits, part_stride, rows, cols, scal, out, ld);
+}
+
 int width_for(int n) { return n <= 128 ? 128 : 256; }
 
 struct ClassPlan {
@@ -292,7 +389,7 @@ struct ClassPlan {
     int npieces;
     Cut cut_h, cut_w;
     bool h_parts, w_parts;
-    int64_t o_hp, o_wp, o_targets, o_rowk, o_rowc, o_stats, o_scal, o_g, o_dh, o_dw, total;
+    int64_t o_hp, o_wp, o_targets, o_rowk, o_rowc, o_stats, o_shares, o_scal, o_g, o_colsum, o_dh, o_dw, total;
 };
 
 ClassPlan plan_class(const gad_class_loss_args& a) {
@@ -330,8 +427,10 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     p.o_rowk = room(16 * N);
     p.o_rowc = room(16 * N);
     p.o_stats = room(16 * N * 2 * p.tiles_v);
+    p.o_shares = room((int64_t)sizeof(LossShare) * ((N + kFinishRows - 1) / kFinishRows));
     if (p.grads) {
         p.o_g = room(2 * p.parts * N * p.ldg);
+        if (a.db) p.o_colsum = room(4 * 8 * (int64_t)p.tiles_m * p.ldg);
         if (a.dH && p.h_parts) p.o_dh = room(4 * p.cut_h.splits * N * D);
         if (a.dW && p.w_parts) p.o_dw = room(4 * p.cut_w.splits * std::min<int64_t>(p.piece, V) * D);
     }
@@ -339,18 +438,29 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     return p;
 }
 
-template <int USE, bool A_MN, bool B_MN, class T, int NL>
-cudaError_t gemm_go(const CUtensorMap& A, const CUtensorMap& B, const TileArgs& a, cudaStream_t s) {
-    const auto kernel = class_gemm_kernel<USE, A_MN, B_MN, T, NL>;
+// Ring stages (64 terms each) of a chunk: 64 additions to an accumulator, about 3e-7 of its value.
+constexpr int kChunk = 16;
+
+template <int USE, bool A_MN, bool B_MN, class T, int NL, bool ADD_UP>
+cudaError_t gemm_launch(const CUtensorMap& A, const CUtensorMap& B, const TileArgs& a, cudaStream_t s) {
+    const auto kernel = class_gemm_kernel<USE, A_MN, B_MN, T, NL, ADD_UP>;
     cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), CT_SMEM, false);
     if (e != cudaSuccess) return e;
     static std::atomic<int> known{0};
     if (known.load() <= 0) known.store(max_active_pairs(reinterpret_cast<const void*>(kernel), CT_THREADS, CT_SMEM, 148));
     const int64_t units = (int64_t)a.tiles_m * a.tiles_n * a.splits;
     const int ncl = (int)std::min<int64_t>(units, known.load());
-    kernel<<<2 * ncl, CT_THREADS, CT_SMEM, s>>>(A, B, a);
-    ++g_kernel_launches;
-    return cudaGetLastError();
+    return chain(kernel, dim3((unsigned)(2 * ncl)), CT_THREADS, CT_SMEM, s, false, A, B, a);
+}
+// What is wanted to fp32 accuracy and longer than a chunk is added up in chunks: everything of fp32 operands, and the logits of the loss.
+template <int USE, bool A_MN, bool B_MN, class T, int NL>
+cudaError_t gemm_go(const CUtensorMap& A, const CUtensorMap& B, TileArgs a, cudaStream_t s) {
+    a.chunk = kChunk;
+    const bool exact = (a.pairs > 1 || USE == kStats) && a.kb_split * a.pairs > kChunk;
+    if constexpr (USE == kStats || USE == kPartial || sizeof(T) == 4)
+        if (exact) return gemm_launch<USE, A_MN, B_MN, T, NL, true>(A, B, a, s);
+    if constexpr (!(USE == kGrad && sizeof(T) == 4)) return gemm_launch<USE, A_MN, B_MN, T, NL, false>(A, B, a, s);
+    else return gemm_launch<USE, A_MN, B_MN, T, NL, true>(A, B, a, s);   // (of one chunk)
 }
 
 template <class T>
@@ -371,13 +481,15 @@ int run_class(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) {
     ra.tclasses = a.target_classes; ra.tclass_bytes = a.target_bytes; ra.teacher = a.teacher; ra.teacher_type = a.teacher_dtype; ra.k = a.k;
     ra.weights = a.row_weights; ra.hard = a.k > 0 ? (a.labels ? a.hard_weight : 0.f) : 1.f; ra.temperature = T0;
     ra.Hp = Hp; ra.ldp = p.ldp; ra.part_stride = (int64_t)N * p.ldp; ra.targets = targets; ra.ntargets = p.ntargets; ra.rowk = rowk; ra.status = a.status;
-    class_rows_kernel<T><<<(unsigned)N, kRowThreads, 8 * (size_t)p.ntargets, s>>>(ra);
-    ++g_kernel_launches;
+    ra.rows = N; ra.ticket = reinterpret_cast<unsigned*>(scal + 2);
+    cudaError_t e = a.k > 0 ? chain(class_rows_kernel<T>, dim3((unsigned)N), kRowThreads, 8 * (size_t)p.ntargets, s, true, ra)
+                            : chain(class_label_rows_kernel<T>, dim3((unsigned)((N + 7) / 8)), 256, 0, s, true, ra);
+    if (e != cudaSuccess) return GAD_ERR_CUDA;
     const void* Wo = a.W;
     int64_t ldw = a.ldw;
     if (p.pack_w) {
-        class_pack_kernel<T><<<(unsigned)((V + 7) / 8), 256, 0, s>>>((const T*)a.W, a.ldw, V, D, ws + p.o_wp, p.ldp, (int64_t)V * p.ldp);
-        ++g_kernel_launches;
+        if (chain(class_pack_kernel<T>, dim3((unsigned)((V + 7) / 8)), 256, 0, s, false, (const T*)a.W, a.ldw, V, D, (void*)(ws + p.o_wp), p.ldp, (int64_t)V * p.ldp) != cudaSuccess)
+            return GAD_ERR_CUDA;
         Wo = ws + p.o_wp;
         ldw = p.ldp;
     }
@@ -396,12 +508,11 @@ int run_class(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) {
     t.sc = kLog2e * (p.nl == 1 && a.k > 0 && ra.hard < 1.f ? 1.f / T0 : 1.f);
     t.inv_t = 1.f / T0;
     t.targets = targets; t.ntargets = p.ntargets; t.stats = stats; t.rowk = rowk; t.rowc = rowc; t.scal = scal;
-    cudaError_t e = p.nl == 2 ? gemm_go<kStats, false, false, float, 2>(mapH, mapW, t, s) : gemm_go<kStats, false, false, float, 1>(mapH, mapW, t, s);
+    e = p.nl == 2 ? gemm_go<kStats, false, false, float, 2>(mapH, mapW, t, s) : gemm_go<kStats, false, false, float, 1>(mapH, mapW, t, s);
     if (e != cudaSuccess) return GAD_ERR_CUDA;
-    const auto finish = p.nl == 2 ? class_finish_kernel<2> : class_finish_kernel<1>;
-    finish<<<(unsigned)((N + 31) / 32), 256, 0, s>>>(stats, 2 * p.tiles_v, N, rowk, t.sc, t.inv_t, T0, rowc, a.row_loss);
-    class_total_kernel<<<1, 1024, 0, s>>>(rowk, rowc, a.row_loss, N, a.scale, a.mean, scal, a.loss);
-    g_kernel_launches += 2;
+    e = chain(p.nl == 2 ? class_finish_kernel<2> : class_finish_kernel<1>, dim3((unsigned)((N + kFinishRows - 1) / kFinishRows)), 256, 0, s, false, (const float4*)stats, 2 * p.tiles_v, N,
+              (const float4*)rowk, t.sc, t.inv_t, T0, rowc, a.row_loss, reinterpret_cast<LossShare*>(ws + p.o_shares), ra.ticket, a.scale, (int)a.mean, scal, a.loss);
+    if (e != cudaSuccess) return GAD_ERR_CUDA;
     if (!p.grads) return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
 
     if (!make(mapH_mn, Hp, D, N, p.ldp, CT_K) || !make(mapW_mn, Wo, D, V, ldw, CT_K)) return GAD_ERR_CUDA;
@@ -412,6 +523,7 @@ int run_class(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) {
         TileArgs g = t;
         g.N = nv; g.tiles_n = (nv + p.width_v - 1) / p.width_v; g.col0 = v0; g.b_row0 = v0;
         g.C = G; g.ldc = p.ldg; g.part_stride = (int64_t)N * p.ldg;
+        g.colsum = a.db ? reinterpret_cast<float*>(ws + p.o_colsum) : nullptr;
         e = p.nl == 2 ? gemm_go<kGrad, false, false, T, 2>(mapH, mapW, g, s) : gemm_go<kGrad, false, false, T, 1>(mapH, mapW, g, s);
         if (e != cudaSuccess) return GAD_ERR_CUDA;
         const auto makeg = [&](CUtensorMap& m, uint32_t box) {
@@ -442,11 +554,7 @@ int run_class(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) {
                 w.C = dw_part; w.ldc = D; w.part_stride = (int64_t)nv * D;
                 e = gemm_go<kPartial, true, true, float, 1>(mapG_mn, mapH_mn, w, s);
                 if (e != cudaSuccess) return GAD_ERR_CUDA;
-                for (int r0 = 0; r0 < nv; r0 += 32768) {
-                    const int n = std::min(32768, nv - r0);
-                    join_parts_kernel<T><<<dim3((unsigned)std::min(8, (D + 255) / 256), (unsigned)n), 256, 0, s>>>(dw_part + (int64_t)r0 * D, w.splits, w.part_stride, D, scal, out + (int64_t)r0 * a.lddw, a.lddw);
-                    ++g_kernel_launches;
-                }
+                if (join_parts<T>(dw_part, w.splits, w.part_stride, nv, D, scal, out, a.lddw, s) != cudaSuccess) return GAD_ERR_CUDA;
             } else {
                 w.C = out; w.ldc = a.lddw;
                 e = gemm_go<kOut, true, true, T, 1>(mapG_mn, mapH_mn, w, s);
@@ -454,17 +562,11 @@ int run_class(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) {
             }
         }
         if (a.db) {
-            class_bias_kernel<T><<<(unsigned)((nv + 63) / 64), 256, 0, s>>>(G, p.ldg, (int64_t)N * p.ldg, N, nv, scal, reinterpret_cast<T*>(a.db) + v0);
-            ++g_kernel_launches;
+            e = chain(class_bias_kernel<T>, dim3((unsigned)((nv + 31) / 32)), 256, 0, s, false, (const float*)g.colsum, p.ldg, 8 * p.tiles_m, nv, (const float*)scal, reinterpret_cast<T*>(a.db) + v0);
+            if (e != cudaSuccess) return GAD_ERR_CUDA;
         }
     }
-    if (a.dH && p.h_parts)
-        for (int r0 = 0; r0 < N; r0 += 32768) {
-            const int n = std::min(32768, N - r0);
-            join_parts_kernel<T><<<dim3((unsigned)std::min(8, (D + 255) / 256), (unsigned)n), 256, 0, s>>>(dh_part + (int64_t)r0 * D, p.cut_h.splits, (int64_t)N * D, D, scal,
-                                                                                                           reinterpret_cast<T*>(a.dH) + (int64_t)r0 * a.lddh, a.lddh);
-            ++g_kernel_launches;
-        }
+    if (a.dH && p.h_parts && join_parts<T>(dh_part, p.cut_h.splits, (int64_t)N * D, N, D, scal, reinterpret_cast<T*>(a.dH), a.lddh, s) != cudaSuccess) return GAD_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
 }
 
