@@ -1,9 +1,8 @@
 // The matrix product of the output head: C [M x N] = A B^T over 16-bit operands with fp32 accumulators, by pairs of CTAs on tcgen05, and what
 // the loss does with a finished tile.  Used by class_loss.cu for
-//   kStats     z = H W^T + b, not kept: per row the largest value, the sum(s) of the softmax and the product with the row's targets
-//   kGrad      z again, turned into G = d loss / d z and rounded to the operand type (fp32: into three parts)
+//   kStats     z = H W^T + b: per row and half a tile the largest value, the sum(s) of the softmax and the product with the row's targets; where gradients are
+//              wanted, z itself for class_grad_kernel: in 16 bits below that largest value, or in fp32
 //   kOut       dH = G W and dW = G^T H, scaled and rounded to the result's type
-//   kPartial   the same as fp32 sums of a share of the reduction, for join_parts_kernel
 #pragma once
 
 #include <cuda.h>
@@ -28,35 +27,43 @@ constexpr int CT_STAGING = CT_EPI_WARPS * 2048;             // and 64 bytes of e
 constexpr int CT_SMEM = CT_RING + 1024 + 256 + CT_BIAS + CT_STAGING;
 constexpr int CT_TMEM = 512;                                // two accumulators of 256 columns
 
-enum TileUse { kStats, kGrad, kOut, kPartial };
+enum TileUse { kStats, kOut };
 
-// An operand of the product: a matrix [parts][rows][inner] behind a TMA descriptor.  K-major: inner is the reduction; MN-major: rows are.
+// z of a row is kept as whole numbers of 1 / 2048 octaves below the largest of the 128 (64) classes that a draining warp has of it: 16 bits reach 32 octaves, and a
+// probability is off by 1.7e-4 of itself, a fourteenth of what bfloat16 and two thirds of what fp16 rounds off it.  The last code is a probability of zero.
+constexpr float kCodeSteps = 2048.f;
+constexpr int kCodeZero = 65535;
+enum SaveAs { kSaveNone, kSaveCode, kSaveFloat };
+enum AddTo { kAddNone, kAddFirst, kAddMore, kAddLast };   // result; sums [M x N] in fp32: begun, added to, added and turned into the result
+
 struct TileArgs {
     int M, N;                  // result
     int tiles_m, tiles_n, width;   // tiles of 256 x width (128 or 256)
     int nkb;                   // 64-blocks of the reduction
-    int splits, kb_split;      // shares of it, blocks a share
+    int whole;                 // tiles whose reduction is one unit of work; those behind them come in `shares` of kb_share blocks each
+    int shares, kb_share;
     int group;                 // row tiles that are gone through together, for the L2
     int pairs;                 // products of operand parts: 1, or 6 for operands in three parts
     int chunk;                 // ADD_UP: ring stages that are summed in tensor memory before the sum moves to registers
-    int b_row0;                // first row of B (MN-major: added to the reduction, K-major: to the column)
+    int a_row0;                // first row of A (K-major)
+    int b_row0;                // first row of B (MN-major)
     int bf16;                  // operand type: 1 bfloat16, 0 fp16
     int32_t* err;
-    // kStats, kGrad
+    // kStats
     const void* bias;          // [classes] in the caller's type, or null
     int bias_type;
-    int col0, classes;         // first class of the piece; all of them
     float sc, inv_t;           // log2(e) (/ T with one softmax), 1 / T of the second
     const int2* targets;       // [M x ntargets] (class, weight), classes ascending
     int ntargets;
     float4* stats;             // [2 tiles_n x M]
-    const float4* rowc;        // [M] coefficients of the softmaxes, their log2 sums
-    const float4* rowk;        // [M] .w = weight of the row
-    const float* scal;         // [0] scale of G, [1] factor of the results
-    void* C;                   // kGrad: G [parts][M x ldc]; kOut, kPartial: the result
-    long long ldc, part_stride;
-    int accumulate;            // kPartial: add to what is there
-    float* colsum;             // kGrad: [8 tiles_m][ldc] column sums of 32 rows each, or null
+    int save;                  // SaveAs
+    // what is written
+    void* C;                   // kStats: z as saved [M x ldc]; kOut: the result
+    long long ldc;
+    int add;                   // AddTo
+    float* sums;               // [M x N]
+    float* slots;              // [tiles - whole][shares][256 x width] sums of shares
+    const float* scal;         // [1] factor of the results
 };
 
 // Products of operand parts, the smallest first, so that what an addition to the accumulator cuts off is small for as long as possible.
@@ -185,31 +192,34 @@ __device__ __forceinline__ void drain_rows(uint8_t* buf, int lane, const float (
     }
 }
 
-// Sum over the warp's lanes of every one of 32 values: lane c gets that of v[c].
-__device__ __forceinline__ float column_sums(const float (&v)[32], int lane) {
-    float a[16];
+// The same for codes, already whole numbers in the low 16 bits of the values.
+__device__ __forceinline__ void drain_codes(uint8_t* buf, int lane, const float (&v)[32], uint16_t* __restrict__ out, long long ld, int rows) {
+    __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const float keep = (lane & 16) ? v[j + 16] : v[j], give = (lane & 16) ? v[j] : v[j + 16];
-        a[j] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+    for (int k = 0; k < 4; ++k) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __byte_perm(__float_as_uint(v[8 * k + 2 * i]), __float_as_uint(v[8 * k + 2 * i + 1]), 0x5410);
+        *reinterpret_cast<uint4*>(staged(buf, lane, k)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
-#pragma unroll
-    for (int w = 8; w > 0; w >>= 1)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < w) {
-                const float keep = (lane & w) ? a[j + w] : a[j], give = (lane & w) ? a[j] : a[j + w];
-                a[j] = keep + __shfl_xor_sync(0xffffffffu, give, w);
-            }
-    return a[0];
+    __syncwarp();
+    copy_out<16, uint16_t, false>(buf, lane, out, ld, rows, 32);
 }
 
-struct TileAt { int m, n, split; };
+// A unit of work: a tile, and the blocks of its reduction.
+struct TileAt { int m, n, kb0, nkb, slot; };
+__device__ __forceinline__ long long units_of(const TileArgs& a) { return a.whole + ((long long)a.tiles_m * a.tiles_n - a.whole) * a.shares; }
 __device__ __forceinline__ TileAt tile_at(const TileArgs& a, long long u) {
-    const long long tiles = (long long)a.tiles_m * a.tiles_n;
     TileAt t;
-    t.split = (int)(u / tiles);
-    const long long i = u - t.split * tiles, per = (long long)a.group * a.tiles_n;
+    long long i = u;
+    t.kb0 = 0; t.nkb = a.nkb; t.slot = -1;
+    if (u >= a.whole && a.shares > 1) {
+        t.slot = (int)(u - a.whole);
+        i = a.whole + t.slot / a.shares;
+        t.kb0 = t.slot % a.shares * a.kb_share;
+        t.nkb = min(a.kb_share, a.nkb - t.kb0);
+    }
+    const long long per = (long long)a.group * a.tiles_n;
     const int g = (int)(i / per), first = g * a.group, rows = min(a.group, a.tiles_m - first);
     const int r = (int)(i - g * per);
     t.m = first + r % rows;
@@ -217,7 +227,7 @@ __device__ __forceinline__ TileAt tile_at(const TileArgs& a, long long u) {
     return t;
 }
 
-// USE as above; A_MN, B_MN: operand is MN-major; T: type of the result (kGrad: float = three bfloat16 parts); NL: softmaxes (temperatures) at once.
+// USE as above; A_MN, B_MN: operand is MN-major; T: type of the result; NL: softmaxes (temperatures) at once.
 // ADD_UP: the tensor core cuts its accumulator off at every addition (it does not round), half a step a time and always towards zero: long reductions lose
 // 5e-9 of their value per 16 terms (128 000 x 4096 logits of one row: loss off by 1.3e-6).  Where a result is wanted to fp32 accuracy the
 // reduction is cut into chunks whose sums the draining threads add up in registers.
@@ -256,11 +266,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     pdl_wait();
 
     const int ncl = gridDim.x >> 1, half_w = a.width / 2;
-    const long long units = (long long)a.tiles_m * a.tiles_n * a.splits;
-    auto blocks_of = [&](int split, int& kb0) {
-        kb0 = split * a.kb_split;
-        return min(a.kb_split, a.nkb - kb0);
-    };
+    const long long units = units_of(a);
 
     if (warp == 0 && lane == 0) {
         // ---------------- TMA producer: this CTA's rows of A and half of the rows of B, 64 of the reduction at a time ----------------
@@ -270,12 +276,10 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
             const TileAt t = tile_at(a, u);
             const int ra = t.m * CT_M + (int)rank * CT_H, rb = t.n * a.width + (int)rank * half_w;
-            int kb0;
-            const int nkb = blocks_of(t.split, kb0);
             for (int p = 0; p < a.pairs && ok; ++p) {
                 int za, zb;
                 part_pair(p, a.pairs, za, zb);
-                for (int kb = kb0; kb < kb0 + nkb; ++kb) {
+                for (int kb = t.kb0; kb < t.kb0 + t.nkb; ++kb) {
                     if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, 31))) break;
                     mbar_expect_tx(full(stage), (uint32_t)(CT_H + half_w) * (CT_K * 2));
                     const uint32_t base = sm_addr + stage * CT_STAGE;
@@ -283,12 +287,12 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                         tma_load_3d(base, &tmA, ra, kb * CT_K, za, full(stage));
                         tma_load_3d(base + 8192, &tmA, ra + 64, kb * CT_K, za, full(stage));
                     } else {
-                        tma_load_3d(base, &tmA, kb * CT_K, ra, za, full(stage));
+                        tma_load_3d(base, &tmA, kb * CT_K, a.a_row0 + ra, za, full(stage));
                     }
                     if (B_MN) {
                         for (int j = 0; j < half_w; j += 64) tma_load_3d(base + CT_OPERAND + j * 128, &tmB, rb + j, a.b_row0 + kb * CT_K, zb, full(stage));
                     } else {
-                        tma_load_3d(base + CT_OPERAND, &tmB, kb * CT_K, a.b_row0 + rb, zb, full(stage));
+                        tma_load_3d(base + CT_OPERAND, &tmB, kb * CT_K, rb, zb, full(stage));
                     }
                     if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
                 }
@@ -300,8 +304,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         uint32_t phase = 0;
         bool ok = true;
         for (long long u = blockIdx.x >> 1; u < units && ok && lane == 0; u += ncl) {
-            int kb0;
-            const int steps = blocks_of(tile_at(a, u).split, kb0) * a.pairs;
+            const int steps = tile_at(a, u).nkb * a.pairs;
             for (int i = 0; i < steps; ++i) {
                 if (!(ok = mbar_wait(full(stage), phase, abort_flag, a.err, 34))) break;
                 mbar_arrive_leader(pfull(stage));
@@ -316,8 +319,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         constexpr uint32_t stepA = A_MN ? 128 : 2, stepB = B_MN ? 128 : 2;    // 16 values of the reduction: 16 rows of 128 bytes, or 32 bytes of a row
         bool ok = true;
         for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
-            int kb0;
-            const int steps = blocks_of(tile_at(a, u).split, kb0) * a.pairs;
+            const int steps = tile_at(a, u).nkb * a.pairs;
             int left = 0;                                          // stages until this accumulator is full
             for (int i = 0; i < steps; ++i) {
                 const bool first = left == 0;
@@ -349,25 +351,23 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         uint8_t* buf = sm + CT_RING + 256 + CT_BIAS + ew * 2048;
         int acc = 0;
         uint32_t acc_phase = 0;
-        float gscale = 1.f, factor = 1.f;
-        if (USE == kGrad) gscale = a.scal[0];
-        if (USE == kOut) factor = a.scal[1];
-        const int bytes = USE == kOut || USE == kPartial ? store_bytes(a.C, a.ldc * (long long)sizeof(T)) : 16;
+        const float factor = USE == kOut ? a.scal[1] : 1.f;
+        const int bytes = USE == kOut ? store_bytes(a.C, a.ldc * (long long)sizeof(T)) : 16, sum_bytes = a.N % 4 == 0 ? 16 : a.N % 2 == 0 ? 8 : 4;
         for (long long u = blockIdx.x >> 1; u < units; u += ncl) {
             const TileAt t = tile_at(a, u);
-            const int row = t.m * CT_M + (int)rank * CT_H + q * 32 + lane;
+            const int row0 = t.m * CT_M + (int)rank * CT_H + q * 32, rows = a.M - row0;   // this warp's rows
+            const int row = row0 + lane;
             const bool rv = row < a.M;
-            const int tile_c = t.n * a.width + half * half_w;               // first column of this warp, in the piece
-            float m2 = -INFINITY, s1 = 0.f, s2 = 0.f, dot = 0.f, fw = 0.f, fa = 0.f, fb = 0.f;
-            float4 rc = make_float4(0.f, 0.f, 0.f, 0.f);
+            const int tile_c = t.n * a.width + half * half_w;               // first column of this warp
+            float m2 = -INFINITY, s1 = 0.f, s2 = 0.f, dot = 0.f;
             int e = 0, next = INT_MAX;
             const int2* tg = nullptr;
-            if (USE == kStats || USE == kGrad) {
+            if (USE == kStats) {
                 __syncwarp();                                               // the previous tile's biases have been read
                 for (int j = lane; j < half_w; j += 32) {
-                    const int c = a.col0 + tile_c + j;
-                    float b = c < a.classes ? 0.f : -INFINITY;              // columns that are no class carry no weight
-                    if (a.bias && c < a.classes)
+                    const int c = tile_c + j;
+                    float b = c < a.N ? 0.f : -INFINITY;                    // columns that are no class carry no weight
+                    if (a.bias && c < a.N)
                         b = a.bias_type == GAD_F32 ? reinterpret_cast<const float*>(a.bias)[c]
                             : a.bias_type == GAD_F16 ? to_float(reinterpret_cast<const __half*>(a.bias)[c]) : to_float(reinterpret_cast<const __nv_bfloat16*>(a.bias)[c]);
                     bias[j] = b * a.sc;
@@ -378,81 +378,61 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     int hi = a.ntargets;                                    // the first target at or behind this warp's columns
                     while (e < hi) {
                         const int mid = (e + hi) >> 1;
-                        if (tg[mid].x < a.col0 + tile_c) e = mid + 1; else hi = mid;
+                        if (tg[mid].x < tile_c) e = mid + 1; else hi = mid;
                     }
                     if (e < a.ntargets) next = tg[e].x;
-                    if (USE == kGrad) {
-                        rc = a.rowc[row];
-                        fw = a.rowk[row].w * gscale;
-                        fa = rc.x * fw;
-                        fb = rc.y * fw;
-                    }
                 }
             }
-            const int row0 = t.m * CT_M + (int)rank * CT_H + q * 32, rows = a.M - row0;   // this warp's rows
             // 32 finished values of this thread's row, from column c0 of the warp's columns on
             const auto take = [&](int c0, float (&v)[32]) {
-                const int gc = a.col0 + tile_c + c0;                        // class of v[0]
                 if (USE == kStats) {
-                    float most = m2;
+                    const float base = m2 == -INFINITY ? 0.f : m2;          // nothing but masked classes: all terms are zero
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
                         v[j] = fmaf(v[j], a.sc, bias[c0 + j]);
-                        most = fmaxf(most, v[j]);
-                    }
-                    const float base = most == -INFINITY ? 0.f : most;      // nothing but masked classes so far: all terms are zero
-                    s1 *= exp2_fast(m2 - base);
-                    if (NL == 2) s2 *= exp2_fast((m2 - base) * a.inv_t);
-                    m2 = most;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
                         s1 += exp2_fast(v[j] - base);
                         if (NL == 2) s2 += exp2_fast((v[j] - base) * a.inv_t);
                     }
-                    while (next < gc + 32) {
-                        dot = fmaf(__int_as_float(tg[e].y), pick(v, next - gc), dot);
+                    while (next < tile_c + c0 + 32) {
+                        dot = fmaf(__int_as_float(tg[e].y), pick(v, next - tile_c - c0), dot);
                         next = ++e < a.ntargets ? tg[e].x : INT_MAX;
                     }
-                } else if (USE == kGrad) {
+                    if (a.save == kSaveCode) {
+                        // rounded by the addition of 2^23, whose sum has the whole number in its low bits
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const float z = fmaf(v[j], a.sc, bias[c0 + j]);
-                        v[j] = fw == 0.f ? 0.f : fa * exp2_fast(z - rc.z);
-                        if (NL == 2) v[j] += fw == 0.f ? 0.f : fb * exp2_fast(fmaf(z, a.inv_t, -rc.w));
-                    }
-                    while (next < gc + 32) {
-                        const int at = next - gc;
-                        const float w = fw * __int_as_float(tg[e].y);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] -= j == at ? w : 0.f;
-                        next = ++e < a.ntargets ? tg[e].x : INT_MAX;
-                    }
-                    __syncwarp();
-                    if (a.colsum) a.colsum[(long long)(t.m * 8 + (int)rank * 4 + q) * a.ldc + tile_c + c0 + lane] = column_sums(v, lane);
-                    if constexpr (sizeof(T) == 4) {                         // three bfloat16 parts
-                        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.C) + (long long)row0 * a.ldc + tile_c + c0;
-#pragma unroll
-                        for (int k = 0; k < 3; ++k) {
-                            float p[32];
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                p[j] = v[j];
-                                v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
-                            }
-                            drain_rows<__nv_bfloat16>(buf, lane, p, out + k * a.part_stride, a.ldc, rows, 32, 16);
-                        }
-                    } else {
-                        drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, 32, 16);
+                        for (int j = 0; j < 32; ++j) v[j] = fminf(base - v[j], (float)kCodeZero / kCodeSteps) * kCodeSteps + 8388608.f;
+                        drain_codes(buf, lane, v, reinterpret_cast<uint16_t*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows);
+                    } else if (a.save == kSaveFloat) {
+                        drain_rows<float>(buf, lane, v, reinterpret_cast<float*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, 32, 16);
                     }
                 } else if (tile_c + c0 < a.N) {
-                    if (USE == kOut) {
+                    const int cols = a.N - tile_c - c0;
+                    const long long at = (long long)row0 * a.N + tile_c + c0;
+                    if (t.slot >= 0) {
+                        float* out = a.slots + (long long)t.slot * CT_M * a.width + (long long)(row0 - t.m * CT_M) * a.width + half * half_w + c0;
+                        drain_rows<float>(buf, lane, v, out, a.width, 32, 32, 16);
+                    } else if (a.add == kAddFirst) {
+                        drain_rows<float>(buf, lane, v, a.sums + at, a.N, rows, cols, sum_bytes);
+                    } else if (a.add == kAddMore) {
+                        drain_rows<float, true>(buf, lane, v, a.sums + at, a.N, rows, cols, sum_bytes);
+                    } else {
+                        if (a.add == kAddLast) {
+                            // sums come in through the staging buffer, as they left
+#pragma unroll
+                            for (int c = 0; c < 32; c += 16) {
+                                __syncwarp();
+                                for (int i = lane; i < 32 * 16; i += 32) {
+                                    const int r = i >> 4, x = i & 15;
+                                    *reinterpret_cast<float*>(staged(buf, r, x >> 2) + (x & 3) * 4) = r < rows && c + x < cols ? a.sums[at + (long long)r * a.N + c + x] : 0.f;
+                                }
+                                __syncwarp();
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) v[c + j] += *reinterpret_cast<const float*>(staged(buf, lane, j >> 2) + (j & 3) * 4);
+                            }
+                        }
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] *= factor;
-                        drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, a.N - tile_c - c0, bytes);
-                    } else {
-                        float* out = reinterpret_cast<float*>(a.C) + t.split * a.part_stride + (long long)row0 * a.ldc + tile_c + c0;
-                        if (a.accumulate) drain_rows<float, true>(buf, lane, v, out, a.ldc, rows, a.N - tile_c - c0, bytes);
-                        else drain_rows<float>(buf, lane, v, out, a.ldc, rows, a.N - tile_c - c0, bytes);
+                        drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, cols, bytes);
                     }
                 }
             };
@@ -470,8 +450,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 return ok;
             };
             if constexpr (ADD_UP) {
-                int kb0;
-                const int chunks = (blocks_of(t.split, kb0) * a.pairs + a.chunk - 1) / a.chunk;
+                const int chunks = (t.nkb * a.pairs + a.chunk - 1) / a.chunk;
                 if (chunks > 1) {
                     float sum[4][32];
 #pragma unroll
@@ -498,6 +477,14 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     tmem_wait_st();
                 } else if (!wait_full()) break;
             } else if (!wait_full()) break;
+            if (USE == kStats)                                              // the largest first, then everything relative to it
+                for (int c0 = 0; c0 < half_w; c0 += 32) {
+                    float v[32];
+                    __syncwarp();
+                    tmem_ld32(tm_row + (uint32_t)(acc * 256 + c0), v);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) m2 = fmaxf(m2, fmaf(v[j], a.sc, bias[c0 + j]));
+                }
             for (int c0 = 0; c0 < half_w; c0 += 32) {
                 float v[32];
                 __syncwarp();

@@ -4,13 +4,15 @@
 // Both kinds of target are one sparse list of (class, weight): tau = a [y] + (1 - a) T q at the teacher's classes.  Then
 //   l_i = a lse(z) + (1 - a) T^2 (lse(z / T) + sum q log q) - sum_v tau_v z_v,     dl_i / dz = a p + (1 - a) T p^T - tau.
 //
-// One call: the rows' targets are sorted by class and the rows copied to the operand type (class_rows_kernel); z = H W^T tile by tile leaves per row and tile
-// half the largest value, the sums and sum tau z (kStats), class_finish_kernel joins them.  For the gradients the classes are gone through in pieces: z
-// again, turned into G (kGrad), and from it dH += G W and dW = G^T H (kOut, kPartial).  The logits take 2 N V D flops twice instead of N V values kept.
+// One call: the rows' targets are sorted by class and the rows copied to the operand type (class_rows_kernel).  z = H W^T tile by tile leaves per row and tile
+// half the largest value, the sums and sum tau z (kStats); class_finish_kernel joins them.  For gradients the rows are gone through in blocks: of a
+// block the tiles leave z too, as 16-bit codes (fp32: as it is), class_grad_kernel turns it into G where it lies, and dH = G W and dW += G^T H follow
+// (kOut).  So what is held of the rows x classes matrix is bounded (kBlockBytes), whatever its size.  Taking z again from H and W instead, once its row sums are
+// known, needs no codes but a third more flops: 4096 x 1024 bf16 against 32 768 classes 918 us, now 770.
 //
 // Operands: fp16 and bfloat16 as they are.  fp32 in three bfloat16 parts (24 bits), of whose nine products the six that reach 2^-24 are summed.
 // G is rounded to the operand type (fp32: not rounded), times a power of two that brings its largest possible value to 2^14 .. 2^15: in fp16 a probability of 1e-9 keeps
-// eight bits.  One rounding of each term of a sum whose result is rounded to the same type: the result's error grows by at most the square root of 2.
+// eight bits.  One rounding of each term of a sum whose result is rounded to the same type: the result's error grows by about the square root of 2.
 #include <algorithm>
 #include <atomic>
 
@@ -22,7 +24,7 @@ namespace {
 
 constexpr int kRowThreads = 128;
 constexpr int kMostTargets = 1024;                       // teacher logits a row
-constexpr int64_t kPieceBytes = 512ll << 20;             // of G held at once
+constexpr int64_t kBlockBytes = 1ll << 30;               // of probabilities and gradients of logits held at once
 constexpr float kLog2e = 1.44269504f;
 
 template <class P> __device__ __forceinline__ float load_as_float(const void* p, int64_t i) { return to_float(reinterpret_cast<const P*>(p)[i]); }
@@ -78,26 +80,39 @@ struct RowArgs {
     void* Hp; int64_t ldp, part_stride;
     int2* targets; int ntargets;
     float4* rowk;
-    int32_t* status;
     int64_t rows;
-    unsigned* ticket;
+    struct RowShare* shares; unsigned* ticket;
+    int32_t* status;
 };
+
+// What a block of the row kernels contributes to the scale of the gradients: rows that count, the largest coefficient of G.
+struct RowShare { int n; float most; };
 
 // Labels alone: a warp a row.
 template <class T>
 __global__ void __launch_bounds__(256) class_label_rows_kernel(const RowArgs a) {
+    __shared__ RowShare part[8];
     const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
     pdl_next();
-    if (blockIdx.x == 0 && threadIdx.x == 0) { *a.status = 0; *a.ticket = 0u; }
-    if (r >= a.rows) return;
-    const int64_t y = load_index(a.labels, a.label_bytes, r);
-    const bool counts = y >= 0, bad = y >= a.classes;
-    if (lane == 0) {
-        a.targets[r] = make_int2(counts && !bad ? (int)y : INT_MAX, __float_as_int(counts && !bad ? 1.f : 0.f));
-        a.rowk[r] = make_float4(counts ? 1.f : 0.f, 0.f, bad ? NAN : 0.f, counts ? (a.weights ? a.weights[r] : 1.f) : 0.f);
-    }
-    pack_row<T>(reinterpret_cast<const T*>(a.H) + r * a.ldh, a.cols, counts, a.Hp, r * a.ldp, a.part_stride, lane, 32);
+    pdl_wait();
+    if (r < a.rows) {
+        const int64_t y = load_index(a.labels, a.label_bytes, r);
+        const bool counts = y >= 0, bad = y >= a.classes;
+        const float w = counts ? (a.weights ? a.weights[r] : 1.f) : 0.f;
+        if (lane == 0) {
+            a.targets[r] = make_int2(counts && !bad ? (int)y : INT_MAX, __float_as_int(counts && !bad ? 1.f : 0.f));
+            a.rowk[r] = make_float4(counts ? 1.f : 0.f, 0.f, bad ? NAN : 0.f, w);
+            part[threadIdx.x >> 5] = {counts, fabsf(w)};
+        }
+        pack_row<T>(reinterpret_cast<const T*>(a.H) + r * a.ldh, a.cols, counts, a.Hp, r * a.ldp, a.part_stride, lane, 32);
+    } else if (lane == 0) part[threadIdx.x >> 5] = {0, 0.f};
+    __syncthreads();
+    if (threadIdx.x) return;
+    RowShare mine = part[0];
+    for (int i = 1; i < 8; ++i) { mine.n += part[i].n; mine.most = fmaxf(mine.most, part[i].most); }
+    a.shares[blockIdx.x] = mine;
+    if (blockIdx.x == 0) { *a.ticket = 0u; *a.status = 0; }
 }
 
 // A block a row.  rowk = (coefficient of lse(z), of lse(z / T), sum of q log q with its factor, weight of the row); a row without target: (0, 0, 0, 0).
@@ -111,7 +126,8 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
     const int64_t r = blockIdx.x;
     const int t = threadIdx.x, lane = t & 31, w = t >> 5;
     pdl_next();
-    if (t == 0) { bad = 0; soft_any = 0; if (r == 0) { *a.status = 0; *a.ticket = 0u; } }
+    pdl_wait();
+    if (t == 0) { bad = 0; soft_any = 0; }
     __syncthreads();
     float most = -INFINITY;
     for (int j = t; j < a.k; j += kRowThreads) {
@@ -173,8 +189,13 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
         const float tv = tau[j];
         a.targets[r * a.ntargets + at] = make_int2(c, __float_as_int(c == INT_MAX ? 0.f : tv));
     }
-    if (t == 0) a.rowk[r] = make_float4(ha, hb * tt * tt, counts && bad ? NAN : hb * tt * tt * ent, counts ? (a.weights ? a.weights[r] : 1.f) : 0.f);
+    const float weight = counts ? (a.weights ? a.weights[r] : 1.f) : 0.f;
+    if (t == 0) a.rowk[r] = make_float4(ha, hb * tt * tt, counts && bad ? NAN : hb * tt * tt * ent, weight);
     pack_row<T>(reinterpret_cast<const T*>(a.H) + r * a.ldh, a.cols, counts, a.Hp, r * a.ldp, a.part_stride, t, kRowThreads);
+    if (t == 0) {
+        a.shares[r] = {counts, counts ? fabsf(weight) * (ha + hb * tt) : 0.f};
+        if (r == 0) { *a.ticket = 0u; *a.status = 0; }
+    }
 }
 
 // Class vectors that no descriptor can reach (fp32, or rows that do not start on 16 bytes) as operands: a warp a row.
@@ -186,25 +207,33 @@ __global__ void __launch_bounds__(256) class_pack_kernel(const T* __restrict__ W
     if (r < rows) pack_row<T>(W + r * ldw, cols, true, Wp, r * ldp, part_stride, threadIdx.x & 31, 32);
 }
 
-// What a block of class_finish_kernel adds to the loss: sum of weighted row losses, the largest coefficient of G, counted rows.
-struct LossShare { double sum; float most; int n; };
 constexpr int kFinishRows = 8;
 
-// The parts of a row's statistics joined (a block has 8 rows, 32 threads each, every 32nd part a thread; joined pairwise in a fixed order), and in the block that
-// comes last the loss and what the gradients are multiplied with.  scal[0]: a power of two that brings the largest coefficient of G to 2^14 .. 2^15;
-// [1]: scale / counted rows / that.
+struct FinishArgs {
+    const float4* stats; int parts, rows;
+    const float4* rowk;
+    float sc, inv_t, temperature;
+    float4* rowc; float* row_loss;
+    double* shares; int share0, nshares;          // of the loss: a block's sum of weighted row losses
+    const RowShare* row_shares; int nrow_shares;
+    unsigned* ticket;
+    float scale; int mean, first, final;
+    float *scal, *loss;
+};
+
+// The parts of a row's statistics joined: a block has 8 rows, 32 threads each, every 32nd part a thread; joined pairwise in a fixed order.  The block that comes last
+// writes, for the first block of rows, scal[0], a power of two that brings the largest coefficient of G to 2^14 .. 2^15, [1]: scale / counted rows / that,
+// [2]: scale / counted rows; and for the last one the loss.
 template <int NL>
-__global__ void __launch_bounds__(256) class_finish_kernel(const float4* __restrict__ stats, int parts, int rows, const float4* __restrict__ rowk, float sc, float inv_t, float hard_t,
-                                                           float4* __restrict__ rowc, float* __restrict__ row_loss, LossShare* shares, unsigned* ticket, float scale, int mean,
-                                                           float* __restrict__ scal, float* __restrict__ loss) {
+__global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
     __shared__ float4 sm[8][kFinishRows];
     __shared__ bool last;
-    __shared__ LossShare smt[8];
+    __shared__ double smt[8];
+    __shared__ RowShare smr[8];
     const int rl = threadIdx.x % kFinishRows, lane = threadIdx.x & 31, w = threadIdx.x >> 5, r = blockIdx.x * kFinishRows + rl;
     pdl_next();
     pdl_wait();
-    after_wait(stats);
-    after_wait(rowk);
+    const float inv_t = a.inv_t;
     const float4 none = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     const auto join = [&](const float4& u, const float4& v) {
         const float most = fmaxf(u.x, v.x), base = most == -INFINITY ? 0.f : most;
@@ -216,11 +245,11 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const float4* __restr
         return o;
     };
     float4 at = none;
-    if (r < rows)
-        for (int p = threadIdx.x / kFinishRows; p < parts; p += 128) {
+    if (r < a.rows)
+        for (int p = threadIdx.x / kFinishRows; p < a.parts; p += 128) {
             float4 v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = p + 32 * i < parts ? stats[(int64_t)(p + 32 * i) * rows + r] : none;
+            for (int i = 0; i < 4; ++i) v[i] = p + 32 * i < a.parts ? a.stats[(int64_t)(p + 32 * i) * a.rows + r] : none;
             at = join(at, join(join(v[0], v[1]), join(v[2], v[3])));
         }
 #pragma unroll
@@ -231,98 +260,197 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const float4* __restr
     if (lane < kFinishRows) sm[w][lane] = at;
     __syncthreads();
     if (w == 0) {
-        LossShare mine{0.0, 0.f, 0};
-        if (lane < kFinishRows && r < rows) {
+        double mine = 0.0;
+        if (lane < kFinishRows && r < a.rows) {
             at = sm[0][lane];
             for (int i = 1; i < 8; ++i) at = join(at, sm[i][lane]);
-            const float4 k = rowk[r];
+            const float4 k = a.rowk[r];
             // in log2: of the (first) softmax, whose logits were scaled by sc, and of the second
             const float l1 = at.x + log2f(at.y), l2 = NL == 2 ? at.x * inv_t + log2f(at.z) : l1;
             const float ln2 = 0.693147181f;
             const bool counts = k.x > 0.f || k.y > 0.f;
-            const float l = counts ? k.x * (l1 * ln2) + k.y * (l2 * ln2) + k.z - at.w / sc : 0.f;
-            row_loss[r] = l;
+            const float l = counts ? k.x * (l1 * ln2) + k.y * (l2 * ln2) + k.z - at.w / a.sc : 0.f;
+            a.row_loss[r] = l;
             // gradient: a p + (1 - a) T p^T; with one softmax both coefficients are its
-            const float a = k.x, b = k.y / hard_t;
-            if (rowc) rowc[r] = NL == 2 ? make_float4(a, b, l1, l2) : make_float4(a + b, 0.f, l1, 0.f);
-            if (counts) { mine.sum = (double)k.w * (double)l; mine.most = fabsf(k.w) * (a + b); mine.n = 1; }
+            const float ca = k.x, cb = k.y / a.temperature;
+            if (a.rowc) a.rowc[r] = NL == 2 ? make_float4(ca, cb, l1, l2) : make_float4(ca + cb, 0.f, l1, 0.f);
+            if (counts) mine = (double)k.w * (double)l;
         }
 #pragma unroll
-        for (int o = 1; o < kFinishRows; o <<= 1) {
-            mine.sum += __shfl_xor_sync(0xffffffffu, mine.sum, o);
-            mine.most = fmaxf(mine.most, __shfl_xor_sync(0xffffffffu, mine.most, o));
-            mine.n += __shfl_xor_sync(0xffffffffu, mine.n, o);
-        }
+        for (int o = 1; o < kFinishRows; o <<= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
         if (lane == 0) {
-            shares[blockIdx.x] = mine;
+            a.shares[a.share0 + blockIdx.x] = mine;
             __threadfence();
-            last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+            last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
         }
     }
     __syncthreads();
     if (!last) return;
     __threadfence();
-    LossShare all{0.0, 0.f, 0};
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += 256) {
-        const double s = __ldcg(&shares[i].sum);
-        all.sum += s;
-        all.most = fmaxf(all.most, __ldcg(&shares[i].most));
-        all.n += __ldcg(&shares[i].n);
-    }
+    if (a.first) {
+        RowShare rows{0, 0.f};
+        for (int i = threadIdx.x; i < a.nrow_shares; i += 256) {
+            const RowShare v = a.row_shares[i];
+            rows.n += v.n;
+            rows.most = fmaxf(rows.most, v.most);
+        }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        all.sum += __shfl_xor_sync(0xffffffffu, all.sum, o);
-        all.most = fmaxf(all.most, __shfl_xor_sync(0xffffffffu, all.most, o));
-        all.n += __shfl_xor_sync(0xffffffffu, all.n, o);
+        for (int o = 16; o > 0; o >>= 1) {
+            rows.n += __shfl_xor_sync(0xffffffffu, rows.n, o);
+            rows.most = fmaxf(rows.most, __shfl_xor_sync(0xffffffffu, rows.most, o));
+        }
+        if (lane == 0) smr[w] = rows;
     }
+    double all = 0.0;
+    if (a.final)
+        for (int i = threadIdx.x; i < a.nshares; i += 256) all += __ldcg(a.shares + i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
     if (lane == 0) smt[w] = all;
     __syncthreads();
     if (threadIdx.x) return;
-    all = smt[0];
-    for (int i = 1; i < 8; ++i) { all.sum += smt[i].sum; all.most = fmaxf(all.most, smt[i].most); all.n += smt[i].n; }
-    const double f = mean ? (all.n ? (double)scale / all.n : 0.0) : (double)scale;
-    loss[0] = (float)(f * all.sum);
-    const int e = all.most > 0.f && all.most < INFINITY ? 14 - ilogbf(all.most) : 0;
-    scal[0] = ldexpf(1.f, max(-100, min(100, e)));
-    scal[1] = (float)(f / (double)scal[0]);
+    if (a.first) {
+        RowShare v = smr[0];
+        for (int i = 1; i < 8; ++i) { v.n += smr[i].n; v.most = fmaxf(v.most, smr[i].most); }
+        const double f = a.mean ? (v.n ? (double)a.scale / v.n : 0.0) : (double)a.scale;
+        const int e = v.most > 0.f && v.most < INFINITY ? 14 - ilogbf(v.most) : 0;
+        const float g = ldexpf(1.f, max(-100, min(100, e)));
+        a.scal[0] = g;
+        a.scal[1] = (float)(f / (double)g);
+        a.scal[2] = (float)f;
+    }
+    if (a.final) {
+        all = smt[0];
+        for (int i = 1; i < 8; ++i) all += smt[i];
+        a.loss[0] = (float)((double)a.scal[2] * all);
+    }
+    *a.ticket = 0u;                               // for the next block of rows
 }
 
-// result [rows x cols] = factor x the sum of the shares, in order; VEC columns a thread.
-template <class T, int VEC>
-__global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ part, int splits, int64_t part_stride, int64_t rows, int cols, const float* __restrict__ scal,
-                                                         T* __restrict__ out, int64_t ld) {
+// G from what the tiles left of z, in its place (16-bit codes) or beside it (fp32): G = w (a p + (1 - a) T p^T - tau) times scal[0], in the operand type or (T = float) in
+// three bfloat16 parts.  A warp takes 256 classes of a row at a time, a block 32 rows of them, so column sums (for db, before any rounding) cost one
+// exchange.  Bound by memory: 4 bytes a value.
+struct GradArgs {
+    const void* z; long long ldz;             // codes or fp32 [rows x ldz]
+    void* G; long long ldg, part_stride;
+    const float4* stats; int half_w;          // .x = largest value of (part, row)
+    const float4 *rowc, *rowk;
+    const int2* targets; int ntargets;
+    const float* scal;
+    float inv_t;
+    float* colsum;                            // [row blocks x ldg] or null
+    int rows, classes;
+};
+template <class T, class Z, int NL>
+__global__ void __launch_bounds__(256) class_grad_kernel(const GradArgs a) {
+    __shared__ float sm[8][256 + 8];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c0 = blockIdx.x * 256, c = c0 + 8 * lane;
     pdl_next();
     pdl_wait();
-    after_wait(part);
-    after_wait(scal);
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC;
-    if (i >= rows * cols) return;
-    const int64_t r = i / cols;
-    const int c = (int)(i - r * cols);
-    float s[VEC];
+    const float gs = a.scal[0];
+    float sums[8];
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) s[j] = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < splits; ++k) {
-        const float* p = part + k * part_stride + i;
-        if constexpr (VEC == 4) {
-            const float4 v = *reinterpret_cast<const float4*>(p);
-            s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
-        } else s[0] += *p;
+    for (int j = 0; j < 8; ++j) sums[j] = 0.f;
+    const bool in = c < a.ldg;                // (rows of G are whole tiles of 128 classes)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = blockIdx.y * 32 + 8 * i + w;
+        if (r >= a.rows) break;
+        const float4 rc = a.rowc[r];
+        const float fw = a.rowk[r].w * gs;
+        // a sum that is not finite makes the whole row not a number, also where the code says zero; a row without weight is zero whatever it holds
+        const float fa = fw == 0.f ? 0.f : fw * rc.x + 0.f * rc.z, fb = fw == 0.f ? 0.f : fw * rc.y;
+        float v[8];
+        if (in) {
+            float z[8];                       // log2 of exp(z) relative to the first sum
+            if constexpr (sizeof(Z) == 2) {
+                union { uint4 u; uint16_t h[8]; } q;
+                q.u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.z) + (long long)r * a.ldz + c);
+                const float m = a.stats[(long long)(c / a.half_w) * a.rows + r].x;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] = q.h[j] == kCodeZero ? -INFINITY : fmaf((float)q.h[j], -1.f / kCodeSteps, m);
+            } else {
+                const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.z) + (long long)r * a.ldz + c);
+                const float4 x = p[0], y = p[1];
+                z[0] = x.x; z[1] = x.y; z[2] = x.z; z[3] = x.w; z[4] = y.x; z[5] = y.y; z[6] = y.z; z[7] = y.w;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = fw == 0.f ? 0.f : fa * exp2_fast(z[j] - rc.z);
+                if (NL == 2) v[j] += fw == 0.f ? 0.f : fb * exp2_fast(fmaf(z[j], a.inv_t, -rc.w));
+            }
+        }
+        const int2* tg = a.targets + (long long)r * a.ntargets;
+        int e = 0, hi = a.ntargets;
+        while (e < hi) {
+            const int mid = (e + hi) >> 1;
+            if (tg[mid].x < c0) e = mid + 1; else hi = mid;
+        }
+        for (; e < a.ntargets; ++e) {
+            const int2 t = tg[e];
+            if (t.x >= c0 + 256) break;
+            const float x = fw * __int_as_float(t.y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] -= t.x == c + j ? x : 0.f;
+        }
+        if (!in) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[j] += v[j];
+        if constexpr (sizeof(T) == 4) {
+            union { uint4 u; __nv_bfloat16 h[8]; } o[3];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                __nv_bfloat16 p[3];
+                split3(v[j], p);
+                o[0].h[j] = p[0]; o[1].h[j] = p[1]; o[2].h[j] = p[2];
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.G) + k * a.part_stride + (long long)r * a.ldg + c) = o[k].u;
+        } else {
+            union { uint4 u; T h[8]; } o;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o.h[j] = from_float<T>(v[j]);
+            *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.G) + (long long)r * a.ldg + c) = o.u;
+        }
     }
-    const float f = scal[1];
-    union { T e[VEC]; uint4 u4; uint2 u2; } w;
+    if (!a.colsum) return;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) w.e[j] = from_float<T>(f * s[j]);
-    T* o = out + r * ld + c;
-    if constexpr (VEC == 4 && sizeof(T) == 4) *reinterpret_cast<uint4*>(o) = w.u4;
-    else if constexpr (VEC == 4) *reinterpret_cast<uint2*>(o) = w.u2;
-    else *o = w.e[0];
+    for (int j = 0; j < 8; ++j) sm[w][8 * lane + j] = sums[j];
+    __syncthreads();
+    const int x = c0 + threadIdx.x;
+    if (x >= a.classes) return;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += sm[i][threadIdx.x];
+    a.colsum[(long long)blockIdx.y * a.ldg + x] = s;
 }
 
-// db of a piece from the column sums of 32 rows each that the drain of G leaves: 32 classes a block, each of its eight warps a run of them, in order.
+// The shares of the tiles that were cut along their reduction, added up in order, and put where an uncut tile would have gone.  A block has 32 rows of a tile.
 template <class T>
-__global__ void __launch_bounds__(256) class_bias_kernel(const float* __restrict__ colsum, int64_t ld, int n, int classes, const float* __restrict__ scal, T* __restrict__ db) {
+__global__ void __launch_bounds__(256) class_join_kernel(const TileArgs a) {
+    const int per_tile = CT_M / 32, i = blockIdx.x / per_tile, r0 = blockIdx.x % per_tile * 32;
+    pdl_next();
+    pdl_wait();
+    const TileAt t = tile_at(a, a.whole + (long long)i * a.shares);
+    const float factor = a.scal[1];
+    const float* slot = a.slots + (long long)i * a.shares * CT_M * a.width;
+    for (int j = threadIdx.x; j < 32 * a.width; j += 256) {
+        const int r = r0 + j / a.width, x = j % a.width, row = t.m * CT_M + r, c = t.n * a.width + x;
+        if (row >= a.M || c >= a.N) continue;
+        float s = 0.f;
+#pragma unroll 8
+        for (int k = 0; k < a.shares; ++k) s += slot[((long long)k * CT_M + r) * a.width + x];
+        float* sum = a.sums + (long long)row * a.N + c;
+        if (a.add == kAddMore || a.add == kAddLast) s += *sum;
+        if (a.add == kAddFirst || a.add == kAddMore) *sum = s;
+        else reinterpret_cast<T*>(a.C)[(long long)row * a.ldc + c] = from_float<T>(factor * s);
+    }
+}
+
+// db from the column sums of 32 rows each that class_grad_kernel leaves: 32 classes a block, each of its eight warps a run of them, in order.
+template <class T>
+__global__ void __launch_bounds__(256) class_bias_kernel(const float* __restrict__ colsum, int64_t ld, int n, int classes, const float* __restrict__ scal, int add, float* __restrict__ sums,
+                                                         T* __restrict__ db) {
     __shared__ float sm[8][32];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
     const int per = (n + 7) / 8, lo = min(n, w * per), hi = min(n, lo + per);
@@ -339,7 +467,9 @@ __global__ void __launch_bounds__(256) class_bias_kernel(const float* __restrict
     if (w || c >= classes) return;
     s = 0.f;
     for (int k = 0; k < 8; ++k) s += sm[k][threadIdx.x & 31];
-    db[c] = from_float<T>(s * scal[1]);
+    if (add == kAddMore || add == kAddLast) s += sums[c];
+    if (add == kAddFirst || add == kAddMore) sums[c] = s;
+    else db[c] = from_float<T>(s * scal[1]);
 }
 
 template <class T>
@@ -351,13 +481,8 @@ __global__ void class_empty_kernel(float* loss, int32_t* status) { *loss = 0.f; 
 // ---------------------------------------------------------------------------------------------
 // How a call is cut up; the same for the workspace and the launches.
 // ---------------------------------------------------------------------------------------------
-struct Cut { int splits, kb; };
-// Shares of the reduction: where there are fewer tiles than pairs of CTAs, as many as bring them near, of 8 blocks (512 values) and more.
-Cut cut_reduction(int64_t tiles, int nkb) {
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(74 / tiles, nkb / 8));
-    const int kb = (int)((nkb + want - 1) / want);
-    return {(nkb + kb - 1) / kb, kb};
-}
+constexpr int kPairs = 74;                               // pairs of CTAs that run at once
+
 // Kernels of one call follow each other by programmatic dependent launch: each comes up while the one in front ends and waits (pdl_wait) before it touches
 // memory.  The first waits for all that is in front of it on the stream.
 template <class... P, class... Args>
@@ -371,25 +496,18 @@ cudaError_t chain(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, 
     ++g_kernel_launches;
     return cudaLaunchKernelEx(&cfg, kernel, P(std::forward<Args>(args))...);
 }
-template <class T>
-cudaError_t join_parts(const float* part, int splits, int64_t part_stride, int64_t rows, int cols, const float* scal, T* out, int64_t ld, cudaStream_t s) {
-    const bool wide = cols % 4 == 0 && ld % 4 == 0 && ((uintptr_t)out & (4 * sizeof(T) - 1)) == 0;
-    const int64_t n = rows * cols, per = wide ? 1024 : 256;
-    return chain(wide ? join_parts_kernel<T, 4> : join_parts_kernel<T, 1>, dim3((unsigned)((n + per - 1) / per)), 256, 0, s, false, part, splits, part_stride, rows, cols, scal, out, ld);
-}
 
 int width_for(int n) { return n <= 128 ? 128 : 256; }
 
 struct ClassPlan {
-    int parts, pairs, es;            // operand parts, products of them, bytes of a caller's value
+    int parts, pairs;                // operand parts, products of them
     bool grads, pack_w;
-    int ntargets, nl;
-    int width_v, tiles_v, tiles_m, width_d, tiles_d;
-    int64_t ldp, ldg, piece;         // row lengths of the packed operands and of G, classes a piece
-    int npieces;
-    Cut cut_h, cut_w;
-    bool h_parts, w_parts;
-    int64_t o_hp, o_wp, o_targets, o_rowk, o_rowc, o_stats, o_shares, o_scal, o_g, o_colsum, o_dh, o_dw, total;
+    int ntargets, nl, save;
+    int width_v, tiles_v, width_d, tiles_d;
+    int64_t ldp, ldg;                // row lengths of the packed operands, and of z and G
+    int64_t block;                   // rows a block
+    int nblocks;
+    int64_t o_hp, o_wp, o_targets, o_rowk, o_rowc, o_stats, o_rshares, o_lshares, o_scal, o_z, o_g, o_colsum, o_dbsum, o_slots, o_sums, total;
 };
 
 ClassPlan plan_class(const gad_class_loss_args& a) {
@@ -398,48 +516,47 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     const int D = a.cols, V = a.classes;
     p.parts = a.dtype == GAD_F32 ? 3 : 1;
     p.pairs = a.dtype == GAD_F32 ? 6 : 1;
-    p.es = a.dtype == GAD_F32 ? 4 : 2;
     p.grads = a.dH || a.dW || a.db;
     p.pack_w = a.dtype == GAD_F32 || ((uintptr_t)a.W & 15) != 0 || (a.ldw * 2) % 16 != 0;
     p.ntargets = a.k + (a.labels ? 1 : 0);
     p.nl = a.k > 0 && a.labels && a.hard_weight > 0.f && a.hard_weight < 1.f && a.temperature != 1.f ? 2 : 1;
+    // a code's step is 1 / T times as large in the second softmax: up to twice it is still below what G is rounded by
+    p.save = !p.grads ? kSaveNone : a.dtype == GAD_F32 || (p.nl == 2 && a.temperature < 0.5f) ? kSaveFloat : kSaveCode;
     p.ldp = round_up(D, 8);
-    p.tiles_m = (int)((N + CT_M - 1) / CT_M);
     p.width_v = width_for(V);
     p.tiles_v = (V + p.width_v - 1) / p.width_v;
     p.width_d = width_for(D);
     p.tiles_d = (D + p.width_d - 1) / p.width_d;
-    int64_t most = std::max<int64_t>(1, kPieceBytes / (2 * p.parts * N * p.width_v)) * p.width_v;
-    p.npieces = (int)((V + most - 1) / most);
-    p.piece = round_up((V + p.npieces - 1) / p.npieces, p.width_v);
-    p.npieces = (int)((V + p.piece - 1) / p.piece);
-    p.ldg = p.piece;
-    p.cut_h = cut_reduction((int64_t)p.tiles_m * p.tiles_d, (int)((std::min<int64_t>(p.piece, V) + CT_K - 1) / CT_K));
-    p.cut_w = cut_reduction((int64_t)((p.piece + CT_M - 1) / CT_M) * p.tiles_d, (int)((N + CT_K - 1) / CT_K));
-    p.h_parts = p.cut_h.splits > 1 || p.npieces > 1;
-    p.w_parts = p.cut_w.splits > 1;
+    p.ldg = (int64_t)p.tiles_v * p.width_v;
+    const int64_t per_logit = !p.grads ? 1 : p.save == kSaveCode ? 2 : 4 + 2 * p.parts;
+    const int64_t most = std::min<int64_t>(1 << 20, std::max<int64_t>(CT_M, kBlockBytes / (per_logit * p.ldg) / CT_M * CT_M));
+    p.nblocks = (int)((N + most - 1) / most);
+    p.block = std::min(N, round_up((N + p.nblocks - 1) / p.nblocks, CT_M));
+    p.nblocks = (int)((N + p.block - 1) / p.block);
     int64_t at = 0;
     const auto room = [&](int64_t bytes) { const int64_t o = at; at += round_up(bytes, 256); return o; };
     p.o_scal = room(256);
     p.o_hp = room(2 * p.parts * N * p.ldp);
     p.o_wp = p.pack_w ? room(2 * p.parts * (int64_t)V * p.ldp) : 0;
-    p.o_targets = room(8 * N * std::max(1, p.ntargets));
+    p.o_targets = room(8 * N * p.ntargets);
     p.o_rowk = room(16 * N);
-    p.o_rowc = room(16 * N);
-    p.o_stats = room(16 * N * 2 * p.tiles_v);
-    p.o_shares = room((int64_t)sizeof(LossShare) * ((N + kFinishRows - 1) / kFinishRows));
+    p.o_rshares = room((int64_t)sizeof(RowShare) * N);
+    p.o_lshares = room((int64_t)sizeof(double) * ((N + kFinishRows - 1) / kFinishRows));
+    p.o_stats = room(16 * p.block * 2 * p.tiles_v);
     if (p.grads) {
-        p.o_g = room(2 * p.parts * N * p.ldg);
-        if (a.db) p.o_colsum = room(4 * 8 * (int64_t)p.tiles_m * p.ldg);
-        if (a.dH && p.h_parts) p.o_dh = room(4 * p.cut_h.splits * N * D);
-        if (a.dW && p.w_parts) p.o_dw = room(4 * p.cut_w.splits * std::min<int64_t>(p.piece, V) * D);
+        p.o_rowc = room(16 * p.block);
+        p.o_z = room((p.save == kSaveCode ? 2 : 4) * p.block * p.ldg);
+        p.o_g = p.save == kSaveCode ? p.o_z : room(2 * p.parts * p.block * p.ldg);
+        if (a.db) { p.o_colsum = room(4 * ((p.block + 31) / 32) * p.ldg); p.o_dbsum = room(4 * (int64_t)V); }
+        if (a.dH || a.dW) p.o_slots = room((int64_t)kPairs * CT_M * p.width_d * 4);
+        if (a.dW && p.nblocks > 1) p.o_sums = room(4 * (int64_t)V * D);
     }
     p.total = at;
     return p;
 }
 
-// Ring stages (64 terms each) of a chunk: 64 additions to an accumulator, about 3e-7 of its value.
-constexpr int kChunk = 16;
+// Ring stages (64 terms each) of a chunk: 64 additions to an accumulator, about 3e-7 of its value; for fp32 operands half of that.
+constexpr int kChunk = 16, kChunkParts = 8;
 
 template <int USE, bool A_MN, bool B_MN, class T, int NL, bool ADD_UP>
 cudaError_t gemm_launch(const CUtensorMap& A, const CUtensorMap& B, const TileArgs& a, cudaStream_t s) {
@@ -447,128 +564,132 @@ cudaError_t gemm_launch(const CUtensorMap& A, const CUtensorMap& B, const TileAr
     cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), CT_SMEM, false);
     if (e != cudaSuccess) return e;
     static std::atomic<int> known{0};
-    if (known.load() <= 0) known.store(max_active_pairs(reinterpret_cast<const void*>(kernel), CT_THREADS, CT_SMEM, 148));
-    const int64_t units = (int64_t)a.tiles_m * a.tiles_n * a.splits;
+    if (known.load() <= 0) known.store(max_active_pairs(reinterpret_cast<const void*>(kernel), CT_THREADS, CT_SMEM, 2 * kPairs));
+    const int64_t units = a.whole + ((int64_t)a.tiles_m * a.tiles_n - a.whole) * a.shares;
     const int ncl = (int)std::min<int64_t>(units, known.load());
     return chain(kernel, dim3((unsigned)(2 * ncl)), CT_THREADS, CT_SMEM, s, false, A, B, a);
 }
-// What is wanted to fp32 accuracy and longer than a chunk is added up in chunks: everything of fp32 operands, and the logits of the loss.
-template <int USE, bool A_MN, bool B_MN, class T, int NL>
-cudaError_t gemm_go(const CUtensorMap& A, const CUtensorMap& B, TileArgs a, cudaStream_t s) {
-    a.chunk = kChunk;
-    const bool exact = (a.pairs > 1 || USE == kStats) && a.kb_split * a.pairs > kChunk;
-    if constexpr (USE == kStats || USE == kPartial || sizeof(T) == 4)
-        if (exact) return gemm_launch<USE, A_MN, B_MN, T, NL, true>(A, B, a, s);
-    if constexpr (!(USE == kGrad && sizeof(T) == 4)) return gemm_launch<USE, A_MN, B_MN, T, NL, false>(A, B, a, s);
-    else return gemm_launch<USE, A_MN, B_MN, T, NL, true>(A, B, a, s);   // (of one chunk)
+// The statistics of a block of rows.  Logits longer than a chunk are added up in chunks.
+template <int NL>
+cudaError_t go_stats(const CUtensorMap& A, const CUtensorMap& B, const TileArgs& a, cudaStream_t s) {
+    return a.nkb * a.pairs > a.chunk ? gemm_launch<kStats, false, false, float, NL, true>(A, B, a, s) : gemm_launch<kStats, false, false, float, NL, false>(A, B, a, s);
+}
+// A gradient.  Tiles that are left over when all pairs have had the same number are cut along their reduction, so that they keep every pair busy too
+// (4096 x 1024 over 47 classes: 4 tiles, 18 shares each), down to 8 ring stages a share.  Sums for an fp32 result are added up in chunks.
+template <bool A_MN, class T>
+cudaError_t go_out(const CUtensorMap& A, const CUtensorMap& B, TileArgs a, cudaStream_t s) {
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, rest = tiles % kPairs;
+    a.whole = (int)tiles; a.shares = 1; a.kb_share = a.nkb;
+    if (rest) {
+        const int want = (int)std::min<int64_t>(kPairs / rest, (int64_t)a.nkb * a.pairs / 8);
+        if (want > 1) {
+            a.kb_share = (a.nkb + want - 1) / want;
+            a.shares = (a.nkb + a.kb_share - 1) / a.kb_share;
+            a.whole = (int)(tiles - rest);
+        }
+    }
+    cudaError_t e = gemm_launch<kOut, A_MN, true, T, 1, sizeof(T) == 4>(A, B, a, s);
+    if (e == cudaSuccess && a.shares > 1) e = chain(class_join_kernel<T>, dim3((unsigned)(rest * (CT_M / 32))), 256, 0, s, false, a);
+    return e;
 }
 
 template <class T>
-int run_class(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) {
+cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) {
+#define GAD_TRY(x) do { const cudaError_t e_ = (x); if (e_ != cudaSuccess) return e_; } while (0)
     const ClassPlan p = plan_class(a);
-    const int N = (int)a.rows, D = a.cols, V = a.classes;
+    const int64_t N = a.rows;
+    const int D = a.cols, V = a.classes;
     float* scal = reinterpret_cast<float*>(ws + p.o_scal);
     float4* rowk = reinterpret_cast<float4*>(ws + p.o_rowk);
     float4* rowc = p.grads ? reinterpret_cast<float4*>(ws + p.o_rowc) : nullptr;
     float4* stats = reinterpret_cast<float4*>(ws + p.o_stats);
     int2* targets = reinterpret_cast<int2*>(ws + p.o_targets);
     uint8_t* Hp = ws + p.o_hp;
-    uint8_t* G = ws + p.o_g;
     const float T0 = a.k > 0 ? a.temperature : 1.f;
 
     RowArgs ra{};
     ra.H = a.H; ra.ldh = a.ldh; ra.cols = D; ra.classes = V; ra.labels = a.labels; ra.label_bytes = a.label_bytes;
     ra.tclasses = a.target_classes; ra.tclass_bytes = a.target_bytes; ra.teacher = a.teacher; ra.teacher_type = a.teacher_dtype; ra.k = a.k;
     ra.weights = a.row_weights; ra.hard = a.k > 0 ? (a.labels ? a.hard_weight : 0.f) : 1.f; ra.temperature = T0;
-    ra.Hp = Hp; ra.ldp = p.ldp; ra.part_stride = (int64_t)N * p.ldp; ra.targets = targets; ra.ntargets = p.ntargets; ra.rowk = rowk; ra.status = a.status;
-    ra.rows = N; ra.ticket = reinterpret_cast<unsigned*>(scal + 2);
-    cudaError_t e = a.k > 0 ? chain(class_rows_kernel<T>, dim3((unsigned)N), kRowThreads, 8 * (size_t)p.ntargets, s, true, ra)
-                            : chain(class_label_rows_kernel<T>, dim3((unsigned)((N + 7) / 8)), 256, 0, s, true, ra);
-    if (e != cudaSuccess) return GAD_ERR_CUDA;
+    ra.Hp = Hp; ra.ldp = p.ldp; ra.part_stride = N * p.ldp; ra.targets = targets; ra.ntargets = p.ntargets; ra.rowk = rowk;
+    ra.rows = N; ra.shares = reinterpret_cast<RowShare*>(ws + p.o_rshares); ra.ticket = reinterpret_cast<unsigned*>(scal + 8); ra.status = a.status;
+    const int nrshares = (int)(a.k > 0 ? N : (N + 7) / 8);
+    GAD_TRY(a.k > 0 ? chain(class_rows_kernel<T>, dim3((unsigned)N), kRowThreads, 8 * (size_t)p.ntargets, s, true, ra)
+                    : chain(class_label_rows_kernel<T>, dim3((unsigned)nrshares), 256, 0, s, true, ra));
     const void* Wo = a.W;
     int64_t ldw = a.ldw;
     if (p.pack_w) {
-        if (chain(class_pack_kernel<T>, dim3((unsigned)((V + 7) / 8)), 256, 0, s, false, (const T*)a.W, a.ldw, V, D, (void*)(ws + p.o_wp), p.ldp, (int64_t)V * p.ldp) != cudaSuccess)
-            return GAD_ERR_CUDA;
+        GAD_TRY(chain(class_pack_kernel<T>, dim3((unsigned)((V + 7) / 8)), 256, 0, s, false, (const T*)a.W, a.ldw, V, D, (void*)(ws + p.o_wp), p.ldp, (int64_t)V * p.ldp));
         Wo = ws + p.o_wp;
         ldw = p.ldp;
     }
-
     CUtensorMap mapH, mapW, mapH_mn, mapW_mn, mapG, mapG_mn;
-    const auto make = [&](CUtensorMap& m, const void* base, int64_t inner, int64_t rows, int64_t ld, uint32_t box) {
-        return tc_make_map(&m, base, (uint64_t)inner, (uint64_t)rows, (uint64_t)p.parts, (uint64_t)ld * 2, (uint64_t)(ld * 2 * rows), box, false, true);
+    const auto make = [&](CUtensorMap& m, const void* base, int64_t inner, int64_t rows, int64_t ld, int64_t part_rows, uint32_t box) {
+        return tc_make_map(&m, base, (uint64_t)inner, (uint64_t)rows, (uint64_t)p.parts, (uint64_t)ld * 2, (uint64_t)(ld * 2 * part_rows), box, false, true) ? cudaSuccess : cudaErrorInvalidValue;
     };
-    if (!make(mapH, Hp, D, N, p.ldp, CT_H) || !make(mapW, Wo, D, V, ldw, (uint32_t)p.width_v / 2)) return GAD_ERR_CUDA;
-
-    TileArgs t{};
-    t.err = a.status; t.bf16 = a.dtype != GAD_F16; t.pairs = p.pairs;
-    t.M = N; t.N = V; t.tiles_m = p.tiles_m; t.tiles_n = p.tiles_v; t.width = p.width_v;
-    t.nkb = (D + CT_K - 1) / CT_K; t.splits = 1; t.kb_split = t.nkb; t.group = 32;
-    t.bias = a.bias; t.bias_type = a.dtype; t.classes = V;
-    t.sc = kLog2e * (p.nl == 1 && a.k > 0 && ra.hard < 1.f ? 1.f / T0 : 1.f);
-    t.inv_t = 1.f / T0;
-    t.targets = targets; t.ntargets = p.ntargets; t.stats = stats; t.rowk = rowk; t.rowc = rowc; t.scal = scal;
-    e = p.nl == 2 ? gemm_go<kStats, false, false, float, 2>(mapH, mapW, t, s) : gemm_go<kStats, false, false, float, 1>(mapH, mapW, t, s);
-    if (e != cudaSuccess) return GAD_ERR_CUDA;
-    e = chain(p.nl == 2 ? class_finish_kernel<2> : class_finish_kernel<1>, dim3((unsigned)((N + kFinishRows - 1) / kFinishRows)), 256, 0, s, false, (const float4*)stats, 2 * p.tiles_v, N,
-              (const float4*)rowk, t.sc, t.inv_t, T0, rowc, a.row_loss, reinterpret_cast<LossShare*>(ws + p.o_shares), ra.ticket, a.scale, (int)a.mean, scal, a.loss);
-    if (e != cudaSuccess) return GAD_ERR_CUDA;
-    if (!p.grads) return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
-
-    if (!make(mapH_mn, Hp, D, N, p.ldp, CT_K) || !make(mapW_mn, Wo, D, V, ldw, CT_K)) return GAD_ERR_CUDA;
-    float* dh_part = reinterpret_cast<float*>(ws + p.o_dh);
-    float* dw_part = reinterpret_cast<float*>(ws + p.o_dw);
-    for (int i = 0; i < p.npieces; ++i) {
-        const int v0 = (int)(i * p.piece), nv = (int)std::min<int64_t>(p.piece, V - v0);
-        TileArgs g = t;
-        g.N = nv; g.tiles_n = (nv + p.width_v - 1) / p.width_v; g.col0 = v0; g.b_row0 = v0;
-        g.C = G; g.ldc = p.ldg; g.part_stride = (int64_t)N * p.ldg;
-        g.colsum = a.db ? reinterpret_cast<float*>(ws + p.o_colsum) : nullptr;
-        e = p.nl == 2 ? gemm_go<kGrad, false, false, T, 2>(mapH, mapW, g, s) : gemm_go<kGrad, false, false, T, 1>(mapH, mapW, g, s);
-        if (e != cudaSuccess) return GAD_ERR_CUDA;
-        const auto makeg = [&](CUtensorMap& m, uint32_t box) {
-            return tc_make_map(&m, G, (uint64_t)nv, (uint64_t)N, (uint64_t)p.parts, (uint64_t)p.ldg * 2, (uint64_t)(p.ldg * 2 * (int64_t)N), box, false, true);
-        };
-        if (!makeg(mapG, CT_H) || !makeg(mapG_mn, CT_K)) return GAD_ERR_CUDA;
+    GAD_TRY(make(mapH, Hp, D, N, p.ldp, N, CT_H));
+    GAD_TRY(make(mapW, Wo, D, V, ldw, V, (uint32_t)p.width_v / 2));
+    if (p.grads) {
+        GAD_TRY(make(mapH_mn, Hp, D, N, p.ldp, N, CT_K));
+        GAD_TRY(make(mapW_mn, Wo, D, V, ldw, V, CT_K));
+    }
+    for (int b = 0; b < p.nblocks; ++b) {
+        const int64_t r0 = b * p.block;
+        const int nr = (int)std::min(p.block, N - r0), blocks = (nr + kFinishRows - 1) / kFinishRows;
+        TileArgs t{};
+        t.err = a.status; t.bf16 = a.dtype != GAD_F16; t.pairs = p.pairs; t.chunk = p.parts > 1 ? kChunkParts : kChunk; t.scal = scal;
+        t.M = nr; t.tiles_m = (nr + CT_M - 1) / CT_M;
+        TileArgs z = t;
+        z.N = V; z.tiles_n = p.tiles_v; z.width = p.width_v; z.nkb = (D + CT_K - 1) / CT_K; z.whole = z.tiles_m * z.tiles_n; z.shares = 1; z.kb_share = z.nkb;
+        z.group = 32; z.a_row0 = (int)r0;
+        z.bias = a.bias; z.bias_type = a.dtype;
+        z.sc = kLog2e * (p.nl == 1 && a.k > 0 && ra.hard < 1.f ? 1.f / T0 : 1.f);
+        z.inv_t = 1.f / T0;
+        z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.stats = stats;
+        z.save = p.save; z.C = ws + p.o_z; z.ldc = p.ldg;
+        GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, s) : go_stats<1>(mapH, mapW, z, s));
+        FinishArgs f{};
+        f.stats = stats; f.parts = 2 * p.tiles_v; f.rows = nr; f.rowk = rowk + r0; f.sc = z.sc; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
+        f.shares = reinterpret_cast<double*>(ws + p.o_lshares); f.share0 = (int)(r0 / kFinishRows); f.nshares = (int)((N + kFinishRows - 1) / kFinishRows);
+        f.row_shares = ra.shares; f.nrow_shares = nrshares; f.ticket = ra.ticket; f.scale = a.scale; f.mean = a.mean; f.first = b == 0; f.final = b == p.nblocks - 1;
+        f.scal = scal; f.loss = a.loss;
+        GAD_TRY(chain(p.nl == 2 ? class_finish_kernel<2> : class_finish_kernel<1>, dim3((unsigned)blocks), 256, 0, s, false, f));
+        if (!p.grads) continue;
+        GradArgs g{};
+        g.z = z.C; g.ldz = p.ldg; g.G = ws + p.o_g; g.ldg = p.ldg; g.part_stride = nr * p.ldg; g.stats = stats; g.half_w = p.width_v / 2;
+        g.rowc = rowc; g.rowk = rowk + r0; g.targets = z.targets; g.ntargets = p.ntargets; g.scal = scal; g.inv_t = z.inv_t;
+        g.colsum = a.db ? reinterpret_cast<float*>(ws + p.o_colsum) : nullptr; g.rows = nr; g.classes = V;
+        auto grad = p.nl == 2 ? class_grad_kernel<T, float, 2> : class_grad_kernel<T, float, 1>;
+        if constexpr (sizeof(T) == 2)
+            if (p.save == kSaveCode) grad = p.nl == 2 ? class_grad_kernel<T, uint16_t, 2> : class_grad_kernel<T, uint16_t, 1>;
+        const int slices = (nr + 31) / 32;
+        GAD_TRY(chain(grad, dim3((unsigned)((p.ldg + 255) / 256), (unsigned)slices), 256, 0, s, false, g));
+        const int add = p.nblocks == 1 ? kAddNone : b == 0 ? kAddFirst : b < p.nblocks - 1 ? kAddMore : kAddLast;
+        if (a.db)
+            GAD_TRY(chain(class_bias_kernel<T>, dim3((unsigned)((V + 31) / 32)), 256, 0, s, false, (const float*)g.colsum, p.ldg, slices, V, (const float*)scal, add,
+                          reinterpret_cast<float*>(ws + p.o_dbsum), reinterpret_cast<T*>(a.db)));
+        t.slots = reinterpret_cast<float*>(ws + p.o_slots);
+        t.N = D; t.tiles_n = p.tiles_d; t.width = p.width_d; t.group = 8;
         if (a.dH) {
             TileArgs h = t;
-            h.M = N; h.N = D; h.tiles_m = p.tiles_m; h.tiles_n = p.tiles_d; h.width = p.width_d; h.group = 8;
-            h.nkb = (nv + CT_K - 1) / CT_K;
-            h.kb_split = std::min(p.cut_h.kb, h.nkb); h.splits = (h.nkb + h.kb_split - 1) / h.kb_split;
-            h.b_row0 = v0;
-            if (p.h_parts) {
-                h.C = dh_part; h.ldc = D; h.part_stride = (int64_t)N * D; h.accumulate = i > 0;
-                e = gemm_go<kPartial, false, true, float, 1>(mapG, mapW_mn, h, s);
-            } else {
-                h.C = a.dH; h.ldc = a.lddh;
-                e = gemm_go<kOut, false, true, T, 1>(mapG, mapW_mn, h, s);
-            }
-            if (e != cudaSuccess) return GAD_ERR_CUDA;
+            GAD_TRY(make(mapG, g.G, V, nr, p.ldg, nr, CT_H));
+            h.nkb = (V + CT_K - 1) / CT_K;
+            h.C = reinterpret_cast<T*>(a.dH) + r0 * a.lddh; h.ldc = a.lddh;
+            GAD_TRY((go_out<false, T>(mapG, mapW_mn, h, s)));
         }
         if (a.dW) {
             TileArgs w = t;
-            w.M = nv; w.N = D; w.tiles_m = (nv + CT_M - 1) / CT_M; w.tiles_n = p.tiles_d; w.width = p.width_d; w.group = 8;
-            w.nkb = (N + CT_K - 1) / CT_K; w.kb_split = p.cut_w.kb; w.splits = p.cut_w.splits; w.b_row0 = 0;
-            T* out = reinterpret_cast<T*>(a.dW) + (int64_t)v0 * a.lddw;
-            if (p.w_parts) {
-                w.C = dw_part; w.ldc = D; w.part_stride = (int64_t)nv * D;
-                e = gemm_go<kPartial, true, true, float, 1>(mapG_mn, mapH_mn, w, s);
-                if (e != cudaSuccess) return GAD_ERR_CUDA;
-                if (join_parts<T>(dw_part, w.splits, w.part_stride, nv, D, scal, out, a.lddw, s) != cudaSuccess) return GAD_ERR_CUDA;
-            } else {
-                w.C = out; w.ldc = a.lddw;
-                e = gemm_go<kOut, true, true, T, 1>(mapG_mn, mapH_mn, w, s);
-                if (e != cudaSuccess) return GAD_ERR_CUDA;
-            }
-        }
-        if (a.db) {
-            e = chain(class_bias_kernel<T>, dim3((unsigned)((nv + 31) / 32)), 256, 0, s, false, (const float*)g.colsum, p.ldg, 8 * p.tiles_m, nv, (const float*)scal, reinterpret_cast<T*>(a.db) + v0);
-            if (e != cudaSuccess) return GAD_ERR_CUDA;
+            GAD_TRY(make(mapG_mn, g.G, V, nr, p.ldg, nr, CT_K));
+            w.M = V; w.tiles_m = (V + CT_M - 1) / CT_M; w.nkb = (nr + CT_K - 1) / CT_K; w.b_row0 = (int)r0;
+            w.C = a.dW; w.ldc = a.lddw; w.add = add; w.sums = reinterpret_cast<float*>(ws + p.o_sums);
+            GAD_TRY((go_out<true, T>(mapG_mn, mapH_mn, w, s)));
         }
     }
-    if (a.dH && p.h_parts && join_parts<T>(dh_part, p.cut_h.splits, (int64_t)N * D, N, D, scal, reinterpret_cast<T*>(a.dH), a.lddh, s) != cudaSuccess) return GAD_ERR_CUDA;
-    return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
+    return cudaGetLastError();
+#undef GAD_TRY
 }
+template <class T>
+int run_class(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) { return run_class_steps<T>(a, ws, s) == cudaSuccess ? GAD_OK : GAD_ERR_CUDA; }
 
 // No rows: no loss, and gradients of zero.
 template <class T>
@@ -583,7 +704,7 @@ int run_empty(const gad_class_loss_args& a, cudaStream_t s) {
 int check_class(const gad_class_loss_args* a) {
     if (!a) return GAD_ERR_ARG;
     if (a->dtype < GAD_F32 || a->dtype > GAD_BF16 || a->rows < 0 || a->cols < 1 || a->classes < 1) return GAD_ERR_ARG;
-    if (a->rows > (1 << 30) || a->cols > (1 << 20) || a->classes > (1 << 30)) return GAD_ERR_RANGE;
+    if (a->rows > (1 << 30) || a->cols > (1 << 20) || a->classes > (1 << 24)) return GAD_ERR_RANGE;
     if (a->k < 0) return GAD_ERR_ARG;
     if (a->k > kMostTargets) return GAD_ERR_RANGE;
     if (a->ldw < a->cols || (a->rows > 0 && a->ldh != 0 && a->ldh < a->cols) || (a->dH && a->lddh < a->cols) || (a->dW && a->lddw < a->cols)) return GAD_ERR_ARG;
