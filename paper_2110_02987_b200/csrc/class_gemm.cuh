@@ -97,6 +97,27 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
 }
 
+// The same in two steps, so that a block of columns is on its way while the one in front is worked on.
+__device__ __forceinline__ void tmem_ld32_start(uint32_t addr, float (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
+        "%23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+          "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]),
+          "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        : "r"(addr)
+        : "memory");
+}
+// (the values pass through, so that nothing reads them before)
+__device__ __forceinline__ void tmem_ld32_wait(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]),
+          "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
+          "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+        :
+        : "memory");
+}
+
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -383,27 +404,52 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     if (e < a.ntargets) next = tg[e].x;
                 }
             }
+            // No bias, nothing but classes, and codes or nothing kept: the logit and its distance from the largest are one multiply-add.
+            const bool plain = !a.bias && (t.n + 1) * a.width <= a.N && a.save != kSaveFloat;
+            const auto largest = [&](int c0, const float (&v)[32]) {
+                float m[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) m[k] = plain ? v[k] : fmaf(v[k], a.sc, bias[c0 + k]);
+                if (plain) {
+#pragma unroll
+                    for (int j = 4; j < 32; ++j) m[j & 3] = fmaxf(m[j & 3], v[j]);
+                } else {
+#pragma unroll
+                    for (int j = 4; j < 32; ++j) m[j & 3] = fmaxf(m[j & 3], fmaf(v[j], a.sc, bias[c0 + j]));
+                }
+                m2 = fmaxf(m2, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+            };
             // 32 finished values of this thread's row, from column c0 of the warp's columns on
             const auto take = [&](int c0, float (&v)[32]) {
                 if (USE == kStats) {
                     const float base = m2 == -INFINITY ? 0.f : m2;          // nothing but masked classes: all terms are zero
+                    if (plain) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], a.sc, -base);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], a.sc, bias[c0 + j]);
+                        if (a.save == kSaveFloat) drain_rows<float>(buf, lane, v, reinterpret_cast<float*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, 32, 16);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] -= base;
+                    }
+                    float p1[4] = {0.f, 0.f, 0.f, 0.f}, p2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        v[j] = fmaf(v[j], a.sc, bias[c0 + j]);
-                        s1 += exp2_fast(v[j] - base);
-                        if (NL == 2) s2 += exp2_fast((v[j] - base) * a.inv_t);
+                        p1[j & 3] += exp2_fast(v[j]);
+                        if (NL == 2) p2[j & 3] += exp2_fast(v[j] * a.inv_t);
                     }
+                    s1 += (p1[0] + p1[1]) + (p1[2] + p1[3]);
+                    if (NL == 2) s2 += (p2[0] + p2[1]) + (p2[2] + p2[3]);
                     while (next < tile_c + c0 + 32) {
-                        dot = fmaf(__int_as_float(tg[e].y), pick(v, next - tile_c - c0), dot);
+                        dot = fmaf(__int_as_float(tg[e].y), pick(v, next - tile_c - c0) + base, dot);
                         next = ++e < a.ntargets ? tg[e].x : INT_MAX;
                     }
                     if (a.save == kSaveCode) {
                         // rounded by the addition of 2^23, whose sum has the whole number in its low bits
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fminf(base - v[j], (float)kCodeZero / kCodeSteps) * kCodeSteps + 8388608.f;
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(fmaxf(v[j], -(float)kCodeZero / kCodeSteps), -kCodeSteps, 8388608.f);
                         drain_codes(buf, lane, v, reinterpret_cast<uint16_t*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows);
-                    } else if (a.save == kSaveFloat) {
-                        drain_rows<float>(buf, lane, v, reinterpret_cast<float*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, 32, 16);
                     }
                 } else if (tile_c + c0 < a.N) {
                     const int cols = a.N - tile_c - c0;
@@ -477,19 +523,38 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     tmem_wait_st();
                 } else if (!wait_full()) break;
             } else if (!wait_full()) break;
-            if (USE == kStats)                                              // the largest first, then everything relative to it
+            if constexpr (USE == kStats) {
+                // the largest first, then everything relative to it; two blocks of columns in turn (half_w is 64 or 128)
+                const uint32_t at = tm_row + (uint32_t)(acc * 256);
+                float u[32], v[32];
+                __syncwarp();
+                tmem_ld32_start(at, u);
+                for (int c0 = 0; c0 < half_w; c0 += 64) {
+                    tmem_ld32_wait(u);
+                    tmem_ld32_start(at + c0 + 32, v);
+                    largest(c0, u);
+                    tmem_ld32_wait(v);
+                    tmem_ld32_start(at + (c0 + 64 < half_w ? c0 + 64 : 0), u);
+                    largest(c0 + 32, v);
+                }
+                if (plain) m2 *= a.sc;
+                for (int c0 = 0; c0 < half_w; c0 += 64) {
+                    tmem_ld32_wait(u);
+                    tmem_ld32_start(at + c0 + 32, v);
+                    take(c0, u);
+                    __syncwarp();
+                    tmem_ld32_wait(v);
+                    if (c0 + 64 < half_w) tmem_ld32_start(at + c0 + 64, u);
+                    take(c0 + 32, v);
+                    __syncwarp();
+                }
+            } else {
                 for (int c0 = 0; c0 < half_w; c0 += 32) {
                     float v[32];
                     __syncwarp();
                     tmem_ld32(tm_row + (uint32_t)(acc * 256 + c0), v);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) m2 = fmaxf(m2, fmaf(v[j], a.sc, bias[c0 + j]));
+                    take(c0, v);
                 }
-            for (int c0 = 0; c0 < half_w; c0 += 32) {
-                float v[32];
-                __syncwarp();
-                tmem_ld32(tm_row + (uint32_t)(acc * 256 + c0), v);
-                take(c0, v);
             }
             release();
             if (USE == kStats && rv) a.stats[(long long)(2 * t.n + half) * a.M + row] = make_float4(m2, s1, s2, dot);

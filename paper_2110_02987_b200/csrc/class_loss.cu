@@ -352,46 +352,64 @@ __global__ void __launch_bounds__(256) class_grad_kernel(const GradArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[j] = 0.f;
     const bool in = c < a.ldg;                // (rows of G are whole tiles of 128 classes)
+    constexpr int LOADS = sizeof(Z) / 2, ROWS = 4;
+    uint4 q[ROWS][LOADS];                     // all loads of a warp's rows first
+    float4 rc[ROWS];
+    float m[ROWS], fw[ROWS];
+    int2 tg[ROWS];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
+        const int r = min((int)blockIdx.y * 32 + 8 * i + w, a.rows - 1);
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k)
+            q[i][k] = in ? reinterpret_cast<const uint4*>(reinterpret_cast<const Z*>(a.z) + (long long)r * a.ldz + c)[k] : make_uint4(0u, 0u, 0u, 0u);
+        m[i] = sizeof(Z) == 2 && in ? a.stats[(long long)(c / a.half_w) * a.rows + r].x : 0.f;
+        rc[i] = a.rowc[r];
+        fw[i] = a.rowk[r].w;
+        tg[i] = lane < a.ntargets ? a.targets[(long long)r * a.ntargets + lane] : make_int2(INT_MAX, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
         const int r = blockIdx.y * 32 + 8 * i + w;
         if (r >= a.rows) break;
-        const float4 rc = a.rowc[r];
-        const float fw = a.rowk[r].w * gs;
+        const float f = fw[i] * gs;
         // a sum that is not finite makes the whole row not a number, also where the code says zero; a row without weight is zero whatever it holds
-        const float fa = fw == 0.f ? 0.f : fw * rc.x + 0.f * rc.z, fb = fw == 0.f ? 0.f : fw * rc.y;
+        const float fa = f == 0.f ? 0.f : f * rc[i].x + 0.f * rc[i].z, fb = f == 0.f ? 0.f : f * rc[i].y;
         float v[8];
-        if (in) {
-            float z[8];                       // log2 of exp(z) relative to the first sum
+        {
+            float z[8];                       // log2 of exp(z), as the first sum is
             if constexpr (sizeof(Z) == 2) {
-                union { uint4 u; uint16_t h[8]; } q;
-                q.u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.z) + (long long)r * a.ldz + c);
-                const float m = a.stats[(long long)(c / a.half_w) * a.rows + r].x;
+                const uint32_t h[4] = {q[i][0].x, q[i][0].y, q[i][0].z, q[i][0].w};
 #pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] = q.h[j] == kCodeZero ? -INFINITY : fmaf((float)q.h[j], -1.f / kCodeSteps, m);
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t code = j & 1 ? h[j >> 1] >> 16 : h[j >> 1] & 0xFFFFu;
+                    z[j] = code == (uint32_t)kCodeZero ? -INFINITY : fmaf((float)code, -1.f / kCodeSteps, m[i]);
+                }
             } else {
-                const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.z) + (long long)r * a.ldz + c);
-                const float4 x = p[0], y = p[1];
-                z[0] = x.x; z[1] = x.y; z[2] = x.z; z[3] = x.w; z[4] = y.x; z[5] = y.y; z[6] = y.z; z[7] = y.w;
+#pragma unroll
+                for (int k = 0; k < LOADS; ++k) {
+                    z[4 * k] = __uint_as_float(q[i][k].x); z[4 * k + 1] = __uint_as_float(q[i][k].y); z[4 * k + 2] = __uint_as_float(q[i][k].z); z[4 * k + 3] = __uint_as_float(q[i][k].w);
+                }
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[j] = fw == 0.f ? 0.f : fa * exp2_fast(z[j] - rc.z);
-                if (NL == 2) v[j] += fw == 0.f ? 0.f : fb * exp2_fast(fmaf(z[j], a.inv_t, -rc.w));
+                v[j] = f == 0.f ? 0.f : fa * exp2_fast(z[j] - rc[i].z);
+                if (NL == 2) v[j] += f == 0.f ? 0.f : fb * exp2_fast(fmaf(z[j], a.inv_t, -rc[i].w));
             }
         }
-        const int2* tg = a.targets + (long long)r * a.ntargets;
-        int e = 0, hi = a.ntargets;
-        while (e < hi) {
-            const int mid = (e + hi) >> 1;
-            if (tg[mid].x < c0) e = mid + 1; else hi = mid;
-        }
-        for (; e < a.ntargets; ++e) {
-            const int2 t = tg[e];
-            if (t.x >= c0 + 256) break;
-            const float x = fw * __int_as_float(t.y);
+        // the row's targets among these 256 classes: 32 of the list at a time (it is ascending)
+        int2 t = tg[i];
+        for (int at = 0;;) {
+            for (uint32_t hit = __ballot_sync(0xffffffffu, t.x >= c0 && t.x < c0 + 256); hit; hit &= hit - 1) {
+                const int src = __ffs(hit) - 1, x = __shfl_sync(0xffffffffu, t.x, src);
+                const float d = f * __int_as_float(__shfl_sync(0xffffffffu, t.y, src));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] -= t.x == c + j ? x : 0.f;
+                for (int j = 0; j < 8; ++j) v[j] -= x == c + j ? d : 0.f;
+            }
+            if (__shfl_sync(0xffffffffu, t.x, 31) >= c0 + 256) break;
+            at += 32;
+            if (at >= a.ntargets) break;
+            t = at + lane < a.ntargets ? a.targets[(long long)r * a.ntargets + at + lane] : make_int2(INT_MAX, 0);
         }
         if (!in) continue;
 #pragma unroll
@@ -425,25 +443,33 @@ __global__ void __launch_bounds__(256) class_grad_kernel(const GradArgs a) {
     a.colsum[(long long)blockIdx.y * a.ldg + x] = s;
 }
 
-// The shares of the tiles that were cut along their reduction, added up in order, and put where an uncut tile would have gone.  A block has 32 rows of a tile.
+// The shares of the tiles that were cut along their reduction, added up in order, and put where an uncut tile would have gone: four columns a thread, four (eight)
+// rows of a tile a block.
 template <class T>
 __global__ void __launch_bounds__(256) class_join_kernel(const TileArgs a) {
-    const int per_tile = CT_M / 32, i = blockIdx.x / per_tile, r0 = blockIdx.x % per_tile * 32;
+    const int per_row = a.width / 4, rows = 256 / per_row, per_tile = CT_M / rows;
+    const int i = blockIdx.x / per_tile, r = blockIdx.x % per_tile * rows + threadIdx.x / per_row, x = threadIdx.x % per_row * 4;
     pdl_next();
     pdl_wait();
     const TileAt t = tile_at(a, a.whole + (long long)i * a.shares);
+    const int row = t.m * CT_M + r, c = t.n * a.width + x;
+    if (row >= a.M || c >= a.N) return;
     const float factor = a.scal[1];
-    const float* slot = a.slots + (long long)i * a.shares * CT_M * a.width;
-    for (int j = threadIdx.x; j < 32 * a.width; j += 256) {
-        const int r = r0 + j / a.width, x = j % a.width, row = t.m * CT_M + r, c = t.n * a.width + x;
-        if (row >= a.M || c >= a.N) continue;
-        float s = 0.f;
-#pragma unroll 8
-        for (int k = 0; k < a.shares; ++k) s += slot[((long long)k * CT_M + r) * a.width + x];
-        float* sum = a.sums + (long long)row * a.N + c;
-        if (a.add == kAddMore || a.add == kAddLast) s += *sum;
-        if (a.add == kAddFirst || a.add == kAddMore) *sum = s;
-        else reinterpret_cast<T*>(a.C)[(long long)row * a.ldc + c] = from_float<T>(factor * s);
+    const float* slot = a.slots + ((long long)i * a.shares * CT_M + r) * a.width + x;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < a.shares; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(slot + (long long)k * CT_M * a.width);
+        s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+    }
+    float* sum = a.sums + (long long)row * a.N + c;
+    T* out = reinterpret_cast<T*>(a.C) + (long long)row * a.ldc + c;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (c + j >= a.N) break;
+        if (a.add == kAddMore || a.add == kAddLast) s[j] += sum[j];
+        if (a.add == kAddFirst || a.add == kAddMore) sum[j] = s[j];
+        else out[j] = from_float<T>(factor * s[j]);
     }
 }
 
@@ -589,7 +615,7 @@ cudaError_t go_out(const CUtensorMap& A, const CUtensorMap& B, TileArgs a, cudaS
         }
     }
     cudaError_t e = gemm_launch<kOut, A_MN, true, T, 1, sizeof(T) == 4>(A, B, a, s);
-    if (e == cudaSuccess && a.shares > 1) e = chain(class_join_kernel<T>, dim3((unsigned)(rest * (CT_M / 32))), 256, 0, s, false, a);
+    if (e == cudaSuccess && a.shares > 1) e = chain(class_join_kernel<T>, dim3((unsigned)(rest * (CT_M * a.width / 1024))), 256, 0, s, false, a);
     return e;
 }
 
