@@ -404,8 +404,8 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     if (e < a.ntargets) next = tg[e].x;
                 }
             }
-            // No bias, nothing but classes, and codes or nothing kept: the logit and its distance from the largest are one multiply-add.
-            const bool plain = !a.bias && (t.n + 1) * a.width <= a.N && a.save != kSaveFloat;
+            // No bias and nothing but classes: the logit and its distance from the largest are one multiply-add.
+            const bool plain = !a.bias && (t.n + 1) * a.width <= a.N;
             const auto largest = [&](int c0, const float (&v)[32]) {
                 float m[4];
 #pragma unroll
@@ -423,15 +423,18 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             const auto take = [&](int c0, float (&v)[32]) {
                 if (USE == kStats) {
                     const float base = m2 == -INFINITY ? 0.f : m2;          // nothing but masked classes: all terms are zero
+                    if (a.save == kSaveFloat) {
+                        float z[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] = plain ? v[j] * a.sc : fmaf(v[j], a.sc, bias[c0 + j]);
+                        drain_rows<float>(buf, lane, z, reinterpret_cast<float*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, 32, 16);
+                    }
                     if (plain) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], a.sc, -base);
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], a.sc, bias[c0 + j]);
-                        if (a.save == kSaveFloat) drain_rows<float>(buf, lane, v, reinterpret_cast<float*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows, 32, 16);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] -= base;
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], a.sc, bias[c0 + j]) - base;
                     }
                     float p1[4] = {0.f, 0.f, 0.f, 0.f}, p2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -497,33 +500,41 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             };
             if constexpr (ADD_UP) {
                 const int chunks = (t.nkb * a.pairs + a.chunk - 1) / a.chunk;
-                if (chunks > 1) {
-                    float sum[4][32];
+                float sum[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
+                for (int i = 0; i < chunks; ++i) {
+                    if (!wait_full()) break;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (32 * c >= half_w) break;
+                        float v[32];
+                        tmem_ld32(tm_row + (uint32_t)(acc * 256 + 32 * c), v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+                    }
+                    if (USE == kStats || i < chunks - 1) release();
+                }
+                if (!ok) break;
+                if constexpr (USE == kStats) {                              // from the registers: the tensor cores go on in both accumulators meanwhile
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
+                        if (32 * c < half_w) largest(32 * c, sum[c]);
+                    if (plain) m2 *= a.sc;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
-                    for (int i = 0; i < chunks; ++i) {
-                        if (!wait_full()) break;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            if (32 * c >= half_w) break;
-                            float v[32];
-                            tmem_ld32(tm_row + (uint32_t)(acc * 256 + 32 * c), v);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
-                        }
-                        if (i < chunks - 1) release();
-                    }
-                    if (!ok) break;
+                    for (int c = 0; c < 4; ++c)
+                        if (32 * c < half_w) take(32 * c, sum[c]);
+                } else {
                     // the sums take the place of the last chunk, and are taken from there block by block: held in registers beside what follows they would spill
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
                         if (32 * c < half_w) tmem_st_32x32b_x32(tm_row + (uint32_t)(acc * 256 + 32 * c), sum[c]);
                     tmem_wait_st();
-                } else if (!wait_full()) break;
+                }
             } else if (!wait_full()) break;
-            if constexpr (USE == kStats) {
+            if constexpr (USE == kStats && !ADD_UP) {
                 // the largest first, then everything relative to it; two blocks of columns in turn (half_w is 64 or 128)
                 const uint32_t at = tm_row + (uint32_t)(acc * 256);
                 float u[32], v[32];
@@ -548,15 +559,16 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     take(c0 + 32, v);
                     __syncwarp();
                 }
-            } else {
+                release();
+            } else if constexpr (USE == kOut) {
                 for (int c0 = 0; c0 < half_w; c0 += 32) {
                     float v[32];
                     __syncwarp();
                     tmem_ld32(tm_row + (uint32_t)(acc * 256 + c0), v);
                     take(c0, v);
                 }
+                release();
             }
-            release();
             if (USE == kStats && rv) a.stats[(long long)(2 * t.n + half) * a.M + row] = make_float4(m2, s1, s2, dot);
         }
     }

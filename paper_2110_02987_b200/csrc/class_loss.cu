@@ -207,6 +207,133 @@ __global__ void __launch_bounds__(256) class_pack_kernel(const T* __restrict__ W
     if (r < rows) pack_row<T>(W + r * ldw, cols, true, Wp, r * ldp, part_stride, threadIdx.x & 31, 32);
 }
 
+// Statistics of a few rows (up to 8: serving): reading W is all that costs, and a tile of 256 rows on the tensor cores mostly multiplies zeros (one row, 128 000 x 4096
+// bf16: 237 us at the card's power limit).  A warp takes four classes at a time, each lane every 32nd vector of their rows; the rows of H lie in shared memory in fp32.
+// The 4 NR sums over lanes are halved at each of the first exchanges, so that lane l ends up with sum l / (32 / (4 NR)), and keeps its own running softmax
+// over the classes it sees, in ascending order.
+constexpr int kFewRows = 8, kFewBlocks = 296, kFewSmem = 160 << 10;
+struct FewArgs {
+    const void* H; long long ldh;
+    const void* W; long long ldw;
+    int rows, cols, classes;
+    const void* bias;
+    const int2* targets; int ntargets;
+    const float4* rowk;
+    float sc, inv_t;
+    float* z; long long ldz;                  // or null
+    float4* stats;                            // [blocks x rows]
+};
+template <class T, int VEC>
+__device__ __forceinline__ void unpack(const uint4& u, float (&v)[VEC]) {
+    if constexpr (sizeof(T) == 4) {
+        v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
+    } else {
+        union { uint4 u; T e[8]; } w;
+        w.u = u;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[j] = to_float(w.e[j]);
+    }
+}
+template <class T, int NR, int NL, bool WIDE>
+__global__ void __launch_bounds__(256, 2) class_few_kernel(const FewArgs a) {
+    extern __shared__ float h[];              // [NR][cols, rounded up to a vector]
+    __shared__ float4 sm[8][32];
+    constexpr int VEC = WIDE ? 16 / sizeof(T) : 1, C = 4 * NR, LC = NR == 1 ? 2 : NR == 2 ? 3 : NR == 4 ? 4 : 5;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, ldv = (a.cols + VEC - 1) / VEC * VEC;
+    pdl_next();
+    pdl_wait();
+    for (int n = 0; n < NR; ++n) {
+        const float4 k = n < a.rows ? a.rowk[n] : make_float4(0.f, 0.f, 0.f, 0.f);
+        const bool counts = k.x > 0.f || k.y > 0.f;
+        for (int c = threadIdx.x; c < ldv; c += 256) h[n * ldv + c] = counts && c < a.cols ? to_float(reinterpret_cast<const T*>(a.H)[n * a.ldh + c]) : 0.f;
+    }
+    __syncthreads();
+    const int idx = lane >> (5 - LC), kc = idx / NR, row = idx % NR;   // this lane's class of the four, and row
+    const bool mine = (lane & ((1 << (5 - LC)) - 1)) == 0 && row < a.rows;
+    const int2* tg = a.targets + (long long)min(row, a.rows - 1) * a.ntargets;
+    float m = -INFINITY, s1 = 0.f, s2 = 0.f, dot = 0.f;
+    int e = 0;
+    const int whole = WIDE ? a.cols / VEC * VEC : a.cols, last = a.z ? (int)a.ldz : a.classes;
+    for (int c0 = (blockIdx.x * 8 + w) * 4; c0 < last; c0 += gridDim.x * 32) {
+        float acc[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) acc[i] = 0.f;
+        const T* wr[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) wr[k] = reinterpret_cast<const T*>(a.W) + (long long)min(c0 + k, a.classes - 1) * a.ldw;
+        if constexpr (WIDE) {
+#pragma unroll 2
+            for (int x = lane * VEC; x < whole; x += 32 * VEC) {
+                uint4 u[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) u[k] = __ldcs(reinterpret_cast<const uint4*>(wr[k] + x));
+                float v[4][VEC];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) unpack<T, VEC>(u[k], v[k]);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    float hv[VEC];
+#pragma unroll
+                    for (int j = 0; j < VEC; j += 4) {
+                        const float4 q = *reinterpret_cast<const float4*>(h + n * ldv + x + j);
+                        hv[j] = q.x; hv[j + 1] = q.y; hv[j + 2] = q.z; hv[j + 3] = q.w;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) acc[k * NR + n] = fmaf(v[k][j], hv[j], acc[k * NR + n]);
+                }
+            }
+        }
+        for (int x = (WIDE ? whole : 0) + lane; x < a.cols; x += 32)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float v = to_float(wr[k][x]);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) acc[k * NR + n] = fmaf(v, h[n * ldv + x], acc[k * NR + n]);
+            }
+#pragma unroll
+        for (int i = 0, n = C; i < 5; ++i) {
+            const int o = 16 >> i;
+            if (n > 1) {
+                n >>= 1;
+#pragma unroll
+                for (int j = 0; j < C / 2; ++j)
+                    if (j < n) {
+                        const float keep = (lane & o) ? acc[j + n] : acc[j], give = (lane & o) ? acc[j] : acc[j + n];
+                        acc[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                    }
+            } else acc[0] += __shfl_xor_sync(0xffffffffu, acc[0], o);
+        }
+        const int c = c0 + kc;
+        const bool cls = c < a.classes;
+        const float b = cls ? (a.bias ? to_float(reinterpret_cast<const T*>(a.bias)[c]) : 0.f) : -INFINITY;
+        const float z = cls ? (acc[0] + b) * a.sc : -INFINITY;
+        if (a.z && mine && c < last) a.z[row * a.ldz + c] = z;
+        if (!cls) continue;
+        const float most = fmaxf(m, z), base = most == -INFINITY ? 0.f : most;
+        s1 = s1 * exp2_fast(m - base) + exp2_fast(z - base);
+        if (NL == 2) s2 = s2 * exp2_fast((m - base) * a.inv_t) + exp2_fast((z - base) * a.inv_t);
+        m = most;
+        while (e < a.ntargets && tg[e].x < c) ++e;
+        for (; e < a.ntargets && tg[e].x == c; ++e) dot = fmaf(__int_as_float(tg[e].y), z, dot);
+    }
+    sm[w][lane] = make_float4(m, s1, s2, dot);
+    __syncthreads();
+    if (threadIdx.x >= a.rows) return;
+    float4 at = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    for (int i = 0; i < 8; ++i)
+        for (int k = 0; k < 4; ++k) {
+            const float4 v = sm[i][(k * NR + threadIdx.x) << (5 - LC)];
+            const float most = fmaxf(at.x, v.x), base = most == -INFINITY ? 0.f : most;
+            at.y = at.y * exp2f(at.x - base) + v.y * exp2f(v.x - base);
+            if (NL == 2) at.z = at.z * exp2f((at.x - base) * a.inv_t) + v.z * exp2f((v.x - base) * a.inv_t);
+            at.x = most;
+            at.w += v.w;
+        }
+    a.stats[(long long)blockIdx.x * a.rows + threadIdx.x] = at;
+}
+
 constexpr int kFinishRows = 8;
 
 struct FinishArgs {
@@ -328,7 +455,7 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
 }
 
 // G from what the tiles left of z, in its place (16-bit codes) or beside it (fp32): G = w (a p + (1 - a) T p^T - tau) times scal[0], in the operand type or (T = float) in
-// three bfloat16 parts.  A warp takes 256 classes of a row at a time, a block 32 rows of them, so column sums (for db, before any rounding) cost one
+// three bfloat16 parts.  A warp takes 1024 classes of a row at a time, a block 32 rows of them, so column sums (for db, before any rounding) cost one
 // exchange.  Bound by memory: 4 bytes a value.
 struct GradArgs {
     const void* z; long long ldz;             // codes or fp32 [rows x ldz]
@@ -341,106 +468,140 @@ struct GradArgs {
     float* colsum;                            // [row blocks x ldg] or null
     int rows, classes;
 };
-template <class T, class Z, int NL>
+template <class T, class Z, int NL, bool SUMS>
 __global__ void __launch_bounds__(256) class_grad_kernel(const GradArgs a) {
-    __shared__ float sm[8][256 + 8];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c0 = blockIdx.x * 256, c = c0 + 8 * lane;
+    constexpr int SEG = 4;                    // 256 classes (8 a lane) each
+    __shared__ float sm[SUMS ? 8 : 1][256 + 8];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c0 = blockIdx.x * 256 * SEG;
     pdl_next();
     pdl_wait();
     const float gs = a.scal[0];
-    float sums[8];
+    float sums[SUMS ? SEG : 1][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[j] = 0.f;
-    const bool in = c < a.ldg;                // (rows of G are whole tiles of 128 classes)
-    constexpr int LOADS = sizeof(Z) / 2, ROWS = 4;
-    uint4 q[ROWS][LOADS];                     // all loads of a warp's rows first
-    float4 rc[ROWS];
-    float m[ROWS], fw[ROWS];
-    int2 tg[ROWS];
+    for (int s = 0; s < (SUMS ? SEG : 1); ++s)
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int r = min((int)blockIdx.y * 32 + 8 * i + w, a.rows - 1);
-#pragma unroll
-        for (int k = 0; k < LOADS; ++k)
-            q[i][k] = in ? reinterpret_cast<const uint4*>(reinterpret_cast<const Z*>(a.z) + (long long)r * a.ldz + c)[k] : make_uint4(0u, 0u, 0u, 0u);
-        m[i] = sizeof(Z) == 2 && in ? a.stats[(long long)(c / a.half_w) * a.rows + r].x : 0.f;
-        rc[i] = a.rowc[r];
-        fw[i] = a.rowk[r].w;
-        tg[i] = lane < a.ntargets ? a.targets[(long long)r * a.ntargets + lane] : make_int2(INT_MAX, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
+        for (int j = 0; j < 8; ++j) sums[s][j] = 0.f;
+    constexpr int LOADS = sizeof(Z) / 2;
+    for (int i = 0; i < 4; ++i) {
         const int r = blockIdx.y * 32 + 8 * i + w;
         if (r >= a.rows) break;
-        const float f = fw[i] * gs;
+        uint4 q[SEG][LOADS];                  // all loads of a row first
+        float m[SEG];
+#pragma unroll
+        for (int s = 0; s < SEG; ++s) {
+            const int c = c0 + 256 * s + 8 * lane;
+            const bool in = c < a.ldg;        // (rows of G are whole tiles of 128 classes)
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k)
+                q[s][k] = in ? reinterpret_cast<const uint4*>(reinterpret_cast<const Z*>(a.z) + (long long)r * a.ldz + c)[k] : make_uint4(0u, 0u, 0u, 0u);
+            m[s] = sizeof(Z) == 2 && in ? a.stats[(long long)(c / a.half_w) * a.rows + r].x : 0.f;
+        }
+        const float4 rc = a.rowc[r];
+        const float f = a.rowk[r].w * gs;
+        const int2* list = a.targets + (long long)r * a.ntargets;
+        int e = 0;
+        if (a.ntargets > 128) {               // the first target of these classes
+            int hi = a.ntargets;
+            while (e < hi) {
+                const int mid = (e + hi) >> 1;
+                if (list[mid].x < c0) e = mid + 1; else hi = mid;
+            }
+        }
+        int2 t = e + lane < a.ntargets ? list[e + lane] : make_int2(INT_MAX, 0);
         // a sum that is not finite makes the whole row not a number, also where the code says zero; a row without weight is zero whatever it holds
-        const float fa = f == 0.f ? 0.f : f * rc[i].x + 0.f * rc[i].z, fb = f == 0.f ? 0.f : f * rc[i].y;
-        float v[8];
-        {
-            float z[8];                       // log2 of exp(z), as the first sum is
-            if constexpr (sizeof(Z) == 2) {
-                const uint32_t h[4] = {q[i][0].x, q[i][0].y, q[i][0].z, q[i][0].w};
+        const float fa = f * rc.x + 0.f * rc.z, fb = f * rc.y;
+        float v[SEG][8];
+        if (f == 0.f) {
+#pragma unroll
+            for (int s = 0; s < SEG; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[s][j] = 0.f;
+        } else {
+#pragma unroll
+            for (int s = 0; s < SEG; ++s) {
+                const uint32_t* h = reinterpret_cast<const uint32_t*>(q[s]);
+                float z[8];                   // log2 of exp(z) relative to the (first) sum
+                if constexpr (sizeof(Z) == 2) {
+                    const float d = m[s] - rc.z;
+                    // a code behind the exponent of 2^23 is that number of steps above 2^23 = 4096 x 2048 of them: exact
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        z[j] = fmaf(__uint_as_float(__byte_perm(h[j >> 1], 0x4B000000u, j & 1 ? 0x7632 : 0x7610)), -1.f / kCodeSteps, 4096.f) + d;
+                    const uint32_t top = __vmaxu2(__vmaxu2(h[0], h[1]), __vmaxu2(h[2], h[3]));
+                    if ((top >> 16) == kCodeZero || (top & 0xFFFFu) == kCodeZero) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (((h[j >> 1] >> (16 * (j & 1))) & 0xFFFFu) == kCodeZero) z[j] = -INFINITY;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(h[j]) - rc.z;
+                }
+                const float shift = fmaf(rc.z, a.inv_t, -rc.w);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint32_t code = j & 1 ? h[j >> 1] >> 16 : h[j >> 1] & 0xFFFFu;
-                    z[j] = code == (uint32_t)kCodeZero ? -INFINITY : fmaf((float)code, -1.f / kCodeSteps, m[i]);
+                    v[s][j] = fa * exp2_fast(z[j]);
+                    if (NL == 2) v[s][j] = fmaf(fb, exp2_fast(fmaf(z[j], a.inv_t, shift)), v[s][j]);
                 }
+            }
+            // the row's targets among these classes, 32 of the list at a time (it is ascending)
+            for (;;) {
+                for (uint32_t hit = __ballot_sync(0xffffffffu, t.x >= c0 && t.x < c0 + 256 * SEG); hit; hit &= hit - 1) {
+                    const int src = __ffs(hit) - 1, x = __shfl_sync(0xffffffffu, t.x, src) - c0 - 8 * lane;
+                    const float d = f * __int_as_float(__shfl_sync(0xffffffffu, t.y, src));
+#pragma unroll
+                    for (int s = 0; s < SEG; ++s)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[s][j] -= x == 256 * s + j ? d : 0.f;
+                }
+                if (__shfl_sync(0xffffffffu, t.x, 31) >= c0 + 256 * SEG) break;
+                e += 32;
+                if (e >= a.ntargets) break;
+                t = e + lane < a.ntargets ? list[e + lane] : make_int2(INT_MAX, 0);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < SEG; ++s) {
+            const int c = c0 + 256 * s + 8 * lane;
+            if (c >= a.ldg) break;
+            if constexpr (SUMS) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sums[s][j] += v[s][j];
+            }
+            if constexpr (sizeof(T) == 4) {
+                union { uint4 u; __nv_bfloat16 h[8]; } o[3];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    __nv_bfloat16 p[3];
+                    split3(v[s][j], p);
+                    o[0].h[j] = p[0]; o[1].h[j] = p[1]; o[2].h[j] = p[2];
+                }
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.G) + k * a.part_stride + (long long)r * a.ldg + c) = o[k].u;
             } else {
+                union { uint4 u; T h[8]; } o;
 #pragma unroll
-                for (int k = 0; k < LOADS; ++k) {
-                    z[4 * k] = __uint_as_float(q[i][k].x); z[4 * k + 1] = __uint_as_float(q[i][k].y); z[4 * k + 2] = __uint_as_float(q[i][k].z); z[4 * k + 3] = __uint_as_float(q[i][k].w);
-                }
+                for (int j = 0; j < 8; ++j) o.h[j] = from_float<T>(v[s][j]);
+                *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.G) + (long long)r * a.ldg + c) = o.u;
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = f == 0.f ? 0.f : fa * exp2_fast(z[j] - rc[i].z);
-                if (NL == 2) v[j] += f == 0.f ? 0.f : fb * exp2_fast(fmaf(z[j], a.inv_t, -rc[i].w));
-            }
-        }
-        // the row's targets among these 256 classes: 32 of the list at a time (it is ascending)
-        int2 t = tg[i];
-        for (int at = 0;;) {
-            for (uint32_t hit = __ballot_sync(0xffffffffu, t.x >= c0 && t.x < c0 + 256); hit; hit &= hit - 1) {
-                const int src = __ffs(hit) - 1, x = __shfl_sync(0xffffffffu, t.x, src);
-                const float d = f * __int_as_float(__shfl_sync(0xffffffffu, t.y, src));
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] -= x == c + j ? d : 0.f;
-            }
-            if (__shfl_sync(0xffffffffu, t.x, 31) >= c0 + 256) break;
-            at += 32;
-            if (at >= a.ntargets) break;
-            t = at + lane < a.ntargets ? a.targets[(long long)r * a.ntargets + at + lane] : make_int2(INT_MAX, 0);
-        }
-        if (!in) continue;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sums[j] += v[j];
-        if constexpr (sizeof(T) == 4) {
-            union { uint4 u; __nv_bfloat16 h[8]; } o[3];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                __nv_bfloat16 p[3];
-                split3(v[j], p);
-                o[0].h[j] = p[0]; o[1].h[j] = p[1]; o[2].h[j] = p[2];
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.G) + k * a.part_stride + (long long)r * a.ldg + c) = o[k].u;
-        } else {
-            union { uint4 u; T h[8]; } o;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o.h[j] = from_float<T>(v[j]);
-            *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.G) + (long long)r * a.ldg + c) = o.u;
         }
     }
-    if (!a.colsum) return;
+    if constexpr (SUMS) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sm[w][8 * lane + j] = sums[j];
-    __syncthreads();
-    const int x = c0 + threadIdx.x;
-    if (x >= a.classes) return;
-    float s = 0.f;
+        for (int s = 0; s < SEG; ++s) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += sm[i][threadIdx.x];
-    a.colsum[(long long)blockIdx.y * a.ldg + x] = s;
+            for (int j = 0; j < 8; ++j) sm[w][8 * lane + j] = sums[s][j];
+            __syncthreads();
+            const int x = c0 + 256 * s + threadIdx.x;
+            if (x < a.classes) {
+                float d = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d += sm[i][threadIdx.x];
+                a.colsum[(long long)blockIdx.y * a.ldg + x] = d;
+            }
+            __syncthreads();
+        }
+    }
 }
 
 // The shares of the tiles that were cut along their reduction, added up in order, and put where an uncut tile would have gone: four columns a thread, four (eight)
@@ -525,9 +686,12 @@ cudaError_t chain(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, 
 
 int width_for(int n) { return n <= 128 ? 128 : 256; }
 
+int few_rows(int64_t n) { return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8; }
+size_t few_smem(const gad_class_loss_args& a) { return 4 * (size_t)few_rows(a.rows) * (size_t)round_up(a.cols, 8); }
+
 struct ClassPlan {
     int parts, pairs;                // operand parts, products of them
-    bool grads, pack_w;
+    bool grads, pack_w, few;
     int ntargets, nl, save;
     int width_v, tiles_v, width_d, tiles_d;
     int64_t ldp, ldg;                // row lengths of the packed operands, and of z and G
@@ -543,11 +707,12 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     p.parts = a.dtype == GAD_F32 ? 3 : 1;
     p.pairs = a.dtype == GAD_F32 ? 6 : 1;
     p.grads = a.dH || a.dW || a.db;
-    p.pack_w = a.dtype == GAD_F32 || ((uintptr_t)a.W & 15) != 0 || (a.ldw * 2) % 16 != 0;
+    p.few = N <= kFewRows && few_smem(a) <= kFewSmem;
+    p.pack_w = (!p.few || a.dH) && (a.dtype == GAD_F32 || ((uintptr_t)a.W & 15) != 0 || (a.ldw * 2) % 16 != 0);
     p.ntargets = a.k + (a.labels ? 1 : 0);
     p.nl = a.k > 0 && a.labels && a.hard_weight > 0.f && a.hard_weight < 1.f && a.temperature != 1.f ? 2 : 1;
     // a code's step is 1 / T times as large in the second softmax: up to twice it is still below what G is rounded by
-    p.save = !p.grads ? kSaveNone : a.dtype == GAD_F32 || (p.nl == 2 && a.temperature < 0.5f) ? kSaveFloat : kSaveCode;
+    p.save = !p.grads ? kSaveNone : a.dtype == GAD_F32 || p.few || (p.nl == 2 && a.temperature < 0.5f) ? kSaveFloat : kSaveCode;
     p.ldp = round_up(D, 8);
     p.width_v = width_for(V);
     p.tiles_v = (V + p.width_v - 1) / p.width_v;
@@ -568,7 +733,7 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     p.o_rowk = room(16 * N);
     p.o_rshares = room((int64_t)sizeof(RowShare) * N);
     p.o_lshares = room((int64_t)sizeof(double) * ((N + kFinishRows - 1) / kFinishRows));
-    p.o_stats = room(16 * p.block * 2 * p.tiles_v);
+    p.o_stats = room(16 * p.block * (p.few ? kFewBlocks : 2 * p.tiles_v));
     if (p.grads) {
         p.o_rowc = room(16 * p.block);
         p.o_z = room((p.save == kSaveCode ? 2 : 4) * p.block * p.ldg);
@@ -581,8 +746,8 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     return p;
 }
 
-// Ring stages (64 terms each) of a chunk: 64 additions to an accumulator, about 3e-7 of its value; for fp32 operands half of that.
-constexpr int kChunk = 16, kChunkParts = 8;
+// Ring stages (64 terms each) of a chunk: 128 additions to an accumulator, about 6e-7 of its value; for fp32 operands a quarter of that.
+constexpr int kChunk = 32, kChunkParts = 8;
 
 template <int USE, bool A_MN, bool B_MN, class T, int NL, bool ADD_UP>
 cudaError_t gemm_launch(const CUtensorMap& A, const CUtensorMap& B, const TileArgs& a, cudaStream_t s) {
@@ -599,6 +764,13 @@ cudaError_t gemm_launch(const CUtensorMap& A, const CUtensorMap& B, const TileAr
 template <int NL>
 cudaError_t go_stats(const CUtensorMap& A, const CUtensorMap& B, const TileArgs& a, cudaStream_t s) {
     return a.nkb * a.pairs > a.chunk ? gemm_launch<kStats, false, false, float, NL, true>(A, B, a, s) : gemm_launch<kStats, false, false, float, NL, false>(A, B, a, s);
+}
+template <class T, int NL, bool WIDE>
+cudaError_t few_launch(const FewArgs& f, size_t smem, int blocks, cudaStream_t s) {
+    const int n = few_rows(f.rows);
+    const auto kernel = n == 1 ? class_few_kernel<T, 1, NL, WIDE> : n == 2 ? class_few_kernel<T, 2, NL, WIDE> : n == 4 ? class_few_kernel<T, 4, NL, WIDE> : class_few_kernel<T, 8, NL, WIDE>;
+    const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), kFewSmem, false);
+    return e != cudaSuccess ? e : chain(kernel, dim3((unsigned)blocks), 256, smem, s, false, f);
 }
 // A gradient.  Tiles that are left over when all pairs have had the same number are cut along their reduction, so that they keep every pair busy too
 // (4096 x 1024 over 47 classes: 4 tiles, 18 shares each), down to 8 ring stages a share.  Sums for an fp32 result are added up in chunks.
@@ -653,12 +825,12 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
     const auto make = [&](CUtensorMap& m, const void* base, int64_t inner, int64_t rows, int64_t ld, int64_t part_rows, uint32_t box) {
         return tc_make_map(&m, base, (uint64_t)inner, (uint64_t)rows, (uint64_t)p.parts, (uint64_t)ld * 2, (uint64_t)(ld * 2 * part_rows), box, false, true) ? cudaSuccess : cudaErrorInvalidValue;
     };
-    GAD_TRY(make(mapH, Hp, D, N, p.ldp, N, CT_H));
-    GAD_TRY(make(mapW, Wo, D, V, ldw, V, (uint32_t)p.width_v / 2));
-    if (p.grads) {
-        GAD_TRY(make(mapH_mn, Hp, D, N, p.ldp, N, CT_K));
-        GAD_TRY(make(mapW_mn, Wo, D, V, ldw, V, CT_K));
+    if (!p.few) {
+        GAD_TRY(make(mapH, Hp, D, N, p.ldp, N, CT_H));
+        GAD_TRY(make(mapW, Wo, D, V, ldw, V, (uint32_t)p.width_v / 2));
     }
+    if (a.dW) GAD_TRY(make(mapH_mn, Hp, D, N, p.ldp, N, CT_K));
+    if (a.dH) GAD_TRY(make(mapW_mn, Wo, D, V, ldw, V, CT_K));
     for (int b = 0; b < p.nblocks; ++b) {
         const int64_t r0 = b * p.block;
         const int nr = (int)std::min(p.block, N - r0), blocks = (nr + kFinishRows - 1) / kFinishRows;
@@ -673,9 +845,18 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         z.inv_t = 1.f / T0;
         z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.stats = stats;
         z.save = p.save; z.C = ws + p.o_z; z.ldc = p.ldg;
-        GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, s) : go_stats<1>(mapH, mapW, z, s));
+        int nparts = 2 * p.tiles_v;
+        if (p.few) {
+            FewArgs w{};
+            w.H = a.H; w.ldh = a.ldh; w.W = a.W; w.ldw = a.ldw; w.rows = nr; w.cols = D; w.classes = V; w.bias = a.bias; w.targets = targets; w.ntargets = p.ntargets; w.rowk = rowk;
+            w.sc = z.sc; w.inv_t = z.inv_t; w.z = p.grads ? reinterpret_cast<float*>(z.C) : nullptr; w.ldz = p.ldg; w.stats = stats;
+            nparts = (int)std::min<int64_t>(kFewBlocks, (p.ldg + 31) / 32);
+            const bool wide = ((uintptr_t)a.W & 15) == 0 && (a.ldw * (int64_t)sizeof(T)) % 16 == 0;
+            GAD_TRY(p.nl == 2 ? (wide ? few_launch<T, 2, true>(w, few_smem(a), nparts, s) : few_launch<T, 2, false>(w, few_smem(a), nparts, s))
+                              : (wide ? few_launch<T, 1, true>(w, few_smem(a), nparts, s) : few_launch<T, 1, false>(w, few_smem(a), nparts, s)));
+        } else GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, s) : go_stats<1>(mapH, mapW, z, s));
         FinishArgs f{};
-        f.stats = stats; f.parts = 2 * p.tiles_v; f.rows = nr; f.rowk = rowk + r0; f.sc = z.sc; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
+        f.stats = stats; f.parts = nparts; f.rows = nr; f.rowk = rowk + r0; f.sc = z.sc; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
         f.shares = reinterpret_cast<double*>(ws + p.o_lshares); f.share0 = (int)(r0 / kFinishRows); f.nshares = (int)((N + kFinishRows - 1) / kFinishRows);
         f.row_shares = ra.shares; f.nrow_shares = nrshares; f.ticket = ra.ticket; f.scale = a.scale; f.mean = a.mean; f.first = b == 0; f.final = b == p.nblocks - 1;
         f.scal = scal; f.loss = a.loss;
@@ -685,11 +866,14 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         g.z = z.C; g.ldz = p.ldg; g.G = ws + p.o_g; g.ldg = p.ldg; g.part_stride = nr * p.ldg; g.stats = stats; g.half_w = p.width_v / 2;
         g.rowc = rowc; g.rowk = rowk + r0; g.targets = z.targets; g.ntargets = p.ntargets; g.scal = scal; g.inv_t = z.inv_t;
         g.colsum = a.db ? reinterpret_cast<float*>(ws + p.o_colsum) : nullptr; g.rows = nr; g.classes = V;
-        auto grad = p.nl == 2 ? class_grad_kernel<T, float, 2> : class_grad_kernel<T, float, 1>;
+        auto grad = a.db ? (p.nl == 2 ? class_grad_kernel<T, float, 2, true> : class_grad_kernel<T, float, 1, true>)
+                         : (p.nl == 2 ? class_grad_kernel<T, float, 2, false> : class_grad_kernel<T, float, 1, false>);
         if constexpr (sizeof(T) == 2)
-            if (p.save == kSaveCode) grad = p.nl == 2 ? class_grad_kernel<T, uint16_t, 2> : class_grad_kernel<T, uint16_t, 1>;
+            if (p.save == kSaveCode)
+                grad = a.db ? (p.nl == 2 ? class_grad_kernel<T, uint16_t, 2, true> : class_grad_kernel<T, uint16_t, 1, true>)
+                            : (p.nl == 2 ? class_grad_kernel<T, uint16_t, 2, false> : class_grad_kernel<T, uint16_t, 1, false>);
         const int slices = (nr + 31) / 32;
-        GAD_TRY(chain(grad, dim3((unsigned)((p.ldg + 255) / 256), (unsigned)slices), 256, 0, s, false, g));
+        GAD_TRY(chain(grad, dim3((unsigned)((p.ldg + 1023) / 1024), (unsigned)slices), 256, 0, s, false, g));
         const int add = p.nblocks == 1 ? kAddNone : b == 0 ? kAddFirst : b < p.nblocks - 1 ? kAddMore : kAddLast;
         if (a.db)
             GAD_TRY(chain(class_bias_kernel<T>, dim3((unsigned)((V + 31) / 32)), 256, 0, s, false, (const float*)g.colsum, p.ldg, slices, V, (const float*)scal, add,

@@ -132,16 +132,20 @@ def compare(got, ref, s, T=1.0):
         assert off <= tol + sub + 1e-37, (name, off / max(want.norm().item(), 1e-300), tol / max(want.norm().item(), 1e-300))
 
 
-CLASS_SHAPES = [(1, 1, 1), (1, 64, 2), (5, 7, 3), (3, 72, 128), (130, 100, 129), (257, 64, 300), (2, 4096, 1000), (777, 500, 2049), (300, 130, 47), (1, 256, 40000)]
+CLASS_SHAPES = [(1, 1, 1), (1, 64, 2), (5, 7, 3), (3, 72, 128), (130, 100, 129), (257, 64, 300), (2, 4096, 1000), (777, 500, 2049), (300, 130, 47), (1, 256, 40000), (4, 1001, 700), (8, 328, 5000), (7, 6000, 90)]
 
 
 @gpu
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
 @pytest.mark.parametrize("N,D,V", CLASS_SHAPES)
 def test_class_loss(N, D, V, dtype):
+    import torch
     for bias, weights, ignored, int64 in ((False, False, 0.0, False), (True, True, 0.4, True)):
         s = make(N, D, V, dtype, 1, bias=bias, weights=weights, ignored=ignored, int64=int64)
-        compare(pkg.class_loss(**s), reference(**s), s)
+        got = pkg.class_loss(**s)
+        compare(got, reference(**s), s)
+        alone = pkg.class_loss(**s, grads=False)
+        assert torch.equal(alone.loss, got.loss) and torch.equal(alone.row_loss, got.row_loss)
 
 
 @gpu
