@@ -689,9 +689,12 @@ int width_for(int n) { return n <= 128 ? 128 : 256; }
 int few_rows(int64_t n) { return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8; }
 size_t few_smem(const gad_class_loss_args& a) { return 4 * (size_t)few_rows(a.rows) * (size_t)round_up(a.cols, 8); }
 
+// Blocks of 64 terms of a chunk: 128 additions to an accumulator, about 6e-7 of its value; for fp32 operands a quarter of that.
+constexpr int kChunk = 32, kChunkParts = 8;
+
 struct ClassPlan {
     int parts, pairs;                // operand parts, products of them
-    bool grads, pack_w, few;
+    bool grads, pack_w, few, add_up;   // add_up: logits longer than a chunk are added up in chunks
     int ntargets, nl, save;
     int width_v, tiles_v, width_d, tiles_d;
     int64_t ldp, ldg;                // row lengths of the packed operands, and of z and G
@@ -714,7 +717,8 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     // a code's step is 1 / T times as large in the second softmax: up to twice it is still below what G is rounded by
     p.save = !p.grads ? kSaveNone : a.dtype == GAD_F32 || p.few || (p.nl == 2 && a.temperature < 0.5f) ? kSaveFloat : kSaveCode;
     p.ldp = round_up(D, 8);
-    p.width_v = width_for(V);
+    p.add_up = (D + CT_K - 1) / CT_K > (p.parts > 1 ? kChunkParts : kChunk);
+    p.width_v = p.add_up ? 128 : width_for(V);
     p.tiles_v = (V + p.width_v - 1) / p.width_v;
     p.width_d = width_for(D);
     p.tiles_d = (D + p.width_d - 1) / p.width_d;
@@ -746,9 +750,6 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     return p;
 }
 
-// Ring stages (64 terms each) of a chunk: 128 additions to an accumulator, about 6e-7 of its value; for fp32 operands a quarter of that.
-constexpr int kChunk = 32, kChunkParts = 8;
-
 template <int USE, bool A_MN, bool B_MN, class T, int NL, bool ADD_UP>
 cudaError_t gemm_launch(const CUtensorMap& A, const CUtensorMap& B, const TileArgs& a, cudaStream_t s) {
     const auto kernel = class_gemm_kernel<USE, A_MN, B_MN, T, NL, ADD_UP>;
@@ -760,10 +761,10 @@ cudaError_t gemm_launch(const CUtensorMap& A, const CUtensorMap& B, const TileAr
     const int ncl = (int)std::min<int64_t>(units, known.load());
     return chain(kernel, dim3((unsigned)(2 * ncl)), CT_THREADS, CT_SMEM, s, false, A, B, a);
 }
-// The statistics of a block of rows.  Logits longer than a chunk are added up in chunks.
+// The statistics of a block of rows.
 template <int NL>
-cudaError_t go_stats(const CUtensorMap& A, const CUtensorMap& B, const TileArgs& a, cudaStream_t s) {
-    return a.nkb * a.pairs > a.chunk ? gemm_launch<kStats, false, false, float, NL, true>(A, B, a, s) : gemm_launch<kStats, false, false, float, NL, false>(A, B, a, s);
+cudaError_t go_stats(const CUtensorMap& A, const CUtensorMap& B, const TileArgs& a, bool add_up, cudaStream_t s) {
+    return add_up ? gemm_launch<kStats, false, false, float, NL, true>(A, B, a, s) : gemm_launch<kStats, false, false, float, NL, false>(A, B, a, s);
 }
 template <class T, int NL, bool WIDE>
 cudaError_t few_launch(const FewArgs& f, size_t smem, int blocks, cudaStream_t s) {
@@ -854,7 +855,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
             const bool wide = ((uintptr_t)a.W & 15) == 0 && (a.ldw * (int64_t)sizeof(T)) % 16 == 0;
             GAD_TRY(p.nl == 2 ? (wide ? few_launch<T, 2, true>(w, few_smem(a), nparts, s) : few_launch<T, 2, false>(w, few_smem(a), nparts, s))
                               : (wide ? few_launch<T, 1, true>(w, few_smem(a), nparts, s) : few_launch<T, 1, false>(w, few_smem(a), nparts, s)));
-        } else GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, s) : go_stats<1>(mapH, mapW, z, s));
+        } else GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, p.add_up, s) : go_stats<1>(mapH, mapW, z, p.add_up, s));
         FinishArgs f{};
         f.stats = stats; f.parts = nparts; f.rows = nr; f.rowk = rowk + r0; f.sc = z.sc; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
         f.shares = reinterpret_cast<double*>(ws + p.o_lshares); f.share0 = (int)(r0 / kFinishRows); f.nshares = (int)((N + kFinishRows - 1) / kFinishRows);
