@@ -670,20 +670,6 @@ __global__ void class_empty_kernel(float* loss, int32_t* status) { *loss = 0.f; 
 // ---------------------------------------------------------------------------------------------
 constexpr int kPairs = 74;                               // pairs of CTAs that run at once
 
-// Kernels of one call follow each other by programmatic dependent launch: each comes up while the one in front ends and waits (pdl_wait) before it touches
-// memory.  The first waits for all that is in front of it on the stream.
-template <class... P, class... Args>
-cudaError_t chain(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t s, bool first, Args&&... args) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = first ? 0 : 1;
-    ++g_kernel_launches;
-    return cudaLaunchKernelEx(&cfg, kernel, P(std::forward<Args>(args))...);
-}
-
 int width_for(int n) { return n <= 128 ? 128 : 256; }
 
 int few_rows(int64_t n) { return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8; }

@@ -1,9 +1,13 @@
-// The element types of the output head (fp32, fp16, bfloat16): conversions, and vectors of a row that end at its last column.
+// Shared by the operators of the output head: their element types (fp32, fp16, bfloat16), vectors of a row that end at its last column, and launches in a chain.
 #pragma once
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <stdint.h>
+
+#include <utility>
+
+#include "gad_internal.h"
 
 namespace gad {
 
@@ -19,19 +23,27 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// row[c .. c + VEC) as fp32, zeros from `cols` on.  VEC > 1: 16 bytes, aligned.
+// VEC values of a row as they lie in memory (VEC > 1: 16 bytes, aligned), and as fp32.
 template <class T, int VEC>
-__device__ __forceinline__ void load_vec(const T* __restrict__ row, int c, int cols, float (&v)[VEC]) {
-    if (VEC > 1 && c + VEC <= cols) {
-        static_assert(VEC == 1 || VEC * sizeof(T) == 16, "vectors are 16 bytes");
-        union { uint4 u; T e[VEC]; } w;
-        w.u = *reinterpret_cast<const uint4*>(row + c);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) v[j] = to_float(w.e[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) v[j] = c + j < cols ? to_float(row[c + j]) : 0.f;
+union RowVec {
+    static_assert(VEC == 1 || VEC * sizeof(T) == 16, "vectors are 16 bytes");
+    uint4 u;
+    T e[VEC];
+    __device__ RowVec() {}
+};
+template <class T>
+union RowVec<T, 1> {
+    T e[1];
+    __device__ RowVec() {}
+};
+// row[c .. c + VEC), zeros from `cols` on.
+template <class T, int VEC>
+__device__ __forceinline__ void load_raw(const T* __restrict__ row, int c, int cols, RowVec<T, VEC>& v) {
+    if constexpr (VEC > 1) {
+        if (c + VEC <= cols) { v.u = *reinterpret_cast<const uint4*>(row + c); return; }
     }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) v.e[j] = c + j < cols ? row[c + j] : from_float<T>(0.f);
 }
 template <class T, int VEC>
 __device__ __forceinline__ void store_vec(T* __restrict__ row, int c, int cols, const float (&v)[VEC]) {
@@ -45,6 +57,20 @@ __device__ __forceinline__ void store_vec(T* __restrict__ row, int c, int cols, 
         for (int j = 0; j < VEC; ++j)
             if (c + j < cols) row[c + j] = from_float<T>(v[j]);
     }
+}
+
+// Kernels of one call follow each other by programmatic dependent launch: each comes up while the one in front ends and waits (pdl_wait) before it touches
+// memory.  The first waits for all that is in front of it on the stream.
+template <class... P, class... Args>
+cudaError_t chain(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t s, bool first, Args&&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = first ? 0 : 1;
+    ++g_kernel_launches;
+    return cudaLaunchKernelEx(&cfg, kernel, P(std::forward<Args>(args))...);
 }
 
 }  // namespace

@@ -8,6 +8,8 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <map>
+#include <mutex>
 
 #include "gad_internal.h"
 #include "half_types.cuh"
@@ -19,13 +21,30 @@ namespace {
 // Blocks of the backward pass at most, each with a partial sum of dgamma and dbeta: four on every SM.
 constexpr int kNormBlocks = 592;
 
-// gamma / beta in fp32 or in the matrix's own type; null is 1 or 0.
+// gamma / beta in fp32 or in the matrix's own type; null is 1 or 0.  `wide`: both start on 16 bytes.
 template <class T, int VEC>
-__device__ __forceinline__ void load_param(const void* p, bool fp32, int c, int cols, float none, float (&v)[VEC]) {
+__device__ __forceinline__ void load_param(const void* p, bool fp32, bool wide, int c, int cols, float none, float (&v)[VEC]) {
     if (!p) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) v[j] = none;
         return;
+    }
+    if constexpr (VEC > 1) {
+        if (wide && c + VEC <= cols) {
+            if (fp32 || sizeof(T) == 4) {
+#pragma unroll
+                for (int j = 0; j < VEC; j += 4) {
+                    const float4 q = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + c + j);
+                    v[j] = q.x; v[j + 1] = q.y; v[j + 2] = q.z; v[j + 3] = q.w;
+                }
+            } else {
+                RowVec<T, VEC> q;
+                q.u = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p) + c);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) v[j] = to_float(q.e[j]);
+            }
+            return;
+        }
     }
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
@@ -64,110 +83,153 @@ __device__ __forceinline__ void row_sum(float (&v)[NS], float* sm, int slot) {
     }
 }
 
-// NV vectors of VEC values a thread hold a row: vector k of thread t starts at column (k * threads + t) * VEC.
+// NV vectors of VEC values a thread hold a row: vector k of thread t starts at column (k * threads + t) * VEC.  A block takes every gridDim-th row (group of rows),
+// keeps gamma and beta in registers and has the next row on its way while it works on one.
 template <class T, int VEC, int NV, int WPR>
 __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* __restrict__ x, long long ldx, long long rows, int cols, const void* __restrict__ gamma,
-                                                                       const void* __restrict__ beta, bool p32, float eps, T* __restrict__ y, long long ldy,
+                                                                       const void* __restrict__ beta, bool p32, bool pwide, float eps, T* __restrict__ y, long long ldy,
                                                                        float* __restrict__ mean, float* __restrict__ rstd) {
-    constexpr int TPR = 32 * WPR;
+    constexpr int TPR = 32 * WPR, ROWS = RowGroup<WPR>::kRows;
     __shared__ float sm[2 * WPR];
     const int t = threadIdx.x % TPR;
-    const long long r = (long long)blockIdx.x * RowGroup<WPR>::kRows + threadIdx.x / TPR;
-    if (r >= rows) return;                       // (a whole warp, or a whole block)
-    float v[NV][VEC];
-    const T* xr = x + r * ldx;
-    float s[1] = {0.f};
+    const long long step = (long long)gridDim.x * ROWS;
+    long long r = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
+    RowVec<T, VEC> next[NV];
+    if (r < rows)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) load_raw<T, VEC>(x + r * ldx, (k * TPR + t) * VEC, cols, next[k]);
+    float g[NV][VEC], b[NV][VEC];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const int c = (k * TPR + t) * VEC;
-        load_vec<T, VEC>(xr, c, cols, v[k]);     // zeros behind the last column
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) s[0] += v[k][j];
+        load_param<T, VEC>(gamma, p32, pwide, (k * TPR + t) * VEC, cols, 1.f, g[k]);
+        load_param<T, VEC>(beta, p32, pwide, (k * TPR + t) * VEC, cols, 0.f, b[k]);
     }
-    row_sum<WPR, 1>(s, sm, 0);
-    const float mu = s[0] / (float)cols;
-    float q[1] = {0.f};
+    const float inv = 1.f / (float)cols;
+    for (; r < rows; r += step) {                // (a whole warp, or a whole block)
+        float v[NV][VEC];
+        float s[1] = {0.f};
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int c = (k * TPR + t) * VEC;
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j)
-            if (c + j < cols) { const float d = v[k][j] - mu; q[0] = fmaf(d, d, q[0]); }
+            for (int j = 0; j < VEC; ++j) {
+                v[k][j] = to_float(next[k].e[j]);
+                s[0] += v[k][j];                 // (zeros behind the last column)
+            }
+        if (r + step < rows)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) load_raw<T, VEC>(x + (r + step) * ldx, (k * TPR + t) * VEC, cols, next[k]);
+        row_sum<WPR, 1>(s, sm, 0);
+        const float mu = s[0] * inv;
+        float q[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TPR + t) * VEC;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                v[k][j] -= mu;
+                if (c + j < cols) q[0] = fmaf(v[k][j], v[k][j], q[0]);
+            }
+        }
+        row_sum<WPR, 1>(q, sm, 1);
+        const float rs = 1.f / sqrtf(q[0] * inv + eps);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TPR + t) * VEC;
+            if (c >= cols) break;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[k][j] = fmaf(v[k][j] * rs, g[k][j], b[k][j]);
+            store_vec<T, VEC>(y + r * ldy, c, cols, v[k]);
+        }
+        if (t == 0) { mean[r] = mu; rstd[r] = rs; }
     }
-    row_sum<WPR, 1>(q, sm, 1);
-    const float rs = 1.f / sqrtf(q[0] / (float)cols + eps);
-    T* yr = y + r * ldy;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int c = (k * TPR + t) * VEC;
-        if (c >= cols) continue;
-        float g[VEC], b[VEC];
-        load_param<T, VEC>(gamma, p32, c, cols, 1.f, g);
-        load_param<T, VEC>(beta, p32, c, cols, 0.f, b);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) v[k][j] = fmaf((v[k][j] - mu) * rs, g[j], b[j]);
-        store_vec<T, VEC>(yr, c, cols, v[k]);
-    }
-    if (t == 0) { mean[r] = mu; rstd[r] = rs; }
 }
 
-// Rows longer than a block's registers hold: read three times, from L2 as long as they fit it.
-template <class T>
+// Rows longer than a block's registers hold: read three times, twice of them from L2 (148 blocks of two rows at once).
+template <class T, int VEC>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const T* __restrict__ x, long long ldx, int cols, const void* __restrict__ gamma, const void* __restrict__ beta,
-                                                         bool p32, float eps, T* __restrict__ y, long long ldy, float* __restrict__ mean, float* __restrict__ rstd) {
+                                                         bool p32, bool pwide, float eps, T* __restrict__ y, long long ldy, float* __restrict__ mean, float* __restrict__ rstd) {
     __shared__ float sm[2 * 32];
     const long long r = blockIdx.x;
     const T* xr = x + r * ldx;
+    RowVec<T, VEC> v;
     float s[1] = {0.f};
-    for (int c = threadIdx.x; c < cols; c += 1024) s[0] += to_float(xr[c]);
+    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+        load_raw<T, VEC>(xr, c, cols, v);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) s[0] += to_float(v.e[j]);
+    }
     row_sum<32, 1>(s, sm, 0);
     const float mu = s[0] / (float)cols;
     float q[1] = {0.f};
-    for (int c = threadIdx.x; c < cols; c += 1024) { const float d = to_float(xr[c]) - mu; q[0] = fmaf(d, d, q[0]); }
+    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+        load_raw<T, VEC>(xr, c, cols, v);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+            if (c + j < cols) { const float d = to_float(v.e[j]) - mu; q[0] = fmaf(d, d, q[0]); }
+    }
     row_sum<32, 1>(q, sm, 1);
     const float rs = 1.f / sqrtf(q[0] / (float)cols + eps);
-    for (int c = threadIdx.x; c < cols; c += 1024) {
-        float g[1], b[1];
-        load_param<T, 1>(gamma, p32, c, cols, 1.f, g);
-        load_param<T, 1>(beta, p32, c, cols, 0.f, b);
-        y[r * ldy + c] = from_float<T>(fmaf((to_float(xr[c]) - mu) * rs, g[0], b[0]));
+    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+        float g[VEC], b[VEC], o[VEC];
+        load_raw<T, VEC>(xr, c, cols, v);
+        load_param<T, VEC>(gamma, p32, pwide, c, cols, 1.f, g);
+        load_param<T, VEC>(beta, p32, pwide, c, cols, 0.f, b);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) o[j] = fmaf((to_float(v.e[j]) - mu) * rs, g[j], b[j]);
+        store_vec<T, VEC>(y + r * ldy, c, cols, o);
     }
     if (threadIdx.x == 0) { mean[r] = mu; rstd[r] = rs; }
 }
 
-// Every block takes rows blockIdx, blockIdx + gridDim ... (several at once where a row is a warp's) and keeps the sums of dy h and dy of its
-// columns in registers; they go to partial[block][2][cols], which norm_columns_kernel adds up in block order.
+// Every block takes rows blockIdx, blockIdx + gridDim ... (several at once where a row is a warp's), the next one on its way, and keeps the sums of dy h and dy of
+// its columns in registers; they go to partial[block][2][cols], which norm_columns_kernel adds up in block order.
 template <class T, int VEC, int NV, int WPR>
 __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, long long rows,
-                                                                                int cols, const void* __restrict__ gamma, bool p32, const float* __restrict__ mean,
+                                                                                int cols, const void* __restrict__ gamma, bool p32, bool pwide, const float* __restrict__ mean,
                                                                                 const float* __restrict__ rstd, T* __restrict__ dx, long long lddx, float* __restrict__ partial) {
     constexpr int TPR = 32 * WPR, ROWS = RowGroup<WPR>::kRows;
     __shared__ float sm[2 * 2 * WPR];
     extern __shared__ float cs[];                // with several rows a block: [2][cols]
+    pdl_next();
     const int t = threadIdx.x % TPR;
+    const long long step = (long long)gridDim.x * ROWS;
+    long long r = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
+    RowVec<T, VEC> nd[NV], nx[NV];
+    float nmu = 0.f, nrs = 0.f;
+    const auto fetch = [&](long long i) {
+        nmu = mean[i];
+        nrs = rstd[i];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            load_raw<T, VEC>(dy + i * lddy, (k * TPR + t) * VEC, cols, nd[k]);
+            load_raw<T, VEC>(x + i * ldx, (k * TPR + t) * VEC, cols, nx[k]);
+        }
+    };
+    if (r < rows) fetch(r);
     float ag[NV][VEC], ab[NV][VEC], g[NV][VEC];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        load_param<T, VEC>(gamma, p32, (k * TPR + t) * VEC, cols, 1.f, g[k]);
+        load_param<T, VEC>(gamma, p32, pwide, (k * TPR + t) * VEC, cols, 1.f, g[k]);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) ag[k][j] = ab[k][j] = 0.f;
     }
     const float inv = 1.f / (float)cols;
     int slot = 0;
-    for (long long r = (long long)blockIdx.x * ROWS + threadIdx.x / TPR; r < rows; r += (long long)gridDim.x * ROWS, slot ^= 1) {
-        const float mu = mean[r], rs = rstd[r];
+    for (; r < rows; r += step, slot ^= 1) {
+        const float mu = nmu, rs = nrs;
         float d[NV][VEC], h[NV][VEC], s[2] = {0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c = (k * TPR + t) * VEC;
-            load_vec<T, VEC>(dy + r * lddy, c, cols, d[k]);
-            load_vec<T, VEC>(x + r * ldx, c, cols, h[k]);
-        }
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                h[k][j] = (h[k][j] - mu) * rs;   // (behind the last column d = 0: adds nothing)
+                d[k][j] = to_float(nd[k].e[j]);
+                h[k][j] = (to_float(nx[k].e[j]) - mu) * rs;   // (behind the last column d = 0: adds nothing)
+            }
+        if (r + step < rows) fetch(r + step);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
                 ag[k][j] = fmaf(d[k][j], h[k][j], ag[k][j]);
                 ab[k][j] += d[k][j];
                 d[k][j] *= g[k][j];
@@ -215,25 +277,36 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(
 }
 
 // Long rows: dx by a block a row, read twice.
-template <class T>
+template <class T, int VEC>
 __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, int cols,
-                                                                  const void* __restrict__ gamma, bool p32, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                                  T* __restrict__ dx, long long lddx) {
+                                                                  const void* __restrict__ gamma, bool p32, bool pwide, const float* __restrict__ mean,
+                                                                  const float* __restrict__ rstd, T* __restrict__ dx, long long lddx) {
     __shared__ float sm[2 * 2 * 32];
     const long long r = blockIdx.x;
     const float mu = mean[r], rs = rstd[r], inv = 1.f / (float)cols;
-    float s[2] = {0.f, 0.f}, g[1];
-    for (int c = threadIdx.x; c < cols; c += 1024) {
-        load_param<T, 1>(gamma, p32, c, cols, 1.f, g);
-        const float d = to_float(dy[r * lddy + c]) * g[0];
-        s[0] += d;
-        s[1] = fmaf(d, (to_float(x[r * ldx + c]) - mu) * rs, s[1]);
+    RowVec<T, VEC> vd, vx;
+    float s[2] = {0.f, 0.f}, g[VEC];
+    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+        load_raw<T, VEC>(dy + r * lddy, c, cols, vd);
+        load_raw<T, VEC>(x + r * ldx, c, cols, vx);
+        load_param<T, VEC>(gamma, p32, pwide, c, cols, 1.f, g);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float d = to_float(vd.e[j]) * g[j];
+            s[0] += d;
+            s[1] = fmaf(d, (to_float(vx.e[j]) - mu) * rs, s[1]);
+        }
     }
     row_sum<32, 2>(s, sm, 0);
     const float m0 = s[0] * inv, m1 = s[1] * inv;
-    for (int c = threadIdx.x; c < cols; c += 1024) {
-        load_param<T, 1>(gamma, p32, c, cols, 1.f, g);
-        dx[r * lddx + c] = from_float<T>((to_float(dy[r * lddy + c]) * g[0] - m0 - (to_float(x[r * ldx + c]) - mu) * rs * m1) * rs);
+    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+        float o[VEC];
+        load_raw<T, VEC>(dy + r * lddy, c, cols, vd);
+        load_raw<T, VEC>(x + r * ldx, c, cols, vx);
+        load_param<T, VEC>(gamma, p32, pwide, c, cols, 1.f, g);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) o[j] = (to_float(vd.e[j]) * g[j] - m0 - (to_float(vx.e[j]) - mu) * rs * m1) * rs;
+        store_vec<T, VEC>(dx + r * lddx, c, cols, o);
     }
 }
 // ... and their column sums: a block has 32 columns and every gridDim.y-th eight rows.
@@ -263,10 +336,13 @@ __global__ void __launch_bounds__(256) norm_long_columns_kernel(const T* __restr
 template <class T>
 __global__ void __launch_bounds__(256) norm_columns_kernel(const float* __restrict__ partial, int nblocks, int cols, bool p32, void* __restrict__ dgamma, void* __restrict__ dbeta) {
     __shared__ float sm[8][32];
+    pdl_wait();
+    after_wait(partial);
     const int i = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
     const int per = (nblocks + 7) / 8, lo = min(nblocks, w * per), hi = min(nblocks, lo + per);
     float s = 0.f;
     if (i < 2 * cols)
+#pragma unroll 8
         for (int b = lo; b < hi; ++b) s += partial[(long long)b * 2 * cols + i];
     sm[w][threadIdx.x & 31] = s;
     __syncthreads();
@@ -286,17 +362,34 @@ struct NormCall {
     const void *x, *gamma, *beta;
     int64_t ldx, rows;
     int cols;
-    bool p32;
+    bool p32, pwide;
     float eps;
     void* y;
     int64_t ldy;
     float *mean, *rstd;
 };
 
+// Blocks of a kernel that the GPU holds at once, at most kNormBlocks.
+int blocks_at_once(const void* kernel, int threads, size_t smem) {
+    static std::mutex lock;
+    static std::map<std::pair<const void*, size_t>, int> known;
+    std::lock_guard<std::mutex> guard(lock);
+    int& n = known[{kernel, smem}];
+    if (n == 0) {
+        int per_sm = 0;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1) { cudaGetLastError(); per_sm = 1; }
+        n = std::min(kNormBlocks, 148 * per_sm);
+    }
+    return n;
+}
+
 template <class T, int VEC, int NV, int WPR>
 void norm_go(const NormCall& a, cudaStream_t s) {
+    const auto kernel = norm_kernel<T, VEC, NV, WPR>;
     const int64_t blocks = (a.rows + RowGroup<WPR>::kRows - 1) / RowGroup<WPR>::kRows;
-    norm_kernel<T, VEC, NV, WPR><<<(unsigned)blocks, RowGroup<WPR>::kThreads, 0, s>>>((const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.beta, a.p32, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
+    // short calls: a block a row (group), without asking the runtime
+    const int64_t grid = blocks <= 148 ? blocks : std::min<int64_t>(blocks, blocks_at_once((const void*)kernel, RowGroup<WPR>::kThreads, 0));
+    kernel<<<(unsigned)grid, RowGroup<WPR>::kThreads, 0, s>>>((const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.beta, a.p32, a.pwide, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
 }
 template <class T>
 void norm_pick(const NormCall& a, cudaStream_t s) {
@@ -305,26 +398,27 @@ void norm_pick(const NormCall& a, cudaStream_t s) {
         const int n = (a.cols + V - 1) / V;
         if (n <= 32) return norm_go<T, V, 1, 1>(a, s);
         if (n <= 64) return norm_go<T, V, 2, 1>(a, s);
-        if (n <= 128) return norm_go<T, V, 4, 1>(a, s);
+        if (n <= 128) return norm_go<T, V, 1, 4>(a, s);
         if (n <= 256) return norm_go<T, V, 2, 4>(a, s);
         if (n <= 512) return norm_go<T, V, 2, 8>(a, s);
         if (n <= 1024) return norm_go<T, V, 4, 8>(a, s);
         if (n <= 2048) return norm_go<T, V, 4, 16>(a, s);
-        if (n <= 4096) return norm_go<T, V, 4, 32>(a, s);
     } else {
         if (a.cols <= 128) return norm_go<T, 1, 4, 1>(a, s);
         if (a.cols <= 1024) return norm_go<T, 1, 8, 4>(a, s);
+        if (a.cols <= 1536) return norm_go<T, 1, 6, 8>(a, s);
         if (a.cols <= 2048) return norm_go<T, 1, 8, 8>(a, s);
         if (a.cols <= 8192) return norm_go<T, 1, 16, 16>(a, s);
     }
-    norm_long_kernel<T><<<(unsigned)a.rows, 1024, 0, s>>>((const T*)a.x, a.ldx, a.cols, a.gamma, a.beta, a.p32, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
+    const auto kernel = wide_rows(a.x, a.ldx, sizeof(T)) && wide_rows(a.y, a.ldy, sizeof(T)) ? norm_long_kernel<T, V> : norm_long_kernel<T, 1>;
+    kernel<<<(unsigned)a.rows, 1024, 0, s>>>((const T*)a.x, a.ldx, a.cols, a.gamma, a.beta, a.p32, a.pwide, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
 }
 
 struct NormBackCall {
     const void *dy, *x, *gamma;
     int64_t lddy, ldx, rows;
     int cols;
-    bool p32;
+    bool p32, pwide;
     const float *mean, *rstd;
     void* dx;
     int64_t lddx;
@@ -335,9 +429,10 @@ struct NormBackCall {
 template <class T, int VEC, int NV, int WPR>
 int norm_back_go(const NormBackCall& a, cudaStream_t s) {
     constexpr int ROWS = RowGroup<WPR>::kRows;
-    const int blocks = (int)std::min<int64_t>((a.rows + ROWS - 1) / ROWS, kNormBlocks);
-    norm_backward_kernel<T, VEC, NV, WPR><<<(unsigned)blocks, RowGroup<WPR>::kThreads, ROWS > 1 ? 8 * (size_t)a.cols : 0, s>>>(
-        (const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.p32, a.mean, a.rstd, (T*)a.dx, a.lddx, a.partial);
+    const auto kernel = norm_backward_kernel<T, VEC, NV, WPR>;
+    const size_t smem = ROWS > 1 ? 8 * (size_t)a.cols : 0;
+    const int blocks = (int)std::min<int64_t>((a.rows + ROWS - 1) / ROWS, blocks_at_once((const void*)kernel, RowGroup<WPR>::kThreads, smem));
+    kernel<<<(unsigned)blocks, RowGroup<WPR>::kThreads, smem, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.p32, a.pwide, a.mean, a.rstd, (T*)a.dx, a.lddx, a.partial);
     return blocks;
 }
 template <class T>
@@ -351,14 +446,14 @@ int norm_back_rows(const NormBackCall& a, cudaStream_t s) {
         if (n <= 256) return norm_back_go<T, V, 1, 8>(a, s);
         if (n <= 512) return norm_back_go<T, V, 2, 8>(a, s);
         if (n <= 1024) return norm_back_go<T, V, 2, 16>(a, s);
-        if (n <= 2048) return norm_back_go<T, V, 2, 32>(a, s);
     } else {
         if (a.cols <= 128) return norm_back_go<T, 1, 4, 1>(a, s);
         if (a.cols <= 1024) return norm_back_go<T, 1, 8, 4>(a, s);
         if (a.cols <= 2048) return norm_back_go<T, 1, 8, 8>(a, s);
         if (a.cols <= 8192) return norm_back_go<T, 1, 16, 16>(a, s);
     }
-    norm_backward_long_kernel<T><<<(unsigned)a.rows, 1024, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.cols, a.gamma, a.p32, a.mean, a.rstd, (T*)a.dx, a.lddx);
+    const auto kernel = wide_rows(a.x, a.ldx, sizeof(T)) && wide_rows(a.dy, a.lddy, sizeof(T)) && wide_rows(a.dx, a.lddx, sizeof(T)) ? norm_backward_long_kernel<T, V> : norm_backward_long_kernel<T, 1>;
+    kernel<<<(unsigned)a.rows, 1024, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.cols, a.gamma, a.p32, a.pwide, a.mean, a.rstd, (T*)a.dx, a.lddx);
     const int blocks = (int)std::min<int64_t>((a.rows + 7) / 8, 64);
     if (a.partial) {
         norm_long_columns_kernel<T><<<dim3((unsigned)((a.cols + 31) / 32), (unsigned)blocks), 256, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.rows, a.cols, a.mean, a.rstd, a.partial);
@@ -371,8 +466,8 @@ void norm_back_pick(const NormBackCall& a, cudaStream_t s) {
     const int blocks = a.rows > 0 ? norm_back_rows<T>(a, s) : 0;
     if (a.rows > 0) ++g_kernel_launches;
     if (!a.dgamma && !a.dbeta) return;
-    norm_columns_kernel<T><<<(unsigned)((2ll * a.cols + 31) / 32), 256, 0, s>>>(a.partial, blocks, a.cols, a.p32, a.dgamma, a.dbeta);
-    ++g_kernel_launches;
+    // (behind the kernel that leaves the sums; with no rows it stands alone)
+    chain(norm_columns_kernel<T>, dim3((unsigned)((2ll * a.cols + 31) / 32)), 256, 0, s, a.rows == 0, (const float*)a.partial, blocks, a.cols, a.p32, a.dgamma, a.dbeta);
 }
 
 bool norm_sizes_ok(int64_t rows, int32_t cols, int32_t dtype, int32_t param_dtype) {
@@ -388,7 +483,7 @@ extern "C" int gad_layer_norm(const void* x, int64_t ldx, int64_t rows, int32_t 
     if (!norm_sizes_ok(rows, cols, dtype, param_dtype) || !(eps >= 0.f)) return GAD_ERR_ARG;
     if (rows == 0) return GAD_OK;
     if (!x || !y || !mean || !rstd || (ldx && ldx < cols) || ldy < cols) return GAD_ERR_ARG;
-    const NormCall a{x, gamma, beta, ldx, rows, cols, param_dtype == GAD_F32, eps, y, ldy, mean, rstd};
+    const NormCall a{x, gamma, beta, ldx, rows, cols, param_dtype == GAD_F32, (((uintptr_t)gamma | (uintptr_t)beta) & 15) == 0, eps, y, ldy, mean, rstd};
     const cudaStream_t s = (cudaStream_t)stream;
     if (dtype == GAD_F32) norm_pick<float>(a, s);
     else if (dtype == GAD_F16) norm_pick<__half>(a, s);
@@ -412,7 +507,7 @@ extern "C" int gad_layer_norm_backward(const void* dy, int64_t lddy, const void*
     size_t need = 0;
     gad_layer_norm_backward_workspace_bytes(rows, cols, &need);
     if ((dgamma || dbeta) && need > 0 && (!workspace || workspace_bytes < need)) return GAD_ERR_OOM;
-    const NormBackCall a{dy, x, gamma, lddy, ldx, rows, cols, param_dtype == GAD_F32, mean, rstd, dx, lddx, dgamma, dbeta, dgamma || dbeta ? (float*)workspace : nullptr};
+    const NormBackCall a{dy, x, gamma, lddy, ldx, rows, cols, param_dtype == GAD_F32, ((uintptr_t)gamma & 15) == 0, mean, rstd, dx, lddx, dgamma, dbeta, dgamma || dbeta ? (float*)workspace : nullptr};
     const cudaStream_t s = (cudaStream_t)stream;
     if (dtype == GAD_F32) norm_back_pick<float>(a, s);
     else if (dtype == GAD_F16) norm_back_pick<__half>(a, s);
