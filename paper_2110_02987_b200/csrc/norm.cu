@@ -38,10 +38,7 @@ __device__ __forceinline__ void load_param(const void* p, bool fp32, bool wide, 
                     v[j] = q.x; v[j + 1] = q.y; v[j + 2] = q.z; v[j + 3] = q.w;
                 }
             } else {
-                RowVec<T, VEC> q;
-                q.u = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p) + c);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) v[j] = to_float(q.e[j]);
+                unpack_vec<T, VEC>(*reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p) + c), v);
             }
             return;
         }
@@ -75,29 +72,53 @@ __device__ __forceinline__ void row_sum(float (&v)[NS], float* sm, int slot) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            float s = 0.f;
+            if constexpr (WPR % 4 == 0) {
+                float4 s = *reinterpret_cast<const float4*>(at + i * WPR);
 #pragma unroll
-            for (int k = 0; k < WPR; ++k) s += at[i * WPR + k];
-            v[i] = s;
+                for (int k = 4; k < WPR; k += 4) {
+                    const float4 q = *reinterpret_cast<const float4*>(at + i * WPR + k);
+                    s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
+                }
+                v[i] = (s.x + s.y) + (s.z + s.w);
+            } else {
+                float s = 0.f;
+#pragma unroll
+                for (int k = 0; k < WPR; ++k) s += at[i * WPR + k];
+                v[i] = s;
+            }
         }
     }
 }
 
+// Vector k of a row; without TAIL the row ends with a vector, which is then in it as a whole or not at all.
+template <class T, int VEC, bool TAIL>
+__device__ __forceinline__ void fetch_vec(const T* __restrict__ row, int c, int cols, RowVec<T, VEC>& v) {
+    if constexpr (VEC > 1 && !TAIL) v.u = c < cols ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
+    else load_raw<T, VEC>(row, c, cols, v);
+}
+template <class T, int VEC, bool TAIL>
+__device__ __forceinline__ void put_vec(T* __restrict__ row, int c, int cols, const float (&v)[VEC]) {
+    if constexpr (VEC > 1 && !TAIL) { if (c < cols) *reinterpret_cast<uint4*>(row + c) = pack_vec<T, VEC>(v); }
+    else store_vec<T, VEC>(row, c, cols, v);
+}
+
 // NV vectors of VEC values a thread hold a row: vector k of thread t starts at column (k * threads + t) * VEC.  A block takes every gridDim-th row (group of rows),
 // keeps gamma and beta in registers and has the next row on its way while it works on one.
-template <class T, int VEC, int NV, int WPR>
+template <class T, int VEC, int NV, int WPR, bool TAIL>
 __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* __restrict__ x, long long ldx, long long rows, int cols, const void* __restrict__ gamma,
                                                                        const void* __restrict__ beta, bool p32, bool pwide, float eps, T* __restrict__ y, long long ldy,
                                                                        float* __restrict__ mean, float* __restrict__ rstd) {
     constexpr int TPR = 32 * WPR, ROWS = RowGroup<WPR>::kRows;
-    __shared__ float sm[2 * WPR];
+    __shared__ __align__(16) float sm[2 * WPR];
     const int t = threadIdx.x % TPR;
     const long long step = (long long)gridDim.x * ROWS;
     long long r = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
     RowVec<T, VEC> next[NV];
+    const T* xr = x + r * ldx;
+    T* yr = y + r * ldy;
     if (r < rows)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) load_raw<T, VEC>(x + r * ldx, (k * TPR + t) * VEC, cols, next[k]);
+        for (int k = 0; k < NV; ++k) fetch_vec<T, VEC, TAIL>(xr, (k * TPR + t) * VEC, cols, next[k]);
     float g[NV][VEC], b[NV][VEC];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -109,25 +130,26 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* 
         float v[NV][VEC];
         float s[1] = {0.f};
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            to_floats<T, VEC>(next[k], v[k]);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                v[k][j] = to_float(next[k].e[j]);
-                s[0] += v[k][j];                 // (zeros behind the last column)
-            }
+            for (int j = 0; j < VEC; ++j) s[0] += v[k][j];   // (zeros behind the last column)
+        }
+        xr += step * ldx;
         if (r + step < rows)
 #pragma unroll
-            for (int k = 0; k < NV; ++k) load_raw<T, VEC>(x + (r + step) * ldx, (k * TPR + t) * VEC, cols, next[k]);
+            for (int k = 0; k < NV; ++k) fetch_vec<T, VEC, TAIL>(xr, (k * TPR + t) * VEC, cols, next[k]);
         row_sum<WPR, 1>(s, sm, 0);
         const float mu = s[0] * inv;
         float q[1] = {0.f};
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * TPR + t) * VEC;
+            const bool in = TAIL || c < cols;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                v[k][j] -= mu;
-                if (c + j < cols) q[0] = fmaf(v[k][j], v[k][j], q[0]);
+                v[k][j] = in ? v[k][j] - mu : 0.f;
+                if (!TAIL || c + j < cols) q[0] = fmaf(v[k][j], v[k][j], q[0]);
             }
         }
         row_sum<WPR, 1>(q, sm, 1);
@@ -135,11 +157,11 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* 
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * TPR + t) * VEC;
-            if (c >= cols) break;
 #pragma unroll
             for (int j = 0; j < VEC; ++j) v[k][j] = fmaf(v[k][j] * rs, g[k][j], b[k][j]);
-            store_vec<T, VEC>(y + r * ldy, c, cols, v[k]);
+            put_vec<T, VEC, TAIL>(yr, c, cols, v[k]);
         }
+        yr += step * ldy;
         if (t == 0) { mean[r] = mu; rstd[r] = rs; }
     }
 }
@@ -148,7 +170,7 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* 
 template <class T, int VEC>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const T* __restrict__ x, long long ldx, int cols, const void* __restrict__ gamma, const void* __restrict__ beta,
                                                          bool p32, bool pwide, float eps, T* __restrict__ y, long long ldy, float* __restrict__ mean, float* __restrict__ rstd) {
-    __shared__ float sm[2 * 32];
+    __shared__ __align__(16) float sm[2 * 32];
     const long long r = blockIdx.x;
     const T* xr = x + r * ldx;
     RowVec<T, VEC> v;
@@ -183,12 +205,12 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const T* __restrict__ x
 
 // Every block takes rows blockIdx, blockIdx + gridDim ... (several at once where a row is a warp's), the next one on its way, and keeps the sums of dy h and dy of
 // its columns in registers; they go to partial[block][2][cols], which norm_columns_kernel adds up in block order.
-template <class T, int VEC, int NV, int WPR>
+template <class T, int VEC, int NV, int WPR, bool TAIL>
 __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, long long rows,
                                                                                 int cols, const void* __restrict__ gamma, bool p32, bool pwide, const float* __restrict__ mean,
                                                                                 const float* __restrict__ rstd, T* __restrict__ dx, long long lddx, float* __restrict__ partial) {
     constexpr int TPR = 32 * WPR, ROWS = RowGroup<WPR>::kRows;
-    __shared__ float sm[2 * 2 * WPR];
+    __shared__ __align__(16) float sm[2 * 2 * WPR];
     extern __shared__ float cs[];                // with several rows a block: [2][cols]
     pdl_next();
     const int t = threadIdx.x % TPR;
@@ -196,13 +218,15 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(
     long long r = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
     RowVec<T, VEC> nd[NV], nx[NV];
     float nmu = 0.f, nrs = 0.f;
+    const T *dyr = dy + r * lddy, *xr = x + r * ldx;
+    T* dxr = dx + r * lddx;
     const auto fetch = [&](long long i) {
         nmu = mean[i];
         nrs = rstd[i];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            load_raw<T, VEC>(dy + i * lddy, (k * TPR + t) * VEC, cols, nd[k]);
-            load_raw<T, VEC>(x + i * ldx, (k * TPR + t) * VEC, cols, nx[k]);
+            fetch_vec<T, VEC, TAIL>(dyr, (k * TPR + t) * VEC, cols, nd[k]);
+            fetch_vec<T, VEC, TAIL>(xr, (k * TPR + t) * VEC, cols, nx[k]);
         }
     };
     if (r < rows) fetch(r);
@@ -219,12 +243,14 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(
         const float mu = nmu, rs = nrs;
         float d[NV][VEC], h[NV][VEC], s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            to_floats<T, VEC>(nd[k], d[k]);
+            to_floats<T, VEC>(nx[k], h[k]);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                d[k][j] = to_float(nd[k].e[j]);
-                h[k][j] = (to_float(nx[k].e[j]) - mu) * rs;   // (behind the last column d = 0: adds nothing)
-            }
+            for (int j = 0; j < VEC; ++j) h[k][j] = (h[k][j] - mu) * rs;   // (behind the last column d = 0: adds nothing)
+        }
+        dyr += step * lddy;
+        xr += step * ldx;
         if (r + step < rows) fetch(r + step);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
@@ -242,9 +268,10 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(
         for (int k = 0; k < NV; ++k) {
             const int c = (k * TPR + t) * VEC;
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) d[k][j] = (d[k][j] - m0 - h[k][j] * m1) * rs;
-            if (c < cols) store_vec<T, VEC>(dx + r * lddx, c, cols, d[k]);
+            for (int j = 0; j < VEC; ++j) d[k][j] = fmaf(-h[k][j], m1, d[k][j] - m0) * rs;
+            put_vec<T, VEC, TAIL>(dxr, c, cols, d[k]);
         }
+        dxr += step * lddx;
     }
     if (!partial) return;
     float* out = partial + (long long)blockIdx.x * 2 * cols;
@@ -281,7 +308,7 @@ template <class T, int VEC>
 __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, int cols,
                                                                   const void* __restrict__ gamma, bool p32, bool pwide, const float* __restrict__ mean,
                                                                   const float* __restrict__ rstd, T* __restrict__ dx, long long lddx) {
-    __shared__ float sm[2 * 2 * 32];
+    __shared__ __align__(16) float sm[2 * 2 * 32];
     const long long r = blockIdx.x;
     const float mu = mean[r], rs = rstd[r], inv = 1.f / (float)cols;
     RowVec<T, VEC> vd, vx;
@@ -332,25 +359,28 @@ __global__ void __launch_bounds__(256) norm_long_columns_kernel(const T* __restr
     }
 }
 
-// dgamma, dbeta [2 x cols] = the blocks' partial sums, in block order: 32 columns a block, each of its eight warps a run of blocks.
+// dgamma, dbeta [2 x cols] = the blocks' partial sums, in block order: 32 columns a block, each of its 32 warps a run of blocks.
 template <class T>
-__global__ void __launch_bounds__(256) norm_columns_kernel(const float* __restrict__ partial, int nblocks, int cols, bool p32, void* __restrict__ dgamma, void* __restrict__ dbeta) {
-    __shared__ float sm[8][32];
+__global__ void __launch_bounds__(1024) norm_columns_kernel(const float* __restrict__ partial, int nblocks, int cols, bool p32, void* __restrict__ dgamma, void* __restrict__ dbeta) {
+    __shared__ float sm[32][33];
     pdl_wait();
     after_wait(partial);
-    const int i = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
-    const int per = (nblocks + 7) / 8, lo = min(nblocks, w * per), hi = min(nblocks, lo + per);
+    const int lane = threadIdx.x & 31, i = blockIdx.x * 32 + lane, w = threadIdx.x >> 5;
+    const int per = (nblocks + 31) / 32, lo = min(nblocks, w * per), hi = min(nblocks, lo + per);
     float s = 0.f;
     if (i < 2 * cols)
 #pragma unroll 8
         for (int b = lo; b < hi; ++b) s += partial[(long long)b * 2 * cols + i];
-    sm[w][threadIdx.x & 31] = s;
+    sm[w][lane] = s;
     __syncthreads();
-    if (w || i >= 2 * cols) return;
-    s = 0.f;
-    for (int k = 0; k < 8; ++k) s += sm[k][threadIdx.x & 31];
-    void* out = i < cols ? dgamma : dbeta;
-    const int c = i < cols ? i : i - cols;
+    // warp w sums column w of the 32, a run a lane
+    s = sm[lane][w];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    const int j = blockIdx.x * 32 + w;
+    if (lane || j >= 2 * cols) return;
+    void* out = j < cols ? dgamma : dbeta;
+    const int c = j < cols ? j : j - cols;
     if (!out) return;
     if (p32) reinterpret_cast<float*>(out)[c] = s;
     else reinterpret_cast<T*>(out)[c] = from_float<T>(s);
@@ -385,7 +415,7 @@ int blocks_at_once(const void* kernel, int threads, size_t smem) {
 
 template <class T, int VEC, int NV, int WPR>
 void norm_go(const NormCall& a, cudaStream_t s) {
-    const auto kernel = norm_kernel<T, VEC, NV, WPR>;
+    const auto kernel = VEC > 1 && a.cols % VEC == 0 ? norm_kernel<T, VEC, NV, WPR, false> : norm_kernel<T, VEC, NV, WPR, true>;
     const int64_t blocks = (a.rows + RowGroup<WPR>::kRows - 1) / RowGroup<WPR>::kRows;
     // short calls: a block a row (group), without asking the runtime
     const int64_t grid = blocks <= 148 ? blocks : std::min<int64_t>(blocks, blocks_at_once((const void*)kernel, RowGroup<WPR>::kThreads, 0));
@@ -398,9 +428,9 @@ void norm_pick(const NormCall& a, cudaStream_t s) {
         const int n = (a.cols + V - 1) / V;
         if (n <= 32) return norm_go<T, V, 1, 1>(a, s);
         if (n <= 64) return norm_go<T, V, 2, 1>(a, s);
-        if (n <= 128) return norm_go<T, V, 1, 4>(a, s);
-        if (n <= 256) return norm_go<T, V, 2, 4>(a, s);
-        if (n <= 512) return norm_go<T, V, 2, 8>(a, s);
+        if (n <= 128) return norm_go<T, V, 4, 1>(a, s);
+        if (n <= 256) return norm_go<T, V, 4, 2>(a, s);
+        if (n <= 512) return norm_go<T, V, 4, 4>(a, s);
         if (n <= 1024) return norm_go<T, V, 4, 8>(a, s);
         if (n <= 2048) return norm_go<T, V, 4, 16>(a, s);
     } else {
@@ -429,7 +459,7 @@ struct NormBackCall {
 template <class T, int VEC, int NV, int WPR>
 int norm_back_go(const NormBackCall& a, cudaStream_t s) {
     constexpr int ROWS = RowGroup<WPR>::kRows;
-    const auto kernel = norm_backward_kernel<T, VEC, NV, WPR>;
+    const auto kernel = VEC > 1 && a.cols % VEC == 0 ? norm_backward_kernel<T, VEC, NV, WPR, false> : norm_backward_kernel<T, VEC, NV, WPR, true>;
     const size_t smem = ROWS > 1 ? 8 * (size_t)a.cols : 0;
     const int blocks = (int)std::min<int64_t>((a.rows + ROWS - 1) / ROWS, blocks_at_once((const void*)kernel, RowGroup<WPR>::kThreads, smem));
     kernel<<<(unsigned)blocks, RowGroup<WPR>::kThreads, smem, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.p32, a.pwide, a.mean, a.rstd, (T*)a.dx, a.lddx, a.partial);
@@ -442,8 +472,8 @@ int norm_back_rows(const NormBackCall& a, cudaStream_t s) {
         const int n = (a.cols + V - 1) / V;
         if (n <= 32) return norm_back_go<T, V, 1, 1>(a, s);
         if (n <= 64) return norm_back_go<T, V, 2, 1>(a, s);
-        if (n <= 128) return norm_back_go<T, V, 1, 4>(a, s);
-        if (n <= 256) return norm_back_go<T, V, 1, 8>(a, s);
+        if (n <= 128) return norm_back_go<T, V, 2, 2>(a, s);
+        if (n <= 256) return norm_back_go<T, V, 2, 4>(a, s);
         if (n <= 512) return norm_back_go<T, V, 2, 8>(a, s);
         if (n <= 1024) return norm_back_go<T, V, 2, 16>(a, s);
     } else {
@@ -467,7 +497,7 @@ void norm_back_pick(const NormBackCall& a, cudaStream_t s) {
     if (a.rows > 0) ++g_kernel_launches;
     if (!a.dgamma && !a.dbeta) return;
     // (behind the kernel that leaves the sums; with no rows it stands alone)
-    chain(norm_columns_kernel<T>, dim3((unsigned)((2ll * a.cols + 31) / 32)), 256, 0, s, a.rows == 0, (const float*)a.partial, blocks, a.cols, a.p32, a.dgamma, a.dbeta);
+    chain(norm_columns_kernel<T>, dim3((unsigned)((2ll * a.cols + 31) / 32)), 1024, 0, s, a.rows == 0, (const float*)a.partial, blocks, a.cols, a.p32, a.dgamma, a.dbeta);
 }
 
 bool norm_sizes_ok(int64_t rows, int32_t cols, int32_t dtype, int32_t param_dtype) {
