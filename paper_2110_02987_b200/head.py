@@ -14,7 +14,7 @@ from typing import NamedTuple, Optional
 from .binding import GAD_OK, GadError, load
 
 _DTYPES = {}     # torch dtype -> GAD_F32 / GAD_F16 / GAD_BF16, filled on first use (torch is imported late, as in the rest of the binding)
-_lib = None
+_lib = torch = None
 
 
 class _ClassLossArgs(C.Structure):
@@ -27,7 +27,7 @@ class _ClassLossArgs(C.Structure):
 
 
 def _load():
-    global _lib
+    global _lib, torch
     if _lib is None:
         import torch
         L = load()
@@ -72,35 +72,25 @@ def _vector(t, name, n, dtypes, device):
 
 @contextlib.contextmanager
 def _switch(device, stream):
-    import torch
+    """The tensors' device, and the stream asked for, made current: what is allocated then belongs to the stream that uses it."""
     with torch.cuda.device(device):
         if stream is None:
-            yield torch.cuda.current_stream(device)
+            yield
         else:
             if stream.device != device:
                 raise GadError(-1, "the stream belongs to another device")
-            with torch.cuda.stream(stream):     # what is allocated belongs to the stream that uses it
-                yield stream
+            with torch.cuda.stream(stream):
+                yield
 
 
-class _Here:
-    """The common case: the tensors' device is current and so is the stream."""
-
-    def __init__(self, stream):
-        self.stream = stream
-
-    def __enter__(self):
-        return self.stream
-
-    def __exit__(self, *a):
-        return False
+def _elsewhere(device, stream):
+    return stream is not None or device.index != torch.cuda.current_device()
 
 
-def _on(device, stream):
-    import torch
-    if stream is None and device.index == torch.cuda.current_device():
-        return _Here(torch.cuda.current_stream(device))
-    return _switch(device, stream)
+def _stream(device):
+    """Address of torch's current stream (its object costs 2 us to make, a tenth of a small call)."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _ck(rc, what):
@@ -113,30 +103,30 @@ def layer_norm(x, gamma=None, beta=None, *, eps=1e-5, stream=None):
 
     x float32, float16 or bfloat16 with any row stride; gamma and beta [cols] in x's type or float32 (both in the same), or None.
     y has x's type and is contiguous; mean and rstd are float32 [rows] (``layer_norm_backward`` takes them)."""
-    import torch
     L = _load()
     ldx = _matrix(x, "x")
     rows, cols = x.shape
-    params = gamma if gamma is not None else beta
-    ptype = x.dtype if params is None else params.dtype
-    if ptype is not x.dtype and ptype is not torch.float32:
+    dt, dev = x.dtype, x.device
+    ptype = dt if gamma is None and beta is None else (gamma if gamma is not None else beta).dtype
+    if ptype is not dt and ptype is not torch.float32:
         raise GadError(-1, "gamma and beta must have x's type or float32")
-    g = _vector(gamma, "gamma", cols, (ptype,), x.device)
-    b = _vector(beta, "beta", cols, (ptype,), x.device)
-    with _on(x.device, stream) as st:
-        y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-        stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-        at = stats.data_ptr()
-        _ck(L.gad_layer_norm(x.data_ptr(), ldx, rows, cols, _DTYPES[x.dtype], g, b, _DTYPES[ptype], eps, y.data_ptr(), cols, at, at + 4 * rows,
-                             st.cuda_stream), "gad_layer_norm")
-    return y, stats[0], stats[1]
+    g = _vector(gamma, "gamma", cols, (ptype,), dev)
+    b = _vector(beta, "beta", cols, (ptype,), dev)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return layer_norm(x, gamma, beta, eps=eps)
+    y = x.new_empty((rows, cols))
+    stats = x.new_empty((2, rows), dtype=torch.float32)
+    at = stats.data_ptr()
+    _ck(L.gad_layer_norm(x.data_ptr(), ldx, rows, cols, _DTYPES[dt], g, b, _DTYPES[ptype], eps, y.data_ptr(), cols, at, at + 4 * rows, _stream(dev)), "gad_layer_norm")
+    mean, rstd = stats.unbind(0)
+    return y, mean, rstd
 
 
 def layer_norm_backward(dy, x, mean, rstd, gamma=None, *, param_grads=True, stream=None):
     """gad_layer_norm_backward: ``(dx, dgamma, dbeta)`` for the upstream gradient ``dy`` of ``layer_norm(x, gamma, beta)``.
 
     dx has x's type, dgamma and dbeta gamma's (x's without one); with ``param_grads=False`` they are None."""
-    import torch
     L = _load()
     ldx = _matrix(x, "x")
     rows, cols = x.shape
@@ -151,18 +141,20 @@ def layer_norm_backward(dy, x, mean, rstd, gamma=None, *, param_grads=True, stre
     r = _vector(rstd, "rstd", rows, (torch.float32,), x.device)
     if m is None or r is None:
         raise GadError(-1, "mean and rstd of the forward pass are needed")
-    with _on(x.device, stream) as st:
-        dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-        dgamma = dbeta = ws = None
-        nbytes = C.c_size_t(0)
-        if param_grads:
-            both = torch.empty((2, cols), dtype=ptype, device=x.device)
-            dgamma, dbeta = both[0], both[1]
-            _ck(L.gad_layer_norm_backward_workspace_bytes(rows, cols, C.byref(nbytes)), "gad_layer_norm_backward_workspace_bytes")
-            ws = torch.empty(nbytes.value, dtype=torch.uint8, device=x.device)
-        _ck(L.gad_layer_norm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, rows, cols, _DTYPES[x.dtype], g, _DTYPES[ptype], m, r, dx.data_ptr(), cols,
-                                      dgamma.data_ptr() if param_grads else None, dbeta.data_ptr() if param_grads else None,
-                                      ws.data_ptr() if param_grads else None, nbytes.value, st.cuda_stream), "gad_layer_norm_backward")
+    if _elsewhere(x.device, stream):
+        with _switch(x.device, stream):
+            return layer_norm_backward(dy, x, mean, rstd, gamma, param_grads=param_grads)
+    dx = x.new_empty((rows, cols))
+    dgamma = dbeta = ws = None
+    nbytes = C.c_size_t(0)
+    at = [None, None, None]
+    if param_grads:
+        dgamma, dbeta = x.new_empty((2, cols), dtype=ptype).unbind(0)
+        _ck(L.gad_layer_norm_backward_workspace_bytes(rows, cols, C.byref(nbytes)), "gad_layer_norm_backward_workspace_bytes")
+        ws = x.new_empty(nbytes.value, dtype=torch.uint8)
+        at = [dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr()]
+    _ck(L.gad_layer_norm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, rows, cols, _DTYPES[x.dtype], g, _DTYPES[ptype], m, r, dx.data_ptr(), cols,
+                                  at[0], at[1], at[2], nbytes.value, _stream(x.device)), "gad_layer_norm_backward")
     return dx, dgamma, dbeta
 
 
@@ -188,14 +180,12 @@ class ClassLoss(NamedTuple):
 
 def _indices(t, name, shape, device):
     """Checks contiguous int32 / int64 indices; returns (address, bytes of one)."""
-    import torch
     if not (t.is_cuda and t.device == device and t.dtype in (torch.int32, torch.int64) and tuple(t.shape) == shape and t.is_contiguous()):
         raise GadError(-1, "%s must be a contiguous int32 or int64 tensor of shape %s on the same device" % (name, list(shape)))
     return t.data_ptr(), t.element_size()
 
 
 def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, row_weights, mean, scale, grads, stream):
-    import torch
     L = _load()
     ldh = _matrix(H, "H")
     N, D = H.shape
@@ -221,20 +211,22 @@ def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, 
     want = {"H", "W", "b"} if grads is True else set() if not grads else set(grads)
     if not want <= {"H", "W", "b"}:
         raise GadError(-1, "grads is True, False or some of H, W and b")
-    with _on(dev, stream) as st:
-        out = torch.empty(N + 1, dtype=torch.float32, device=dev)
-        status = torch.empty(1, dtype=torch.int32, device=dev)
-        dH = torch.empty((N, D), dtype=dt, device=dev) if "H" in want else None
-        dW = torch.empty((V, D), dtype=dt, device=dev) if "W" in want else None
-        db = torch.empty(V, dtype=dt, device=dev) if "b" in want and b is not None else None
-        at = out.data_ptr()
-        a = _ClassLossArgs(_DTYPES[dt], D, V, N, H.data_ptr(), ldh, W.data_ptr(), ldw, b, lab, lab_bytes, k, tc, tc_bytes, te_type, te, temperature,
-                           hard_weight, w, scale, 1 if mean else 0, at + 4 * N, at, dH.data_ptr() if dH is not None else None, D,
-                           dW.data_ptr() if dW is not None else None, D, db.data_ptr() if db is not None else None, status.data_ptr())
-        nbytes = C.c_size_t(0)
-        _ck(L.gad_class_loss_workspace_bytes(C.byref(a), C.byref(nbytes)), "gad_class_loss")
-        ws = torch.empty(nbytes.value, dtype=torch.uint8, device=dev)     # (torch's blocks start on 512 bytes)
-        _ck(L.gad_class_loss(C.byref(a), ws.data_ptr(), nbytes.value, st.cuda_stream), "gad_class_loss")
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, row_weights, mean, scale, grads, None)
+    out = H.new_empty(N + 1, dtype=torch.float32)
+    status = H.new_empty(1, dtype=torch.int32)
+    dH = H.new_empty((N, D)) if "H" in want else None
+    dW = W.new_empty((V, D)) if "W" in want else None
+    db = W.new_empty(V) if "b" in want and b is not None else None
+    at = out.data_ptr()
+    a = _ClassLossArgs(_DTYPES[dt], D, V, N, H.data_ptr(), ldh, W.data_ptr(), ldw, b, lab, lab_bytes, k, tc, tc_bytes, te_type, te, temperature,
+                       hard_weight, w, scale, 1 if mean else 0, at + 4 * N, at, dH.data_ptr() if dH is not None else None, D,
+                       dW.data_ptr() if dW is not None else None, D, db.data_ptr() if db is not None else None, status.data_ptr())
+    nbytes = C.c_size_t(0)
+    _ck(L.gad_class_loss_workspace_bytes(C.byref(a), C.byref(nbytes)), "gad_class_loss")
+    ws = H.new_empty(nbytes.value, dtype=torch.uint8)     # (torch's blocks start on 512 bytes)
+    _ck(L.gad_class_loss(C.byref(a), ws.data_ptr(), nbytes.value, _stream(dev)), "gad_class_loss")
     return ClassLoss(out[N:], out[:N], dH, dW, db, status)
 
 
