@@ -536,7 +536,9 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     tmem_wait_st();
                 }
             } else if (!wait_full()) break;
-            if constexpr (USE == kStats && !ADD_UP) {
+            if (!ADD_UP && rows <= 0) {                                     // (nothing of this warp's rows is asked for)
+                release();
+            } else if constexpr (USE == kStats && !ADD_UP) {
                 // the largest first, then everything relative to it; two blocks of columns in turn (half_w is 64 or 128)
                 const uint32_t at = tm_row + (uint32_t)(acc * ACC_COLS);
                 float u[32], v[32];

@@ -60,14 +60,15 @@ __device__ __forceinline__ void pack_row(const T* __restrict__ src, int cols, bo
         }
     } else {
         T* d = reinterpret_cast<T*>(dst) + at;
-        if (((uintptr_t)src & 15) == 0) {
-            const int n8 = cols >> 3;
-            for (int c = t; c < n8; c += threads)
-                reinterpret_cast<uint4*>(d)[c] = keep ? reinterpret_cast<const uint4*>(src)[c] : make_uint4(0u, 0u, 0u, 0u);
-            for (int c = 8 * n8 + t; c < cols; c += threads) d[c] = keep ? src[c] : from_float<T>(0.f);
-        } else {
-            for (int c = t; c < cols; c += threads) d[c] = keep ? src[c] : from_float<T>(0.f);
-        }
+        // in the widest words that the row starts on (the copy does on all)
+        const int wide = ((uintptr_t)src & 15) == 0 ? 8 : ((uintptr_t)src & 7) == 0 ? 4 : ((uintptr_t)src & 3) == 0 ? 2 : 1, n = cols / wide;
+        if (wide == 8)
+            for (int c = t; c < n; c += threads) reinterpret_cast<uint4*>(d)[c] = keep ? reinterpret_cast<const uint4*>(src)[c] : make_uint4(0u, 0u, 0u, 0u);
+        else if (wide == 4)
+            for (int c = t; c < n; c += threads) reinterpret_cast<uint2*>(d)[c] = keep ? reinterpret_cast<const uint2*>(src)[c] : make_uint2(0u, 0u);
+        else if (wide == 2)
+            for (int c = t; c < n; c += threads) reinterpret_cast<uint32_t*>(d)[c] = keep ? reinterpret_cast<const uint32_t*>(src)[c] : 0u;
+        for (int c = (wide > 1 ? wide * n : 0) + t; c < cols; c += threads) d[c] = keep ? src[c] : from_float<T>(0.f);
     }
 }
 

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import functools
 from typing import NamedTuple, Optional
 
 from .binding import GAD_OK, GadError, load
@@ -123,6 +124,13 @@ def layer_norm(x, gamma=None, beta=None, *, eps=1e-5, stream=None):
     return y, mean, rstd
 
 
+@functools.lru_cache(maxsize=256)
+def _norm_workspace(rows, cols):
+    n = C.c_size_t(0)
+    _ck(_load().gad_layer_norm_backward_workspace_bytes(rows, cols, C.byref(n)), "gad_layer_norm_backward_workspace_bytes")
+    return n.value
+
+
 def layer_norm_backward(dy, x, mean, rstd, gamma=None, *, param_grads=True, stream=None):
     """gad_layer_norm_backward: ``(dx, dgamma, dbeta)`` for the upstream gradient ``dy`` of ``layer_norm(x, gamma, beta)``.
 
@@ -146,15 +154,14 @@ def layer_norm_backward(dy, x, mean, rstd, gamma=None, *, param_grads=True, stre
             return layer_norm_backward(dy, x, mean, rstd, gamma, param_grads=param_grads)
     dx = x.new_empty((rows, cols))
     dgamma = dbeta = ws = None
-    nbytes = C.c_size_t(0)
-    at = [None, None, None]
+    nbytes, at_g, at_b, at_ws = 0, None, None, None
     if param_grads:
         dgamma, dbeta = x.new_empty((2, cols), dtype=ptype).unbind(0)
-        _ck(L.gad_layer_norm_backward_workspace_bytes(rows, cols, C.byref(nbytes)), "gad_layer_norm_backward_workspace_bytes")
-        ws = x.new_empty(nbytes.value, dtype=torch.uint8)
-        at = [dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr()]
+        nbytes = _norm_workspace(rows, cols)
+        ws = x.new_empty(nbytes, dtype=torch.uint8)
+        at_g, at_b, at_ws = dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr()
     _ck(L.gad_layer_norm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, rows, cols, _DTYPES[x.dtype], g, _DTYPES[ptype], m, r, dx.data_ptr(), cols,
-                                  at[0], at[1], at[2], nbytes.value, _stream(x.device)), "gad_layer_norm_backward")
+                                  at_g, at_b, at_ws, nbytes, _stream(x.device)), "gad_layer_norm_backward")
     return dx, dgamma, dbeta
 
 
