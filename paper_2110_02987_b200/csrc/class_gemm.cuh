@@ -55,6 +55,7 @@ struct TileArgs {
     float sc, inv_t;           // log2(e) (/ T with one softmax), 1 / T of the second
     const int2* targets;       // [M x ntargets] (class, weight), classes ascending
     int ntargets;
+    const uint16_t* starts;    // [M x 2 tiles_n] a row's first target at or behind the first column of each half tile; null with one target
     float4* stats;             // [2 tiles_n x M]
     int save;                  // SaveAs
     // what is written
@@ -384,8 +385,9 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             const bool rv = row < a.M;
             const int tile_c = t.n * a.width + half * half_w;               // first column of this warp
             float m2 = -INFINITY, s1 = 0.f, s2 = 0.f, dot = 0.f;
-            int e = 0, next = INT_MAX;
-            const int2* tg = nullptr;
+            int e = 0;
+            int2 cur = make_int2(INT_MAX, 0), nxt = cur;                    // the row's next target among these columns, and the one behind it
+            const int2* tg = a.targets + (long long)(rv ? row : 0) * a.ntargets;
             if (USE == kStats) {
                 __syncwarp();                                               // the previous tile's biases have been read
                 for (int j = lane; j < half_w; j += 32) {
@@ -398,13 +400,10 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 }
                 __syncwarp();
                 if (rv) {
-                    tg = a.targets + (long long)row * a.ntargets;
-                    int hi = a.ntargets;                                    // the first target at or behind this warp's columns
-                    while (e < hi) {
-                        const int mid = (e + hi) >> 1;
-                        if (tg[mid].x < tile_c) e = mid + 1; else hi = mid;
-                    }
-                    if (e < a.ntargets) next = tg[e].x;
+                    if (a.starts) e = a.starts[(long long)row * (2 * a.tiles_n) + 2 * t.n + half];
+                    if (e < a.ntargets) cur = tg[e];
+                    if (e + 1 < a.ntargets) nxt = tg[e + 1];
+                    if (cur.x < tile_c) cur.x = INT_MAX;                    // (one target, in front of these columns)
                 }
             }
             // No bias and nothing but classes: the logit and its distance from the largest are one multiply-add.
@@ -447,9 +446,11 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     }
                     s1 += (p1[0] + p1[1]) + (p1[2] + p1[3]);
                     if (NL == 2) s2 += (p2[0] + p2[1]) + (p2[2] + p2[3]);
-                    while (next < tile_c + c0 + 32) {
-                        dot = fmaf(__int_as_float(tg[e].y), pick(v, next - tile_c - c0) + base, dot);
-                        next = ++e < a.ntargets ? tg[e].x : INT_MAX;
+                    while (cur.x < tile_c + c0 + 32) {                      // (the target that is loaded here is not looked at before the next but one)
+                        dot = fmaf(__int_as_float(cur.y), pick(v, cur.x - tile_c - c0) + base, dot);
+                        cur = nxt;
+                        ++e;
+                        nxt = e + 1 < a.ntargets ? tg[e + 1] : make_int2(INT_MAX, 0);
                     }
                     if (a.save == kSaveCode) {
                         // rounded by the addition of 2^23, whose sum has the whole number in its low bits

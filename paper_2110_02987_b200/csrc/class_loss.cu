@@ -80,6 +80,7 @@ struct RowArgs {
     float hard, temperature;
     void* Hp; int64_t ldp, part_stride;
     int2* targets; int ntargets;
+    uint16_t* starts; int nstarts, start_w;               // [rows x nstarts] first target at or behind every start_w-th class
     float4* rowk;
     int64_t rows;
     struct RowShare* shares; unsigned* ticket;
@@ -122,6 +123,7 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
     extern __shared__ int sm_rows[];
     int* idx = sm_rows;                                   // [ntargets]
     float* tau = reinterpret_cast<float*>(sm_rows + a.ntargets);
+    int* sorted = sm_rows + 2 * a.ntargets;
     __shared__ float red[2][kRowThreads / 32];
     __shared__ int bad, soft_any;
     const int64_t r = blockIdx.x;
@@ -189,6 +191,18 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
         for (int i = 0; i < a.ntargets; ++i) at += idx[i] < c || (idx[i] == c && i < j);
         const float tv = tau[j];
         a.targets[r * a.ntargets + at] = make_int2(c, __float_as_int(c == INT_MAX ? 0.f : tv));
+        sorted[at] = c;
+    }
+    if (a.starts) {
+        __syncthreads();
+        for (int b = t; b < a.nstarts; b += kRowThreads) {
+            int e = 0, hi = a.ntargets;
+            while (e < hi) {
+                const int mid = (e + hi) >> 1;
+                if (sorted[mid] < b * a.start_w) e = mid + 1; else hi = mid;
+            }
+            a.starts[r * a.nstarts + b] = (uint16_t)e;
+        }
     }
     const float weight = counts ? (a.weights ? a.weights[r] : 1.f) : 0.f;
     if (t == 0) a.rowk[r] = make_float4(ha, hb * tt * tt, counts && bad ? NAN : hb * tt * tt * ent, weight);
@@ -687,7 +701,7 @@ struct ClassPlan {
     int64_t ldp, ldg;                // row lengths of the packed operands, and of z and G
     int64_t block;                   // rows a block
     int nblocks;
-    int64_t o_hp, o_wp, o_targets, o_rowk, o_rowc, o_stats, o_rshares, o_lshares, o_scal, o_z, o_g, o_colsum, o_dbsum, o_slots, o_sums, total;
+    int64_t o_hp, o_wp, o_targets, o_starts, o_rowk, o_rowc, o_stats, o_rshares, o_lshares, o_scal, o_z, o_g, o_colsum, o_dbsum, o_slots, o_sums, total;
 };
 
 ClassPlan plan_class(const gad_class_loss_args& a) {
@@ -721,6 +735,7 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     p.o_hp = room(2 * p.parts * N * p.ldp);
     p.o_wp = p.pack_w ? room(2 * p.parts * (int64_t)V * p.ldp) : 0;
     p.o_targets = room(8 * N * p.ntargets);
+    p.o_starts = p.ntargets > 1 && !p.few ? room(2 * N * 2 * p.tiles_v) : 0;
     p.o_rowk = room(16 * N);
     p.o_rshares = room((int64_t)sizeof(RowShare) * N);
     p.o_lshares = room((int64_t)sizeof(double) * ((N + kFinishRows - 1) / kFinishRows));
@@ -798,9 +813,11 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
     ra.tclasses = a.target_classes; ra.tclass_bytes = a.target_bytes; ra.teacher = a.teacher; ra.teacher_type = a.teacher_dtype; ra.k = a.k;
     ra.weights = a.row_weights; ra.hard = a.k > 0 ? (a.labels ? a.hard_weight : 0.f) : 1.f; ra.temperature = T0;
     ra.Hp = Hp; ra.ldp = p.ldp; ra.part_stride = N * p.ldp; ra.targets = targets; ra.ntargets = p.ntargets; ra.rowk = rowk;
+    ra.starts = p.o_starts ? reinterpret_cast<uint16_t*>(ws + p.o_starts) : nullptr; ra.nstarts = 2 * p.tiles_v; ra.start_w = p.width_v / 2;
+   
     ra.rows = N; ra.shares = reinterpret_cast<RowShare*>(ws + p.o_rshares); ra.ticket = reinterpret_cast<unsigned*>(scal + 8); ra.status = a.status;
     const int nrshares = (int)(a.k > 0 ? N : (N + 7) / 8);
-    GAD_TRY(a.k > 0 ? chain(class_rows_kernel<T>, dim3((unsigned)N), kRowThreads, 8 * (size_t)p.ntargets, s, true, ra)
+    GAD_TRY(a.k > 0 ? chain(class_rows_kernel<T>, dim3((unsigned)N), kRowThreads, 12 * (size_t)p.ntargets, s, true, ra)
                     : chain(class_label_rows_kernel<T>, dim3((unsigned)nrshares), 256, 0, s, true, ra));
     const void* Wo = a.W;
     int64_t ldw = a.ldw;
@@ -831,7 +848,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         z.bias = a.bias; z.bias_type = a.dtype;
         z.sc = kLog2e * (p.nl == 1 && a.k > 0 && ra.hard < 1.f ? 1.f / T0 : 1.f);
         z.inv_t = 1.f / T0;
-        z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.stats = stats;
+        z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.starts = ra.starts ? ra.starts + r0 * ra.nstarts : nullptr; z.stats = stats;
         z.save = p.save; z.C = ws + p.o_z; z.ldc = p.ldg;
         int nparts = 2 * p.tiles_v;
         if (p.few) {
