@@ -44,7 +44,7 @@ struct TileArgs {
     int shares, kb_share;
     int group;                 // row tiles that are gone through together, for the L2
     int pairs;                 // products of operand parts: 1, or 6 for operands in three parts
-    int chunk;                 // ADD_UP: blocks of the largest product that are summed in tensor memory before the sum moves to registers
+    int chunk;                 // ADD_UP: blocks that are summed in tensor memory (of operands in parts all products, the smallest first) before the sum moves to registers
     int a_row0;                // first row of A (K-major)
     int b_row0;                // first row of B (MN-major)
     int bf16;                  // operand type: 1 bfloat16, 0 fp16
@@ -252,7 +252,8 @@ __device__ __forceinline__ TileAt tile_at(const TileArgs& a, long long u) {
 // USE as above; A_MN, B_MN: operand is MN-major; T: type of the result; NL: softmaxes (temperatures) at once.
 // ADD_UP: the tensor core cuts its accumulator off at every addition (it does not round), half a step a time and always towards zero: long reductions lose
 // 5e-9 of their value per 16 terms (128 000 x 4096 logits of one row: loss off by 1.3e-6).  Where a result is wanted to fp32 accuracy the
-// reduction is cut into chunks whose sums the draining threads add up in registers (of operands in parts the small products are one chunk: what they lose is small).
+// reduction is cut into chunks whose sums the draining threads add up in registers.  Of operands in parts a chunk has all products, the smallest first (what they lose is
+// small), so that the parts come from HBM once: with the products one behind the other over the whole reduction G was read six times (8192 x 4096 x 256: 92 us).
 // Logits are then taken in tiles 128 columns wide: 64 sums a thread, four accumulators, three of which fill while the sums of a tile are worked on.  Gradients, with many
 // chunks a tile, keep tiles of 256: at 128 the operands come from L2 half as fast again as it can (8192 x 256 x 4096 fp32: 157 us instead of 92).
 template <int USE, bool A_MN, bool B_MN, class T, int NL, bool ADD_UP>
@@ -301,27 +302,29 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
             const TileAt t = tile_at(a, u);
             const int ra = t.m * CT_M + (int)rank * CT_H, rb = t.n * a.width + (int)rank * half_w;
-            for (int p = 0; p < a.pairs && ok; ++p) {
-                int za, zb;
-                part_pair(p, a.pairs, za, zb);
-                for (int kb = t.kb0; kb < t.kb0 + t.nkb; ++kb) {
-                    if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, 31))) break;
-                    mbar_expect_tx(full(stage), (uint32_t)(CT_H + half_w) * (CT_K * 2));
-                    const uint32_t base = sm_addr + stage * CT_STAGE;
-                    if (A_MN) {
-                        tma_load_3d(base, &tmA, ra, kb * CT_K, za, full(stage));
-                        tma_load_3d(base + 8192, &tmA, ra + 64, kb * CT_K, za, full(stage));
-                    } else {
-                        tma_load_3d(base, &tmA, kb * CT_K, a.a_row0 + ra, za, full(stage));
+            const int group = ADD_UP ? a.chunk : t.nkb;
+            for (int g = 0; g < t.nkb && ok; g += group)
+                for (int p = 0; p < a.pairs && ok; ++p) {
+                    int za, zb;
+                    part_pair(p, a.pairs, za, zb);
+                    for (int kb = t.kb0 + g; kb < t.kb0 + min(g + group, t.nkb); ++kb) {
+                        if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, 31))) break;
+                        mbar_expect_tx(full(stage), (uint32_t)(CT_H + half_w) * (CT_K * 2));
+                        const uint32_t base = sm_addr + stage * CT_STAGE;
+                        if (A_MN) {
+                            tma_load_3d(base, &tmA, ra, kb * CT_K, za, full(stage));
+                            tma_load_3d(base + 8192, &tmA, ra + 64, kb * CT_K, za, full(stage));
+                        } else {
+                            tma_load_3d(base, &tmA, kb * CT_K, a.a_row0 + ra, za, full(stage));
+                        }
+                        if (B_MN) {
+                            for (int j = 0; j < half_w; j += 64) tma_load_3d(base + CT_OPERAND + j * 128, &tmB, rb + j, a.b_row0 + kb * CT_K, zb, full(stage));
+                        } else {
+                            tma_load_3d(base + CT_OPERAND, &tmB, kb * CT_K, rb, zb, full(stage));
+                        }
+                        if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
                     }
-                    if (B_MN) {
-                        for (int j = 0; j < half_w; j += 64) tma_load_3d(base + CT_OPERAND + j * 128, &tmB, rb + j, a.b_row0 + kb * CT_K, zb, full(stage));
-                    } else {
-                        tma_load_3d(base + CT_OPERAND, &tmB, kb * CT_K, rb, zb, full(stage));
-                    }
-                    if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
                 }
-            }
         }
     } else if (warp == 1 && rank == 1) {
         // ---------------- the other CTA's stages: the leader is told of each ----------------
@@ -344,14 +347,14 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         constexpr uint32_t stepA = A_MN ? 128 : 2, stepB = B_MN ? 128 : 2;    // 16 values of the reduction: 16 rows of 128 bytes, or 32 bytes of a row
         bool ok = true;
         for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
-            const int nkb = tile_at(a, u).nkb, steps = nkb * a.pairs, small = nkb * (a.pairs - 1);
+            const int steps = tile_at(a, u).nkb * a.pairs;
             int left = 0;                                          // stages until this accumulator is full
             for (int i = 0; i < steps; ++i) {
                 const bool first = left == 0;
                 if (first) {
                     if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 32)))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    left = !ADD_UP ? steps : i < small ? small : min(a.chunk, steps - i);
+                    left = ADD_UP ? min(a.chunk * a.pairs, steps - i) : steps;
                 }
                 const uint32_t d = tmem_base + (uint32_t)(acc * ACC_COLS);
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag, a.err, 33) && mbar_wait<true>(pfull(stage), phase, abort_flag, a.err, 35)))) break;
@@ -503,7 +506,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 return ok;
             };
             if constexpr (ADD_UP) {
-                const int chunks = (a.pairs > 1) + (t.nkb + a.chunk - 1) / a.chunk;
+                const int chunks = (t.nkb + a.chunk - 1) / a.chunk;
                 constexpr int BLOCKS = USE == kStats ? 2 : 4;               // of 32 columns a warp has
                 float sum[BLOCKS][32];
 #pragma unroll
