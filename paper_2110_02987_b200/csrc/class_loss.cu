@@ -630,7 +630,7 @@ __global__ void __launch_bounds__(256) class_join_kernel(const TileArgs a) {
     const TileAt t = tile_at(a, a.whole + (long long)i * a.shares);
     const int row = t.m * CT_M + r, c = t.n * a.width + x;
     if (row >= a.M || c >= a.N) return;
-    const float factor = a.scal[1];
+    const float factor = a.scal[1] * a.whole_sum;
     const float* slot = a.slots + ((long long)i * a.shares * CT_M + r) * a.width + x;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -781,6 +781,7 @@ template <bool A_MN, class T>
 cudaError_t go_out(const CUtensorMap& A, const CUtensorMap& B, TileArgs a, cudaStream_t s) {
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, rest = tiles % kPairs;
     a.whole = (int)tiles; a.shares = 1; a.kb_share = a.nkb;
+    a.whole_sum = sizeof(T) == 4 ? cut_back(std::min(a.nkb, a.chunk)) : 1.f;   // (below what the other types round)
     if (rest) {
         const int want = (int)std::min<int64_t>(kPairs / rest, (int64_t)a.nkb * a.pairs / 8);
         if (want > 1) {
@@ -846,7 +847,8 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         z.N = V; z.tiles_n = p.tiles_v; z.width = p.width_v; z.nkb = (D + CT_K - 1) / CT_K; z.whole = z.tiles_m * z.tiles_n; z.shares = 1; z.kb_share = z.nkb;
         z.group = 32; z.a_row0 = (int)r0;
         z.bias = a.bias; z.bias_type = a.dtype;
-        z.sc = kLog2e * (p.nl == 1 && a.k > 0 && ra.hard < 1.f ? 1.f / T0 : 1.f);
+        z.unit = kLog2e * (p.nl == 1 && a.k > 0 && ra.hard < 1.f ? 1.f / T0 : 1.f);
+        z.sc = z.unit * cut_back(std::min(z.nkb, p.add_up ? z.chunk : z.nkb));
         z.inv_t = 1.f / T0;
         z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.starts = ra.starts ? ra.starts + r0 * ra.nstarts : nullptr; z.stats = stats;
         z.save = p.save; z.C = ws + p.o_z; z.ldc = p.ldg;
@@ -854,14 +856,14 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         if (p.few) {
             FewArgs w{};
             w.H = a.H; w.ldh = a.ldh; w.W = a.W; w.ldw = a.ldw; w.rows = nr; w.cols = D; w.classes = V; w.bias = a.bias; w.targets = targets; w.ntargets = p.ntargets; w.rowk = rowk;
-            w.sc = z.sc; w.inv_t = z.inv_t; w.z = p.grads ? reinterpret_cast<float*>(z.C) : nullptr; w.ldz = p.ldg; w.stats = stats;
+            w.sc = z.unit; w.inv_t = z.inv_t; w.z = p.grads ? reinterpret_cast<float*>(z.C) : nullptr; w.ldz = p.ldg; w.stats = stats;
             nparts = (int)std::min<int64_t>(kFewBlocks, (p.ldg + 31) / 32);
             const bool wide = ((uintptr_t)a.W & 15) == 0 && (a.ldw * (int64_t)sizeof(T)) % 16 == 0;
             GAD_TRY(p.nl == 2 ? (wide ? few_launch<T, 2, true>(w, few_smem(a), nparts, s) : few_launch<T, 2, false>(w, few_smem(a), nparts, s))
                               : (wide ? few_launch<T, 1, true>(w, few_smem(a), nparts, s) : few_launch<T, 1, false>(w, few_smem(a), nparts, s)));
         } else GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, p.add_up, s) : go_stats<1>(mapH, mapW, z, p.add_up, s));
         FinishArgs f{};
-        f.stats = stats; f.parts = nparts; f.rows = nr; f.rowk = rowk + r0; f.sc = z.sc; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
+        f.stats = stats; f.parts = nparts; f.rows = nr; f.rowk = rowk + r0; f.sc = z.unit; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
         f.shares = reinterpret_cast<double*>(ws + p.o_lshares); f.share0 = (int)(r0 / kFinishRows); f.nshares = (int)((N + kFinishRows - 1) / kFinishRows);
         f.row_shares = ra.shares; f.nrow_shares = nrshares; f.ticket = ra.ticket; f.scale = a.scale; f.mean = a.mean; f.first = b == 0; f.final = b == p.nblocks - 1;
         f.scal = scal; f.loss = a.loss;
