@@ -956,5 +956,9 @@ extern "C" int gad_class_loss(const gad_class_loss_args* args, void* workspace, 
     if (a.rows == 0) return a.dtype == GAD_F32 ? run_empty<float>(a, s) : a.dtype == GAD_F16 ? run_empty<__half>(a, s) : run_empty<__nv_bfloat16>(a, s);
     if (!a.H || !a.row_loss || (a.k == 0 && !a.labels) || (a.k > 0 && (!a.target_classes || !a.teacher))) return GAD_ERR_ARG;
     if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < (size_t)plan_class(a).total) return GAD_ERR_OOM;
-    return a.dtype == GAD_F32 ? run_class<float>(a, (uint8_t*)workspace, s) : a.dtype == GAD_F16 ? run_class<__half>(a, (uint8_t*)workspace, s) : run_class<__nv_bfloat16>(a, (uint8_t*)workspace, s);
+    try {
+        return a.dtype == GAD_F32 ? run_class<float>(a, (uint8_t*)workspace, s) : a.dtype == GAD_F16 ? run_class<__half>(a, (uint8_t*)workspace, s) : run_class<__nv_bfloat16>(a, (uint8_t*)workspace, s);
+    } catch (...) {   // (the table of configured kernels could not grow)
+        return GAD_ERR_OOM;
+    }
 }

@@ -515,9 +515,13 @@ extern "C" int gad_layer_norm(const void* x, int64_t ldx, int64_t rows, int32_t 
     if (!x || !y || !mean || !rstd || (ldx && ldx < cols) || ldy < cols) return GAD_ERR_ARG;
     const NormCall a{x, gamma, beta, ldx, rows, cols, param_dtype == GAD_F32, (((uintptr_t)gamma | (uintptr_t)beta) & 15) == 0, eps, y, ldy, mean, rstd};
     const cudaStream_t s = (cudaStream_t)stream;
-    if (dtype == GAD_F32) norm_pick<float>(a, s);
-    else if (dtype == GAD_F16) norm_pick<__half>(a, s);
-    else norm_pick<__nv_bfloat16>(a, s);
+    try {
+        if (dtype == GAD_F32) norm_pick<float>(a, s);
+        else if (dtype == GAD_F16) norm_pick<__half>(a, s);
+        else norm_pick<__nv_bfloat16>(a, s);
+    } catch (...) {   // (the table of occupancies could not grow)
+        return GAD_ERR_OOM;
+    }
     ++g_kernel_launches;
     return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
 }
@@ -539,8 +543,12 @@ extern "C" int gad_layer_norm_backward(const void* dy, int64_t lddy, const void*
     if ((dgamma || dbeta) && need > 0 && (!workspace || workspace_bytes < need)) return GAD_ERR_OOM;
     const NormBackCall a{dy, x, gamma, lddy, ldx, rows, cols, param_dtype == GAD_F32, ((uintptr_t)gamma & 15) == 0, mean, rstd, dx, lddx, dgamma, dbeta, dgamma || dbeta ? (float*)workspace : nullptr};
     const cudaStream_t s = (cudaStream_t)stream;
-    if (dtype == GAD_F32) norm_back_pick<float>(a, s);
-    else if (dtype == GAD_F16) norm_back_pick<__half>(a, s);
-    else norm_back_pick<__nv_bfloat16>(a, s);
+    try {
+        if (dtype == GAD_F32) norm_back_pick<float>(a, s);
+        else if (dtype == GAD_F16) norm_back_pick<__half>(a, s);
+        else norm_back_pick<__nv_bfloat16>(a, s);
+    } catch (...) {   // (the table of occupancies could not grow)
+        return GAD_ERR_OOM;
+    }
     return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
 }

@@ -132,7 +132,8 @@ def compare(got, ref, s, T=1.0):
         assert off <= tol + sub + 1e-37, (name, off / max(want.norm().item(), 1e-300), tol / max(want.norm().item(), 1e-300))
 
 
-CLASS_SHAPES = [(1, 1, 1), (1, 64, 2), (5, 7, 3), (3, 72, 128), (130, 100, 129), (257, 64, 300), (2, 4096, 1000), (777, 500, 2049), (300, 130, 47), (1, 256, 40000), (4, 1001, 700), (8, 328, 5000), (7, 6000, 90)]
+CLASS_SHAPES = [(1, 1, 1), (1, 64, 2), (5, 7, 3), (3, 72, 128), (130, 100, 129), (257, 64, 300), (2, 4096, 1000), (777, 500, 2049), (300, 130, 47), (1, 256, 40000), (4, 1001, 700), (8, 328, 5000), (7, 6000, 90),
+                (20, 2500, 300), (130, 640, 257), (9, 64, 1 << 20)]
 
 
 @gpu
@@ -151,7 +152,8 @@ def test_class_loss(N, D, V, dtype):
 @gpu
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
 @pytest.mark.parametrize("N,D,V,k,T,a", [(1, 64, 2, 1, 1.0, 0.0), (5, 7, 3, 3, 2.0, 0.0), (130, 100, 129, 17, 2.0, 0.3), (257, 64, 300, 130, 1.0, 0.5), (40, 512, 10007, 64, 0.5, 0.25),
-                                         (33, 96, 2000, 1024, 4.0, 0.1), (64, 128, 500, 8, 3.0, 1.0)])
+                                         (33, 96, 2000, 1024, 4.0, 0.1), (64, 128, 500, 8, 3.0, 1.0),
+                                         (50, 72, 600, 5, 0.25, 0.5), (6, 200, 900, 7, 2.0, 0.5), (21, 2500, 300, 40, 1.5, 0.5)])
 def test_distill_loss(N, D, V, k, T, a, dtype):
     for bias, weights, ignored in ((False, False, 0.0), (True, True, 0.4)):
         s = make(N, D, V, dtype, 2, k=k, bias=bias, weights=weights, ignored=ignored)
@@ -303,6 +305,63 @@ def test_equal_bits_streams_and_graphs():
     kept = [t.clone() for t in out]
     want = pkg.distill_loss(**s)
     assert all(torch.equal(u, v) for u, v in zip(kept, want))
+
+
+@gpu
+def test_rows_that_are_one_row():
+    """H broadcast over the rows (a row stride of zero): dH is that of every row."""
+    import torch
+    for N in (5, 300):
+        s = make(N, 64, 90, "bfloat16", 14)
+        one = dict(s, H=s["H"][:1].expand(N, 64))
+        whole = dict(s, H=one["H"].contiguous())
+        assert all(torch.equal(u, v) for u, v in zip(pkg.class_loss(**one), pkg.class_loss(**whole)) if u is not None)
+
+
+@gpu
+def test_first_call_of_a_process_inside_a_capture():
+    import subprocess
+    import sys
+    code = """if 1:
+        import torch, paper_2110_02987_b200 as pkg
+        x = torch.randn(300, 64, device="cuda").bfloat16(); W = torch.randn(500, 64, device="cuda").bfloat16()
+        y = torch.randint(0, 500, (300,), device="cuda"); gamma = torch.rand(64, device="cuda")
+        def step():
+            h, mean, rstd = pkg.layer_norm(x, gamma)
+            r = pkg.class_loss(h, W, y)
+            return (r.loss, r.dW) + pkg.layer_norm_backward(r.dH, x, mean, rstd, gamma)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step()
+        g.replay(); torch.cuda.synchronize()
+        kept = [t.clone() for t in out]
+        assert all(torch.equal(u, v) for u, v in zip(kept, step()))
+        print("same")
+    """
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=entry.ROOT)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
+def test_kernels_of_a_chain_wait_for_the_one_in_front():
+    """Every kernel that is launched to come up before the one in front of it has ended has to wait for it; a missing wait shows on the GPU only where the overlap happens."""
+    import os
+    import re
+    from test_launch_contract import closing, kernels, CSRC
+    text = "".join(open(os.path.join(CSRC, f)).read() for f in ("class_gemm.cuh", "class_loss.cu", "norm.cu"))
+    text = re.sub(r"//[^\n]*", "", text)
+    bodies = kernels(text)
+    chained = set()
+    for m in re.finditer(r"\bchain\s*\(", text):
+        args = text[m.end():closing(text, m.end() - 1, "()")]
+        chained |= set(re.findall(r"\b\w+_kernel\b", args))
+    for name in ("grad", "kernel"):                                  # chosen beforehand
+        for m in re.finditer(r"\b%s = ([^;]*);" % name, text):
+            chained |= set(re.findall(r"\b(class_\w+_kernel)\b", m.group(1)))
+    assert {"class_gemm_kernel", "class_grad_kernel", "class_finish_kernel", "class_few_kernel", "class_join_kernel", "class_bias_kernel", "class_pack_kernel",
+            "class_rows_kernel", "class_label_rows_kernel", "norm_columns_kernel"} <= chained, chained
+    for name in chained:
+        assert "pdl_wait();" in bodies[name], name
 
 
 @gpu
