@@ -92,18 +92,50 @@ __device__ __forceinline__ void row_sum(float (&v)[NS], float* sm, int slot) {
 
 // Vector k of a row; without TAIL the row ends with a vector, which is then in it as a whole or not at all.
 template <class T, int VEC, bool TAIL>
-__device__ __forceinline__ void fetch_vec(const T* __restrict__ row, int c, int cols, RowVec<T, VEC>& v) {
-    if constexpr (VEC > 1 && !TAIL) v.u = c < cols ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
-    else load_raw<T, VEC>(row, c, cols, v);
-}
-template <class T, int VEC, bool TAIL>
 __device__ __forceinline__ void put_vec(T* __restrict__ row, int c, int cols, const float (&v)[VEC]) {
-    if constexpr (VEC > 1 && !TAIL) { if (c < cols) *reinterpret_cast<uint4*>(row + c) = pack_vec<T, VEC>(v); }
+    if constexpr (VEC > 1 && !TAIL) { if (c < cols) __stcs(reinterpret_cast<uint4*>(row + c), pack_vec<T, VEC>(v)); }
     else store_vec<T, VEC>(row, c, cols, v);
 }
 
+// The next rows of a thread's vectors on their way into shared memory (cp.async: no registers, and no barrier, since a thread reads only what it has asked for
+// itself): STAGES rows of NMAT matrices.  One row ahead in registers left 24 to 32 KB on their way on an SM, and HBM wants 43 (32768 x 2048
+// backward 81 us).  Rows that do not come as vectors wait in registers, one row ahead.
+template <class T, int VEC, int NV, int WPR, int NMAT>
+struct RowRing {
+    static constexpr int THREADS = RowGroup<WPR>::kThreads, TPR = 32 * WPR;
+    static constexpr bool ASYNC = VEC > 1;
+    static constexpr int STAGE = NMAT * NV * THREADS * 16, STAGES = STAGE > (32 << 10) ? 2 : 3;
+    static constexpr int AHEAD = ASYNC ? STAGES : 1;
+    static constexpr size_t kSmem = ASYNC ? (size_t)STAGES * STAGE : 0;
+    uint8_t* at;                                  // this thread's place in the first stage
+    RowVec<T, VEC> reg[ASYNC ? 1 : NMAT][ASYNC ? 1 : NV];
+    __device__ __forceinline__ explicit RowRing(uint8_t* smem) : at(smem + threadIdx.x * 16) {}
+    __device__ __forceinline__ uint8_t* place(int stage, int m, int k) const { return at + stage * STAGE + (m * NV + k) * THREADS * 16; }
+    __device__ __forceinline__ void ask(int stage, int m, const T* row, int t, int cols) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TPR + t) * VEC;
+            if constexpr (ASYNC) {
+                const int n = max(0, min(VEC, cols - c));                              // behind the last column: zeros
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(place(stage, m, k))), "l"(n ? row + c : row),
+                             "r"(n * (int)sizeof(T)) : "memory");
+            } else load_raw<T, VEC>(row, c, cols, reg[m][k]);
+        }
+    }
+    static __device__ __forceinline__ void close() {
+        if constexpr (ASYNC) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    static __device__ __forceinline__ void wait() {                                     // for the oldest row
+        if constexpr (ASYNC) asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
+    }
+    __device__ __forceinline__ void take(int stage, int m, int k, float (&v)[VEC]) const {
+        if constexpr (ASYNC) unpack_vec<T, VEC>(*reinterpret_cast<const uint4*>(place(stage, m, k)), v);
+        else v[0] = to_float(reg[m][k].e[0]);
+    }
+};
+
 // NV vectors of VEC values a thread hold a row: vector k of thread t starts at column (k * threads + t) * VEC.  A block takes every gridDim-th row (group of rows),
-// keeps gamma and beta in registers and has the next row on its way while it works on one.
+// keeps gamma and beta in registers and has the next rows on their way while it works on one.
 template <class T, int VEC, int NV, int WPR, bool TAIL>
 __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* __restrict__ x, long long ldx, long long rows, int cols, const void* __restrict__ gamma,
                                                                        const void* __restrict__ beta, bool p32, bool pwide, float eps, T* __restrict__ y, long long ldy,
@@ -113,12 +145,16 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* 
     const int t = threadIdx.x % TPR;
     const long long step = (long long)gridDim.x * ROWS;
     long long r = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
-    RowVec<T, VEC> next[NV];
-    const T* xr = x + r * ldx;
+    extern __shared__ __align__(16) uint8_t ring_smem[];
+    typedef RowRing<T, VEC, NV, WPR, 1> Ring;
+    Ring ring(ring_smem);
+    long long ra = r;                            // the next row to ask for
     T* yr = y + r * ldy;
-    if (r < rows)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) fetch_vec<T, VEC, TAIL>(xr, (k * TPR + t) * VEC, cols, next[k]);
+    for (int i = 0; i < Ring::AHEAD; ++i, ra += step) {
+        if (ra < rows) ring.ask(i, 0, x + ra * ldx, t, cols);
+        Ring::close();
+    }
     float g[NV][VEC], b[NV][VEC];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -126,20 +162,25 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* 
         load_param<T, VEC>(beta, p32, pwide, (k * TPR + t) * VEC, cols, 0.f, b[k]);
     }
     const float inv = 1.f / (float)cols;
+    int stage = 0;
     for (; r < rows; r += step) {                // (a whole warp, or a whole block)
         float v[NV][VEC];
         float s[1] = {0.f};
+        Ring::wait();
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            to_floats<T, VEC>(next[k], v[k]);
+            ring.take(stage, 0, k, v[k]);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) s[0] += v[k][j];   // (zeros behind the last column)
         }
-        xr += step * ldx;
-        if (r + step < rows)
-#pragma unroll
-            for (int k = 0; k < NV; ++k) fetch_vec<T, VEC, TAIL>(xr, (k * TPR + t) * VEC, cols, next[k]);
+        if constexpr (!Ring::ASYNC) { if (ra < rows) ring.ask(0, 0, x + ra * ldx, t, cols); }
         row_sum<WPR, 1>(s, sm, 0);
+        if constexpr (Ring::ASYNC) {             // (behind the sum: this stage has been read)
+            if (ra < rows) ring.ask(stage, 0, x + ra * ldx, t, cols);
+            Ring::close();
+            if (++stage == Ring::AHEAD) stage = 0;
+        }
+        ra += step;
         const float mu = s[0] * inv;
         float q[1] = {0.f};
 #pragma unroll
@@ -211,25 +252,27 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(
                                                                                 const float* __restrict__ rstd, T* __restrict__ dx, long long lddx, float* __restrict__ partial) {
     constexpr int TPR = 32 * WPR, ROWS = RowGroup<WPR>::kRows;
     __shared__ __align__(16) float sm[2 * 2 * WPR];
-    extern __shared__ float cs[];                // with several rows a block: [2][cols]
+    extern __shared__ __align__(16) uint8_t ring_smem[];
     pdl_next();
     const int t = threadIdx.x % TPR;
     const long long step = (long long)gridDim.x * ROWS;
     long long r = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
-    RowVec<T, VEC> nd[NV], nx[NV];
-    float nmu = 0.f, nrs = 0.f;
-    const T *dyr = dy + r * lddy, *xr = x + r * ldx;
+    typedef RowRing<T, VEC, NV, WPR, 2> Ring;
+    float* cs = reinterpret_cast<float*>(ring_smem + Ring::kSmem);   // with several rows a block: [2][cols]
+    Ring ring(ring_smem);
     T* dxr = dx + r * lddx;
-    const auto fetch = [&](long long i) {
-        nmu = mean[i];
-        nrs = rstd[i];
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            fetch_vec<T, VEC, TAIL>(dyr, (k * TPR + t) * VEC, cols, nd[k]);
-            fetch_vec<T, VEC, TAIL>(xr, (k * TPR + t) * VEC, cols, nx[k]);
+    long long ra = r;                            // the next row to ask for
+    float nmu = r < rows ? mean[r] : 0.f, nrs = r < rows ? rstd[r] : 0.f;
+    const auto fetch = [&](int stage) {
+        if (ra < rows) {
+            ring.ask(stage, 0, dy + ra * lddy, t, cols);
+            ring.ask(stage, 1, x + ra * ldx, t, cols);
         }
+        Ring::close();
+        ra += step;
     };
-    if (r < rows) fetch(r);
+#pragma unroll
+    for (int i = 0; i < Ring::AHEAD; ++i) fetch(i);
     float ag[NV][VEC], ab[NV][VEC], g[NV][VEC];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -238,20 +281,20 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(
         for (int j = 0; j < VEC; ++j) ag[k][j] = ab[k][j] = 0.f;
     }
     const float inv = 1.f / (float)cols;
-    int slot = 0;
+    int slot = 0, stage = 0;
     for (; r < rows; r += step, slot ^= 1) {
         const float mu = nmu, rs = nrs;
         float d[NV][VEC], h[NV][VEC], s[2] = {0.f, 0.f};
+        Ring::wait();
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            to_floats<T, VEC>(nd[k], d[k]);
-            to_floats<T, VEC>(nx[k], h[k]);
+            ring.take(stage, 0, k, d[k]);
+            ring.take(stage, 1, k, h[k]);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) h[k][j] = (h[k][j] - mu) * rs;   // (behind the last column d = 0: adds nothing)
         }
-        dyr += step * lddy;
-        xr += step * ldx;
-        if (r + step < rows) fetch(r + step);
+        if (r + step < rows) { nmu = mean[r + step]; nrs = rstd[r + step]; }
+        if constexpr (!Ring::ASYNC) fetch(0);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -263,6 +306,10 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(
                 s[1] = fmaf(d[k][j], h[k][j], s[1]);
             }
         row_sum<WPR, 2>(s, sm, slot);
+        if constexpr (Ring::ASYNC) {             // (behind the sum: this stage has been read)
+            fetch(stage);
+            if (++stage == Ring::AHEAD) stage = 0;
+        }
         const float m0 = s[0] * inv, m1 = s[1] * inv;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -399,7 +446,7 @@ struct NormCall {
     float *mean, *rstd;
 };
 
-// Blocks of a kernel that the GPU holds at once, at most kNormBlocks.
+// Blocks of a kernel that the GPU holds at once.
 int blocks_at_once(const void* kernel, int threads, size_t smem) {
     static std::mutex lock;
     static std::map<std::pair<const void*, size_t>, int> known;
@@ -408,7 +455,7 @@ int blocks_at_once(const void* kernel, int threads, size_t smem) {
     if (n == 0) {
         int per_sm = 0;
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess || per_sm < 1) { cudaGetLastError(); per_sm = 1; }
-        n = std::min(kNormBlocks, 148 * per_sm);
+        n = 148 * per_sm;
     }
     return n;
 }
@@ -417,9 +464,11 @@ template <class T, int VEC, int NV, int WPR>
 void norm_go(const NormCall& a, cudaStream_t s) {
     const auto kernel = VEC > 1 && a.cols % VEC == 0 ? norm_kernel<T, VEC, NV, WPR, false> : norm_kernel<T, VEC, NV, WPR, true>;
     const int64_t blocks = (a.rows + RowGroup<WPR>::kRows - 1) / RowGroup<WPR>::kRows;
+    constexpr size_t smem = RowRing<T, VEC, NV, WPR, 1>::kSmem;
+    if (smem > (48 << 10)) configure_kernel_once((const void*)kernel, (int)smem, false);
     // short calls: a block a row (group), without asking the runtime
-    const int64_t grid = blocks <= 148 ? blocks : std::min<int64_t>(blocks, blocks_at_once((const void*)kernel, RowGroup<WPR>::kThreads, 0));
-    kernel<<<(unsigned)grid, RowGroup<WPR>::kThreads, 0, s>>>((const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.beta, a.p32, a.pwide, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
+    const int64_t grid = blocks <= 148 ? blocks : std::min<int64_t>(blocks, blocks_at_once((const void*)kernel, RowGroup<WPR>::kThreads, smem));
+    kernel<<<(unsigned)grid, RowGroup<WPR>::kThreads, smem, s>>>((const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.beta, a.p32, a.pwide, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
 }
 template <class T>
 void norm_pick(const NormCall& a, cudaStream_t s) {
@@ -430,7 +479,7 @@ void norm_pick(const NormCall& a, cudaStream_t s) {
         if (n <= 64) return norm_go<T, V, 2, 1>(a, s);
         if (n <= 128) return norm_go<T, V, 4, 1>(a, s);
         if (n <= 256) return norm_go<T, V, 4, 2>(a, s);
-        if (n <= 512) return norm_go<T, V, 4, 4>(a, s);
+        if (n <= 512) return norm_go<T, V, 2, 8>(a, s);
         if (n <= 1024) return norm_go<T, V, 4, 8>(a, s);
         if (n <= 2048) return norm_go<T, V, 4, 16>(a, s);
     } else {
@@ -460,8 +509,9 @@ template <class T, int VEC, int NV, int WPR>
 int norm_back_go(const NormBackCall& a, cudaStream_t s) {
     constexpr int ROWS = RowGroup<WPR>::kRows;
     const auto kernel = VEC > 1 && a.cols % VEC == 0 ? norm_backward_kernel<T, VEC, NV, WPR, false> : norm_backward_kernel<T, VEC, NV, WPR, true>;
-    const size_t smem = ROWS > 1 ? 8 * (size_t)a.cols : 0;
-    const int blocks = (int)std::min<int64_t>((a.rows + ROWS - 1) / ROWS, blocks_at_once((const void*)kernel, RowGroup<WPR>::kThreads, smem));
+    const size_t smem = RowRing<T, VEC, NV, WPR, 2>::kSmem + (ROWS > 1 ? 8 * (size_t)a.cols : 0);
+    if (smem > (48 << 10)) configure_kernel_once((const void*)kernel, 200 << 10, false);
+    const int blocks = (int)std::min<int64_t>({(a.rows + ROWS - 1) / ROWS, (int64_t)kNormBlocks, (int64_t) blocks_at_once((const void*)kernel, RowGroup<WPR>::kThreads, smem)});
     kernel<<<(unsigned)blocks, RowGroup<WPR>::kThreads, smem, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.rows, a.cols, a.gamma, a.p32, a.pwide, a.mean, a.rstd, (T*)a.dx, a.lddx, a.partial);
     return blocks;
 }
