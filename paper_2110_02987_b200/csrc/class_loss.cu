@@ -24,7 +24,9 @@ namespace {
 
 constexpr int kRowThreads = 128;
 constexpr int kMostTargets = 1024;                       // teacher logits a row
-constexpr int64_t kBlockBytes = 1ll << 30;               // of probabilities and gradients of logits held at once
+// Bytes of probabilities and gradients of logits held at once, about a hundredth of the GPU's memory.  Several blocks of rows also hold the sums of dW in fp32 and read and
+// write them (8192 x 2048 against 100 003 classes: one block of 1.6 GB 8.6 ms, two of 0.8 GB and 0.8 GB of sums 9.1 ms).
+constexpr int64_t kBlockBytes = 2ll << 30;
 constexpr float kLog2e = 1.44269504f;
 
 template <class P> __device__ __forceinline__ float load_as_float(const void* p, int64_t i) { return to_float(reinterpret_cast<const P*>(p)[i]); }
