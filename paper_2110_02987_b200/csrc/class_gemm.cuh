@@ -83,6 +83,18 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(8192 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 
+// A tile into this CTA's shared memory whose bytes count at a barrier of the pair's leader.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t leader_bar) {
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(leader_bar)
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t leader_address(uint32_t addr) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+
 // This warp's 32 tensor-memory lanes x 32 columns, complete on return.
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
     uint32_t r[32];
@@ -274,16 +286,15 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     const uint32_t bars = sm_addr + CT_RING;
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (CT_STAGES + s); };
-    auto pfull = [&](int s) { return bars + 8u * (2 * CT_STAGES + s); };     // leader: the other CTA's stage is full
-    auto tfull = [&](int i) { return bars + 8u * (3 * CT_STAGES + i); };
+    auto tfull = [&](int i) { return bars + 8u * (2 * CT_STAGES + i); };
     constexpr int NACC = ADD_UP && USE == kStats ? 4 : 2, ACC_COLS = CT_TMEM / NACC;
-    auto tempty = [&](int i) { return bars + 8u * (3 * CT_STAGES + NACC + i); };
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + CT_RING + 8 * (3 * CT_STAGES + 2 * NACC));
+    auto tempty = [&](int i) { return bars + 8u * (2 * CT_STAGES + NACC + i); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + CT_RING + 8 * (2 * CT_STAGES + 2 * NACC));
     volatile uint32_t* abort_flag = tmem_slot + 1;
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < CT_STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); mbar_init(pfull(s), 1); }
+        for (int s = 0; s < CT_STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         for (int i = 0; i < NACC; ++i) { mbar_init(tfull(i), 1); mbar_init(tempty(i), 2 * CT_EPI_WARPS); }
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -301,7 +312,8 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     const long long units = units_of(a);
 
     if (warp == 0 && lane == 0) {
-        // ---------------- TMA producer: this CTA's rows of A and half of the rows of B, 64 of the reduction at a time ----------------
+        // ---------------- TMA producer: this CTA's rows of A and half of the rows of B, 64 of the reduction at a time; the leader's barrier counts both CTAs' bytes
+        // (with a thread of the other CTA passing on that its stage is full, a stage came round later than the six of the ring bridge) ----------------
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
@@ -315,37 +327,24 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     part_pair(p, a.pairs, za, zb);
                     for (int kb = t.kb0 + g; kb < t.kb0 + min(g + group, t.nkb); ++kb) {
                         if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, 31))) break;
-                        mbar_expect_tx(full(stage), (uint32_t)(CT_H + half_w) * (CT_K * 2));
-                        const uint32_t base = sm_addr + stage * CT_STAGE;
+                        if (rank == 0) mbar_expect_tx(full(stage), 2u * (uint32_t)(CT_H + half_w) * (CT_K * 2));
+                        const uint32_t base = sm_addr + stage * CT_STAGE, bar = leader_address(full(stage));
                         if (A_MN) {
-                            tma_load_3d(base, &tmA, ra, kb * CT_K, za, full(stage));
-                            tma_load_3d(base + 8192, &tmA, ra + 64, kb * CT_K, za, full(stage));
+                            tma_load_3d_pair(base, &tmA, ra, kb * CT_K, za, bar);
+                            tma_load_3d_pair(base + 8192, &tmA, ra + 64, kb * CT_K, za, bar);
                         } else {
-                            tma_load_3d(base, &tmA, kb * CT_K, a.a_row0 + ra, za, full(stage));
+                            tma_load_3d_pair(base, &tmA, kb * CT_K, a.a_row0 + ra, za, bar);
                         }
                         if (B_MN) {
-                            for (int j = 0; j < half_w; j += 64) tma_load_3d(base + CT_OPERAND + j * 128, &tmB, rb + j, a.b_row0 + kb * CT_K, zb, full(stage));
+                            for (int j = 0; j < half_w; j += 64) tma_load_3d_pair(base + CT_OPERAND + j * 128, &tmB, rb + j, a.b_row0 + kb * CT_K, zb, bar);
                         } else {
-                            tma_load_3d(base + CT_OPERAND, &tmB, kb * CT_K, rb, zb, full(stage));
+                            tma_load_3d_pair(base + CT_OPERAND, &tmB, kb * CT_K, rb, zb, bar);
                         }
                         if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
                     }
                 }
         }
-    } else if (warp == 1 && rank == 1) {
-        // ---------------- the other CTA's stages: the leader is told of each ----------------
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (long long u = blockIdx.x >> 1; u < units && ok && lane == 0; u += ncl) {
-            const int steps = tile_at(a, u).nkb * a.pairs;
-            for (int i = 0; i < steps; ++i) {
-                if (!(ok = mbar_wait(full(stage), phase, abort_flag, a.err, 34))) break;
-                mbar_arrive_leader(pfull(stage));
-                if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
-            }
-        }
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
         // ---------------- MMA issuer (leader of the pair): the whole warp runs the loop, one elected lane issues ----------------
         int stage = 0, acc = 0;
         uint32_t phase = 0, acc_phase = 0;
@@ -363,7 +362,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     left = ADD_UP ? min(a.chunk * a.pairs, steps - i) : steps;
                 }
                 const uint32_t d = tmem_base + (uint32_t)(acc * ACC_COLS);
-                if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag, a.err, 33) && mbar_wait<true>(pfull(stage), phase, abort_flag, a.err, 35)))) break;
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(full(stage), phase, abort_flag, a.err, 33)))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t base = sm_addr + stage * CT_STAGE;
                 const uint64_t da = operand_desc<A_MN>(base), db = operand_desc<B_MN>(base + CT_OPERAND);
@@ -378,7 +377,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 if (--left == 0 && ++acc == NACC) { acc = 0; acc_phase ^= 1u; }
             }
         }
-    } else if (warp >= CT_EPI_WARP0) {
+    } else if (warp >= CT_EPI_WARP0) {   // (warp 1 of the other CTA has nothing to do)
         // ---------------- drain: this warp's 32 rows (a row a lane) x half of the tile's columns ----------------
         const int ew = warp - CT_EPI_WARP0, q = warp & 3, half = ew >> 2;
         float* bias = reinterpret_cast<float*>(sm + CT_RING + 256) + ew * 128;
@@ -587,10 +586,10 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         }
     }
 
-    // Tear-down.  After a time-out, give loads that may still be in flight a bounded chance to land before the shared memory is
-    // released.  Neither CTA leaves while the other may still read its operands or arrive at its barriers.
+    // Tear-down.  After a time-out, the leader gives loads that may still be in flight, its own and the other CTA's, a bounded chance to land before the shared
+    // memory is released.  Neither CTA leaves while the other may still read its operands or arrive at its barriers.
     __syncthreads();
-    if (*abort_flag && threadIdx.x == 0)
+    if (*abort_flag && threadIdx.x == 0 && rank == 0)
         for (int s = 0; s < CT_STAGES; ++s)
             for (uint32_t i = 0; i < 4096u; ++i)
                 if (mbar_try_wait(full(s), 0) || mbar_try_wait(full(s), 1)) break;
