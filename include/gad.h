@@ -383,9 +383,10 @@ int gad_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t
  * whatever H, teacher and weight hold there, and add nothing to dW and db.  If no row counts the loss and all gradients are zero.  A class named twice
  * in a row's slots has the sum of both.  A label or slot of `classes` or more makes that row's loss, and the whole, NaN.
  * A bias of -inf takes a class out (its W row must be finite).
- * Gradients are those of `loss`, in dtype; any of dH, dW, db may be NULL (db needs a bias).  fp32 matrices are multiplied to fp32
- * accuracy (24-bit operands in three parts); with fp16 and bfloat16 the softmax's gradient is rounded to that type, and row weights
- * should lie within 2^20 of the largest one in fp16.  Equal calls give equal bits. */
+ * Gradients are those of `loss`, in dtype; any of dH, dW, db may be NULL (db needs a bias).  Sums, statistics and losses are fp32.
+ * fp32 matrices are multiplied to fp32 accuracy (24-bit operands in three parts); with fp16 and bfloat16 the softmax's gradient is
+ * rounded to that type, probabilities below 2^-32 of the largest among 128 neighbouring classes count as zero in it, and row weights
+ * should lie within 2^20 of the largest one in fp16.  Outputs must not overlap inputs.  Equal calls give equal bits. */
 typedef struct {
     int32_t dtype;                 /* of H, W, bias, dH, dW, db: GAD_F32, GAD_F16, GAD_BF16                 */
     int32_t cols, classes;         /* D and V                                                               */
@@ -412,8 +413,9 @@ typedef struct {
     int32_t* status;               /* device [1]: 0, or the code of a bounded wait that ran out (the other outputs are then undefined) */
 } gad_class_loss_args;
 
-/* Device workspace of gad_class_loss (256-byte aligned), at most about 0.5 GB for the gradients of a piece of the classes beside copies of H (and of W where it is
- * fp32 or its rows do not start on 16 bytes).  Depends on sizes, types, strides, which pointers are NULL, and W's alignment.  Host-only. */
+/* Device workspace of gad_class_loss (256-byte aligned): a copy of H (and of W where it is fp32 or its rows do not start on 16 bytes) and, for gradients, at most
+ * about 2 GB for a block of the rows x classes matrix (or 256 rows of it, where those take more), and the sums of dW in fp32 where that does not
+ * hold all rows.  Depends on sizes, types, strides, which pointers are NULL, and W's alignment.  Host-only. */
 int gad_class_loss_workspace_bytes(const gad_class_loss_args* args, size_t* bytes);
 int gad_class_loss(const gad_class_loss_args* args, void* workspace, size_t workspace_bytes, void* stream);
 

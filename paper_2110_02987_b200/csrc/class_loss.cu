@@ -8,7 +8,8 @@
 // half the largest value, the sums and sum tau z (kStats); class_finish_kernel joins them.  For gradients the rows are gone through in blocks: of a
 // block the tiles leave z too, as 16-bit codes (fp32: as it is), class_grad_kernel turns it into G where it lies, and dH = G W and dW += G^T H follow
 // (kOut).  So what is held of the rows x classes matrix is bounded (kBlockBytes), whatever its size.  Taking z again from H and W instead, once its row sums are
-// known, needs no codes but a third more flops: 4096 x 1024 bf16 against 32 768 classes 918 us, now 770.
+// known, needs no codes but a third more flops (8192 x 2048 bf16 against 100 003 classes: 10.7 ms, from codes 9.9 ms at that time, 8.65 now).  Going from z to G in strips of
+// 512 to 1024 rows, while the codes are in the L2, cost more tiles than it saved bytes (4096 x 1024 against 32 768: 896 us instead of 851).
 //
 // Operands: fp16 and bfloat16 as they are.  fp32 in three bfloat16 parts (24 bits), of whose nine products the six that reach 2^-24 are summed.
 // G is rounded to the operand type (fp32: not rounded), times a power of two that brings its largest possible value to 2^14 .. 2^15: in fp16 a probability of 1e-9 keeps
@@ -92,7 +93,7 @@ struct RowArgs {
 // What a block of the row kernels contributes to the scale of the gradients: rows that count, the largest coefficient of G.
 struct RowShare { int n; float most; };
 
-// Labels alone: a warp a row.
+// Labels alone: a warp a row.  Bound by the copy of H (4096 x 1024 bf16: 6 us).
 template <class T>
 __global__ void __launch_bounds__(256) class_label_rows_kernel(const RowArgs a) {
     __shared__ RowShare part[8];
@@ -119,7 +120,8 @@ __global__ void __launch_bounds__(256) class_label_rows_kernel(const RowArgs a) 
     if (blockIdx.x == 0) { *a.ticket = 0u; *a.status = 0; }
 }
 
-// A block a row.  rowk = (coefficient of lse(z), of lse(z / T), sum of q log q with its factor, weight of the row); a row without target: (0, 0, 0, 0).
+// A block a row; the copy of H, the sort of its targets (by counting, k^2 / 128 steps a thread) and where they start in every half tile (4096 x 2048 bf16, 65 targets:
+// 29 us of 2.3 ms).  rowk = (coefficient of lse(z), of lse(z / T), sum of q log q with its factor, weight of the row); a row without target: (0, 0, 0, 0).
 template <class T>
 __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a) {
     extern __shared__ int sm_rows[];
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
     }
 }
 
-// Class vectors that no descriptor can reach (fp32, or rows that do not start on 16 bytes) as operands: a warp a row.
+// Class vectors that no descriptor can reach (fp32, or rows that do not start on 16 bytes) as operands: a warp a row, bound by memory (16 384 x 512 fp32 to three parts: 14 us).
 template <class T>
 __global__ void __launch_bounds__(256) class_pack_kernel(const T* __restrict__ W, int64_t ldw, int rows, int cols, void* Wp, int64_t ldp, int64_t part_stride) {
     const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(256) class_pack_kernel(const T* __restrict__ W
 // Statistics of a few rows (up to 8: serving): reading W is all that costs, and a tile of 256 rows on the tensor cores mostly multiplies zeros (one row, 128 000 x 4096
 // bf16: 237 us at the card's power limit).  A warp takes four classes at a time, each lane every 32nd vector of their rows; the rows of H lie in shared memory in fp32.
 // The 4 NR sums over lanes are halved at each of the first exchanges, so that lane l ends up with sum l / (32 / (4 NR)), and keeps its own running softmax
-// over the classes it sees, in ascending order.
+// over the classes it sees, in ascending order.  Bound by HBM: one row of 4096 against 128 000 classes bf16 158 us, 6.65 TB/s.
 constexpr int kFewRows = 8, kFewBlocks = 296, kFewSmem = 160 << 10;
 struct FewArgs {
     const void* H; long long ldh;
@@ -240,17 +242,6 @@ struct FewArgs {
     float* z; long long ldz;                  // or null
     float4* stats;                            // [blocks x rows]
 };
-template <class T, int VEC>
-__device__ __forceinline__ void unpack(const uint4& u, float (&v)[VEC]) {
-    if constexpr (sizeof(T) == 4) {
-        v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
-    } else {
-        union { uint4 u; T e[8]; } w;
-        w.u = u;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) v[j] = to_float(w.e[j]);
-    }
-}
 template <class T, int NR, int NL, bool WIDE>
 __global__ void __launch_bounds__(256, 2) class_few_kernel(const FewArgs a) {
     extern __shared__ float h[];              // [NR][cols, rounded up to a vector]
@@ -286,7 +277,7 @@ __global__ void __launch_bounds__(256, 2) class_few_kernel(const FewArgs a) {
                 for (int k = 0; k < 4; ++k) u[k] = __ldcs(reinterpret_cast<const uint4*>(wr[k] + x));
                 float v[4][VEC];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) unpack<T, VEC>(u[k], v[k]);
+                for (int k = 0; k < 4; ++k) unpack_vec<T, VEC>(u[k], v[k]);
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     float hv[VEC];
@@ -365,7 +356,7 @@ struct FinishArgs {
     float *scal, *loss;
 };
 
-// The parts of a row's statistics joined: a block has 8 rows, 32 threads each, every 32nd part a thread; joined pairwise in a fixed order.  The block that comes last
+// The parts of a row's statistics joined (bound by the latency of its loads: 4096 rows of 256 parts 12 us): a block has 8 rows, 32 threads each, every 32nd part a thread; joined pairwise in a fixed order.  The block that comes last
 // writes, for the first block of rows, scal[0], a power of two that brings the largest coefficient of G to 2^14 .. 2^15, [1]: scale / counted rows / that,
 // [2]: scale / counted rows; and for the last one the loss.
 template <int NL>
@@ -473,7 +464,7 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
 
 // G from what the tiles left of z, in its place (16-bit codes) or beside it (fp32): G = w (a p + (1 - a) T p^T - tau) times scal[0], in the operand type or (T = float) in
 // three bfloat16 parts.  A warp takes 1024 classes of a row at a time, a block 32 rows of them, so column sums (for db, before any rounding) cost one
-// exchange.  Bound by memory: 4 bytes a value.
+// exchange.  Bound by memory: 4 bytes a value (4096 x 32 768 bf16 104 us, 5.2 TB/s).
 struct GradArgs {
     const void* z; long long ldz;             // codes or fp32 [rows x ldz]
     void* G; long long ldg, part_stride;
@@ -621,7 +612,7 @@ __global__ void __launch_bounds__(256) class_grad_kernel(const GradArgs a) {
     }
 }
 
-// The shares of the tiles that were cut along their reduction, added up in order, and put where an uncut tile would have gone: four columns a thread, four (eight)
+// The shares of the tiles that were cut along their reduction (from L2: 32 tiles of two shares 8 us), added up in order, and put where an uncut tile would have gone: four columns a thread, four (eight)
 // rows of a tile a block.
 template <class T>
 __global__ void __launch_bounds__(256) class_join_kernel(const TileArgs a) {

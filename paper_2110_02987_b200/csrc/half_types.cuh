@@ -72,11 +72,6 @@ __device__ __forceinline__ void load_raw(const T* __restrict__ row, int c, int c
     for (int j = 0; j < VEC; ++j) v.e[j] = c + j < cols ? row[c + j] : from_float<T>(0.f);
 }
 template <class T, int VEC>
-__device__ __forceinline__ void to_floats(const RowVec<T, VEC>& q, float (&v)[VEC]) {
-    if constexpr (VEC > 1) unpack_vec<T, VEC>(q.u, v);
-    else v[0] = to_float(q.e[0]);
-}
-template <class T, int VEC>
 __device__ __forceinline__ void store_vec(T* __restrict__ row, int c, int cols, const float (&v)[VEC]) {
     if constexpr (VEC > 1) {
         if (c + VEC <= cols) { *reinterpret_cast<uint4*>(row + c) = pack_vec<T, VEC>(v); return; }

@@ -3,7 +3,9 @@ of an output layer with many classes, and distillation from a teacher's top logi
 
 Like the rest of the binding this is argument checking and marshalling; the work is the library's kernels (``include/gad.h``).
 Every call enqueues on ``stream`` (default: torch's current stream of the tensors' device) and does not wait.  Outputs and
-workspaces are allocated per call from torch's allocator on that stream, so calls on different streams, and captured graphs, share nothing.
+workspaces are allocated per call from torch's allocator on that stream, so calls on different streams, and captured graphs, share nothing.  As everywhere
+in torch, tensors made on another stream must be ready when the call's stream gets there.  The calls record nothing for autograd: gradients
+are what they return.
 """
 from __future__ import annotations
 
