@@ -226,11 +226,12 @@ __global__ void __launch_bounds__(256) class_pack_kernel(const T* __restrict__ W
     if (r < rows) pack_row<T>(W + r * ldw, cols, true, Wp, r * ldp, part_stride, threadIdx.x & 31, 32);
 }
 
-// Statistics of a few rows (up to 8: serving): reading W is all that costs, and a tile of 256 rows on the tensor cores mostly multiplies zeros (one row, 128 000 x 4096
+// Statistics of a few rows (up to 4: serving): reading W is all that costs, and a tile of 256 rows on the tensor cores mostly multiplies zeros (one row, 128 000 x 4096
 // bf16: 237 us at the card's power limit).  A warp takes four classes at a time, each lane every 32nd vector of their rows; the rows of H lie in shared memory in fp32.
 // The 4 NR sums over lanes are halved at each of the first exchanges, so that lane l ends up with sum l / (32 / (4 NR)), and keeps its own running softmax
-// over the classes it sees, in ascending order.  Bound by HBM: one row of 4096 against 128 000 classes bf16 158 us, 6.65 TB/s.
-constexpr int kFewRows = 8, kFewBlocks = 296, kFewSmem = 160 << 10;
+// over the classes it sees, in ascending order.  Bound by HBM: one row of 4096 against 128 000 classes bf16 158 us, 6.65 TB/s; with
+// four rows 186 us in all, and with eight the multiply-adds bound it: 407 us, where the tiles take 285 to 310 whatever the number of rows.
+constexpr int kFewRows = 4, kFewBlocks = 296, kFewSmem = 160 << 10;
 struct FewArgs {
     const void* H; long long ldh;
     const void* W; long long ldw;
@@ -246,7 +247,7 @@ template <class T, int NR, int NL, bool WIDE>
 __global__ void __launch_bounds__(256, 2) class_few_kernel(const FewArgs a) {
     extern __shared__ float h[];              // [NR][cols, rounded up to a vector]
     __shared__ float4 sm[8][32];
-    constexpr int VEC = WIDE ? 16 / sizeof(T) : 1, C = 4 * NR, LC = NR == 1 ? 2 : NR == 2 ? 3 : NR == 4 ? 4 : 5;
+    constexpr int VEC = WIDE ? 16 / sizeof(T) : 1, C = 4 * NR, LC = NR == 1 ? 2 : NR == 2 ? 3 : 4;
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, ldv = (a.cols + VEC - 1) / VEC * VEC;
     pdl_next();
     pdl_wait();
@@ -680,7 +681,7 @@ constexpr int kPairs = 74;                               // pairs of CTAs that r
 
 int width_for(int n) { return n <= 128 ? 128 : 256; }
 
-int few_rows(int64_t n) { return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8; }
+int few_rows(int64_t n) { return n <= 1 ? 1 : n <= 2 ? 2 : 4; }
 size_t few_smem(const gad_class_loss_args& a) { return 4 * (size_t)few_rows(a.rows) * (size_t)round_up(a.cols, 8); }
 
 // Blocks of 64 terms of a chunk: 128 additions to an accumulator, about 6e-7 of its value; for fp32 operands a quarter of that.
@@ -764,7 +765,7 @@ cudaError_t go_stats(const CUtensorMap& A, const CUtensorMap& B, const TileArgs&
 template <class T, int NL, bool WIDE>
 cudaError_t few_launch(const FewArgs& f, size_t smem, int blocks, cudaStream_t s) {
     const int n = few_rows(f.rows);
-    const auto kernel = n == 1 ? class_few_kernel<T, 1, NL, WIDE> : n == 2 ? class_few_kernel<T, 2, NL, WIDE> : n == 4 ? class_few_kernel<T, 4, NL, WIDE> : class_few_kernel<T, 8, NL, WIDE>;
+    const auto kernel = n == 1 ? class_few_kernel<T, 1, NL, WIDE> : n == 2 ? class_few_kernel<T, 2, NL, WIDE> : class_few_kernel<T, 4, NL, WIDE>;
     const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), kFewSmem, false);
     return e != cudaSuccess ? e : chain(kernel, dim3((unsigned)blocks), 256, smem, s, false, f);
 }

@@ -22,6 +22,8 @@ namespace {
 
 // Blocks of the backward pass at most, each with a partial sum of dgamma and dbeta: four on every SM, as many as 128 threads of 122 registers leave room for.
 constexpr int kNormBlocks = 592;
+// Long rows from which on a row is eight warps' (2048 x 16 392 bf16 forward: with 32 warps 81 us).
+constexpr int kLongRows = 592;
 
 // gamma / beta in fp32 or in the matrix's own type; null is 1 or 0.  `wide`: both start on 16 bytes.
 template <class T, int VEC>
@@ -209,32 +211,35 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_kernel(const T* 
     }
 }
 
-// Rows longer than a block's registers hold: read three times, twice of them from L2 (148 blocks of two rows at once).
-template <class T, int VEC>
-__global__ void __launch_bounds__(1024) norm_long_kernel(const T* __restrict__ x, long long ldx, int cols, const void* __restrict__ gamma, const void* __restrict__ beta,
+// Rows longer than a block's registers hold: read three times, twice of them from L2.  Eight warps a row where there are rows for all SMs, else 32.
+template <class T, int VEC, int WPR>
+__global__ void __launch_bounds__(32 * WPR) norm_long_kernel(const T* __restrict__ x, long long ldx, int cols, const void* __restrict__ gamma, const void* __restrict__ beta,
                                                          bool p32, bool pwide, float eps, T* __restrict__ y, long long ldy, float* __restrict__ mean, float* __restrict__ rstd) {
-    __shared__ __align__(16) float sm[2 * 32];
+    __shared__ __align__(16) float sm[2 * WPR];
     const long long r = blockIdx.x;
     const T* xr = x + r * ldx;
     RowVec<T, VEC> v;
     float s[1] = {0.f};
-    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+#pragma unroll 4
+    for (int c = threadIdx.x * VEC; c < cols; c += 32 * WPR * VEC) {
         load_raw<T, VEC>(xr, c, cols, v);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) s[0] += to_float(v.e[j]);
     }
-    row_sum<32, 1>(s, sm, 0);
+    row_sum<WPR, 1>(s, sm, 0);
     const float mu = s[0] / (float)cols;
     float q[1] = {0.f};
-    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+#pragma unroll 4
+    for (int c = threadIdx.x * VEC; c < cols; c += 32 * WPR * VEC) {
         load_raw<T, VEC>(xr, c, cols, v);
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
             if (c + j < cols) { const float d = to_float(v.e[j]) - mu; q[0] = fmaf(d, d, q[0]); }
     }
-    row_sum<32, 1>(q, sm, 1);
+    row_sum<WPR, 1>(q, sm, 1);
     const float rs = 1.f / sqrtf(q[0] / (float)cols + eps);
-    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+#pragma unroll 4
+    for (int c = threadIdx.x * VEC; c < cols; c += 32 * WPR * VEC) {
         float g[VEC], b[VEC], o[VEC];
         load_raw<T, VEC>(xr, c, cols, v);
         load_param<T, VEC>(gamma, p32, pwide, c, cols, 1.f, g);
@@ -353,16 +358,17 @@ __global__ void __launch_bounds__(RowGroup<WPR>::kThreads) norm_backward_kernel(
 }
 
 // Long rows: dx by a block a row, read twice.
-template <class T, int VEC>
-__global__ void __launch_bounds__(1024) norm_backward_long_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, int cols,
+template <class T, int VEC, int WPR>
+__global__ void __launch_bounds__(32 * WPR) norm_backward_long_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, int cols,
                                                                   const void* __restrict__ gamma, bool p32, bool pwide, const float* __restrict__ mean,
                                                                   const float* __restrict__ rstd, T* __restrict__ dx, long long lddx) {
-    __shared__ __align__(16) float sm[2 * 2 * 32];
+    __shared__ __align__(16) float sm[2 * 2 * WPR];
     const long long r = blockIdx.x;
     const float mu = mean[r], rs = rstd[r], inv = 1.f / (float)cols;
     RowVec<T, VEC> vd, vx;
     float s[2] = {0.f, 0.f}, g[VEC];
-    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+#pragma unroll 2
+    for (int c = threadIdx.x * VEC; c < cols; c += 32 * WPR * VEC) {
         load_raw<T, VEC>(dy + r * lddy, c, cols, vd);
         load_raw<T, VEC>(x + r * ldx, c, cols, vx);
         load_param<T, VEC>(gamma, p32, pwide, c, cols, 1.f, g);
@@ -373,9 +379,10 @@ __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const T* __res
             s[1] = fmaf(d, (to_float(vx.e[j]) - mu) * rs, s[1]);
         }
     }
-    row_sum<32, 2>(s, sm, 0);
+    row_sum<WPR, 2>(s, sm, 0);
     const float m0 = s[0] * inv, m1 = s[1] * inv;
-    for (int c = threadIdx.x * VEC; c < cols; c += 1024 * VEC) {
+#pragma unroll 2
+    for (int c = threadIdx.x * VEC; c < cols; c += 32 * WPR * VEC) {
         float o[VEC];
         load_raw<T, VEC>(dy + r * lddy, c, cols, vd);
         load_raw<T, VEC>(x + r * ldx, c, cols, vx);
@@ -385,26 +392,44 @@ __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const T* __res
         store_vec<T, VEC>(dx + r * lddx, c, cols, o);
     }
 }
-// ... and their column sums: a block has 32 columns and every gridDim.y-th eight rows.
-template <class T>
+// ... and their column sums: a block has 32 vectors of columns and every gridDim.y-th eight rows.
+template <class T, int VEC>
 __global__ void __launch_bounds__(256) norm_long_columns_kernel(const T* __restrict__ dy, long long lddy, const T* __restrict__ x, long long ldx, long long rows, int cols,
                                                                 const float* __restrict__ mean, const float* __restrict__ rstd, float* __restrict__ partial) {
-    __shared__ float sm[2][8][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
-    float ag = 0.f, ab = 0.f;
+    __shared__ float sm[8][32 * VEC];
+    pdl_next();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * VEC;
+    float ag[VEC], ab[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) ag[j] = ab[j] = 0.f;
     if (c < cols)
+#pragma unroll 4
         for (long long r = (long long)blockIdx.y * 8 + w; r < rows; r += 8ll * gridDim.y) {
-            const float d = to_float(dy[r * lddy + c]);
-            ag = fmaf(d, (to_float(x[r * ldx + c]) - mean[r]) * rstd[r], ag);
-            ab += d;
+            RowVec<T, VEC> vd, vx;
+            load_raw<T, VEC>(dy + r * lddy, c, cols, vd);
+            load_raw<T, VEC>(x + r * ldx, c, cols, vx);
+            const float mu = mean[r], rs = rstd[r];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float d = to_float(vd.e[j]);
+                ag[j] = fmaf(d, (to_float(vx.e[j]) - mu) * rs, ag[j]);
+                ab[j] += d;
+            }
         }
-    sm[0][w][threadIdx.x & 31] = ag;
-    sm[1][w][threadIdx.x & 31] = ab;
-    __syncthreads();
-    if (w < 2 && c < cols) {
-        float s = 0.f;
-        for (int i = 0; i < 8; ++i) s += sm[w][i][threadIdx.x & 31];
-        partial[((long long)blockIdx.y * 2 + w) * cols + c] = s;
+    for (int k = 0; k < 2; ++k) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sm[w][lane * VEC + j] = k ? ab[j] : ag[j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < 32 * VEC; i += 256) {
+            const int at = blockIdx.x * 32 * VEC + i;
+            if (at >= cols) continue;
+            float s = 0.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s += sm[q][i];
+            partial[((long long)blockIdx.y * 2 + k) * cols + at] = s;
+        }
     }
 }
 
@@ -493,8 +518,9 @@ void norm_pick(const NormCall& a, cudaStream_t s) {
         if (a.cols <= 2048) return norm_go<T, 1, 8, 8>(a, s);
         if (a.cols <= 8192) return norm_go<T, 1, 16, 16>(a, s);
     }
-    const auto kernel = wide_rows(a.x, a.ldx, sizeof(T)) && wide_rows(a.y, a.ldy, sizeof(T)) ? norm_long_kernel<T, V> : norm_long_kernel<T, 1>;
-    kernel<<<(unsigned)a.rows, 1024, 0, s>>>((const T*)a.x, a.ldx, a.cols, a.gamma, a.beta, a.p32, a.pwide, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
+    const bool wide = wide_rows(a.x, a.ldx, sizeof(T)) && wide_rows(a.y, a.ldy, sizeof(T)), many = a.rows >= kLongRows;
+    const auto kernel = wide ? (many ? norm_long_kernel<T, V, 8> : norm_long_kernel<T, V, 32>) : many ? norm_long_kernel<T, 1, 8> : norm_long_kernel<T, 1, 32>;
+    kernel<<<(unsigned)a.rows, many ? 256 : 1024, 0, s>>>((const T*)a.x, a.ldx, a.cols, a.gamma, a.beta, a.p32, a.pwide, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
 }
 
 struct NormBackCall {
@@ -538,13 +564,14 @@ int norm_back_rows(const NormBackCall& a, cudaStream_t s) {
         if (a.cols <= 2048) return norm_back_go<T, 1, 8, 8>(a, s);
         if (a.cols <= 8192) return norm_back_go<T, 1, 16, 16>(a, s);
     }
-    const auto kernel = wide_rows(a.x, a.ldx, sizeof(T)) && wide_rows(a.dy, a.lddy, sizeof(T)) && wide_rows(a.dx, a.lddx, sizeof(T)) ? norm_backward_long_kernel<T, V> : norm_backward_long_kernel<T, 1>;
-    kernel<<<(unsigned)a.rows, 1024, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.cols, a.gamma, a.p32, a.pwide, a.mean, a.rstd, (T*)a.dx, a.lddx);
+    const bool wide = wide_rows(a.x, a.ldx, sizeof(T)) && wide_rows(a.dy, a.lddy, sizeof(T)) && wide_rows(a.dx, a.lddx, sizeof(T)), many = a.rows >= kLongRows;
+    const auto kernel = wide ? (many ? norm_backward_long_kernel<T, V, 8> : norm_backward_long_kernel<T, V, 32>)
+                             : many ? norm_backward_long_kernel<T, 1, 8> : norm_backward_long_kernel<T, 1, 32>;
+    kernel<<<(unsigned)a.rows, many ? 256 : 1024, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.cols, a.gamma, a.p32, a.pwide, a.mean, a.rstd, (T*)a.dx, a.lddx);
     const int blocks = (int)std::min<int64_t>((a.rows + 7) / 8, 64);
-    if (a.partial) {
-        norm_long_columns_kernel<T><<<dim3((unsigned)((a.cols + 31) / 32), (unsigned)blocks), 256, 0, s>>>((const T*)a.dy, a.lddy, (const T*)a.x, a.ldx, a.rows, a.cols, a.mean, a.rstd, a.partial);
-        ++g_kernel_launches;
-    }
+    if (a.partial)
+        chain(wide ? norm_long_columns_kernel<T, V> : norm_long_columns_kernel<T, 1>, dim3((unsigned)((a.cols + 32 * (wide ? V : 1) - 1) / (32 * (wide ? V : 1))), (unsigned)blocks), 256, 0, s, false,
+              (const T*)a.dy, (long long)a.lddy, (const T*)a.x, (long long)a.ldx, (long long)a.rows, a.cols, a.mean, a.rstd, a.partial);
     return blocks;
 }
 template <class T>
