@@ -16,6 +16,7 @@
 // eight bits.  One rounding of each term of a sum whose result is rounded to the same type: the result's error grows by about the square root of 2.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "class_gemm.cuh"
 
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(256) class_pack_kernel(const T* __restrict__ W
 // bf16: 237 us at the card's power limit).  A warp takes four classes at a time, each lane every 32nd vector of their rows; the rows of H lie in shared memory in fp32.
 // The 4 NR sums over lanes are halved at each of the first exchanges, so that lane l ends up with sum l / (32 / (4 NR)), and keeps its own running softmax
 // over the classes it sees, in ascending order.  Bound by HBM: one row of 4096 against 128 000 classes bf16 158 us, 6.65 TB/s; with
-// four rows 186 us in all, and with eight the multiply-adds bound it: 407 us, where the tiles take 285 to 310 whatever the number of rows.
+// four rows 186 us in all, and with eight the multiply-adds bound it: 407 us, where class_some_kernel takes 203.
 constexpr int kFewRows = 4, kFewBlocks = 296, kFewSmem = 160 << 10;
 struct FewArgs {
     const void* H; long long ldh;
@@ -340,6 +341,154 @@ __global__ void __launch_bounds__(256, 2) class_few_kernel(const FewArgs a) {
             at.x = most;
             at.w += v.w;
         }
+    a.stats[(long long)blockIdx.x * a.rows + threadIdx.x] = at;
+}
+
+// Statistics of 5 to 16 rows of 16-bit operands that fit shared memory (a batch of serving), still bound by reading W: sixteen classes a warp as the rows of
+// mma.m16n8k16, eight rows of H as its columns.  (tcgen05 has 128 rows at least: with H as A it multiplies zeros at the card's power limit, 16 rows of 4096 against 128 000
+// classes 320 us, here 206, 5.1 TB/s; 32 rows of 2048, at 250 registers a lane, took 144 us here and 125 as tiles.)  The order of the terms is free as long as both operands have the same one, so that a lane's fragments are the 16 bytes it loads: of
+// each 32 values lane (g, t) takes 8 t .. 8 t + 7 of class g, of class g + 8 and of row g of H; two products.  A lane ends up with classes g and g + 8 of rows
+// 2 t and 2 t + 1 and keeps their running softmax.
+constexpr int kSomeRows = 16, kSomeSmem = 200 << 10;
+template <class T>
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (std::is_same<T, __half>::value)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Bytes between the rows of H: eight rows of 64 bytes meet no bank twice.
+__host__ __device__ __forceinline__ int some_stride(int cols) { return (cols * 2 + 127) / 128 * 128 + 64; }
+// NT: groups of eight rows.
+constexpr int kSomeWarps = 16;
+template <class T, int NT, int NL>
+__global__ void __launch_bounds__(32 * kSomeWarps, 1) class_some_kernel(const FewArgs a) {
+    constexpr int WARPS = kSomeWarps, U = 4;             // U steps of 32 values are on their way while the U in front are multiplied
+    extern __shared__ __align__(16) uint8_t hs[];
+    __shared__ float4 sm[WARPS][8 * NT];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, stride = some_stride(a.cols);
+    pdl_next();
+    pdl_wait();
+    for (int n = w; n < 8 * NT; n += WARPS) {
+        const float4 k = n < a.rows ? a.rowk[n] : make_float4(0.f, 0.f, 0.f, 0.f);
+        const bool counts = k.x > 0.f || k.y > 0.f;
+        for (int c = lane; 2 * c < stride; c += 32)
+            reinterpret_cast<T*>(hs + (long long)n * stride)[c] = counts && c < a.cols ? reinterpret_cast<const T*>(a.H)[n * a.ldh + c] : from_float<T>(0.f);
+    }
+    __syncthreads();
+    float m[2 * NT], s1[2 * NT], s2[2 * NT], dot[2 * NT];
+    int e[2 * NT], cur[2 * NT];
+#pragma unroll
+    for (int i = 0; i < 2 * NT; ++i) {
+        const int n = i / 2 * 8 + 2 * t + (i & 1);
+        m[i] = -INFINITY; s1[i] = s2[i] = dot[i] = 0.f;
+        e[i] = 0;
+        cur[i] = n < a.rows ? a.targets[(long long)n * a.ntargets].x : INT_MAX;
+    }
+    const int last = a.z ? (int)a.ldz : a.classes, steps = (a.cols + 31) / 32;
+    const uint8_t* hb = hs + g * stride + t * 16;
+    for (int c0 = (blockIdx.x * WARPS + w) * 16; c0 < last; c0 += gridDim.x * WARPS * 16) {
+        float sum[NT][4];
+#pragma unroll
+        for (int k = 0; k < NT; ++k) sum[k][0] = sum[k][1] = sum[k][2] = sum[k][3] = 0.f;
+        const T* w0 = reinterpret_cast<const T*>(a.W) + (long long)min(c0 + g, a.classes - 1) * a.ldw;
+        const T* w1 = reinterpret_cast<const T*>(a.W) + (long long)min(c0 + g + 8, a.classes - 1) * a.ldw;
+        uint4 u[U], v[U];
+        const auto load = [&](int i0) {
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const int c = 32 * (i0 + j) + 8 * t;
+                if (c + 8 <= a.cols) {
+                    u[j] = __ldcs(reinterpret_cast<const uint4*>(w0 + c));
+                    v[j] = __ldcs(reinterpret_cast<const uint4*>(w1 + c));
+                } else {                                     // the end of the rows
+                    RowVec<T, 8> q, r;
+                    load_raw<T, 8>(w0, c, a.cols, q);
+                    load_raw<T, 8>(w1, c, a.cols, r);
+                    u[j] = q.u; v[j] = r.u;
+                }
+            }
+        };
+        load(0);
+        float acc[NT][4];
+        for (int i0 = 0; i0 < steps; i0 += U) {
+            if (i0 % 32 == 0) {                              // (the accumulator is cut off at every addition: 64 of them at most)
+#pragma unroll
+                for (int k = 0; k < NT; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) { if (i0) sum[k][j] += acc[k][j]; acc[k][j] = 0.f; }
+            }
+            uint4 pu[U], pv[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) { pu[j] = u[j]; pv[j] = v[j]; }
+            if (i0 + U < steps) load(i0 + U);
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                if (i0 + j >= steps) break;
+#pragma unroll
+                for (int k = 0; k < NT; ++k) {
+                    const uint4 b = *reinterpret_cast<const uint4*>(hb + k * 8 * stride + 64 * (i0 + j));
+                    mma_16x8x16<T>(acc[k], pu[j].x, pv[j].x, pu[j].y, pv[j].y, b.x, b.y);
+                    mma_16x8x16<T>(acc[k], pu[j].z, pv[j].z, pu[j].w, pv[j].w, b.z, b.w);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < NT; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[k][j] += acc[k][j];
+        float bias[2];
+        bool cls[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int c = c0 + g + 8 * r;
+            cls[r] = c < a.classes;
+            bias[r] = cls[r] && a.bias ? to_float(reinterpret_cast<const T*>(a.bias)[c]) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) {
+            const int n = i / 2 * 8 + 2 * t + (i & 1);
+            float z[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int c = c0 + g + 8 * r;
+                z[r] = cls[r] ? (sum[i / 2][2 * r + (i & 1)] + bias[r]) * a.sc : -INFINITY;
+                if (a.z && n < a.rows && c < last) a.z[(long long)n * a.ldz + c] = z[r];
+                while (cur[i] <= c) {                        // (classes ascend; INT_MAX is none)
+                    if (cur[i] == c) dot[i] = fmaf(__int_as_float(a.targets[(long long)n * a.ntargets + e[i]].y), z[r], dot[i]);
+                    cur[i] = ++e[i] < a.ntargets ? a.targets[(long long)n * a.ntargets + e[i]].x : INT_MAX;
+                }
+            }
+            const float most = fmaxf(m[i], fmaxf(z[0], z[1])), base = most == -INFINITY ? 0.f : most;
+            s1[i] = fmaf(s1[i], exp2_fast(m[i] - base), exp2_fast(z[0] - base) + exp2_fast(z[1] - base));
+            if (NL == 2) s2[i] = fmaf(s2[i], exp2_fast((m[i] - base) * a.inv_t), exp2_fast((z[0] - base) * a.inv_t) + exp2_fast((z[1] - base) * a.inv_t));
+            m[i] = most;
+        }
+    }
+    // lanes of the same rows (equal t), then warps, in order
+    const auto join = [&](float4& u, const float4& v) {
+        const float most = fmaxf(u.x, v.x), base = most == -INFINITY ? 0.f : most;
+        u.y = u.y * exp2f(u.x - base) + v.y * exp2f(v.x - base);
+        if (NL == 2) u.z = u.z * exp2f((u.x - base) * a.inv_t) + v.z * exp2f((v.x - base) * a.inv_t);
+        u.x = most;
+        u.w += v.w;
+    };
+#pragma unroll
+    for (int i = 0; i < 2 * NT; ++i) {
+        float4 at = make_float4(m[i], s1[i], s2[i], dot[i]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+            float4 v = make_float4(__shfl_xor_sync(0xffffffffu, at.x, o), __shfl_xor_sync(0xffffffffu, at.y, o), __shfl_xor_sync(0xffffffffu, at.z, o), __shfl_xor_sync(0xffffffffu, at.w, o));
+            if (lane & o) { join(v, at); at = v; } else join(at, v);
+        }
+        if (g == 0) sm[w][i / 2 * 8 + 2 * t + (i & 1)] = at;
+    }
+    __syncthreads();
+    if (threadIdx.x >= a.rows) return;
+    float4 at = sm[0][threadIdx.x];
+    for (int i = 1; i < WARPS; ++i) join(at, sm[i][threadIdx.x]);
     a.stats[(long long)blockIdx.x * a.rows + threadIdx.x] = at;
 }
 
@@ -682,6 +831,7 @@ constexpr int kPairs = 74;                               // pairs of CTAs that r
 int width_for(int n) { return n <= 128 ? 128 : 256; }
 
 int few_rows(int64_t n) { return n <= 1 ? 1 : n <= 2 ? 2 : 4; }
+size_t some_smem(const gad_class_loss_args& a) { return (size_t)(a.rows <= 8 ? 8 : 16) * some_stride(a.cols); }
 size_t few_smem(const gad_class_loss_args& a) { return 4 * (size_t)few_rows(a.rows) * (size_t)round_up(a.cols, 8); }
 
 // Blocks of 64 terms of a chunk: 128 additions to an accumulator, about 6e-7 of its value; for fp32 operands a quarter of that.
@@ -689,7 +839,7 @@ constexpr int kChunk = 32, kChunkParts = 8;
 
 struct ClassPlan {
     int parts, pairs;                // operand parts, products of them
-    bool grads, pack_w, few, add_up;   // add_up: logits longer than a chunk are added up in chunks
+    bool grads, pack_w, few, some, add_up;   // add_up: logits longer than a chunk are added up in chunks
     int ntargets, nl, save;
     int width_v, tiles_v, width_d, tiles_d;
     int64_t ldp, ldg;                // row lengths of the packed operands, and of z and G
@@ -705,7 +855,10 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     p.parts = a.dtype == GAD_F32 ? 3 : 1;
     p.pairs = a.dtype == GAD_F32 ? 6 : 1;
     p.grads = a.dH || a.dW || a.db;
+    const bool wide = ((uintptr_t)a.W & 15) == 0 && (a.ldw * (a.dtype == GAD_F32 ? 4 : 2)) % 16 == 0;
     p.few = N <= kFewRows && few_smem(a) <= kFewSmem;
+    p.some = !p.few && N <= kSomeRows && a.dtype != GAD_F32 && wide && some_smem(a) <= kSomeSmem;
+    p.few |= p.some;
     p.pack_w = (!p.few || a.dH) && (a.dtype == GAD_F32 || ((uintptr_t)a.W & 15) != 0 || (a.ldw * 2) % 16 != 0);
     p.ntargets = a.k + (a.labels ? 1 : 0);
     p.nl = a.k > 0 && a.labels && a.hard_weight > 0.f && a.hard_weight < 1.f && a.temperature != 1.f ? 2 : 1;
@@ -768,6 +921,12 @@ cudaError_t few_launch(const FewArgs& f, size_t smem, int blocks, cudaStream_t s
     const auto kernel = n == 1 ? class_few_kernel<T, 1, NL, WIDE> : n == 2 ? class_few_kernel<T, 2, NL, WIDE> : class_few_kernel<T, 4, NL, WIDE>;
     const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), kFewSmem, false);
     return e != cudaSuccess ? e : chain(kernel, dim3((unsigned)blocks), 256, smem, s, false, f);
+}
+template <class T, int NL>
+cudaError_t some_launch(const FewArgs& f, size_t smem, int blocks, cudaStream_t s) {
+    const auto kernel = f.rows <= 8 ? class_some_kernel<T, 1, NL> : class_some_kernel<T, 2, NL>;
+    const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), kSomeSmem, false);
+    return e != cudaSuccess ? e : chain(kernel, dim3((unsigned)blocks), 32 * kSomeWarps, smem, s, false, f);
 }
 // A gradient.  Tiles that are left over when all pairs have had the same number are cut along their reduction, so that they keep every pair busy too
 // (4096 x 1024 over 47 classes: 4 tiles, 18 shares each), down to 8 ring stages a share.  Sums for an fp32 result are added up in chunks.
@@ -852,9 +1011,15 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
             w.H = a.H; w.ldh = a.ldh; w.W = a.W; w.ldw = a.ldw; w.rows = nr; w.cols = D; w.classes = V; w.bias = a.bias; w.targets = targets; w.ntargets = p.ntargets; w.rowk = rowk;
             w.sc = z.unit; w.inv_t = z.inv_t; w.z = p.grads ? reinterpret_cast<float*>(z.C) : nullptr; w.ldz = p.ldg; w.stats = stats;
             nparts = (int)std::min<int64_t>(kFewBlocks, (p.ldg + 31) / 32);
-            const bool wide = ((uintptr_t)a.W & 15) == 0 && (a.ldw * (int64_t)sizeof(T)) % 16 == 0;
-            GAD_TRY(p.nl == 2 ? (wide ? few_launch<T, 2, true>(w, few_smem(a), nparts, s) : few_launch<T, 2, false>(w, few_smem(a), nparts, s))
+            if (p.some) {
+                const size_t smem = some_smem(a);
+                nparts = (int)std::min<int64_t>(2 * kPairs, (p.ldg + 127) / 128);
+                if constexpr (sizeof(T) == 2) GAD_TRY(p.nl == 2 ? (some_launch<T, 2>(w, smem, nparts, s)) : (some_launch<T, 1>(w, smem, nparts, s)));
+            } else {
+                const bool wide = ((uintptr_t)a.W & 15) == 0 && (a.ldw * (int64_t)sizeof(T)) % 16 == 0;
+                GAD_TRY(p.nl == 2 ? (wide ? few_launch<T, 2, true>(w, few_smem(a), nparts, s) : few_launch<T, 2, false>(w, few_smem(a), nparts, s))
                               : (wide ? few_launch<T, 1, true>(w, few_smem(a), nparts, s) : few_launch<T, 1, false>(w, few_smem(a), nparts, s)));
+            }
         } else GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, p.add_up, s) : go_stats<1>(mapH, mapW, z, p.add_up, s));
         FinishArgs f{};
         f.stats = stats; f.parts = nparts; f.rows = nr; f.rowk = rowk + r0; f.sc = z.unit; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;

@@ -133,7 +133,8 @@ def compare(got, ref, s, T=1.0):
 
 
 CLASS_SHAPES = [(1, 1, 1), (1, 64, 2), (5, 7, 3), (3, 72, 128), (130, 100, 129), (257, 64, 300), (2, 4096, 1000), (777, 500, 2049), (300, 130, 47), (1, 256, 40000), (4, 1001, 700), (8, 328, 5000), (7, 6000, 90),
-                (20, 2500, 300), (130, 640, 257), (9, 64, 1 << 20)]
+                (20, 2500, 300), (130, 640, 257), (9, 64, 1 << 20),
+                (5, 4096, 1000), (16, 1032, 4099), (32, 72, 33), (17, 40, 2000), (31, 3000, 515)]
 
 
 @gpu
@@ -153,7 +154,7 @@ def test_class_loss(N, D, V, dtype):
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
 @pytest.mark.parametrize("N,D,V,k,T,a", [(1, 64, 2, 1, 1.0, 0.0), (5, 7, 3, 3, 2.0, 0.0), (130, 100, 129, 17, 2.0, 0.3), (257, 64, 300, 130, 1.0, 0.5), (40, 512, 10007, 64, 0.5, 0.25),
                                          (33, 96, 2000, 1024, 4.0, 0.1), (64, 128, 500, 8, 3.0, 1.0),
-                                         (50, 72, 600, 5, 0.25, 0.5), (6, 200, 900, 7, 2.0, 0.5), (21, 2500, 300, 40, 1.5, 0.5)])
+                                         (50, 72, 600, 5, 0.25, 0.5), (6, 200, 900, 7, 2.0, 0.5), (21, 2500, 300, 40, 1.5, 0.5), (12, 328, 900, 33, 2.0, 0.3), (30, 96, 150, 60, 1.0, 0.0)])
 def test_distill_loss(N, D, V, k, T, a, dtype):
     for bias, weights, ignored in ((False, False, 0.0), (True, True, 0.4)):
         s = make(N, D, V, dtype, 2, k=k, bias=bias, weights=weights, ignored=ignored)
