@@ -51,12 +51,12 @@ def _matrix(t, name, device=None, shape=None):
         raise GadError(-1, "%s must be a float32, float16 or bfloat16 CUDA matrix" % name)
     if device is not None and t.device != device:
         raise GadError(-1, "%s is on another device" % name)
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         raise GadError(-1, "%s must be %d x %d" % ((name,) + shape))
     rows, cols = t.shape
-    if cols < 1 or (cols > 1 and t.stride(1) != 1):
+    ld, inner = t.stride()
+    if cols < 1 or (cols > 1 and inner != 1):
         raise GadError(-1, "%s must have at least one column, and its rows contiguous" % name)
-    ld = t.stride(0)
     if rows <= 1:
         return max(ld, cols)
     if ld != 0 and ld < cols:
@@ -68,7 +68,7 @@ def _vector(t, name, n, dtypes, device):
     """Checks a contiguous CUDA vector of n elements (None passes); returns its address or None."""
     if t is None:
         return None
-    if not (t.is_cuda and t.device == device and t.dtype in dtypes and t.dim() == 1 and t.shape[0] == n and (n <= 1 or t.stride(0) == 1)):
+    if not (t.dtype in dtypes and t.device == device and t.shape == (n,) and t.is_contiguous()):
         raise GadError(-1, "%s must be a contiguous vector of %d elements (%s) on the same device" % (name, n, " or ".join(str(d) for d in dtypes)))
     return t.data_ptr()
 
@@ -118,7 +118,7 @@ def layer_norm(x, gamma=None, beta=None, *, eps=1e-5, stream=None):
     if _elsewhere(dev, stream):
         with _switch(dev, stream):
             return layer_norm(x, gamma, beta, eps=eps)
-    y = x.new_empty((rows, cols))
+    y = torch.empty_like(x) if ldx == cols and not x.requires_grad else x.new_empty((rows, cols))     # (the former is the quicker)
     stats = x.new_empty((2, rows), dtype=torch.float32)
     at = stats.data_ptr()
     _ck(L.gad_layer_norm(x.data_ptr(), ldx, rows, cols, _DTYPES[dt], g, b, _DTYPES[ptype], eps, y.data_ptr(), cols, at, at + 4 * rows, _stream(dev)), "gad_layer_norm")
