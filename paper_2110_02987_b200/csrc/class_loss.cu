@@ -41,10 +41,11 @@ __device__ __forceinline__ int64_t load_index(const void* p, int bytes, int64_t 
 
 // A row as operands: copied (16-bit types), or in three bfloat16 parts.  dst rows are 16-byte aligned.
 template <class T>
-__device__ __forceinline__ void pack_row(const T* __restrict__ src, int cols, bool keep, void* dst, int64_t at, int64_t part_stride, int t, int threads) {
+__device__ __forceinline__ void pack_row(const T* __restrict__ src, int cols, bool keep, void* __restrict__ dst, int64_t at, int64_t part_stride, int t, int threads) {
     if constexpr (sizeof(T) == 4) {
         __nv_bfloat16* d = reinterpret_cast<__nv_bfloat16*>(dst) + at;
         const int n4 = ((uintptr_t)src & 15) == 0 ? cols >> 2 : 0;
+#pragma unroll 4
         for (int c = t; c < n4; c += threads) {
             const float4 x = keep ? reinterpret_cast<const float4*>(src)[c] : make_float4(0.f, 0.f, 0.f, 0.f);
             __nv_bfloat16 p[4][3];
@@ -66,12 +67,16 @@ __device__ __forceinline__ void pack_row(const T* __restrict__ src, int cols, bo
         T* d = reinterpret_cast<T*>(dst) + at;
         // in the widest words that the row starts on (the copy does on all)
         const int wide = ((uintptr_t)src & 15) == 0 ? 8 : ((uintptr_t)src & 7) == 0 ? 4 : ((uintptr_t)src & 3) == 0 ? 2 : 1, n = cols / wide;
-        if (wide == 8)
+        if (wide == 8) {
+#pragma unroll 4
             for (int c = t; c < n; c += threads) reinterpret_cast<uint4*>(d)[c] = keep ? reinterpret_cast<const uint4*>(src)[c] : make_uint4(0u, 0u, 0u, 0u);
-        else if (wide == 4)
+        } else if (wide == 4) {
+#pragma unroll 4
             for (int c = t; c < n; c += threads) reinterpret_cast<uint2*>(d)[c] = keep ? reinterpret_cast<const uint2*>(src)[c] : make_uint2(0u, 0u);
-        else if (wide == 2)
+        } else if (wide == 2) {
+#pragma unroll 4
             for (int c = t; c < n; c += threads) reinterpret_cast<uint32_t*>(d)[c] = keep ? reinterpret_cast<const uint32_t*>(src)[c] : 0u;
+        }
         for (int c = (wide > 1 ? wide * n : 0) + t; c < cols; c += threads) d[c] = keep ? src[c] : from_float<T>(0.f);
     }
 }

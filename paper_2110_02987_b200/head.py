@@ -154,7 +154,7 @@ def layer_norm_backward(dy, x, mean, rstd, gamma=None, *, param_grads=True, stre
     if _elsewhere(x.device, stream):
         with _switch(x.device, stream):
             return layer_norm_backward(dy, x, mean, rstd, gamma, param_grads=param_grads)
-    dx = x.new_empty((rows, cols))
+    dx = torch.empty_like(x) if ldx == cols and not x.requires_grad else x.new_empty((rows, cols))
     dgamma = dbeta = ws = None
     nbytes, at_g, at_b, at_ws = 0, None, None, None
     if param_grads:
