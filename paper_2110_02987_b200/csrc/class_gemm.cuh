@@ -38,6 +38,7 @@ enum TileUse { kStats, kOut };
 
 // z of a row is kept as whole numbers of 1 / 2048 octaves below the largest of the 128 (64) classes that a draining warp has of it: 16 bits reach 32 octaves, and a
 // probability is off by 1.7e-4 of itself, a fourteenth of what bfloat16 and two thirds of what fp16 rounds off it.  The last code is a probability of zero.
+// Of two softmaxes the flatter one's octaves count (T > 1: those of z / T), or else classes behind the last code would lose their part of it; the sharper one is off by T (1 / T) times as much.
 constexpr float kCodeSteps = 2048.f;
 constexpr int kCodeZero = 65535;
 enum SaveAs { kSaveNone, kSaveCode, kSaveFloat };
@@ -65,6 +66,7 @@ struct TileArgs {
     const uint16_t* starts;    // [M x 2 tiles_n] a row's first target at or behind the first column of each half tile; null with one target
     float4* stats;             // [2 tiles_n x M]
     int save;                  // SaveAs
+    float code_steps, code_lowest;   // codes a unit of z (two softmaxes may need fewer than kCodeSteps), and what the last code stands for
     // what is written
     void* C;                   // kStats: z as saved [M x ldc]; kOut: the result
     long long ldc;
@@ -469,8 +471,9 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     }
                     if (a.save == kSaveCode) {
                         // rounded by the addition of 2^23, whose sum has the whole number in its low bits
+                        const float steps = NL == 2 ? a.code_steps : kCodeSteps, lowest = NL == 2 ? a.code_lowest : -(float)kCodeZero / kCodeSteps;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(fmaxf(v[j], -(float)kCodeZero / kCodeSteps), -kCodeSteps, 8388608.f);
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(fmaxf(v[j], lowest), -steps, 8388608.f);
                         drain_codes(buf, lane, v, reinterpret_cast<uint16_t*>(a.C) + (long long)row0 * a.ldc + tile_c + c0, a.ldc, rows);
                     }
                 } else if (tile_c + c0 < a.N) {

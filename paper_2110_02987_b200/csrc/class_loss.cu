@@ -627,7 +627,7 @@ struct GradArgs {
     const float4 *rowc, *rowk;
     const int2* targets; int ntargets;
     const float* scal;
-    float inv_t;
+    float inv_t, code_unit;                   // code_unit: of z a code (1 / code_steps)
     float* colsum;                            // [row blocks x ldg] or null
     int rows, classes;
 };
@@ -686,10 +686,11 @@ __global__ void __launch_bounds__(256) class_grad_kernel(const GradArgs a) {
                 float z[8];                   // log2 of exp(z) relative to the (first) sum
                 if constexpr (sizeof(Z) == 2) {
                     const float d = m[s] - rc.z;
-                    // a code behind the exponent of 2^23 is that number of steps above 2^23 = 4096 x 2048 of them: exact
+                    const float unit = NL == 2 ? a.code_unit : 1.f / kCodeSteps;
+                    // a code behind the exponent of 2^23 is that number of steps above 2^23 of them: exact
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        z[j] = fmaf(__uint_as_float(__byte_perm(h[j >> 1], 0x4B000000u, j & 1 ? 0x7632 : 0x7610)), -1.f / kCodeSteps, 4096.f) + d;
+                        z[j] = fmaf(__uint_as_float(__byte_perm(h[j >> 1], 0x4B000000u, j & 1 ? 0x7632 : 0x7610)), -unit, 8388608.f * unit) + d;
                     const uint32_t top = __vmaxu2(__vmaxu2(h[0], h[1]), __vmaxu2(h[2], h[3]));
                     if ((top >> 16) == kCodeZero || (top & 0xFFFFu) == kCodeZero) {
 #pragma unroll
@@ -847,6 +848,7 @@ struct ClassPlan {
     int parts, pairs;                // operand parts, products of them
     bool grads, pack_w, few, some, add_up;   // add_up: logits longer than a chunk are added up in chunks
     int ntargets, nl, save;
+    float code_steps;
     int width_v, tiles_v, width_d, tiles_d;
     int64_t ldp, ldg;                // row lengths of the packed operands, and of z and G
     int64_t block;                   // rows a block
@@ -868,8 +870,10 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     p.pack_w = (!p.few || a.dH) && (a.dtype == GAD_F32 || ((uintptr_t)a.W & 15) != 0 || (a.ldw * 2) % 16 != 0);
     p.ntargets = a.k + (a.labels ? 1 : 0);
     p.nl = a.k > 0 && a.labels && a.hard_weight > 0.f && a.hard_weight < 1.f && a.temperature != 1.f ? 2 : 1;
-    // a code's step is 1 / T times as large in the second softmax: up to twice it is still below what G is rounded by
-    p.save = !p.grads ? kSaveNone : a.dtype == GAD_F32 || p.few || (p.nl == 2 && a.temperature < 0.5f) ? kSaveFloat : kSaveCode;
+    // a code's step is T (1 / T) times as large in the sharper of two softmaxes: twice it is still below what G is rounded by in fp16, eight times in bfloat16
+    const float most_t = a.dtype == GAD_F16 ? 2.f : 8.f;
+    p.save = !p.grads ? kSaveNone : a.dtype == GAD_F32 || p.few || (p.nl == 2 && (a.temperature > most_t || a.temperature * most_t < 1.f)) ? kSaveFloat : kSaveCode;
+    p.code_steps = p.nl == 2 ? kCodeSteps / std::max(1.f, a.temperature) : kCodeSteps;
     p.ldp = round_up(D, 8);
     p.add_up = (D + CT_K - 1) / CT_K > (p.parts > 1 ? kChunkParts : kChunk);
     p.width_v = p.add_up ? 128 : width_for(V);
@@ -1010,7 +1014,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         z.sc = z.unit * cut_back(std::min(z.nkb, p.add_up ? z.chunk : z.nkb));
         z.inv_t = 1.f / T0;
         z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.starts = ra.starts ? ra.starts + r0 * ra.nstarts : nullptr; z.stats = stats;
-        z.save = p.save; z.C = ws + p.o_z; z.ldc = p.ldg;
+        z.save = p.save; z.code_steps = p.code_steps; z.code_lowest = -(float)kCodeZero / p.code_steps; z.C = ws + p.o_z; z.ldc = p.ldg;
         int nparts = 2 * p.tiles_v;
         if (p.few) {
             FewArgs w{};
@@ -1036,7 +1040,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         if (!p.grads) continue;
         GradArgs g{};
         g.z = z.C; g.ldz = p.ldg; g.G = ws + p.o_g; g.ldg = p.ldg; g.part_stride = nr * p.ldg; g.stats = stats; g.half_w = p.width_v / 2;
-        g.rowc = rowc; g.rowk = rowk + r0; g.targets = z.targets; g.ntargets = p.ntargets; g.scal = scal; g.inv_t = z.inv_t;
+        g.rowc = rowc; g.rowk = rowk + r0; g.targets = z.targets; g.ntargets = p.ntargets; g.scal = scal; g.inv_t = z.inv_t; g.code_unit = 1.f / p.code_steps;
         g.colsum = a.db ? reinterpret_cast<float*>(ws + p.o_colsum) : nullptr; g.rows = nr; g.classes = V;
         auto grad = a.db ? (p.nl == 2 ? class_grad_kernel<T, float, 2, true> : class_grad_kernel<T, float, 1, true>)
                          : (p.nl == 2 ? class_grad_kernel<T, float, 2, false> : class_grad_kernel<T, float, 1, false>);

@@ -6,7 +6,7 @@ which five are 2^-8 of the first, plus 2^-24 dropped: counted as K / 16 + K / 25
 than the result, so errors of whole tensors are held to ``steps * u`` relative to their norm.
 A logit's error d goes to p as a relative error of d + (error of lse <= largest d); exp2 and the log of the sum add 2^-21 each, and the argument's rounding u |z| log2(e).
 G is rounded to the operand type (half a step h = eps / 2), the result once more; the terms of a result's sum may cancel, so the first counts over their magnitudes.  With 16-bit operands a logarithm of a probability is kept in steps of 2^-11
-octaves: off by 2^-12 ln 2 of the probability (1 / T times that in the softmax of z / T).  Everything is summed with a factor of 1, none is tuned."""
+octaves of the flatter softmax (of z, or of z / T): off by 2^-12 ln 2 of its probability, and T or 1 / T times that in the sharper one.  Everything is summed with a factor of 1, none is tuned."""
 import math
 
 import pytest
@@ -118,7 +118,7 @@ def compare(got, ref, s, T=1.0):
     assert ((got.row_loss.double() - ref["row_loss"]).abs() <= one + 2 * U * ref["row_loss"].abs() * max(1.0, T)).all()
     rows = ((ref["weights"] / max(1, int(ref["counts"].sum()))) * ref["row_loss"].abs().sum()).item()
     assert abs(got.loss.double() - ref["loss"]).item() <= one * ref["weights"] + 4 * U * max(1.0, T) * max(rows, abs(ref["loss"].item())) + 1e-30
-    p_rel = 2 * logit + 2.0 ** -20 + (0.0 if dt == torch.float32 else 2.0 ** -12 * 0.6932 * max(1.0, 1 / T))
+    p_rel = 2 * logit + 2.0 ** -20 + (0.0 if dt == torch.float32 else 2.0 ** -12 * 0.6932 * max(T, 1 / T))
     Wa, Ha = s["W"].double().abs(), torch.where(ref["counts"][:, None], s["H"].double().abs(), 0.0)
     sums = dict(dH=lambda m: m @ Wa, dW=lambda m: m.t() @ Ha, db=lambda m: m.sum(0))
     for name, K in (("dH", V), ("dW", N), ("db", N)):
@@ -259,6 +259,33 @@ def test_masked_classes_repeated_and_unknown_classes():
     s["classes"][5, 2] = 300
     got = pkg.distill_loss(**s)
     assert math.isnan(got.row_loss[5].item()) and math.isnan(got.loss.item()) and torch.isfinite(got.row_loss[:5]).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("T", [0.4, 2.0, 4.0, 8.0, 20.0])
+def test_classes_that_only_the_flatter_softmax_sees(T, dtype):
+    """Each 128 classes have one 26 above the others: 38 octaves in the softmax of z, but exp(-26 / T) in the other one, of 127 classes."""
+    import torch
+    s = make(300, 64, 2050, dtype, 5, k=5)
+    s["W"] *= 0.125
+    s["bias"] = torch.full((2050,), -26.0, dtype=s["W"].dtype, device="cuda")
+    s["bias"][17::128] = 0.0
+    s.update(temperature=T, hard_weight=0.5)
+    ref = reference(**s)
+    got = pkg.distill_loss(**s)
+    compare(got, ref, s, T)
+    if T >= 4:                                # without those classes the gradient of their biases would be off by all of it
+        low = torch.ones(2050, dtype=torch.bool, device="cuda")
+        low[17::128] = False
+        low[s["classes"].long().clamp(min=0).flatten().unique()] = False
+        low[s["labels"].long().clamp(min=0).unique()] = False
+        assert low.any()
+        want = ref["db"][low]
+        h = torch.finfo(s["W"].dtype).eps / 2
+        z_err = 2 * (dot_steps(64, s["W"].dtype) * 2 * U * ref["size"] + 4 * U * 1.45 * ref["zmax"]) / T + 2.0 ** -20 + 2.0 ** -12 * 0.6932
+        tiny = torch.finfo(s["W"].dtype).smallest_normal * torch.finfo(s["W"].dtype).eps / 2      # half a step of subnormals (the column sums are in fp32)
+        assert ((got.db.double()[low] - want).abs() <= (h + z_err + 16 * U) * want.abs() + tiny).all()
 
 
 @gpu
