@@ -18,6 +18,7 @@ from .binding import GAD_OK, GadError, load
 
 _DTYPES = {}     # torch dtype -> GAD_F32 / GAD_F16 / GAD_BF16, filled on first use (torch is imported late, as in the rest of the binding)
 _lib = torch = None
+_MOST = 2 ** 31 - 1     # the library's columns, classes and slots are 32-bit integers, to which ctypes would cut a longer one without a word
 
 
 class _ClassLossArgs(C.Structure):
@@ -57,6 +58,8 @@ def _matrix(t, name, device=None, shape=None):
     ld, inner = t.stride()
     if cols < 1 or (cols > 1 and inner != 1):
         raise GadError(-1, "%s must have at least one column, and its rows contiguous" % name)
+    if cols > _MOST:
+        raise GadError(-2, "%s has too many columns" % name)
     if rows <= 1:
         return max(ld, cols)
     if ld != 0 and ld < cols:
@@ -205,6 +208,8 @@ def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, 
         raise GadError(-1, "W must have H's type and number of columns")
     if V < 1 or (V > 1 and ldw == 0):
         raise GadError(-1, "W must have a row for every class")
+    if V > _MOST:
+        raise GadError(-2, "W has too many rows")
     b = _vector(bias, "bias", V, (dt,), dev)
     w = _vector(row_weights, "row_weights", N, (torch.float32,), dev)
     lab, lab_bytes = _indices(labels, "labels", (N,), dev) if labels is not None else (None, 4)
@@ -213,6 +218,8 @@ def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, 
         if classes.dim() != 2 or classes.shape[1] < 1:
             raise GadError(-1, "classes must be rows x k, k of 1 and more")
         k = classes.shape[1]
+        if k > _MOST:
+            raise GadError(-2, "classes has too many slots")
         tc, tc_bytes = _indices(classes, "classes", (N, k), dev)
         if not (teacher.is_cuda and teacher.device == dev and teacher.dtype in _DTYPES and tuple(teacher.shape) == (N, k) and teacher.is_contiguous()):
             raise GadError(-1, "teacher must be a contiguous floating tensor of the shape of classes on the same device")

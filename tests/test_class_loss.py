@@ -8,6 +8,7 @@ A logit's error d goes to p as a relative error of d + (error of lse <= largest 
 G is rounded to the operand type (half a step h = eps / 2), the result once more; the terms of a result's sum may cancel, so the first counts over their magnitudes.  With 16-bit operands a logarithm of a probability is kept in steps of 2^-11
 octaves of the flatter softmax (of z, or of z / T): off by 2^-12 ln 2 of its probability, and T or 1 / T times that in the sharper one.  Everything is summed with a factor of 1, none is tuned."""
 import math
+import types
 
 import pytest
 
@@ -468,6 +469,22 @@ def test_refusals_on_the_host():
     for code, kw, ws, nws in ((-1, dict(W=None), 256, need), (-1, dict(H=None), 256, need), (-1, dict(labels=None), 256, need), (-1, dict(loss=None), 256, need), (-1, dict(row_loss=None), 256, need),
                               (-1, dict(status=None), 256, need), (-1, dict(k=2), 256, need), (-5, dict(), None, need), (-5, dict(), 256, need - 1), (-5, dict(), 128, need)):
         assert L.gad_class_loss(C.byref(_args(**kw)), ws, nws, None) == code, kw
+
+
+def test_sizes_behind_32_bits_are_refused_not_cut():
+    import torch
+    from paper_2110_02987_b200 import head
+    head._load()
+
+    def tensor(*shape, dtype=torch.bfloat16):      # what the checks look at; nothing is allocated
+        return types.SimpleNamespace(dim=lambda: 2, dtype=dtype, is_cuda=True, device="a device", shape=shape, stride=lambda: (shape[1], 1))
+    many = 2 ** 32 + 8
+    for call in (lambda: pkg.class_loss(tensor(4, 8), tensor(many, 8), tensor(4)), lambda: pkg.class_loss(tensor(4, many), tensor(8, many), tensor(4)),
+                 lambda: pkg.distill_loss(tensor(4, 8), tensor(8, 8), tensor(4, many, dtype=torch.int32), tensor(4, many)),
+                 lambda: pkg.layer_norm(tensor(1, many)), lambda: pkg.layer_norm_backward(tensor(1, many), tensor(1, many), None, None)):
+        with pytest.raises(GadError) as e:
+            call()
+        assert e.value.code == -2
 
 
 def test_refusals_of_tensors_without_a_gpu():
