@@ -423,7 +423,8 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     if (cur.x < tile_c) cur.x = INT_MAX;                    // (one target, in front of these columns)
                 }
             }
-            // No bias and nothing but classes: the logit and its distance from the largest are one multiply-add.
+            // No bias and nothing but classes: the logit and its distance from the largest are one multiply-add, which rounds once.  The largest logit is therefore rounded up: rounded
+            // to nearest it can lie below the exact product, and the distance of its own class, behind the multiply-add, above zero, where there is no code.
             const bool plain = !a.bias && (t.n + 1) * a.width <= a.N;
             const auto largest = [&](int c0, const float (&v)[32]) {
                 float m[4];
@@ -544,7 +545,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 if constexpr (USE == kStats) {
                     largest(0, sum[0]);
                     largest(32, sum[1]);
-                    if (plain) m2 *= a.sc;
+                    if (plain) m2 = __fmul_ru(m2, a.sc);
                     take(0, sum[0]);
                     take(32, sum[1]);
                 } else {
@@ -571,7 +572,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     tmem_ld32_start(at + (c0 + 64 < half_w ? c0 + 64 : 0), u);
                     largest(c0 + 32, v);
                 }
-                if (plain) m2 *= a.sc;
+                if (plain) m2 = __fmul_ru(m2, a.sc);
                 for (int c0 = 0; c0 < half_w; c0 += 64) {
                     tmem_ld32_wait(u);
                     tmem_ld32_start(at + c0 + 32, v);

@@ -1,0 +1,78 @@
+"""Gradients of the losses over many classes element by element, where a norm over the whole tensor would not see a lost row, tile or class.
+
+Bounds, in the notation of test_class_loss.py (u = 2^-24, h half a step of the type, K terms of a sum in ``dot_steps(K)`` steps of the tensor core).  An element of dH or dW is a sum over
+G of magnitude A = |G| |W| (|G|^T |H|).  Worst case of each part: the cut of the sum 2u a step; G's rounding h and the result's h of the result; p off by exp(2 d + ...) - 1 of
+itself for logits off by d, over the magnitudes B of p and tau (they cancel in G); a probability below 2^-32 of its neighbours' largest, and a G below fp16's normal numbers, 2^-31 of the
+largest coefficient together (the latter is 2^14 or more in fp16, whose half step there is 2^-25).  db is summed in fp32 before any rounding: four rows a warp, eight warps, then runs of an eighth of
+the blocks of 32 rows."""
+import math
+
+import pytest
+
+import __graft_entry__ as entry
+import paper_2110_02987_b200 as pkg
+from test_class_loss import U, dot_steps, make, reference
+
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    entry.build()
+
+
+def compare_elements(got, ref, s, T=1.0):
+    import torch
+    dt = s["H"].dtype
+    N, D = s["H"].shape
+    V = s["W"].shape[0]
+    h = torch.finfo(dt).eps / 2 if dt != torch.float32 else U
+    two = "classes" in s and s["labels"] is not None and 0 < s["hard_weight"] < 1 and T != 1     # softmaxes: the sharper one's steps are longer
+    code = 0.0 if dt == torch.float32 else 2.0 ** -12 * 0.6932 * (max(T, 1 / T) if two else 1.0)
+    T = min(T, 1.0)                                                      # z / T is what is off, by 1 / T times as much
+    logit = (dot_steps(D, dt) * 2 * U * ref["size"] + 4 * U * 1.45 * ref["zmax"]) / T
+    p_rel = math.expm1(2 * logit + 2.0 ** -20 + code) + 2 * U
+    assert p_rel < 0.3                                                   # (or the comparison says nothing)
+    assert int(got.status.item()) == 0
+    Wa, Ha = s["W"].double().abs(), torch.where(ref["counts"][:, None], s["H"].double().abs(), 0.0)
+    G, B = ref["G"].abs(), ref["terms"]
+    low = 2.0 ** -31 * B.sum(1).max()
+    tiny = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}.get(dt, 1e-37)
+    for name, of, K in (("dH", lambda m: m @ Wa, V), ("dW", lambda m: m.t() @ Ha, N), ("db", lambda m: m.sum(0), 0)):
+        x = getattr(got, name)
+        if x is None:
+            continue
+        want = ref[name]
+        steps = dot_steps(K, dt) * 2 + 2 if K else N / 256 + 24
+        tol = h * want.abs() + ((h if K else 0) + steps * U) * of(G) + p_rel * (1 + h) * of(B) + of(torch.full_like(G, 1.0) * low) + tiny
+        off = (x.double() - want).abs()
+        assert bool((off <= tol).all()), "%s: element %s off by %.3g, %.3g times its bound" % (
+            name, torch.nonzero(~(off <= tol))[0].tolist(), off[~(off <= tol)][0].item(), (off / tol).nan_to_num(nan=math.inf).max().item())
+
+
+def offset_logits(s, offset):
+    """Every logit of every row moved by `offset`, in the first column of the matrices; the others decide between the classes."""
+    s["H"][:, 0] = 64.0
+    s["W"][:, 0] = offset / 64.0
+    return s
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("offset", [1024.0, 3000.0, -3000.0, 6016.0, 12032.0, -20032.0])
+def test_gradients_at_large_logits_without_a_bias(offset, dtype):
+    """The largest class's distance from itself is no more than zero, whatever its product with log2(e) is rounded to."""
+    s = offset_logits(make(300, 64, 768, dtype, 3), offset)
+    compare_elements(pkg.class_loss(**s), reference(**s), s)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("D", [64, 2112])
+@pytest.mark.parametrize("T,offset", [(0.25, 1500.0), (0.05, 256.0), (0.01, 31.0), (0.01, -62.0), (0.004, 16.0)])
+def test_gradients_at_small_temperatures_without_a_bias(T, offset, D, dtype):
+    s = make(300, D, 512, dtype, 4, k=3)
+    s["W"] *= T                                                          # logits / T as spread as the others
+    offset_logits(s, offset)
+    s.update(temperature=T, labels=None)
+    compare_elements(pkg.distill_loss(**s), reference(**s), s, T)
