@@ -38,13 +38,13 @@ def compare_elements(got, ref, s, T=1.0):
     G, B = ref["G"].abs(), ref["terms"]
     low = 2.0 ** -31 * B.sum(1).max()
     tiny = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}.get(dt, 1e-37)
-    for name, of, K in (("dH", lambda m: m @ Wa, V), ("dW", lambda m: m.t() @ Ha, N), ("db", lambda m: m.sum(0), 0)):
+    for name, of, ones, K in (("dH", lambda m: m @ Wa, Wa.sum(0), V), ("dW", lambda m: m.t() @ Ha, Ha.sum(0), N), ("db", lambda m: m.sum(0), N, 0)):
         x = getattr(got, name)
         if x is None:
             continue
         want = ref[name]
         steps = dot_steps(K, dt) * 2 + 2 if K else N / 256 + 24
-        tol = h * want.abs() + ((h if K else 0) + steps * U) * of(G) + p_rel * (1 + h) * of(B) + of(torch.full_like(G, 1.0) * low) + tiny
+        tol = h * want.abs() + ((h if K else 0) + steps * U) * of(G) + p_rel * (1 + h) * of(B) + low * ones + tiny
         off = (x.double() - want).abs()
         assert bool((off <= tol).all()), "%s: element %s off by %.3g, %.3g times its bound" % (
             name, torch.nonzero(~(off <= tol))[0].tolist(), off[~(off <= tol)][0].item(), (off / tol).nan_to_num(nan=math.inf).max().item())
@@ -76,3 +76,65 @@ def test_gradients_at_small_temperatures_without_a_bias(T, offset, D, dtype):
     offset_logits(s, offset)
     s.update(temperature=T, labels=None)
     compare_elements(pkg.distill_loss(**s), reference(**s), s, T)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("N,D,V", [(1, 1, 1), (5, 7, 3), (130, 100, 129), (257, 64, 300), (777, 500, 2049), (300, 130, 47), (2, 4096, 1000), (16, 1032, 4099), (20, 2500, 300), (31, 3000, 515), (1300, 200, 5000),
+                                   (40000, 33, 47), (2600, 500, 513)])
+def test_every_element_of_the_gradients(N, D, V, dtype):
+    """Odd sizes: what is left over in the last tile of every kind, tiles cut along their reduction, sums in chunks."""
+    for bias, weights, ignored in ((False, False, 0.0), (True, True, 0.4)):
+        s = make(N, D, V, dtype, 1, bias=bias, weights=weights, ignored=ignored)
+        compare_elements(pkg.class_loss(**s), reference(**s), s)
+
+
+@gpu
+@pytest.mark.parametrize("N,D,V,dtype", [(60000, 40, 20011, "bfloat16"), (50000, 40, 9001, "float32")])
+def test_every_element_over_blocks_of_rows(N, D, V, dtype):
+    s = make(N, D, V, dtype, 4, ignored=0.1, bias=True)
+    compare_elements(pkg.class_loss(**s), reference(**s), s)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("N,D,V,k,T,a", [(5, 7, 3, 3, 2.0, 0.0), (130, 100, 129, 17, 2.0, 0.3), (257, 64, 300, 130, 1.0, 0.5), (40, 512, 10007, 64, 0.5, 0.25), (33, 96, 2000, 1024, 4.0, 0.1), (21, 2500, 300, 40, 1.5, 0.5),
+                                         (777, 500, 2049, 9, 3.0, 0.5)])
+def test_every_element_of_a_distillation(N, D, V, k, T, a, dtype):
+    for bias, weights, ignored in ((False, False, 0.0), (True, True, 0.4)):
+        s = make(N, D, V, dtype, 2, k=k, bias=bias, weights=weights, ignored=ignored)
+        s.update(temperature=T, hard_weight=a)
+        if a == 0:
+            s["labels"] = None
+        compare_elements(pkg.distill_loss(**s), reference(**s), s, T)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("N,D,V,pad", [(1, 9, 5, 0), (4, 72, 700, 3), (16, 72, 130, 8), (70, 120, 333, 1), (300, 257, 2049, 5), (1300, 2100, 515, 0)])
+def test_what_the_outputs_held_before_is_gone_and_nothing_else_is_written(N, D, V, pad, dtype):
+    """Through the C entry: outputs of NaN, a row stride beyond the columns, and a margin on either side."""
+    import ctypes as C
+    import torch
+    from paper_2110_02987_b200 import head
+    L = head._load()
+    s = make(N, D, V, dtype, 6, bias=True)
+    dt, margin = s["H"].dtype, 64
+    want = pkg.class_loss(**s)
+
+    def room(rows, cols, ld, t=dt):
+        buf = torch.full((margin + rows * ld + margin,), math.nan, dtype=t, device="cuda")
+        return buf, buf[margin:margin + rows * ld].view(rows, ld)[:, :cols]
+    outs = dict(loss=room(1, 1, 1, torch.float32), row_loss=room(1, N, N, torch.float32), dH=room(N, D, D + pad), dW=room(V, D, D + pad), db=room(1, V, V))
+    status = torch.full((3,), 77, dtype=torch.int32, device="cuda")
+    at = {k: v[1].data_ptr() for k, v in outs.items()}
+    a = head._ClassLossArgs(dtype=head._DTYPES[dt], cols=D, classes=V, rows=N, H=s["H"].data_ptr(), ldh=D, W=s["W"].data_ptr(), ldw=D, bias=s["bias"].data_ptr(), labels=s["labels"].data_ptr(),
+                            label_bytes=4, k=0, target_bytes=4, temperature=1.0, hard_weight=1.0, scale=1.0, mean=1, lddh=D + pad, lddw=D + pad, status=status[1:].data_ptr(), **at)
+    need = C.c_size_t(0)
+    assert L.gad_class_loss_workspace_bytes(C.byref(a), C.byref(need)) == 0
+    ws = torch.full((need.value + 256,), 255, dtype=torch.uint8, device="cuda")       # (NaN in every type)
+    assert L.gad_class_loss(C.byref(a), ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == 0
+    assert status.tolist() == [77, 0, 77] and bool((ws[need.value:] == 255).all())
+    for name, (buf, view) in outs.items():
+        assert torch.equal(view.reshape(-1), getattr(want, name).reshape(-1)), name
+        assert bool(torch.isfinite(view.float()).all()) and int(torch.isnan(buf.float()).sum()) == buf.numel() - view.numel(), name
