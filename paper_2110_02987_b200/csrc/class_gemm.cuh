@@ -278,7 +278,7 @@ __device__ __forceinline__ TileAt tile_at(const TileArgs& a, long long u) {
 
 // USE as above; A_MN, B_MN: operand is MN-major; T: type of the result; NL: softmaxes (temperatures) at once.
 // ADD_UP: the tensor core cuts its accumulator off at every addition (it does not round), always towards zero, so that a sum comes out short in proportion to its
-// length (cut_back) and the more uncertain the longer it is.  Where a result is wanted to fp32 accuracy the
+// length (cut_back) and the more uncertain the longer it is.  Where a result is wanted to fp32 accuracy, or the sum is so long that a 16-bit result would show it, the
 // reduction is cut into chunks whose sums the draining threads add up in registers.  Of operands in parts a chunk has all products, the smallest first (what they lose is
 // small), so that the parts come from HBM once: with the products one behind the other over the whole reduction G was read six times (8192 x 4096 x 256: 92 us).
 // Logits are then taken in tiles 128 columns wide: 64 sums a thread, four accumulators, three of which fill while the sums of a tile are worked on.  Gradients, with many

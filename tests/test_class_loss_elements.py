@@ -138,3 +138,26 @@ def test_what_the_outputs_held_before_is_gone_and_nothing_else_is_written(N, D, 
     for name, (buf, view) in outs.items():
         assert torch.equal(view.reshape(-1), getattr(want, name).reshape(-1)), name
         assert bool(torch.isfinite(view.float()).all()) and int(torch.isnan(buf.float()).sum()) == buf.numel() - view.numel(), name
+
+
+@gpu
+@pytest.mark.parametrize("dtype,V", [("float16", 1 << 19), ("bfloat16", 1 << 20)])
+def test_sums_over_very_many_classes_are_not_cut_short(dtype, V):
+    """dH over very many classes, in so many tiles that none is cut along its reduction, where all terms have one sign and G is exact: logits of zero, so that every probability is
+    2^-19 (2^-20).  The tensor core adds 16 terms at a time and cuts off at most 2u of the sum; what it adds up before the sum goes on in fp32 may cost an eighth of half a step h of the
+    result, whatever V is, and the sums in fp32 one u each, of at most 2^7.  (G of the label, 1 / V - 1, is rounded to -1.)"""
+    import torch
+    N, D = 1280, 2048                                                    # 5 x 8 tiles for 74 pairs: two of them are not to share one
+    dt = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    W = torch.rand(V, D, generator=g, device="cuda", dtype=torch.float32).add_(0.5).to(dt)
+    labels = torch.randint(0, V, (N,), generator=g, device="cuda")
+    got = pkg.class_loss(torch.zeros(N, D, dtype=dt, device="cuda"), W, labels, mean=False, grads="H").check()
+    total = torch.zeros(D, dtype=torch.float64, device="cuda")
+    for i in range(0, V, 1 << 17):
+        total += W[i:i + (1 << 17)].double().sum(0)
+    hot = W[labels].double()
+    want = total / V - hot
+    h = torch.finfo(dt).eps / 2
+    sizes = total / V + hot                                              # no partial sum is larger
+    assert ((got.dH.double() - want).abs() <= h * want.abs() + (h / 8 + 2 ** 7 * U + 1 / V) * sizes).all()
