@@ -60,7 +60,7 @@ struct TileArgs {
     // kStats
     const void* bias;          // [classes] in the caller's type, or null
     int bias_type;
-    float sc, unit, inv_t;     // of the accumulator and of the bias: log2(e) (/ T with one softmax); 1 / T of the second softmax
+    float sc, inv_t;           // of the logits: log2(e) (/ T with one softmax); 1 / T of the second softmax
     const int2* targets;       // [M x ntargets] (class, weight), classes ascending
     int ntargets;
     const uint16_t* starts;    // [M x 2 tiles_n] a row's first target at or behind the first column of each half tile; null with one target
@@ -74,7 +74,6 @@ struct TileArgs {
     float* sums;               // [M x N]
     float* slots;              // [tiles - whole][shares][256 x width] sums of shares
     const float* scal;         // [1] factor of the results
-    float whole_sum;           // what the accumulators' cut leaves out, as a factor (cut_back)
 };
 
 // Products of operand parts, the smallest first, so that what an addition to the accumulator cuts off is small for as long as possible.
@@ -250,11 +249,6 @@ __device__ __forceinline__ void drain_codes(uint8_t* buf, int lane, const float 
     copy_out<16, uint16_t, false>(buf, lane, out, ld, rows, 32);
 }
 
-// The cut of the accumulator makes a sum of 16 n terms short by 1.4e-8 n of itself: measured over logits of 256 to 2048 terms of either sign (bfloat16 1.3e-8 to 1.5e-8,
-// fp16 1.6e-8 to 1.7e-8; with a drift 1.6e-8 to 2.0e-8 and 4e-8 to 5e-8; of one sign 2e-8 to 4e-8 and 8e-8 to 9e-8, the parts of a product that are cut too).  The mean of the
-// ordinary case is given back with a factor that the result is multiplied by anyway; 2048 terms are then off by 7e-7 at random instead of 2e-6 on one side.
-inline float cut_back(int blocks) { return (float)(1.0 + 1.4e-8 * 4 * blocks); }
-
 // A unit of work: a tile, and the blocks of its reduction.
 struct TileAt { int m, n, kb0, nkb, slot; };
 __device__ __forceinline__ long long units_of(const TileArgs& a) { return a.whole + ((long long)a.tiles_m * a.tiles_n - a.whole) * a.shares; }
@@ -277,8 +271,9 @@ __device__ __forceinline__ TileAt tile_at(const TileArgs& a, long long u) {
 }
 
 // USE as above; A_MN, B_MN: operand is MN-major; T: type of the result; NL: softmaxes (temperatures) at once.
-// ADD_UP: the tensor core cuts its accumulator off at every addition (it does not round), always towards zero, so that a sum comes out short in proportion to its
-// length (cut_back) and the more uncertain the longer it is.  Where a result is wanted to fp32 accuracy, or the sum is so long that a 16-bit result would show it, the
+// ADD_UP: the tensor core cuts its accumulator off at every addition (it does not round), always towards zero, so that a sum of 16 n terms comes out short by about 1.4e-8 n of
+// itself (measured over logits of 256 to 2048 terms of either sign; of one sign 4e-8 in bfloat16 and 9e-8 in fp16; the worst is 2^-23), and one whose parts need no more
+// than 24 bits, as whole numbers or rows with few values, not at all.  (A factor that gave the mean back made those wrong by as much.)  Where a result is wanted to fp32 accuracy, or the sum is so long that a 16-bit result would show it, the
 // reduction is cut into chunks whose sums the draining threads add up in registers.  Of operands in parts a chunk has all products, the smallest first (what they lose is
 // small), so that the parts come from HBM once: with the products one behind the other over the whole reduction G was read six times (8192 x 4096 x 256: 92 us).
 // Logits are then taken in tiles 128 columns wide: 64 sums a thread, four accumulators, three of which fill while the sums of a tile are worked on.  Gradients, with many
@@ -393,7 +388,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         uint8_t* buf = sm + CT_RING + 256 + CT_BIAS + ew * 2048;
         int acc = 0;
         uint32_t acc_phase = 0;
-        const float factor = USE == kOut ? a.scal[1] * a.whole_sum : 1.f;
+        const float factor = USE == kOut ? a.scal[1] : 1.f;
         const int bytes = USE == kOut ? store_bytes(a.C, a.ldc * (long long)sizeof(T)) : 16, sum_bytes = a.N % 4 == 0 ? 16 : a.N % 2 == 0 ? 8 : 4;
         for (long long u = blockIdx.x >> 1; u < units; u += ncl) {
             const TileAt t = tile_at(a, u);
@@ -413,7 +408,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                     if (a.bias && c < a.N)
                         b = a.bias_type == GAD_F32 ? reinterpret_cast<const float*>(a.bias)[c]
                             : a.bias_type == GAD_F16 ? to_float(reinterpret_cast<const __half*>(a.bias)[c]) : to_float(reinterpret_cast<const __nv_bfloat16*>(a.bias)[c]);
-                    bias[j] = b * a.unit;
+                    bias[j] = b * a.sc;
                 }
                 __syncwarp();
                 if (rv) {

@@ -779,7 +779,7 @@ __global__ void __launch_bounds__(256) class_join_kernel(const TileArgs a) {
     const TileAt t = tile_at(a, a.whole + (long long)i * a.shares);
     const int row = t.m * CT_M + r, c = t.n * a.width + x;
     if (row >= a.M || c >= a.N) return;
-    const float factor = a.scal[1] * a.whole_sum;
+    const float factor = a.scal[1];
     const float* slot = a.slots + ((long long)i * a.shares * CT_M + r) * a.width + x;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -840,7 +840,7 @@ int few_rows(int64_t n) { return n <= 1 ? 1 : n <= 2 ? 2 : 4; }
 size_t some_smem(const gad_class_loss_args& a) { return (size_t)(a.rows <= 8 ? 8 : 16) * some_stride(a.cols); }
 size_t few_smem(const gad_class_loss_args& a) { return 4 * (size_t)few_rows(a.rows) * (size_t)round_up(a.cols, 8); }
 
-// Blocks of 64 terms of a chunk: 2048 terms are cut by 1.8e-6 of their sum, of which cut_back gives the mean back; of fp32 operands 512, by 4.5e-7.  Longer logits go in tiles
+// Blocks of 64 terms of a chunk: 2048 terms are cut by 1.8e-6 of their sum; of fp32 operands 512, by 4.5e-7.  Longer logits go in tiles
 // 128 wide: with chunks of 1024 the distillation of 4096 x 2048 took 2.71 ms instead of 2.34.
 constexpr int kChunk = 32, kChunkParts = 8;
 
@@ -938,10 +938,11 @@ cudaError_t some_launch(const FewArgs& f, size_t smem, int blocks, cudaStream_t 
     const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), kSomeSmem, false);
     return e != cudaSuccess ? e : chain(kernel, dim3((unsigned)blocks), 32 * kSomeWarps, smem, s, false, f);
 }
-// Blocks of 64 terms of a 16-bit gradient's sum that the tensor core adds up before the sum moves to registers: it cuts off at most 2^-23 of the sum every 16 terms, and
-// all of a chunk at most an eighth of what the result is rounded by (2^-11 in fp16, 2^-8 in bfloat16).  Uncut sums of one sign over 2^19 classes
-// were off by 3.6 times the rounding of fp16, now 0.1; 4096 x 1024 fp16 against 32 768 classes 848 us instead of 838.
-template <class T> constexpr int kChunkOut = kChunkParts;
+// Blocks of 64 terms of a gradient's sum that the tensor core adds up before the sum moves to registers: it cuts off at most 2^-23 of the sum every 16 terms.  In 16-bit types
+// all of a chunk costs at most an eighth of what the result is rounded by (2^-11 in fp16, 2^-8 in bfloat16): uncut sums of one sign over 2^19 classes
+// were off by 3.6 times the rounding of fp16, now 0.1; 4096 x 1024 fp16 against 32 768 classes 848 us instead of 838.  fp32 gradients are off by 3.2e-7 to 3.6e-7 with chunks of 256 terms,
+// by 6.6e-7 with 512 (8192 x 256 against 4096 classes 374 us instead of 371, 2048 x 512 against 16 384 645 instead of 628).
+template <class T> constexpr int kChunkOut = 4;
 template <> constexpr int kChunkOut<__half> = 128;
 template <> constexpr int kChunkOut<__nv_bfloat16> = 1024;
 // A gradient.  Tiles that are left over when all pairs have had the same number are cut along their reduction, so that they keep every pair busy too
@@ -950,7 +951,6 @@ template <bool A_MN, class T>
 cudaError_t go_out(const CUtensorMap& A, const CUtensorMap& B, TileArgs a, cudaStream_t s) {
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, rest = tiles % kPairs;
     a.whole = (int)tiles; a.shares = 1; a.kb_share = a.nkb; a.chunk = kChunkOut<T>;
-    a.whole_sum = sizeof(T) == 4 ? cut_back(std::min(a.nkb, a.chunk)) : 1.f;   // (below what the other types round)
     if (rest) {
         const int want = (int)std::min<int64_t>(kPairs / rest, (int64_t)a.nkb * a.pairs / 8);
         if (want > 1) {
@@ -1017,8 +1017,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         z.N = V; z.tiles_n = p.tiles_v; z.width = p.width_v; z.nkb = (D + CT_K - 1) / CT_K; z.whole = z.tiles_m * z.tiles_n; z.shares = 1; z.kb_share = z.nkb;
         z.group = 32; z.a_row0 = (int)r0;
         z.bias = a.bias; z.bias_type = a.dtype;
-        z.unit = kLog2e * (p.nl == 1 && a.k > 0 && ra.hard < 1.f ? 1.f / T0 : 1.f);
-        z.sc = z.unit * cut_back(std::min(z.nkb, p.add_up ? z.chunk : z.nkb));
+        z.sc = kLog2e * (p.nl == 1 && a.k > 0 && ra.hard < 1.f ? 1.f / T0 : 1.f);
         z.inv_t = 1.f / T0;
         z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.starts = ra.starts ? ra.starts + r0 * ra.nstarts : nullptr; z.stats = stats;
         z.save = p.save; z.code_steps = p.code_steps; z.code_lowest = -(float)kCodeZero / p.code_steps; z.C = ws + p.o_z; z.ldc = p.ldg;
@@ -1026,7 +1025,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         if (p.few) {
             FewArgs w{};
             w.H = a.H; w.ldh = a.ldh; w.W = a.W; w.ldw = a.ldw; w.rows = nr; w.cols = D; w.classes = V; w.bias = a.bias; w.targets = targets; w.ntargets = p.ntargets; w.rowk = rowk;
-            w.sc = z.unit; w.inv_t = z.inv_t; w.z = p.grads ? reinterpret_cast<float*>(z.C) : nullptr; w.ldz = p.ldg; w.stats = stats;
+            w.sc = z.sc; w.inv_t = z.inv_t; w.z = p.grads ? reinterpret_cast<float*>(z.C) : nullptr; w.ldz = p.ldg; w.stats = stats;
             nparts = (int)std::min<int64_t>(kFewBlocks, (p.ldg + 31) / 32);
             if (p.some) {
                 const size_t smem = some_smem(a);
@@ -1039,7 +1038,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
             }
         } else GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, p.add_up, s) : go_stats<1>(mapH, mapW, z, p.add_up, s));
         FinishArgs f{};
-        f.stats = stats; f.parts = nparts; f.rows = nr; f.rowk = rowk + r0; f.sc = z.unit; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
+        f.stats = stats; f.parts = nparts; f.rows = nr; f.rowk = rowk + r0; f.sc = z.sc; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
         f.shares = reinterpret_cast<double*>(ws + p.o_lshares); f.share0 = (int)(r0 / kFinishRows); f.nshares = (int)((N + kFinishRows - 1) / kFinishRows);
         f.row_shares = ra.shares; f.nrow_shares = nrshares; f.ticket = ra.ticket; f.scale = a.scale; f.mean = a.mean; f.first = b == 0; f.final = b == p.nblocks - 1;
         f.scal = scal; f.loss = a.loss;

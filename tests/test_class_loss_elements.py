@@ -161,3 +161,46 @@ def test_sums_over_very_many_classes_are_not_cut_short(dtype, V):
     h = torch.finfo(dt).eps / 2
     sizes = total / V + hot                                              # no partial sum is larger
     assert ((got.dH.double() - want).abs() <= h * want.abs() + (h / 8 + 2 ** 7 * U + 1 / V) * sizes).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("D,sparse", [(512, False), (2048, False), (4096, False), (1433, True)])
+def test_logits_that_fp32_holds_exactly_are_exact(D, sparse, dtype):
+    """Whole numbers, and rows with few values (bag-of-words features): no partial sum needs more than 24 bits, so nothing is cut off and nothing is to be given back.  What is left:
+    the product with log2(e), its constant, the sum of the softmax, its logarithm and the way back, a rounding of the largest number each (|z| log2(e) is below 2 |z|: 2u of it counts as 4u of |z|)."""
+    import torch
+    N, V = 300, 500
+    g = torch.Generator().manual_seed(5)
+    dt = getattr(torch, dtype)
+    H = (torch.rand(N, D, generator=g) < 0.0125).float() if sparse else torch.randint(-4, 5, (N, D), generator=g).float()
+    W = torch.randint(-64 if sparse else -2, 65 if sparse else 3, (V, D), generator=g).float()
+    H, W = H.to(dt).cuda(), W.to(dt).cuda()
+    z = H.double() @ W.double().t()
+    labels = z.argmin(1)                                                 # the largest losses: twice the largest logit
+    row = torch.logsumexp(z, 1) - z.min(1).values
+    got = pkg.class_loss(H, W, labels, grads=False)
+    most = z.abs().amax(1)
+    assert ((got.row_loss.double() - row).abs() <= 3 * U * 2 * most + 2.0 ** -20).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("N", [64, 512, 2048])
+def test_gradients_that_are_whole_numbers_are_exact(N, dtype):
+    """One class has all of the probability and another is the label: G is 1 and -1, and dW, over whole numbers, has no rounding to do; N a power of two."""
+    import torch
+    D, V = 72, 300
+    dt = getattr(torch, dtype)
+    g = torch.Generator().manual_seed(6)
+    H = torch.zeros(N, D)
+    H[torch.arange(N), torch.randint(0, D, (N,), generator=g)] = 1.0    # a value a row: column sums of at most 2^8
+    bias = torch.zeros(V)
+    bias[17] = 1024.0
+    got = pkg.class_loss(H.to(dt).cuda(), torch.zeros(V, D, dtype=dt, device="cuda"), torch.full((N,), 290, device="cuda"), bias=bias.to(dt).cuda())
+    count = H.double().sum(0)
+    assert count.max() <= 2 ** 8
+    want = torch.zeros(V, D, dtype=torch.float64)
+    want[17], want[290] = count / N, -count / N
+    assert torch.equal(got.dW.double().cpu(), want)
+    assert not got.dH.any() and got.db[17].item() == 1.0 and got.db[290].item() == -1.0
