@@ -413,9 +413,14 @@ typedef struct {
     int32_t* status;               /* device [1]: 0, or the code of a bounded wait that ran out (the other outputs are then undefined) */
 } gad_class_loss_args;
 
-/* Device workspace of gad_class_loss (256-byte aligned): a copy of H (and of W where it is fp32 or its rows do not start on 16 bytes) and, for gradients, at most
- * about 2 GB for a block of the rows x classes matrix (or 256 rows of it, where those take more), and the sums of dW in fp32 where that does not
- * hold all rows.  Depends on sizes, types, strides, which pointers are NULL, and W's alignment.  Host-only. */
+/* Device workspace of gad_class_loss (256-byte aligned):
+ *   - a copy of H, and of W where it is fp32 or its rows do not start on 16 bytes: 2 bytes a value, 6 in fp32;
+ *   - for gradients, logits and gradients of logits of a block of rows: 2 bytes a logit in fp16 and bfloat16 (6 with up to 16 rows, or with two softmaxes of
+ *     temperatures outside 1/2 .. 2 in fp16, 1/8 .. 8 in bfloat16), 10 in fp32.  A block takes about 2 GB at most, or 256 rows where those take more: all rows
+ *     in one block where that holds them, else dW's sums in fp32 beside it;
+ *   - statistics, about 0.15 bytes a logit of a block (without gradients a block has about 2^31 logits at most);
+ *   - 8 (k + 1) + 41 bytes a row, and where its targets start: rows x classes / 64 bytes (/ 32 with long rows) up to 256 MB, or that of a block.
+ * Depends on sizes, types, strides, which pointers are NULL, and W's alignment.  Host-only. */
 int gad_class_loss_workspace_bytes(const gad_class_loss_args* args, size_t* bytes);
 int gad_class_loss(const gad_class_loss_args* args, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -29,6 +29,7 @@ constexpr int kMostTargets = 1024;                       // teacher logits a row
 // Bytes of probabilities and gradients of logits held at once, about a hundredth of the GPU's memory.  Several blocks of rows also hold the sums of dW in fp32 and read and
 // write them (8192 x 2048 against 100 003 classes: one block of 1.6 GB 8.6 ms, two of 0.8 GB and 0.8 GB of sums 9.1 ms).
 constexpr int64_t kBlockBytes = 2ll << 30;
+constexpr int64_t kStartsBytes = kBlockBytes / 8;        // of target starts at once
 constexpr float kLog2e = 1.44269504f;
 
 template <class P> __device__ __forceinline__ float load_as_float(const void* p, int64_t i) { return to_float(reinterpret_cast<const P*>(p)[i]); }
@@ -89,7 +90,7 @@ struct RowArgs {
     float hard, temperature;
     void* Hp; int64_t ldp, part_stride;
     int2* targets; int ntargets;
-    uint16_t* starts; int nstarts, start_w;               // [rows x nstarts] first target at or behind every start_w-th class
+    uint16_t* starts; int nstarts, start_w;               // [rows x nstarts] first target at or behind every start_w-th class; or null
     float4* rowk;
     int64_t rows;
     struct RowShare* shares; unsigned* ticket;
@@ -220,6 +221,24 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
     if (t == 0) {
         a.shares[r] = {counts, counts ? fabsf(weight) * (ha + hb * tt) : 0.f};
         if (r == 0) { *a.ticket = 0u; *a.status = 0; }
+    }
+}
+
+// Where a row's targets start in every half tile, for a block of rows: where the table for all rows at once (rows x classes / 64 bytes, from the rows kernel) would be larger than
+// kStartsBytes.  A block a row, bound by the latency of its look-ups (16 384 rows of 9 targets against 131 072 classes 90 us of 6.1 ms, in the rows kernel 25).
+__global__ void __launch_bounds__(128) class_starts_kernel(const int2* __restrict__ targets, int ntargets, uint16_t* __restrict__ starts, int nstarts, int start_w) {
+    const int64_t r = blockIdx.x;
+    pdl_next();
+    pdl_wait();
+    after_wait(targets);
+    const int2* list = targets + r * ntargets;
+    for (int b = threadIdx.x; b < nstarts; b += 128) {
+        int e = 0, hi = ntargets;
+        while (e < hi) {
+            const int mid = (e + hi) >> 1;
+            if (list[mid].x < b * start_w) e = mid + 1; else hi = mid;
+        }
+        starts[r * nstarts + b] = (uint16_t)e;
     }
 }
 
@@ -847,6 +866,7 @@ constexpr int kChunk = 32, kChunkParts = 8;
 struct ClassPlan {
     int parts, pairs;                // operand parts, products of them
     bool grads, pack_w, few, some, add_up;   // add_up: logits longer than a chunk are added up in chunks
+    bool starts_at_once;             // target starts of all rows from the rows kernel
     int ntargets, nl, save;
     float code_steps;
     int width_v, tiles_v, width_d, tiles_d;
@@ -892,7 +912,8 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
     p.o_hp = room(2 * p.parts * N * p.ldp);
     p.o_wp = p.pack_w ? room(2 * p.parts * (int64_t)V * p.ldp) : 0;
     p.o_targets = room(8 * N * p.ntargets);
-    p.o_starts = p.ntargets > 1 && !p.few ? room(2 * N * 2 * p.tiles_v) : 0;
+    p.starts_at_once = 4 * N * p.tiles_v <= kStartsBytes;
+    p.o_starts = p.ntargets > 1 && !p.few ? room(4 * (p.starts_at_once ? N : p.block) * p.tiles_v) : 0;
     p.o_rowk = room(16 * N);
     p.o_rshares = room((int64_t)sizeof(RowShare) * N);
     p.o_lshares = room((int64_t)sizeof(double) * ((N + kFinishRows - 1) / kFinishRows));
@@ -984,8 +1005,8 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
     ra.tclasses = a.target_classes; ra.tclass_bytes = a.target_bytes; ra.teacher = a.teacher; ra.teacher_type = a.teacher_dtype; ra.k = a.k;
     ra.weights = a.row_weights; ra.hard = a.k > 0 ? (a.labels ? a.hard_weight : 0.f) : 1.f; ra.temperature = T0;
     ra.Hp = Hp; ra.ldp = p.ldp; ra.part_stride = N * p.ldp; ra.targets = targets; ra.ntargets = p.ntargets; ra.rowk = rowk;
-    ra.starts = p.o_starts ? reinterpret_cast<uint16_t*>(ws + p.o_starts) : nullptr; ra.nstarts = 2 * p.tiles_v; ra.start_w = p.width_v / 2;
-   
+    uint16_t* starts = p.o_starts ? reinterpret_cast<uint16_t*>(ws + p.o_starts) : nullptr;
+    ra.starts = p.starts_at_once ? starts : nullptr; ra.nstarts = 2 * p.tiles_v; ra.start_w = p.width_v / 2;
     ra.rows = N; ra.shares = reinterpret_cast<RowShare*>(ws + p.o_rshares); ra.ticket = reinterpret_cast<unsigned*>(scal + 8); ra.status = a.status;
     const int nrshares = (int)(a.k > 0 ? N : (N + 7) / 8);
     GAD_TRY(a.k > 0 ? chain(class_rows_kernel<T>, dim3((unsigned)N), kRowThreads, 12 * (size_t)p.ntargets, s, true, ra)
@@ -1019,7 +1040,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         z.bias = a.bias; z.bias_type = a.dtype;
         z.sc = kLog2e * (p.nl == 1 && a.k > 0 && ra.hard < 1.f ? 1.f / T0 : 1.f);
         z.inv_t = 1.f / T0;
-        z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.starts = ra.starts ? ra.starts + r0 * ra.nstarts : nullptr; z.stats = stats;
+        z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.starts = ra.starts ? ra.starts + r0 * ra.nstarts : starts; z.stats = stats;
         z.save = p.save; z.code_steps = p.code_steps; z.code_lowest = -(float)kCodeZero / p.code_steps; z.C = ws + p.o_z; z.ldc = p.ldg;
         int nparts = 2 * p.tiles_v;
         if (p.few) {
@@ -1036,7 +1057,10 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
                 GAD_TRY(p.nl == 2 ? (wide ? few_launch<T, 2, true>(w, few_smem(a), nparts, s) : few_launch<T, 2, false>(w, few_smem(a), nparts, s))
                               : (wide ? few_launch<T, 1, true>(w, few_smem(a), nparts, s) : few_launch<T, 1, false>(w, few_smem(a), nparts, s)));
             }
-        } else GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, p.add_up, s) : go_stats<1>(mapH, mapW, z, p.add_up, s));
+        } else {
+            if (starts && !p.starts_at_once) GAD_TRY(chain(class_starts_kernel, dim3((unsigned)nr), 128, 0, s, false, z.targets, p.ntargets, starts, ra.nstarts, ra.start_w));
+            GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, p.add_up, s) : go_stats<1>(mapH, mapW, z, p.add_up, s));
+        }
         FinishArgs f{};
         f.stats = stats; f.parts = nparts; f.rows = nr; f.rowk = rowk + r0; f.sc = z.sc; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
         f.shares = reinterpret_cast<double*>(ws + p.o_lshares); f.share0 = (int)(r0 / kFinishRows); f.nshares = (int)((N + kFinishRows - 1) / kFinishRows);

@@ -204,3 +204,66 @@ def test_gradients_that_are_whole_numbers_are_exact(N, dtype):
     want[17], want[290] = count / N, -count / N
     assert torch.equal(got.dW.double().cpu(), want)
     assert not got.dH.any() and got.db[17].item() == 1.0 and got.db[290].item() == -1.0
+
+
+def test_the_workspace_does_not_grow_with_rows_times_classes():
+    """Of the rows x classes matrix 2 GB are held at most, whatever its size, and beside each logit of such a block a sixteenth of a byte to half a byte of statistics, sums and starts (16 bytes of
+    statistics and 2 of starts for 128, or 64 with long rows; 4 bytes of sums of biases for 32 rows), of starts 256 MB at least; the rest goes with the rows, the classes, or their columns."""
+    import ctypes as C
+    from paper_2110_02987_b200 import head
+    from test_class_loss import _args
+    L = head._load()
+    n = C.c_size_t(0)
+    for dtype in (0, 1, 2):
+        for rows, classes, cols, k, grads in ((16384, 1 << 24, 64, 8, False), (1 << 20, 131072, 64, 8, False), (1 << 20, 131072, 64, 8, True), (1 << 17, 1 << 22, 64, 1, True), (1 << 16, 1 << 20, 4096, 64, True),
+                                              (1 << 26, 1 << 17, 8, 4, True)):
+            out = 256 if grads else None
+            a = _args(dtype=dtype, rows=rows, classes=classes, cols=cols, ldh=cols, ldw=cols, lddh=cols, lddw=cols, k=k, target_classes=256, teacher=256, hard_weight=0.5, temperature=2.0,
+                      bias=256, dH=out, dW=out, db=out)
+            assert L.gad_class_loss_workspace_bytes(C.byref(a), C.byref(n)) == 0
+            parts = 6 if dtype == 0 else 2
+            by_rows = rows * (parts * cols + 8 * (k + 1) + 16 + 8 + 1 + 16)
+            by_classes = classes * ((parts * cols if dtype == 0 else 0) + (4 * cols + 4 if grads else 0))
+            block = max(2 << 30, 256 * 16 * (classes + 256))
+            assert n.value <= by_rows + by_classes + 1.5 * block + (320 << 20), (dtype, rows, classes, n.value)
+
+
+@gpu
+def test_targets_over_blocks_of_rows():
+    s = make(60000, 40, 20011, "bfloat16", 7, k=5, ignored=0.1)
+    s.update(temperature=2.0, hard_weight=0.5)
+    compare_elements(pkg.distill_loss(**s), reference(**s), s, 2.0)
+
+
+@gpu
+@pytest.mark.parametrize("k,a", [(1, 0.5), (40, 0.0)])
+def test_targets_of_many_rows_against_very_many_classes(k, a):
+    """So many that where a row's targets start is looked up for a block of rows at a time; every row has all its classes in the last tile, the first, or anywhere."""
+    import torch
+    N, D, V = 2100, 8, (1 << 24) - 300
+    g = torch.Generator(device="cuda").manual_seed(8)
+    H = torch.randn(N, D, generator=g, device="cuda").bfloat16()
+    W = (0.25 * torch.randn(V, D, generator=g, device="cuda")).bfloat16()
+    cls = torch.randint(0, V, (N, k), generator=g, device="cuda")
+    cls[::3] = V - 1 - torch.arange(k, device="cuda")
+    cls[1::3] = torch.arange(k, device="cuda")
+    labels = torch.randint(0, V, (N,), generator=g, device="cuda") if a else None
+    teacher = torch.randn(N, k, generator=g, device="cuda")
+    got = pkg.distill_loss(H, W, cls, teacher, temperature=2.0, labels=labels, hard_weight=a, grads=False).check()
+    assert N * V // 64 > 1 << 28
+    h, w = H.double(), W.double()
+    lse, lse2 = [], []
+    for i in range(0, N, 100):
+        z = h[i:i + 100] @ w.t()
+        lse.append(torch.logsumexp(z, 1))
+        lse2.append(torch.logsumexp(z.mul_(0.5), 1))
+        del z
+    lse, lse2 = torch.cat(lse), torch.cat(lse2)
+    q = torch.softmax(teacher.double() / 2, 1)
+    zt = torch.einsum("nkd,nd->nk", w[cls], h)
+    want = (1 - a) * 4 * (q * (q.log() - zt / 2 + lse2[:, None])).sum(1)
+    if a:
+        want += a * (lse - (w[labels] * h).sum(1))
+    size = (h.abs() @ w.abs().amax(0)[:, None]).max().item()
+    one = 4 * (2 * (dot_steps(D, H.dtype) * 2 * U * size + 4 * U * 1.45 * size) + 2.0 ** -20) + 16 * U * want.abs()
+    assert ((got.row_loss.double() - want).abs() <= one).all()
