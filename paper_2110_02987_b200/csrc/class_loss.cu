@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
         if (idx[j] != INT_MAX) {
             const float lq = tau[j] - most - logs, q = expf(lq);
             ent += q > 0.f ? q * lq : q;                  // (a q that is not a number stays one)
-            tau[j] = hb * tt * q;
+            tau[j] = hb > 0.f ? hb * tt * q : 0.f;        // (without weight nothing counts, nor a q that is no number)
             if (tau[j] == 0.f) idx[j] = INT_MAX;          // (its class may be masked: 0 times -infinity)
         }
     if (t == 0 && a.ntargets > a.k) {
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kRowThreads) class_rows_kernel(const RowArgs a
         }
     }
     const float weight = counts ? (a.weights ? a.weights[r] : 1.f) : 0.f;
-    if (t == 0) a.rowk[r] = make_float4(ha, hb * tt * tt, counts && bad ? NAN : hb * tt * tt * ent, weight);
+    if (t == 0) a.rowk[r] = make_float4(ha, hb * tt * tt, counts && bad ? NAN : hb > 0.f ? hb * tt * tt * ent : 0.f, weight);
     pack_row<T>(reinterpret_cast<const T*>(a.H) + r * a.ldh, a.cols, counts, a.Hp, r * a.ldp, a.part_stride, t, kRowThreads);
     if (t == 0) {
         a.shares[r] = {counts, counts ? fabsf(weight) * (ha + hb * tt) : 0.f};

@@ -267,3 +267,17 @@ def test_targets_of_many_rows_against_very_many_classes(k, a):
     size = (h.abs() @ w.abs().amax(0)[:, None]).max().item()
     one = 4 * (2 * (dot_steps(D, H.dtype) * 2 * U * size + 4 * U * 1.45 * size) + 2.0 ** -20) + 16 * U * want.abs()
     assert ((got.row_loss.double() - want).abs() <= one).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("N", [3, 12, 300])
+def test_a_teacher_without_weight_adds_nothing_whatever_it_holds(N, dtype):
+    """hard_weight 1: the cross entropy against the labels alone, also where the teacher's logits have no softmax."""
+    import torch
+    s = make(N, 64, 500, dtype, 9, k=4, bias=True)
+    s["classes"].clamp_(min=0)
+    s["teacher"][0], s["teacher"][1], s["teacher"][2, 1] = -math.inf, math.nan, math.inf
+    want = pkg.class_loss(s["H"], s["W"], s["labels"], bias=s["bias"]).check()
+    got = pkg.distill_loss(**s, temperature=3.0, hard_weight=1.0).check()
+    assert all(torch.equal(u, v) for u, v in zip(got, want))
