@@ -349,6 +349,7 @@ const char* gad_last_error(const gad_ctx* ctx);
 void gad_destroy(gad_ctx* ctx);
 
 /* ---- operators of an output head: they need no context, and work on device memory of the caller --------------------------------
+ * The current device is the one that they run on; a process's devices are taken to be alike.
  * Element types of their matrices (sums and statistics are fp32 whatever the type): */
 #define GAD_F32 0
 #define GAD_F16 1
@@ -357,7 +358,7 @@ void gad_destroy(gad_ctx* ctx);
 /* Layer norm over the columns of x [rows x cols] (row stride ldx elements, at least cols; 0 = every row is the first):
  *   mean_i, rstd_i = 1 / sqrt(mean((x_i - mean_i)^2) + eps),  y = (x - mean) rstd gamma + beta.
  * gamma, beta [cols] in param_dtype (that of x, or GAD_F32); NULL means 1 and 0.  mean, rstd [rows] are what the backward pass needs.
- * Outputs must not overlap inputs.  Enqueued on `stream`; nothing waits. */
+ * Outputs must not overlap inputs.  Enqueued on `stream`; nothing waits.  Refused: 2^31 rows and more, more than 2^29 columns. */
 int gad_layer_norm(const void* x, int64_t ldx, int64_t rows, int32_t cols, int32_t dtype, const void* gamma,
                    const void* beta, int32_t param_dtype, float eps, void* y, int64_t ldy, float* mean, float* rstd,
                    void* stream);
@@ -372,7 +373,7 @@ int gad_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t
                             void* dx, int64_t lddx, void* dgamma, void* dbeta, void* workspace, size_t workspace_bytes,
                             void* stream);
 
-/* Loss of an output layer z = H W^T + b over many classes, and its gradients, without keeping z (rows x classes): softmax cross
+/* Loss of an output layer z = H W^T + b over many classes, and its gradients, without the rows x classes logits as a result: softmax cross
  * entropy against labels (k = 0), or distillation from the k largest logits of a teacher (k > 0).  With q_i = softmax(teacher_i / T)
  * over the slots of row i that are used:
  *   k = 0:  l_i = log sum_v exp(z_iv) - z_{i, label}
@@ -381,12 +382,16 @@ int gad_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t
  *   loss = scale * sum_i w_i l_i, divided by the number of rows that count with `mean`.
  * A row counts if it has a label (>= 0) and a > 0, or a used slot (target_classes >= 0) and a < 1.  Rows that do not count get loss and dH of zero
  * whatever H, teacher and weight hold there, and add nothing to dW and db.  If no row counts the loss and all gradients are zero.  A class named twice
- * in a row's slots has the sum of both.  A label or slot of `classes` or more makes that row's loss, and the whole, NaN.
- * A bias of -inf takes a class out (its W row must be finite).
+ * in a row's slots has the sum of both in the gradient; sum q log q is taken slot by slot (a constant of the student), so that such a row's
+ * loss lies below the divergence from that sum, and can be below zero.  A row with weight (a < 1) whose used slots are all -infinity has no q: NaN.
+ * A label or slot of `classes` or more makes that row's loss, and the whole, NaN (the gradients are then finite, without that target).
+ * A bias of -inf takes a class out (its W row must be finite).  Refused (GAD_ERR_RANGE): more than 2^30 rows, 2^20 columns, 2^24 classes, 1024 slots.
  * Gradients are those of `loss`, in dtype; any of dH, dW, db may be NULL (db needs a bias).  Sums, statistics and losses are fp32.
  * fp32 matrices are multiplied to fp32 accuracy (24-bit operands in three parts); with fp16 and bfloat16 the softmax's gradient is
  * rounded to that type, probabilities below 2^-32 of the largest among 128 neighbouring classes count as zero in it, and row weights
- * should lie within 2^20 of the largest one in fp16.  Outputs must not overlap inputs.  Equal calls give equal bits. */
+ * should lie within 2^20 of the largest one in fp16.  The tensor core does not round its sums but cuts them, at most 2^-23 of a sum every 16 terms: logits are
+ * short by up to 1.5e-5 of the sum of their terms' magnitudes (measured over 2048 dense terms 1.8e-6 of the logit; in fp32 a quarter of that), 16-bit gradients by an eighth
+ * of their rounding at most.  Outputs must not overlap inputs.  Equal calls give equal bits. */
 typedef struct {
     int32_t dtype;                 /* of H, W, bias, dH, dW, db: GAD_F32, GAD_F16, GAD_BF16                 */
     int32_t cols, classes;         /* D and V                                                               */
@@ -418,7 +423,7 @@ typedef struct {
  *   - for gradients, logits and gradients of logits of a block of rows: 2 bytes a logit in fp16 and bfloat16 (6 with up to 16 rows, or with two softmaxes of
  *     temperatures outside 1/2 .. 2 in fp16, 1/8 .. 8 in bfloat16), 10 in fp32.  A block takes about 2 GB at most, or 256 rows where those take more: all rows
  *     in one block where that holds them, else dW's sums in fp32 beside it;
- *   - statistics, about 0.15 bytes a logit of a block (without gradients a block has about 2^31 logits at most);
+ *   - statistics and sums, 0.1 to 0.4 bytes a logit of a block (without gradients a block has about 2^31 logits at most);
  *   - 8 (k + 1) + 41 bytes a row, and where its targets start: rows x classes / 64 bytes (/ 32 with long rows) up to 256 MB, or that of a block.
  * Depends on sizes, types, strides, which pointers are NULL, and W's alignment.  Host-only. */
 int gad_class_loss_workspace_bytes(const gad_class_loss_args* args, size_t* bytes);

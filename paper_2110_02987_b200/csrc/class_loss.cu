@@ -1,4 +1,4 @@
-// Loss of an output layer with many classes, without keeping its logits, and the gradients: softmax cross entropy against labels, and distillation
+// Loss of an output layer with many classes, holding no more than a block of its logits, and the gradients: softmax cross entropy against labels, and distillation
 // from a teacher's top logits.  With z_i = W h_i + b over all classes, p = softmax(z), p^T = softmax(z / T), q_i = softmax of row i's teacher logits / T:
 //   l_i = a (lse(z) - z_y) + (1 - a) T^2 sum_j q_j (log q_j - log p^T_{c_j})
 // Both kinds of target are one sparse list of (class, weight): tau = a [y] + (1 - a) T q at the teacher's classes.  Then
@@ -8,12 +8,13 @@
 // half the largest value, the sums and sum tau z (kStats); class_finish_kernel joins them.  For gradients the rows are gone through in blocks: of a
 // block the tiles leave z too, as 16-bit codes (fp32: as it is), class_grad_kernel turns it into G where it lies, and dH = G W and dW += G^T H follow
 // (kOut).  So what is held of the rows x classes matrix is bounded (kBlockBytes), whatever its size.  Taking z again from H and W instead, once its row sums are
-// known, needs no codes but a third more flops (8192 x 2048 bf16 against 100 003 classes: 10.7 ms, from codes 9.9 ms at that time, 8.5 now).  Going from z to G in strips of
+// known, needs no codes but a third more flops (8192 x 2048 bf16 against 100 003 classes: 10.7 ms, from codes 9.9 ms at that time, 8.7 now).  Going from z to G in strips of
 // 512 to 1024 rows, while the codes are in the L2, cost more tiles than it saved bytes (4096 x 1024 against 32 768: 896 us instead of 851).
 //
 // Operands: fp16 and bfloat16 as they are.  fp32 in three bfloat16 parts (24 bits), of whose nine products the six that reach 2^-24 are summed.
 // G is rounded to the operand type (fp32: not rounded), times a power of two that brings its largest possible value to 2^14 .. 2^15: in fp16 a probability of 1e-9 keeps
-// eight bits.  One rounding of each term of a sum whose result is rounded to the same type: the result's error grows by about the square root of 2.
+// eight bits.  One rounding of each term of a sum whose result is rounded to the same type: in the norm of a tensor the result's error grows by up to the square root of 2 (measured 1.0 to
+// 1.5); a row of dH that is mostly its target's shares that one rounding, and is off by up to 2.4 times its own.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>

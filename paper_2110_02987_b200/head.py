@@ -4,8 +4,8 @@ of an output layer with many classes, and distillation from a teacher's top logi
 Like the rest of the binding this is argument checking and marshalling; the work is the library's kernels (``include/gad.h``).
 Every call enqueues on ``stream`` (default: torch's current stream of the tensors' device) and does not wait.  Outputs and
 workspaces are allocated per call from torch's allocator on that stream, so calls on different streams, and captured graphs, share nothing.  As everywhere
-in torch, tensors made on another stream must be ready when the call's stream gets there.  The calls record nothing for autograd: gradients
-are what they return.
+in torch, tensors made on another stream must be ready when the call's stream gets there.  The calls record nothing for autograd, whether their inputs require
+gradients or not: gradients are what they return, to be handed on (``h.backward(r.dH)`` for an ``h`` that autograd knows).
 """
 from __future__ import annotations
 
@@ -108,7 +108,7 @@ def layer_norm(x, gamma=None, beta=None, *, eps=1e-5, stream=None):
     """gad_layer_norm: ``(y, mean, rstd)`` of the rows of ``x`` [rows x cols]: y = (x - mean) * rstd * gamma + beta.
 
     x float32, float16 or bfloat16 with any row stride; gamma and beta [cols] in x's type or float32 (both in the same), or None.
-    y has x's type and is contiguous; mean and rstd are float32 [rows] (``layer_norm_backward`` takes them)."""
+    y has x's type and is contiguous; mean and rstd are float32 [rows] (``layer_norm_backward`` takes them).  Autograd does not see the call."""
     L = _load()
     ldx = _matrix(x, "x")
     rows, cols = x.shape
@@ -247,12 +247,13 @@ def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, 
 
 
 def class_loss(H, W, labels, *, bias=None, row_weights=None, mean=True, scale=1.0, grads=True, stream=None):
-    """gad_class_loss with labels: softmax cross entropy of the output layer z = H W^T + bias over many classes, without keeping z.
+    """gad_class_loss with labels: softmax cross entropy of the output layer z = H W^T + bias over many classes.  Of z a block of about 2 GB at
+    most is held at a time for gradients (2 bytes a logit in the 16-bit types, 10 in float32), and none without.
 
     H [rows x cols] and W [classes x cols] float32, float16 or bfloat16 (both the same), any row stride; labels int32 / int64 [rows], below
     zero: the row does not count; bias [classes] in the same type, -inf takes a class out.
     loss = scale * sum_i row_weights_i row_loss_i, with ``mean`` divided by the number of rows that count.
-    grads: True, False, or some of "H", "W", "b" as a string or set.  Returns a ``ClassLoss``."""
+    grads: True, False, or some of "H", "W", "b" as a string or set.  Returns a ``ClassLoss``; autograd does not see the call."""
     if labels is None:
         raise GadError(-1, "labels are needed")
     return _class_loss(H, W, labels, None, None, 1.0, 1.0, bias, row_weights, mean, scale, grads, stream)
