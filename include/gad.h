@@ -429,6 +429,63 @@ typedef struct {
 int gad_class_loss_workspace_bytes(const gad_class_loss_args* args, size_t* bytes);
 int gad_class_loss(const gad_class_loss_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Gated feed-forward block:  g = x Wg^T,  u = x Wu^T,  h = act(g) u,  y = h Wd^T   for x [rows x cols], Wg and Wu [inner x cols], Wd [cols x inner].
+ * For a backward pass act, slope and h [rows x inner] (all three, or none) receive act(g), u act'(g) and h, rounded to dtype.  The activations: g / (1 + exp(-g)); g times the
+ * normal distribution's cumulated density (gelu, by erf); max(g, 0), whose slope at 0 is 0; 1 / (1 + exp(-g)).
+ * Sums are fp32.  fp32 matrices are multiplied to fp32 accuracy (24-bit operands in three parts); in fp16 and bfloat16 h is rounded to that type before the second product, so in fp16
+ * an h above 65 504 is infinite.  The tensor core does not round its sums but cuts them, at most 2^-23 of a sum every 16 terms; longer ones than cost an eighth of the result's
+ * rounding are added up in chunks (fp32: of 256 terms).  Outputs must not overlap inputs or one another.  Equal calls give equal bits.  Refused (GAD_ERR_RANGE): more than 2^30 rows, 2^20 columns,
+ * 2^20 inner columns. */
+#define GAD_SILU 0
+#define GAD_GELU 1
+#define GAD_RELU 2
+#define GAD_SIGMOID 3
+typedef struct {
+    int32_t dtype;                  /* of all matrices: GAD_F32, GAD_F16, GAD_BF16                            */
+    int32_t cols, inner;            /* D and F                                                               */
+    int32_t activation;
+    int64_t rows;                   /* N                                                                     */
+    const void* x; int64_t ldx;     /* [rows x cols], row stride in elements (0: every row is the first)      */
+    const void* w_gate; int64_t ldwg;   /* [inner x cols]                                                    */
+    const void* w_up; int64_t ldwu;     /* [inner x cols]                                                    */
+    const void* w_down; int64_t ldwd;   /* [cols x inner]                                                    */
+    void* y; int64_t ldy;           /* [rows x cols]                                                         */
+    void* act; int64_t ldact;       /* [rows x inner] or NULL                                                */
+    void* slope; int64_t ldslope;
+    void* h; int64_t ldh;           /* in fp16 and bfloat16: rows start on 16 bytes                          */
+    int32_t* status;                /* device [1]: 0, or the code of a bounded wait that ran out (the other outputs are then undefined) */
+} gad_gated_args;
+
+/* Device workspace (256-byte aligned): h in operand form where it is not kept (2 bytes a value, 6 in fp32), copies of matrices that are fp32 or whose rows do not start on
+ * 16 bytes (2 bytes a value, 6 in fp32), 19 MB for sums of tiles that are cut along their reduction.  Host-only. */
+int gad_gated_feed_forward_workspace_bytes(const gad_gated_args* args, size_t* bytes);
+int gad_gated_feed_forward(const gad_gated_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its backward pass, from the upstream gradient dy [rows x cols] of y and what the forward pass has left:
+ *   dh = dy Wd,  dg = dh slope,  du = dh act,   dx = dg Wg + du Wu,  dw_gate = dg^T x,  dw_up = du^T x,  dw_down = dy^T h.
+ * Any of the gradients may be NULL.  In fp16 and bfloat16 dg and du are rounded to that type.  act, slope and h may have any row stride. */
+typedef struct {
+    int32_t dtype, cols, inner;
+    int64_t rows;
+    const void* dy; int64_t lddy;   /* [rows x cols] (0: every row is the first)                             */
+    const void* x; int64_t ldx;
+    const void* w_gate; int64_t ldwg;
+    const void* w_up; int64_t ldwu;
+    const void* w_down; int64_t ldwd;
+    const void* act; int64_t ldact; /* [rows x inner]                                                        */
+    const void* slope; int64_t ldslope;
+    const void* h; int64_t ldh;
+    void* dx; int64_t lddx;
+    void* dw_gate; int64_t lddwg;
+    void* dw_up; int64_t lddwu;
+    void* dw_down; int64_t lddwd;
+    int32_t* status;
+} gad_gated_grad_args;
+
+/* Device workspace (256-byte aligned): dg and du (4 bytes a value of h, 12 in fp32), and copies and sums as above.  Host-only. */
+int gad_gated_feed_forward_backward_workspace_bytes(const gad_gated_grad_args* args, size_t* bytes);
+int gad_gated_feed_forward_backward(const gad_gated_grad_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Frees the pinned host memory that the library keeps and no context or call is using. */
 int gad_release_pinned(void);
 

@@ -1,0 +1,409 @@
+// Gated feed-forward block and its backward pass:
+//   g = x Wg^T,  u = x Wu^T,  h = act(g) u,  y = h Wd^T            x [N x D], Wg, Wu [F x D], Wd [D x F]
+//   dh = dy Wd,  dg = dh u act'(g),  du = dh act(g);   dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x,  dWd = dy^T h.
+//
+// Forward, two products: kGate leaves h (g and u never leave the chip), kPlain y.  For a backward pass kGate also leaves the two factors that dh is multiplied by there, act(g) and
+// u act'(g), instead of g and u: one rounding to the tensors' type each where g and u would bring theirs into every factor, and the backward pass has no activation to take again.
+// Backward: kHidden leaves dg and du, then three launches of kPlain: dx (one reduction over both), dWg and dWu, dWd.
+//
+// Operands as in class_loss.cu: fp16 and bfloat16 as they are, fp32 in three bfloat16 parts with six products.  h, dg and du are operands of a second product, so they are rounded to
+// fp16 or bfloat16 (fp32: 24 bits): in norm the results' error grows by the square root of two over their own rounding.
+#include <algorithm>
+#include <atomic>
+
+#include "gated_gemm.cuh"
+#include "operand_pack.cuh"
+
+namespace gad {
+
+namespace {
+
+constexpr int kPairs = 74;                               // pairs of CTAs that run at once
+
+// Matrices to be copied to operands, in one launch: a warp a row.
+struct PackJob { const void* src; long long ld; int rows, cols; void* dst; long long ldp, part_stride; };
+struct PackJobs { PackJob job[6]; long long first[7]; int n; };
+template <class T>
+__global__ void __launch_bounds__(256) gated_pack_kernel(const __grid_constant__ PackJobs a) {
+    const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    pdl_next();
+    pdl_wait();
+    if (r >= a.first[a.n]) return;
+    int j = 0;
+    while (r >= a.first[j + 1]) ++j;
+    const PackJob& k = a.job[j];
+    const long long row = r - a.first[j];
+    pack_row<T>(reinterpret_cast<const T*>(k.src) + row * k.ld, k.cols, true, k.dst, row * k.ldp, k.part_stride, threadIdx.x & 31, 32);
+}
+
+// The shares of the tiles that were cut along their reduction, added up in order: four columns a thread.
+template <class T>
+__global__ void __launch_bounds__(256) gated_join_kernel(const __grid_constant__ GatedArgs ga) {
+    const TileArgs& a = ga.t;
+    const int per_row = a.width / 4, rows = 256 / per_row, per_tile = CT_M / rows;
+    const int i = blockIdx.x / per_tile, r = blockIdx.x % per_tile * rows + threadIdx.x / per_row, x = threadIdx.x % per_row * 4;
+    pdl_next();
+    pdl_wait();
+    const TileAt t = tile_at(a, a.whole + (long long)i * a.shares);
+    const int plane = t.m / ga.plane_tiles, row = (t.m - plane * ga.plane_tiles) * CT_M + r, c = t.n * a.width + x;
+    if (row >= a.M || c >= a.N) return;
+    const float* slot = a.slots + ((long long)i * a.shares * CT_M + r) * a.width + x;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < a.shares; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(slot + (long long)k * CT_M * a.width);
+        s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+    }
+    T* out = reinterpret_cast<T*>(ga.C[plane]) + (long long)row * ga.ldc[plane] + c;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (c + j < a.N) out[j] = from_float<T>(s[j]);
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) gated_zero_kernel(T* __restrict__ p, int64_t ld, int64_t rows, int cols) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) p[i / cols * ld + i % cols] = from_float<T>(0.f);
+}
+__global__ void gated_empty_kernel(int32_t* status) { *status = 0; }
+
+// ---------------------------------------------------------------------------------------------
+// How a call is cut up; the same for the workspace and the launches.
+// ---------------------------------------------------------------------------------------------
+
+// An operand matrix [rows x cols] as a descriptor reaches it: where it lies, or a copy in the workspace.
+struct Operand {
+    const void* src; int64_t ld; int64_t rows; int cols;
+    bool pack; int64_t at, ldp;        // of the copy
+};
+
+struct Room {
+    int64_t at = 0;
+    int64_t take(int64_t bytes) { const int64_t o = at; at += round_up(bytes, 256); return o; }
+};
+
+Operand operand(const void* p, int64_t ld, int64_t rows, int cols, int dtype, Room& room) {
+    Operand o{p, ld, rows, cols, false, 0, round_up(cols, 8)};
+    if (rows == 1 && dtype != GAD_F32) o.ld = o.ldp;                                      // (one row has no stride)
+    o.pack = dtype == GAD_F32 || ((uintptr_t)p & 15) != 0 || o.ld == 0 || (o.ld * 2) % 16 != 0;
+    if (o.pack) o.at = room.take((dtype == GAD_F32 ? 6 : 2) * rows * o.ldp);
+    return o;
+}
+
+// The kernels of a call: the first waits for all that is in front of it on the stream, the others for the one in front; the first product clears the status.
+struct Sequence {
+    cudaStream_t s;
+    bool first = true, clear = true;
+    template <class... P, class... Args>
+    cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, Args&&... args) {
+        const bool f = first;
+        first = false;
+        return chain(kernel, grid, block, smem, s, f, std::forward<Args>(args)...);
+    }
+};
+
+int width_for(int n) { return n <= 128 ? 128 : 256; }
+
+// Blocks of 64 terms that the tensor core adds up before the sum moves to registers: it cuts its accumulator off at every addition, 2^-23 of the sum every 16 terms at most (see
+// class_gemm_kernel).  As for the head's gradients: fp32 results 256 terms, 16-bit ones as many as cost an eighth of their rounding at most.
+template <class T> constexpr int kGatedChunk = 4;
+template <> constexpr int kGatedChunk<__half> = 128;
+template <> constexpr int kGatedChunk<__nv_bfloat16> = 1024;
+
+template <int USE, bool A_MN, bool B_MN, class T, bool ADD_UP>
+cudaError_t launch_gated(const CUtensorMap& A, const CUtensorMap& B0, const CUtensorMap& B1, const GatedArgs& g, Sequence& q) {
+    const auto kernel = gated_gemm_kernel<USE, A_MN, B_MN, T, ADD_UP>;
+    cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), CT_SMEM, false);
+    if (e != cudaSuccess) return e;
+    static std::atomic<int> known{0};
+    if (known.load() <= 0) known.store(max_active_pairs(reinterpret_cast<const void*>(kernel), CT_THREADS, CT_SMEM, 2 * kPairs));
+    const int64_t units = g.t.whole + ((int64_t)g.t.tiles_m * g.t.tiles_n - g.t.whole) * g.t.shares;
+    const int ncl = (int)std::min<int64_t>(units, known.load());
+    return q.launch(kernel, dim3((unsigned)(2 * ncl)), CT_THREADS, CT_SMEM, A, B0, B1, g);
+}
+
+// One product.  Where results go as they are (kPlain), tiles that are left over when all pairs have had the same number are cut along their reduction, down to 8 ring stages a share.
+template <int USE, bool A_MN, bool B_MN, class T>
+cudaError_t go(const CUtensorMap& A, const CUtensorMap& B0, const CUtensorMap& B1, GatedArgs g, Sequence& q) {
+    TileArgs& a = g.t;
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, rest = tiles % kPairs;
+    a.whole = (int)tiles; a.shares = 1; a.kb_share = a.nkb; a.chunk = kGatedChunk<T>;
+    if (USE == kPlain && rest) {
+        const int want = (int)std::min<int64_t>(kPairs / rest, (int64_t)a.nkb * a.pairs * g.segs / 8);
+        if (want > 1) {
+            a.kb_share = (a.nkb + want - 1) / want;
+            a.shares = (a.nkb + a.kb_share - 1) / a.kb_share;
+            a.whole = (int)(tiles - rest);
+        }
+    }
+    g.clear = q.clear;
+    const bool add_up = sizeof(T) == 4 || (int64_t)(a.whole > 0 ? a.nkb : a.kb_share) * g.segs > a.chunk;
+    const cudaError_t e = add_up ? launch_gated<USE, A_MN, B_MN, T, true>(A, B0, B1, g, q) : launch_gated<USE, A_MN, B_MN, T, sizeof(T) == 4>(A, B0, B1, g, q);
+    q.clear = false;
+    if (e != cudaSuccess || a.shares == 1) return e;
+    return q.launch(gated_join_kernel<T>, dim3((unsigned)(rest * (CT_M * a.width / 1024))), 256, 0, g);
+}
+
+template <class T>
+cudaError_t pack(std::initializer_list<const Operand*> all, uint8_t* ws, Sequence& q) {
+    PackJobs p{};
+    for (const Operand* o : all)
+        if (o->pack && o->src && o->rows > 0) {
+            p.job[p.n] = {o->src, o->ld, (int)o->rows, o->cols, ws + o->at, o->ldp, o->rows * o->ldp};
+            p.first[p.n + 1] = p.first[p.n] + o->rows;
+            ++p.n;
+        }
+    if (!p.n) return cudaSuccess;
+    return q.launch(gated_pack_kernel<T>, dim3((unsigned)((p.first[p.n] + 7) / 8)), 256, 0, p);
+}
+
+#define GAD_TRY(x) do { const cudaError_t e_ = (x); if (e_ != cudaSuccess) return e_; } while (0)
+
+// Descriptor of an operand; `box` rows at a time (64 where the reduction runs over its rows).
+cudaError_t map_of(CUtensorMap& m, const Operand& o, uint8_t* ws, int parts, uint32_t box) {
+    const void* base = o.pack ? ws + o.at : o.src;
+    const int64_t ld = o.pack ? o.ldp : o.ld;
+    return tc_make_map(&m, base, (uint64_t)o.cols, (uint64_t)o.rows, (uint64_t)parts, (uint64_t)ld * 2, (uint64_t)(ld * 2 * o.rows), box, false, true) ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+GatedArgs product(int64_t M, int N, int64_t K, int width, int dtype, int planes, int segs, int group, int32_t* status) {
+    GatedArgs g{};
+    g.parts = dtype == GAD_F32 ? 3 : 1;
+    g.segs = segs;
+    g.t.M = (int)M; g.t.N = N;
+    g.plane_tiles = (int)((M + CT_M - 1) / CT_M);
+    g.t.tiles_m = planes * g.plane_tiles;
+    g.t.width = width;
+    g.t.nkb = (int)((K + CT_K - 1) / CT_K);
+    g.t.group = group;
+    g.t.pairs = dtype == GAD_F32 ? 6 : 1;
+    g.t.bf16 = dtype != GAD_F16;
+    g.t.err = status;
+    g.t.tiles_n = (N + width - 1) / width;
+    return g;
+}
+
+struct ForwardPlan {
+    Operand x, wg, wu, wd, h;
+    int64_t o_slots, total;
+};
+ForwardPlan plan_forward(const gad_gated_args& a) {
+    ForwardPlan p{};
+    Room room;
+    p.x = operand(a.x, a.ldx, a.rows, a.cols, a.dtype, room);
+    p.wg = operand(a.w_gate, a.ldwg, a.inner, a.cols, a.dtype, room);
+    p.wu = operand(a.w_up, a.ldwu, a.inner, a.cols, a.dtype, room);
+    p.wd = operand(a.w_down, a.ldwd, a.cols, a.inner, a.dtype, room);
+    // h: kept where the caller wants it and a descriptor reaches it, else in the workspace
+    const bool kept = a.h && a.dtype != GAD_F32;
+    p.h = {kept ? a.h : nullptr, a.rows == 1 ? round_up(a.inner, 8) : a.ldh, a.rows, a.inner, !kept, 0, round_up(a.inner, 8)};
+    if (!kept) p.h.at = room.take((a.dtype == GAD_F32 ? 6 : 2) * a.rows * p.h.ldp);
+    p.o_slots = room.take((int64_t)kPairs * CT_M * width_for(a.cols) * 4);
+    p.total = room.at;
+    return p;
+}
+
+template <class T>
+cudaError_t run_forward(const gad_gated_args& a, uint8_t* ws, cudaStream_t s) {
+    const ForwardPlan p = plan_forward(a);
+    const int parts = a.dtype == GAD_F32 ? 3 : 1;
+    Sequence q{s};
+    GAD_TRY(pack<T>({&p.x, &p.wg, &p.wu, &p.wd}, ws, q));
+    CUtensorMap A, B0, B1;
+    GatedArgs g = product(a.rows, a.inner, a.cols, 256, a.dtype, 1, 1, 16, a.status);
+    g.t.tiles_n = (a.inner + CT_H - 1) / CT_H;
+    g.activation = a.activation;
+    g.h = p.h.pack ? ws + p.h.at : const_cast<void*>(p.h.src);
+    g.ldh = p.h.pack ? p.h.ldp : p.h.ld;
+    g.h_part = a.rows * g.ldh;
+    g.act = a.act; g.ldact = a.ldact; g.slope = a.slope; g.ldslope = a.ldslope;
+    g.C[0] = a.dtype == GAD_F32 ? a.h : nullptr; g.ldc[0] = a.ldh;
+    GAD_TRY(map_of(A, p.x, ws, parts, CT_H));
+    GAD_TRY(map_of(B0, p.wg, ws, parts, CT_H));
+    GAD_TRY(map_of(B1, p.wu, ws, parts, CT_H));
+    GAD_TRY((go<kGate, false, false, T>(A, B0, B1, g, q)));
+    const int width = width_for(a.cols);
+    g = product(a.rows, a.cols, a.inner, width, a.dtype, 1, 1, 8, a.status);
+    g.C[0] = a.y; g.ldc[0] = a.ldy;
+    g.t.slots = reinterpret_cast<float*>(ws + p.o_slots);
+    GAD_TRY(map_of(A, p.h, ws, parts, CT_H));
+    GAD_TRY(map_of(B0, p.wd, ws, parts, (uint32_t)width / 2));
+    GAD_TRY((go<kPlain, false, false, T>(A, B0, B0, g, q)));
+    return cudaGetLastError();
+}
+
+struct BackwardPlan {
+    Operand dy, x, wg, wu, wd, h;
+    int64_t o_dg, ldg, o_slots, total;
+};
+BackwardPlan plan_backward(const gad_gated_grad_args& a) {
+    BackwardPlan p{};
+    Room room;
+    const bool hidden = a.dx || a.dw_gate || a.dw_up;
+    const auto maybe = [&](bool wanted, const void* ptr, int64_t ld, int64_t rows, int cols) { return wanted ? operand(ptr, ld, rows, cols, a.dtype, room) : Operand{}; };
+    p.dy = maybe(hidden || a.dw_down, a.dy, a.lddy, a.rows, a.cols);
+    p.wd = maybe(hidden, a.w_down, a.ldwd, a.cols, a.inner);
+    p.wg = maybe(a.dx, a.w_gate, a.ldwg, a.inner, a.cols);
+    p.wu = maybe(a.dx, a.w_up, a.ldwu, a.inner, a.cols);
+    p.x = maybe(a.dw_gate || a.dw_up, a.x, a.ldx, a.rows, a.cols);
+    p.h = maybe(a.dw_down, a.h, a.ldh, a.rows, a.inner);
+    p.ldg = round_up(a.inner, 8);
+    if (hidden) p.o_dg = room.take((a.dtype == GAD_F32 ? 12 : 4) * a.rows * p.ldg);
+    p.o_slots = room.take((int64_t)kPairs * CT_M * std::max(width_for(a.cols), width_for(a.inner)) * 4);
+    p.total = room.at;
+    return p;
+}
+
+template <class T>
+cudaError_t run_backward(const gad_gated_grad_args& a, uint8_t* ws, cudaStream_t s) {
+    const BackwardPlan p = plan_backward(a);
+    const int parts = a.dtype == GAD_F32 ? 3 : 1;
+    const int64_t N = a.rows;
+    const int D = a.cols, F = a.inner;
+    Sequence q{s};
+    GAD_TRY(pack<T>({&p.dy, &p.wd, &p.wg, &p.wu, &p.x, &p.h}, ws, q));
+    CUtensorMap A, B0, B1;
+    float* slots = reinterpret_cast<float*>(ws + p.o_slots);
+    uint8_t* dg = ws + p.o_dg;
+    const int64_t part = N * p.ldg;                       // values of a part of dg; du lies behind all of dg's
+    const int width_d = width_for(D), width_f = width_for(F);
+    if (a.dx || a.dw_gate || a.dw_up) {
+        GatedArgs g = product(N, F, D, width_f, a.dtype, 1, 1, 16, a.status);
+        g.act = const_cast<void*>(a.act); g.ldact = a.ldact; g.slope = const_cast<void*>(a.slope); g.ldslope = a.ldslope;
+        g.C[0] = dg; g.ldh = p.ldg; g.h_part = part;
+        GAD_TRY(map_of(A, p.dy, ws, parts, CT_H));
+        GAD_TRY(map_of(B0, p.wd, ws, parts, CT_K));
+        GAD_TRY((go<kHidden, false, true, T>(A, B0, B0, g, q)));
+    }
+    const auto map_dg = [&](CUtensorMap& m, int plane, int planes, uint32_t box) {
+        return tc_make_map(&m, dg + plane * parts * part * 2, (uint64_t)F, (uint64_t)N, (uint64_t)(planes * parts), (uint64_t)p.ldg * 2, (uint64_t)part * 2, box, false, true) ? cudaSuccess : cudaErrorInvalidValue;
+    };
+    if (a.dx) {
+        GatedArgs g = product(N, D, F, width_d, a.dtype, 1, 2, 8, a.status);
+        g.C[0] = a.dx; g.ldc[0] = a.lddx; g.t.slots = slots;
+        GAD_TRY(map_dg(A, 0, 2, CT_H));
+        GAD_TRY(map_of(B0, p.wg, ws, parts, CT_K));
+        GAD_TRY(map_of(B1, p.wu, ws, parts, CT_K));
+        GAD_TRY((go<kPlain, false, true, T>(A, B0, B1, g, q)));
+    }
+    if (a.dw_gate || a.dw_up) {
+        const int planes = a.dw_gate && a.dw_up ? 2 : 1;
+        GatedArgs g = product(F, D, N, width_d, a.dtype, planes, 1, 8, a.status);
+        g.C[0] = a.dw_gate ? a.dw_gate : a.dw_up; g.ldc[0] = a.dw_gate ? a.lddwg : a.lddwu;
+        g.C[1] = a.dw_up; g.ldc[1] = a.lddwu;
+        g.t.slots = slots;
+        GAD_TRY(map_dg(A, a.dw_gate ? 0 : 1, planes, CT_K));
+        GAD_TRY(map_of(B0, p.x, ws, parts, CT_K));
+        GAD_TRY((go<kPlain, true, true, T>(A, B0, B0, g, q)));
+    }
+    if (a.dw_down) {
+        GatedArgs g = product(D, F, N, width_f, a.dtype, 1, 1, 8, a.status);
+        g.C[0] = a.dw_down; g.ldc[0] = a.lddwd; g.t.slots = slots;
+        GAD_TRY(map_of(A, p.dy, ws, parts, CT_K));
+        GAD_TRY(map_of(B0, p.h, ws, parts, CT_K));
+        GAD_TRY((go<kPlain, true, true, T>(A, B0, B0, g, q)));
+    }
+    return cudaGetLastError();
+}
+#undef GAD_TRY
+
+template <class T> int zero(void* p, int64_t ld, int64_t rows, int cols, cudaStream_t s) {
+    if (!p) return 0;
+    gated_zero_kernel<T><<<592, 256, 0, s>>>((T*)p, ld, rows, cols);
+    ++g_kernel_launches;
+    return 0;
+}
+int empty(int32_t* status, cudaStream_t s) {
+    gated_empty_kernel<<<1, 1, 0, s>>>(status);
+    ++g_kernel_launches;
+    return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
+}
+// No rows: gradients of the weights are zero.
+template <class T>
+int run_no_rows(const gad_gated_grad_args& a, cudaStream_t s) {
+    zero<T>(a.dw_gate, a.lddwg, a.inner, a.cols, s);
+    zero<T>(a.dw_up, a.lddwu, a.inner, a.cols, s);
+    zero<T>(a.dw_down, a.lddwd, a.cols, a.inner, s);
+    return empty(a.status, s);
+}
+
+bool sizes_ok(int dtype, int64_t rows, int cols, int inner) { return dtype >= GAD_F32 && dtype <= GAD_BF16 && rows >= 0 && cols >= 1 && inner >= 1; }
+bool in_range(int64_t rows, int cols, int inner) { return rows <= (1 << 30) && cols <= (1 << 20) && inner <= (1 << 20); }
+
+int check_forward(const gad_gated_args* a) {
+    if (!a || !sizes_ok(a->dtype, a->rows, a->cols, a->inner)) return GAD_ERR_ARG;
+    if (!in_range(a->rows, a->cols, a->inner)) return GAD_ERR_RANGE;
+    if (a->activation < GAD_SILU || a->activation > GAD_SIGMOID) return GAD_ERR_ARG;
+    if ((a->rows > 1 && a->ldx != 0 && a->ldx < a->cols) || a->ldwg < a->cols || a->ldwu < a->cols || a->ldwd < a->inner || (a->rows > 1 && a->ldy < a->cols)) return GAD_ERR_ARG;
+    const int kept = (a->act != nullptr) + (a->slope != nullptr) + (a->h != nullptr);
+    if (kept != 0 && kept != 3) return GAD_ERR_ARG;
+    if (kept && a->rows > 1 && (a->ldact < a->inner || a->ldslope < a->inner || a->ldh < a->inner)) return GAD_ERR_ARG;
+    // h is an operand of the second product where it lies
+    if (kept && a->dtype != GAD_F32 && (((uintptr_t)a->h & 15) != 0 || (a->rows > 1 && a->ldh % 8 != 0))) return GAD_ERR_ARG;
+    return GAD_OK;
+}
+int check_backward(const gad_gated_grad_args* a) {
+    if (!a || !sizes_ok(a->dtype, a->rows, a->cols, a->inner)) return GAD_ERR_ARG;
+    if (!in_range(a->rows, a->cols, a->inner)) return GAD_ERR_RANGE;
+    if (a->rows > 1 && ((a->lddy != 0 && a->lddy < a->cols) || (a->ldx != 0 && a->ldx < a->cols) || (a->dx && a->lddx < a->cols) || a->ldact < a->inner || a->ldslope < a->inner || a->ldh < a->inner))
+        return GAD_ERR_ARG;
+    if (a->ldwg < a->cols || a->ldwu < a->cols || a->ldwd < a->inner || (a->dw_gate && a->lddwg < a->cols) || (a->dw_up && a->lddwu < a->cols) || (a->dw_down && a->lddwd < a->inner)) return GAD_ERR_ARG;
+    return GAD_OK;
+}
+
+}  // namespace
+}  // namespace gad
+
+extern "C" int gad_gated_feed_forward_workspace_bytes(const gad_gated_args* args, size_t* bytes) {
+    const int rc = gad::check_forward(args);
+    if (rc != GAD_OK) return rc;
+    if (!bytes) return GAD_ERR_ARG;
+    *bytes = args->rows == 0 ? 0 : (size_t)gad::plan_forward(*args).total;
+    return GAD_OK;
+}
+
+extern "C" int gad_gated_feed_forward(const gad_gated_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace gad;
+    const int rc = check_forward(args);
+    if (rc != GAD_OK) return rc;
+    const gad_gated_args& a = *args;
+    if (!a.status) return GAD_ERR_ARG;
+    const cudaStream_t s = (cudaStream_t)stream;
+    if (a.rows == 0) return empty(a.status, s);
+    if (!a.x || !a.w_gate || !a.w_up || !a.w_down || !a.y) return GAD_ERR_ARG;
+    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < (size_t)plan_forward(a).total) return GAD_ERR_OOM;
+    try {
+        uint8_t* ws = (uint8_t*)workspace;
+        const cudaError_t e = a.dtype == GAD_F32 ? run_forward<float>(a, ws, s) : a.dtype == GAD_F16 ? run_forward<__half>(a, ws, s) : run_forward<__nv_bfloat16>(a, ws, s);
+        return e == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
+    } catch (...) {   // (the table of configured kernels could not grow)
+        return GAD_ERR_OOM;
+    }
+}
+
+extern "C" int gad_gated_feed_forward_backward_workspace_bytes(const gad_gated_grad_args* args, size_t* bytes) {
+    const int rc = gad::check_backward(args);
+    if (rc != GAD_OK) return rc;
+    if (!bytes) return GAD_ERR_ARG;
+    *bytes = args->rows == 0 ? 0 : (size_t)gad::plan_backward(*args).total;
+    return GAD_OK;
+}
+
+extern "C" int gad_gated_feed_forward_backward(const gad_gated_grad_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace gad;
+    const int rc = check_backward(args);
+    if (rc != GAD_OK) return rc;
+    const gad_gated_grad_args& a = *args;
+    if (!a.status) return GAD_ERR_ARG;
+    const cudaStream_t s = (cudaStream_t)stream;
+    if (a.rows == 0) return a.dtype == GAD_F32 ? run_no_rows<float>(a, s) : a.dtype == GAD_F16 ? run_no_rows<__half>(a, s) : run_no_rows<__nv_bfloat16>(a, s);
+    if (!a.dy || !a.x || !a.w_gate || !a.w_up || !a.w_down || !a.act || !a.slope || !a.h) return GAD_ERR_ARG;
+    if (!a.dx && !a.dw_gate && !a.dw_up && !a.dw_down) return empty(a.status, s);
+    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < (size_t)plan_backward(a).total) return GAD_ERR_OOM;
+    try {
+        uint8_t* ws = (uint8_t*)workspace;
+        const cudaError_t e = a.dtype == GAD_F32 ? run_backward<float>(a, ws, s) : a.dtype == GAD_F16 ? run_backward<__half>(a, ws, s) : run_backward<__nv_bfloat16>(a, ws, s);
+        return e == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
+    } catch (...) {
+        return GAD_ERR_OOM;
+    }
+}

@@ -1,0 +1,341 @@
+// The matrix products of the gated feed-forward block on tcgen05, by pairs of CTAs, and what is done with a finished tile.  Used by gated.cu for
+//   kGate      g = x Wg^T and u = x Wu^T side by side: h = act(g) u, and for a backward pass act(g) and u act'(g)
+//   kHidden    dh = dy Wd: dg = dh u act'(g) and du = dh act(g)
+//   kPlain     y = h Wd^T;  dx = dg Wg + du Wu;  dWg = dg^T x, dWu = du^T x, dWd = dy^T h
+//
+// The ring, the roles and the tiles are those of the output head's product (class_gemm.cuh): tiles of 256 rows by two CTAs (cta_group::2), 64 values of the reduction a
+// stage, two accumulators of 256 columns, eight draining warps.  Of B each CTA of a pair holds half of the columns, so for kGate one CTA loads 128 rows of Wg and the
+// other 128 rows of Wu: the accumulator has g in its left half and u, of the same units, in its right one, and no copy of the weights is laid out for it.
+// The sum dg Wg + du Wu is one reduction over two segments with a B of its own each; dWg and dWu are one launch over two planes of A with an output each.
+#pragma once
+
+#include "class_gemm.cuh"
+
+namespace gad {
+
+namespace {
+
+enum GatedUse { kGate, kHidden, kPlain };
+enum Activation { kSilu, kGelu, kRelu, kSigmoid };
+
+struct GatedArgs {
+    TileArgs t;                // tiles and shares (M rows of a plane)
+    int parts, segs;           // operand parts; segments of the reduction (t.pairs products each)
+    int plane_tiles;           // row tiles of a plane
+    int activation;
+    int clear;                 // the call's first product: its first block sets the status to zero (blocks come up in order, and a wait takes 2^22 polls to run out)
+    void *C[2];                // kPlain: result of each plane; kGate with T = float: C[0] is h where it is kept, or null
+    long long ldc[2];
+    // kGate: h in the operand type, parts `h_part` values apart; act(g) and u act'(g), or null.  kHidden: those two read, dg and du written (C[0], parts and planes h_part apart)
+    void *h, *act, *slope;
+    long long ldh, h_part, ldact, ldslope;
+};
+
+// act(x) and act'(x).  The logistic function from exp2 and a reciprocal, each within 2 ulp.
+__device__ __forceinline__ void activation(int kind, float x, float& a, float& d) {
+    if (kind == kRelu) {
+        a = x > 0.f || x != x ? x : 0.f;                   // (what is no number stays none)
+        d = x > 0.f ? 1.f : 0.f;
+    } else if (kind == kGelu) {
+        const float cdf = 0.5f * erfcf(-0.707106781f * x);     // (erfc: no digits are lost in the left tail)
+        a = x == -INFINITY ? 0.f : x * cdf;
+        d = fabsf(x) == INFINITY ? cdf : fmaf(x, 0.398942280f * __expf(-0.5f * x * x), cdf);
+    } else {
+        const float e = exp2_fast(-1.44269504f * x), s = __fdividef(1.f, 1.f + e);
+        const float r = e == INFINITY ? 1.f : e * s;           // 1 - s
+        if (kind == kSigmoid) { a = s; d = s * r; }
+        else {
+            a = x == -INFINITY ? 0.f : x * s;
+            d = fabsf(x) == INFINITY ? s : s * fmaf(x, r, 1.f);
+        }
+    }
+}
+
+// 32 values of a row from column c on; zeros behind its end.  wide: every row starts on 16 bytes.
+template <class T>
+__device__ __forceinline__ void load_row32(const T* __restrict__ row, int cols, bool wide, float (&v)[32]) {
+    constexpr int VEC = 16 / sizeof(T);
+    if (wide && cols >= 32) {
+#pragma unroll
+        for (int i = 0; i < 32 / VEC; ++i) {
+            float w[VEC];
+            unpack_vec<T, VEC>(reinterpret_cast<const uint4*>(row)[i], w);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[i * VEC + j] = w[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = j < cols ? to_float(row[j]) : 0.f;
+    }
+}
+
+// A lane's 32 values as operands: in the operand type, or (T = float) in three bfloat16 parts, each the nearest to what is left.
+template <class T>
+__device__ __forceinline__ void drain_operand(uint8_t* buf, int lane, float (&v)[32], void* out, long long at, long long part, long long ld, int rows, int cols) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll 1
+        for (int k = 0; k < 3; ++k) {
+            float p[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                __nv_bfloat16 b = __float2bfloat16_rn(v[j]);
+                if (__hisinf(b) && !isinf(v[j])) b = __ushort_as_bfloat16((unsigned short)(0x7F7F | (__float_as_uint(v[j]) >> 31 << 15)));   // a finite value stays finite
+                p[j] = __bfloat162float(b);
+                v[j] -= p[j];
+            }
+            drain_rows<__nv_bfloat16>(buf, lane, p, reinterpret_cast<__nv_bfloat16*>(out) + k * part + at, ld, rows, cols, 16);
+        }
+    } else {
+        drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(out) + at, ld, rows, cols, 16);
+    }
+}
+
+// USE as above; A_MN, B_MN: operand is MN-major; T: type of the tensors; ADD_UP: sums in chunks (t.chunk), as class_gemm_kernel takes them.
+template <int USE, bool A_MN, bool B_MN, class T, bool ADD_UP>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(CT_THREADS, 1)
+gated_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ GatedArgs ga) {
+    const TileArgs& a = ga.t;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;   // the same in both CTAs
+    uint8_t* sm = smem_raw + pad;
+    const uint32_t sm_addr = raw_addr + pad;
+    const uint32_t rank = cluster_rank();
+    const uint32_t bars = sm_addr + CT_RING;
+    constexpr int NACC = 2, ACC_COLS = CT_TMEM / NACC;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (CT_STAGES + s); };
+    auto tfull = [&](int i) { return bars + 8u * (2 * CT_STAGES + i); };
+    auto tempty = [&](int i) { return bars + 8u * (2 * CT_STAGES + NACC + i); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + CT_RING + 8 * (2 * CT_STAGES + 2 * NACC));
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < CT_STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int i = 0; i < NACC; ++i) { mbar_init(tfull(i), 1); mbar_init(tempty(i), 2 * CT_EPI_WARPS); }
+        *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    pdl_next();
+    if (warp == 0) tmem_alloc2(smem_u32(tmem_slot), CT_TMEM);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();           // the peer's barriers exist before anything arrives at them
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_wait();
+    if (ga.clear && blockIdx.x == 0 && threadIdx.x == 0) *a.err = 0;
+
+    const int ncl = gridDim.x >> 1, half_w = a.width / 2, products = a.pairs * ga.segs;
+    const long long units = units_of(a);
+
+    if (warp == 0 && lane == 0) {
+        // ---------------- TMA producer: this CTA's rows of A and half of the columns' rows of B; the leader's barrier counts both CTAs' bytes ----------------
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
+            const TileAt t = tile_at(a, u);
+            const int plane = t.m / ga.plane_tiles;
+            const int ra = (t.m - plane * ga.plane_tiles) * CT_M + (int)rank * CT_H;
+            const int rb = USE == kGate ? t.n * CT_H : t.n * a.width + (int)rank * half_w;
+            const int group = ADD_UP ? a.chunk : t.nkb;
+            for (int g = 0; g < t.nkb && ok; g += group)
+                for (int p = 0; p < products && ok; ++p) {
+                    const int seg = p / a.pairs;
+                    int za, zb;
+                    part_pair(p - seg * a.pairs, a.pairs, za, zb);
+                    za += (plane + seg) * ga.parts;
+                    const CUtensorMap* tmB = (USE == kGate ? (int)rank : seg) ? &tmB1 : &tmB0;
+                    for (int kb = t.kb0 + g; kb < t.kb0 + min(g + group, t.nkb); ++kb) {
+                        if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, 41))) break;
+                        if (rank == 0) mbar_expect_tx(full(stage), 2u * (uint32_t)(CT_H + half_w) * (CT_K * 2));
+                        const uint32_t base = sm_addr + stage * CT_STAGE, bar = leader_address(full(stage));
+                        if (A_MN) {
+                            tma_load_3d_pair(base, &tmA, ra, kb * CT_K, za, bar);
+                            tma_load_3d_pair(base + 8192, &tmA, ra + 64, kb * CT_K, za, bar);
+                        } else {
+                            tma_load_3d_pair(base, &tmA, kb * CT_K, ra, za, bar);
+                        }
+                        if (B_MN) {
+                            for (int j = 0; j < half_w; j += 64) tma_load_3d_pair(base + CT_OPERAND + j * 128, tmB, rb + j, kb * CT_K, zb, bar);
+                        } else {
+                            tma_load_3d_pair(base + CT_OPERAND, tmB, kb * CT_K, rb, zb, bar);
+                        }
+                        if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
+                    }
+                }
+        }
+    } else if (warp == 1 && rank == 0) {
+        // ---------------- MMA issuer (leader of the pair): the whole warp runs the loop, one elected lane issues ----------------
+        int stage = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        const uint32_t idesc = instr_desc_f16(a.width, CT_M) | (a.bf16 ? (1u << 7) | (1u << 10) : 0u) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+        constexpr uint32_t stepA = A_MN ? 128 : 2, stepB = B_MN ? 128 : 2;    // 16 values of the reduction: 16 rows of 128 bytes, or 32 bytes of a row
+        bool ok = true;
+        for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
+            const int steps = tile_at(a, u).nkb * products;
+            int left = 0;                                          // stages until this accumulator is full
+            for (int i = 0; i < steps; ++i) {
+                const bool first = left == 0;
+                if (first) {
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 42)))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    left = ADD_UP ? min(a.chunk * products, steps - i) : steps;
+                }
+                const uint32_t d = tmem_base + (uint32_t)(acc * ACC_COLS);
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(full(stage), phase, abort_flag, a.err, 43)))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t base = sm_addr + stage * CT_STAGE;
+                const uint64_t da = operand_desc<A_MN>(base), db = operand_desc<B_MN>(base + CT_OPERAND);
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_pair(d, da + stepA * ks, db + stepB * ks, idesc, !first || ks != 0 ? 1u : 0u);
+                    mma_commit2(empty(stage));                    // in both CTAs
+                    if (left == 1) mma_commit2(tfull(acc));
+                }
+                __syncwarp();
+                if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
+                if (--left == 0 && ++acc == NACC) { acc = 0; acc_phase ^= 1u; }
+            }
+        }
+    } else if (warp >= CT_EPI_WARP0) {   // (warp 1 of the other CTA has nothing to do)
+        // ---------------- drain: this warp's 32 rows (a row a lane) x half of the tile's columns (kGate: half of g and of u) ----------------
+        const int ew = warp - CT_EPI_WARP0, q = warp & 3, half = ew >> 2;
+        uint8_t* buf = sm + CT_RING + 256 + CT_BIAS + ew * 2048;
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        const auto store = [](const void* p, long long ld) { return store_bytes(p, ld * (long long)sizeof(T)); };
+        for (long long u = blockIdx.x >> 1; u < units; u += ncl) {
+            const TileAt t = tile_at(a, u);
+            const int plane = t.m / ga.plane_tiles, tm = t.m - plane * ga.plane_tiles;
+            const int row0 = tm * CT_M + (int)rank * CT_H + q * 32, rows = a.M - row0;   // this warp's rows
+            const int row = row0 + lane;
+            const uint32_t tm_row = tmem_base + ((uint32_t)(q * 32) << 16);
+            const auto release = [&]() {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_leader_tmem(tempty(acc));
+                if (++acc == NACC) { acc = 0; acc_phase ^= 1u; }
+            };
+            bool ok = true;
+            const auto wait_full = [&]() {
+                ok = __all_sync(0xffffffffu, mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 46));
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                return ok;
+            };
+            // this warp's columns of the accumulator: blocks of 32, for kGate two of g and the same two of u behind them
+            const auto block_at = [&](int c) { return USE == kGate ? (c >> 1) * CT_H + half * 64 + (c & 1) * 32 : half * half_w + 32 * c; };
+            const int blocks = USE == kGate ? 4 : half_w / 32;
+            if constexpr (ADD_UP) {
+                const int chunks = (t.nkb + a.chunk - 1) / a.chunk;
+                float sum[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
+                for (int i = 0; i < chunks; ++i) {
+                    if (!wait_full()) break;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (c >= blocks) break;
+                        float v[32];
+                        tmem_ld32(tm_row + (uint32_t)(acc * ACC_COLS + block_at(c)), v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+                    }
+                    if (i < chunks - 1) release();
+                }
+                if (!ok) break;
+                // the sums take the place of the last chunk, and are taken from there block by block: held in registers beside what follows they would spill
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (c < blocks) tmem_st_32x32b_x32(tm_row + (uint32_t)(acc * ACC_COLS + block_at(c)), sum[c]);
+                tmem_wait_st();
+            } else if (!wait_full()) break;
+            const uint32_t at = tm_row + (uint32_t)(acc * ACC_COLS);
+            if constexpr (USE == kGate) {
+                for (int c = 0; c < 2; ++c) {
+                    const int col = t.n * CT_H + half * 64 + 32 * c, cols = a.N - col;
+                    if (rows <= 0 || cols <= 0) break;
+                    float g[32], v[32];
+                    __syncwarp();
+                    tmem_ld32_start(at + (uint32_t)block_at(c), g);
+                    tmem_ld32_start(at + (uint32_t)block_at(c + 2), v);
+                    tmem_ld32_wait(g);
+                    tmem_ld32_wait(v);
+                    if (ga.act) {
+                        float s[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            float d;
+                            activation(ga.activation, g[j], g[j], d);
+                            s[j] = v[j] * d;
+                            v[j] *= g[j];
+                        }
+                        drain_rows<T>(buf, lane, s, reinterpret_cast<T*>(ga.slope) + (long long)row0 * ga.ldslope + col, ga.ldslope, rows, cols, store(ga.slope, ga.ldslope));
+                        drain_rows<T>(buf, lane, g, reinterpret_cast<T*>(ga.act) + (long long)row0 * ga.ldact + col, ga.ldact, rows, cols, store(ga.act, ga.ldact));
+                        if (sizeof(T) == 4) drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(ga.C[0]) + (long long)row0 * ga.ldc[0] + col, ga.ldc[0], rows, cols, store(ga.C[0], ga.ldc[0]));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            float d;
+                            activation(ga.activation, g[j], g[j], d);
+                            v[j] *= g[j];
+                        }
+                    }
+                    drain_operand<T>(buf, lane, v, ga.h, (long long)row0 * ga.ldh + col, ga.h_part, ga.ldh, rows, cols);
+                }
+                release();
+            } else if constexpr (USE == kHidden) {
+                for (int c0 = 0; c0 < half_w; c0 += 32) {
+                    const int col = t.n * a.width + half * half_w + c0, cols = a.N - col;
+                    if (rows <= 0 || cols <= 0) break;
+                    float dh[32], f[32], v[32];
+                    __syncwarp();
+                    tmem_ld32(at + (uint32_t)(half * half_w + c0), dh);
+                    for (int k = 0; k < 2; ++k) {
+                        const T* src = reinterpret_cast<const T*>(k ? ga.act : ga.slope) + (long long)(row < a.M ? row : 0) * (k ? ga.ldact : ga.ldslope) + col;
+                        load_row32<T>(src, row < a.M ? cols : 0, store(k ? ga.act : ga.slope, k ? ga.ldact : ga.ldslope) == 16, f);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = dh[j] * f[j];
+                        drain_operand<T>(buf, lane, v, ga.C[0], (long long)k * ga.parts * ga.h_part + (long long)row0 * ga.ldh + col, ga.h_part, ga.ldh, rows, cols);
+                    }
+                }
+                release();
+            } else {
+                for (int c0 = 0; c0 < half_w; c0 += 32) {
+                    const int col = t.n * a.width + half * half_w + c0, cols = a.N - col;
+                    if (rows <= 0 || cols <= 0) break;
+                    float v[32];
+                    __syncwarp();
+                    tmem_ld32(at + (uint32_t)(half * half_w + c0), v);
+                    if (t.slot >= 0)
+                        drain_rows<float>(buf, lane, v, a.slots + (long long)t.slot * CT_M * a.width + (long long)((int)rank * CT_H + q * 32) * a.width + half * half_w + c0, a.width, 32, 32, 16);
+                    else
+                        drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(ga.C[plane]) + (long long)row0 * ga.ldc[plane] + col, ga.ldc[plane], rows, cols, store(ga.C[plane], ga.ldc[plane]));
+                }
+                release();
+            }
+        }
+    }
+
+    // Tear-down, as in class_gemm_kernel: after a time-out loads in flight get a bounded chance to land; neither CTA leaves while the other may still read its operands or arrive at its barriers.
+    __syncthreads();
+    if (*abort_flag && threadIdx.x == 0 && rank == 0)
+        for (int s = 0; s < CT_STAGES; ++s)
+            for (uint32_t i = 0; i < 4096u; ++i)
+                if (mbar_try_wait(full(s), 0) || mbar_try_wait(full(s), 1)) break;
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();
+    if (warp == 0) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        tmem_dealloc2(tmem_base, CT_TMEM);
+    }
+}
+
+}  // namespace
+
+}  // namespace gad
