@@ -486,6 +486,25 @@ typedef struct {
 int gad_gated_feed_forward_backward_workspace_bytes(const gad_gated_grad_args* args, size_t* bytes);
 int gad_gated_feed_forward_backward(const gad_gated_grad_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Clipping of gradients by their global norm:  n = sqrt(sum over all tensors of g^2),  g' = g min(1, max_norm / n).
+ * A tensor is [rows x cols] with a row stride of ld elements (whatever lies one value behind the other is one row).  out: where g' goes, in g's type or GAD_F32; g itself: in place (nothing is
+ * written where the norm is max_norm at most); NULL: the tensor only counts for the norm.  A norm that is not finite in fp32 leaves the gradients as they are (copied to out).
+ * Sums are fp32 over 32 values and fp64 above; no square over- or underflows.  Equal calls give equal bits.
+ * The list is read on the host before the call returns.  What is written must not overlap anything else in the list (GAD_ERR_ARG; columns of one matrix may be tensors of their own); a tensor that is only
+ * read may be there twice, and counts twice.  count 0: the norm is 0.  Refused (GAD_ERR_RANGE): more than 2^20 tensors, 2^40 values in one. */
+typedef struct {
+    const void* g;
+    int32_t dtype, out_dtype;
+    int64_t rows, cols, ld;
+    void* out;
+    int64_t out_ld;
+} gad_grad_tensor;
+
+/* workspace: device, 16-byte aligned; its size depends on count alone.  norm: device [1].  max_norm: 0 and more; infinity: the norm alone. */
+int gad_clip_grads_workspace_bytes(int64_t count, size_t* bytes);
+int gad_clip_grads(const gad_grad_tensor* tensors, int64_t count, float max_norm, float* norm, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
 /* Frees the pinned host memory that the library keeps and no context or call is using. */
 int gad_release_pinned(void);
 

@@ -6,3 +6,4 @@ from .binding import (  # noqa: F401
 from .multi import ShardedEpoch, RoundsEpoch, shard_subgraphs  # noqa: F401
 from .head import ClassLoss, class_loss, distill_loss, layer_norm, layer_norm_backward  # noqa: F401
 from .feed_forward import GatedForward, GatedGrads, gated_feed_forward, gated_feed_forward_backward  # noqa: F401
+from .grads import clip_grads, grad_norm  # noqa: F401

@@ -31,6 +31,7 @@ SYMBOLS = (
     "gad_layer_norm", "gad_layer_norm_backward_workspace_bytes", "gad_layer_norm_backward",
     "gad_class_loss_workspace_bytes", "gad_class_loss",
     "gad_gated_feed_forward_workspace_bytes", "gad_gated_feed_forward", "gad_gated_feed_forward_backward_workspace_bytes", "gad_gated_feed_forward_backward",
+    "gad_clip_grads_workspace_bytes", "gad_clip_grads",
 )
 
 

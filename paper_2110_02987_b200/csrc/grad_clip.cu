@@ -1,0 +1,333 @@
+// The norm over all gradients of a program, n = sqrt(sum g^2), and the gradients scaled by f = min(1, max_norm / n), in place or into tensors of their own.
+//
+// Two launches for up to 440 tensors.  The list of tensors is a parameter of the kernels, so nothing is copied to the device beforehand and a captured graph holds it.  Tensors are cut
+// into chunks of 8192 values; block b takes chunks b, b + blocks, ... and leaves one sum (grad_squares_kernel).  Every block of the second launch adds those sums up
+// itself, in the same order (a ticket for the last block would have to be cleared beforehand: a launch more), and scales its chunks, the last first: those the L2 still holds.
+// Bound by HBM: the gradients are read twice, as far as the L2 does not hold them, and written once.
+//
+// Sums of squares are fp32 over the values of a chunk a thread has (32 of them), fp64 above.  A thread's sum outside 2^-80 .. 2^100 is taken again in fp64, so no
+// square over- or underflows; whether a sum of zero is one of zeros shows in the values' bits.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+#include <vector>
+
+#include "half_types.cuh"
+
+namespace gad {
+
+namespace {
+
+constexpr int kChunkValues = 8192, kClipThreads = 256;
+constexpr int kClipBlocks = 592;                         // four a multiprocessor: 1024 threads, 4 x 16 bytes on their way each
+
+struct ClipEntry {
+    const void* g; void* out;
+    long long rows, cols, ld, out_ld;
+    int type, out_type;
+    int first;                                           // chunk, among those of a launch
+    int rows_per, pieces;                                // rows a chunk has, or pieces a row has
+    int wide;                                            // every row of both starts on 16 bytes
+};
+template <int MOST> struct ClipTable { ClipEntry e[MOST]; int n, chunks; };
+
+// A chunk: `rows` rows of `cols` values.
+struct ClipChunk { long long row, col; int rows, cols; };
+template <int MOST>
+__device__ __forceinline__ const ClipEntry& find_chunk(const ClipTable<MOST>& t, int c, ClipChunk& k) {
+    int lo = 0, hi = t.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (t.e[mid].first <= c) lo = mid; else hi = mid - 1;
+    }
+    const ClipEntry& e = t.e[lo];
+    const long long i = c - e.first;
+    if (e.pieces > 1) {
+        k.row = i / e.pieces;
+        k.col = (i - k.row * e.pieces) * kChunkValues;
+        k.rows = 1;
+        k.cols = (int)min((long long)kChunkValues, e.cols - k.col);
+    } else {
+        k.row = i * e.rows_per;
+        k.col = 0;
+        k.rows = (int)min((long long)e.rows_per, e.rows - k.row);
+        k.cols = (int)e.cols;
+    }
+    return e;
+}
+
+// This thread's values of a chunk: f(row of the chunk, column, values) for vectors of 16 bytes (VEC) or one value.  A warp has a row, or, of rows narrower than 32 vectors, a part of one.
+template <int VEC, class F>
+__device__ __forceinline__ void each_vector(const ClipChunk& k, F f) {
+    const int n = (k.cols + VEC - 1) / VEC, total = n * k.rows;
+    if (k.rows == 1) {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n; i += kClipThreads) f(0, i * VEC);
+    } else {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < total; i += kClipThreads) { const int r = i / n; f(r, (i - r * n) * VEC); }
+    }
+}
+
+template <class T, int VEC>
+__device__ __forceinline__ double chunk_squares(const ClipEntry& e, const ClipChunk& k) {
+    const T* base = reinterpret_cast<const T*>(e.g) + k.row * e.ld + k.col;
+    float s = 0.f;
+    uint32_t bits = 0;
+    each_vector<VEC>(k, [&](int r, int c) {
+        RowVec<T, VEC> raw;
+        load_raw<T, VEC>(base + r * e.ld, c, k.cols, raw);
+        float v[VEC];
+        if constexpr (VEC > 1) {
+            unpack_vec<T, VEC>(raw.u, v);
+            bits |= raw.u.x | raw.u.y | raw.u.z | raw.u.w;
+        } else {
+            v[0] = to_float(raw.e[0]);
+            bits |= __float_as_uint(v[0]);
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) s = fmaf(v[j], v[j], s);
+    });
+    if (s >= 0x1p-80f && s <= 0x1p100f) return s;
+    if ((bits & (sizeof(T) == 4 || VEC == 1 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0) return 0.0;
+    double d = 0.0;
+    each_vector<VEC>(k, [&](int r, int c) {
+        for (int j = 0; j < VEC && c + j < k.cols; ++j) { const double v = to_float(base[r * e.ld + c + j]); d = fma(v, v, d); }
+    });
+    return d;
+}
+template <class T>
+__device__ __forceinline__ double chunk_squares(const ClipEntry& e, const ClipChunk& k) { return e.wide ? chunk_squares<T, 16 / (int)sizeof(T)>(e, k) : chunk_squares<T, 1>(e, k); }
+
+__device__ __forceinline__ double block_sum(double s, double* sm) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int i = 0; i < kClipThreads / 32; ++i) s += sm[i];
+    return s;
+}
+
+template <int MOST>
+__global__ void __launch_bounds__(kClipThreads) grad_squares_kernel(const __grid_constant__ ClipTable<MOST> t, double* __restrict__ sums) {
+    __shared__ double sm[kClipThreads / 32];
+    pdl_next();
+    pdl_wait();
+    double s = 0.0;
+    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+        ClipChunk k;
+        const ClipEntry& e = find_chunk(t, c, k);
+        s += e.type == GAD_F32 ? chunk_squares<float>(e, k) : e.type == GAD_F16 ? chunk_squares<__half>(e, k) : chunk_squares<__nv_bfloat16>(e, k);
+    }
+    s = block_sum(s, sm);
+    if (threadIdx.x == 0) sums[blockIdx.x] = s;
+}
+
+template <class T, class O, int VEC>
+__device__ __forceinline__ void scale_chunk(const ClipEntry& e, const ClipChunk& k, float f) {
+    const T* src = reinterpret_cast<const T*>(e.g) + k.row * e.ld + k.col;
+    O* dst = reinterpret_cast<O*>(e.out) + k.row * e.out_ld + k.col;
+    each_vector<VEC>(k, [&](int r, int c) {
+        RowVec<T, VEC> raw;
+        load_raw<T, VEC>(src + r * e.ld, c, k.cols, raw);
+        O* to = dst + r * e.out_ld;
+        if constexpr (std::is_same<T, O>::value) {
+            if (f == 1.f) {                              // a copy, to the bit: a product makes one NaN of all
+                if constexpr (VEC > 1) {
+                    if (c + VEC <= k.cols) { *reinterpret_cast<uint4*>(to + c) = raw.u; return; }
+                }
+#pragma unroll
+                for (int j = 0; j < VEC; ++j)
+                    if (c + j < k.cols) to[c + j] = raw.e[j];
+                return;
+            }
+        }
+        float v[VEC];
+        if constexpr (VEC > 1) unpack_vec<T, VEC>(raw.u, v); else v[0] = to_float(raw.e[0]);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[j] *= f;
+        if constexpr (VEC == 1) to[c] = from_float<O>(v[0]);
+        else if constexpr (sizeof(O) == sizeof(T)) store_vec<O, VEC>(to, c, k.cols, v);
+        else {
+            // 16-bit gradients into fp32: two vectors
+            float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+            store_vec<O, 4>(to, c, k.cols, a);
+            store_vec<O, 4>(to, c + 4, k.cols, b);
+        }
+    });
+}
+template <class T, class O>
+__device__ __forceinline__ void scale_chunk(const ClipEntry& e, const ClipChunk& k, float f) {
+    if (e.wide) scale_chunk<T, O, 16 / (int)sizeof(T)>(e, k, f); else scale_chunk<T, O, 1>(e, k, f);
+}
+
+// write: this launch writes the norm.
+template <int MOST>
+__global__ void __launch_bounds__(kClipThreads) grad_scale_kernel(const __grid_constant__ ClipTable<MOST> t, const double* __restrict__ sums, int nsums, float max_norm, float* __restrict__ norm, int write) {
+    __shared__ double sm[kClipThreads / 32];
+    pdl_next();
+    pdl_wait();
+    after_wait(sums);
+    double s = 0.0;
+    for (int i = threadIdx.x; i < nsums; i += kClipThreads) s += sums[i];
+    s = block_sum(s, sm);
+    const double n = sqrt(s);
+    const float nf = (float)n;
+    if (write && blockIdx.x == 0 && threadIdx.x == 0) *norm = nf;
+    // a norm that is not finite (in fp32) leaves the gradients as they are
+    const float f = nf > max_norm && isfinite(nf) ? (float)((double)max_norm / n) : 1.f;
+    for (int c = t.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
+        ClipChunk k;
+        const ClipEntry& e = find_chunk(t, c, k);
+        if (!e.out || (f == 1.f && e.out == e.g)) continue;
+        if (e.type == GAD_F32) scale_chunk<float, float>(e, k, f);
+        else if (e.type == GAD_F16) { if (e.out_type == GAD_F32) scale_chunk<__half, float>(e, k, f); else scale_chunk<__half, __half>(e, k, f); }
+        else { if (e.out_type == GAD_F32) scale_chunk<__nv_bfloat16, float>(e, k, f); else scale_chunk<__nv_bfloat16, __nv_bfloat16>(e, k, f); }
+    }
+}
+
+constexpr int kClipMost = 440;                           // tensors a launch; parameters may take 32 764 bytes
+
+int64_t value_bytes(int type) { return type == GAD_F32 ? 4 : 2; }
+bool empty_tensor(const gad_grad_tensor& t) { return t.rows == 0 || t.cols == 0; }
+// Whole rows one behind the other are one row.
+void as_rows(const gad_grad_tensor& t, int64_t& rows, int64_t& cols) {
+    rows = t.rows; cols = t.cols;
+    if (rows > 1 && t.ld == cols && (!t.out || t.out_ld == cols)) { cols *= rows; rows = 1; }
+}
+
+int check_tensor(const gad_grad_tensor& t) {
+    if (t.dtype < GAD_F32 || t.dtype > GAD_BF16 || t.rows < 0 || t.cols < 0) return GAD_ERR_ARG;
+    if (t.rows > (int64_t)1 << 40 || t.cols > (int64_t)1 << 40 || (t.cols && t.rows > ((int64_t)1 << 40) / t.cols) || t.ld > (int64_t)1 << 40 || t.out_ld > (int64_t)1 << 40) return GAD_ERR_RANGE;
+    if (empty_tensor(t)) return GAD_OK;
+    const uintptr_t mask = (uintptr_t)value_bytes(t.dtype) - 1;
+    if (!t.g || ((uintptr_t)t.g & mask) != 0 || (t.rows > 1 && t.ld < t.cols)) return GAD_ERR_ARG;
+    if (!t.out) return GAD_OK;
+    if (t.out_dtype != t.dtype && t.out_dtype != GAD_F32) return GAD_ERR_ARG;
+    if (((uintptr_t)t.out & ((uintptr_t)value_bytes(t.out_dtype) - 1)) != 0 || (t.rows > 1 && t.out_ld < t.cols)) return GAD_ERR_ARG;
+    if (t.out == t.g && (t.out_dtype != t.dtype || (t.rows > 1 && t.out_ld != t.ld))) return GAD_ERR_ARG;
+    return GAD_OK;
+}
+
+// What is written must not be read or written elsewhere in the list.  Column ranges of the same matrix do not meet although their first to last bytes do.
+struct Region { uintptr_t lo, hi; int64_t ld, width; bool written; };
+bool meet(const Region& a, const Region& b) {
+    if (a.ld && a.ld == b.ld) {
+        const int64_t d = (int64_t)((b.lo - a.lo) % (uintptr_t)a.ld);
+        if (d >= a.width && d + b.width <= a.ld) return false;
+    }
+    return true;
+}
+int check_regions(const gad_grad_tensor* t, int64_t count) {
+    std::vector<Region> all;
+    all.reserve(2 * (size_t)count);
+    for (int64_t i = 0; i < count; ++i) {
+        if (empty_tensor(t[i])) continue;
+        const auto add = [&](const void* p, int64_t ld, int type, bool written) {
+            const int64_t e = value_bytes(type);
+            const bool rows = t[i].rows > 1 && ld != t[i].cols;
+            all.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((t[i].rows - 1) * (t[i].rows > 1 ? ld : 0) + t[i].cols) * e), rows ? ld * e : 0, t[i].cols * e, written});
+        };
+        const bool inside = t[i].out == t[i].g;
+        add(t[i].g, t[i].ld, t[i].dtype, inside);
+        if (t[i].out && !inside) add(t[i].out, t[i].out_ld, t[i].out_dtype, true);
+    }
+    std::sort(all.begin(), all.end(), [](const Region& a, const Region& b) { return a.lo < b.lo; });
+    for (size_t i = 0; i < all.size(); ++i)
+        for (size_t j = i + 1; j < all.size() && all[j].lo < all[i].hi; ++j)
+            if ((all[i].written || all[j].written) && meet(all[i], all[j])) return GAD_ERR_ARG;
+    return GAD_OK;
+}
+
+template <int MOST>
+int fill_table(const gad_grad_tensor* t, int64_t& i, int64_t count, bool scaled, ClipTable<MOST>& table) {
+    table.n = 0;
+    int64_t chunks = 0;
+    for (; i < count && table.n < MOST; ++i) {
+        if (empty_tensor(t[i]) || (scaled && !t[i].out)) continue;
+        ClipEntry& e = table.e[table.n];
+        int64_t rows, cols;
+        as_rows(t[i], rows, cols);
+        const int64_t a = value_bytes(t[i].dtype), b = value_bytes(t[i].out_dtype);
+        e.g = t[i].g; e.out = t[i].out; e.rows = rows; e.cols = cols; e.ld = t[i].ld; e.out_ld = t[i].out_ld;
+        e.type = t[i].dtype; e.out_type = t[i].out_dtype;
+        e.wide = ((uintptr_t)e.g % 16 == 0) && (rows == 1 || t[i].ld * a % 16 == 0);
+        if (t[i].out) e.wide = e.wide && ((uintptr_t)e.out % 16 == 0) && (rows == 1 || t[i].out_ld * b % 16 == 0);
+        e.pieces = (int)((cols + kChunkValues - 1) / kChunkValues);
+        e.rows_per = e.pieces > 1 ? 1 : (int)std::min<int64_t>(rows, std::max<int64_t>(1, kChunkValues / cols));
+        e.first = (int)chunks;
+        const int64_t more = e.pieces > 1 ? rows * e.pieces : (rows + e.rows_per - 1) / e.rows_per;
+        if (chunks + more > INT32_MAX / 2) { if (table.n == 0) return GAD_ERR_RANGE; break; }
+        chunks += more;
+        ++table.n;
+    }
+    table.chunks = (int)chunks;
+    return GAD_OK;
+}
+
+int blocks_for(int chunks) { return std::max(1, std::min(chunks, kClipBlocks)); }
+
+template <int MOST>
+int run_clip(const gad_grad_tensor* t, int64_t count, float max_norm, float* norm, double* sums, cudaStream_t s) {
+    ClipTable<MOST> table;
+    int nsums = 0;
+    bool first = true;
+    for (int64_t i = 0; i < count || first;) {
+        const int rc = fill_table(t, i, count, false, table);
+        if (rc != GAD_OK) return rc;
+        const int blocks = blocks_for(table.chunks);
+        if (chain(grad_squares_kernel<MOST>, dim3((unsigned)blocks), kClipThreads, 0, s, first, table, sums + nsums) != cudaSuccess) return GAD_ERR_CUDA;
+        nsums += blocks;
+        first = false;
+    }
+    bool write = true;
+    for (int64_t i = 0; i < count || write;) {
+        const int rc = fill_table(t, i, count, true, table);
+        if (rc != GAD_OK) return rc;
+        if (!table.chunks && !write) break;
+        if (chain(grad_scale_kernel<MOST>, dim3((unsigned)blocks_for(table.chunks)), kClipThreads, 0, s, false, table, (const double*)sums, nsums, max_norm, norm, (int)write) != cudaSuccess) return GAD_ERR_CUDA;
+        write = false;
+    }
+    return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
+}
+
+// Launches of the first kernel are at most one a kClipMost tensors, and one for every run of 2^30 chunks.
+size_t clip_bytes(int64_t count) { return sizeof(double) * kClipBlocks * (size_t)(2 + count / 16); }
+
+int check_list(const gad_grad_tensor* t, int64_t count) {
+    if (count < 0 || (count > 0 && !t)) return GAD_ERR_ARG;
+    if (count > 1 << 20) return GAD_ERR_RANGE;
+    for (int64_t i = 0; i < count; ++i) {
+        const int rc = check_tensor(t[i]);
+        if (rc != GAD_OK) return rc;
+    }
+    return GAD_OK;
+}
+
+}  // namespace
+}  // namespace gad
+
+extern "C" int gad_clip_grads_workspace_bytes(int64_t count, size_t* bytes) {
+    if (count < 0 || !bytes) return GAD_ERR_ARG;
+    if (count > 1 << 20) return GAD_ERR_RANGE;
+    *bytes = gad::clip_bytes(count);
+    return GAD_OK;
+}
+
+extern "C" int gad_clip_grads(const gad_grad_tensor* tensors, int64_t count, float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace gad;
+    try {
+        int rc = check_list(tensors, count);
+        if (rc != GAD_OK) return rc;
+        if (!norm || !(max_norm >= 0.f)) return GAD_ERR_ARG;
+        rc = check_regions(tensors, count);
+        if (rc != GAD_OK) return rc;
+        if (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < clip_bytes(count)) return GAD_ERR_OOM;
+        const cudaStream_t s = (cudaStream_t)stream;
+        double* sums = (double*)workspace;
+        return count <= 16 ? run_clip<16>(tensors, count, max_norm, norm, sums, s) : count <= 64 ? run_clip<64>(tensors, count, max_norm, norm, sums, s) : run_clip<kClipMost>(tensors, count, max_norm, norm, sums, s);
+    } catch (...) {   // (the list of regions could not grow)
+        return GAD_ERR_OOM;
+    }
+}
