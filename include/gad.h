@@ -429,6 +429,24 @@ typedef struct {
 int gad_class_loss_workspace_bytes(const gad_class_loss_args* args, size_t* bytes);
 int gad_class_loss(const gad_class_loss_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Clipped policy loss of actions chosen among the classes of an output layer, with a KL term: head.labels are the actions (k = 0).  With lp_i = log softmax(z_i)_action and r = exp(lp - old):
+ *   l_i = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_weight (exp(ref - lp) - (ref - lp) - 1)          (the last term where ref_logp is given)
+ * and loss, weights, rows that count and gradients as in gad_class_loss; a row whose ratio is clipped has no gradient of the first term.  Rows that do not count (action < 0) get a loss
+ * and a log-probability of zero whatever old_logp, advantages and ref_logp hold there.  An action of `classes` or more makes that row's loss, and the whole, NaN; the gradients are then those of the other rows. */
+typedef struct {
+    gad_class_loss_args head;
+    const float* old_logp;         /* [rows] log-probability of the action when it was drawn                */
+    const float* advantages;       /* [rows]                                                                */
+    const float* ref_logp;         /* [rows] of the reference policy, or NULL: no KL term                   */
+    float clip_low, clip_high;     /* 0 .. 1 and 0 .. infinity                                              */
+    float kl_weight;               /* 0 and more                                                            */
+    float* logp;                   /* device [rows]: lp_i                                                   */
+} gad_policy_loss_args;
+
+/* Workspace as that of gad_class_loss, and half a byte a row. */
+int gad_policy_loss_workspace_bytes(const gad_policy_loss_args* args, size_t* bytes);
+int gad_policy_loss(const gad_policy_loss_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Gated feed-forward block:  g = x Wg^T,  u = x Wu^T,  h = act(g) u,  y = h Wd^T   for x [rows x cols], Wg and Wu [inner x cols], Wd [cols x inner].
  * For a backward pass act, slope and h [rows x inner] (all three, or none) receive act(g), u act'(g) and h, rounded to dtype.  The activations: g / (1 + exp(-g)); g times the
  * normal distribution's cumulated density (gelu, by erf); max(g, 0), whose slope at 0 is 0; 1 / (1 + exp(-g)).

@@ -29,7 +29,7 @@ SYMBOLS = (
     "gad_consensus_apply", "gad_export_params", "gad_get_train_counts", "gad_augment_workspace_bytes", "gad_augment",
     "gad_augment_last_error", "gad_debug_expire_wait", "gad_default_params", "gad_check_store", "gad_release_pinned",
     "gad_layer_norm", "gad_layer_norm_backward_workspace_bytes", "gad_layer_norm_backward",
-    "gad_class_loss_workspace_bytes", "gad_class_loss",
+    "gad_class_loss_workspace_bytes", "gad_class_loss", "gad_policy_loss_workspace_bytes", "gad_policy_loss",
     "gad_gated_feed_forward_workspace_bytes", "gad_gated_feed_forward", "gad_gated_feed_forward_backward_workspace_bytes", "gad_gated_feed_forward_backward",
     "gad_clip_grads_workspace_bytes", "gad_clip_grads",
 )

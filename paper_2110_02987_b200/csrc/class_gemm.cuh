@@ -73,7 +73,7 @@ struct TileArgs {
     int add;                   // AddTo
     float* sums;               // [M x N]
     float* slots;              // [tiles - whole][shares][256 x width] sums of shares
-    const float* scal;         // [1] factor of the results
+    const float* scal;         // factors: [1] of a result without sums; [3] of what is added to the sums, [4] of a result with them
 };
 
 // Products of operand parts, the smallest first, so that what an addition to the accumulator cuts off is small for as long as possible.
@@ -388,7 +388,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         uint8_t* buf = sm + CT_RING + 256 + CT_BIAS + ew * 2048;
         int acc = 0;
         uint32_t acc_phase = 0;
-        const float factor = USE == kOut ? a.scal[1] : 1.f;
+        const float factor = USE == kOut ? a.scal[a.add == kAddNone ? 1 : 4] : 1.f, pre = USE == kOut && a.add != kAddNone ? a.scal[3] : 1.f;
         const int bytes = USE == kOut ? store_bytes(a.C, a.ldc * (long long)sizeof(T)) : 16, sum_bytes = a.N % 4 == 0 ? 16 : a.N % 2 == 0 ? 8 : 4;
         for (long long u = blockIdx.x >> 1; u < units; u += ncl) {
             const TileAt t = tile_at(a, u);
@@ -479,8 +479,12 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                         float* out = a.slots + (long long)t.slot * CT_M * a.width + (long long)(row0 - t.m * CT_M) * a.width + half * half_w + c0;
                         drain_rows<float>(buf, lane, v, out, a.width, 32, 32, 16);
                     } else if (a.add == kAddFirst) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= pre;
                         drain_rows<float>(buf, lane, v, a.sums + at, a.N, rows, cols, sum_bytes);
                     } else if (a.add == kAddMore) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= pre;
                         drain_rows<float, true>(buf, lane, v, a.sums + at, a.N, rows, cols, sum_bytes);
                     } else {
                         if (a.add == kAddLast) {
@@ -494,7 +498,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                                 }
                                 __syncwarp();
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) v[c + j] += *reinterpret_cast<const float*>(staged(buf, lane, j >> 2) + (j & 3) * 4);
+                                for (int j = 0; j < 16; ++j) v[c + j] = fmaf(v[c + j], pre, *reinterpret_cast<const float*>(staged(buf, lane, j >> 2) + (j & 3) * 4));
                             }
                         }
 #pragma unroll

@@ -478,9 +478,18 @@ __global__ void __launch_bounds__(32 * kSomeWarps, 1) class_some_kernel(const Fe
 
 constexpr int kFinishRows = 8;
 
+// The policy loss: with lp the log-probability of a row's label, r = exp(lp - old), its row loss is  -min(r A, clip(r, lo, hi) A) + kl (exp(ref - lp) - (ref - lp) - 1).
+struct PolicyArgs {
+    const float *old, *advantages, *ref;          // of this block of rows; ref null: no KL term.  old null: no policy loss
+    float lo, hi, kl;
+    float* logp;
+    float* most;                                  // [blocks] largest coefficient of G among a block's rows
+};
+
 struct FinishArgs {
     const float4* stats; int parts, rows;
-    const float4* rowk;
+    float4* rowk;
+    PolicyArgs policy;
     float sc, inv_t, temperature;
     float4* rowc; float* row_loss;
     double* shares; int share0, nshares;          // of the loss: a block's sum of weighted row losses
@@ -492,7 +501,8 @@ struct FinishArgs {
 
 // The parts of a row's statistics joined (bound by the latency of its loads: 4096 rows of 256 parts 12 us): a block has 8 rows, 32 threads each, every 32nd part a thread; joined pairwise in a fixed order.  The block that comes last
 // writes, for the first block of rows, scal[0], a power of two that brings the largest coefficient of G to 2^14 .. 2^15, [1]: scale / counted rows / that,
-// [2]: scale / counted rows; and for the last one the loss.
+// [2]: scale / counted rows; and for the last one the loss.  [3] and [4]: factors of a block's sums and of what they add up to.  The coefficients of a policy loss are
+// known when its rows are finished, block by block, so each block of rows has a power of two of its own, and leaves it out of the sums.
 template <int NL>
 __global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
     __shared__ float4 sm[8][kFinishRows];
@@ -530,6 +540,7 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
     __syncthreads();
     if (w == 0) {
         double mine = 0.0;
+        float coefficient = 0.f;
         if (lane < kFinishRows && r < a.rows) {
             at = sm[0][lane];
             for (int i = 1; i < 8; ++i) at = join(at, sm[i][lane]);
@@ -538,7 +549,29 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
             const float l1 = at.x + log2f(at.y), l2 = NL == 2 ? at.x * inv_t + log2f(at.z) : l1;
             const float ln2 = 0.693147181f;
             const bool counts = k.x > 0.f || k.y > 0.f;
-            const float l = counts ? k.x * (l1 * ln2) + k.y * (l2 * ln2) + k.z - at.w / a.sc : 0.f;
+            float l = counts ? k.x * (l1 * ln2) + k.y * (l2 * ln2) + k.z - at.w / a.sc : 0.f;
+            if (a.policy.old) {
+                const PolicyArgs& y = a.policy;
+                float lp = 0.f, slope = 0.f;                        // slope: of the row loss by lp
+                if (counts) {
+                    // dl / dz = slope (one-hot - p): what G = w (p - tau) is given for w, tau = 1
+                    lp = (at.w - l1) * ln2 - k.z;
+                    const float adv = y.advantages[r], ratio = expf(lp - y.old[r]), plain = ratio * adv, held = fminf(fmaxf(ratio, y.lo), y.hi) * adv;
+                    const bool clipped = plain > held;              // (a product that is no number is taken)
+                    l = clipped ? -held : -plain;
+                    slope = clipped ? 0.f : -plain;
+                    if (y.ref) {
+                        const float d = y.ref[r] - lp, e = expm1f(d);
+                        l = fmaf(y.kl, e - d, l);
+                        slope = fmaf(-y.kl, e, slope);
+                    }
+                    if (k.z != k.z) slope = 0.f;                    // a label that is no class: the loss says so, the gradients are without the row
+                }
+                y.logp[r] = lp;
+                const float c = counts ? -slope * k.w : 0.f;
+                a.rowk[r].w = c;
+                coefficient = fabsf(c);
+            }
             a.row_loss[r] = l;
             // gradient: a p + (1 - a) T p^T; with one softmax both coefficients are its
             const float ca = k.x, cb = k.y / a.temperature;
@@ -546,8 +579,12 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
             if (counts) mine = (double)k.w * (double)l;
         }
 #pragma unroll
-        for (int o = 1; o < kFinishRows; o <<= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        for (int o = 1; o < kFinishRows; o <<= 1) {
+            mine += __shfl_xor_sync(0xffffffffu, mine, o);
+            coefficient = fmaxf(coefficient, __shfl_xor_sync(0xffffffffu, coefficient, o));
+        }
         if (lane == 0) {
+            if (a.policy.old) a.policy.most[blockIdx.x] = coefficient;
             a.shares[a.share0 + blockIdx.x] = mine;
             __threadfence();
             last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
@@ -556,12 +593,16 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
     __syncthreads();
     if (!last) return;
     __threadfence();
-    if (a.first) {
+    if (a.first || a.policy.old) {
         RowShare rows{0, 0.f};
         for (int i = threadIdx.x; i < a.nrow_shares; i += 256) {
             const RowShare v = a.row_shares[i];
             rows.n += v.n;
             rows.most = fmaxf(rows.most, v.most);
+        }
+        if (a.policy.old) {
+            rows.most = 0.f;
+            for (int i = threadIdx.x; i < gridDim.x; i += 256) rows.most = fmaxf(rows.most, __ldcg(a.policy.most + i));
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
@@ -578,7 +619,7 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
     if (lane == 0) smt[w] = all;
     __syncthreads();
     if (threadIdx.x) return;
-    if (a.first) {
+    if (a.first || a.policy.old) {
         RowShare v = smr[0];
         for (int i = 1; i < 8; ++i) { v.n += smr[i].n; v.most = fmaxf(v.most, smr[i].most); }
         const double f = a.mean ? (v.n ? (double)a.scale / v.n : 0.0) : (double)a.scale;
@@ -587,6 +628,8 @@ __global__ void __launch_bounds__(256) class_finish_kernel(const FinishArgs a) {
         a.scal[0] = g;
         a.scal[1] = (float)(f / (double)g);
         a.scal[2] = (float)f;
+        a.scal[3] = a.policy.old ? 1.f / g : 1.f;
+        a.scal[4] = a.policy.old ? (float)f : a.scal[1];
     }
     if (a.final) {
         all = smt[0];
@@ -758,7 +801,7 @@ __global__ void __launch_bounds__(256) class_join_kernel(const TileArgs a) {
     const TileAt t = tile_at(a, a.whole + (long long)i * a.shares);
     const int row = t.m * CT_M + r, c = t.n * a.width + x;
     if (row >= a.M || c >= a.N) return;
-    const float factor = a.scal[1];
+    const float factor = a.scal[a.add == kAddNone ? 1 : 4], pre = a.add == kAddNone ? 1.f : a.scal[3];
     const float* slot = a.slots + ((long long)i * a.shares * CT_M + r) * a.width + x;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -771,6 +814,7 @@ __global__ void __launch_bounds__(256) class_join_kernel(const TileArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         if (c + j >= a.N) break;
+        if (a.add != kAddNone) s[j] *= pre;
         if (a.add == kAddMore || a.add == kAddLast) s[j] += sum[j];
         if (a.add == kAddFirst || a.add == kAddMore) sum[j] = s[j];
         else out[j] = from_float<T>(factor * s[j]);
@@ -797,9 +841,10 @@ __global__ void __launch_bounds__(256) class_bias_kernel(const float* __restrict
     if (w || c >= classes) return;
     s = 0.f;
     for (int k = 0; k < 8; ++k) s += sm[k][threadIdx.x & 31];
+    if (add != kAddNone) s *= scal[3];
     if (add == kAddMore || add == kAddLast) s += sums[c];
     if (add == kAddFirst || add == kAddMore) sums[c] = s;
-    else db[c] = from_float<T>(s * scal[1]);
+    else db[c] = from_float<T>(s * scal[add == kAddNone ? 1 : 4]);
 }
 
 template <class T>
@@ -833,10 +878,10 @@ struct ClassPlan {
     int64_t ldp, ldg;                // row lengths of the packed operands, and of z and G
     int64_t block;                   // rows a block
     int nblocks;
-    int64_t o_hp, o_wp, o_targets, o_starts, o_rowk, o_rowc, o_stats, o_rshares, o_lshares, o_scal, o_z, o_g, o_colsum, o_dbsum, o_slots, o_sums, total;
+    int64_t o_hp, o_wp, o_targets, o_starts, o_rowk, o_rowc, o_stats, o_rshares, o_lshares, o_scal, o_z, o_g, o_colsum, o_dbsum, o_slots, o_sums, o_most, total;
 };
 
-ClassPlan plan_class(const gad_class_loss_args& a) {
+ClassPlan plan_class(const gad_class_loss_args& a, bool policy = false) {
     ClassPlan p{};
     const int64_t N = a.rows;
     const int D = a.cols, V = a.classes;
@@ -886,6 +931,7 @@ ClassPlan plan_class(const gad_class_loss_args& a) {
         if (a.dH || a.dW) p.o_slots = room((int64_t)kPairs * CT_M * p.width_d * 4);
         if (a.dW && p.nblocks > 1) p.o_sums = room(4 * (int64_t)V * D);
     }
+    if (policy) p.o_most = room(4 * ((p.block + kFinishRows - 1) / kFinishRows));
     p.total = at;
     return p;
 }
@@ -947,9 +993,9 @@ cudaError_t go_out(const CUtensorMap& A, const CUtensorMap& B, TileArgs a, cudaS
 }
 
 template <class T>
-cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) {
+cudaError_t run_class_steps(const gad_class_loss_args& a, const gad_policy_loss_args* policy, uint8_t* ws, cudaStream_t s) {
 #define GAD_TRY(x) do { const cudaError_t e_ = (x); if (e_ != cudaSuccess) return e_; } while (0)
-    const ClassPlan p = plan_class(a);
+    const ClassPlan p = plan_class(a, policy != nullptr);
     const int64_t N = a.rows;
     const int D = a.cols, V = a.classes;
     float* scal = reinterpret_cast<float*>(ws + p.o_scal);
@@ -1026,6 +1072,9 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
         f.shares = reinterpret_cast<double*>(ws + p.o_lshares); f.share0 = (int)(r0 / kFinishRows); f.nshares = (int)((N + kFinishRows - 1) / kFinishRows);
         f.row_shares = ra.shares; f.nrow_shares = nrshares; f.ticket = ra.ticket; f.scale = a.scale; f.mean = a.mean; f.first = b == 0; f.final = b == p.nblocks - 1;
         f.scal = scal; f.loss = a.loss;
+        if (policy)
+            f.policy = {policy->old_logp + r0, policy->advantages + r0, policy->ref_logp && policy->kl_weight != 0.f ? policy->ref_logp + r0 : nullptr, 1.f - policy->clip_low, 1.f + policy->clip_high,
+                        policy->kl_weight, policy->logp + r0, reinterpret_cast<float*>(ws + p.o_most)};
         GAD_TRY(chain(p.nl == 2 ? class_finish_kernel<2> : class_finish_kernel<1>, dim3((unsigned)blocks), 256, 0, s, false, f));
         if (!p.grads) continue;
         GradArgs g{};
@@ -1065,7 +1114,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, uint8_t* ws, cudaStrea
 #undef GAD_TRY
 }
 template <class T>
-int run_class(const gad_class_loss_args& a, uint8_t* ws, cudaStream_t s) { return run_class_steps<T>(a, ws, s) == cudaSuccess ? GAD_OK : GAD_ERR_CUDA; }
+int run_class(const gad_class_loss_args& a, const gad_policy_loss_args* policy, uint8_t* ws, cudaStream_t s) { return run_class_steps<T>(a, policy, ws, s) == cudaSuccess ? GAD_OK : GAD_ERR_CUDA; }
 
 // No rows: no loss, and gradients of zero.
 template <class T>
@@ -1105,19 +1154,50 @@ extern "C" int gad_class_loss_workspace_bytes(const gad_class_loss_args* args, s
     return GAD_OK;
 }
 
-extern "C" int gad_class_loss(const gad_class_loss_args* args, void* workspace, size_t workspace_bytes, void* stream) {
-    using namespace gad;
-    const int rc = check_class(args);
-    if (rc != GAD_OK) return rc;
-    const gad_class_loss_args& a = *args;
+namespace gad {
+namespace {
+
+int run_loss(const gad_class_loss_args& a, const gad_policy_loss_args* policy, void* workspace, size_t workspace_bytes, void* stream) {
     if (!a.W || !a.loss || !a.status) return GAD_ERR_ARG;
     const cudaStream_t s = (cudaStream_t)stream;
     if (a.rows == 0) return a.dtype == GAD_F32 ? run_empty<float>(a, s) : a.dtype == GAD_F16 ? run_empty<__half>(a, s) : run_empty<__nv_bfloat16>(a, s);
     if (!a.H || !a.row_loss || (a.k == 0 && !a.labels) || (a.k > 0 && (!a.target_classes || !a.teacher))) return GAD_ERR_ARG;
-    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < (size_t)plan_class(a).total) return GAD_ERR_OOM;
+    if (policy && (!policy->old_logp || !policy->advantages || !policy->logp)) return GAD_ERR_ARG;
+    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < (size_t)plan_class(a, policy != nullptr).total) return GAD_ERR_OOM;
     try {
-        return a.dtype == GAD_F32 ? run_class<float>(a, (uint8_t*)workspace, s) : a.dtype == GAD_F16 ? run_class<__half>(a, (uint8_t*)workspace, s) : run_class<__nv_bfloat16>(a, (uint8_t*)workspace, s);
+        uint8_t* ws = (uint8_t*)workspace;
+        return a.dtype == GAD_F32 ? run_class<float>(a, policy, ws, s) : a.dtype == GAD_F16 ? run_class<__half>(a, policy, ws, s) : run_class<__nv_bfloat16>(a, policy, ws, s);
     } catch (...) {   // (the table of configured kernels could not grow)
         return GAD_ERR_OOM;
     }
+}
+
+int check_policy(const gad_policy_loss_args* a) {
+    if (!a) return GAD_ERR_ARG;
+    const int rc = check_class(&a->head);
+    if (rc != GAD_OK) return rc;
+    if (a->head.k != 0 || (a->head.rows > 0 && !a->head.labels)) return GAD_ERR_ARG;
+    if (!(a->clip_low >= 0.f && a->clip_low <= 1.f) || !(a->clip_high >= 0.f) || !(a->kl_weight >= 0.f) || !std::isfinite(a->kl_weight)) return GAD_ERR_ARG;
+    return GAD_OK;
+}
+
+}  // namespace
+}  // namespace gad
+
+extern "C" int gad_class_loss(const gad_class_loss_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = gad::check_class(args);
+    return rc != GAD_OK ? rc : gad::run_loss(*args, nullptr, workspace, workspace_bytes, stream);
+}
+
+extern "C" int gad_policy_loss_workspace_bytes(const gad_policy_loss_args* args, size_t* bytes) {
+    const int rc = gad::check_policy(args);
+    if (rc != GAD_OK) return rc;
+    if (!bytes) return GAD_ERR_ARG;
+    *bytes = args->head.rows == 0 ? 0 : (size_t)gad::plan_class(args->head, true).total;
+    return GAD_OK;
+}
+
+extern "C" int gad_policy_loss(const gad_policy_loss_args* args, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = gad::check_policy(args);
+    return rc != GAD_OK ? rc : gad::run_loss(args->head, args, workspace, workspace_bytes, stream);
 }

@@ -1,5 +1,5 @@
 """Operators of an output head on CUDA tensors the caller owns (no context): layer norm and its backward pass, the softmax cross entropy
-of an output layer with many classes, and distillation from a teacher's top logits.
+of an output layer with many classes, distillation from a teacher's top logits, and the clipped policy loss of actions among the classes.
 
 Like the rest of the binding this is argument checking and marshalling; the work is the library's kernels (``include/gad.h``).
 Every call enqueues on ``stream`` (default: torch's current stream of the tensors' device) and does not wait.  Outputs and
@@ -30,6 +30,11 @@ class _ClassLossArgs(C.Structure):
                 ("db", C.c_void_p), ("status", C.c_void_p)]
 
 
+class _PolicyLossArgs(C.Structure):
+    _fields_ = [("head", _ClassLossArgs), ("old_logp", C.c_void_p), ("advantages", C.c_void_p), ("ref_logp", C.c_void_p), ("clip_low", C.c_float), ("clip_high", C.c_float),
+                ("kl_weight", C.c_float), ("logp", C.c_void_p)]
+
+
 def _load():
     global _lib, torch
     if _lib is None:
@@ -41,6 +46,8 @@ def _load():
         L.gad_layer_norm_backward.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp, i32, vp, vp, vp, i64, vp, vp, vp, C.c_size_t, vp]
         L.gad_class_loss_workspace_bytes.argtypes = [C.POINTER(_ClassLossArgs), C.POINTER(C.c_size_t)]
         L.gad_class_loss.argtypes = [C.POINTER(_ClassLossArgs), vp, C.c_size_t, vp]
+        L.gad_policy_loss_workspace_bytes.argtypes = [C.POINTER(_PolicyLossArgs), C.POINTER(C.c_size_t)]
+        L.gad_policy_loss.argtypes = [C.POINTER(_PolicyLossArgs), vp, C.c_size_t, vp]
         _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
         _lib = L
     return _lib
@@ -182,12 +189,31 @@ class ClassLoss(NamedTuple):
 
     def check(self):
         """Waits for the result; raises GAD_ERR_DEVICE_TIMEOUT if a bounded wait ran out, GAD_ERR_NONFINITE if the loss is not finite."""
-        code = int(self.status.item())
-        if code:
-            raise GadError(-7, "wait %d ran out" % code)
-        if not bool(self.loss.isfinite().item()):
-            raise GadError(-6, "the loss is not finite")
-        return self
+        return _check_loss(self)
+
+
+class PolicyLoss(NamedTuple):
+    """What ``policy_loss`` returns: as ``ClassLoss``, and ``logp`` float32 [rows], the actions' log-probabilities (zero where a row does not count)."""
+    loss: "object"
+    row_loss: "object"
+    logp: "object"
+    dH: Optional["object"]
+    dW: Optional["object"]
+    db: Optional["object"]
+    status: "object"
+
+    def check(self):
+        """Waits for the result; raises GAD_ERR_DEVICE_TIMEOUT if a bounded wait ran out, GAD_ERR_NONFINITE if the loss is not finite."""
+        return _check_loss(self)
+
+
+def _check_loss(r):
+    code = int(r.status.item())
+    if code:
+        raise GadError(-7, "wait %d ran out" % code)
+    if not bool(r.loss.isfinite().item()):
+        raise GadError(-6, "the loss is not finite")
+    return r
 
 
 def _indices(t, name, shape, device):
@@ -197,7 +223,8 @@ def _indices(t, name, shape, device):
     return t.data_ptr(), t.element_size()
 
 
-def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, row_weights, mean, scale, grads, stream):
+def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, row_weights, mean, scale, grads, stream, policy=None):
+    """policy: None, or (old_logp, advantages, ref_logp, clip_low, clip_high, kl_weight)."""
     L = _load()
     ldh = _matrix(H, "H")
     N, D = H.shape
@@ -224,13 +251,15 @@ def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, 
         if not (teacher.is_cuda and teacher.device == dev and teacher.dtype in _DTYPES and tuple(teacher.shape) == (N, k) and teacher.is_contiguous()):
             raise GadError(-1, "teacher must be a contiguous floating tensor of the shape of classes on the same device")
         te, te_type = teacher.data_ptr(), _DTYPES[teacher.dtype]
+    if policy is not None:
+        of_rows = [_vector(t, name, N, (torch.float32,), dev) for t, name in zip(policy[:3], ("old_logp", "advantages", "ref_logp"))]
     want = {"H", "W", "b"} if grads is True else set() if not grads else set(grads)
     if not want <= {"H", "W", "b"}:
         raise GadError(-1, "grads is True, False or some of H, W and b")
     if _elsewhere(dev, stream):
         with _switch(dev, stream):
-            return _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, row_weights, mean, scale, grads, None)
-    out = H.new_empty(N + 1, dtype=torch.float32)
+            return _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, row_weights, mean, scale, grads, None, policy)
+    out = H.new_empty(N + 1 if policy is None else 2 * N + 1, dtype=torch.float32)
     status = H.new_empty(1, dtype=torch.int32)
     dH = H.new_empty((N, D)) if "H" in want else None
     dW = W.new_empty((V, D)) if "W" in want else None
@@ -240,6 +269,12 @@ def _class_loss(H, W, labels, classes, teacher, temperature, hard_weight, bias, 
                        hard_weight, w, scale, 1 if mean else 0, at + 4 * N, at, dH.data_ptr() if dH is not None else None, D,
                        dW.data_ptr() if dW is not None else None, D, db.data_ptr() if db is not None else None, status.data_ptr())
     nbytes = C.c_size_t(0)
+    if policy is not None:
+        a = _PolicyLossArgs(a, *of_rows, *policy[3:], at + 4 * (N + 1))
+        _ck(L.gad_policy_loss_workspace_bytes(C.byref(a), C.byref(nbytes)), "gad_policy_loss")
+        ws = H.new_empty(nbytes.value, dtype=torch.uint8)
+        _ck(L.gad_policy_loss(C.byref(a), ws.data_ptr(), nbytes.value, _stream(dev)), "gad_policy_loss")
+        return PolicyLoss(out[N:N + 1], out[:N], out[N + 1:], dH, dW, db, status)
     _ck(L.gad_class_loss_workspace_bytes(C.byref(a), C.byref(nbytes)), "gad_class_loss")
     ws = H.new_empty(nbytes.value, dtype=torch.uint8)     # (torch's blocks start on 512 bytes)
     _ck(L.gad_class_loss(C.byref(a), ws.data_ptr(), nbytes.value, _stream(dev)), "gad_class_loss")
@@ -267,3 +302,16 @@ def distill_loss(H, W, classes, teacher, *, temperature=1.0, labels=None, hard_w
     if classes is None or teacher is None:
         raise GadError(-1, "classes and teacher are needed")
     return _class_loss(H, W, labels, classes, teacher, temperature, hard_weight if labels is not None else 0.0, bias, row_weights, mean, scale, grads, stream)
+
+
+def policy_loss(H, W, actions, old_logp, advantages, *, ref_logp=None, clip=0.2, kl_weight=0.0, bias=None, row_weights=None, mean=True, scale=1.0, grads=True, stream=None):
+    """gad_policy_loss: the clipped policy loss of actions chosen among the classes of z = H W^T + bias, with a KL term towards a reference policy.
+
+    With lp the log-probability of a row's action and r = exp(lp - old_logp), row_loss = -min(r A, clip(r, 1 - low, 1 + high) A) + kl_weight (exp(ref_logp - lp) -
+    (ref_logp - lp) - 1).  actions as ``class_loss``'s labels (below zero: the row does not count); old_logp, advantages and ref_logp float32 [rows] (without ref_logp there is no
+    KL term); clip: one number, or (low, high) with high up to infinity.  Everything else as in ``class_loss``.  Returns a ``PolicyLoss``, whose ``logp`` a later call may be given as
+    ``old_logp``; for the log-probabilities alone: ``-class_loss(H, W, actions, grads=False).row_loss``."""
+    if actions is None or old_logp is None or advantages is None:
+        raise GadError(-1, "actions, old_logp and advantages are needed")
+    low, high = clip if isinstance(clip, (tuple, list)) else (clip, clip)
+    return _class_loss(H, W, actions, None, None, 1.0, 1.0, bias, row_weights, mean, scale, grads, stream, (old_logp, advantages, ref_logp, low, high, kl_weight))
