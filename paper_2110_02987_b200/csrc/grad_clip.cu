@@ -1,11 +1,11 @@
 // The norm over all gradients of a program, n = sqrt(sum g^2), and the gradients scaled by f = min(1, max_norm / n), in place or into tensors of their own.
 //
 // Two launches for up to 440 tensors.  The list of tensors is a parameter of the kernels, so nothing is copied to the device beforehand and a captured graph holds it.  Tensors are cut
-// into chunks of 8192 values; block b takes chunks b, b + blocks, ... and leaves one sum (grad_squares_kernel).  Every block of the second launch adds those sums up
+// into chunks of 8192 or 32 768 values; block b takes chunks b, b + blocks, ... and leaves one sum (grad_squares_kernel).  Every block of the second launch adds those sums up
 // itself, in the same order (a ticket for the last block would have to be cleared beforehand: a launch more), and scales its chunks, the last first: those the L2 still holds.
 // Bound by HBM: the gradients are read twice, as far as the L2 does not hold them, and written once.
 //
-// Sums of squares are fp32 over the values of a chunk a thread has (32 of them), fp64 above.  A thread's sum outside 2^-80 .. 2^100 is taken again in fp64, so no
+// Sums of squares are fp32 over the values of a chunk a thread has (two sums of 64 at most), fp64 above.  A thread's sum outside 2^-80 .. 2^100 is taken again in fp64, so no
 // square over- or underflows; whether a sum of zero is one of zeros shows in the values' bits.
 #include <algorithm>
 #include <cmath>
@@ -18,7 +18,8 @@ namespace gad {
 
 namespace {
 
-constexpr int kChunkValues = 8192, kClipThreads = 256;
+constexpr int kClipThreads = 256;
+constexpr int kSmallChunk = 8192, kLargeChunk = 32768;    // values
 constexpr int kClipBlocks = 592;                         // four a multiprocessor: 1024 threads, 4 x 16 bytes on their way each
 
 struct ClipEntry {
@@ -29,7 +30,7 @@ struct ClipEntry {
     int rows_per, pieces;                                // rows a chunk has, or pieces a row has
     int wide;                                            // every row of both starts on 16 bytes
 };
-template <int MOST> struct ClipTable { ClipEntry e[MOST]; int n, chunks; };
+template <int MOST> struct ClipTable { ClipEntry e[MOST]; int n, chunks, values; };   // values: of a chunk
 
 // A chunk: `rows` rows of `cols` values.
 struct ClipChunk { long long row, col; int rows, cols; };
@@ -44,9 +45,9 @@ __device__ __forceinline__ const ClipEntry& find_chunk(const ClipTable<MOST>& t,
     const long long i = c - e.first;
     if (e.pieces > 1) {
         k.row = i / e.pieces;
-        k.col = (i - k.row * e.pieces) * kChunkValues;
+        k.col = (i - k.row * e.pieces) * t.values;
         k.rows = 1;
-        k.cols = (int)min((long long)kChunkValues, e.cols - k.col);
+        k.cols = (int)min((long long)t.values, e.cols - k.col);
     } else {
         k.row = i * e.rows_per;
         k.col = 0;
@@ -56,48 +57,116 @@ __device__ __forceinline__ const ClipEntry& find_chunk(const ClipTable<MOST>& t,
     return e;
 }
 
-// This thread's values of a chunk: f(row of the chunk, column, values) for vectors of 16 bytes (VEC) or one value.  A warp has a row, or, of rows narrower than 32 vectors, a part of one.
+// A thread's vectors of a chunk (16 bytes, or one value: VEC = 1), kAhead of them at a time: all are loaded before the first is used, since a store may be to where the next load is from.
+constexpr int kAhead = 8;
 template <int VEC, class F>
-__device__ __forceinline__ void each_vector(const ClipChunk& k, F f) {
+__device__ __forceinline__ void each_vectors(const ClipChunk& k, F f) {
     const int n = (k.cols + VEC - 1) / VEC, total = n * k.rows;
-    if (k.rows == 1) {
-#pragma unroll 4
-        for (int i = threadIdx.x; i < n; i += kClipThreads) f(0, i * VEC);
-    } else {
-#pragma unroll 4
-        for (int i = threadIdx.x; i < total; i += kClipThreads) { const int r = i / n; f(r, (i - r * n) * VEC); }
+    for (int i0 = threadIdx.x; i0 < total; i0 += kAhead * kClipThreads) {
+        int r[kAhead], c[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int i = i0 + j * kClipThreads;
+            r[j] = k.rows == 1 ? 0 : i / n;
+            c[j] = i < total ? (i - r[j] * n) * VEC : k.cols;             // (behind the end of a row: nothing)
+        }
+        f(r, c);
     }
 }
 
 template <class T, int VEC>
 __device__ __forceinline__ double chunk_squares(const ClipEntry& e, const ClipChunk& k) {
     const T* base = reinterpret_cast<const T*>(e.g) + k.row * e.ld + k.col;
-    float s = 0.f;
+    float s[2] = {0.f, 0.f};
     uint32_t bits = 0;
-    each_vector<VEC>(k, [&](int r, int c) {
-        RowVec<T, VEC> raw;
-        load_raw<T, VEC>(base + r * e.ld, c, k.cols, raw);
-        float v[VEC];
-        if constexpr (VEC > 1) {
-            unpack_vec<T, VEC>(raw.u, v);
-            bits |= raw.u.x | raw.u.y | raw.u.z | raw.u.w;
-        } else {
-            v[0] = to_float(raw.e[0]);
-            bits |= __float_as_uint(v[0]);
-        }
+    each_vectors<VEC>(k, [&](const int (&r)[kAhead], const int (&c)[kAhead]) {
+        RowVec<T, VEC> raw[kAhead];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) s = fmaf(v[j], v[j], s);
+        for (int j = 0; j < kAhead; ++j) load_raw<T, VEC>(base + r[j] * e.ld, c[j], k.cols, raw[j]);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            float v[VEC];
+            if constexpr (VEC > 1) {
+                unpack_vec<T, VEC>(raw[j].u, v);
+                bits |= raw[j].u.x | raw[j].u.y | raw[j].u.z | raw[j].u.w;
+            } else {
+                v[0] = to_float(raw[j].e[0]);
+                bits |= __float_as_uint(v[0]);
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s[j & 1] = fmaf(v[i], v[i], s[j & 1]);
+        }
     });
-    if (s >= 0x1p-80f && s <= 0x1p100f) return s;
+    const float both = s[0] + s[1];
+    if (both >= 0x1p-80f && both <= 0x1p100f) return both;
     if ((bits & (sizeof(T) == 4 || VEC == 1 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0) return 0.0;
     double d = 0.0;
-    each_vector<VEC>(k, [&](int r, int c) {
-        for (int j = 0; j < VEC && c + j < k.cols; ++j) { const double v = to_float(base[r * e.ld + c + j]); d = fma(v, v, d); }
+    each_vectors<VEC>(k, [&](const int (&r)[kAhead], const int (&c)[kAhead]) {
+        for (int j = 0; j < kAhead; ++j)
+            for (int i = 0; i < VEC && c[j] + i < k.cols; ++i) { const double v = to_float(base[r[j] * e.ld + c[j] + i]); d = fma(v, v, d); }
+    });
+    return d;
+}
+// Rows that start anywhere: a warp has up to kRun values of a row at a time, single ones up to the first and from the last 16-byte boundary on, vectors between.  (A value a lane, with a
+// division for its place, took 92 us for the norm of clip-sized 60 million values of three types, half of them in such rows, and 177 us for scaling them into fp32; now 57 and 120.)
+constexpr int kRun = 2048, kLeastRun = 128;
+template <class F>
+__device__ __forceinline__ void each_run(const ClipChunk& k, F f) {
+    const int per = (k.cols + kRun - 1) / kRun, n = per * k.rows;
+    for (int i = threadIdx.x >> 5; i < n; i += kClipThreads / 32) {
+        const int r = per == 1 ? i : i / per, c = (i - r * per) * kRun;
+        f(r, c, min(kRun, k.cols - c));
+    }
+}
+template <class T> __device__ __forceinline__ int values_to_16(const T* p) { return (int)((16 - ((uintptr_t)p & 15)) & 15) / (int)sizeof(T); }
+
+template <class T>
+__device__ __forceinline__ double run_squares(const ClipEntry& e, const ClipChunk& k) {
+    constexpr int VEC = 16 / sizeof(T), U = 4;
+    const T* base = reinterpret_cast<const T*>(e.g) + k.row * e.ld + k.col;
+    const int lane = threadIdx.x & 31;
+    float s[2] = {0.f, 0.f};
+    uint32_t some = 0;                                   // any bit of a value but its sign
+    const auto one = [&](const T* p) { const float v = to_float(*p); some |= __float_as_uint(v) & 0x7FFFFFFFu; s[0] = fmaf(v, v, s[0]); };
+    each_run(k, [&](int r, int c, int len) {
+        const T* p = base + r * e.ld + c;
+        const int head = min(len, values_to_16(p)), nv = (len - head) / VEC, tail = head + nv * VEC;
+        const uint4* q = reinterpret_cast<const uint4*>(p + head);
+        if (lane < head) one(p + lane);
+        if (tail + lane < len) one(p + tail + lane);
+        for (int i = lane; i < nv; i += 32 * U) {
+            uint4 u[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) u[j] = i + 32 * j < nv ? q[i + 32 * j] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                float v[VEC];
+                unpack_vec<T, VEC>(u[j], v);
+                some |= (u[j].x | u[j].y | u[j].z | u[j].w) & (sizeof(T) == 4 ? 0x7FFFFFFFu : 0x7FFF7FFFu);
+#pragma unroll
+                for (int x = 0; x < VEC; ++x) s[j & 1] = fmaf(v[x], v[x], s[j & 1]);
+            }
+        }
+    });
+    const float both = s[0] + s[1];
+    if (both >= 0x1p-80f && both <= 0x1p100f) return both;
+    if (some == 0) return 0.0;
+    double d = 0.0;
+    each_run(k, [&](int r, int c, int len) {
+        const T* p = base + r * e.ld + c;
+        const int head = min(len, values_to_16(p)), nv = (len - head) / VEC, tail = head + nv * VEC;
+        const auto more = [&](int i) { const double v = to_float(p[i]); d = fma(v, v, d); };
+        if (lane < head) more(lane);
+        if (tail + lane < len) more(tail + lane);
+        for (int i = lane; i < nv; i += 32)
+            for (int x = 0; x < VEC; ++x) more(head + i * VEC + x);
     });
     return d;
 }
 template <class T>
-__device__ __forceinline__ double chunk_squares(const ClipEntry& e, const ClipChunk& k) { return e.wide ? chunk_squares<T, 16 / (int)sizeof(T)>(e, k) : chunk_squares<T, 1>(e, k); }
+__device__ __forceinline__ double any_squares(const ClipEntry& e, const ClipChunk& k) {
+    return e.wide ? chunk_squares<T, 16 / (int)sizeof(T)>(e, k) : k.cols >= kLeastRun ? run_squares<T>(e, k) : chunk_squares<T, 1>(e, k);
+}
 
 __device__ __forceinline__ double block_sum(double s, double* sm) {
 #pragma unroll
@@ -118,7 +187,7 @@ __global__ void __launch_bounds__(kClipThreads) grad_squares_kernel(const __grid
     for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         ClipChunk k;
         const ClipEntry& e = find_chunk(t, c, k);
-        s += e.type == GAD_F32 ? chunk_squares<float>(e, k) : e.type == GAD_F16 ? chunk_squares<__half>(e, k) : chunk_squares<__nv_bfloat16>(e, k);
+        s += e.type == GAD_F32 ? any_squares<float>(e, k) : e.type == GAD_F16 ? any_squares<__half>(e, k) : any_squares<__nv_bfloat16>(e, k);
     }
     s = block_sum(s, sm);
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
@@ -128,44 +197,105 @@ template <class T, class O, int VEC>
 __device__ __forceinline__ void scale_chunk(const ClipEntry& e, const ClipChunk& k, float f) {
     const T* src = reinterpret_cast<const T*>(e.g) + k.row * e.ld + k.col;
     O* dst = reinterpret_cast<O*>(e.out) + k.row * e.out_ld + k.col;
-    each_vector<VEC>(k, [&](int r, int c) {
-        RowVec<T, VEC> raw;
-        load_raw<T, VEC>(src + r * e.ld, c, k.cols, raw);
-        O* to = dst + r * e.out_ld;
-        if constexpr (std::is_same<T, O>::value) {
-            if (f == 1.f) {                              // a copy, to the bit: a product makes one NaN of all
-                if constexpr (VEC > 1) {
-                    if (c + VEC <= k.cols) { *reinterpret_cast<uint4*>(to + c) = raw.u; return; }
-                }
+    each_vectors<VEC>(k, [&](const int (&r)[kAhead], const int (&c)[kAhead]) {
+        RowVec<T, VEC> raw[kAhead];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (c + j < k.cols) to[c + j] = raw.e[j];
-                return;
+        for (int j = 0; j < kAhead; ++j) load_raw<T, VEC>(src + r[j] * e.ld, c[j], k.cols, raw[j]);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            O* to = dst + r[j] * e.out_ld;
+            if constexpr (std::is_same<T, O>::value) {
+                if (f == 1.f) {                          // a copy, to the bit: a product makes one NaN of all
+                    if constexpr (VEC > 1) {
+                        if (c[j] + VEC <= k.cols) { *reinterpret_cast<uint4*>(to + c[j]) = raw[j].u; continue; }
+                    }
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i)
+                        if (c[j] + i < k.cols) to[c[j] + i] = raw[j].e[i];
+                    continue;
+                }
+            }
+            float v[VEC];
+            if constexpr (VEC > 1) unpack_vec<T, VEC>(raw[j].u, v); else v[0] = to_float(raw[j].e[0]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] *= f;
+            if constexpr (VEC == 1) {
+                if (c[j] < k.cols) to[c[j]] = from_float<O>(v[0]);
+            } else if constexpr (sizeof(O) == sizeof(T)) store_vec<O, VEC>(to, c[j], k.cols, v);
+            else {
+                // 16-bit gradients into fp32: two vectors
+                const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+                store_vec<O, 4>(to, c[j], k.cols, a);
+                store_vec<O, 4>(to, c[j] + 4, k.cols, b);
             }
         }
-        float v[VEC];
-        if constexpr (VEC > 1) unpack_vec<T, VEC>(raw.u, v); else v[0] = to_float(raw.e[0]);
+    });
+}
+// Scaled values leave through shared memory (256 of a warp at a time), a value a lane, where the result does not start on 16 bytes when the gradient does.
+template <class T, class O>
+__device__ __forceinline__ void scale_runs(const ClipEntry& e, const ClipChunk& k, float f, O* __restrict__ buf) {
+    constexpr int VEC = 16 / sizeof(T), U = 4;
+    const T* src = reinterpret_cast<const T*>(e.g) + k.row * e.ld + k.col;
+    O* dst = reinterpret_cast<O*>(e.out) + k.row * e.out_ld + k.col;
+    const int lane = threadIdx.x & 31;
+    const bool copy = std::is_same<T, O>::value && f == 1.f;
+    each_run(k, [&](int r, int c, int len) {
+        const T* p = src + r * e.ld + c;
+        O* to = dst + r * e.out_ld + c;
+        const int head = min(len, values_to_16(p)), nv = (len - head) / VEC, tail = head + nv * VEC;
+        const uint4* q = reinterpret_cast<const uint4*>(p + head);
+        const bool vectors = ((uintptr_t)(to + head) & 15) == 0;
+        const auto one = [&](int i) {
+            if constexpr (std::is_same<T, O>::value) { if (copy) { to[i] = p[i]; return; } }
+            to[i] = from_float<O>(to_float(p[i]) * f);
+        };
+        if (lane < head) one(lane);
+        if (tail + lane < len) one(tail + lane);
+        for (int i0 = 0; i0 < nv; i0 += 32 * U) {
+            uint4 u[U];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) v[j] *= f;
-        if constexpr (VEC == 1) to[c] = from_float<O>(v[0]);
-        else if constexpr (sizeof(O) == sizeof(T)) store_vec<O, VEC>(to, c, k.cols, v);
-        else {
-            // 16-bit gradients into fp32: two vectors
-            float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
-            store_vec<O, 4>(to, c, k.cols, a);
-            store_vec<O, 4>(to, c + 4, k.cols, b);
+            for (int j = 0; j < U; ++j) u[j] = i0 + 32 * j + lane < nv ? q[i0 + 32 * j + lane] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const int first = i0 + 32 * j, n = (nv - first) * VEC;      // values of this and the following vectors
+                if (n <= 0) break;
+                union { uint4 q[sizeof(O) / sizeof(T)]; O v[VEC]; } w;
+                if (copy) w.q[0] = u[j];
+                else {
+                    float v[VEC];
+                    unpack_vec<T, VEC>(u[j], v);
+#pragma unroll
+                    for (int x = 0; x < VEC; ++x) w.v[x] = from_float<O>(v[x] * f);
+                }
+                if (vectors) {
+                    if (first + lane < nv)
+#pragma unroll
+                        for (int x = 0; x < (int)(sizeof(O) / sizeof(T)); ++x) reinterpret_cast<uint4*>(to + head + (first + lane) * VEC)[x] = w.q[x];
+                } else {
+                    __syncwarp();
+#pragma unroll
+                    for (int x = 0; x < (int)(sizeof(O) / sizeof(T)); ++x) reinterpret_cast<uint4*>(buf + lane * VEC)[x] = w.q[x];
+                    __syncwarp();
+#pragma unroll
+                    for (int x = 0; x < VEC; ++x)
+                        if (32 * x + lane < n) to[head + first * VEC + 32 * x + lane] = buf[32 * x + lane];
+                }
+            }
         }
     });
 }
 template <class T, class O>
-__device__ __forceinline__ void scale_chunk(const ClipEntry& e, const ClipChunk& k, float f) {
-    if (e.wide) scale_chunk<T, O, 16 / (int)sizeof(T)>(e, k, f); else scale_chunk<T, O, 1>(e, k, f);
+__device__ __forceinline__ void scale_any(const ClipEntry& e, const ClipChunk& k, float f, float* buf) {
+    if (e.wide) scale_chunk<T, O, 16 / (int)sizeof(T)>(e, k, f);
+    else if (k.cols >= kLeastRun) scale_runs<T, O>(e, k, f, reinterpret_cast<O*>(buf));
+    else scale_chunk<T, O, 1>(e, k, f);
 }
 
 // write: this launch writes the norm.
 template <int MOST>
 __global__ void __launch_bounds__(kClipThreads) grad_scale_kernel(const __grid_constant__ ClipTable<MOST> t, const double* __restrict__ sums, int nsums, float max_norm, float* __restrict__ norm, int write) {
     __shared__ double sm[kClipThreads / 32];
+    __shared__ __align__(16) float staging[kClipThreads / 32][256];
     pdl_next();
     pdl_wait();
     after_wait(sums);
@@ -175,15 +305,16 @@ __global__ void __launch_bounds__(kClipThreads) grad_scale_kernel(const __grid_c
     const double n = sqrt(s);
     const float nf = (float)n;
     if (write && blockIdx.x == 0 && threadIdx.x == 0) *norm = nf;
+    float* buf = staging[threadIdx.x >> 5];
     // a norm that is not finite (in fp32) leaves the gradients as they are
     const float f = nf > max_norm && isfinite(nf) ? (float)((double)max_norm / n) : 1.f;
     for (int c = t.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         ClipChunk k;
         const ClipEntry& e = find_chunk(t, c, k);
         if (!e.out || (f == 1.f && e.out == e.g)) continue;
-        if (e.type == GAD_F32) scale_chunk<float, float>(e, k, f);
-        else if (e.type == GAD_F16) { if (e.out_type == GAD_F32) scale_chunk<__half, float>(e, k, f); else scale_chunk<__half, __half>(e, k, f); }
-        else { if (e.out_type == GAD_F32) scale_chunk<__nv_bfloat16, float>(e, k, f); else scale_chunk<__nv_bfloat16, __nv_bfloat16>(e, k, f); }
+        if (e.type == GAD_F32) scale_any<float, float>(e, k, f, buf);
+        else if (e.type == GAD_F16) { if (e.out_type == GAD_F32) scale_any<__half, float>(e, k, f, buf); else scale_any<__half, __half>(e, k, f, buf); }
+        else { if (e.out_type == GAD_F32) scale_any<__nv_bfloat16, float>(e, k, f, buf); else scale_any<__nv_bfloat16, __nv_bfloat16>(e, k, f, buf); }
     }
 }
 
@@ -241,8 +372,9 @@ int check_regions(const gad_grad_tensor* t, int64_t count) {
 }
 
 template <int MOST>
-int fill_table(const gad_grad_tensor* t, int64_t& i, int64_t count, bool scaled, ClipTable<MOST>& table) {
+int fill_table(const gad_grad_tensor* t, int64_t& i, int64_t count, bool scaled, int values, ClipTable<MOST>& table) {
     table.n = 0;
+    table.values = values;
     int64_t chunks = 0;
     for (; i < count && table.n < MOST; ++i) {
         if (empty_tensor(t[i]) || (scaled && !t[i].out)) continue;
@@ -254,8 +386,8 @@ int fill_table(const gad_grad_tensor* t, int64_t& i, int64_t count, bool scaled,
         e.type = t[i].dtype; e.out_type = t[i].out_dtype;
         e.wide = ((uintptr_t)e.g % 16 == 0) && (rows == 1 || t[i].ld * a % 16 == 0);
         if (t[i].out) e.wide = e.wide && ((uintptr_t)e.out % 16 == 0) && (rows == 1 || t[i].out_ld * b % 16 == 0);
-        e.pieces = (int)((cols + kChunkValues - 1) / kChunkValues);
-        e.rows_per = e.pieces > 1 ? 1 : (int)std::min<int64_t>(rows, std::max<int64_t>(1, kChunkValues / cols));
+        e.pieces = (int)((cols + values - 1) / values);
+        e.rows_per = e.pieces > 1 ? 1 : (int)std::min<int64_t>(rows, std::max<int64_t>(1, values / cols));
         e.first = (int)chunks;
         const int64_t more = e.pieces > 1 ? rows * e.pieces : (rows + e.rows_per - 1) / e.rows_per;
         if (chunks + more > INT32_MAX / 2) { if (table.n == 0) return GAD_ERR_RANGE; break; }
@@ -271,10 +403,14 @@ int blocks_for(int chunks) { return std::max(1, std::min(chunks, kClipBlocks)); 
 template <int MOST>
 int run_clip(const gad_grad_tensor* t, int64_t count, float max_norm, float* norm, double* sums, cudaStream_t s) {
     ClipTable<MOST> table;
+    int64_t all = 0;
+    for (int64_t i = 0; i < count; ++i) all += t[i].rows * t[i].cols;
+    // long chunks, so that a tensor is looked up less often, where every block still has several
+    const int values = all >= (int64_t)8 * kClipBlocks * kLargeChunk ? kLargeChunk : kSmallChunk;
     int nsums = 0;
     bool first = true;
     for (int64_t i = 0; i < count || first;) {
-        const int rc = fill_table(t, i, count, false, table);
+        const int rc = fill_table(t, i, count, false, values, table);
         if (rc != GAD_OK) return rc;
         const int blocks = blocks_for(table.chunks);
         if (chain(grad_squares_kernel<MOST>, dim3((unsigned)blocks), kClipThreads, 0, s, first, table, sums + nsums) != cudaSuccess) return GAD_ERR_CUDA;
@@ -283,7 +419,7 @@ int run_clip(const gad_grad_tensor* t, int64_t count, float max_norm, float* nor
     }
     bool write = true;
     for (int64_t i = 0; i < count || write;) {
-        const int rc = fill_table(t, i, count, true, table);
+        const int rc = fill_table(t, i, count, true, values, table);
         if (rc != GAD_OK) return rc;
         if (!table.chunks && !write) break;
         if (chain(grad_scale_kernel<MOST>, dim3((unsigned)blocks_for(table.chunks)), kClipThreads, 0, s, false, table, (const double*)sums, nsums, max_norm, norm, (int)write) != cudaSuccess) return GAD_ERR_CUDA;

@@ -86,9 +86,14 @@ def _clip(grads, max_norm, out, stream):
     dev = pairs[0][0].device
     if dev.type != "cuda":
         raise GadError(-1, "gradients must be float32, float16 or bfloat16 CUDA tensors on one device")
-    values = []
+    values, types = [], head._DTYPES
     for g, o in pairs:
-        values += _entry(g, o, dev, head._DTYPES)
+        t = types.get(g.dtype)
+        if t is not None and (o is g or (o is not None and o.dtype is g.dtype and o.shape == g.shape and o.device == dev and o.is_contiguous())) and g.device == dev and g.is_contiguous():
+            n = g.numel()                                        # (most are like this)
+            values += (g.data_ptr(), t, t, 1, n, n, o.data_ptr(), n)
+        else:
+            values += _entry(g, o, dev, types)
     if not max_norm >= 0:
         raise GadError(-1, "max_norm must be 0 or more")
     if _elsewhere(dev, stream):
