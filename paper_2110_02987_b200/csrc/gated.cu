@@ -12,6 +12,7 @@
 #include <atomic>
 
 #include "gated_gemm.cuh"
+#include "gated_skinny.cuh"
 #include "operand_pack.cuh"
 
 namespace gad {
@@ -182,9 +183,28 @@ GatedArgs product(int64_t M, int N, int64_t K, int width, int dtype, int planes,
     return g;
 }
 
+// Few rows: how a product is cut.  In units of a stage (16 KB of weights an SM, 0.37 us): a unit takes its stages and one to change over, a join about eight and its sums' way through the L2.
+struct SkinnyCut { int tiles, nkb, shares, kb_share; };
+SkinnyCut skinny_cut(int64_t rows, int n, int per_tile, int64_t K) {
+    SkinnyCut best{(n + per_tile - 1) / per_tile, (int)((K + CT_K - 1) / CT_K), 1, 0};
+    best.kb_share = best.nkb;
+    double least = 1e30;
+    const int sms = 2 * kPairs;
+    for (int want = 1; want <= std::min(best.nkb, 64); ++want) {
+        const int kb = (best.nkb + want - 1) / want, shares = (best.nkb + kb - 1) / kb;
+        if (shares != want) continue;
+        const double waves = (double)(((int64_t)best.tiles * shares + sms - 1) / sms);
+        const double cost = waves * (kb + 1) + (shares > 1 ? 8.0 + (double)shares * best.tiles * rows / (sms * 16) : 0.0);
+        if (cost < least) { least = cost; best.shares = shares; best.kb_share = kb; }
+    }
+    return best;
+}
+bool is_skinny(const gad_gated_args& a) { return a.dtype != GAD_F32 && !a.act && a.rows <= SK_MOST_ROWS; }
+
 struct ForwardPlan {
     Operand x, wg, wu, wd, h;
-    int64_t o_slots, total;
+    SkinnyCut gate, down;
+    int64_t o_slots, o_gate, total;
 };
 ForwardPlan plan_forward(const gad_gated_args& a) {
     ForwardPlan p{};
@@ -197,9 +217,52 @@ ForwardPlan plan_forward(const gad_gated_args& a) {
     const bool kept = a.h && a.dtype != GAD_F32;
     p.h = {kept ? a.h : nullptr, a.rows == 1 ? round_up(a.inner, 8) : a.ldh, a.rows, a.inner, !kept, 0, round_up(a.inner, 8)};
     if (!kept) p.h.at = room.take((a.dtype == GAD_F32 ? 6 : 2) * a.rows * p.h.ldp);
-    p.o_slots = room.take((int64_t)kPairs * CT_M * width_for(a.cols) * 4);
+    if (is_skinny(a)) {
+        p.gate = skinny_cut(a.rows, a.inner, 64, a.cols);
+        p.down = skinny_cut(a.rows, a.cols, SK_M, a.inner);
+        const auto parts = [&](const SkinnyCut& c) { return c.shares > 1 ? (int64_t)c.shares * c.tiles * a.rows * SK_M * 4 : 0; };
+        p.o_gate = room.take(parts(p.gate));
+        p.o_slots = room.take(parts(p.down));
+    } else {
+        p.o_slots = room.take((int64_t)kPairs * CT_M * width_for(a.cols) * 4);
+    }
     p.total = room.at;
     return p;
+}
+
+template <int USE, class T>
+cudaError_t go_skinny(const CUtensorMap& W0, const CUtensorMap& W1, const CUtensorMap& X, SkinnyArgs k, const SkinnyCut& c, float* parts, void* out, int64_t ldo, Sequence& q) {
+    const auto kernel = skinny_kernel<USE, T>;
+    const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), SK_SMEM, false);
+    if (e != cudaSuccess) return e;
+    k.tiles = c.tiles; k.nkb = c.nkb; k.shares = c.shares; k.kb_share = c.kb_share;
+    k.stages = std::min<int>(SK_MOST_STAGES, SK_RING / (SK_A + k.width * (CT_K * 2)));
+    k.clear = q.clear;
+    q.clear = false;
+    k.parts = c.shares > 1 ? parts : nullptr;
+    k.out = out; k.ldo = ldo;
+    GAD_TRY(q.launch(kernel, dim3((unsigned)std::min(2 * kPairs, c.tiles * c.shares)), SK_THREADS, SK_SMEM, W0, W1, X, k));
+    if (c.shares == 1) return cudaSuccess;
+    return q.launch(skinny_join_kernel<USE, T>, dim3((unsigned)((k.N + 255) / 256), (unsigned)k.rows), 256, 0, k, out, (long long)ldo);
+}
+
+// Few rows of 16-bit operands.
+template <class T>
+cudaError_t run_skinny(const gad_gated_args& a, const ForwardPlan& p, uint8_t* ws, Sequence& q) {
+    CUtensorMap W0, W1, X;
+    SkinnyArgs k{};
+    k.rows = (int)a.rows; k.width = (int)round_up(a.rows, 16); k.bf16 = a.dtype != GAD_F16; k.activation = a.activation; k.err = a.status;
+    k.N = a.inner;
+    k.early = !p.wg.pack && !p.wu.pack;
+    GAD_TRY(map_of(X, p.x, ws, 1, (uint32_t)k.width));
+    GAD_TRY(map_of(W0, p.wg, ws, 1, 64));
+    GAD_TRY(map_of(W1, p.wu, ws, 1, 64));
+    GAD_TRY((go_skinny<kGate, T>(W0, W1, X, k, p.gate, reinterpret_cast<float*>(ws + p.o_gate), ws + p.h.at, p.h.ldp, q)));
+    k.N = a.cols;
+    k.early = !p.wd.pack;
+    GAD_TRY(map_of(X, p.h, ws, 1, (uint32_t)k.width));
+    GAD_TRY(map_of(W0, p.wd, ws, 1, SK_M));
+    return go_skinny<kPlain, T>(W0, W0, X, k, p.down, reinterpret_cast<float*>(ws + p.o_slots), a.y, a.ldy, q);
 }
 
 template <class T>
@@ -208,6 +271,9 @@ cudaError_t run_forward(const gad_gated_args& a, uint8_t* ws, cudaStream_t s) {
     const int parts = a.dtype == GAD_F32 ? 3 : 1;
     Sequence q{s};
     GAD_TRY(pack<T>({&p.x, &p.wg, &p.wu, &p.wd}, ws, q));
+    if constexpr (sizeof(T) == 2) {
+        if (is_skinny(a)) { GAD_TRY(run_skinny<T>(a, p, ws, q)); return cudaGetLastError(); }
+    }
     CUtensorMap A, B0, B1;
     GatedArgs g = product(a.rows, a.inner, a.cols, 256, a.dtype, 1, 1, 16, a.status);
     g.t.tiles_n = (a.inner + CT_H - 1) / CT_H;

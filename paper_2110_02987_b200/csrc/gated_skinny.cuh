@@ -1,0 +1,267 @@
+// The products of the gated feed-forward block for few rows (serving: one token to a batch of 256), 16-bit operands: reading the weights is all that costs, so the weights are the
+// operand with many rows (128 rows of a tile, M of the instruction) and the rows of x or h the narrow one (N of the instruction, 16 to 256 in steps of 16).  As the tiles of
+// gated_gemm.cuh have it, 256 rows of x on the other side, a call of 48 rows mostly multiplies zeros and has too few tiles to read with.
+//   kGate      a tile is 64 rows of Wg and the same 64 of Wu: rows 0 .. 63 of the accumulator are g, 64 .. 127 u of the same units
+//   kPlain     128 rows of Wd
+// Each CTA by itself (cta_group::1) streams stages of 64 values of the reduction through a ring as deep as shared memory allows (16 rows: 12 stages of 18 KB, so that an SM has 190 KB on their
+// way).  Where there are too few tiles for all SMs the reduction is cut into shares, whose sums skinny_join_kernel adds up.
+// The second product's first weights are loaded before the wait for the first product: they fill the time in which the last tiles in front are drained.
+#pragma once
+
+#include "gated_gemm.cuh"
+
+namespace gad {
+
+namespace {
+
+constexpr int SK_M = 128, SK_THREADS = 192, SK_MOST_ROWS = 256;
+constexpr int SK_A = SK_M * CT_K * 2;                       // 16 KiB of weights a stage
+constexpr int SK_XCH = 32 * 64 * 4;                         // u of 32 rows on their way to the threads that have g
+constexpr int SK_MOST_STAGES = 12;
+constexpr int SK_SMEM = 227 * 1024;
+constexpr int SK_RING = SK_SMEM - 1024 - 512 - SK_XCH;
+
+struct SkinnyArgs {
+    int rows, width;           // rows of x; rounded up to the instruction's N
+    int N;                     // rows of the weights (kGate: of each)
+    int tiles, nkb, shares, kb_share;
+    int stages;
+    int early;                 // the weights are the caller's: they may be loaded before the kernel in front has ended
+    int bf16, activation, clear;
+    int32_t* err;
+    void* out; long long ldo;  // h or y, or null: sums to parts
+    float* parts;              // [shares x tiles][rows][128]
+};
+
+__device__ __forceinline__ void mma_f16_one(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "}\n" ::"r"(tmem_d),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// Whether ok is true in all 128 draining threads.
+__device__ __forceinline__ bool all_drain(bool ok) {
+    uint32_t r;
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.b32 p, %1, 0;\n"
+        "bar.red.and.pred q, 1, 128, p;\n"
+        "selp.b32 %0, 1, 0, q;\n"
+        "}\n"
+        : "=r"(r)
+        : "r"((uint32_t)ok)
+        : "memory");
+    return r != 0;
+}
+
+// A unit of work: a share of a tile.
+struct SkinnyAt { int tile, kb0, nkb; };
+__device__ __forceinline__ SkinnyAt skinny_at(const SkinnyArgs& a, int u) {
+    const int share = u / a.tiles;
+    SkinnyAt t;
+    t.tile = u - share * a.tiles;
+    t.kb0 = share * a.kb_share;
+    t.nkb = min(a.kb_share, a.nkb - t.kb0);
+    return t;
+}
+
+template <int USE, class T>
+__global__ void __launch_bounds__(SK_THREADS, 1)
+skinny_kernel(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ SkinnyArgs a) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;
+    uint8_t* sm = smem_raw + pad;
+    const uint32_t sm_addr = raw_addr + pad;
+    const uint32_t bars = sm_addr + SK_RING;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (SK_MOST_STAGES + s); };
+    auto tfull = [&](int i) { return bars + 8u * (2 * SK_MOST_STAGES + i); };
+    auto tempty = [&](int i) { return bars + 8u * (2 * SK_MOST_STAGES + 2 + i); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + SK_RING + 8 * (2 * SK_MOST_STAGES + 4));
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+    float* xch = reinterpret_cast<float*>(sm + SK_RING + 512);
+
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < a.stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(tfull(i), 1); mbar_init(tempty(i), 4); }
+        *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    pdl_next();
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(CT_TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = *tmem_slot;
+
+    const int units = a.tiles * a.shares;
+    const uint32_t stage_bytes = SK_A + (uint32_t)a.width * (CT_K * 2);
+    if (warp == 0) {
+        if (lane == 0) {
+            // ---------------- TMA producer ----------------
+            const auto load_w = [&](int s, const SkinnyAt& t, int kb) {
+                const uint32_t base = sm_addr + s * stage_bytes;
+                mbar_expect_tx(full(s), stage_bytes);
+                if (USE == kGate) {
+                    tma_load_3d(base, &tmW0, kb * CT_K, t.tile * 64, 0, full(s));
+                    tma_load_3d(base + SK_A / 2, &tmW1, kb * CT_K, t.tile * 64, 0, full(s));
+                } else {
+                    tma_load_3d(base, &tmW0, kb * CT_K, t.tile * SK_M, 0, full(s));
+                }
+            };
+            const auto load_x = [&](int s, int kb) { tma_load_3d(sm_addr + s * stage_bytes + SK_A, &tmX, kb * CT_K, 0, 0, full(s)); };
+            const SkinnyAt first = skinny_at(a, blockIdx.x);
+            const int ahead = a.early ? min(a.stages, first.nkb) : 0;
+            for (int i = 0; i < ahead; ++i) load_w(i, first, first.kb0 + i);
+            pdl_wait();
+            if (a.clear && blockIdx.x == 0) *a.err = 0;
+            for (int i = 0; i < ahead; ++i) load_x(i, first.kb0 + i);
+            int stage = ahead == a.stages ? 0 : ahead, done = ahead;
+            uint32_t phase = ahead == a.stages ? 1u : 0u;
+            bool ok = true;
+            for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+                const SkinnyAt t = skinny_at(a, u);
+                for (int kb = t.kb0 + done; kb < t.kb0 + t.nkb; ++kb) {
+                    if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, 51))) break;
+                    load_w(stage, t, kb);
+                    load_x(stage, kb);
+                    if (++stage == a.stages) { stage = 0; phase ^= 1u; }
+                }
+                done = 0;
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer: the whole warp runs the loop, one elected lane issues ----------------
+        int stage = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        const uint32_t idesc = instr_desc_f16(a.width, SK_M) | (a.bf16 ? (1u << 7) | (1u << 10) : 0u);
+        bool ok = true;
+        for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+            const int steps = skinny_at(a, u).nkb;
+            if (!(ok = __all_sync(0xffffffffu, mbar_wait(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 52)))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t d = tmem_base + (uint32_t)(acc * 256);
+            for (int i = 0; i < steps; ++i) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag, a.err, 53)))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t base = sm_addr + stage * stage_bytes;
+                const uint64_t da = smem_desc(base), db = smem_desc(base + SK_A);
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_one(d, da + 2 * ks, db + 2 * ks, idesc, i != 0 || ks != 0 ? 1u : 0u);
+                    mma_commit(empty(stage));
+                    if (i == steps - 1) mma_commit(tfull(acc));
+                }
+                __syncwarp();
+                if (++stage == a.stages) { stage = 0; phase ^= 1u; }
+            }
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+    } else {
+        // ---------------- drain: a row of the weights a lane, rows of x along the columns ----------------
+        const int q = warp & 3;
+        pdl_wait();
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        for (int u = blockIdx.x; u < units; u += gridDim.x) {
+            const SkinnyAt t = skinny_at(a, u);
+            // all four warps go on or none does: they meet at a barrier below
+            if (!all_drain(mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 56))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * 256);
+            const int unit_row = USE == kGate ? t.tile * 64 + (q & 1) * 32 + lane : t.tile * SK_M + q * 32 + lane;
+            const bool valid = unit_row < a.N;
+            for (int c0 = 0; c0 < a.rows; c0 += 32) {
+                float v[32];
+                __syncwarp();
+                tmem_ld32(at + (uint32_t)c0, v);
+                const int n = min(32, a.rows - c0);
+                if (a.parts) {
+                    float* out = a.parts + ((long long)u * a.rows + c0) * SK_M + q * 32 + lane;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < n) out[(long long)j * SK_M] = v[j];
+                } else if (USE == kGate) {
+                    if (q >= 2) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j < n) xch[j * 64 + (q & 1) * 32 + lane] = v[j];
+                    }
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                    if (q < 2) {
+                        T* out = reinterpret_cast<T*>(a.out) + (long long)c0 * a.ldo + unit_row;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j < n && valid) {
+                                float g, d;
+                                activation(a.activation, v[j], g, d);
+                                out[j * a.ldo] = from_float<T>(g * xch[j * 64 + (q & 1) * 32 + lane]);
+                            }
+                    }
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                } else {
+                    T* out = reinterpret_cast<T*>(a.out) + (long long)c0 * a.ldo + unit_row;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < n && valid) out[j * a.ldo] = from_float<T>(v[j]);
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(tempty(acc));
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+    }
+
+    // Tear-down: after a time-out loads in flight get a bounded chance to land.
+    __syncthreads();
+    if (*abort_flag && threadIdx.x == 0)
+        for (int s = 0; s < a.stages; ++s)
+            for (uint32_t i = 0; i < 4096u; ++i)
+                if (mbar_try_wait(full(s), 0) || mbar_try_wait(full(s), 1)) break;
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 0) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(CT_TMEM));
+    }
+}
+
+// Sums of shares added up in order: for kGate g and u, and h of them.  A thread a value of h or y.
+template <int USE, class T>
+__global__ void __launch_bounds__(256) skinny_join_kernel(const __grid_constant__ SkinnyArgs a, void* out, long long ldo) {
+    pdl_next();
+    pdl_wait();
+    const int c = blockIdx.x * 256 + threadIdx.x, n = blockIdx.y;
+    if (c >= a.N) return;
+    constexpr int PER = USE == kGate ? 64 : SK_M;
+    const float* p = a.parts + ((long long)(c / PER) * a.rows + n) * SK_M + c % PER;
+    const long long share = (long long)a.tiles * a.rows * SK_M;
+    float s = 0.f, v = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < a.shares; ++k) {
+        s += p[k * share];
+        if (USE == kGate) v += p[k * share + 64];
+    }
+    if (USE == kGate) {
+        float g, d;
+        activation(a.activation, s, g, d);
+        s = g * v;
+    }
+    reinterpret_cast<T*>(out)[n * ldo + c] = from_float<T>(s);
+}
+
+}  // namespace
+
+}  // namespace gad
