@@ -183,19 +183,22 @@ GatedArgs product(int64_t M, int N, int64_t K, int width, int dtype, int planes,
     return g;
 }
 
-// Few rows: how a product is cut.  In units of a stage (16 KB of weights an SM, 0.37 us): a unit takes its stages and one to change over, a join about eight and its sums' way through the L2.
-struct SkinnyCut { int tiles, nkb, shares, kb_share; };
-SkinnyCut skinny_cut(int64_t rows, int n, int per_tile, int64_t K) {
-    SkinnyCut best{(n + per_tile - 1) / per_tile, (int)((K + CT_K - 1) / CT_K), 1, 0};
-    best.kb_share = best.nkb;
+// Few rows: how a product is cut.  In units of a stage (16 KB of weights an SM, 0.37 us): a unit takes its stages, shorter by as many rows as a tile has fewer, and one to change over; a join takes about
+// eight, and its sums' way through the L2.  per: a multiple of 8 rows of a matrix, the swizzle's period (kGate: of two matrices).
+struct SkinnyCut { int per, tiles, nkb, shares, kb_share; };
+SkinnyCut skinny_cut(int64_t rows, int n, bool gate, int64_t K) {
+    const int sms = 2 * kPairs, nkb = (int)((K + CT_K - 1) / CT_K), each = gate ? 2 : 1;
+    SkinnyCut best{};
     double least = 1e30;
-    const int sms = 2 * kPairs;
-    for (int want = 1; want <= std::min(best.nkb, 64); ++want) {
-        const int kb = (best.nkb + want - 1) / want, shares = (best.nkb + kb - 1) / kb;
-        if (shares != want) continue;
-        const double waves = (double)(((int64_t)best.tiles * shares + sms - 1) / sms);
-        const double cost = waves * (kb + 1) + (shares > 1 ? 8.0 + (double)shares * best.tiles * rows / (sms * 16) : 0.0);
-        if (cost < least) { least = cost; best.shares = shares; best.kb_share = kb; }
+    for (int per = SK_M; per >= SK_M / 2; per -= 8 * each) {
+        const int tiles = (n + per / each - 1) / (per / each);
+        for (int want = 1; want <= std::min(nkb, 64); ++want) {
+            const int kb = (nkb + want - 1) / want, shares = (nkb + kb - 1) / kb;
+            if (shares != want) continue;
+            const double waves = (double)(((int64_t)tiles * shares + sms - 1) / sms);
+            const double cost = waves * (kb * (per / (double)SK_M) + 1) + (shares > 1 ? 8.0 + (double)shares * tiles * rows / (sms * 16) : 0.0);
+            if (cost < least) { least = cost; best = {per, tiles, nkb, shares, kb}; }
+        }
     }
     return best;
 }
@@ -218,8 +221,8 @@ ForwardPlan plan_forward(const gad_gated_args& a) {
     p.h = {kept ? a.h : nullptr, a.rows == 1 ? round_up(a.inner, 8) : a.ldh, a.rows, a.inner, !kept, 0, round_up(a.inner, 8)};
     if (!kept) p.h.at = room.take((a.dtype == GAD_F32 ? 6 : 2) * a.rows * p.h.ldp);
     if (is_skinny(a)) {
-        p.gate = skinny_cut(a.rows, a.inner, 64, a.cols);
-        p.down = skinny_cut(a.rows, a.cols, SK_M, a.inner);
+        p.gate = skinny_cut(a.rows, a.inner, true, a.cols);
+        p.down = skinny_cut(a.rows, a.cols, false, a.inner);
         const auto parts = [&](const SkinnyCut& c) { return c.shares > 1 ? (int64_t)c.shares * c.tiles * a.rows * SK_M * 4 : 0; };
         p.o_gate = room.take(parts(p.gate));
         p.o_slots = room.take(parts(p.down));
@@ -235,7 +238,7 @@ cudaError_t go_skinny(const CUtensorMap& W0, const CUtensorMap& W1, const CUtens
     const auto kernel = skinny_kernel<USE, T>;
     const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), SK_SMEM, false);
     if (e != cudaSuccess) return e;
-    k.tiles = c.tiles; k.nkb = c.nkb; k.shares = c.shares; k.kb_share = c.kb_share;
+    k.per = c.per; k.tiles = c.tiles; k.nkb = c.nkb; k.shares = c.shares; k.kb_share = c.kb_share;
     k.stages = std::min<int>(SK_MOST_STAGES, SK_RING / (SK_A + k.width * (CT_K * 2)));
     k.clear = q.clear;
     q.clear = false;
@@ -255,13 +258,13 @@ cudaError_t run_skinny(const gad_gated_args& a, const ForwardPlan& p, uint8_t* w
     k.N = a.inner;
     k.early = !p.wg.pack && !p.wu.pack;
     GAD_TRY(map_of(X, p.x, ws, 1, (uint32_t)k.width));
-    GAD_TRY(map_of(W0, p.wg, ws, 1, 64));
-    GAD_TRY(map_of(W1, p.wu, ws, 1, 64));
+    GAD_TRY(map_of(W0, p.wg, ws, 1, (uint32_t)p.gate.per / 2));
+    GAD_TRY(map_of(W1, p.wu, ws, 1, (uint32_t)p.gate.per / 2));
     GAD_TRY((go_skinny<kGate, T>(W0, W1, X, k, p.gate, reinterpret_cast<float*>(ws + p.o_gate), ws + p.h.at, p.h.ldp, q)));
     k.N = a.cols;
     k.early = !p.wd.pack;
     GAD_TRY(map_of(X, p.h, ws, 1, (uint32_t)k.width));
-    GAD_TRY(map_of(W0, p.wd, ws, 1, SK_M));
+    GAD_TRY(map_of(W0, p.wd, ws, 1, (uint32_t)p.down.per));
     return go_skinny<kPlain, T>(W0, W0, X, k, p.down, reinterpret_cast<float*>(ws + p.o_slots), a.y, a.ldy, q);
 }
 

@@ -1,10 +1,11 @@
 // The products of the gated feed-forward block for few rows (serving: one token to a batch of 256), 16-bit operands: reading the weights is all that costs, so the weights are the
 // operand with many rows (128 rows of a tile, M of the instruction) and the rows of x or h the narrow one (N of the instruction, 16 to 256 in steps of 16).  As the tiles of
 // gated_gemm.cuh have it, 256 rows of x on the other side, a call of 48 rows mostly multiplies zeros and has too few tiles to read with.
-//   kGate      a tile is 64 rows of Wg and the same 64 of Wu: rows 0 .. 63 of the accumulator are g, 64 .. 127 u of the same units
-//   kPlain     128 rows of Wd
-// Each CTA by itself (cta_group::1) streams stages of 64 values of the reduction through a ring as deep as shared memory allows (16 rows: 12 stages of 18 KB, so that an SM has 190 KB on their
-// way).  Where there are too few tiles for all SMs the reduction is cut into shares, whose sums skinny_join_kernel adds up.
+//   kGate      a tile is up to 64 rows of Wg and the same of Wu: rows 0 .. 63 of the accumulator are g, 64 .. 127 u of the same units
+//   kPlain     up to 128 rows of Wd
+// Each CTA by itself (cta_group::1) streams stages of 64 values of the reduction through a ring as deep as shared memory allows (16 rows: 11 stages of 18 KB, so that an SM has 180 KB on their
+// way).  Tiles have fewer rows where that deals them out more
+// evenly (8192 units: 147 tiles of 56 instead of 128 of 64), and where there are too few for all SMs the reduction is cut into shares, whose sums skinny_join_kernel adds up.
 // The second product's first weights are loaded before the wait for the first product: they fill the time in which the last tiles in front are drained.
 #pragma once
 
@@ -14,9 +15,11 @@ namespace gad {
 
 namespace {
 
-constexpr int SK_M = 128, SK_THREADS = 192, SK_MOST_ROWS = 256;
+constexpr int SK_M = 128, SK_MOST_ROWS = 256;
+constexpr int SK_GROUPS = 4;                                // of four draining warps (a quarter of the accumulator's rows each), in turn 16 rows of x each
+constexpr int SK_DRAIN = SK_GROUPS * 128, SK_THREADS = 64 + SK_DRAIN;
 constexpr int SK_A = SK_M * CT_K * 2;                       // 16 KiB of weights a stage
-constexpr int SK_XCH = 32 * 64 * 4;                         // u of 32 rows on their way to the threads that have g
+constexpr int SK_XCH = SK_GROUPS * 2 * 8 * 64 * 4;          // per group, g of eight rows and u of eight rows on their way to the threads that have the other
 constexpr int SK_MOST_STAGES = 12;
 constexpr int SK_SMEM = 227 * 1024;
 constexpr int SK_RING = SK_SMEM - 1024 - 512 - SK_XCH;
@@ -24,7 +27,7 @@ constexpr int SK_RING = SK_SMEM - 1024 - 512 - SK_XCH;
 struct SkinnyArgs {
     int rows, width;           // rows of x; rounded up to the instruction's N
     int N;                     // rows of the weights (kGate: of each)
-    int tiles, nkb, shares, kb_share;
+    int per, tiles, nkb, shares, kb_share;   // per: rows of the weights a tile has (kGate: half of them of each), at most 128
     int stages;
     int early;                 // the weights are the caller's: they may be loaded before the kernel in front has ended
     int bf16, activation, clear;
@@ -44,20 +47,30 @@ __device__ __forceinline__ void mma_f16_one(uint32_t tmem_d, uint64_t adesc, uin
         : "memory");
 }
 
-// Whether ok is true in all 128 draining threads.
+// Whether ok is true in all draining threads.
 __device__ __forceinline__ bool all_drain(bool ok) {
     uint32_t r;
     asm volatile(
         "{\n"
         ".reg .pred p, q;\n"
         "setp.ne.b32 p, %1, 0;\n"
-        "bar.red.and.pred q, 1, 128, p;\n"
+        "bar.red.and.pred q, 1, %2, p;\n"
         "selp.b32 %0, 1, 0, q;\n"
         "}\n"
         : "=r"(r)
-        : "r"((uint32_t)ok)
+        : "r"((uint32_t)ok), "n"(SK_DRAIN)
         : "memory");
     return r != 0;
+}
+// This warp's 32 tensor-memory lanes x 16 columns, complete on return.
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+        "tcgen05.wait::ld.sync.aligned;\n"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]),
+          "=f"(v[14]), "=f"(v[15])
+        : "r"(addr)
+        : "memory");
 }
 
 // A unit of work: a share of a tile.
@@ -91,7 +104,7 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < a.stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(tfull(i), 1); mbar_init(tempty(i), 4); }
+        for (int i = 0; i < 2; ++i) { mbar_init(tfull(i), 1); mbar_init(tempty(i), SK_DRAIN / 32); }
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -106,18 +119,18 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ 
     const uint32_t tmem_base = *tmem_slot;
 
     const int units = a.tiles * a.shares;
-    const uint32_t stage_bytes = SK_A + (uint32_t)a.width * (CT_K * 2);
+    const uint32_t stage_bytes = SK_A + (uint32_t)a.width * (CT_K * 2), loaded = (uint32_t)(a.per + a.width) * (CT_K * 2);
     if (warp == 0) {
         if (lane == 0) {
             // ---------------- TMA producer ----------------
             const auto load_w = [&](int s, const SkinnyAt& t, int kb) {
                 const uint32_t base = sm_addr + s * stage_bytes;
-                mbar_expect_tx(full(s), stage_bytes);
+                mbar_expect_tx(full(s), loaded);
                 if (USE == kGate) {
-                    tma_load_3d(base, &tmW0, kb * CT_K, t.tile * 64, 0, full(s));
-                    tma_load_3d(base + SK_A / 2, &tmW1, kb * CT_K, t.tile * 64, 0, full(s));
+                    tma_load_3d(base, &tmW0, kb * CT_K, t.tile * (a.per / 2), 0, full(s));
+                    tma_load_3d(base + SK_A / 2, &tmW1, kb * CT_K, t.tile * (a.per / 2), 0, full(s));
                 } else {
-                    tma_load_3d(base, &tmW0, kb * CT_K, t.tile * SK_M, 0, full(s));
+                    tma_load_3d(base, &tmW0, kb * CT_K, t.tile * a.per, 0, full(s));
                 }
             };
             const auto load_x = [&](int s, int kb) { tma_load_3d(sm_addr + s * stage_bytes + SK_A, &tmX, kb * CT_K, 0, 0, full(s)); };
@@ -170,51 +183,58 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ 
         }
     } else {
         // ---------------- drain: a row of the weights a lane, rows of x along the columns ----------------
-        const int q = warp & 3;
+        // (rows of the accumulator behind the tile's hold whatever the shared memory held: nothing of them is written)
+        const int q = warp & 3, group = (warp - 2) >> 2, half = a.per / 2;
+        float* xg = xch + group * 1024;
+        float* xu = xg + 512;
         pdl_wait();
         int acc = 0;
         uint32_t acc_phase = 0;
         for (int u = blockIdx.x; u < units; u += gridDim.x) {
             const SkinnyAt t = skinny_at(a, u);
-            // all four warps go on or none does: they meet at a barrier below
+            // all warps go on or none does: they meet at barriers below
             if (!all_drain(mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 56))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * 256);
-            const int unit_row = USE == kGate ? t.tile * 64 + (q & 1) * 32 + lane : t.tile * SK_M + q * 32 + lane;
-            const bool valid = unit_row < a.N;
-            for (int c0 = 0; c0 < a.rows; c0 += 32) {
-                float v[32];
+            const int local = USE == kGate ? (q & 1) * 32 + lane : q * 32 + lane;
+            const int unit_row = USE == kGate ? t.tile * half + local : t.tile * a.per + local;
+            const bool valid = local < (USE == kGate ? half : a.per) && unit_row < a.N;
+            for (int c0 = group * 16; c0 < a.rows; c0 += SK_GROUPS * 16) {
+                float v[16];
                 __syncwarp();
-                tmem_ld32(at + (uint32_t)c0, v);
-                const int n = min(32, a.rows - c0);
+                tmem_ld16(at + (uint32_t)c0, v);
+                const int n = min(16, a.rows - c0);
                 if (a.parts) {
                     float* out = a.parts + ((long long)u * a.rows + c0) * SK_M + q * 32 + lane;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (j < n) out[(long long)j * SK_M] = v[j];
+                    for (int j = 0; j < 16; ++j)
+                        if (j < n) out[j * SK_M] = v[j];
                 } else if (USE == kGate) {
-                    if (q >= 2) {
+                    // the threads that have g take the first eight rows, those that have u the others
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (j < n) xch[j * 64 + (q & 1) * 32 + lane] = v[j];
+                    for (int j = 0; j < 8; ++j) {
+                        if (q < 2) xg[j * 64 + local] = v[8 + j];
+                        else xu[j * 64 + local] = v[j];
                     }
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
-                    if (q < 2) {
-                        T* out = reinterpret_cast<T*>(a.out) + (long long)c0 * a.ldo + unit_row;
+                    asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory");
+                    const int first = q < 2 ? 0 : 8;
+                    T* out = reinterpret_cast<T*>(a.out) + (long long)(c0 + first) * a.ldo + unit_row;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (j < n && valid) {
-                                float g, d;
-                                activation(a.activation, v[j], g, d);
-                                out[j * a.ldo] = from_float<T>(g * xch[j * 64 + (q & 1) * 32 + lane]);
-                            }
+                    for (int j = 0; j < 8; ++j) {
+                        float g, d;
+                        activation(a.activation, q < 2 ? v[j] : xg[j * 64 + local], g, d);
+                        g *= q < 2 ? xu[j * 64 + local] : v[8 + j];
+                        if (first + j < n && valid) *out = from_float<T>(g);
+                        out += a.ldo;
                     }
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                    asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory");
                 } else {
                     T* out = reinterpret_cast<T*>(a.out) + (long long)c0 * a.ldo + unit_row;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (j < n && valid) out[j * a.ldo] = from_float<T>(v[j]);
+                    for (int j = 0; j < 16; ++j) {
+                        if (j < n && valid) *out = from_float<T>(v[j]);
+                        out += a.ldo;
+                    }
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -245,8 +265,8 @@ __global__ void __launch_bounds__(256) skinny_join_kernel(const __grid_constant_
     pdl_wait();
     const int c = blockIdx.x * 256 + threadIdx.x, n = blockIdx.y;
     if (c >= a.N) return;
-    constexpr int PER = USE == kGate ? 64 : SK_M;
-    const float* p = a.parts + ((long long)(c / PER) * a.rows + n) * SK_M + c % PER;
+    const int per = USE == kGate ? a.per / 2 : a.per;
+    const float* p = a.parts + ((long long)(c / per) * a.rows + n) * SK_M + c % per;
     const long long share = (long long)a.tiles * a.rows * SK_M;
     float s = 0.f, v = 0.f;
 #pragma unroll 4
