@@ -183,8 +183,10 @@ GatedArgs product(int64_t M, int N, int64_t K, int width, int dtype, int planes,
     return g;
 }
 
-// Few rows: how a product is cut.  In units of a stage (16 KB of weights an SM, 0.37 us): a unit takes its stages, shorter by as many rows as a tile has fewer, and one to change over; a join takes about
-// eight, and its sums' way through the L2.  per: a multiple of 8 rows of a matrix, the swizzle's period (kGate: of two matrices).
+// Few rows: how a product is cut.  In units of the time in which HBM gives every SM 16 KB (0.37 us): all weights once; or, where more, the stages of the SM that has most (0.45 each with few
+// rows, about 0.17 us: the latency of its loads over the stages of the ring; some of it shows in any case), or what all SMs take from the L2, rows of x or h again in every stage (at 1.7 times
+// HBM's rate).  To that a unit to change over, and four for a join beside its sums' way through the L2.  Fitted to a sweep of per and shares (512 x 1408 to 4096 x 16 384, 1 to 200 rows), where it stays within 5 % of
+// the best.  per: a multiple of 8 rows of a matrix, the swizzle's period (kGate: of two matrices).
 struct SkinnyCut { int per, tiles, nkb, shares, kb_share; };
 SkinnyCut skinny_cut(int64_t rows, int n, bool gate, int64_t K) {
     const int sms = 2 * kPairs, nkb = (int)((K + CT_K - 1) / CT_K), each = gate ? 2 : 1;
@@ -196,7 +198,8 @@ SkinnyCut skinny_cut(int64_t rows, int n, bool gate, int64_t K) {
             const int kb = (nkb + want - 1) / want, shares = (nkb + kb - 1) / kb;
             if (shares != want) continue;
             const double waves = (double)(((int64_t)tiles * shares + sms - 1) / sms);
-            const double cost = waves * (kb * (per / (double)SK_M) + 1) + (shares > 1 ? 8.0 + (double)shares * tiles * rows / (sms * 16) : 0.0);
+            const double stages = (double)tiles * nkb / sms / SK_M, width = (double)round_up(rows, 16), one = waves * kb * 0.45 * (1 + width / 256);
+            const double cost = std::max({stages * per, one, 0.6 * stages * (per + width)}) + 0.15 * one + waves + (shares > 1 ? 4.0 + (double)shares * tiles * rows / (sms * 32) : 0.0);
             if (cost < least) { least = cost; best = {per, tiles, nkb, shares, kb}; }
         }
     }
