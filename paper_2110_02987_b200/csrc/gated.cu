@@ -4,12 +4,13 @@
 //
 // Forward, two products: kGate leaves h (g and u never leave the chip), kPlain y.  For a backward pass kGate also leaves the two factors that dh is multiplied by there, act(g) and
 // u act'(g), instead of g and u: one rounding to the tensors' type each where g and u would bring theirs into every factor, and the backward pass has no activation to take again.
-// Backward: kHidden leaves dg and du, then three launches of kPlain: dx (one reduction over both), dWg and dWu, dWd.
+// Backward: kHidden leaves dg and du, and one launch of kPlain takes dx (one reduction over both), dWg and dWu, and dWd.
 //
 // Operands as in class_loss.cu: fp16 and bfloat16 as they are, fp32 in three bfloat16 parts with six products.  h, dg and du are operands of a second product, so they are rounded to
 // fp16 or bfloat16 (fp32: 24 bits): in norm the results' error grows by the square root of two over their own rounding.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "gated_gemm.cuh"
 #include "gated_skinny.cuh"
@@ -37,12 +38,16 @@ __global__ void __launch_bounds__(256) gated_pack_kernel(const __grid_constant__
     pack_row<T>(reinterpret_cast<const T*>(k.src) + row * k.ld, k.cols, true, k.dst, row * k.ldp, k.part_stride, threadIdx.x & 31, 32);
 }
 
-// The shares of the tiles that were cut along their reduction, added up in order: four columns a thread.
+// The shares of the tiles that were cut along their reduction, added up in order: four columns a thread, 1024 values a block.  first: blocks in front of each product's, and of all.
+struct JoinArgs { GatedArgs p[kGroup]; int first[kGroup + 1]; };
 template <class T>
-__global__ void __launch_bounds__(256) gated_join_kernel(const __grid_constant__ GatedArgs ga) {
+__global__ void __launch_bounds__(256) gated_join_kernel(const __grid_constant__ JoinArgs j) {
+    const int which = (int)blockIdx.x >= j.first[1] ? (int)blockIdx.x >= j.first[2] ? 2 : 1 : 0;
+    const GatedArgs& ga = j.p[which];
     const TileArgs& a = ga.t;
+    const int b = blockIdx.x - j.first[which];
     const int per_row = a.width / 4, rows = 256 / per_row, per_tile = CT_M / rows;
-    const int i = blockIdx.x / per_tile, r = blockIdx.x % per_tile * rows + threadIdx.x / per_row, x = threadIdx.x % per_row * 4;
+    const int i = b / per_tile, r = b % per_tile * rows + threadIdx.x / per_row, x = threadIdx.x % per_row * 4;
     pdl_next();
     pdl_wait();
     const TileAt t = tile_at(a, a.whole + (long long)i * a.shares);
@@ -57,8 +62,8 @@ __global__ void __launch_bounds__(256) gated_join_kernel(const __grid_constant__
     }
     T* out = reinterpret_cast<T*>(ga.C[plane]) + (long long)row * ga.ldc[plane] + c;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (c + j < a.N) out[j] = from_float<T>(s[j]);
+    for (int k = 0; k < 4; ++k)
+        if (c + k < a.N) out[k] = from_float<T>(s[k]);
 }
 
 template <class T>
@@ -102,46 +107,151 @@ struct Sequence {
     }
 };
 
-int width_for(int n) { return n <= 128 ? 128 : 256; }
-
 // Blocks of 64 terms that the tensor core adds up before the sum moves to registers: it cuts its accumulator off at every addition, 2^-23 of the sum every 16 terms at most (see
 // class_gemm_kernel).  As for the head's gradients: fp32 results 256 terms, 16-bit ones as many as cost an eighth of their rounding at most.
 template <class T> constexpr int kGatedChunk = 4;
 template <> constexpr int kGatedChunk<__half> = 128;
 template <> constexpr int kGatedChunk<__nv_bfloat16> = 1024;
 
-template <int USE, bool A_MN, bool B_MN, class T, bool ADD_UP>
-cudaError_t launch_gated(const CUtensorMap& A, const CUtensorMap& B0, const CUtensorMap& B1, const GatedArgs& g, Sequence& q) {
-    const auto kernel = gated_gemm_kernel<USE, A_MN, B_MN, T, ADD_UP>;
+// ---- sizes of products, and how their tiles are cut: the same for the workspace and the launches ----
+
+// One product: planes of M x N over K, in segs segments and pairs products of parts.
+struct Shape { int64_t M; int N; int64_t K; int planes, segs; };
+struct Cut { int width, tiles_m, tiles_n, nkb, whole, shares, kb_share; int64_t tiles() const { return (int64_t)tiles_m * tiles_n; } int64_t units() const { return whole + (tiles() - whole) * shares; } };
+
+// Tiles are 256 columns wide; narrow: 128, which take about three quarters of the time (their operands come from L2 half as fast again).
+Cut whole_tiles(const Shape& s, bool narrow) {
+    Cut c{};
+    c.width = narrow || s.N <= 128 ? 128 : 256;
+    c.tiles_m = s.planes * (int)((s.M + CT_M - 1) / CT_M);
+    c.tiles_n = (s.N + c.width - 1) / c.width;
+    c.nkb = (int)((s.K + CT_K - 1) / CT_K);
+    c.shares = 1;
+    c.kb_share = c.nkb;
+    c.whole = (int)c.tiles();
+    return c;
+}
+// kGate and kHidden: what is done with a finished tile is not additive, so tiles stay whole.  Narrow where their rounds are shorter all the same (22 wide tiles on 74 pairs: 44 narrow ones).
+Cut cut_alone(const Shape& s) {
+    const Cut wide = whole_tiles(s, false), narrow = whole_tiles(s, true);
+    const auto rounds = [](const Cut& c) { return (double)((c.tiles() + kPairs - 1) / kPairs); };
+    return 0.75 * rounds(narrow) < rounds(wide) && wide.tiles() < 8 * kPairs ? narrow : wide;
+}
+
+// Products whose results go as they are.  With three rounds of tiles and more, those of the last product that are left over when all pairs have had the same number are cut along their
+// reduction, down to 8 ring stages a share; with fewer, every tile is cut into shares of about the same number of stages, the number that lets the pair with most work finish first.
+constexpr int kMostUnits = 4 * kPairs;                    // of a launch whose tiles are cut
+void cut_group(const Shape* s, int n, int pairs, Cut* c) {
+    const auto stages = [&](int i, int kb) { return (int64_t)kb * pairs * s[i].segs; };
+    int64_t tiles = 0, units = 0;
+    for (int i = 0; i < n; ++i) {
+        c[i] = whole_tiles(s[i], false);
+        tiles += c[i].tiles();
+        units += c[i].tiles() * std::max<int64_t>(1, stages(i, c[i].nkb) / 8);
+    }
+    if (units < kPairs) {                                 // not even cut are there enough
+        tiles = 0;
+        for (int i = 0; i < n; ++i) { c[i] = whole_tiles(s[i], true); tiles += c[i].tiles(); }
+    }
+    const auto share = [&](int i, int want) {
+        c[i].kb_share = (c[i].nkb + want - 1) / want;
+        c[i].shares = (c[i].nkb + c[i].kb_share - 1) / c[i].kb_share;
+    };
+    if (tiles >= 3 * kPairs) {
+        const int i = n - 1;
+        const int64_t rest = std::min<int64_t>(tiles % kPairs, c[i].tiles());
+        if (!rest) return;
+        const int want = (int)std::min<int64_t>(kPairs / rest, stages(i, c[i].nkb) / 8);
+        if (want < 2) return;
+        share(i, want);
+        if (c[i].shares > 1) c[i].whole = (int)(c[i].tiles() - rest);
+        return;
+    }
+    int64_t longest = 0;
+    for (int i = 0; i < n; ++i) longest = std::max(longest, stages(i, c[i].nkb));
+    const auto share_all = [&](int64_t most) {             // units of at most so many stages; their number
+        int64_t units = 0;
+        for (int i = 0; i < n; ++i) {
+            share(i, (int)std::max<int64_t>(1, std::min<int64_t>((stages(i, c[i].nkb) + most - 1) / most, stages(i, c[i].nkb) / 8)));
+            units += c[i].tiles() * c[i].shares;
+        }
+        return units;
+    };
+    double least = 1e30;
+    int64_t best = longest;
+    for (int64_t most = longest; most >= 8; most = most * 3 / 4) {
+        if (share_all(most) > kMostUnits) break;
+        int load[kPairs] = {}, at = 0, top = 0;
+        for (int i = 0; i < n; ++i)
+            for (int64_t k = 0; k < c[i].tiles(); ++k)
+                for (int x = 0; x < c[i].shares; ++x) {
+                    load[at] += (int)stages(i, std::min(c[i].kb_share, c[i].nkb - x * c[i].kb_share)) + 4;
+                    top = std::max(top, load[at]);
+                    if (++at == kPairs) at = 0;
+                }
+        const double cost = top + (most < longest ? 12 : 0);
+        if (cost < least) { least = cost; best = most; }
+    }
+    share_all(best);
+    for (int i = 0; i < n; ++i)
+        if (c[i].shares > 1) c[i].whole = 0;
+}
+int64_t slot_bytes(const Cut& c) { return (c.tiles() - c.whole) * (c.shares > 1 ? c.shares : 0) * CT_M * c.width * 4; }
+
+GatedArgs product(const Shape& s, const Cut& c, int dtype, bool a_mn, int group, int32_t* status) {
+    GatedArgs g{};
+    g.parts = dtype == GAD_F32 ? 3 : 1;
+    g.segs = s.segs;
+    g.a_mn = a_mn;
+    g.plane_tiles = (int)((s.M + CT_M - 1) / CT_M);
+    g.t.M = (int)s.M; g.t.N = s.N;
+    g.t.tiles_m = c.tiles_m; g.t.tiles_n = c.tiles_n; g.t.width = c.width;
+    g.t.nkb = c.nkb; g.t.whole = c.whole; g.t.shares = c.shares; g.t.kb_share = c.kb_share;
+    g.t.group = group;
+    g.t.pairs = dtype == GAD_F32 ? 6 : 1;
+    g.t.bf16 = dtype != GAD_F16;
+    g.t.err = status;
+    return g;
+}
+
+template <int USE, int LAYOUT, class T, bool ADD_UP, int G>
+cudaError_t launch_gated(const GatedGroup<G>& g, Sequence& q) {
+    const auto kernel = gated_gemm_kernel<USE, LAYOUT, T, ADD_UP, G>;
     cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), CT_SMEM, false);
     if (e != cudaSuccess) return e;
     static std::atomic<int> known{0};
     if (known.load() <= 0) known.store(max_active_pairs(reinterpret_cast<const void*>(kernel), CT_THREADS, CT_SMEM, 2 * kPairs));
-    const int64_t units = g.t.whole + ((int64_t)g.t.tiles_m * g.t.tiles_n - g.t.whole) * g.t.shares;
-    const int ncl = (int)std::min<int64_t>(units, known.load());
-    return q.launch(kernel, dim3((unsigned)(2 * ncl)), CT_THREADS, CT_SMEM, A, B0, B1, g);
+    return q.launch(kernel, dim3((unsigned)(2 * std::min(g.first[G], known.load()))), CT_THREADS, CT_SMEM, g);
 }
 
-// One product.  Where results go as they are (kPlain), tiles that are left over when all pairs have had the same number are cut along their reduction, down to 8 ring stages a share.
-template <int USE, bool A_MN, bool B_MN, class T>
-cudaError_t go(const CUtensorMap& A, const CUtensorMap& B0, const CUtensorMap& B1, GatedArgs g, Sequence& q) {
-    TileArgs& a = g.t;
-    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, rest = tiles % kPairs;
-    a.whole = (int)tiles; a.shares = 1; a.kb_share = a.nkb; a.chunk = kGatedChunk<T>;
-    if (USE == kPlain && rest) {
-        const int want = (int)std::min<int64_t>(kPairs / rest, (int64_t)a.nkb * a.pairs * g.segs / 8);
-        if (want > 1) {
-            a.kb_share = (a.nkb + want - 1) / want;
-            a.shares = (a.nkb + a.kb_share - 1) / a.kb_share;
-            a.whole = (int)(tiles - rest);
-        }
+// A launch of g.n products, and the join of the tiles that were cut.
+template <int USE, int LAYOUT, class T, int G>
+cudaError_t go(GatedGroup<G>& g, Sequence& q) {
+    bool add_up = sizeof(T) == 4;
+    int64_t u = 0;
+    JoinArgs j{};
+    for (int i = 0; i < kGroup; ++i) {
+        if (i < g.n) {
+            g.first[i] = (int)u;
+            TileArgs& a = g.p[i].t;
+            a.chunk = kGatedChunk<T>;
+            if (sizeof(T) == 2) {
+                // a sum that is no longer than a chunk is one
+                const int64_t most = (int64_t)(a.whole > 0 ? a.nkb : a.kb_share) * g.p[i].segs;
+                if (most > a.chunk) { add_up = true; a.chunk = std::max(1, a.chunk / g.p[i].segs); } else a.chunk = a.nkb;
+            }
+            u += a.whole + ((int64_t)a.tiles_m * a.tiles_n - a.whole) * a.shares;
+            j.p[i] = g.p[i];
+            j.first[i + 1] = j.first[i] + (a.shares > 1 ? (int)(((int64_t)a.tiles_m * a.tiles_n - a.whole) * (CT_M * a.width / 1024)) : 0);
+        } else j.first[i + 1] = j.first[i];
     }
-    g.clear = q.clear;
-    const bool add_up = sizeof(T) == 4 || (int64_t)(a.whole > 0 ? a.nkb : a.kb_share) * g.segs > a.chunk;
-    const cudaError_t e = add_up ? launch_gated<USE, A_MN, B_MN, T, true>(A, B0, B1, g, q) : launch_gated<USE, A_MN, B_MN, T, sizeof(T) == 4>(A, B0, B1, g, q);
+    if (u > INT32_MAX) return cudaErrorInvalidValue;
+    for (int i = g.n; i <= G; ++i) g.first[i] = (int)u;
+    g.p[0].clear = q.clear;
     q.clear = false;
-    if (e != cudaSuccess || a.shares == 1) return e;
-    return q.launch(gated_join_kernel<T>, dim3((unsigned)(rest * (CT_M * a.width / 1024))), 256, 0, g);
+    const cudaError_t e = add_up ? launch_gated<USE, LAYOUT, T, true>(g, q) : launch_gated<USE, LAYOUT, T, sizeof(T) == 4>(g, q);
+    if (e != cudaSuccess || j.first[kGroup] == 0) return e;
+    return q.launch(gated_join_kernel<T>, dim3((unsigned)j.first[kGroup]), 256, 0, j);
 }
 
 template <class T>
@@ -164,23 +274,6 @@ cudaError_t map_of(CUtensorMap& m, const Operand& o, uint8_t* ws, int parts, uin
     const void* base = o.pack ? ws + o.at : o.src;
     const int64_t ld = o.pack ? o.ldp : o.ld;
     return tc_make_map(&m, base, (uint64_t)o.cols, (uint64_t)o.rows, (uint64_t)parts, (uint64_t)ld * 2, (uint64_t)(ld * 2 * o.rows), box, false, true) ? cudaSuccess : cudaErrorInvalidValue;
-}
-
-GatedArgs product(int64_t M, int N, int64_t K, int width, int dtype, int planes, int segs, int group, int32_t* status) {
-    GatedArgs g{};
-    g.parts = dtype == GAD_F32 ? 3 : 1;
-    g.segs = segs;
-    g.t.M = (int)M; g.t.N = N;
-    g.plane_tiles = (int)((M + CT_M - 1) / CT_M);
-    g.t.tiles_m = planes * g.plane_tiles;
-    g.t.width = width;
-    g.t.nkb = (int)((K + CT_K - 1) / CT_K);
-    g.t.group = group;
-    g.t.pairs = dtype == GAD_F32 ? 6 : 1;
-    g.t.bf16 = dtype != GAD_F16;
-    g.t.err = status;
-    g.t.tiles_n = (N + width - 1) / width;
-    return g;
 }
 
 // Few rows: how a product is cut.  In units of the time in which HBM gives every SM 16 KB (0.37 us): all weights once; or, where more, the stages of the SM that has most (0.45 each with few
@@ -210,8 +303,12 @@ bool is_skinny(const gad_gated_args& a) { return a.dtype != GAD_F32 && !a.act &&
 struct ForwardPlan {
     Operand x, wg, wu, wd, h;
     SkinnyCut gate, down;
+    Cut hidden, out;
     int64_t o_slots, o_gate, total;
 };
+// (a tile of kGate has g and u of half as many units as it is wide)
+Shape gate_shape(const gad_gated_args& a) { return {a.rows, 2 * a.inner, a.cols, 1, 1}; }
+Shape out_shape(const gad_gated_args& a) { return {a.rows, a.cols, a.inner, 1, 1}; }
 ForwardPlan plan_forward(const gad_gated_args& a) {
     ForwardPlan p{};
     Room room;
@@ -230,7 +327,10 @@ ForwardPlan plan_forward(const gad_gated_args& a) {
         p.o_gate = room.take(parts(p.gate));
         p.o_slots = room.take(parts(p.down));
     } else {
-        p.o_slots = room.take((int64_t)kPairs * CT_M * width_for(a.cols) * 4);
+        p.hidden = cut_alone(gate_shape(a));
+        const Shape s = out_shape(a);
+        cut_group(&s, 1, a.dtype == GAD_F32 ? 6 : 1, &p.out);
+        p.o_slots = room.take(slot_bytes(p.out));
     }
     p.total = room.at;
     return p;
@@ -280,37 +380,43 @@ cudaError_t run_forward(const gad_gated_args& a, uint8_t* ws, cudaStream_t s) {
     if constexpr (sizeof(T) == 2) {
         if (is_skinny(a)) { GAD_TRY(run_skinny<T>(a, p, ws, q)); return cudaGetLastError(); }
     }
-    CUtensorMap A, B0, B1;
-    GatedArgs g = product(a.rows, a.inner, a.cols, 256, a.dtype, 1, 1, 16, a.status);
-    g.t.tiles_n = (a.inner + CT_H - 1) / CT_H;
+    GatedGroup<1> r{};
+    r.n = 1;
+    GatedArgs& g = r.p[0];
+    g = product(gate_shape(a), p.hidden, a.dtype, false, 16, a.status);
+    g.t.N = a.inner;
     g.activation = a.activation;
     g.h = p.h.pack ? ws + p.h.at : const_cast<void*>(p.h.src);
     g.ldh = p.h.pack ? p.h.ldp : p.h.ld;
     g.h_part = a.rows * g.ldh;
     g.act = a.act; g.ldact = a.ldact; g.slope = a.slope; g.ldslope = a.ldslope;
     g.C[0] = a.dtype == GAD_F32 ? a.h : nullptr; g.ldc[0] = a.ldh;
-    GAD_TRY(map_of(A, p.x, ws, parts, CT_H));
-    GAD_TRY(map_of(B0, p.wg, ws, parts, CT_H));
-    GAD_TRY(map_of(B1, p.wu, ws, parts, CT_H));
-    GAD_TRY((go<kGate, false, false, T>(A, B0, B1, g, q)));
-    const int width = width_for(a.cols);
-    g = product(a.rows, a.cols, a.inner, width, a.dtype, 1, 1, 8, a.status);
+    GAD_TRY(map_of(r.A[0], p.x, ws, parts, CT_H));
+    GAD_TRY(map_of(r.B0[0], p.wg, ws, parts, (uint32_t)g.t.width / 2));
+    GAD_TRY(map_of(r.B1[0], p.wu, ws, parts, (uint32_t)g.t.width / 2));
+    GAD_TRY((go<kGate, kBothK, T>(r, q)));
+    g = product(out_shape(a), p.out, a.dtype, false, 8, a.status);
     g.C[0] = a.y; g.ldc[0] = a.ldy;
     g.t.slots = reinterpret_cast<float*>(ws + p.o_slots);
-    GAD_TRY(map_of(A, p.h, ws, parts, CT_H));
-    GAD_TRY(map_of(B0, p.wd, ws, parts, (uint32_t)width / 2));
-    GAD_TRY((go<kPlain, false, false, T>(A, B0, B0, g, q)));
+    GAD_TRY(map_of(r.A[0], p.h, ws, parts, CT_H));
+    GAD_TRY(map_of(r.B0[0], p.wd, ws, parts, (uint32_t)g.t.width / 2));
+    GAD_TRY((go<kPlain, kBothK, T>(r, q)));
     return cudaGetLastError();
 }
 
 struct BackwardPlan {
     Operand dy, x, wg, wu, wd, h;
-    int64_t o_dg, ldg, o_slots, total;
+    Cut hidden, cut[kGroup];
+    Shape shape[kGroup];
+    int n, at_x, at_gu, at_d;          // products behind dg and du, and which is which (-1: not wanted)
+    int64_t o_dg, ldg, o_slots[kGroup], total;
 };
+bool wants_hidden(const gad_gated_grad_args& a) { return a.dx || a.dw_gate || a.dw_up; }
+Shape hidden_shape(const gad_gated_grad_args& a) { return {a.rows, a.inner, a.cols, 1, 1}; }
 BackwardPlan plan_backward(const gad_gated_grad_args& a) {
     BackwardPlan p{};
     Room room;
-    const bool hidden = a.dx || a.dw_gate || a.dw_up;
+    const bool hidden = wants_hidden(a);
     const auto maybe = [&](bool wanted, const void* ptr, int64_t ld, int64_t rows, int cols) { return wanted ? operand(ptr, ld, rows, cols, a.dtype, room) : Operand{}; };
     p.dy = maybe(hidden || a.dw_down, a.dy, a.lddy, a.rows, a.cols);
     p.wd = maybe(hidden, a.w_down, a.ldwd, a.cols, a.inner);
@@ -319,8 +425,16 @@ BackwardPlan plan_backward(const gad_gated_grad_args& a) {
     p.x = maybe(a.dw_gate || a.dw_up, a.x, a.ldx, a.rows, a.cols);
     p.h = maybe(a.dw_down, a.h, a.ldh, a.rows, a.inner);
     p.ldg = round_up(a.inner, 8);
-    if (hidden) p.o_dg = room.take((a.dtype == GAD_F32 ? 12 : 4) * a.rows * p.ldg);
-    p.o_slots = room.take((int64_t)kPairs * CT_M * std::max(width_for(a.cols), width_for(a.inner)) * 4);
+    if (hidden) {
+        p.o_dg = room.take((a.dtype == GAD_F32 ? 12 : 4) * a.rows * p.ldg);
+        p.hidden = cut_alone(hidden_shape(a));
+    }
+    p.at_x = p.at_gu = p.at_d = -1;
+    if (a.dx) { p.at_x = p.n; p.shape[p.n++] = {a.rows, a.cols, a.inner, 1, 2}; }
+    if (a.dw_gate || a.dw_up) { p.at_gu = p.n; p.shape[p.n++] = {a.inner, a.cols, a.rows, a.dw_gate && a.dw_up ? 2 : 1, 1}; }
+    if (a.dw_down) { p.at_d = p.n; p.shape[p.n++] = {a.cols, a.inner, a.rows, 1, 1}; }
+    cut_group(p.shape, p.n, a.dtype == GAD_F32 ? 6 : 1, p.cut);
+    for (int i = 0; i < p.n; ++i) p.o_slots[i] = room.take(slot_bytes(p.cut[i]));
     p.total = room.at;
     return p;
 }
@@ -330,50 +444,51 @@ cudaError_t run_backward(const gad_gated_grad_args& a, uint8_t* ws, cudaStream_t
     const BackwardPlan p = plan_backward(a);
     const int parts = a.dtype == GAD_F32 ? 3 : 1;
     const int64_t N = a.rows;
-    const int D = a.cols, F = a.inner;
     Sequence q{s};
     GAD_TRY(pack<T>({&p.dy, &p.wd, &p.wg, &p.wu, &p.x, &p.h}, ws, q));
-    CUtensorMap A, B0, B1;
-    float* slots = reinterpret_cast<float*>(ws + p.o_slots);
     uint8_t* dg = ws + p.o_dg;
     const int64_t part = N * p.ldg;                       // values of a part of dg; du lies behind all of dg's
-    const int width_d = width_for(D), width_f = width_for(F);
-    if (a.dx || a.dw_gate || a.dw_up) {
-        GatedArgs g = product(N, F, D, width_f, a.dtype, 1, 1, 16, a.status);
+    if (wants_hidden(a)) {
+        GatedGroup<1> r{};
+        r.n = 1;
+        GatedArgs& g = r.p[0];
+        g = product(hidden_shape(a), p.hidden, a.dtype, false, 16, a.status);
         g.act = const_cast<void*>(a.act); g.ldact = a.ldact; g.slope = const_cast<void*>(a.slope); g.ldslope = a.ldslope;
         g.C[0] = dg; g.ldh = p.ldg; g.h_part = part;
-        GAD_TRY(map_of(A, p.dy, ws, parts, CT_H));
-        GAD_TRY(map_of(B0, p.wd, ws, parts, CT_K));
-        GAD_TRY((go<kHidden, false, true, T>(A, B0, B0, g, q)));
+        GAD_TRY(map_of(r.A[0], p.dy, ws, parts, CT_H));
+        GAD_TRY(map_of(r.B0[0], p.wd, ws, parts, CT_K));
+        GAD_TRY((go<kHidden, kBMN, T>(r, q)));
     }
     const auto map_dg = [&](CUtensorMap& m, int plane, int planes, uint32_t box) {
-        return tc_make_map(&m, dg + plane * parts * part * 2, (uint64_t)F, (uint64_t)N, (uint64_t)(planes * parts), (uint64_t)p.ldg * 2, (uint64_t)part * 2, box, false, true) ? cudaSuccess : cudaErrorInvalidValue;
+        return tc_make_map(&m, dg + plane * parts * part * 2, (uint64_t)a.inner, (uint64_t)N, (uint64_t)(planes * parts), (uint64_t)p.ldg * 2, (uint64_t)part * 2, box, false, true) ? cudaSuccess : cudaErrorInvalidValue;
     };
-    if (a.dx) {
-        GatedArgs g = product(N, D, F, width_d, a.dtype, 1, 2, 8, a.status);
-        g.C[0] = a.dx; g.ldc[0] = a.lddx; g.t.slots = slots;
-        GAD_TRY(map_dg(A, 0, 2, CT_H));
-        GAD_TRY(map_of(B0, p.wg, ws, parts, CT_K));
-        GAD_TRY(map_of(B1, p.wu, ws, parts, CT_K));
-        GAD_TRY((go<kPlain, false, true, T>(A, B0, B1, g, q)));
+    GatedGroup<kGroup> r{};
+    r.n = p.n;
+    for (int i = 0; i < p.n; ++i) {
+        r.p[i] = product(p.shape[i], p.cut[i], a.dtype, i != p.at_x, 8, a.status);
+        r.p[i].t.slots = reinterpret_cast<float*>(ws + p.o_slots[i]);
     }
-    if (a.dw_gate || a.dw_up) {
-        const int planes = a.dw_gate && a.dw_up ? 2 : 1;
-        GatedArgs g = product(F, D, N, width_d, a.dtype, planes, 1, 8, a.status);
-        g.C[0] = a.dw_gate ? a.dw_gate : a.dw_up; g.ldc[0] = a.dw_gate ? a.lddwg : a.lddwu;
-        g.C[1] = a.dw_up; g.ldc[1] = a.lddwu;
-        g.t.slots = slots;
-        GAD_TRY(map_dg(A, a.dw_gate ? 0 : 1, planes, CT_K));
-        GAD_TRY(map_of(B0, p.x, ws, parts, CT_K));
-        GAD_TRY((go<kPlain, true, true, T>(A, B0, B0, g, q)));
+    if (p.at_x >= 0) {
+        const int i = p.at_x;
+        r.p[i].C[0] = a.dx; r.p[i].ldc[0] = a.lddx;
+        GAD_TRY(map_dg(r.A[i], 0, 2, CT_H));
+        GAD_TRY(map_of(r.B0[i], p.wg, ws, parts, CT_K));
+        GAD_TRY(map_of(r.B1[i], p.wu, ws, parts, CT_K));
     }
-    if (a.dw_down) {
-        GatedArgs g = product(D, F, N, width_f, a.dtype, 1, 1, 8, a.status);
-        g.C[0] = a.dw_down; g.ldc[0] = a.lddwd; g.t.slots = slots;
-        GAD_TRY(map_of(A, p.dy, ws, parts, CT_K));
-        GAD_TRY(map_of(B0, p.h, ws, parts, CT_K));
-        GAD_TRY((go<kPlain, true, true, T>(A, B0, B0, g, q)));
+    if (p.at_gu >= 0) {
+        const int i = p.at_gu;
+        r.p[i].C[0] = a.dw_gate ? a.dw_gate : a.dw_up; r.p[i].ldc[0] = a.dw_gate ? a.lddwg : a.lddwu;
+        r.p[i].C[1] = a.dw_up; r.p[i].ldc[1] = a.lddwu;
+        GAD_TRY(map_dg(r.A[i], a.dw_gate ? 0 : 1, p.shape[i].planes, CT_K));
+        GAD_TRY(map_of(r.B0[i], p.x, ws, parts, CT_K));
     }
+    if (p.at_d >= 0) {
+        const int i = p.at_d;
+        r.p[i].C[0] = a.dw_down; r.p[i].ldc[0] = a.lddwd;
+        GAD_TRY(map_of(r.A[i], p.dy, ws, parts, CT_K));
+        GAD_TRY(map_of(r.B0[i], p.h, ws, parts, CT_K));
+    }
+    GAD_TRY((go<kPlain, kAnyMN, T>(r, q)));
     return cudaGetLastError();
 }
 #undef GAD_TRY
@@ -442,7 +557,8 @@ extern "C" int gad_gated_feed_forward(const gad_gated_args* args, void* workspac
     const cudaStream_t s = (cudaStream_t)stream;
     if (a.rows == 0) return empty(a.status, s);
     if (!a.x || !a.w_gate || !a.w_up || !a.w_down || !a.y) return GAD_ERR_ARG;
-    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < (size_t)plan_forward(a).total) return GAD_ERR_OOM;
+    const size_t need = (size_t)plan_forward(a).total;
+    if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need)) return GAD_ERR_OOM;
     try {
         uint8_t* ws = (uint8_t*)workspace;
         const cudaError_t e = a.dtype == GAD_F32 ? run_forward<float>(a, ws, s) : a.dtype == GAD_F16 ? run_forward<__half>(a, ws, s) : run_forward<__nv_bfloat16>(a, ws, s);
@@ -470,7 +586,8 @@ extern "C" int gad_gated_feed_forward_backward(const gad_gated_grad_args* args, 
     if (a.rows == 0) return a.dtype == GAD_F32 ? run_no_rows<float>(a, s) : a.dtype == GAD_F16 ? run_no_rows<__half>(a, s) : run_no_rows<__nv_bfloat16>(a, s);
     if (!a.dy || !a.x || !a.w_gate || !a.w_up || !a.w_down || !a.act || !a.slope || !a.h) return GAD_ERR_ARG;
     if (!a.dx && !a.dw_gate && !a.dw_up && !a.dw_down) return empty(a.status, s);
-    if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < (size_t)plan_backward(a).total) return GAD_ERR_OOM;
+    const size_t need = (size_t)plan_backward(a).total;
+    if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need)) return GAD_ERR_OOM;
     try {
         uint8_t* ws = (uint8_t*)workspace;
         const cudaError_t e = a.dtype == GAD_F32 ? run_backward<float>(a, ws, s) : a.dtype == GAD_F16 ? run_backward<__half>(a, ws, s) : run_backward<__nv_bfloat16>(a, ws, s);

@@ -6,7 +6,8 @@
 // The ring, the roles and the tiles are those of the output head's product (class_gemm.cuh): tiles of 256 rows by two CTAs (cta_group::2), 64 values of the reduction a
 // stage, two accumulators of 256 columns, eight draining warps.  Of B each CTA of a pair holds half of the columns, so for kGate one CTA loads 128 rows of Wg and the
 // other 128 rows of Wu: the accumulator has g in its left half and u, of the same units, in its right one, and no copy of the weights is laid out for it.
-// The sum dg Wg + du Wu is one reduction over two segments with a B of its own each; dWg and dWu are one launch over two planes of A with an output each.
+// The sum dg Wg + du Wu is one reduction over two segments with a B of its own each; dWg and dWu are one product over two planes of A with an output each; and the products that do not wait for
+// one another (dx, both of these, dWd) are one launch, whose tiles are gone through one product behind the other.
 #pragma once
 
 #include "class_gemm.cuh"
@@ -22,6 +23,7 @@ struct GatedArgs {
     TileArgs t;                // tiles and shares (M rows of a plane)
     int parts, segs;           // operand parts; segments of the reduction (t.pairs products each)
     int plane_tiles;           // row tiles of a plane
+    int a_mn;                  // kAnyMN: A is MN-major
     int activation;
     int clear;                 // the call's first product: its first block sets the status to zero (blocks come up in order, and a wait takes 2^22 polls to run out)
     void *C[2];                // kPlain: result of each plane; kGate with T = float: C[0] is h where it is kept, or null
@@ -30,6 +32,19 @@ struct GatedArgs {
     void *h, *act, *slope;
     long long ldh, h_part, ldact, ldslope;
 };
+
+// The products of a launch: one, or up to three.
+constexpr int kGroup = 3;
+template <int G>
+struct GatedGroup {
+    CUtensorMap A[G], B0[G], B1[G];
+    GatedArgs p[G];
+    int n;
+    int first[G + 1];          // units of work in front of each, and of all
+};
+template <int G> __device__ __forceinline__ int product_of(const GatedGroup<G>& gr, int u) { return G > 1 && u >= gr.first[1] ? (u >= gr.first[2] ? 2 : 1) : 0; }
+// Which operands are MN-major (the reduction runs over their rows): neither; B; B, and A as its product says (GatedArgs::a_mn).
+enum Layout { kBothK, kBMN, kAnyMN };
 
 // act(x) and act'(x).  The logistic function from exp2 and a reciprocal, each within 2 ulp.
 __device__ __forceinline__ void activation(int kind, float x, float& a, float& d) {
@@ -90,11 +105,13 @@ __device__ __forceinline__ void drain_operand(uint8_t* buf, int lane, float (&v)
     }
 }
 
-// USE as above; A_MN, B_MN: operand is MN-major; T: type of the tensors; ADD_UP: sums in chunks (t.chunk), as class_gemm_kernel takes them.
-template <int USE, bool A_MN, bool B_MN, class T, bool ADD_UP>
+// USE as above; T: type of the tensors; ADD_UP: sums in chunks (t.chunk), as class_gemm_kernel takes them; G: products a launch may have.  (With the layouts of all products and their number known only
+// at run time, in one kernel for all uses, 8192 x 2048 x 5504 took 428 us instead of 416, and the gradients of 16 384 x 4096 x 10 240 6.2 ms instead of 5.8.)
+template <int USE, int LAYOUT, class T, bool ADD_UP, int G>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(CT_THREADS, 1)
-gated_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB0, const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ GatedArgs ga) {
-    const TileArgs& a = ga.t;
+gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
+    constexpr bool B_MN = LAYOUT != kBothK;
+    int32_t* const err = gr.p[0].t.err;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
     const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;   // the same in both CTAs
@@ -125,38 +142,46 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = *tmem_slot;
     pdl_wait();
-    if (ga.clear && blockIdx.x == 0 && threadIdx.x == 0) *a.err = 0;
+    if (gr.p[0].clear && blockIdx.x == 0 && threadIdx.x == 0) *err = 0;
 
-    const int ncl = gridDim.x >> 1, half_w = a.width / 2, products = a.pairs * ga.segs;
-    const long long units = units_of(a);
+    const int ncl = gridDim.x >> 1, units = gr.first[G];
 
     if (warp == 0 && lane == 0) {
         // ---------------- TMA producer: this CTA's rows of A and half of the columns' rows of B; the leader's barrier counts both CTAs' bytes ----------------
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
-            const TileAt t = tile_at(a, u);
+        for (int u = blockIdx.x >> 1; u < units && ok; u += ncl) {
+            const int which = product_of(gr, u);
+            const GatedArgs& ga = gr.p[which];
+            const TileArgs& a = ga.t;
+            const CUtensorMap* tmA = &gr.A[which];
+            const CUtensorMap *tmB0 = &gr.B0[which], *tmB1 = &gr.B1[which];
+            const int half_w = a.width / 2, pairs = a.pairs, parts = ga.parts, products = pairs * ga.segs;
+            const bool a_mn = LAYOUT == kAnyMN && ga.a_mn;
+            const uint32_t bytes = 2u * (uint32_t)(CT_H + half_w) * (CT_K * 2);
+            const TileAt t = tile_at(a, u - gr.first[which]);
             const int plane = t.m / ga.plane_tiles;
             const int ra = (t.m - plane * ga.plane_tiles) * CT_M + (int)rank * CT_H;
-            const int rb = USE == kGate ? t.n * CT_H : t.n * a.width + (int)rank * half_w;
+            const int rb = USE == kGate ? t.n * half_w : t.n * a.width + (int)rank * half_w;
             const int group = ADD_UP ? a.chunk : t.nkb;
             for (int g = 0; g < t.nkb && ok; g += group)
                 for (int p = 0; p < products && ok; ++p) {
-                    const int seg = p / a.pairs;
+                    const int seg = p >= pairs ? 1 : 0;
                     int za, zb;
-                    part_pair(p - seg * a.pairs, a.pairs, za, zb);
-                    za += (plane + seg) * ga.parts;
-                    const CUtensorMap* tmB = (USE == kGate ? (int)rank : seg) ? &tmB1 : &tmB0;
-                    for (int kb = t.kb0 + g; kb < t.kb0 + min(g + group, t.nkb); ++kb) {
-                        if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, 41))) break;
-                        if (rank == 0) mbar_expect_tx(full(stage), 2u * (uint32_t)(CT_H + half_w) * (CT_K * 2));
+                    part_pair(p - seg * pairs, pairs, za, zb);
+                    za += (plane + seg) * parts;
+                    const CUtensorMap* tmB = (USE == kGate ? (int)rank : seg) ? tmB1 : tmB0;
+                    const int last = t.kb0 + min(g + group, t.nkb);
+                    for (int kb = t.kb0 + g; kb < last; ++kb) {
+                        if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, err, 41))) break;
+                        if (rank == 0) mbar_expect_tx(full(stage), bytes);
                         const uint32_t base = sm_addr + stage * CT_STAGE, bar = leader_address(full(stage));
-                        if (A_MN) {
-                            tma_load_3d_pair(base, &tmA, ra, kb * CT_K, za, bar);
-                            tma_load_3d_pair(base + 8192, &tmA, ra + 64, kb * CT_K, za, bar);
+                        if (a_mn) {
+                            tma_load_3d_pair(base, tmA, ra, kb * CT_K, za, bar);
+                            tma_load_3d_pair(base + 8192, tmA, ra + 64, kb * CT_K, za, bar);
                         } else {
-                            tma_load_3d_pair(base, &tmA, kb * CT_K, ra, za, bar);
+                            tma_load_3d_pair(base, tmA, kb * CT_K, ra, za, bar);
                         }
                         if (B_MN) {
                             for (int j = 0; j < half_w; j += 64) tma_load_3d_pair(base + CT_OPERAND + j * 128, tmB, rb + j, kb * CT_K, zb, bar);
@@ -171,24 +196,30 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         // ---------------- MMA issuer (leader of the pair): the whole warp runs the loop, one elected lane issues ----------------
         int stage = 0, acc = 0;
         uint32_t phase = 0, acc_phase = 0;
-        const uint32_t idesc = instr_desc_f16(a.width, CT_M) | (a.bf16 ? (1u << 7) | (1u << 10) : 0u) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
-        constexpr uint32_t stepA = A_MN ? 128 : 2, stepB = B_MN ? 128 : 2;    // 16 values of the reduction: 16 rows of 128 bytes, or 32 bytes of a row
         bool ok = true;
-        for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
-            const int steps = tile_at(a, u).nkb * products;
+        for (int u = blockIdx.x >> 1; u < units && ok; u += ncl) {
+            const int which = product_of(gr, u);
+            const GatedArgs& ga = gr.p[which];
+            const TileArgs& a = ga.t;
+            const bool a_mn = LAYOUT == kAnyMN && ga.a_mn;
+            const uint32_t idesc = instr_desc_f16(a.width, CT_M) | (a.bf16 ? (1u << 7) | (1u << 10) : 0u) | (a_mn ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+            const uint32_t stepA = a_mn ? 128 : 2;
+            constexpr uint32_t stepB = B_MN ? 128 : 2;                        // 16 values of the reduction: 16 rows of 128 bytes, or 32 bytes of a row
+            const uint64_t descA = a_mn ? operand_desc<true>(0) : operand_desc<false>(0);
+            const int products = a.pairs * ga.segs, steps = tile_at(a, u - gr.first[which]).nkb * products, chunk = a.chunk * products;
             int left = 0;                                          // stages until this accumulator is full
             for (int i = 0; i < steps; ++i) {
                 const bool first = left == 0;
                 if (first) {
-                    if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 42)))) break;
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(tempty(acc), acc_phase ^ 1u, abort_flag, err, 42)))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    left = ADD_UP ? min(a.chunk * products, steps - i) : steps;
+                    left = ADD_UP ? min(chunk, steps - i) : steps;
                 }
                 const uint32_t d = tmem_base + (uint32_t)(acc * ACC_COLS);
-                if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(full(stage), phase, abort_flag, a.err, 43)))) break;
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(full(stage), phase, abort_flag, err, 43)))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t base = sm_addr + stage * CT_STAGE;
-                const uint64_t da = operand_desc<A_MN>(base), db = operand_desc<B_MN>(base + CT_OPERAND);
+                const uint64_t da = descA | (base >> 4), db = operand_desc<B_MN>(base + CT_OPERAND);
                 if (elect_one()) {
 #pragma unroll
                     for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_pair(d, da + stepA * ks, db + stepB * ks, idesc, !first || ks != 0 ? 1u : 0u);
@@ -207,8 +238,12 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         int acc = 0;
         uint32_t acc_phase = 0;
         const auto store = [](const void* p, long long ld) { return store_bytes(p, ld * (long long)sizeof(T)); };
-        for (long long u = blockIdx.x >> 1; u < units; u += ncl) {
-            const TileAt t = tile_at(a, u);
+        for (int u = blockIdx.x >> 1; u < units; u += ncl) {
+            const int which = product_of(gr, u);
+            const GatedArgs& ga = gr.p[which];
+            const TileArgs& a = ga.t;
+            const int half_w = a.width / 2;
+            const TileAt t = tile_at(a, u - gr.first[which]);
             const int plane = t.m / ga.plane_tiles, tm = t.m - plane * ga.plane_tiles;
             const int row0 = tm * CT_M + (int)rank * CT_H + q * 32, rows = a.M - row0;   // this warp's rows
             const int row = row0 + lane;
@@ -221,13 +256,13 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             };
             bool ok = true;
             const auto wait_full = [&]() {
-                ok = __all_sync(0xffffffffu, mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 46));
+                ok = __all_sync(0xffffffffu, mbar_wait(tfull(acc), acc_phase, abort_flag, err, 46));
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 return ok;
             };
-            // this warp's columns of the accumulator: blocks of 32, for kGate two of g and the same two of u behind them
-            const auto block_at = [&](int c) { return USE == kGate ? (c >> 1) * CT_H + half * 64 + (c & 1) * 32 : half * half_w + 32 * c; };
-            const int blocks = USE == kGate ? 4 : half_w / 32;
+            // this warp's columns of the accumulator: blocks of 32, for kGate one or two of g and the same of u behind them
+            const int blocks = half_w / 32, of_g = blocks / 2;
+            const auto block_at = [&](int c) { return USE != kGate ? half * half_w + 32 * c : c < of_g ? half * (half_w / 2) + 32 * c : half_w + half * (half_w / 2) + 32 * (c - of_g); };
             if constexpr (ADD_UP) {
                 const int chunks = (t.nkb + a.chunk - 1) / a.chunk;
                 float sum[4][32];
@@ -256,13 +291,13 @@ gated_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             } else if (!wait_full()) break;
             const uint32_t at = tm_row + (uint32_t)(acc * ACC_COLS);
             if constexpr (USE == kGate) {
-                for (int c = 0; c < 2; ++c) {
-                    const int col = t.n * CT_H + half * 64 + 32 * c, cols = a.N - col;
+                for (int c = 0; c < of_g; ++c) {
+                    const int col = t.n * half_w + half * (half_w / 2) + 32 * c, cols = a.N - col;
                     if (rows <= 0 || cols <= 0) break;
                     float g[32], v[32];
                     __syncwarp();
                     tmem_ld32_start(at + (uint32_t)block_at(c), g);
-                    tmem_ld32_start(at + (uint32_t)block_at(c + 2), v);
+                    tmem_ld32_start(at + (uint32_t)block_at(c + of_g), v);
                     tmem_ld32_wait(g);
                     tmem_ld32_wait(v);
                     if (ga.act) {

@@ -182,18 +182,13 @@ def test_some_of_the_gradients(dtype):
     s = make(200, 136, 264, dtype, 8)
     r = pkg.gated_feed_forward(**s, save=True)
     dy = matrix(200, 136, s["x"].dtype, torch.Generator().manual_seed(9))
-    whole = pkg.gated_feed_forward_backward(dy, **s, act=r.act, slope=r.slope, h=r.h).check()
+    exact = backward(dy, **s, act=r.act, slope=r.slope, h=r.h)
     names = {"x": "dx", "g": "dWg", "u": "dWu", "d": "dWd"}
+    # (how sums are cut into shares goes by what is asked for: each is within the tolerance, not the same to the bit)
     for want in ("x", "g", "u", "d", "xd", "gu", "ud", ""):
         some = pkg.gated_feed_forward_backward(dy, **s, act=r.act, slope=r.slope, h=r.h, grads=want).check()
-        for k, name in names.items():
-            if k not in want:
-                assert getattr(some, name) is None
-            elif dtype == "float32" or k in "xd":
-                assert torch.equal(getattr(some, name), getattr(whole, name)), (want, name)
-    want = backward(dy, **s, act=r.act, slope=r.slope, h=r.h)
-    for k in "gu":
-        near(pkg.gated_feed_forward_backward(dy, **s, act=r.act, slope=r.slope, h=r.h, grads=k), {names[k]: want[names[k]]})
+        assert all(getattr(some, name) is None for k, name in names.items() if k not in want)
+        near(some, {names[k]: exact[names[k]] for k in want})
 
 
 @gpu
