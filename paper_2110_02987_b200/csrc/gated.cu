@@ -283,15 +283,17 @@ cudaError_t map_of(CUtensorMap& m, const Operand& o, uint8_t* ws, int parts, uin
 struct SkinnyCut { int per, tiles, nkb, shares, kb_share; };
 SkinnyCut skinny_cut(int64_t rows, int n, bool gate, int64_t K) {
     const int sms = 2 * kPairs, nkb = (int)((K + CT_K - 1) / CT_K), each = gate ? 2 : 1;
+    const double width = (double)round_up(rows, 16);
     SkinnyCut best{};
     double least = 1e30;
     for (int per = SK_M; per >= SK_M / 2; per -= 8 * each) {
         const int tiles = (n + per / each - 1) / (per / each);
-        for (int want = 1; want <= std::min(nkb, 64); ++want) {
+        const double stages = (double)tiles * nkb / sms / SK_M;
+        for (int want = 1; want <= std::min(nkb, 64); want += 1 + want / 8) {
             const int kb = (nkb + want - 1) / want, shares = (nkb + kb - 1) / kb;
-            if (shares != want) continue;
-            const double waves = (double)(((int64_t)tiles * shares + sms - 1) / sms);
-            const double stages = (double)tiles * nkb / sms / SK_M, width = (double)round_up(rows, 16), one = waves * kb * 0.45 * (1 + width / 256);
+            if (tiles * shares > 4 * sms && shares > 1) break;
+            const double waves = (double)((tiles * shares + sms - 1) / sms);
+            const double one = waves * kb * 0.45 * (1 + width / 256);
             const double cost = std::max({stages * per, one, 0.6 * stages * (per + width)}) + 0.15 * one + waves + (shares > 1 ? 4.0 + (double)shares * tiles * rows / (sms * 32) : 0.0);
             if (cost < least) { least = cost; best = {per, tiles, nkb, shares, kb}; }
         }

@@ -93,11 +93,20 @@ def _weights(x, Wg, Wu, Wd):
     return ldx, ldwg, ldwu, ldwd, inner
 
 
-def _run(L, name, a, like):
-    nbytes = C.c_size_t(0)
-    _ck(getattr(L, name + "_workspace_bytes")(C.byref(a), C.byref(nbytes)), name)
-    ws = like.new_empty(nbytes.value, dtype=head.torch.uint8)     # (torch's blocks start on 512 bytes)
-    _ck(getattr(L, name)(C.byref(a), ws.data_ptr(), nbytes.value, _stream(like.device)), name)
+_sizes = {}     # what a workspace's size depends on -> its bytes (asking for them is a tenth of a small call)
+
+
+def _run(ask, call, a, key, like):
+    at = C.byref(a)
+    nbytes = _sizes.get(key)
+    if nbytes is None:
+        n = C.c_size_t(0)
+        _ck(ask(at, C.byref(n)), call.__name__)
+        if len(_sizes) >= 1024:
+            _sizes.clear()
+        nbytes = _sizes[key] = n.value
+    ws = like.new_empty(nbytes, dtype=head.torch.uint8)     # (torch's blocks start on 512 bytes)
+    _ck(call(at, ws.data_ptr(), nbytes, _stream(like.device)), call.__name__)
 
 
 def gated_feed_forward(x, Wg, Wu, Wd, *, activation="silu", save=False, stream=None):
@@ -122,9 +131,10 @@ def gated_feed_forward(x, Wg, Wu, Wd, *, activation="silu", save=False, stream=N
     if save:
         act, slope, h = (t[:, :inner] for t in x.new_empty((3, rows, wide)).unbind(0))
         at = [act.data_ptr(), slope.data_ptr(), h.data_ptr()]
-    a = _ForwardArgs(head._DTYPES[x.dtype], cols, inner, _ACTIVATIONS[activation], rows, x.data_ptr(), ldx, Wg.data_ptr(), ldwg, Wu.data_ptr(), ldwu, Wd.data_ptr(), ldwd,
-                     y.data_ptr(), cols, at[0], wide, at[1], wide, at[2], wide, status.data_ptr())
-    _run(L, "gad_gated_feed_forward", a, x)
+    dt, px, pg, pu, pd = head._DTYPES[x.dtype], x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr()
+    a = _ForwardArgs(dt, cols, inner, _ACTIVATIONS[activation], rows, px, ldx, pg, ldwg, pu, ldwu, pd, ldwd, y.data_ptr(), cols, at[0], wide, at[1], wide, at[2], wide, status.data_ptr())
+    _run(L.gad_gated_feed_forward_workspace_bytes, L.gad_gated_feed_forward, a,
+         (dt, rows, cols, inner, save, ldx, ldwg, ldwu, ldwd, px & 15, pg & 15, pu & 15, pd & 15), x)
     return GatedForward(y, act, slope, h, status)
 
 
@@ -152,7 +162,9 @@ def gated_feed_forward_backward(dy, x, Wg, Wu, Wd, act, slope, h, *, grads=True,
     dWd = x.new_empty((cols, inner)) if "d" in want else None
     status = x.new_empty(1, dtype=head.torch.int32)
     at = [t.data_ptr() if t is not None else None for t in (dx, dWg, dWu, dWd)]
-    a = _BackwardArgs(head._DTYPES[x.dtype], cols, inner, rows, dy.data_ptr(), lddy, x.data_ptr(), ldx, Wg.data_ptr(), ldwg, Wu.data_ptr(), ldwu, Wd.data_ptr(), ldwd,
-                      act.data_ptr(), lda, slope.data_ptr(), lds, h.data_ptr(), ldh, at[0], cols, at[1], cols, at[2], cols, at[3], inner, status.data_ptr())
-    _run(L, "gad_gated_feed_forward_backward", a, x)
+    dt, py, px, pg, pu, pd, ph = head._DTYPES[x.dtype], dy.data_ptr(), x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), h.data_ptr()
+    a = _BackwardArgs(dt, cols, inner, rows, py, lddy, px, ldx, pg, ldwg, pu, ldwu, pd, ldwd, act.data_ptr(), lda, slope.data_ptr(), lds, ph, ldh,
+                      at[0], cols, at[1], cols, at[2], cols, at[3], inner, status.data_ptr())
+    _run(L.gad_gated_feed_forward_backward_workspace_bytes, L.gad_gated_feed_forward_backward, a,
+         (dt, rows, cols, inner, None, dx is None, dWg is None, dWu is None, dWd is None, lddy, ldx, ldwg, ldwu, ldwd, ldh, py & 15, px & 15, pg & 15, pu & 15, pd & 15, ph & 15), x)
     return GatedGrads(dx, dWg, dWu, dWd, status)
