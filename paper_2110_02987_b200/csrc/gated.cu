@@ -22,20 +22,23 @@ namespace {
 
 constexpr int kPairs = 74;                               // pairs of CTAs that run at once
 
-// Matrices to be copied to operands, in one launch: a warp a row.
+// Matrices to be copied to operands, in one launch: a warp has up to 512 columns of a row.
+constexpr int kPackRun = 512;
 struct PackJob { const void* src; long long ld; int rows, cols; void* dst; long long ldp, part_stride; };
-struct PackJobs { PackJob job[6]; long long first[7]; int n; };
+struct PackJobs { PackJob job[6]; long long first[7]; int n; };   // first: runs in front of each
 template <class T>
 __global__ void __launch_bounds__(256) gated_pack_kernel(const __grid_constant__ PackJobs a) {
-    const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     pdl_next();
     pdl_wait();
-    if (r >= a.first[a.n]) return;
+    if (i >= a.first[a.n]) return;
     int j = 0;
-    while (r >= a.first[j + 1]) ++j;
+    while (i >= a.first[j + 1]) ++j;
     const PackJob& k = a.job[j];
-    const long long row = r - a.first[j];
-    pack_row<T>(reinterpret_cast<const T*>(k.src) + row * k.ld, k.cols, true, k.dst, row * k.ldp, k.part_stride, threadIdx.x & 31, 32);
+    const int runs = (k.cols + kPackRun - 1) / kPackRun;
+    const long long row = (i - a.first[j]) / runs;
+    const int c = (int)(i - a.first[j] - row * runs) * kPackRun;
+    pack_row<T>(reinterpret_cast<const T*>(k.src) + row * k.ld + c, min(kPackRun, k.cols - c), true, k.dst, row * k.ldp + c, k.part_stride, threadIdx.x & 31, 32);
 }
 
 // The shares of the tiles that were cut along their reduction, added up in order: four columns a thread, 1024 values a block.  first: blocks in front of each product's, and of all.
@@ -64,6 +67,81 @@ __global__ void __launch_bounds__(256) gated_join_kernel(const __grid_constant__
 #pragma unroll
     for (int k = 0; k < 4; ++k)
         if (c + k < a.N) out[k] = from_float<T>(s[k]);
+}
+
+// Four values as operands, at most `cols` of them: in the operand type, or in three bfloat16 parts.
+template <class T>
+__device__ __forceinline__ void store_operand4(const float (&v)[4], void* out, long long at, long long part, int cols) {
+    if constexpr (sizeof(T) == 4) {
+        union { uint2 u; __nv_bfloat16 h[4]; } w[3];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            __nv_bfloat16 p[3];
+            split3(v[j], p);
+            for (int k = 0; k < 3; ++k) w[k].h[j] = p[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(out) + k * part + at;
+            if (cols >= 4) *reinterpret_cast<uint2*>(to) = w[k].u;
+            else for (int j = 0; j < cols; ++j) to[j] = w[k].h[j];
+        }
+    } else {
+        T* to = reinterpret_cast<T*>(out) + at;
+        if (cols >= 4) *reinterpret_cast<uint2*>(to) = make_uint2(Pair<T>::pack(v[0], v[1]), Pair<T>::pack(v[2], v[3]));
+        else for (int j = 0; j < cols; ++j) to[j] = from_float<T>(v[j]);
+    }
+}
+// The sums of kGate and kHidden that went to slots, joined, and what those kernels make of a tile: four columns of a row a thread, all of the GPU at once.  With fewer tiles than pairs of CTAs a
+// tile's drain has nothing to hide behind, and in fp32 (three parts of h, dg and du each) it takes as long as 60 to 100 stages of the reduction.
+template <int USE, class T>
+__global__ void __launch_bounds__(256) gated_hidden_join_kernel(const __grid_constant__ GatedArgs ga) {
+    const TileArgs& a = ga.t;
+    const int wide = USE == kGate ? a.width / 2 : a.width;            // columns of h (dg, du) a tile has
+    const int per_row = wide / 4, rows = 256 / per_row, per_tile = CT_M / rows;
+    const int i = blockIdx.x / per_tile, r = blockIdx.x % per_tile * rows + threadIdx.x / per_row, x = threadIdx.x % per_row * 4;
+    pdl_next();
+    pdl_wait();
+    const TileAt t = tile_at(a, (long long)i * a.shares);             // (all tiles are cut, or none)
+    const int row = t.m * CT_M + r, c = t.n * wide + x, cols = a.N - c;
+    if (row >= a.M || cols <= 0) return;
+    const float* slot = a.slots + ((long long)i * a.shares * CT_M + r) * a.width + x;
+    float s[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+    for (int k = 0; k < a.shares; ++k) {
+        const float4 p = *reinterpret_cast<const float4*>(slot + (long long)k * CT_M * a.width);
+        s[0] += p.x; s[1] += p.y; s[2] += p.z; s[3] += p.w;
+        if (USE == kGate) {
+            const float4 q = *reinterpret_cast<const float4*>(slot + (long long)k * CT_M * a.width + wide);
+            v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+        }
+    }
+    if (USE == kGate) {
+        float d[4];
+        activations(ga.activation, s, d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { d[j] *= v[j]; v[j] *= s[j]; }
+        if (ga.act) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j >= cols) break;
+                reinterpret_cast<T*>(ga.act)[(long long)row * ga.ldact + c + j] = from_float<T>(s[j]);
+                reinterpret_cast<T*>(ga.slope)[(long long)row * ga.ldslope + c + j] = from_float<T>(d[j]);
+                if (sizeof(T) == 4) reinterpret_cast<T*>(ga.C[0])[(long long)row * ga.ldc[0] + c + j] = from_float<T>(v[j]);
+            }
+        }
+        store_operand4<T>(v, ga.h, (long long)row * ga.ldh + c, ga.h_part, cols);
+    } else {
+        const T *act = reinterpret_cast<const T*>(ga.act) + (long long)row * ga.ldact + c, *slope = reinterpret_cast<const T*>(ga.slope) + (long long)row * ga.ldslope + c;
+        float g[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            g[j] = j < cols ? s[j] * to_float(slope[j]) : 0.f;
+            v[j] = j < cols ? s[j] * to_float(act[j]) : 0.f;
+        }
+        store_operand4<T>(g, ga.C[0], (long long)row * ga.ldh + c, ga.h_part, cols);
+        store_operand4<T>(v, ga.C[0], (long long)ga.parts * ga.h_part + (long long)row * ga.ldh + c, ga.h_part, cols);
+    }
 }
 
 template <class T>
@@ -117,7 +195,11 @@ template <> constexpr int kGatedChunk<__nv_bfloat16> = 1024;
 
 // One product: planes of M x N over K, in segs segments and pairs products of parts.
 struct Shape { int64_t M; int N; int64_t K; int planes, segs; };
-struct Cut { int width, tiles_m, tiles_n, nkb, whole, shares, kb_share; int64_t tiles() const { return (int64_t)tiles_m * tiles_n; } int64_t units() const { return whole + (tiles() - whole) * shares; } };
+struct Cut {
+    int width, tiles_m, tiles_n, nkb, whole, shares, kb_share;
+    bool split;                        // kGate, kHidden: all sums to slots
+    int64_t tiles() const { return (int64_t)tiles_m * tiles_n; }
+};
 
 // Tiles are 256 columns wide; narrow: 128, which take about three quarters of the time (their operands come from L2 half as fast again).
 Cut whole_tiles(const Shape& s, bool narrow) {
@@ -131,17 +213,10 @@ Cut whole_tiles(const Shape& s, bool narrow) {
     c.whole = (int)c.tiles();
     return c;
 }
-// kGate and kHidden: what is done with a finished tile is not additive, so tiles stay whole.  Narrow where their rounds are shorter all the same (22 wide tiles on 74 pairs: 44 narrow ones).
-Cut cut_alone(const Shape& s) {
-    const Cut wide = whole_tiles(s, false), narrow = whole_tiles(s, true);
-    const auto rounds = [](const Cut& c) { return (double)((c.tiles() + kPairs - 1) / kPairs); };
-    return 0.75 * rounds(narrow) < rounds(wide) && wide.tiles() < 8 * kPairs ? narrow : wide;
-}
-
 // Products whose results go as they are.  With three rounds of tiles and more, those of the last product that are left over when all pairs have had the same number are cut along their
 // reduction, down to 8 ring stages a share; with fewer, every tile is cut into shares of about the same number of stages, the number that lets the pair with most work finish first.
 constexpr int kMostUnits = 4 * kPairs;                    // of a launch whose tiles are cut
-void cut_group(const Shape* s, int n, int pairs, Cut* c) {
+double cut_group(const Shape* s, int n, int pairs, Cut* c) {
     const auto stages = [&](int i, int kb) { return (int64_t)kb * pairs * s[i].segs; };
     int64_t tiles = 0, units = 0;
     for (int i = 0; i < n; ++i) {
@@ -160,12 +235,12 @@ void cut_group(const Shape* s, int n, int pairs, Cut* c) {
     if (tiles >= 3 * kPairs) {
         const int i = n - 1;
         const int64_t rest = std::min<int64_t>(tiles % kPairs, c[i].tiles());
-        if (!rest) return;
+        if (!rest) return 0.0;
         const int want = (int)std::min<int64_t>(kPairs / rest, stages(i, c[i].nkb) / 8);
-        if (want < 2) return;
+        if (want < 2) return 0.0;
         share(i, want);
         if (c[i].shares > 1) c[i].whole = (int)(c[i].tiles() - rest);
-        return;
+        return 0.0;
     }
     int64_t longest = 0;
     for (int i = 0; i < n; ++i) longest = std::max(longest, stages(i, c[i].nkb));
@@ -195,14 +270,35 @@ void cut_group(const Shape* s, int n, int pairs, Cut* c) {
     share_all(best);
     for (int i = 0; i < n; ++i)
         if (c[i].shares > 1) c[i].whole = 0;
+    return least;
 }
-int64_t slot_bytes(const Cut& c) { return (c.tiles() - c.whole) * (c.shares > 1 ? c.shares : 0) * CT_M * c.width * 4; }
+int64_t slot_bytes(const Cut& c) { return c.split ? c.tiles() * c.shares * CT_M * c.width * 4 : (c.tiles() - c.whole) * (c.shares > 1 ? c.shares : 0) * CT_M * c.width * 4; }
+
+// kGate and kHidden: what is made of a finished tile is not additive, so tiles are whole and drained where they lie (`drain`: that of the last tile, in stages), or all sums go
+// to slots, of shares of the reduction where that helps, for a kernel that makes h (dg and du) of them: with few tiles.  Narrow tiles where their rounds are shorter all the same (22 wide tiles on
+// 74 pairs: 44 narrow ones).
+Cut cut_hidden(const Shape& s, int pairs, int drain) {
+    const Cut wide = whole_tiles(s, false), narrow = whole_tiles(s, true);
+    const auto rounds = [](const Cut& c) { return (double)((c.tiles() + kPairs - 1) / kPairs); };
+    const bool is_narrow = 0.75 * rounds(narrow) < rounds(wide) && wide.tiles() < 8 * kPairs;
+    Cut best = is_narrow ? narrow : wide;
+    if (wide.tiles() > 2 * kPairs) return best;
+    const double stages = (double)best.nkb * pairs, factor = is_narrow ? 0.75 : 1.0;
+    const double here = rounds(best) * factor * std::max(stages, (double)drain) + factor * drain;
+    Cut cut;
+    const double there = cut_group(&s, 1, pairs, &cut) + 16;
+    if (there >= here) return best;
+    cut.whole = cut.shares > 1 ? 0 : cut.whole;
+    cut.split = true;
+    return cut;
+}
 
 GatedArgs product(const Shape& s, const Cut& c, int dtype, bool a_mn, int group, int32_t* status) {
     GatedArgs g{};
     g.parts = dtype == GAD_F32 ? 3 : 1;
     g.segs = s.segs;
     g.a_mn = a_mn;
+    g.split = c.split;
     g.plane_tiles = (int)((s.M + CT_M - 1) / CT_M);
     g.t.M = (int)s.M; g.t.N = s.N;
     g.t.tiles_m = c.tiles_m; g.t.tiles_n = c.tiles_n; g.t.width = c.width;
@@ -250,6 +346,12 @@ cudaError_t go(GatedGroup<G>& g, Sequence& q) {
     g.p[0].clear = q.clear;
     q.clear = false;
     const cudaError_t e = add_up ? launch_gated<USE, LAYOUT, T, true>(g, q) : launch_gated<USE, LAYOUT, T, sizeof(T) == 4>(g, q);
+    if constexpr (USE != kPlain) {
+        if (e != cudaSuccess || !g.p[0].split) return e;
+        const TileArgs& a = g.p[0].t;
+        const int wide = USE == kGate ? a.width / 2 : a.width;
+        return q.launch(gated_hidden_join_kernel<USE, T>, dim3((unsigned)((int64_t)a.tiles_m * a.tiles_n * (CT_M * wide / 1024))), 256, 0, g.p[0]);
+    }
     if (e != cudaSuccess || j.first[kGroup] == 0) return e;
     return q.launch(gated_join_kernel<T>, dim3((unsigned)j.first[kGroup]), 256, 0, j);
 }
@@ -260,7 +362,7 @@ cudaError_t pack(std::initializer_list<const Operand*> all, uint8_t* ws, Sequenc
     for (const Operand* o : all)
         if (o->pack && o->src && o->rows > 0) {
             p.job[p.n] = {o->src, o->ld, (int)o->rows, o->cols, ws + o->at, o->ldp, o->rows * o->ldp};
-            p.first[p.n + 1] = p.first[p.n] + o->rows;
+            p.first[p.n + 1] = p.first[p.n] + o->rows * ((o->cols + kPackRun - 1) / kPackRun);
             ++p.n;
         }
     if (!p.n) return cudaSuccess;
@@ -329,7 +431,8 @@ ForwardPlan plan_forward(const gad_gated_args& a) {
         p.o_gate = room.take(parts(p.gate));
         p.o_slots = room.take(parts(p.down));
     } else {
-        p.hidden = cut_alone(gate_shape(a));
+        p.hidden = cut_hidden(gate_shape(a), a.dtype == GAD_F32 ? 6 : 1, a.dtype == GAD_F32 ? (a.act ? 90 : 60) : a.act ? 25 : 15);
+        p.o_gate = room.take(slot_bytes(p.hidden));
         const Shape s = out_shape(a);
         cut_group(&s, 1, a.dtype == GAD_F32 ? 6 : 1, &p.out);
         p.o_slots = room.take(slot_bytes(p.out));
@@ -393,6 +496,7 @@ cudaError_t run_forward(const gad_gated_args& a, uint8_t* ws, cudaStream_t s) {
     g.h_part = a.rows * g.ldh;
     g.act = a.act; g.ldact = a.ldact; g.slope = a.slope; g.ldslope = a.ldslope;
     g.C[0] = a.dtype == GAD_F32 ? a.h : nullptr; g.ldc[0] = a.ldh;
+    g.t.slots = reinterpret_cast<float*>(ws + p.o_gate);
     GAD_TRY(map_of(r.A[0], p.x, ws, parts, CT_H));
     GAD_TRY(map_of(r.B0[0], p.wg, ws, parts, (uint32_t)g.t.width / 2));
     GAD_TRY(map_of(r.B1[0], p.wu, ws, parts, (uint32_t)g.t.width / 2));
@@ -411,7 +515,7 @@ struct BackwardPlan {
     Cut hidden, cut[kGroup];
     Shape shape[kGroup];
     int n, at_x, at_gu, at_d;          // products behind dg and du, and which is which (-1: not wanted)
-    int64_t o_dg, ldg, o_slots[kGroup], total;
+    int64_t o_dg, ldg, o_hidden, o_slots[kGroup], total;
 };
 bool wants_hidden(const gad_gated_grad_args& a) { return a.dx || a.dw_gate || a.dw_up; }
 Shape hidden_shape(const gad_gated_grad_args& a) { return {a.rows, a.inner, a.cols, 1, 1}; }
@@ -429,7 +533,8 @@ BackwardPlan plan_backward(const gad_gated_grad_args& a) {
     p.ldg = round_up(a.inner, 8);
     if (hidden) {
         p.o_dg = room.take((a.dtype == GAD_F32 ? 12 : 4) * a.rows * p.ldg);
-        p.hidden = cut_alone(hidden_shape(a));
+        p.hidden = cut_hidden(hidden_shape(a), a.dtype == GAD_F32 ? 6 : 1, a.dtype == GAD_F32 ? 80 : 15);
+        p.o_hidden = room.take(slot_bytes(p.hidden));
     }
     p.at_x = p.at_gu = p.at_d = -1;
     if (a.dx) { p.at_x = p.n; p.shape[p.n++] = {a.rows, a.cols, a.inner, 1, 2}; }
@@ -457,6 +562,7 @@ cudaError_t run_backward(const gad_gated_grad_args& a, uint8_t* ws, cudaStream_t
         g = product(hidden_shape(a), p.hidden, a.dtype, false, 16, a.status);
         g.act = const_cast<void*>(a.act); g.ldact = a.ldact; g.slope = const_cast<void*>(a.slope); g.ldslope = a.ldslope;
         g.C[0] = dg; g.ldh = p.ldg; g.h_part = part;
+        g.t.slots = reinterpret_cast<float*>(ws + p.o_hidden);
         GAD_TRY(map_of(r.A[0], p.dy, ws, parts, CT_H));
         GAD_TRY(map_of(r.B0[0], p.wd, ws, parts, CT_K));
         GAD_TRY((go<kHidden, kBMN, T>(r, q)));

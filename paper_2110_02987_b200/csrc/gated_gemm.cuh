@@ -24,6 +24,7 @@ struct GatedArgs {
     int parts, segs;           // operand parts; segments of the reduction (t.pairs products each)
     int plane_tiles;           // row tiles of a plane
     int a_mn;                  // kAnyMN: A is MN-major
+    int split;                 // kGate, kHidden: sums go to t.slots, whole tiles' too, and what is made of them is the join's
     int activation;
     int clear;                 // the call's first product: its first block sets the status to zero (blocks come up in order, and a wait takes 2^22 polls to run out)
     void *C[2];                // kPlain: result of each plane; kGate with T = float: C[0] is h where it is kept, or null
@@ -46,15 +47,27 @@ template <int G> __device__ __forceinline__ int product_of(const GatedGroup<G>& 
 // Which operands are MN-major (the reduction runs over their rows): neither; B; B, and A as its product says (GatedArgs::a_mn).
 enum Layout { kBothK, kBMN, kAnyMN };
 
-// act(x) and act'(x).  The logistic function from exp2 and a reciprocal, each within 2 ulp.
+// exp(-x^2 / 2) for 0 <= x <= 20: what the square and its product with log2(e) / 2 round off is put back.
+__device__ __forceinline__ float exp_half_square(float x) {
+    const float c = 0.72134752f, c_lo = 2.0164e-9f, q = x * x, a = q * c;
+    const float lo = fmaf(q, c, -a) + fmaf(fmaf(x, x, -q), c, q * c_lo), e = exp2_fast(-a);
+    return fmaf(e, -0.693147181f * lo, e);
+}
+// act(x) and act'(x).  The logistic function from exp2 and a reciprocal, each within 2 ulp.  gelu: the normal distribution's tail is half of erfc(z), z = |x| / sqrt 2, by the
+// Chebyshev fit of Press et al., Numerical Recipes ("erfcc"): erfc(z) = t exp(-z^2 + p(t)), t = 1 / (1 + z / 2), within 1.2e-7 of itself; in fp32 3.3e-7.  (With erfcf the drain
+// of a tile took 13 us longer than relu's.)
 __device__ __forceinline__ void activation(int kind, float x, float& a, float& d) {
     if (kind == kRelu) {
         a = x > 0.f || x != x ? x : 0.f;                   // (what is no number stays none)
         d = x > 0.f ? 1.f : 0.f;
     } else if (kind == kGelu) {
-        const float cdf = 0.5f * erfcf(-0.707106781f * x);     // (erfc: no digits are lost in the left tail)
+        const float y = fminf(fabsf(x), 20.f), t = __fdividef(1.f, fmaf(0.5f * 0.707106781f, y, 1.f)), e = exp_half_square(y);   // (behind 20 the tail is zero; what is no number comes back with x)
+        float p = 0.17087277f;
+        p = fmaf(p, t, -0.82215223f); p = fmaf(p, t, 1.48851587f); p = fmaf(p, t, -1.13520398f); p = fmaf(p, t, 0.27886807f); p = fmaf(p, t, -0.18628806f);
+        p = fmaf(p, t, 0.09678418f); p = fmaf(p, t, 0.37409196f); p = fmaf(p, t, 1.00002368f); p = fmaf(p, t, -1.26551223f);
+        const float tail = 0.5f * t * (e * exp2_fast(1.44269504f * p)), cdf = x < 0.f ? tail : 1.f - tail;
         a = x == -INFINITY ? 0.f : x * cdf;
-        d = fabsf(x) == INFINITY ? cdf : fmaf(x, 0.398942280f * __expf(-0.5f * x * x), cdf);
+        d = fabsf(x) == INFINITY ? cdf : fmaf(x, 0.398942280f * e, cdf);
     } else {
         const float e = exp2_fast(-1.44269504f * x), s = __fdividef(1.f, 1.f + e);
         const float r = e == INFINITY ? 1.f : e * s;           // 1 - s
@@ -66,21 +79,60 @@ __device__ __forceinline__ void activation(int kind, float x, float& a, float& d
     }
 }
 
-// 32 values of a row from column c on; zeros behind its end.  wide: every row starts on 16 bytes.
+// The same of N values, g becomes act(g), with the kind looked at once: value by value the steps of one wait for one another.  (One way through for calls that keep the slope and calls that
+// do not: with code for each a tile of gelu took 10 us longer than relu's, and 4 with this.)
+template <int KIND, int N>
+__device__ __forceinline__ void activations_of(float (&g)[N], float (&d)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        float a;
+        activation(KIND, g[j], a, d[j]);
+        g[j] = a;
+    }
+}
+template <int N>
+__device__ __forceinline__ void activations(int kind, float (&g)[N], float (&d)[N]) {
+    if (kind == kSilu) activations_of<kSilu>(g, d);
+    else if (kind == kGelu) activations_of<kGelu>(g, d);
+    else if (kind == kRelu) activations_of<kRelu>(g, d);
+    else activations_of<kSigmoid>(g, d);
+}
+
+// 32 rows x 32 columns of a matrix on their way to the threads that have a row each: loaded as they lie, 64 bytes of eight rows at a time (a row a thread, the loads of a warp touched 32
+// lines each), and turned through the warp's staging buffer when they are wanted.  Zeros behind the matrix.  wide: every row starts on 16 bytes.
+template <class T> struct Block32 { uint4 u[2 * sizeof(T)]; };
 template <class T>
-__device__ __forceinline__ void load_row32(const T* __restrict__ row, int cols, bool wide, float (&v)[32]) {
+__device__ __forceinline__ void load_block32(const T* __restrict__ src, long long ld, int rows, int cols, bool wide, int lane, Block32<T>& b) {
     constexpr int VEC = 16 / sizeof(T);
-    if (wide && cols >= 32) {
 #pragma unroll
-        for (int i = 0; i < 32 / VEC; ++i) {
-            float w[VEC];
-            unpack_vec<T, VEC>(reinterpret_cast<const uint4*>(row)[i], w);
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) {
+        const int r = (i & 3) * 8 + (lane >> 2), c = (i >> 2) * (4 * VEC) + (lane & 3) * VEC;
+        const T* at = src + r * ld + c;
+        if (wide && r < rows && c + VEC <= cols) b.u[i] = *reinterpret_cast<const uint4*>(at);
+        else {
+            union { uint4 u; T e[VEC]; } w;
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) v[i * VEC + j] = w[j];
+            for (int j = 0; j < VEC; ++j) w.e[j] = r < rows && c + j < cols ? at[j] : from_float<T>(0.f);
+            b.u[i] = w.u;
         }
-    } else {
+    }
+}
+template <class T>
+__device__ __forceinline__ void take_block32(uint8_t* buf, int lane, const Block32<T>& b, float (&v)[32]) {
+    constexpr int VEC = 16 / sizeof(T);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = j < cols ? to_float(row[j]) : 0.f;
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(staged(buf, i * 8 + (lane >> 2), lane & 3)) = b.u[4 * h + i];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float w[VEC];
+            unpack_vec<T, VEC>(*reinterpret_cast<const uint4*>(staged(buf, lane, i)), w);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[(h * 4 + i) * VEC + j] = w[j];
+        }
     }
 }
 
@@ -88,17 +140,29 @@ __device__ __forceinline__ void load_row32(const T* __restrict__ row, int cols, 
 template <class T>
 __device__ __forceinline__ void drain_operand(uint8_t* buf, int lane, float (&v)[32], void* out, long long at, long long part, long long ld, int rows, int cols) {
     if constexpr (sizeof(T) == 4) {
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) top = fmaxf(top, fabsf(v[j]));
+        const bool large = top > 3.38e38f;                 // (a finite value that would round to infinity stays finite)
 #pragma unroll 1
         for (int k = 0; k < 3; ++k) {
-            float p[32];
+            uint32_t w[16];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                __nv_bfloat16 b = __float2bfloat16_rn(v[j]);
-                if (__hisinf(b) && !isinf(v[j])) b = __ushort_as_bfloat16((unsigned short)(0x7F7F | (__float_as_uint(v[j]) >> 31 << 15)));   // a finite value stays finite
-                p[j] = __bfloat162float(b);
-                v[j] -= p[j];
+            for (int j = 0; j < 16; ++j) {
+                w[j] = Pair<__nv_bfloat16>::pack(v[2 * j], v[2 * j + 1]);
+                if (large) {
+                    if ((w[j] & 0x7FFFu) == 0x7F80u && !isinf(v[2 * j])) --w[j];
+                    if ((w[j] & 0x7FFF0000u) == 0x7F800000u && !isinf(v[2 * j + 1])) w[j] -= 0x10000u;
+                }
+                const float2 f = Pair<__nv_bfloat16>::unpack(w[j]);
+                v[2 * j] -= f.x;
+                v[2 * j + 1] -= f.y;
             }
-            drain_rows<__nv_bfloat16>(buf, lane, p, reinterpret_cast<__nv_bfloat16*>(out) + k * part + at, ld, rows, cols, 16);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(staged(buf, lane, j)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+            __syncwarp();
+            copy_out<16, __nv_bfloat16, false>(buf, lane, reinterpret_cast<__nv_bfloat16*>(out) + k * part + at, ld, rows, cols);
         }
     } else {
         drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(out) + at, ld, rows, cols, 16);
@@ -246,7 +310,6 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
             const TileAt t = tile_at(a, u - gr.first[which]);
             const int plane = t.m / ga.plane_tiles, tm = t.m - plane * ga.plane_tiles;
             const int row0 = tm * CT_M + (int)rank * CT_H + q * 32, rows = a.M - row0;   // this warp's rows
-            const int row = row0 + lane;
             const uint32_t tm_row = tmem_base + ((uint32_t)(q * 32) << 16);
             const auto release = [&]() {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -254,6 +317,13 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
                 if (lane == 0) mbar_arrive_leader_tmem(tempty(acc));
                 if (++acc == NACC) { acc = 0; acc_phase ^= 1u; }
             };
+            // kHidden: the factors of 32 columns are on their way before the product is waited for
+            Block32<T> slope, act;
+            const auto load_factors = [&](int col) {
+                load_block32<T>(reinterpret_cast<const T*>(ga.slope) + (long long)row0 * ga.ldslope + col, ga.ldslope, rows, a.N - col, store(ga.slope, ga.ldslope) == 16, lane, slope);
+                load_block32<T>(reinterpret_cast<const T*>(ga.act) + (long long)row0 * ga.ldact + col, ga.ldact, rows, a.N - col, store(ga.act, ga.ldact) == 16, lane, act);
+            };
+            if (USE == kHidden && !ADD_UP) load_factors(t.n * a.width + half * half_w);   // (beside the sums of chunks they would spill)
             bool ok = true;
             const auto wait_full = [&]() {
                 ok = __all_sync(0xffffffffu, mbar_wait(tfull(acc), acc_phase, abort_flag, err, 46));
@@ -290,7 +360,17 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
                 tmem_wait_st();
             } else if (!wait_full()) break;
             const uint32_t at = tm_row + (uint32_t)(acc * ACC_COLS);
-            if constexpr (USE == kGate) {
+            const int slot = USE != kPlain && ga.split && t.slot < 0 ? u - gr.first[which] : t.slot;
+            if (slot >= 0) {
+                for (int c0 = 0; c0 < half_w; c0 += 32) {
+                    if (rows <= 0) break;
+                    float v[32];
+                    __syncwarp();
+                    tmem_ld32(at + (uint32_t)(half * half_w + c0), v);
+                    drain_rows<float>(buf, lane, v, a.slots + (long long)slot * CT_M * a.width + (long long)((int)rank * CT_H + q * 32) * a.width + half * half_w + c0, a.width, 32, 32, 16);
+                }
+                release();
+            } else if constexpr (USE == kGate) {
                 for (int c = 0; c < of_g; ++c) {
                     const int col = t.n * half_w + half * (half_w / 2) + 32 * c, cols = a.N - col;
                     if (rows <= 0 || cols <= 0) break;
@@ -300,25 +380,17 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
                     tmem_ld32_start(at + (uint32_t)block_at(c + of_g), v);
                     tmem_ld32_wait(g);
                     tmem_ld32_wait(v);
-                    if (ga.act) {
-                        float s[32];
+                    float d[32];
+                    activations(ga.activation, g, d);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            float d;
-                            activation(ga.activation, g[j], g[j], d);
-                            s[j] = v[j] * d;
-                            v[j] *= g[j];
-                        }
-                        drain_rows<T>(buf, lane, s, reinterpret_cast<T*>(ga.slope) + (long long)row0 * ga.ldslope + col, ga.ldslope, rows, cols, store(ga.slope, ga.ldslope));
+                    for (int j = 0; j < 32; ++j) {
+                        d[j] *= v[j];
+                        v[j] *= g[j];
+                    }
+                    if (ga.act) {
+                        drain_rows<T>(buf, lane, d, reinterpret_cast<T*>(ga.slope) + (long long)row0 * ga.ldslope + col, ga.ldslope, rows, cols, store(ga.slope, ga.ldslope));
                         drain_rows<T>(buf, lane, g, reinterpret_cast<T*>(ga.act) + (long long)row0 * ga.ldact + col, ga.ldact, rows, cols, store(ga.act, ga.ldact));
                         if (sizeof(T) == 4) drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(ga.C[0]) + (long long)row0 * ga.ldc[0] + col, ga.ldc[0], rows, cols, store(ga.C[0], ga.ldc[0]));
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            float d;
-                            activation(ga.activation, g[j], g[j], d);
-                            v[j] *= g[j];
-                        }
                     }
                     drain_operand<T>(buf, lane, v, ga.h, (long long)row0 * ga.ldh + col, ga.h_part, ga.ldh, rows, cols);
                 }
@@ -327,16 +399,19 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
                 for (int c0 = 0; c0 < half_w; c0 += 32) {
                     const int col = t.n * a.width + half * half_w + c0, cols = a.N - col;
                     if (rows <= 0 || cols <= 0) break;
-                    float dh[32], f[32], v[32];
+                    if (ADD_UP && c0 == 0) load_factors(col);
+                    float dh[32], v[32];
                     __syncwarp();
                     tmem_ld32(at + (uint32_t)(half * half_w + c0), dh);
-                    for (int k = 0; k < 2; ++k) {
-                        const T* src = reinterpret_cast<const T*>(k ? ga.act : ga.slope) + (long long)(row < a.M ? row : 0) * (k ? ga.ldact : ga.ldslope) + col;
-                        load_row32<T>(src, row < a.M ? cols : 0, store(k ? ga.act : ga.slope, k ? ga.ldact : ga.ldslope) == 16, f);
+                    take_block32<T>(buf, lane, slope, v);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = dh[j] * f[j];
-                        drain_operand<T>(buf, lane, v, ga.C[0], (long long)k * ga.parts * ga.h_part + (long long)row0 * ga.ldh + col, ga.h_part, ga.ldh, rows, cols);
-                    }
+                    for (int j = 0; j < 32; ++j) v[j] *= dh[j];
+                    drain_operand<T>(buf, lane, v, ga.C[0], (long long)row0 * ga.ldh + col, ga.h_part, ga.ldh, rows, cols);
+                    take_block32<T>(buf, lane, act, v);
+                    if (c0 + 32 < half_w) load_factors(col + 32);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] *= dh[j];
+                    drain_operand<T>(buf, lane, v, ga.C[0], (long long)ga.parts * ga.h_part + (long long)row0 * ga.ldh + col, ga.h_part, ga.ldh, rows, cols);
                 }
                 release();
             } else {
@@ -346,10 +421,7 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
                     float v[32];
                     __syncwarp();
                     tmem_ld32(at + (uint32_t)(half * half_w + c0), v);
-                    if (t.slot >= 0)
-                        drain_rows<float>(buf, lane, v, a.slots + (long long)t.slot * CT_M * a.width + (long long)((int)rank * CT_H + q * 32) * a.width + half * half_w + c0, a.width, 32, 32, 16);
-                    else
-                        drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(ga.C[plane]) + (long long)row0 * ga.ldc[plane] + col, ga.ldc[plane], rows, cols, store(ga.C[plane], ga.ldc[plane]));
+                    drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(ga.C[plane]) + (long long)row0 * ga.ldc[plane] + col, ga.ldc[plane], rows, cols, store(ga.C[plane], ga.ldc[plane]));
                 }
                 release();
             }

@@ -219,12 +219,13 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ 
                     asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory");
                     const int first = q < 2 ? 0 : 8;
                     T* out = reinterpret_cast<T*>(a.out) + (long long)(c0 + first) * a.ldo + unit_row;
+                    float g[8], d[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) g[j] = q < 2 ? v[j] : xg[j * 64 + local];
+                    activations(a.activation, g, d);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        float g, d;
-                        activation(a.activation, q < 2 ? v[j] : xg[j * 64 + local], g, d);
-                        g *= q < 2 ? xu[j * 64 + local] : v[8 + j];
-                        if (first + j < n && valid) *out = from_float<T>(g);
+                        if (first + j < n && valid) *out = from_float<T>(g[j] * (q < 2 ? xu[j * 64 + local] : v[8 + j]));
                         out += a.ldo;
                     }
                     asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory");

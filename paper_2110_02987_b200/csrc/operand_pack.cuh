@@ -26,6 +26,7 @@ __device__ __forceinline__ void pack_row(const T* __restrict__ src, int cols, bo
                 *reinterpret_cast<uint2*>(d + k * part_stride + 4 * c) = w.u;
             }
         }
+#pragma unroll 4
         for (int c = 4 * n4 + t; c < cols; c += threads) {
             __nv_bfloat16 p[3];
             split3(keep ? src[c] : 0.f, p);
@@ -45,7 +46,15 @@ __device__ __forceinline__ void pack_row(const T* __restrict__ src, int cols, bo
 #pragma unroll 4
             for (int c = t; c < n; c += threads) reinterpret_cast<uint32_t*>(d)[c] = keep ? reinterpret_cast<const uint32_t*>(src)[c] : 0u;
         }
-        for (int c = (wide > 1 ? wide * n : 0) + t; c < cols; c += threads) d[c] = keep ? src[c] : from_float<T>(0.f);
+        // (eight loads, then their stores: one value behind the other, 500 rows of 1433 single ones took 20 us)
+        for (int c = (wide > 1 ? wide * n : 0) + t; c < cols; c += 8 * threads) {
+            T v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = keep && c + j * threads < cols ? src[c + j * threads] : from_float<T>(0.f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c + j * threads < cols) d[c + j * threads] = v[j];
+        }
     }
 }
 
