@@ -186,8 +186,8 @@ struct Sequence {
 };
 
 // Blocks of 64 terms that the tensor core adds up before the sum moves to registers: it cuts its accumulator off at every addition, 2^-23 of the sum every 16 terms at most (see
-// class_gemm_kernel).  As for the head's gradients: fp32 results 256 terms, 16-bit ones as many as cost an eighth of their rounding at most.
-template <class T> constexpr int kGatedChunk = 4;
+// class_gemm_kernel).  As for the head's gradients, as many as cost an eighth of the results' rounding at most.  (fp32: one.)
+template <class T> constexpr int kGatedChunk = 1;
 template <> constexpr int kGatedChunk<__half> = 128;
 template <> constexpr int kGatedChunk<__nv_bfloat16> = 1024;
 

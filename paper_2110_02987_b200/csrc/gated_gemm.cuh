@@ -21,7 +21,7 @@ enum Activation { kSilu, kGelu, kRelu, kSigmoid };
 
 struct GatedArgs {
     TileArgs t;                // tiles and shares (M rows of a plane)
-    int parts, segs;           // operand parts; segments of the reduction (t.pairs products each)
+    int parts, segs;           // operand parts; segments of the reduction
     int plane_tiles;           // row tiles of a plane
     int a_mn;                  // kAnyMN: A is MN-major
     int split;                 // kGate, kHidden: sums go to t.slots, whole tiles' too, and what is made of them is the join's
@@ -169,12 +169,12 @@ __device__ __forceinline__ void drain_operand(uint8_t* buf, int lane, float (&v)
     }
 }
 
-// USE as above; T: type of the tensors; ADD_UP: sums in chunks (t.chunk), as class_gemm_kernel takes them; G: products a launch may have.  (With the layouts of all products and their number known only
+// USE as above; T: type of the tensors; ADD_UP: sums in chunks (t.chunk; of operands in parts, of one block of 64 terms each), as class_gemm_kernel takes them; G: products a launch may have.  (With the layouts of all products and their number known only
 // at run time, in one kernel for all uses, 8192 x 2048 x 5504 took 428 us instead of 416, and the gradients of 16 384 x 4096 x 10 240 6.2 ms instead of 5.8.)
 template <int USE, int LAYOUT, class T, bool ADD_UP, int G>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(CT_THREADS, 1)
 gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
-    constexpr bool B_MN = LAYOUT != kBothK;
+    constexpr bool B_MN = LAYOUT != kBothK, PARTS = sizeof(T) == 4;   // PARTS: operands in three parts
     int32_t* const err = gr.p[0].t.err;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
@@ -221,39 +221,43 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
             const TileArgs& a = ga.t;
             const CUtensorMap* tmA = &gr.A[which];
             const CUtensorMap *tmB0 = &gr.B0[which], *tmB1 = &gr.B1[which];
-            const int half_w = a.width / 2, pairs = a.pairs, parts = ga.parts, products = pairs * ga.segs;
+            const int half_w = a.width / 2;
             const bool a_mn = LAYOUT == kAnyMN && ga.a_mn;
             const uint32_t bytes = 2u * (uint32_t)(CT_H + half_w) * (CT_K * 2);
             const TileAt t = tile_at(a, u - gr.first[which]);
             const int plane = t.m / ga.plane_tiles;
             const int ra = (t.m - plane * ga.plane_tiles) * CT_M + (int)rank * CT_H;
             const int rb = USE == kGate ? t.n * half_w : t.n * a.width + (int)rank * half_w;
+            const auto load = [&](int kb, int za, int zb, const CUtensorMap* tmB) {
+                if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, err, 41))) return;
+                if (rank == 0) mbar_expect_tx(full(stage), bytes);
+                const uint32_t base = sm_addr + stage * CT_STAGE, bar = leader_address(full(stage));
+                if (a_mn) {
+                    tma_load_3d_pair(base, tmA, ra, kb * CT_K, za, bar);
+                    tma_load_3d_pair(base + 8192, tmA, ra + 64, kb * CT_K, za, bar);
+                } else {
+                    tma_load_3d_pair(base, tmA, kb * CT_K, ra, za, bar);
+                }
+                if (B_MN) {
+                    for (int j = 0; j < half_w; j += 64) tma_load_3d_pair(base + CT_OPERAND + j * 128, tmB, rb + j, kb * CT_K, zb, bar);
+                } else {
+                    tma_load_3d_pair(base + CT_OPERAND, tmB, kb * CT_K, rb, zb, bar);
+                }
+                if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
+            };
+            const auto source = [&](int seg) { return (USE == kGate ? (int)rank : seg) ? tmB1 : tmB0; };
+            if constexpr (PARTS) {
+                // all parts of a block of the reduction, in the order in which the products let go of them
+                for (int seg = 0; seg < ga.segs && ok; ++seg)
+                    for (int kb = t.kb0; kb < t.kb0 + t.nkb && ok; ++kb)
+                        for (int p = 2; p >= 0 && ok; --p) load(kb, (plane + seg) * 3 + p, p, source(seg));
+                continue;
+            }
             const int group = ADD_UP ? a.chunk : t.nkb;
             for (int g = 0; g < t.nkb && ok; g += group)
-                for (int p = 0; p < products && ok; ++p) {
-                    const int seg = p >= pairs ? 1 : 0;
-                    int za, zb;
-                    part_pair(p - seg * pairs, pairs, za, zb);
-                    za += (plane + seg) * parts;
-                    const CUtensorMap* tmB = (USE == kGate ? (int)rank : seg) ? tmB1 : tmB0;
+                for (int seg = 0; seg < ga.segs && ok; ++seg) {
                     const int last = t.kb0 + min(g + group, t.nkb);
-                    for (int kb = t.kb0 + g; kb < last; ++kb) {
-                        if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, err, 41))) break;
-                        if (rank == 0) mbar_expect_tx(full(stage), bytes);
-                        const uint32_t base = sm_addr + stage * CT_STAGE, bar = leader_address(full(stage));
-                        if (a_mn) {
-                            tma_load_3d_pair(base, tmA, ra, kb * CT_K, za, bar);
-                            tma_load_3d_pair(base + 8192, tmA, ra + 64, kb * CT_K, za, bar);
-                        } else {
-                            tma_load_3d_pair(base, tmA, kb * CT_K, ra, za, bar);
-                        }
-                        if (B_MN) {
-                            for (int j = 0; j < half_w; j += 64) tma_load_3d_pair(base + CT_OPERAND + j * 128, tmB, rb + j, kb * CT_K, zb, bar);
-                        } else {
-                            tma_load_3d_pair(base + CT_OPERAND, tmB, kb * CT_K, rb, zb, bar);
-                        }
-                        if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
-                    }
+                    for (int kb = t.kb0 + g; kb < last && ok; ++kb) load(kb, plane + seg, 0, source(seg));
                 }
         }
     } else if (warp == 1 && rank == 0) {
@@ -270,7 +274,44 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
             const uint32_t stepA = a_mn ? 128 : 2;
             constexpr uint32_t stepB = B_MN ? 128 : 2;                        // 16 values of the reduction: 16 rows of 128 bytes, or 32 bytes of a row
             const uint64_t descA = a_mn ? operand_desc<true>(0) : operand_desc<false>(0);
-            const int products = a.pairs * ga.segs, steps = tile_at(a, u - gr.first[which]).nkb * products, chunk = a.chunk * products;
+            const int steps = tile_at(a, u - gr.first[which]).nkb * ga.segs, chunk = a.chunk * ga.segs;
+            if constexpr (PARTS) {
+                // the six products of the parts that reach 2^-24, the smallest first, in an accumulator of each block's own: what an addition cuts off is little, as the accumulator is small for
+                // most of them, and each part comes from the L2 once.  (A stage a product, with each part loaded two or three times, was bound by the L2: 4345 x 4005 x 632 460 us, now 401.)
+                for (int i = 0; i < steps; ++i) {
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait<true>(tempty(acc), acc_phase ^ 1u, abort_flag, err, 42)))) break;
+                    uint32_t base[3], bar[3];
+                    for (int p = 2; p >= 0 && ok; --p) {
+                        ok = __all_sync(0xffffffffu, mbar_wait<true>(full(stage), phase, abort_flag, err, 43));
+                        base[p] = sm_addr + stage * CT_STAGE;
+                        bar[p] = empty(stage);
+                        if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t d = tmem_base + (uint32_t)(acc * ACC_COLS);
+                    if (elect_one()) {
+                        const auto multiply = [&](int pa, int pb, bool first) {
+                            const uint64_t da = descA | (base[pa] >> 4), db = operand_desc<B_MN>(base[pb] + CT_OPERAND);
+#pragma unroll
+                            for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_pair(d, da + stepA * ks, db + stepB * ks, idesc, !first || ks != 0 ? 1u : 0u);
+                        };
+                        multiply(0, 2, true);
+                        multiply(2, 0, false);
+                        mma_commit2(bar[2]);
+                        multiply(1, 1, false);
+                        multiply(0, 1, false);
+                        multiply(1, 0, false);
+                        mma_commit2(bar[1]);
+                        multiply(0, 0, false);
+                        mma_commit2(bar[0]);
+                        mma_commit2(tfull(acc));
+                    }
+                    __syncwarp();
+                    if (++acc == NACC) { acc = 0; acc_phase ^= 1u; }
+                }
+                continue;
+            }
             int left = 0;                                          // stages until this accumulator is full
             for (int i = 0; i < steps; ++i) {
                 const bool first = left == 0;
@@ -334,7 +375,7 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
             const int blocks = half_w / 32, of_g = blocks / 2;
             const auto block_at = [&](int c) { return USE != kGate ? half * half_w + 32 * c : c < of_g ? half * (half_w / 2) + 32 * c : half_w + half * (half_w / 2) + 32 * (c - of_g); };
             if constexpr (ADD_UP) {
-                const int chunks = (t.nkb + a.chunk - 1) / a.chunk;
+                const int chunks = PARTS ? t.nkb * ga.segs : (t.nkb + a.chunk - 1) / a.chunk;
                 float sum[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
@@ -362,12 +403,13 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
             const uint32_t at = tm_row + (uint32_t)(acc * ACC_COLS);
             const int slot = USE != kPlain && ga.split && t.slot < 0 ? u - gr.first[which] : t.slot;
             if (slot >= 0) {
-                for (int c0 = 0; c0 < half_w; c0 += 32) {
+                // (this warp's own blocks: those of the other half may not have been put back yet)
+                for (int c = 0; c < blocks; ++c) {
                     if (rows <= 0) break;
                     float v[32];
                     __syncwarp();
-                    tmem_ld32(at + (uint32_t)(half * half_w + c0), v);
-                    drain_rows<float>(buf, lane, v, a.slots + (long long)slot * CT_M * a.width + (long long)((int)rank * CT_H + q * 32) * a.width + half * half_w + c0, a.width, 32, 32, 16);
+                    tmem_ld32(at + (uint32_t)block_at(c), v);
+                    drain_rows<float>(buf, lane, v, a.slots + (long long)slot * CT_M * a.width + (long long)((int)rank * CT_H + q * 32) * a.width + block_at(c), a.width, 32, 32, 16);
                 }
                 release();
             } else if constexpr (USE == kGate) {

@@ -262,6 +262,21 @@ def test_equal_calls_streams_and_graphs():
 
 
 @gpu
+@pytest.mark.parametrize("N,D,F", [(257, 512, 320), (100, 500, 128), (300, 700, 1440)])
+def test_calls_whose_tiles_go_to_slots_give_equal_bits(N, D, F):
+    """Few tiles of fp32: what a warp reads back of its sums is its own."""
+    import torch
+    s = make(N, D, F, "float32", 30)
+    dy = matrix(N, D, torch.float32, torch.Generator().manual_seed(31))
+    want = None
+    for _ in range(30):
+        r = pkg.gated_feed_forward(**s, save=True)
+        got = tuple(r) + tuple(pkg.gated_feed_forward_backward(dy, **s, act=r.act, slope=r.slope, h=r.h))
+        want = want or got
+        assert all(torch.equal(u, v) for u, v in zip(got, want))
+
+
+@gpu
 def test_no_rows():
     import torch
     W, Wd = torch.ones(10, 16, device="cuda"), torch.ones(16, 10, device="cuda")
