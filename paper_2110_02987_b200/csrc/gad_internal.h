@@ -181,6 +181,7 @@ int tc_rows_bn_whole(int n_cols, int npairs);                // of the others
 int tc_tn_rows();   // rows of the row-box descriptors the weight-gradient kernel reads (mapH / mapZ of launch_gemm_tn_tc)
 bool tc_make_map(void* out_map, const void* base, uint64_t inner, uint64_t rows, uint64_t outer, uint64_t row_stride_bytes,
                  uint64_t outer_stride_bytes, uint32_t box_rows, bool mn_major = false, bool half = false);
+bool tc_make_chunk_map(void* out_map, const void* base, uint64_t chunks, uint64_t rows, uint64_t outer, uint64_t row_stride_bytes, uint64_t outer_stride_bytes, uint32_t box_chunks);
 struct SplitLayer {
     int fi, fo, ldw, ldkt;
     long long w_int;

@@ -293,6 +293,18 @@ Cut cut_hidden(const Shape& s, int pairs, int drain) {
     return cut;
 }
 
+// The same for an operand whose columns are what the result has rows or columns of (the reduction runs over its rows), `box` of them a CTA and stage: with chunks of 64 columns as a dimension
+// where rows have whole chunks.
+cudaError_t map_mn(CUtensorMap& m, const void* base, int64_t ld, int64_t rows, int cols, int planes, int box, int& chunks) {
+    chunks = cols % 64 == 0;
+    const bool ok = chunks ? tc_make_chunk_map(&m, base, (uint64_t)cols / 64, (uint64_t)rows, (uint64_t)planes, (uint64_t)ld * 2, (uint64_t)(ld * 2 * rows), (uint32_t)box / 64)
+                           : tc_make_map(&m, base, (uint64_t)cols, (uint64_t)rows, (uint64_t)planes, (uint64_t)ld * 2, (uint64_t)(ld * 2 * rows), CT_K, false, true);
+    return ok ? cudaSuccess : cudaErrorInvalidValue;
+}
+cudaError_t map_mn(CUtensorMap& m, const Operand& o, uint8_t* ws, int parts, int box, int& chunks) {
+    return map_mn(m, o.pack ? ws + o.at : o.src, o.pack ? o.ldp : o.ld, o.rows, o.cols, parts, box, chunks);
+}
+
 GatedArgs product(const Shape& s, const Cut& c, int dtype, bool a_mn, int group, int32_t* status) {
     GatedArgs g{};
     g.parts = dtype == GAD_F32 ? 3 : 1;
@@ -316,8 +328,8 @@ cudaError_t launch_gated(const GatedGroup<G>& g, Sequence& q) {
     cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), CT_SMEM, false);
     if (e != cudaSuccess) return e;
     static std::atomic<int> known{0};
-    if (known.load() <= 0) known.store(max_active_pairs(reinterpret_cast<const void*>(kernel), CT_THREADS, CT_SMEM, 2 * kPairs));
-    return q.launch(kernel, dim3((unsigned)(2 * std::min(g.first[G], known.load()))), CT_THREADS, CT_SMEM, g);
+    if (known.load() <= 0) known.store(max_active_pairs(reinterpret_cast<const void*>(kernel), GG_THREADS, CT_SMEM, 2 * kPairs));
+    return q.launch(kernel, dim3((unsigned)(2 * std::min(g.first[G], known.load()))), GG_THREADS, CT_SMEM, g);
 }
 
 // A launch of g.n products, and the join of the tiles that were cut.
@@ -564,12 +576,9 @@ cudaError_t run_backward(const gad_gated_grad_args& a, uint8_t* ws, cudaStream_t
         g.C[0] = dg; g.ldh = p.ldg; g.h_part = part;
         g.t.slots = reinterpret_cast<float*>(ws + p.o_hidden);
         GAD_TRY(map_of(r.A[0], p.dy, ws, parts, CT_H));
-        GAD_TRY(map_of(r.B0[0], p.wd, ws, parts, CT_K));
+        GAD_TRY(map_mn(r.B0[0], p.wd, ws, parts, g.t.width / 2, g.b_chunks));
         GAD_TRY((go<kHidden, kBMN, T>(r, q)));
     }
-    const auto map_dg = [&](CUtensorMap& m, int plane, int planes, uint32_t box) {
-        return tc_make_map(&m, dg + plane * parts * part * 2, (uint64_t)a.inner, (uint64_t)N, (uint64_t)(planes * parts), (uint64_t)p.ldg * 2, (uint64_t)part * 2, box, false, true) ? cudaSuccess : cudaErrorInvalidValue;
-    };
     GatedGroup<kGroup> r{};
     r.n = p.n;
     for (int i = 0; i < p.n; ++i) {
@@ -579,22 +588,22 @@ cudaError_t run_backward(const gad_gated_grad_args& a, uint8_t* ws, cudaStream_t
     if (p.at_x >= 0) {
         const int i = p.at_x;
         r.p[i].C[0] = a.dx; r.p[i].ldc[0] = a.lddx;
-        GAD_TRY(map_dg(r.A[i], 0, 2, CT_H));
-        GAD_TRY(map_of(r.B0[i], p.wg, ws, parts, CT_K));
-        GAD_TRY(map_of(r.B1[i], p.wu, ws, parts, CT_K));
+        if (!tc_make_map(&r.A[i], dg, (uint64_t)a.inner, (uint64_t)N, (uint64_t)(2 * parts), (uint64_t)p.ldg * 2, (uint64_t)part * 2, CT_H, false, true)) return cudaErrorInvalidValue;
+        GAD_TRY(map_mn(r.B0[i], p.wg, ws, parts, r.p[i].t.width / 2, r.p[i].b_chunks));
+        GAD_TRY(map_mn(r.B1[i], p.wu, ws, parts, r.p[i].t.width / 2, r.p[i].b_chunks));
     }
     if (p.at_gu >= 0) {
         const int i = p.at_gu;
         r.p[i].C[0] = a.dw_gate ? a.dw_gate : a.dw_up; r.p[i].ldc[0] = a.dw_gate ? a.lddwg : a.lddwu;
         r.p[i].C[1] = a.dw_up; r.p[i].ldc[1] = a.lddwu;
-        GAD_TRY(map_dg(r.A[i], a.dw_gate ? 0 : 1, p.shape[i].planes, CT_K));
-        GAD_TRY(map_of(r.B0[i], p.x, ws, parts, CT_K));
+        GAD_TRY(map_mn(r.A[i], dg + (a.dw_gate ? 0 : 1) * parts * part * 2, p.ldg, N, a.inner, p.shape[i].planes * parts, CT_H, r.p[i].a_chunks));
+        GAD_TRY(map_mn(r.B0[i], p.x, ws, parts, r.p[i].t.width / 2, r.p[i].b_chunks));
     }
     if (p.at_d >= 0) {
         const int i = p.at_d;
         r.p[i].C[0] = a.dw_down; r.p[i].ldc[0] = a.lddwd;
-        GAD_TRY(map_of(r.A[i], p.dy, ws, parts, CT_K));
-        GAD_TRY(map_of(r.B0[i], p.h, ws, parts, CT_K));
+        GAD_TRY(map_mn(r.A[i], p.dy, ws, parts, CT_H, r.p[i].a_chunks));
+        GAD_TRY(map_mn(r.B0[i], p.h, ws, parts, r.p[i].t.width / 2, r.p[i].b_chunks));
     }
     GAD_TRY((go<kPlain, kAnyMN, T>(r, q)));
     return cudaGetLastError();

@@ -10,13 +10,24 @@
 // one another (dx, both of these, dWd) are one launch, whose tiles are gone through one product behind the other.
 #pragma once
 
+#include <type_traits>
+
 #include "class_gemm.cuh"
 
 namespace gad {
 
 namespace {
 
+constexpr int GG_LOADER_B = CT_EPI_WARP0 + CT_EPI_WARPS, GG_THREADS = 32 * (GG_LOADER_B + 1);   // the warp that loads B comes last
+
 enum GatedUse { kGate, kHidden, kPlain };
+// A box of 64 columns x 64 rows x (one or two) chunks of columns.
+__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap* map, int y, int chunk, int z, uint32_t leader_bar) {
+    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(chunk), "r"(z), "r"(leader_bar)
+                 : "memory");
+}
+
 enum Activation { kSilu, kGelu, kRelu, kSigmoid };
 
 struct GatedArgs {
@@ -24,6 +35,7 @@ struct GatedArgs {
     int parts, segs;           // operand parts; segments of the reduction
     int plane_tiles;           // row tiles of a plane
     int a_mn;                  // kAnyMN: A is MN-major
+    int a_chunks, b_chunks;    // MN-major: the descriptor has chunks of 64 columns as a dimension (tc_make_chunk_map), so a box holds all that a CTA has of a stage
     int split;                 // kGate, kHidden: sums go to t.slots, whole tiles' too, and what is made of them is the join's
     int activation;
     int clear;                 // the call's first product: its first block sets the status to zero (blocks come up in order, and a wait takes 2^22 polls to run out)
@@ -172,7 +184,7 @@ __device__ __forceinline__ void drain_operand(uint8_t* buf, int lane, float (&v)
 // USE as above; T: type of the tensors; ADD_UP: sums in chunks (t.chunk; of operands in parts, of one block of 64 terms each), as class_gemm_kernel takes them; G: products a launch may have.  (With the layouts of all products and their number known only
 // at run time, in one kernel for all uses, 8192 x 2048 x 5504 took 428 us instead of 416, and the gradients of 16 384 x 4096 x 10 240 6.2 ms instead of 5.8.)
 template <int USE, int LAYOUT, class T, bool ADD_UP, int G>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(CT_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GG_THREADS, 1)
 gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
     constexpr bool B_MN = LAYOUT != kBothK, PARTS = sizeof(T) == 4;   // PARTS: operands in three parts
     int32_t* const err = gr.p[0].t.err;
@@ -210,56 +222,55 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
 
     const int ncl = gridDim.x >> 1, units = gr.first[G];
 
-    if (warp == 0 && lane == 0) {
-        // ---------------- TMA producer: this CTA's rows of A and half of the columns' rows of B; the leader's barrier counts both CTAs' bytes ----------------
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (int u = blockIdx.x >> 1; u < units && ok; u += ncl) {
-            const int which = product_of(gr, u);
-            const GatedArgs& ga = gr.p[which];
-            const TileArgs& a = ga.t;
-            const CUtensorMap* tmA = &gr.A[which];
-            const CUtensorMap *tmB0 = &gr.B0[which], *tmB1 = &gr.B1[which];
-            const int half_w = a.width / 2;
-            const bool a_mn = LAYOUT == kAnyMN && ga.a_mn;
-            const uint32_t bytes = 2u * (uint32_t)(CT_H + half_w) * (CT_K * 2);
-            const TileAt t = tile_at(a, u - gr.first[which]);
-            const int plane = t.m / ga.plane_tiles;
-            const int ra = (t.m - plane * ga.plane_tiles) * CT_M + (int)rank * CT_H;
-            const int rb = USE == kGate ? t.n * half_w : t.n * a.width + (int)rank * half_w;
-            const auto load = [&](int kb, int za, int zb, const CUtensorMap* tmB) {
-                if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, err, 41))) return;
-                if (rank == 0) mbar_expect_tx(full(stage), bytes);
-                const uint32_t base = sm_addr + stage * CT_STAGE, bar = leader_address(full(stage));
-                if (a_mn) {
-                    tma_load_3d_pair(base, tmA, ra, kb * CT_K, za, bar);
-                    tma_load_3d_pair(base + 8192, tmA, ra + 64, kb * CT_K, za, bar);
-                } else {
-                    tma_load_3d_pair(base, tmA, kb * CT_K, ra, za, bar);
-                }
-                if (B_MN) {
-                    for (int j = 0; j < half_w; j += 64) tma_load_3d_pair(base + CT_OPERAND + j * 128, tmB, rb + j, kb * CT_K, zb, bar);
-                } else {
-                    tma_load_3d_pair(base + CT_OPERAND, tmB, kb * CT_K, rb, zb, bar);
-                }
-                if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
-            };
-            const auto source = [&](int seg) { return (USE == kGate ? (int)rank : seg) ? tmB1 : tmB0; };
-            if constexpr (PARTS) {
-                // all parts of a block of the reduction, in the order in which the products let go of them
-                for (int seg = 0; seg < ga.segs && ok; ++seg)
-                    for (int kb = t.kb0; kb < t.kb0 + t.nkb && ok; ++kb)
-                        for (int p = 2; p >= 0 && ok; --p) load(kb, (plane + seg) * 3 + p, p, source(seg));
-                continue;
+    if ((warp == 0 || warp == GG_LOADER_B) && lane == 0) {
+        // ---------------- TMA producers, one for each operand: this CTA's rows of A, and half of the columns' rows of B; the leader's barrier counts both CTAs' bytes.  (One thread for
+        // both was the bound of MN-major operands, whose stage has two boxes of 64 columns each: dx, dWg and dWu, dWd of 4096 x 2048 x 5504 in 325 us, with these 300.) ----------------
+        const auto produce = [&](auto of_a) {
+            constexpr bool OF_A = decltype(of_a)::value;
+            const uint32_t leader = leader_address(full(0));
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int u = blockIdx.x >> 1; u < units && ok; u += ncl) {
+                const int which = product_of(gr, u);
+                const GatedArgs& ga = gr.p[which];
+                const TileArgs& a = ga.t;
+                const int half_w = a.width / 2;
+                const bool mn = OF_A ? LAYOUT == kAnyMN && ga.a_mn : B_MN, chunks = OF_A ? ga.a_chunks : ga.b_chunks;
+                const uint32_t bytes = 2u * (uint32_t)(CT_H + half_w) * (CT_K * 2);
+                const TileAt t = tile_at(a, u - gr.first[which]);
+                const int plane = t.m / ga.plane_tiles;
+                // first row of the operand's share
+                const int r = OF_A ? (t.m - plane * ga.plane_tiles) * CT_M + (int)rank * CT_H : USE == kGate ? t.n * half_w : t.n * a.width + (int)rank * half_w;
+                const bool two = mn && !chunks && (OF_A || half_w > 64);      // two boxes of 64 columns a stage
+                const auto load = [&](const CUtensorMap* map, int kb, int z) {
+                    if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, err, OF_A ? 41 : 44))) return;
+                    if (OF_A && rank == 0) mbar_expect_tx(full(stage), bytes);
+                    const uint32_t to = sm_addr + stage * CT_STAGE + (OF_A ? 0 : CT_OPERAND), bar = leader + 8u * stage;
+                    if (!mn) tma_load_3d_pair(to, map, kb * CT_K, r, z, bar);
+                    else if (chunks) tma_load_4d_pair(to, map, kb * CT_K, r >> 6, z, bar);
+                    else {
+                        tma_load_3d_pair(to, map, r, kb * CT_K, z, bar);
+                        if (two) tma_load_3d_pair(to + 8192, map, r + 64, kb * CT_K, z, bar);
+                    }
+                    if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
+                };
+                const int group = ADD_UP && !PARTS ? a.chunk : t.nkb;
+                for (int g = 0; g < t.nkb && ok; g += group)
+                    for (int seg = 0; seg < ga.segs && ok; ++seg) {
+                        const CUtensorMap* map = OF_A ? &gr.A[which] : (USE == kGate ? (int)rank : seg) ? &gr.B1[which] : &gr.B0[which];
+                        const int last = t.kb0 + min(g + group, t.nkb), z = OF_A ? plane + seg : 0;
+                        for (int kb = t.kb0 + g; kb < last && ok; ++kb) {
+                            if constexpr (PARTS) {
+                                // all parts of a block of the reduction, in the order in which the products let go of them
+                                for (int p = 2; p >= 0 && ok; --p) load(map, kb, 3 * z + p);
+                            } else load(map, kb, z);
+                        }
+                    }
             }
-            const int group = ADD_UP ? a.chunk : t.nkb;
-            for (int g = 0; g < t.nkb && ok; g += group)
-                for (int seg = 0; seg < ga.segs && ok; ++seg) {
-                    const int last = t.kb0 + min(g + group, t.nkb);
-                    for (int kb = t.kb0 + g; kb < last && ok; ++kb) load(kb, plane + seg, 0, source(seg));
-                }
-        }
+        };
+        if (warp == 0) produce(std::true_type());
+        else produce(std::false_type());
     } else if (warp == 1 && rank == 0) {
         // ---------------- MMA issuer (leader of the pair): the whole warp runs the loop, one elected lane issues ----------------
         int stage = 0, acc = 0;
@@ -336,7 +347,7 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
                 if (--left == 0 && ++acc == NACC) { acc = 0; acc_phase ^= 1u; }
             }
         }
-    } else if (warp >= CT_EPI_WARP0) {   // (warp 1 of the other CTA has nothing to do)
+    } else if (warp >= CT_EPI_WARP0 && warp < GG_LOADER_B) {   // (warp 1 of the other CTA has nothing to do)
         // ---------------- drain: this warp's 32 rows (a row a lane) x half of the tile's columns (kGate: half of g and of u) ----------------
         const int ew = warp - CT_EPI_WARP0, q = warp & 3, half = ew >> 2;
         uint8_t* buf = sm + CT_RING + 256 + CT_BIAS + ew * 2048;

@@ -97,6 +97,19 @@ bool tc_make_map(void* out_map, const void* base, uint64_t inner, uint64_t rows,
     return r == CUDA_SUCCESS;
 }
 
+// 16-bit tensor [outer] x [rows] x [64 chunks columns], the 64 columns of a chunk as the innermost dimension and the chunks as one of their own: a box is 64 rows of `box_chunks` chunks, which lie in
+// shared memory one behind the other.  For operands that are read along their columns; rows have whole chunks.
+bool tc_make_chunk_map(void* out_map, const void* base, uint64_t chunks, uint64_t rows, uint64_t outer, uint64_t row_stride_bytes, uint64_t outer_stride_bytes, uint32_t box_chunks) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[4] = {64, rows, chunks, outer};
+    cuuint64_t strides[3] = {row_stride_bytes, 128, outer_stride_bytes};
+    cuuint32_t box[4] = {64, 64, box_chunks, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(reinterpret_cast<CUtensorMap*>(out_map), CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 cudaError_t launch_expire_wait(int32_t* err, uint32_t polls, cudaStream_t s) {
     expire_wait_kernel<<<1, 32, 0, s>>>(err, polls);
     ++g_kernel_launches;
