@@ -21,6 +21,7 @@
 
 #include "class_gemm.cuh"
 #include "operand_pack.cuh"
+#include "skinny.cuh"
 
 namespace gad {
 
@@ -476,6 +477,185 @@ __global__ void __launch_bounds__(32 * kSomeWarps, 1) class_some_kernel(const Fe
     a.stats[(long long)blockIdx.x * a.rows + threadIdx.x] = at;
 }
 
+// Log-probabilities of 3 to 64 rows' actions (16-bit operands, no gradients: scoring), bound by reading W: classes as the rows of the product (skinny.cuh), a class a thread, sixteen rows of H in its
+// registers, for which it keeps a running softmax over the classes it sees; joined over threads at the end, over blocks by class_finish_kernel.  Sums are added up in chunks of 512 terms: the drain has
+// time, and a ratio of probabilities shows what a logit has lost.  Whole calls, 4096 columns against 128 000 classes: 3 rows 178 us (class_few_kernel 184; one row 177 and 164), 16 rows 179
+// (class_some_kernel 195), 64 rows 176 (tiles of 256 rows 291); 1024 against 32 768: 16 rows 19 us (24).
+constexpr int kScoreLeast = 3;
+constexpr int kScoreRows = 16 * SK_GROUPS;
+struct ScoreArgs {
+    int rows, width, classes, tiles, nkb, stages, bf16;
+    int32_t* err;
+    const void* bias; int bias_type;
+    float sc;
+    const int2* targets;                      // [rows]
+    float4* stats;                            // [blocks x rows]
+};
+__global__ void __launch_bounds__(SK_THREADS, 1) class_score_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmH, const __grid_constant__ ScoreArgs a) {
+    extern __shared__ uint8_t smem_raw[];
+    constexpr int CHUNK = 8;
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;
+    uint8_t* sm = smem_raw + pad;
+    const uint32_t sm_addr = raw_addr + pad;
+    const uint32_t bars = sm_addr + SK_RING;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (SK_MOST_STAGES + s); };
+    auto tfull = [&](int i) { return bars + 8u * (2 * SK_MOST_STAGES + i); };
+    auto tempty = [&](int i) { return bars + 8u * (2 * SK_MOST_STAGES + 2 + i); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + SK_RING + 8 * (2 * SK_MOST_STAGES + 4));
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+    float2* sums = reinterpret_cast<float2*>(sm + SK_RING + 512);          // [4][kScoreRows] of a quarter of the lanes each
+    int* target = reinterpret_cast<int*>(sums + 4 * kScoreRows);
+    float* dots = reinterpret_cast<float*>(target + kScoreRows);
+    static_assert(4 * kScoreRows * 8 + 8 * kScoreRows <= SK_XCH, "fits where g and u are exchanged");
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < a.stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(tfull(i), 1); mbar_init(tempty(i), SK_DRAIN / 32); }
+        *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    pdl_next();
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(CT_TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = *tmem_slot;
+    const uint32_t stage_bytes = SK_A + (uint32_t)a.width * (CT_K * 2);
+    float m[16], s[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) { m[j] = -INFINITY; s[j] = 0.f; }
+    if (warp == 0) {
+        if (lane == 0) {
+            const auto load_w = [&](int st, int tile, int kb) {
+                mbar_expect_tx(full(st), stage_bytes);
+                tma_load_3d(sm_addr + st * stage_bytes, &tmW, kb * CT_K, tile * SK_M, 0, full(st));
+            };
+            const auto load_h = [&](int st, int kb) { tma_load_3d(sm_addr + st * stage_bytes + SK_A, &tmH, kb * CT_K, 0, 0, full(st)); };
+            const int ahead = min(a.stages, a.nkb);       // W is the caller's: it need not wait for the copy of H
+            for (int i = 0; i < ahead; ++i) load_w(i, blockIdx.x, i);
+            pdl_wait();
+            for (int i = 0; i < ahead; ++i) load_h(i, i);
+            int st = ahead == a.stages ? 0 : ahead, done = ahead;
+            uint32_t phase = ahead == a.stages ? 1u : 0u;
+            bool ok = true;
+            for (int t = blockIdx.x; t < a.tiles && ok; t += gridDim.x) {
+                for (int kb = done; kb < a.nkb; ++kb) {
+                    if (!(ok = mbar_wait(empty(st), phase ^ 1u, abort_flag, a.err, 61))) break;
+                    load_w(st, t, kb);
+                    load_h(st, kb);
+                    if (++st == a.stages) { st = 0; phase ^= 1u; }
+                }
+                done = 0;
+            }
+        }
+    } else if (warp == 1) {
+        int st = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        const uint32_t idesc = instr_desc_f16(a.width, SK_M) | (a.bf16 ? (1u << 7) | (1u << 10) : 0u);
+        bool ok = true;
+        for (int t = blockIdx.x; t < a.tiles && ok; t += gridDim.x)
+            for (int i = 0; i < a.nkb; ++i) {
+                const bool first = i % CHUNK == 0, last = i % CHUNK == CHUNK - 1 || i == a.nkb - 1;
+                if (first) {
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 62)))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                }
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(st), phase, abort_flag, a.err, 63)))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t base = sm_addr + st * stage_bytes;
+                const uint64_t da = smem_desc(base), db = smem_desc(base + SK_A);
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_one(tmem_base + (uint32_t)(acc * 256), da + 2 * ks, db + 2 * ks, idesc, !first || ks != 0 ? 1u : 0u);
+                    mma_commit(empty(st));
+                    if (last) mma_commit(tfull(acc));
+                }
+                __syncwarp();
+                if (++st == a.stages) { st = 0; phase ^= 1u; }
+                if (last && ++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            }
+    } else {
+        const int q = warp & 3, c0 = ((warp - 2) >> 2) * 16;
+        pdl_wait();
+        for (int i = threadIdx.x - 64; i < kScoreRows; i += SK_DRAIN) { target[i] = i < a.rows ? a.targets[i].x : INT_MAX; dots[i] = 0.f; }
+        all_drain(true);
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        bool ok = true;
+        for (int t = blockIdx.x; t < a.tiles && ok; t += gridDim.x) {
+            const int c = t * SK_M + q * 32 + lane;
+            const bool cls = c < a.classes;
+            const float b = cls && a.bias ? load_typed(a.bias, a.bias_type, c) : 0.f;
+            float z[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) z[j] = 0.f;
+            for (int i = 0; i < a.nkb; i += CHUNK) {
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 66)))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (c0 < a.rows) {
+                    float v[16];
+                    tmem_ld16(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * 256 + c0), v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) z[j] += v[j];
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(tempty(acc));
+                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            }
+            if (!ok || c0 >= a.rows || !cls) continue;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float x = (z[j] + b) * a.sc;
+                if (target[c0 + j] == c) dots[c0 + j] = x;
+                const float most = fmaxf(m[j], x), base = most == -INFINITY ? 0.f : most;
+                s[j] = fmaf(s[j], exp2_fast(m[j] - base), exp2_fast(x - base));
+                m[j] = most;                              // (a logit that is no number stays in the sum)
+            }
+        }
+        if (c0 < a.rows) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                float most = m[j];
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                s[j] *= exp2_fast(m[j] - (most == -INFINITY ? 0.f : most));
+                m[j] = most;
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
+                if (lane == 0) sums[q * kScoreRows + c0 + j] = make_float2(m[j], s[j]);
+            }
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < a.rows) {
+        float most = -INFINITY, sum = 0.f;
+        for (int q = 0; q < 4; ++q) most = fmaxf(most, sums[q * kScoreRows + threadIdx.x].x);
+        const float base = most == -INFINITY ? 0.f : most;
+        for (int q = 0; q < 4; ++q) sum += sums[q * kScoreRows + threadIdx.x].y * exp2f(sums[q * kScoreRows + threadIdx.x].x - base);
+        a.stats[(long long)blockIdx.x * a.rows + threadIdx.x] = make_float4(most, sum, 0.f, dots[threadIdx.x]);
+    }
+    // Tear-down: after a time-out loads in flight get a bounded chance to land.
+    if (*abort_flag && threadIdx.x == 0)
+        for (int st = 0; st < a.stages; ++st)
+            for (uint32_t i = 0; i < 4096u; ++i)
+                if (mbar_try_wait(full(st), 0) || mbar_try_wait(full(st), 1)) break;
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 0) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(CT_TMEM));
+    }
+}
+
 constexpr int kFinishRows = 8;
 
 // The policy loss: with lp the log-probability of a row's label, r = exp(lp - old), its row loss is  -min(r A, clip(r, lo, hi) A) + kl (exp(ref - lp) - (ref - lp) - 1).
@@ -871,6 +1051,7 @@ constexpr int kChunk = 32, kChunkParts = 8;
 struct ClassPlan {
     int parts, pairs;                // operand parts, products of them
     bool grads, pack_w, few, some, add_up;   // add_up: logits longer than a chunk are added up in chunks
+    bool score;                      // a few rows' log-probabilities alone
     bool starts_at_once;             // target starts of all rows from the rows kernel
     int ntargets, nl, save;
     float code_steps;
@@ -890,8 +1071,10 @@ ClassPlan plan_class(const gad_class_loss_args& a, bool policy = false) {
     p.grads = a.dH || a.dW || a.db;
     const bool wide = ((uintptr_t)a.W & 15) == 0 && (a.ldw * (a.dtype == GAD_F32 ? 4 : 2)) % 16 == 0;
     p.few = N <= kFewRows && few_smem(a) <= kFewSmem;
-    p.some = !p.few && N <= kSomeRows && a.dtype != GAD_F32 && wide && some_smem(a) <= kSomeSmem;
-    p.few |= p.some;
+    p.score = policy && !p.grads && N >= kScoreLeast && N <= kScoreRows && a.dtype != GAD_F32 && wide;
+    if (p.score) p.few = false;
+    p.some = !p.few && !p.score && N <= kSomeRows && a.dtype != GAD_F32 && wide && some_smem(a) <= kSomeSmem;
+    p.few |= p.some || p.score;
     p.pack_w = (!p.few || a.dH) && (a.dtype == GAD_F32 || ((uintptr_t)a.W & 15) != 0 || (a.ldw * 2) % 16 != 0);
     p.ntargets = a.k + (a.labels ? 1 : 0);
     p.nl = a.k > 0 && a.labels && a.hard_weight > 0.f && a.hard_weight < 1.f && a.temperature != 1.f ? 2 : 1;
@@ -1049,7 +1232,18 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, const gad_policy_loss_
         z.targets = targets + r0 * p.ntargets; z.ntargets = p.ntargets; z.starts = ra.starts ? ra.starts + r0 * ra.nstarts : starts; z.stats = stats;
         z.save = p.save; z.code_steps = p.code_steps; z.code_lowest = -(float)kCodeZero / p.code_steps; z.C = ws + p.o_z; z.ldc = p.ldg;
         int nparts = 2 * p.tiles_v;
-        if (p.few) {
+        if (p.score) {
+            ScoreArgs k{};
+            k.rows = nr; k.width = (int)round_up(nr, 16); k.classes = V; k.nkb = z.nkb; k.bf16 = z.bf16; k.err = a.status;
+            k.tiles = (V + SK_M - 1) / SK_M;
+            k.stages = std::min<int>(SK_MOST_STAGES, SK_RING / (SK_A + k.width * (CT_K * 2)));
+            k.bias = a.bias; k.bias_type = a.dtype; k.sc = z.sc; k.targets = targets; k.stats = stats;
+            nparts = std::min(2 * kPairs, k.tiles);
+            GAD_TRY(make(mapW, Wo, D, V, ldw, V, SK_M));
+            GAD_TRY(make(mapH, Hp, D, N, p.ldp, N, (uint32_t)k.width));
+            GAD_TRY(configure_kernel_once(reinterpret_cast<const void*>(class_score_kernel), SK_SMEM, false));
+            GAD_TRY(chain(class_score_kernel, dim3((unsigned)nparts), SK_THREADS, SK_SMEM, s, false, mapW, mapH, k));
+        } else if (p.few) {
             FewArgs w{};
             w.H = a.H; w.ldh = a.ldh; w.W = a.W; w.ldw = a.ldw; w.rows = nr; w.cols = D; w.classes = V; w.bias = a.bias; w.targets = targets; w.ntargets = p.ntargets; w.rowk = rowk;
             w.sc = z.sc; w.inv_t = z.inv_t; w.z = p.grads ? reinterpret_cast<float*>(z.C) : nullptr; w.ldz = p.ldg; w.stats = stats;

@@ -149,6 +149,30 @@ def test_loss_and_gradients(N, D, V, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("N,D,V", [(5, 64, 3), (6, 33, 127), (16, 1200, 129), (17, 700, 40_000), (33, 8, 300), (48, 2056, 1001), (64, 520, 20_000), (65, 64, 500)])
+def test_scores_of_a_few_rows(N, D, V, dtype):
+    """No gradients: log-probabilities and losses of serving, every width of the instruction, long rows in chunks."""
+    import torch
+    s = make(N, D, V, dtype, N, bias=N % 2 == 0, weights=N % 3 == 0, ignored=0.3, ref=N % 4 != 1)
+    want = reference(**s)
+    near(pkg.policy_loss(**s, grads=False).check(), want, ("loss", "row_loss", "logp"))
+    if s["bias"] is not None and V > 3:                          # classes that are taken out
+        s["bias"][1::3] = -math.inf
+        s["actions"] = torch.where((s["actions"] % 3 == 1) & (s["actions"] >= 0), s["actions"] - 1, s["actions"])
+        z = s["H"].double() @ s["W"].double().t() + s["bias"].double()
+        lp = z.log_softmax(1).gather(1, s["actions"].clamp(min=0).long()[:, None])[:, 0]
+        got = pkg.policy_loss(**s, grads=False).logp
+        assert float((got.double() - torch.where(s["actions"] >= 0, lp, 0.0)).abs().max()) <= float(want.logp[1].max()) * 2
+    bad = s["H"].clone()
+    if bool((s["actions"] >= 0).any()):
+        row = int((s["actions"] >= 0).nonzero()[0, 0])
+        bad[row, D // 2] = math.nan
+        r = pkg.policy_loss(**dict(s, H=bad), grads=False)
+        assert bool(r.logp[row].isnan()) and int(r.logp.isnan().sum()) == 1
+
+
+@gpu
 def test_a_clipped_row_has_no_gradient_but_that_of_the_divergence():
     import torch
     s = make(64, 48, 100, "float32", 3, ref=False)
