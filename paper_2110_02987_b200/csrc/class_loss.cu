@@ -1046,12 +1046,13 @@ size_t few_smem(const gad_class_loss_args& a) { return 4 * (size_t)few_rows(a.ro
 
 // Blocks of 64 terms of a chunk: 2048 terms are cut by 1.8e-6 of their sum; of fp32 operands 512, by 4.5e-7.  Longer logits go in tiles
 // 128 wide: with chunks of 1024 the distillation of 4096 x 2048 took 2.71 ms instead of 2.34.
-constexpr int kChunk = 32, kChunkParts = 8;
+constexpr int kChunk = 32, kChunkParts = 8, kChunkPolicy = 16;
 
 struct ClassPlan {
     int parts, pairs;                // operand parts, products of them
     bool grads, pack_w, few, some, add_up;   // add_up: logits longer than a chunk are added up in chunks
     bool score;                      // a few rows' log-probabilities alone
+    bool sums;                       // policy: logits longer than a chunk are added up in chunks, in wide tiles
     bool starts_at_once;             // target starts of all rows from the rows kernel
     int ntargets, nl, save;
     float code_steps;
@@ -1083,7 +1084,8 @@ ClassPlan plan_class(const gad_class_loss_args& a, bool policy = false) {
     p.save = !p.grads ? kSaveNone : a.dtype == GAD_F32 || p.few || (p.nl == 2 && (a.temperature > most_t || a.temperature * most_t < 1.f)) ? kSaveFloat : kSaveCode;
     p.code_steps = p.nl == 2 ? kCodeSteps / std::max(1.f, a.temperature) : kCodeSteps;
     p.ldp = round_up(D, 8);
-    p.add_up = (D + CT_K - 1) / CT_K > (p.parts > 1 ? kChunkParts : kChunk);
+    p.sums = policy && p.parts == 1 && (D + CT_K - 1) / CT_K > kChunkPolicy;
+    p.add_up = !p.sums && (D + CT_K - 1) / CT_K > (p.parts > 1 ? kChunkParts : kChunk);
     p.width_v = p.add_up ? 128 : width_for(V);
     p.tiles_v = (V + p.width_v - 1) / p.width_v;
     p.width_d = width_for(D);
@@ -1221,7 +1223,7 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, const gad_policy_loss_
         const int64_t r0 = b * p.block;
         const int nr = (int)std::min(p.block, N - r0), blocks = (nr + kFinishRows - 1) / kFinishRows;
         TileArgs t{};
-        t.err = a.status; t.bf16 = a.dtype != GAD_F16; t.pairs = p.pairs; t.chunk = p.parts > 1 ? kChunkParts : kChunk; t.scal = scal;
+        t.err = a.status; t.bf16 = a.dtype != GAD_F16; t.pairs = p.pairs; t.chunk = p.parts > 1 ? kChunkParts : p.sums ? kChunkPolicy : kChunk; t.scal = scal;
         t.M = nr; t.tiles_m = (nr + CT_M - 1) / CT_M;
         TileArgs z = t;
         z.N = V; z.tiles_n = p.tiles_v; z.width = p.width_v; z.nkb = (D + CT_K - 1) / CT_K; z.whole = z.tiles_m * z.tiles_n; z.shares = 1; z.kb_share = z.nkb;
@@ -1259,7 +1261,8 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, const gad_policy_loss_
             }
         } else {
             if (starts && !p.starts_at_once) GAD_TRY(chain(class_starts_kernel, dim3((unsigned)nr), 128, 0, s, false, z.targets, p.ntargets, starts, ra.nstarts, ra.start_w));
-            GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, p.add_up, s) : go_stats<1>(mapH, mapW, z, p.add_up, s));
+            if (p.sums) GAD_TRY((gemm_launch<kStatsSums, false, false, float, 1, true>(mapH, mapW, z, s)));
+            else GAD_TRY(p.nl == 2 ? go_stats<2>(mapH, mapW, z, p.add_up, s) : go_stats<1>(mapH, mapW, z, p.add_up, s));
         }
         FinishArgs f{};
         f.stats = stats; f.parts = nparts; f.rows = nr; f.rowk = rowk + r0; f.sc = z.sc; f.inv_t = z.inv_t; f.temperature = T0; f.rowc = rowc; f.row_loss = a.row_loss + r0;
