@@ -14,6 +14,8 @@
 
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "gad_internal.h"
 #include "half_types.cuh"
 #include "tc_common.cuh"
@@ -28,7 +30,8 @@ constexpr int CT_STAGE = 2 * CT_OPERAND;                    // A | B
 constexpr int CT_STAGES = 6;
 constexpr int CT_RING = CT_STAGES * CT_STAGE;
 constexpr int CT_EPI_WARPS = 8, CT_EPI_WARP0 = 2;           // two per quarter of the tensor-memory lanes, half of the columns each
-constexpr int CT_THREADS = 32 * (CT_EPI_WARP0 + CT_EPI_WARPS);
+constexpr int CT_LOADER_B = CT_EPI_WARP0 + CT_EPI_WARPS;     // the warp that loads B comes last
+constexpr int CT_THREADS = 32 * (CT_LOADER_B + 1);
 constexpr int CT_BIAS = CT_EPI_WARPS * 128 * 4;             // a draining warp's biases
 constexpr int CT_STAGING = CT_EPI_WARPS * 2048;             // and 64 bytes of each of its rows on their way out
 constexpr int CT_SMEM = CT_RING + 1024 + 256 + CT_BIAS + CT_STAGING;
@@ -55,6 +58,7 @@ struct TileArgs {
     int chunk;                 // ADD_UP: blocks that are summed in tensor memory (of operands in parts all products, the smallest first) before the sum moves to registers
     int a_row0;                // first row of A (K-major)
     int b_row0;                // first row of B (MN-major)
+    int a_chunks, b_chunks;    // MN-major: the descriptor has chunks of 64 columns as a dimension (tc_make_chunk_map), so a box holds all that a CTA has of a stage
     int bf16;                  // operand type: 1 bfloat16, 0 fp16
     int32_t* err;
     // kStats
@@ -95,6 +99,12 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t leader_bar) {
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(leader_bar)
+                 : "memory");
+}
+// The same of a box of 64 columns x 64 rows x (one or two) chunks of columns.
+__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap* map, int y, int chunk, int z, uint32_t leader_bar) {
+    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(chunk), "r"(z), "r"(leader_bar)
                  : "memory");
 }
 __device__ __forceinline__ uint32_t leader_address(uint32_t addr) {
@@ -318,39 +328,45 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     const int ncl = gridDim.x >> 1, half_w = a.width / 2;
     const long long units = units_of(a);
 
-    if (warp == 0 && lane == 0) {
-        // ---------------- TMA producer: this CTA's rows of A and half of the rows of B, 64 of the reduction at a time; the leader's barrier counts both CTAs' bytes
-        // (passed on by a thread of the other CTA, a full stage was known too late for the six of the ring to bridge: all products 4 to 5 % longer) ----------------
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
-            const TileAt t = tile_at(a, u);
-            const int ra = t.m * CT_M + (int)rank * CT_H, rb = t.n * a.width + (int)rank * half_w;
-            const int group = ADD_UP ? a.chunk : t.nkb;
-            for (int g = 0; g < t.nkb && ok; g += group)
-                for (int p = 0; p < a.pairs && ok; ++p) {
-                    int za, zb;
-                    part_pair(p, a.pairs, za, zb);
-                    for (int kb = t.kb0 + g; kb < t.kb0 + min(g + group, t.nkb); ++kb) {
-                        if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, 31))) break;
-                        if (rank == 0) mbar_expect_tx(full(stage), 2u * (uint32_t)(CT_H + half_w) * (CT_K * 2));
-                        const uint32_t base = sm_addr + stage * CT_STAGE, bar = leader_address(full(stage));
-                        if (A_MN) {
-                            tma_load_3d_pair(base, &tmA, ra, kb * CT_K, za, bar);
-                            tma_load_3d_pair(base + 8192, &tmA, ra + 64, kb * CT_K, za, bar);
-                        } else {
-                            tma_load_3d_pair(base, &tmA, kb * CT_K, a.a_row0 + ra, za, bar);
+    if ((warp == 0 || warp == CT_LOADER_B) && lane == 0) {
+        // ---------------- TMA producers, one for each operand: this CTA's rows of A, and half of the rows of B, 64 of the reduction at a time; the leader's barrier counts both CTAs' bytes
+        // (passed on by a thread of the other CTA, a full stage was known too late for the six of the ring to bridge: all products 4 to 5 % longer).  One thread for both operands was the bound of MN-major
+        // ones, whose stage has two boxes of 64 columns each. ----------------
+        const auto produce = [&](auto of_a) {
+            constexpr bool OF_A = decltype(of_a)::value, MN = OF_A ? A_MN : B_MN;
+            const CUtensorMap* map = OF_A ? &tmA : &tmB;
+            const uint32_t leader = leader_address(full(0)), bytes = 2u * (uint32_t)(CT_H + half_w) * (CT_K * 2);
+            const bool chunks = MN && (OF_A ? a.a_chunks : a.b_chunks), two = MN && !chunks && (OF_A || half_w > 64);
+            const int row0 = OF_A ? a.a_row0 : MN ? a.b_row0 : 0;
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (long long u = blockIdx.x >> 1; u < units && ok; u += ncl) {
+                const TileAt t = tile_at(a, u);
+                const int r = OF_A ? t.m * CT_M + (int)rank * CT_H : t.n * a.width + (int)rank * half_w;
+                const int group = ADD_UP ? a.chunk : t.nkb;
+                for (int g = 0; g < t.nkb && ok; g += group)
+                    for (int p = 0; p < a.pairs && ok; ++p) {
+                        int za, zb;
+                        part_pair(p, a.pairs, za, zb);
+                        const int z = OF_A ? za : zb, last = t.kb0 + min(g + group, t.nkb);
+                        for (int kb = t.kb0 + g; kb < last; ++kb) {
+                            if (!(ok = mbar_wait(empty(stage), phase ^ 1u, abort_flag, a.err, OF_A ? 31 : 34))) break;
+                            if (OF_A && rank == 0) mbar_expect_tx(full(stage), bytes);
+                            const uint32_t to = sm_addr + stage * CT_STAGE + (OF_A ? 0 : CT_OPERAND), bar = leader + 8u * stage;
+                            if (!MN) tma_load_3d_pair(to, map, kb * CT_K, row0 + r, z, bar);
+                            else if (chunks) tma_load_4d_pair(to, map, (OF_A ? 0 : row0) + kb * CT_K, r >> 6, z, bar);
+                            else {
+                                tma_load_3d_pair(to, map, r, (OF_A ? 0 : row0) + kb * CT_K, z, bar);
+                                if (two) tma_load_3d_pair(to + 8192, map, r + 64, (OF_A ? 0 : row0) + kb * CT_K, z, bar);
+                            }
+                            if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
                         }
-                        if (B_MN) {
-                            for (int j = 0; j < half_w; j += 64) tma_load_3d_pair(base + CT_OPERAND + j * 128, &tmB, rb + j, a.b_row0 + kb * CT_K, zb, bar);
-                        } else {
-                            tma_load_3d_pair(base + CT_OPERAND, &tmB, kb * CT_K, rb, zb, bar);
-                        }
-                        if (++stage == CT_STAGES) { stage = 0; phase ^= 1u; }
                     }
-                }
-        }
+            }
+        };
+        if (warp == 0) produce(std::true_type());
+        else produce(std::false_type());
     } else if (warp == 1 && rank == 0) {
         // ---------------- MMA issuer (leader of the pair): the whole warp runs the loop, one elected lane issues ----------------
         int stage = 0, acc = 0;
@@ -384,7 +400,7 @@ class_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 if (--left == 0 && ++acc == NACC) { acc = 0; acc_phase ^= 1u; }
             }
         }
-    } else if (warp >= CT_EPI_WARP0) {   // (warp 1 of the other CTA has nothing to do)
+    } else if (warp >= CT_EPI_WARP0 && warp < CT_LOADER_B) {   // (warp 1 of the other CTA has nothing to do)
         // ---------------- drain: this warp's 32 rows (a row a lane) x half of the tile's columns ----------------
         const int ew = warp - CT_EPI_WARP0, q = warp & 3, half = ew >> 2;
         float* bias = reinterpret_cast<float*>(sm + CT_RING + 256) + ew * 128;

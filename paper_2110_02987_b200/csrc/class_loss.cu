@@ -1213,12 +1213,19 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, const gad_policy_loss_
     const auto make = [&](CUtensorMap& m, const void* base, int64_t inner, int64_t rows, int64_t ld, int64_t part_rows, uint32_t box) {
         return tc_make_map(&m, base, (uint64_t)inner, (uint64_t)rows, (uint64_t)p.parts, (uint64_t)ld * 2, (uint64_t)(ld * 2 * part_rows), box, false, true) ? cudaSuccess : cudaErrorInvalidValue;
     };
+    // operands that are read along their columns, `box` of them a CTA and stage: whole boxes where rows have whole chunks of 64 columns
+    const auto make_mn = [&](CUtensorMap& m, const void* base, int64_t inner, int64_t rows, int64_t ld, int box, int& chunks) {
+        chunks = inner % 64 == 0;
+        if (!chunks) return make(m, base, inner, rows, ld, rows, CT_K);
+        return tc_make_chunk_map(&m, base, (uint64_t)inner / 64, (uint64_t)rows, (uint64_t)p.parts, (uint64_t)ld * 2, (uint64_t)(ld * 2 * rows), (uint32_t)box / 64) ? cudaSuccess : cudaErrorInvalidValue;
+    };
+    int h_chunks = 0, w_chunks = 0;
     if (!p.few) {
         GAD_TRY(make(mapH, Hp, D, N, p.ldp, N, CT_H));
         GAD_TRY(make(mapW, Wo, D, V, ldw, V, (uint32_t)p.width_v / 2));
     }
-    if (a.dW) GAD_TRY(make(mapH_mn, Hp, D, N, p.ldp, N, CT_K));
-    if (a.dH) GAD_TRY(make(mapW_mn, Wo, D, V, ldw, V, CT_K));
+    if (a.dW) GAD_TRY(make_mn(mapH_mn, Hp, D, N, p.ldp, p.width_d / 2, h_chunks));
+    if (a.dH) GAD_TRY(make_mn(mapW_mn, Wo, D, V, ldw, p.width_d / 2, w_chunks));
     for (int b = 0; b < p.nblocks; ++b) {
         const int64_t r0 = b * p.block;
         const int nr = (int)std::min(p.block, N - r0), blocks = (nr + kFinishRows - 1) / kFinishRows;
@@ -1295,13 +1302,15 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, const gad_policy_loss_
         if (a.dH) {
             TileArgs h = t;
             GAD_TRY(make(mapG, g.G, V, nr, p.ldg, nr, CT_H));
-            h.nkb = (V + CT_K - 1) / CT_K;
+            h.nkb = (V + CT_K - 1) / CT_K; h.b_chunks = w_chunks;
             h.C = reinterpret_cast<T*>(a.dH) + r0 * a.lddh; h.ldc = a.lddh;
             GAD_TRY((go_out<false, T>(mapG, mapW_mn, h, s)));
         }
         if (a.dW) {
             TileArgs w = t;
-            GAD_TRY(make(mapG_mn, g.G, V, nr, p.ldg, nr, CT_K));
+            // (rows of G are whole tiles: what lies behind the classes is zero, and rows of dW that are not written)
+            GAD_TRY(make_mn(mapG_mn, g.G, p.ldg, nr, p.ldg, CT_H, w.a_chunks));
+            w.b_chunks = h_chunks;
             w.M = V; w.tiles_m = (V + CT_M - 1) / CT_M; w.nkb = (nr + CT_K - 1) / CT_K; w.b_row0 = (int)r0;
             w.C = a.dW; w.ldc = a.lddw; w.add = add; w.sums = reinterpret_cast<float*>(ws + p.o_sums);
             GAD_TRY((go_out<true, T>(mapG_mn, mapH_mn, w, s)));

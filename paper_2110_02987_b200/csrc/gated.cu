@@ -328,8 +328,8 @@ cudaError_t launch_gated(const GatedGroup<G>& g, Sequence& q) {
     cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), CT_SMEM, false);
     if (e != cudaSuccess) return e;
     static std::atomic<int> known{0};
-    if (known.load() <= 0) known.store(max_active_pairs(reinterpret_cast<const void*>(kernel), GG_THREADS, CT_SMEM, 2 * kPairs));
-    return q.launch(kernel, dim3((unsigned)(2 * std::min(g.first[G], known.load()))), GG_THREADS, CT_SMEM, g);
+    if (known.load() <= 0) known.store(max_active_pairs(reinterpret_cast<const void*>(kernel), CT_THREADS, CT_SMEM, 2 * kPairs));
+    return q.launch(kernel, dim3((unsigned)(2 * std::min(g.first[G], known.load()))), CT_THREADS, CT_SMEM, g);
 }
 
 // A launch of g.n products, and the join of the tiles that were cut.

@@ -10,24 +10,13 @@
 // one another (dx, both of these, dWd) are one launch, whose tiles are gone through one product behind the other.
 #pragma once
 
-#include <type_traits>
-
 #include "class_gemm.cuh"
 
 namespace gad {
 
 namespace {
 
-constexpr int GG_LOADER_B = CT_EPI_WARP0 + CT_EPI_WARPS, GG_THREADS = 32 * (GG_LOADER_B + 1);   // the warp that loads B comes last
-
 enum GatedUse { kGate, kHidden, kPlain };
-// A box of 64 columns x 64 rows x (one or two) chunks of columns.
-__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap* map, int y, int chunk, int z, uint32_t leader_bar) {
-    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-                 ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(chunk), "r"(z), "r"(leader_bar)
-                 : "memory");
-}
-
 enum Activation { kSilu, kGelu, kRelu, kSigmoid };
 
 struct GatedArgs {
@@ -184,7 +173,7 @@ __device__ __forceinline__ void drain_operand(uint8_t* buf, int lane, float (&v)
 // USE as above; T: type of the tensors; ADD_UP: sums in chunks (t.chunk; of operands in parts, of one block of 64 terms each), as class_gemm_kernel takes them; G: products a launch may have.  (With the layouts of all products and their number known only
 // at run time, in one kernel for all uses, 8192 x 2048 x 5504 took 428 us instead of 416, and the gradients of 16 384 x 4096 x 10 240 6.2 ms instead of 5.8.)
 template <int USE, int LAYOUT, class T, bool ADD_UP, int G>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GG_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(CT_THREADS, 1)
 gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
     constexpr bool B_MN = LAYOUT != kBothK, PARTS = sizeof(T) == 4;   // PARTS: operands in three parts
     int32_t* const err = gr.p[0].t.err;
@@ -222,7 +211,7 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
 
     const int ncl = gridDim.x >> 1, units = gr.first[G];
 
-    if ((warp == 0 || warp == GG_LOADER_B) && lane == 0) {
+    if ((warp == 0 || warp == CT_LOADER_B) && lane == 0) {
         // ---------------- TMA producers, one for each operand: this CTA's rows of A, and half of the columns' rows of B; the leader's barrier counts both CTAs' bytes.  (One thread for
         // both was the bound of MN-major operands, whose stage has two boxes of 64 columns each: dx, dWg and dWu, dWd of 4096 x 2048 x 5504 in 325 us, with these 300.) ----------------
         const auto produce = [&](auto of_a) {
@@ -347,7 +336,7 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
                 if (--left == 0 && ++acc == NACC) { acc = 0; acc_phase ^= 1u; }
             }
         }
-    } else if (warp >= CT_EPI_WARP0 && warp < GG_LOADER_B) {   // (warp 1 of the other CTA has nothing to do)
+    } else if (warp >= CT_EPI_WARP0 && warp < CT_LOADER_B) {   // (warp 1 of the other CTA has nothing to do)
         // ---------------- drain: this warp's 32 rows (a row a lane) x half of the tile's columns (kGate: half of g and of u) ----------------
         const int ew = warp - CT_EPI_WARP0, q = warp & 3, half = ew >> 2;
         uint8_t* buf = sm + CT_RING + 256 + CT_BIAS + ew * 2048;
