@@ -20,7 +20,9 @@ namespace {
 
 constexpr int kClipThreads = 256;
 constexpr int kSmallChunk = 8192, kLargeChunk = 32768;    // values
-constexpr int kClipBlocks = 592;                         // four a multiprocessor: 1024 threads, 4 x 16 bytes on their way each
+// Chunks of 8192 values, of which a thread has four vectors (fp32: eight), by 1184 blocks, or where every block still has several of 32 768, eight vectors at a time, by 592: a tensor is looked up less often.
+// (Eight vectors at a time of short chunks: half of them behind their ends, 20 million bf16 values 53 us, with four 30; four of long ones, 750 million 751 us, with eight 716.)
+constexpr int kSmallBlocks = 1184, kLargeBlocks = 592;
 
 struct ClipEntry {
     const void* g; void* out;
@@ -57,15 +59,14 @@ __device__ __forceinline__ const ClipEntry& find_chunk(const ClipTable<MOST>& t,
     return e;
 }
 
-// A thread's vectors of a chunk (16 bytes, or one value: VEC = 1), kAhead of them at a time: all are loaded before the first is used, since a store may be to where the next load is from.
-constexpr int kAhead = 8;
-template <int VEC, class F>
+// A thread's vectors of a chunk (16 bytes, or one value: VEC = 1), AHEAD of them at a time: all are loaded before the first is used, since a store may be to where the next load is from.
+template <int VEC, int AHEAD, class F>
 __device__ __forceinline__ void each_vectors(const ClipChunk& k, F f) {
     const int n = (k.cols + VEC - 1) / VEC, total = n * k.rows;
-    for (int i0 = threadIdx.x; i0 < total; i0 += kAhead * kClipThreads) {
-        int r[kAhead], c[kAhead];
+    for (int i0 = threadIdx.x; i0 < total; i0 += AHEAD * kClipThreads) {
+        int r[AHEAD], c[AHEAD];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
+        for (int j = 0; j < AHEAD; ++j) {
             const int i = i0 + j * kClipThreads;
             r[j] = k.rows == 1 ? 0 : i / n;
             c[j] = i < total ? (i - r[j] * n) * VEC : k.cols;             // (behind the end of a row: nothing)
@@ -74,17 +75,17 @@ __device__ __forceinline__ void each_vectors(const ClipChunk& k, F f) {
     }
 }
 
-template <class T, int VEC>
+template <class T, int VEC, int AHEAD>
 __device__ __forceinline__ double chunk_squares(const ClipEntry& e, const ClipChunk& k) {
     const T* base = reinterpret_cast<const T*>(e.g) + k.row * e.ld + k.col;
     float s[2] = {0.f, 0.f};
     uint32_t bits = 0;
-    each_vectors<VEC>(k, [&](const int (&r)[kAhead], const int (&c)[kAhead]) {
-        RowVec<T, VEC> raw[kAhead];
+    each_vectors<VEC, AHEAD>(k, [&](const int (&r)[AHEAD], const int (&c)[AHEAD]) {
+        RowVec<T, VEC> raw[AHEAD];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) load_raw<T, VEC>(base + r[j] * e.ld, c[j], k.cols, raw[j]);
+        for (int j = 0; j < AHEAD; ++j) load_raw<T, VEC>(base + r[j] * e.ld, c[j], k.cols, raw[j]);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
+        for (int j = 0; j < AHEAD; ++j) {
             float v[VEC];
             if constexpr (VEC > 1) {
                 unpack_vec<T, VEC>(raw[j].u, v);
@@ -101,8 +102,8 @@ __device__ __forceinline__ double chunk_squares(const ClipEntry& e, const ClipCh
     if (both >= 0x1p-80f && both <= 0x1p100f) return both;
     if ((bits & (sizeof(T) == 4 || VEC == 1 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0) return 0.0;
     double d = 0.0;
-    each_vectors<VEC>(k, [&](const int (&r)[kAhead], const int (&c)[kAhead]) {
-        for (int j = 0; j < kAhead; ++j)
+    each_vectors<VEC, AHEAD>(k, [&](const int (&r)[AHEAD], const int (&c)[AHEAD]) {
+        for (int j = 0; j < AHEAD; ++j)
             for (int i = 0; i < VEC && c[j] + i < k.cols; ++i) { const double v = to_float(base[r[j] * e.ld + c[j] + i]); d = fma(v, v, d); }
     });
     return d;
@@ -163,9 +164,9 @@ __device__ __forceinline__ double run_squares(const ClipEntry& e, const ClipChun
     });
     return d;
 }
-template <class T>
+template <class T, int AHEAD>
 __device__ __forceinline__ double any_squares(const ClipEntry& e, const ClipChunk& k) {
-    return e.wide ? chunk_squares<T, 16 / (int)sizeof(T)>(e, k) : k.cols >= kLeastRun ? run_squares<T>(e, k) : chunk_squares<T, 1>(e, k);
+    return e.wide ? chunk_squares<T, 16 / (int)sizeof(T), AHEAD>(e, k) : k.cols >= kLeastRun ? run_squares<T>(e, k) : chunk_squares<T, 1, AHEAD>(e, k);
 }
 
 __device__ __forceinline__ double block_sum(double s, double* sm) {
@@ -178,7 +179,7 @@ __device__ __forceinline__ double block_sum(double s, double* sm) {
     return s;
 }
 
-template <int MOST>
+template <int MOST, int AHEAD>
 __global__ void __launch_bounds__(kClipThreads) grad_squares_kernel(const __grid_constant__ ClipTable<MOST> t, double* __restrict__ sums) {
     __shared__ double sm[kClipThreads / 32];
     pdl_next();
@@ -187,22 +188,22 @@ __global__ void __launch_bounds__(kClipThreads) grad_squares_kernel(const __grid
     for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         ClipChunk k;
         const ClipEntry& e = find_chunk(t, c, k);
-        s += e.type == GAD_F32 ? any_squares<float>(e, k) : e.type == GAD_F16 ? any_squares<__half>(e, k) : any_squares<__nv_bfloat16>(e, k);
+        s += e.type == GAD_F32 ? any_squares<float, AHEAD>(e, k) : e.type == GAD_F16 ? any_squares<__half, AHEAD>(e, k) : any_squares<__nv_bfloat16, AHEAD>(e, k);
     }
     s = block_sum(s, sm);
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 
-template <class T, class O, int VEC>
+template <class T, class O, int VEC, int AHEAD>
 __device__ __forceinline__ void scale_chunk(const ClipEntry& e, const ClipChunk& k, float f) {
     const T* src = reinterpret_cast<const T*>(e.g) + k.row * e.ld + k.col;
     O* dst = reinterpret_cast<O*>(e.out) + k.row * e.out_ld + k.col;
-    each_vectors<VEC>(k, [&](const int (&r)[kAhead], const int (&c)[kAhead]) {
-        RowVec<T, VEC> raw[kAhead];
+    each_vectors<VEC, AHEAD>(k, [&](const int (&r)[AHEAD], const int (&c)[AHEAD]) {
+        RowVec<T, VEC> raw[AHEAD];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) load_raw<T, VEC>(src + r[j] * e.ld, c[j], k.cols, raw[j]);
+        for (int j = 0; j < AHEAD; ++j) load_raw<T, VEC>(src + r[j] * e.ld, c[j], k.cols, raw[j]);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
+        for (int j = 0; j < AHEAD; ++j) {
             O* to = dst + r[j] * e.out_ld;
             if constexpr (std::is_same<T, O>::value) {
                 if (f == 1.f) {                          // a copy, to the bit: a product makes one NaN of all
@@ -284,15 +285,15 @@ __device__ __forceinline__ void scale_runs(const ClipEntry& e, const ClipChunk& 
         }
     });
 }
-template <class T, class O>
+template <class T, class O, int AHEAD>
 __device__ __forceinline__ void scale_any(const ClipEntry& e, const ClipChunk& k, float f, float* buf) {
-    if (e.wide) scale_chunk<T, O, 16 / (int)sizeof(T)>(e, k, f);
+    if (e.wide) scale_chunk<T, O, 16 / (int)sizeof(T), AHEAD>(e, k, f);
     else if (k.cols >= kLeastRun) scale_runs<T, O>(e, k, f, reinterpret_cast<O*>(buf));
-    else scale_chunk<T, O, 1>(e, k, f);
+    else scale_chunk<T, O, 1, AHEAD>(e, k, f);
 }
 
 // write: this launch writes the norm.
-template <int MOST>
+template <int MOST, int AHEAD>
 __global__ void __launch_bounds__(kClipThreads) grad_scale_kernel(const __grid_constant__ ClipTable<MOST> t, const double* __restrict__ sums, int nsums, float max_norm, float* __restrict__ norm, int write) {
     __shared__ double sm[kClipThreads / 32];
     __shared__ __align__(16) float staging[kClipThreads / 32][256];
@@ -312,9 +313,9 @@ __global__ void __launch_bounds__(kClipThreads) grad_scale_kernel(const __grid_c
         ClipChunk k;
         const ClipEntry& e = find_chunk(t, c, k);
         if (!e.out || (f == 1.f && e.out == e.g)) continue;
-        if (e.type == GAD_F32) scale_any<float, float>(e, k, f, buf);
-        else if (e.type == GAD_F16) { if (e.out_type == GAD_F32) scale_any<__half, float>(e, k, f, buf); else scale_any<__half, __half>(e, k, f, buf); }
-        else { if (e.out_type == GAD_F32) scale_any<__nv_bfloat16, float>(e, k, f, buf); else scale_any<__nv_bfloat16, __nv_bfloat16>(e, k, f, buf); }
+        if (e.type == GAD_F32) scale_any<float, float, AHEAD>(e, k, f, buf);
+        else if (e.type == GAD_F16) { if (e.out_type == GAD_F32) scale_any<__half, float, AHEAD>(e, k, f, buf); else scale_any<__half, __half, AHEAD>(e, k, f, buf); }
+        else { if (e.out_type == GAD_F32) scale_any<__nv_bfloat16, float, AHEAD>(e, k, f, buf); else scale_any<__nv_bfloat16, __nv_bfloat16, AHEAD>(e, k, f, buf); }
     }
 }
 
@@ -398,22 +399,19 @@ int fill_table(const gad_grad_tensor* t, int64_t& i, int64_t count, bool scaled,
     return GAD_OK;
 }
 
-int blocks_for(int chunks) { return std::max(1, std::min(chunks, kClipBlocks)); }
 
-template <int MOST>
+template <int MOST, int AHEAD>
 int run_clip(const gad_grad_tensor* t, int64_t count, float max_norm, float* norm, double* sums, cudaStream_t s) {
     ClipTable<MOST> table;
-    int64_t all = 0;
-    for (int64_t i = 0; i < count; ++i) all += t[i].rows * t[i].cols;
-    // long chunks, so that a tensor is looked up less often, where every block still has several
-    const int values = all >= (int64_t)8 * kClipBlocks * kLargeChunk ? kLargeChunk : kSmallChunk;
+    const int values = AHEAD == 8 ? kLargeChunk : kSmallChunk;
+    const auto blocks_for = [](int chunks) { return std::max(1, std::min(chunks, AHEAD == 8 ? kLargeBlocks : kSmallBlocks)); };
     int nsums = 0;
     bool first = true;
     for (int64_t i = 0; i < count || first;) {
         const int rc = fill_table(t, i, count, false, values, table);
         if (rc != GAD_OK) return rc;
         const int blocks = blocks_for(table.chunks);
-        if (chain(grad_squares_kernel<MOST>, dim3((unsigned)blocks), kClipThreads, 0, s, first, table, sums + nsums) != cudaSuccess) return GAD_ERR_CUDA;
+        if (chain((grad_squares_kernel<MOST, AHEAD>), dim3((unsigned)blocks), kClipThreads, 0, s, first, table, sums + nsums) != cudaSuccess) return GAD_ERR_CUDA;
         nsums += blocks;
         first = false;
     }
@@ -422,14 +420,18 @@ int run_clip(const gad_grad_tensor* t, int64_t count, float max_norm, float* nor
         const int rc = fill_table(t, i, count, true, values, table);
         if (rc != GAD_OK) return rc;
         if (!table.chunks && !write) break;
-        if (chain(grad_scale_kernel<MOST>, dim3((unsigned)blocks_for(table.chunks)), kClipThreads, 0, s, false, table, (const double*)sums, nsums, max_norm, norm, (int)write) != cudaSuccess) return GAD_ERR_CUDA;
+        if (chain((grad_scale_kernel<MOST, AHEAD>), dim3((unsigned)blocks_for(table.chunks)), kClipThreads, 0, s, false, table, (const double*)sums, nsums, max_norm, norm, (int)write) != cudaSuccess) return GAD_ERR_CUDA;
         write = false;
     }
     return cudaGetLastError() == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
 }
 
 // Launches of the first kernel are at most one a kClipMost tensors, and one for every run of 2^30 chunks.
-size_t clip_bytes(int64_t count) { return sizeof(double) * kClipBlocks * (size_t)(2 + count / 16); }
+size_t clip_bytes(int64_t count) { return sizeof(double) * kSmallBlocks * (size_t)(2 + count / 16); }
+template <int AHEAD>
+int run_clip(const gad_grad_tensor* t, int64_t count, float max_norm, float* norm, double* sums, cudaStream_t s) {
+    return count <= 16 ? run_clip<16, AHEAD>(t, count, max_norm, norm, sums, s) : count <= 64 ? run_clip<64, AHEAD>(t, count, max_norm, norm, sums, s) : run_clip<kClipMost, AHEAD>(t, count, max_norm, norm, sums, s);
+}
 
 int check_list(const gad_grad_tensor* t, int64_t count) {
     if (count < 0 || (count > 0 && !t)) return GAD_ERR_ARG;
@@ -462,7 +464,9 @@ extern "C" int gad_clip_grads(const gad_grad_tensor* tensors, int64_t count, flo
         if (!workspace || ((uintptr_t)workspace & 15) != 0 || workspace_bytes < clip_bytes(count)) return GAD_ERR_OOM;
         const cudaStream_t s = (cudaStream_t)stream;
         double* sums = (double*)workspace;
-        return count <= 16 ? run_clip<16>(tensors, count, max_norm, norm, sums, s) : count <= 64 ? run_clip<64>(tensors, count, max_norm, norm, sums, s) : run_clip<kClipMost>(tensors, count, max_norm, norm, sums, s);
+        int64_t all = 0;
+        for (int64_t i = 0; i < count; ++i) all += tensors[i].rows * tensors[i].cols;
+        return all >= (int64_t)8 * kLargeBlocks * kLargeChunk ? run_clip<8>(tensors, count, max_norm, norm, sums, s) : run_clip<4>(tensors, count, max_norm, norm, sums, s);
     } catch (...) {   // (the list of regions could not grow)
         return GAD_ERR_OOM;
     }

@@ -81,6 +81,21 @@ def test_norm_and_clipping(shapes, dtype, pad):
 
 
 @gpu
+def test_long_chunks():
+    """Enough values for chunks of 32 768: odd sizes, rows of a wider matrix, in place."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(5)
+    grads = [torch.randn(90_000_001, generator=g, device="cuda").bfloat16(), torch.randn(7000, 10_009, generator=g, device="cuda").half()[:, :9999], torch.randn(33_333, generator=g, device="cuda")]
+    n = norm_of(grads)
+    want = [t.double() * 0.25 for t in grads]
+    rest = grads[1]._base[:, 9999:].clone()
+    assert abs(pkg.clip_grads(grads, n / 4).item() - n) <= 36 * U * n          # (128 values a thread in two sums: 65 roundings, halved)
+    for t, w in zip(grads, want):
+        held(t, w)
+    assert torch.equal(grads[1]._base[:, 9999:], rest)
+
+
+@gpu
 def test_layouts():
     """Transposed matrices, columns of one matrix, tensors of more dimensions, starts off 16 bytes, a matrix with rows into a dense one."""
     import torch
