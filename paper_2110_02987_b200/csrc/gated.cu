@@ -12,6 +12,7 @@
 #include <atomic>
 #include <cmath>
 
+#include "gated_few32.cuh"
 #include "gated_gemm.cuh"
 #include "gated_skinny.cuh"
 #include "operand_pack.cuh"
@@ -416,6 +417,8 @@ SkinnyCut skinny_cut(int64_t rows, int n, bool gate, int64_t K) {
 }
 bool is_skinny(const gad_gated_args& a) { return a.dtype != GAD_F32 && !a.act && a.rows <= SK_MOST_ROWS; }
 
+bool is_few32(const gad_gated_args& a) { return a.dtype == GAD_F32 && !a.act && a.rows <= FEW32_ROWS && few32_group(a.rows, a.cols) > 0 && few32_group(a.rows, a.inner) > 0; }
+
 struct ForwardPlan {
     Operand x, wg, wu, wd, h;
     SkinnyCut gate, down;
@@ -428,6 +431,12 @@ Shape out_shape(const gad_gated_args& a) { return {a.rows, a.cols, a.inner, 1, 1
 ForwardPlan plan_forward(const gad_gated_args& a) {
     ForwardPlan p{};
     Room room;
+    if (is_few32(a)) {                                     // h as it is
+        p.h = {nullptr, 0, a.rows, a.inner, true, 0, round_up(a.inner, 4)};
+        p.h.at = room.take(4 * a.rows * p.h.ldp);
+        p.total = room.at;
+        return p;
+    }
     p.x = operand(a.x, a.ldx, a.rows, a.cols, a.dtype, room);
     p.wg = operand(a.w_gate, a.ldwg, a.inner, a.cols, a.dtype, room);
     p.wu = operand(a.w_up, a.ldwu, a.inner, a.cols, a.dtype, room);
@@ -469,6 +478,32 @@ cudaError_t go_skinny(const CUtensorMap& W0, const CUtensorMap& W1, const CUtens
     return q.launch(skinny_join_kernel<USE, T>, dim3((unsigned)((k.N + 255) / 256), (unsigned)k.rows), 256, 0, k, out, (long long)ldo);
 }
 
+// Few rows of fp32.
+template <int USE, int NR>
+cudaError_t launch_few32(const Few32Args& k, Sequence& q) {
+    const bool wide = ((uintptr_t)k.w0 & 15) == 0 && k.ldw0 % 4 == 0 && (USE != kGate || (((uintptr_t)k.w1 & 15) == 0 && k.ldw1 % 4 == 0));
+    const auto kernel = wide ? few32_kernel<USE, NR, true> : few32_kernel<USE, NR, false>;
+    const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), FEW32_SMEM, false);
+    if (e != cudaSuccess) return e;
+    const size_t smem = 4 * (size_t)NR * (size_t)round_up(k.cols, 4);
+    const int per = (FEW32_THREADS / 32) * (USE == kGate ? 2 : 4), groups = (k.rows + NR - 1) / NR;
+    // (as many blocks as run at once where shared memory allows more than one an SM)
+    const int blocks = std::min((k.n + per - 1) / per, 2 * kPairs * std::max(1, std::min(4, (int)(FEW32_SMEM / smem))));
+    return q.launch(kernel, dim3((unsigned)blocks, (unsigned)groups), FEW32_THREADS, smem, k);
+}
+template <int USE>
+cudaError_t go_few32(Few32Args k, Sequence& q) {
+    k.clear = q.clear;
+    q.clear = false;
+    const int nr = few32_group(k.rows, k.cols);
+    return nr == 4 ? launch_few32<USE, 4>(k, q) : nr == 2 ? launch_few32<USE, 2>(k, q) : launch_few32<USE, 1>(k, q);
+}
+cudaError_t run_few32(const gad_gated_args& a, const ForwardPlan& p, uint8_t* ws, Sequence& q) {
+    float* h = reinterpret_cast<float*>(ws + p.h.at);
+    GAD_TRY(go_few32<kGate>({(const float*)a.x, a.ldx, (const float*)a.w_gate, (const float*)a.w_up, a.ldwg, a.ldwu, (int)a.rows, a.cols, a.inner, h, p.h.ldp, a.activation, 0, a.status}, q));
+    return go_few32<kPlain>({h, p.h.ldp, (const float*)a.w_down, nullptr, a.ldwd, 0, (int)a.rows, a.inner, a.cols, (float*)a.y, a.ldy, a.activation, 0, a.status}, q);
+}
+
 // Few rows of 16-bit operands.
 template <class T>
 cudaError_t run_skinny(const gad_gated_args& a, const ForwardPlan& p, uint8_t* ws, Sequence& q) {
@@ -494,6 +529,9 @@ cudaError_t run_forward(const gad_gated_args& a, uint8_t* ws, cudaStream_t s) {
     const int parts = a.dtype == GAD_F32 ? 3 : 1;
     Sequence q{s};
     GAD_TRY(pack<T>({&p.x, &p.wg, &p.wu, &p.wd}, ws, q));
+    if constexpr (sizeof(T) == 4) {
+        if (is_few32(a)) { GAD_TRY(run_few32(a, p, ws, q)); return cudaGetLastError(); }
+    }
     if constexpr (sizeof(T) == 2) {
         if (is_skinny(a)) { GAD_TRY(run_skinny<T>(a, p, ws, q)); return cudaGetLastError(); }
     }

@@ -129,6 +129,22 @@ def test_forward_and_backward(N, D, F, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("N,D,F", [(1, 2048, 8192), (2, 999, 2050), (3, 4100, 130), (4, 64, 20_000), (5, 131, 77), (7, 2000, 13_000), (16, 300, 1000), (17, 300, 1000), (31, 4096, 64), (64, 520, 3000),
+                                   (100, 72, 5000), (255, 640, 1000), (256, 1000, 640)])
+def test_serving(N, D, F, dtype):
+    """Nothing kept: the forms for few rows, their cuts, rows that do not start on 16 bytes."""
+    kind = ("silu", "gelu", "relu", "sigmoid")[N % 4]
+    for pad, offset in ((0, 0), (4, 1)):
+        s = make(N, D, F, dtype, N, pad, offset)
+        r = pkg.gated_feed_forward(**s, activation=kind).check()
+        near(r, {"y": forward(**s, kind=kind)["y"]})
+        again = pkg.gated_feed_forward(**s, activation=kind).check()
+        import torch
+        assert torch.equal(r.y, again.y)
+
+
+@gpu
 @pytest.mark.parametrize("kind", ["silu", "gelu", "relu", "sigmoid"])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_activations_over_their_range(kind, dtype):
@@ -352,9 +368,9 @@ def test_kernels_wait_for_the_one_in_front():
     import os
     import re
     from test_launch_contract import kernels, CSRC
-    text = re.sub(r"//[^\n]*", "", "".join(open(os.path.join(CSRC, f)).read() for f in ("gated_gemm.cuh", "gated.cu")))
+    text = re.sub(r"//[^\n]*", "", "".join(open(os.path.join(CSRC, f)).read() for f in ("gated_few32.cuh", "gated_gemm.cuh", "gated_skinny.cuh", "gated.cu")))
     bodies = kernels(text)
     chained = set(bodies) - {"gated_zero_kernel", "gated_empty_kernel"}
-    assert {"gated_gemm_kernel", "gated_join_kernel", "gated_pack_kernel"} <= chained
+    assert {"gated_gemm_kernel", "gated_join_kernel", "gated_hidden_join_kernel", "gated_pack_kernel", "skinny_kernel", "skinny_join_kernel", "few32_kernel"} <= chained
     for name in chained:
         assert "pdl_wait();" in bodies[name], name
