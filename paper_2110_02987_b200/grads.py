@@ -94,6 +94,7 @@ def _clip(grads, max_norm, out, stream):
             values += (g.data_ptr(), t, t, 1, n, n, o.data_ptr(), n)
         else:
             values += _entry(g, o, dev, types)
+    max_norm = float(max_norm)
     if not max_norm >= 0:
         raise GadError(-1, "max_norm must be 0 or more")
     if _elsewhere(dev, stream):

@@ -313,5 +313,7 @@ def policy_loss(H, W, actions, old_logp, advantages, *, ref_logp=None, clip=0.2,
     ``old_logp``; for the log-probabilities alone: ``-class_loss(H, W, actions, grads=False).row_loss``."""
     if actions is None or old_logp is None or advantages is None:
         raise GadError(-1, "actions, old_logp and advantages are needed")
+    if isinstance(clip, (tuple, list)) and len(clip) != 2:
+        raise GadError(-1, "clip is one number, or (low, high)")
     low, high = clip if isinstance(clip, (tuple, list)) else (clip, clip)
     return _class_loss(H, W, actions, None, None, 1.0, 1.0, bias, row_weights, mean, scale, grads, stream, (old_logp, advantages, ref_logp, low, high, kl_weight))

@@ -192,6 +192,32 @@ def test_long_sums(N, D, F, dtype):
 
 
 @gpu
+def test_offsets_behind_32_bits():
+    """More than 2^31 units in all: the last rows, and the gradients' sums over all of them, against the same call on pieces."""
+    import torch
+    N, D, F = 70_000, 64, 32_768
+    g = torch.Generator(device="cuda").manual_seed(40)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    x, dy = r(N, D).bfloat16(), (0.01 * r(N, D)).bfloat16()
+    W = (r(F, D) / 8).bfloat16(), (r(F, D) / 8).bfloat16(), (r(D, F) / 180).bfloat16()
+    f = pkg.gated_feed_forward(x, *W, save=True).check()
+    b = pkg.gated_feed_forward_backward(dy, x, *W, f.act, f.slope, f.h).check()
+    parts = [0.0, 0.0, 0.0]
+    for i in range(0, N, 10_000):
+        j = slice(i, i + 10_000)
+        p = pkg.gated_feed_forward(x[j], *W, save=True)
+        assert all(torch.equal(getattr(p, k), getattr(f, k)[j]) for k in ("act", "slope", "h"))
+        q = pkg.gated_feed_forward_backward(dy[j], x[j], *W, p.act, p.slope, p.h)
+        # (how sums are cut goes by the sizes: one rounding on either side)
+        for u, v in ((p.y, f.y[j]), (q.dx, b.dx[j])):
+            assert float((u.double() - v.double()).norm()) <= 2.0 ** -8 * float(v.double().norm())
+        for k, t in enumerate((q.dWg, q.dWu, q.dWd)):
+            parts[k] = parts[k] + t.double()
+    for t, want in zip((b.dWg, b.dWu, b.dWd), parts):     # seven parts, each rounded, and the whole
+        assert float((t.double() - want).norm()) <= 2.0 ** -8 * math.sqrt(8) * float(want.norm())
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_some_of_the_gradients(dtype):
     import torch

@@ -149,6 +149,17 @@ def test_loss_and_gradients(N, D, V, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("N,D,V", [(300, 1100, 700), (130, 2100, 1000), (65, 4096, 300), (520, 1030, 257)])
+def test_long_rows(N, D, V, dtype):
+    """Logits that are added up in chunks, in tiles of 256 columns, the last of them ragged."""
+    s = make(N, D, V, dtype, N, bias=N % 4 == 0, weights=N == 130, ignored=0.2, pad=8 if N == 65 else 0)
+    want = reference(**s)
+    near(pkg.policy_loss(**s).check(), want)
+    near(pkg.policy_loss(**s, grads=False).check(), want, ("loss", "row_loss", "logp"))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
 @pytest.mark.parametrize("N,D,V", [(5, 64, 3), (6, 33, 127), (16, 1200, 129), (17, 700, 40_000), (33, 8, 300), (48, 2056, 1001), (64, 520, 20_000), (65, 64, 500)])
 def test_scores_of_a_few_rows(N, D, V, dtype):
@@ -316,7 +327,7 @@ def test_no_rows_and_refusals_of_tensors():
     assert r.loss.item() == 0 and r.logp.shape == (0,) and not r.dW.any()
     s = make(6, 16, 10, "float32", 12)
     for change in (dict(old_logp=s["old_logp"].double()), dict(old_logp=None), dict(advantages=s["advantages"][:5]), dict(ref_logp=s["ref_logp"].cpu()), dict(actions=s["actions"].float()), dict(clip=-0.1),
-                   dict(clip=(1.5, 0.2)), dict(clip=(0.2, math.nan)), dict(kl_weight=-1.0), dict(kl_weight=math.inf), dict(H=s["H"].half())):
+                   dict(clip=(1.5, 0.2)), dict(clip=(0.2, math.nan)), dict(clip=(0.2,)), dict(clip=(0.1, 0.2, 0.3)), dict(kl_weight=-1.0), dict(kl_weight=math.inf), dict(H=s["H"].half())):
         with pytest.raises(GadError):
             pkg.policy_loss(**{**s, **change})
 
