@@ -12,7 +12,7 @@
 #include <atomic>
 #include <cmath>
 
-#include "gated_few32.cuh"
+#include "gated_few.cuh"
 #include "gated_gemm.cuh"
 #include "gated_skinny.cuh"
 #include "operand_pack.cuh"
@@ -417,11 +417,19 @@ SkinnyCut skinny_cut(int64_t rows, int n, bool gate, int64_t K) {
 }
 bool is_skinny(const gad_gated_args& a) { return a.dtype != GAD_F32 && !a.act && a.rows <= SK_MOST_ROWS; }
 
-bool is_few32(const gad_gated_args& a) { return a.dtype == GAD_F32 && !a.act && a.rows <= FEW32_ROWS && few32_group(a.rows, a.cols) > 0 && few32_group(a.rows, a.inner) > 0; }
+// Few rows of weights that the tensor cores could only read as copies (gated_few.cuh): both products of fp32, and of 16-bit types that of Wg and Wu with one or two rows.
+bool few_gate(const gad_gated_args& a) {
+    const auto off = [](const void* p, int64_t ld, int64_t rows) { return ((uintptr_t)p & 15) != 0 || (rows > 1 && ld % 8 != 0); };
+    if (a.act || few_group(a.rows, a.cols) == 0) return false;
+    return a.dtype == GAD_F32 ? a.rows <= FEW_ROWS : a.rows <= 2 && (off(a.w_gate, a.ldwg, a.inner) || off(a.w_up, a.ldwu, a.inner));
+}
+bool few_down(const gad_gated_args& a) { return a.dtype == GAD_F32 && !a.act && a.rows <= FEW_ROWS && few_group(a.rows, a.inner) > 0; }
+bool is_few(const gad_gated_args& a) { return a.dtype == GAD_F32 && few_gate(a) && few_down(a); }
 
 struct ForwardPlan {
     Operand x, wg, wu, wd, h;
     SkinnyCut gate, down;
+    bool gate_few;
     Cut hidden, out;
     int64_t o_slots, o_gate, total;
 };
@@ -431,15 +439,18 @@ Shape out_shape(const gad_gated_args& a) { return {a.rows, a.cols, a.inner, 1, 1
 ForwardPlan plan_forward(const gad_gated_args& a) {
     ForwardPlan p{};
     Room room;
-    if (is_few32(a)) {                                     // h as it is
+    if (is_few(a)) {                                     // h as it is
         p.h = {nullptr, 0, a.rows, a.inner, true, 0, round_up(a.inner, 4)};
         p.h.at = room.take(4 * a.rows * p.h.ldp);
         p.total = room.at;
         return p;
     }
-    p.x = operand(a.x, a.ldx, a.rows, a.cols, a.dtype, room);
-    p.wg = operand(a.w_gate, a.ldwg, a.inner, a.cols, a.dtype, room);
-    p.wu = operand(a.w_up, a.ldwu, a.inner, a.cols, a.dtype, room);
+    p.gate_few = is_skinny(a) && few_gate(a);
+    if (!p.gate_few) {
+        p.x = operand(a.x, a.ldx, a.rows, a.cols, a.dtype, room);
+        p.wg = operand(a.w_gate, a.ldwg, a.inner, a.cols, a.dtype, room);
+        p.wu = operand(a.w_up, a.ldwu, a.inner, a.cols, a.dtype, room);
+    }
     p.wd = operand(a.w_down, a.ldwd, a.cols, a.inner, a.dtype, room);
     // h: kept where the caller wants it and a descriptor reaches it, else in the workspace
     const bool kept = a.h && a.dtype != GAD_F32;
@@ -478,30 +489,34 @@ cudaError_t go_skinny(const CUtensorMap& W0, const CUtensorMap& W1, const CUtens
     return q.launch(skinny_join_kernel<USE, T>, dim3((unsigned)((k.N + 255) / 256), (unsigned)k.rows), 256, 0, k, out, (long long)ldo);
 }
 
-// Few rows of fp32.
-template <int USE, int NR>
-cudaError_t launch_few32(const Few32Args& k, Sequence& q) {
-    const bool wide = ((uintptr_t)k.w0 & 15) == 0 && k.ldw0 % 4 == 0 && (USE != kGate || (((uintptr_t)k.w1 & 15) == 0 && k.ldw1 % 4 == 0));
-    const auto kernel = wide ? few32_kernel<USE, NR, true> : few32_kernel<USE, NR, false>;
-    const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), FEW32_SMEM, false);
+// Few rows of weights as they lie.
+template <int USE, int NR, class T>
+cudaError_t launch_few(const FewRowsArgs& k, Sequence& q) {
+    const auto on = [](const void* p, int64_t ld, int64_t rows) { return ((uintptr_t)p & 15) == 0 && (rows == 1 || ld * (int64_t)sizeof(T) % 16 == 0); };
+    const bool wide = on(k.w0, k.ldw0, k.n) && (USE != kGate || on(k.w1, k.ldw1, k.n));
+    const auto kernel = wide ? few_rows_kernel<USE, NR, true, T> : few_rows_kernel<USE, NR, false, T>;
+    const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), FEW_SMEM, false);
     if (e != cudaSuccess) return e;
-    const size_t smem = 4 * (size_t)NR * (size_t)round_up(k.cols, 4);
-    const int per = (FEW32_THREADS / 32) * (USE == kGate ? 2 : 4), groups = (k.rows + NR - 1) / NR;
+    const size_t smem = 4 * (size_t)NR * (size_t)round_up(k.cols, 8);
+    const int per = (FEW_THREADS / 32) * (USE == kGate ? 2 : 4), groups = (k.rows + NR - 1) / NR;
     // (as many blocks as run at once where shared memory allows more than one an SM)
-    const int blocks = std::min((k.n + per - 1) / per, 2 * kPairs * std::max(1, std::min(4, (int)(FEW32_SMEM / smem))));
-    return q.launch(kernel, dim3((unsigned)blocks, (unsigned)groups), FEW32_THREADS, smem, k);
+    const int blocks = std::min((k.n + per - 1) / per, 2 * kPairs * std::max(1, std::min(4, (int)(FEW_SMEM / smem))));
+    return q.launch(kernel, dim3((unsigned)blocks, (unsigned)groups), FEW_THREADS, smem, k);
 }
-template <int USE>
-cudaError_t go_few32(Few32Args k, Sequence& q) {
+template <int USE, class T>
+cudaError_t go_few(FewRowsArgs k, Sequence& q) {
     k.clear = q.clear;
     q.clear = false;
-    const int nr = few32_group(k.rows, k.cols);
-    return nr == 4 ? launch_few32<USE, 4>(k, q) : nr == 2 ? launch_few32<USE, 2>(k, q) : launch_few32<USE, 1>(k, q);
+    const int nr = few_group(k.rows, k.cols);
+    return nr == 4 ? launch_few<USE, 4, T>(k, q) : nr == 2 ? launch_few<USE, 2, T>(k, q) : launch_few<USE, 1, T>(k, q);
 }
-cudaError_t run_few32(const gad_gated_args& a, const ForwardPlan& p, uint8_t* ws, Sequence& q) {
-    float* h = reinterpret_cast<float*>(ws + p.h.at);
-    GAD_TRY(go_few32<kGate>({(const float*)a.x, a.ldx, (const float*)a.w_gate, (const float*)a.w_up, a.ldwg, a.ldwu, (int)a.rows, a.cols, a.inner, h, p.h.ldp, a.activation, 0, a.status}, q));
-    return go_few32<kPlain>({h, p.h.ldp, (const float*)a.w_down, nullptr, a.ldwd, 0, (int)a.rows, a.inner, a.cols, (float*)a.y, a.ldy, a.activation, 0, a.status}, q);
+template <class T>
+cudaError_t few_gate_product(const gad_gated_args& a, void* h, int64_t ldh, Sequence& q) {
+    return go_few<kGate, T>({a.x, a.ldx, a.w_gate, a.w_up, a.ldwg, a.ldwu, (int)a.rows, a.cols, a.inner, h, ldh, a.activation, 0, a.status}, q);
+}
+template <class T>
+cudaError_t few_down_product(const gad_gated_args& a, const void* h, int64_t ldh, Sequence& q) {
+    return go_few<kPlain, T>({h, ldh, a.w_down, nullptr, a.ldwd, 0, (int)a.rows, a.inner, a.cols, a.y, a.ldy, a.activation, 0, a.status}, q);
 }
 
 // Few rows of 16-bit operands.
@@ -510,12 +525,15 @@ cudaError_t run_skinny(const gad_gated_args& a, const ForwardPlan& p, uint8_t* w
     CUtensorMap W0, W1, X;
     SkinnyArgs k{};
     k.rows = (int)a.rows; k.width = (int)round_up(a.rows, 16); k.bf16 = a.dtype != GAD_F16; k.activation = a.activation; k.err = a.status;
-    k.N = a.inner;
-    k.early = !p.wg.pack && !p.wu.pack;
-    GAD_TRY(map_of(X, p.x, ws, 1, (uint32_t)k.width));
-    GAD_TRY(map_of(W0, p.wg, ws, 1, (uint32_t)p.gate.per / 2));
-    GAD_TRY(map_of(W1, p.wu, ws, 1, (uint32_t)p.gate.per / 2));
-    GAD_TRY((go_skinny<kGate, T>(W0, W1, X, k, p.gate, reinterpret_cast<float*>(ws + p.o_gate), ws + p.h.at, p.h.ldp, q)));
+    if (p.gate_few) GAD_TRY(few_gate_product<T>(a, ws + p.h.at, p.h.ldp, q));
+    else {
+        k.N = a.inner;
+        k.early = !p.wg.pack && !p.wu.pack;
+        GAD_TRY(map_of(X, p.x, ws, 1, (uint32_t)k.width));
+        GAD_TRY(map_of(W0, p.wg, ws, 1, (uint32_t)p.gate.per / 2));
+        GAD_TRY(map_of(W1, p.wu, ws, 1, (uint32_t)p.gate.per / 2));
+        GAD_TRY((go_skinny<kGate, T>(W0, W1, X, k, p.gate, reinterpret_cast<float*>(ws + p.o_gate), ws + p.h.at, p.h.ldp, q)));
+    }
     k.N = a.cols;
     k.early = !p.wd.pack;
     GAD_TRY(map_of(X, p.h, ws, 1, (uint32_t)k.width));
@@ -530,7 +548,11 @@ cudaError_t run_forward(const gad_gated_args& a, uint8_t* ws, cudaStream_t s) {
     Sequence q{s};
     GAD_TRY(pack<T>({&p.x, &p.wg, &p.wu, &p.wd}, ws, q));
     if constexpr (sizeof(T) == 4) {
-        if (is_few32(a)) { GAD_TRY(run_few32(a, p, ws, q)); return cudaGetLastError(); }
+        if (is_few(a)) {
+            GAD_TRY(few_gate_product<float>(a, ws + p.h.at, p.h.ldp, q));
+            GAD_TRY(few_down_product<float>(a, ws + p.h.at, p.h.ldp, q));
+            return cudaGetLastError();
+        }
     }
     if constexpr (sizeof(T) == 2) {
         if (is_skinny(a)) { GAD_TRY(run_skinny<T>(a, p, ws, q)); return cudaGetLastError(); }
