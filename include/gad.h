@@ -475,7 +475,7 @@ typedef struct {
 } gad_gated_args;
 
 /* Device workspace (256-byte aligned): h in operand form where it is not kept (2 bytes a value, 6 in fp32), copies of matrices that are fp32 or whose rows do not start on
- * 16 bytes (2 bytes a value, 6 in fp32), sums of tiles that are cut along their reduction (with few tiles; at most 160 MB).  Host-only. */
+ * 16 bytes (2 bytes a value, 6 in fp32), sums of tiles that are cut along their reduction (at most 320 MB).  Host-only. */
 int gad_gated_feed_forward_workspace_bytes(const gad_gated_args* args, size_t* bytes);
 int gad_gated_feed_forward(const gad_gated_args* args, void* workspace, size_t workspace_bytes, void* stream);
 

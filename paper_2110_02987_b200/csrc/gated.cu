@@ -214,7 +214,8 @@ Cut whole_tiles(const Shape& s, bool narrow) {
     c.whole = (int)c.tiles();
     return c;
 }
-// Products whose results go as they are.  With three rounds of tiles and more, those of the last product that are left over when all pairs have had the same number are cut along their
+// Products whose results go as they are.  With three rounds of tiles and more, tiles that take long are cut along their reduction where the pair of CTAs with most work finishes sooner so (pairs take units
+// in turn: the 16 tiles of dx of 64 x 4096 x 11 000, 344 stages each, would be 16 pairs' alone: 226 us, cut 150; a unit that is cut costs about ten stages more, and its sums' way through the L2), and those of the last product that are left over when all pairs have had the same number are cut along their
 // reduction, down to 8 ring stages a share; with fewer, every tile is cut into shares of about the same number of stages, the number that lets the pair with most work finish first.
 constexpr int kMostUnits = 4 * kPairs;                    // of a launch whose tiles are cut
 double cut_group(const Shape* s, int n, int pairs, Cut* c) {
@@ -234,9 +235,36 @@ double cut_group(const Shape* s, int n, int pairs, Cut* c) {
         c[i].shares = (c[i].nkb + c[i].kb_share - 1) / c[i].kb_share;
     };
     if (tiles >= 3 * kPairs) {
+        int64_t all = 0;
+        for (int i = 0; i < n; ++i) all += c[i].tiles() * stages(i, c[i].nkb);
+        const auto share_over = [&](int64_t most) {        // tiles of more than so many stages
+            for (int i = 0; i < n; ++i) {
+                const int64_t one = stages(i, c[i].nkb);
+                share(i, most && one > most ? (int)std::min((one + most - 1) / most, std::max<int64_t>(1, one / 8)) : 1);
+            }
+        };
+        double least = 1e30;
+        int64_t best = 0;
+        for (int k = 0; k < 5; ++k) {
+            const int64_t most = k ? std::max<int64_t>(8, (all / kPairs) >> (k - 1)) : 0;
+            share_over(most);
+            int64_t load[kPairs] = {}, at = 0, cut = 0;
+            for (int i = 0; i < n; ++i) {
+                // the pairs' turns go on from one product to the next
+                const int64_t units = c[i].tiles() * c[i].shares, one = stages(i, c[i].kb_share) + (c[i].shares > 1 ? 10 : 2);
+                for (int x = 0; x < kPairs; ++x) load[(at + x) % kPairs] += (units / kPairs + (x < units % kPairs)) * one;
+                at = (at + units) % kPairs;
+                if (c[i].shares > 1) cut += units;
+            }
+            const double cost = (double)*std::max_element(load, load + kPairs) + (cut ? 15 + 0.3 * (double)cut : 0.0);
+            if (cost < 0.97 * least) { least = cost; best = most; }
+        }
+        share_over(best);
+        for (int i = 0; i < n; ++i)
+            if (c[i].shares > 1) c[i].whole = 0;
         const int i = n - 1;
         const int64_t rest = std::min<int64_t>(tiles % kPairs, c[i].tiles());
-        if (!rest) return 0.0;
+        if (!rest || c[i].shares > 1) return 0.0;
         const int want = (int)std::min<int64_t>(kPairs / rest, stages(i, c[i].nkb) / 8);
         if (want < 2) return 0.0;
         share(i, want);
