@@ -429,7 +429,7 @@ SkinnyCut skinny_cut(int64_t rows, int n, bool gate, int64_t K) {
     const double width = (double)round_up(rows, 16);
     SkinnyCut best{};
     double least = 1e30;
-    for (int per = SK_M; per >= SK_M / 2; per -= 8 * each) {
+    for (int per = SK_M; per >= SK_M / 2; per -= 16) {
         const int tiles = (n + per / each - 1) / (per / each);
         const double stages = (double)tiles * nkb / sms / SK_M;
         for (int want = 1; want <= std::min(nkb, 64); want += 1 + want / 8) {
@@ -570,8 +570,7 @@ cudaError_t run_skinny(const gad_gated_args& a, const ForwardPlan& p, uint8_t* w
 }
 
 template <class T>
-cudaError_t run_forward(const gad_gated_args& a, uint8_t* ws, cudaStream_t s) {
-    const ForwardPlan p = plan_forward(a);
+cudaError_t run_forward(const gad_gated_args& a, const ForwardPlan& p, uint8_t* ws, cudaStream_t s) {
     const int parts = a.dtype == GAD_F32 ? 3 : 1;
     Sequence q{s};
     GAD_TRY(pack<T>({&p.x, &p.wg, &p.wu, &p.wd}, ws, q));
@@ -647,8 +646,7 @@ BackwardPlan plan_backward(const gad_gated_grad_args& a) {
 }
 
 template <class T>
-cudaError_t run_backward(const gad_gated_grad_args& a, uint8_t* ws, cudaStream_t s) {
-    const BackwardPlan p = plan_backward(a);
+cudaError_t run_backward(const gad_gated_grad_args& a, const BackwardPlan& p, uint8_t* ws, cudaStream_t s) {
     const int parts = a.dtype == GAD_F32 ? 3 : 1;
     const int64_t N = a.rows;
     Sequence q{s};
@@ -762,11 +760,12 @@ extern "C" int gad_gated_feed_forward(const gad_gated_args* args, void* workspac
     const cudaStream_t s = (cudaStream_t)stream;
     if (a.rows == 0) return empty(a.status, s);
     if (!a.x || !a.w_gate || !a.w_up || !a.w_down || !a.y) return GAD_ERR_ARG;
-    const size_t need = (size_t)plan_forward(a).total;
+    const ForwardPlan p = plan_forward(a);
+    const size_t need = (size_t)p.total;
     if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need)) return GAD_ERR_OOM;
     try {
         uint8_t* ws = (uint8_t*)workspace;
-        const cudaError_t e = a.dtype == GAD_F32 ? run_forward<float>(a, ws, s) : a.dtype == GAD_F16 ? run_forward<__half>(a, ws, s) : run_forward<__nv_bfloat16>(a, ws, s);
+        const cudaError_t e = a.dtype == GAD_F32 ? run_forward<float>(a, p, ws, s) : a.dtype == GAD_F16 ? run_forward<__half>(a, p, ws, s) : run_forward<__nv_bfloat16>(a, p, ws, s);
         return e == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
     } catch (...) {   // (the table of configured kernels could not grow)
         return GAD_ERR_OOM;
@@ -791,11 +790,12 @@ extern "C" int gad_gated_feed_forward_backward(const gad_gated_grad_args* args, 
     if (a.rows == 0) return a.dtype == GAD_F32 ? run_no_rows<float>(a, s) : a.dtype == GAD_F16 ? run_no_rows<__half>(a, s) : run_no_rows<__nv_bfloat16>(a, s);
     if (!a.dy || !a.x || !a.w_gate || !a.w_up || !a.w_down || !a.act || !a.slope || !a.h) return GAD_ERR_ARG;
     if (!a.dx && !a.dw_gate && !a.dw_up && !a.dw_down) return empty(a.status, s);
-    const size_t need = (size_t)plan_backward(a).total;
+    const BackwardPlan p = plan_backward(a);
+    const size_t need = (size_t)p.total;
     if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need)) return GAD_ERR_OOM;
     try {
         uint8_t* ws = (uint8_t*)workspace;
-        const cudaError_t e = a.dtype == GAD_F32 ? run_backward<float>(a, ws, s) : a.dtype == GAD_F16 ? run_backward<__half>(a, ws, s) : run_backward<__nv_bfloat16>(a, ws, s);
+        const cudaError_t e = a.dtype == GAD_F32 ? run_backward<float>(a, p, ws, s) : a.dtype == GAD_F16 ? run_backward<__half>(a, p, ws, s) : run_backward<__nv_bfloat16>(a, p, ws, s);
         return e == cudaSuccess ? GAD_OK : GAD_ERR_CUDA;
     } catch (...) {
         return GAD_ERR_OOM;
