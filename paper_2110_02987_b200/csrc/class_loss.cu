@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "class_gemm.cuh"
+#include "gated_launch.cuh"
 #include "operand_pack.cuh"
 #include "skinny.cuh"
 
@@ -1036,8 +1037,6 @@ __global__ void class_empty_kernel(float* loss, int32_t* status) { *loss = 0.f; 
 // ---------------------------------------------------------------------------------------------
 // How a call is cut up; the same for the workspace and the launches.
 // ---------------------------------------------------------------------------------------------
-constexpr int kPairs = 74;                               // pairs of CTAs that run at once
-
 int width_for(int n) { return n <= 128 ? 128 : 256; }
 
 int few_rows(int64_t n) { return n <= 1 ? 1 : n <= 2 ? 2 : 4; }
@@ -1060,6 +1059,12 @@ struct ClassPlan {
     int64_t ldp, ldg;                // row lengths of the packed operands, and of z and G
     int64_t block;                   // rows a block
     int nblocks;
+    // fp32 gradients of a policy loss in one block of rows: dH and dW in one launch of gated_gemm_kernel, which loads all parts of a block of the reduction at once (8192 x 256 against 2048 classes:
+    // the whole call 177 us, with a launch each of class_gemm_kernel's 203)
+    bool joint;
+    Shape shape[2];
+    Cut cut[2];
+    int64_t o_joint[2];
     int64_t o_hp, o_wp, o_targets, o_starts, o_rowk, o_rowc, o_stats, o_rshares, o_lshares, o_scal, o_z, o_g, o_colsum, o_dbsum, o_slots, o_sums, o_most, total;
 };
 
@@ -1113,7 +1118,14 @@ ClassPlan plan_class(const gad_class_loss_args& a, bool policy = false) {
         p.o_z = room((p.save == kSaveCode ? 2 : 4) * p.block * p.ldg);
         p.o_g = p.save == kSaveCode ? p.o_z : room(2 * p.parts * p.block * p.ldg);
         if (a.db) { p.o_colsum = room(4 * ((p.block + 31) / 32) * p.ldg); p.o_dbsum = room(4 * (int64_t)V); }
-        if (a.dH || a.dW) p.o_slots = room((int64_t)kPairs * CT_M * p.width_d * 4);
+        p.joint = policy && p.parts == 3 && p.nblocks == 1 && (a.dH || a.dW);
+        if (p.joint) {
+            int n = 0;
+            if (a.dH) p.shape[n++] = {N, D, V, 1, 1};
+            if (a.dW) p.shape[n++] = {V, D, N, 1, 1};
+            cut_group(p.shape, n, p.pairs, p.cut);
+            for (int i = 0; i < n; ++i) p.o_joint[i] = room(slot_bytes(p.cut[i]));
+        } else if (a.dH || a.dW) p.o_slots = room((int64_t)kPairs * CT_M * p.width_d * 4);
         if (a.dW && p.nblocks > 1) p.o_sums = room(4 * (int64_t)V * D);
     }
     if (policy) p.o_most = room(4 * ((p.block + kFinishRows - 1) / kFinishRows));
@@ -1297,6 +1309,29 @@ cudaError_t run_class_steps(const gad_class_loss_args& a, const gad_policy_loss_
         if (a.db)
             GAD_TRY(chain(class_bias_kernel<T>, dim3((unsigned)((V + 31) / 32)), 256, 0, s, false, (const float*)g.colsum, p.ldg, slices, V, (const float*)scal, add,
                           reinterpret_cast<float*>(ws + p.o_dbsum), reinterpret_cast<T*>(a.db)));
+        if (p.joint) {
+            if constexpr (sizeof(T) == 4) {
+                GatedGroup<kGroup> r{};
+                Sequence q{s, false, false};
+                const auto add = [&](bool of_w, void* C, int64_t ldc) {
+                    const int i = r.n++;
+                    r.p[i] = product(p.shape[i], p.cut[i], a.dtype, of_w, 8, a.status);
+                    r.p[i].t.slots = reinterpret_cast<float*>(ws + p.o_joint[i]);
+                    r.p[i].C[0] = C; r.p[i].ldc[0] = ldc; r.p[i].factor = scal + 1;
+                    const int box = p.cut[i].width / 2;
+                    if (!of_w) {
+                        const cudaError_t e = make(r.A[i], g.G, V, nr, p.ldg, nr, CT_H);
+                        return e != cudaSuccess ? e : make_mn(r.B0[i], Wo, D, V, ldw, box, r.p[i].b_chunks);
+                    }
+                    const cudaError_t e = make_mn(r.A[i], g.G, p.ldg, nr, p.ldg, CT_H, r.p[i].a_chunks);
+                    return e != cudaSuccess ? e : make_mn(r.B0[i], Hp, D, N, p.ldp, box, r.p[i].b_chunks);
+                };
+                if (a.dH) GAD_TRY(add(false, a.dH, a.lddh));
+                if (a.dW) GAD_TRY(add(true, a.dW, a.lddw));
+                GAD_TRY((go<kPlain, kAnyMN, T>(r, q)));
+            }
+            continue;
+        }
         t.slots = reinterpret_cast<float*>(ws + p.o_slots);
         t.N = D; t.tiles_n = p.tiles_d; t.width = p.width_d; t.group = 8;
         if (a.dH) {

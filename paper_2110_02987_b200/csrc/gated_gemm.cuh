@@ -28,6 +28,7 @@ struct GatedArgs {
     int split;                 // kGate, kHidden: sums go to t.slots, whole tiles' too, and what is made of them is the join's
     int activation;
     int clear;                 // the call's first product: its first block sets the status to zero (blocks come up in order, and a wait takes 2^22 polls to run out)
+    const float* factor;       // kPlain: of the results, or null
     void *C[2];                // kPlain: result of each plane; kGate with T = float: C[0] is h where it is kept, or null
     long long ldc[2];
     // kGate: h in the operand type, parts `h_part` values apart; act(g) and u act'(g), or null.  kHidden: those two read, dg and du written (C[0], parts and planes h_part apart)
@@ -463,6 +464,11 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
                     float v[32];
                     __syncwarp();
                     tmem_ld32(at + (uint32_t)(half * half_w + c0), v);
+                    if (ga.factor) {
+                        const float f = *ga.factor;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= f;
+                    }
                     drain_rows<T>(buf, lane, v, reinterpret_cast<T*>(ga.C[plane]) + (long long)row0 * ga.ldc[plane] + col, ga.ldc[plane], rows, cols, store(ga.C[plane], ga.ldc[plane]));
                 }
                 release();

@@ -394,7 +394,7 @@ def test_kernels_wait_for_the_one_in_front():
     import os
     import re
     from test_launch_contract import kernels, CSRC
-    text = re.sub(r"//[^\n]*", "", "".join(open(os.path.join(CSRC, f)).read() for f in ("gated_few.cuh", "gated_gemm.cuh", "gated_skinny.cuh", "gated.cu")))
+    text = re.sub(r"//[^\n]*", "", "".join(open(os.path.join(CSRC, f)).read() for f in ("gated_few.cuh", "gated_gemm.cuh", "gated_launch.cuh", "gated_skinny.cuh", "gated.cu")))
     bodies = kernels(text)
     chained = set(bodies) - {"gated_zero_kernel", "gated_empty_kernel"}
     assert {"gated_gemm_kernel", "gated_join_kernel", "gated_hidden_join_kernel", "gated_pack_kernel", "skinny_kernel", "skinny_join_kernel", "few_rows_kernel"} <= chained
