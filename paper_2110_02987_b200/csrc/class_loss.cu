@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(32 * kSomeWarps, 1) class_some_kernel(const Fe
 }
 
 // Log-probabilities of 3 to 64 rows' actions (16-bit operands, no gradients: scoring), bound by reading W: classes as the rows of the product (skinny.cuh), a class a thread, sixteen rows of H in its
-// registers, for which it keeps a running softmax over the classes it sees; joined over threads at the end, over blocks by class_finish_kernel.  Sums are added up in chunks of 512 terms: the drain has
+// registers, for which it keeps a running softmax over the classes it sees; joined over threads at the end, over blocks by class_finish_kernel.  Sums are added up in chunks of 256 terms: the drain has
 // time, and a ratio of probabilities shows what a logit has lost.  Whole calls, 4096 columns against 128 000 classes: 3 rows 178 us (class_few_kernel 184; one row 177 and 164), 16 rows 179
 // (class_some_kernel 195), 64 rows 176 (tiles of 256 rows 291); 1024 against 32 768: 16 rows 19 us (24).
 constexpr int kScoreLeast = 3;
@@ -494,7 +494,7 @@ struct ScoreArgs {
 };
 __global__ void __launch_bounds__(SK_THREADS, 1) class_score_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmH, const __grid_constant__ ScoreArgs a) {
     extern __shared__ uint8_t smem_raw[];
-    constexpr int CHUNK = 8;
+    constexpr int CHUNK = 4;
     const uint32_t raw_addr = smem_u32(smem_raw);
     const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;
     uint8_t* sm = smem_raw + pad;
