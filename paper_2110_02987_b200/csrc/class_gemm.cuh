@@ -8,8 +8,8 @@
 // stages of 32 KB, so that a value that is multiplied 256 times comes from L2 62 bytes a cycle and SM; two accumulators, one filled while eight warps drain
 // the other.  Both operands may be K-major (a row of the matrix is a row of the reduction) or MN-major (the reduction runs over rows), so that H, W and G are read as they
 // lie.  Tiles are gone through in groups of rows whose operands fit the L2 beside what streams past.
-// What bounds it, 4096 x 1024 against 32 768 classes (275 GFLOP each): the tensor pipe, 77 to 79 % busy (statistics 173 us, dH 165 us with 64 tiles on 74 pairs, dW 170 us)
-// at 1.7 GHz, and in long runs the card's power: at 990 W it settles at 1.4 to 1.5 GHz, where a library's three plain products of these sizes take 682 us.
+// What bounds it, 4096 x 1024 against 32 768 classes (275 GFLOP each): the tensor pipe, 75 to 79 % busy (statistics 173 us, dH 165 us with 64 tiles on 74 pairs, at 1.7 GHz; 87 % in
+// dW, 175 us at 1.49 GHz, since each operand has a loading thread), and in long runs the card's power: at 990 W it settles at 1.4 to 1.5 GHz, where a library's three plain products of these sizes take 682 us.
 #pragma once
 
 #include <cuda.h>
