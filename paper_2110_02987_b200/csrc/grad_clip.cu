@@ -5,7 +5,7 @@
 // itself, in the same order (a ticket for the last block would have to be cleared beforehand: a launch more), and scales its chunks, the last first: those the L2 still holds.
 // Bound by HBM: the gradients are read twice, as far as the L2 does not hold them, and written once.
 //
-// Sums of squares are fp32 over the values of a chunk a thread has (two sums of 64 at most), fp64 above.  A thread's sum outside 2^-80 .. 2^100 is taken again in fp64, so no
+// Sums of squares are fp32 over the values of a chunk a thread has (two sums of about 64 at most), fp64 above.  A thread's sum outside 2^-80 .. 2^100 is taken again in fp64, so no
 // square over- or underflows; whether a sum of zero is one of zeros shows in the values' bits.
 #include <algorithm>
 #include <cmath>
