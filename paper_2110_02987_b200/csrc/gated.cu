@@ -180,7 +180,9 @@ ForwardPlan plan_forward(const gad_gated_args& a) {
 
 template <int USE, class T>
 cudaError_t go_skinny(const CUtensorMap& W0, const CUtensorMap& W1, const CUtensorMap& X, SkinnyArgs k, const SkinnyCut& c, float* parts, void* out, int64_t ldo, Sequence& q) {
-    const auto kernel = skinny_kernel<USE, T>;
+    // (with shares no longer than a chunk instead, the sums of 256 rows would take an eighth of the weights' bytes to HBM and back)
+    k.chunk = kGatedChunk<T>;
+    const auto kernel = c.kb_share > k.chunk ? skinny_kernel<USE, T, true> : skinny_kernel<USE, T, false>;
     const cudaError_t e = configure_kernel_once(reinterpret_cast<const void*>(kernel), SK_SMEM, false);
     if (e != cudaSuccess) return e;
     k.per = c.per; k.tiles = c.tiles; k.nkb = c.nkb; k.shares = c.shares; k.kb_share = c.kb_share;

@@ -18,6 +18,7 @@ struct SkinnyArgs {
     int N;                     // rows of the weights (kGate: of each)
     int per, tiles, nkb, shares, kb_share;   // per: rows of the weights a tile has (kGate: half of them of each), at most 128
     int stages;
+    int chunk;                 // ADD_UP: blocks of the reduction that an accumulator has before its sums move to registers
     int early;                 // the weights are the caller's: they may be loaded before the kernel in front has ended
     int bf16, activation, clear;
     int32_t* err;
@@ -36,7 +37,8 @@ __device__ __forceinline__ SkinnyAt skinny_at(const SkinnyArgs& a, int u) {
     return t;
 }
 
-template <int USE, class T>
+// ADD_UP: reductions longer than the tensor core may add up (kGatedChunk), in chunks whose sums the draining threads add up in registers and put back for what follows.
+template <int USE, class T, bool ADD_UP>
 __global__ void __launch_bounds__(SK_THREADS, 1)
 skinny_kernel(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ SkinnyArgs a) {
     extern __shared__ uint8_t smem_raw[];
@@ -114,24 +116,29 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ 
         bool ok = true;
         for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
             const int steps = skinny_at(a, u).nkb;
-            if (!(ok = __all_sync(0xffffffffu, mbar_wait(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 52)))) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t d = tmem_base + (uint32_t)(acc * 256);
+            int left = 0;                                          // stages until this accumulator is full
             for (int i = 0; i < steps; ++i) {
+                const bool first = left == 0;
+                if (first) {
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(tempty(acc), acc_phase ^ 1u, abort_flag, a.err, 52)))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    left = ADD_UP ? min(a.chunk, steps - i) : steps;
+                }
+                const uint32_t d = tmem_base + (uint32_t)(acc * 256);
                 if (!(ok = __all_sync(0xffffffffu, mbar_wait(full(stage), phase, abort_flag, a.err, 53)))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t base = sm_addr + stage * stage_bytes;
                 const uint64_t da = smem_desc(base), db = smem_desc(base + SK_A);
                 if (elect_one()) {
 #pragma unroll
-                    for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_one(d, da + 2 * ks, db + 2 * ks, idesc, i != 0 || ks != 0 ? 1u : 0u);
+                    for (int ks = 0; ks < CT_K / 16; ++ks) mma_f16_one(d, da + 2 * ks, db + 2 * ks, idesc, !first || ks != 0 ? 1u : 0u);
                     mma_commit(empty(stage));
-                    if (i == steps - 1) mma_commit(tfull(acc));
+                    if (left == 1) mma_commit(tfull(acc));
                 }
                 __syncwarp();
                 if (++stage == a.stages) { stage = 0; phase ^= 1u; }
+                if (--left == 0 && ++acc == 2) { acc = 0; acc_phase ^= 1u; }
             }
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
     } else {
         // ---------------- drain: a row of the weights a lane, rows of x along the columns ----------------
@@ -144,10 +151,52 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ 
         uint32_t acc_phase = 0;
         for (int u = blockIdx.x; u < units; u += gridDim.x) {
             const SkinnyAt t = skinny_at(a, u);
+            const uint32_t lanes = tmem_base + ((uint32_t)(q * 32) << 16);
             // all warps go on or none does: they meet at barriers below
-            if (!all_drain(mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 56))) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t at = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * 256);
+            const auto wait_full = [&]() {
+                const bool ok = all_drain(mbar_wait(tfull(acc), acc_phase, abort_flag, a.err, 56));
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                return ok;
+            };
+            const auto release = [&]() {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(tempty(acc));
+                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            };
+            if (!wait_full()) break;
+            if constexpr (ADD_UP) {
+                constexpr int BLOCKS = SK_MOST_ROWS / (16 * SK_GROUPS);      // of 16 rows of x, a group
+                float sum[BLOCKS][16];
+#pragma unroll
+                for (int c = 0; c < BLOCKS; ++c)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[c][j] = 0.f;
+                bool ok = true;
+                for (int left = t.nkb; ok; left -= a.chunk) {
+#pragma unroll
+                    for (int c = 0; c < BLOCKS; ++c) {
+                        const int c0 = (c * SK_GROUPS + group) * 16;
+                        if (c0 >= a.rows) break;
+                        float v[16];
+                        __syncwarp();
+                        tmem_ld16(lanes + (uint32_t)(acc * 256 + c0), v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[c][j] += v[j];
+                    }
+                    if (left <= a.chunk) break;
+                    release();
+                    ok = wait_full();
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int c = 0; c < BLOCKS; ++c) {
+                    const int c0 = (c * SK_GROUPS + group) * 16;
+                    if (c0 < a.rows) tmem_st16(lanes + (uint32_t)(acc * 256 + c0), sum[c]);
+                }
+                tmem_wait_st();
+            }
+            const uint32_t at = lanes + (uint32_t)(acc * 256);
             const int local = USE == kGate ? (q & 1) * 32 + lane : q * 32 + lane;
             const int unit_row = USE == kGate ? t.tile * half + local : t.tile * a.per + local;
             const bool valid = local < (USE == kGate ? half : a.per) && unit_row < a.N;
@@ -190,10 +239,7 @@ skinny_kernel(const __grid_constant__ CUtensorMap tmW0, const __grid_constant__ 
                     }
                 }
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(tempty(acc));
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            release();
         }
     }
 

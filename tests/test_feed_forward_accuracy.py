@@ -1,0 +1,83 @@
+"""Where the gated feed-forward block could lose more than its results' own rounding: long sums of few rows.
+
+u = 2^-24.  What is promised of 16-bit types is that the tensor core adds up no more than a chunk (fp16 8192 terms, bfloat16 65 536) before the sum goes on in fp32, each 16 terms cut off by at most 2 u of it:
+an eighth of the results' rounding, counted here with a rounding of fp32 a chunk and share.  The cuts are all to one side, so they show in the mean, where the results' own roundings (uniform where
+results spread over steps of their type, of standard deviation eps / 2 / sqrt 3 at most) leave six of theirs over the square root of the number of results."""
+import math
+
+import pytest
+
+import __graft_entry__ as entry
+import paper_2110_02987_b200 as pkg
+
+U = 2.0 ** -24
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    entry.build()
+
+
+def positive(rows, cols, g, dtype):
+    import torch
+    return torch.rand(rows, cols, generator=g, device="cuda").add_(0.5).to(dtype)
+
+
+def one_column(rows, cols, dtype, values=1.0):
+    """A matrix with values in its first column, and nothing else."""
+    import torch
+    m = torch.zeros(rows, cols, dtype=dtype, device="cuda")
+    m[:, 0] = values
+    return m
+
+
+def cut_off(K, chunk):
+    """Of a sum of K positive products: the tensor core's cuts (and up to 8 for the sums of 16 themselves), a rounding a chunk and share, at most 64 of these."""
+    return 2 * U * (min(K, chunk) / 16 + 8) + U * (K / chunk + 64)
+
+
+def held(got, want, K, chunk):
+    import torch
+    half = torch.finfo(got.dtype).eps / 2
+    off = got.double() / want - 1
+    assert float(off.abs().max()) <= (1 + 2 * half) * half + cut_off(K, chunk)
+    # Positive terms of sum 1 and their K factors in 0.5 .. 1.5: results spread by 0.3 / sqrt K.  fp16: 1.4e-3 and 1.9e-3, two to four steps of at most 2^-10; bfloat16: 0.8e-3, a tenth of a step of
+    # 2^-7, so that all are rounded alike and their mean is no measure.
+    if got.dtype != torch.float16:
+        return
+    assert abs(float(off.mean())) <= 6 * half / math.sqrt(3 * off[:1].numel()) + cut_off(K, chunk), float(off.mean())
+
+
+@gpu
+@pytest.mark.parametrize("rows", [1, 16, 200])
+def test_long_sums_of_few_rows(rows):
+    """Sums of one sign, which lose most.  First y: g is one value a unit and u is 1, so h is exact and the down projection alone rounds.  Then h: a down projection that hands it on."""
+    import torch
+    dt, chunk = torch.float16, 8192
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    D, F = 8192, 49_152
+    a = (torch.rand(F, generator=g, device="cuda") + 0.5).to(dt)
+    x, Wd = one_column(rows, D, dt), positive(D, F, g, dt).div_(16)
+    y = pkg.gated_feed_forward(x, one_column(F, D, dt, a), one_column(F, D, dt), Wd, activation="relu").check().y
+    held(y, (Wd.double() @ a.double())[None].expand(rows, D), F, chunk)
+
+    D, F = 24_576, 8192
+    x, Wg = positive(rows, D, g, dt), positive(F, D, g, dt).div_(16)
+    x[:, 0] = 1
+    y = pkg.gated_feed_forward(x, Wg, one_column(F, D, dt), torch.eye(D, F, dtype=dt, device="cuda"), activation="relu").check().y
+    held(y[:, :F], x.double() @ Wg.double().t(), D, chunk)
+    assert not y[:, F:].any()
+
+
+@gpu
+def test_long_sums_of_few_rows_in_bfloat16():
+    """A bfloat16 chunk has 65 536 terms; a reduction of two of them and a rest, with enough tiles that it is not cut into shares that short."""
+    import torch
+    dt = torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(5)
+    D, F = 9472, 140_000
+    a = (torch.rand(F, generator=g, device="cuda") + 0.5).to(dt)
+    Wd = positive(D, F, g, dt).div_(1 << 17)
+    y = pkg.gated_feed_forward(one_column(3, D, dt), one_column(F, D, dt, a), one_column(F, D, dt), Wd, activation="relu").check().y
+    held(y, torch.stack([Wd[i:i + 1184].double() @ a.double() for i in range(0, D, 1184)]).reshape(1, D).expand(3, D), F, 65_536)
