@@ -54,13 +54,14 @@ enum Layout { kBothK, kBMN, kAnyMN };
 
 // exp(-x^2 / 2) for 0 <= x <= 20: what the square and its product with log2(e) / 2 round off is put back.
 __device__ __forceinline__ float exp_half_square(float x) {
-    const float c = 0.72134752f, c_lo = 2.0164e-9f, q = x * x, a = q * c;
+    const float c = 0.72134752f, c_lo = 9.6298e-9f, q = x * x, a = q * c;
     const float lo = fmaf(q, c, -a) + fmaf(fmaf(x, x, -q), c, q * c_lo), e = exp2_fast(-a);
     return fmaf(e, -0.693147181f * lo, e);
 }
-// act(x) and act'(x).  The logistic function from exp2 and a reciprocal, each within 2 ulp.  gelu: the normal distribution's tail is half of erfc(z), z = |x| / sqrt 2, by the
-// Chebyshev fit of Press et al., Numerical Recipes ("erfcc"): erfc(z) = t exp(-z^2 + p(t)), t = 1 / (1 + z / 2), within 1.2e-7 of itself; in fp32 3.3e-7.  (With erfcf the drain
-// of a tile took 13 us longer than relu's.)
+// act(x) and act'(x).  The logistic function from exp2 and a reciprocal, each within 2 ulp, of an argument that is rounded: silu is off by 3 units of 2^-24 around 0 and by 16 at -12.9, where it is 3e-5.
+// gelu: the normal distribution's tail is half of erfc(z), z = |x| / sqrt 2, by the Chebyshev fit of Press et al., Numerical Recipes ("erfcc"): erfc(z) = t exp(-z^2 + p(t)), t = 1 / (1 + z / 2), within
+// 1.2e-7 of itself; in fp32 gelu is within 5.5e-7 of itself from -12.9 to 13.  (erfcf of -x / sqrt 2, whose rounding the square magnifies, is within 1.2e-5, and with it the drain of a tile took 13 us
+// longer than relu's.)
 __device__ __forceinline__ void activation(int kind, float x, float& a, float& d) {
     if (kind == kRelu) {
         a = x > 0.f || x != x ? x : 0.f;                   // (what is no number stays none)

@@ -81,3 +81,32 @@ def test_long_sums_of_few_rows_in_bfloat16():
     Wd = positive(D, F, g, dt).div_(1 << 17)
     y = pkg.gated_feed_forward(one_column(3, D, dt), one_column(F, D, dt, a), one_column(F, D, dt), Wd, activation="relu").check().y
     held(y, torch.stack([Wd[i:i + 1184].double() @ a.double() for i in range(0, D, 1184)]).reshape(1, D).expand(3, D), F, 65_536)
+
+
+def test_half_of_log2_e_in_two_parts():
+    """exp(-x^2 / 2) takes x^2 log2(e) / 2 with more than fp32's bits: the constant's two parts together are off by no more than the second's rounding."""
+    import os
+    import re
+    import numpy as np
+    text = open(os.path.join(os.path.dirname(pkg.__file__), "csrc", "gated_gemm.cuh")).read()
+    c, lo = (float(np.float32(v)) for v in re.search(r"exp_half_square.*?c = ([0-9.e-]+)f, c_lo = ([0-9.e-]+)f", text, re.S).groups())
+    assert abs(c + lo - math.log2(math.e) / 2) <= 1e-4 * abs(lo)
+
+
+@gpu
+def test_gelus_tail():
+    """fp32: the error relative to gelu itself does not grow with |g|.
+
+    u a part: the fit 2; t 5 (a quotient of 2 ulp, a rounding), which count 1 + 1.3 t times; the exponent's polynomial 4 and its scaling 1.5; two exponentials 3 each; products 4.  On average the roundings go (4000
+    values of either sign), and what may stay is the fit's 2, an ulp of each exponential and of the quotient, and 1 for the rest: 10."""
+    import torch
+    for lo, hi in ((-12.9, -12.4), (-12.9, -6.0), (-6.0, -1.0), (-1.0, -1e-3), (1e-3, 13.0)):
+        x = torch.linspace(lo, hi, 4001, device="cuda")[:, None]
+        one = torch.ones(1, 1, device="cuda")
+        act = pkg.gated_feed_forward(x, one, one, one, activation="gelu", save=True).check().act
+        z = -x.double() / math.sqrt(2)
+        rel = act.double() / (x.double() * 0.5 * torch.erfc(z)) - 1
+        t = 1 / (1 + 0.5 * z.abs())
+        bound = (2 + 5 * (1 + 1.3 * t) + 4 + 1.5 + 6 + 4) * U
+        assert bool((rel.abs() <= bound).all()), (lo, hi, float((rel.abs() - bound).max()) / U)
+        assert abs(float(rel.mean())) <= 10 * U, (lo, hi, float(rel.mean()) / U)
