@@ -449,7 +449,8 @@ int gad_policy_loss(const gad_policy_loss_args* args, void* workspace, size_t wo
 
 /* Gated feed-forward block:  g = x Wg^T,  u = x Wu^T,  h = act(g) u,  y = h Wd^T   for x [rows x cols], Wg and Wu [inner x cols], Wd [cols x inner].
  * For a backward pass act, slope and h [rows x inner] (all three, or none) receive act(g), u act'(g) and h, rounded to dtype.  The activations: g / (1 + exp(-g)); g times the
- * normal distribution's cumulated density (gelu, by erf); max(g, 0), whose slope at 0 is 0; 1 / (1 + exp(-g)).
+ * normal distribution's cumulated density (gelu, by erf); max(g, 0), whose slope at 0 is 0; 1 / (1 + exp(-g)).  Of an infinite g
+ * they are what the formulas give: silu and gelu of minus infinity, and their slopes at either infinity, are no numbers.
  * Sums are fp32.  fp32 matrices are multiplied to fp32 accuracy (24-bit operands in three parts); in fp16 and bfloat16 h is rounded to that type before the second product, so in fp16
  * an h above 65 504 is infinite.  The tensor core does not round its sums but cuts them, at most 2^-23 of a sum every 16 terms; longer ones than cost an eighth of the result's
  * rounding are added up in chunks (fp32: of 64 terms).  Outputs must not overlap inputs or one another.  Equal calls give equal bits.  Refused (GAD_ERR_RANGE): more than 2^30 rows, 2^20 columns,

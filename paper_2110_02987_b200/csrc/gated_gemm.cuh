@@ -72,15 +72,15 @@ __device__ __forceinline__ void activation(int kind, float x, float& a, float& d
         p = fmaf(p, t, -0.82215223f); p = fmaf(p, t, 1.48851587f); p = fmaf(p, t, -1.13520398f); p = fmaf(p, t, 0.27886807f); p = fmaf(p, t, -0.18628806f);
         p = fmaf(p, t, 0.09678418f); p = fmaf(p, t, 0.37409196f); p = fmaf(p, t, 1.00002368f); p = fmaf(p, t, -1.26551223f);
         const float tail = 0.5f * t * (e * exp2_fast(1.44269504f * p)), cdf = x < 0.f ? tail : 1.f - tail;
-        a = x == -INFINITY ? 0.f : x * cdf;
-        d = fabsf(x) == INFINITY ? cdf : fmaf(x, 0.398942280f * e, cdf);
+        a = x * cdf;
+        d = fmaf(x, 0.398942280f * e, cdf);
     } else {
         const float e = exp2_fast(-1.44269504f * x), s = __fdividef(1.f, 1.f + e);
         const float r = e == INFINITY ? 1.f : e * s;           // 1 - s
         if (kind == kSigmoid) { a = s; d = s * r; }
         else {
-            a = x == -INFINITY ? 0.f : x * s;
-            d = fabsf(x) == INFINITY ? s : s * fmaf(x, r, 1.f);
+            a = x * s;
+            d = s * fmaf(x, r, 1.f);
         }
     }
 }

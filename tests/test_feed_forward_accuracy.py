@@ -1,4 +1,4 @@
-"""Where the gated feed-forward block could lose more than its results' own rounding: long sums of few rows.
+"""Where the gated feed-forward block could lose more than its results' own rounding, or hide what is no number: long sums of few rows, gelu's tail, infinite values.
 
 u = 2^-24.  What is promised of 16-bit types is that the tensor core adds up no more than a chunk (fp16 8192 terms, bfloat16 65 536) before the sum goes on in fp32, each 16 terms cut off by at most 2 u of it:
 an eighth of the results' rounding, counted here with a rounding of fp32 a chunk and share.  The cuts are all to one side, so they show in the mean, where the results' own roundings (uniform where
@@ -110,3 +110,31 @@ def test_gelus_tail():
         bound = (2 + 5 * (1 + 1.3 * t) + 4 + 1.5 + 6 + 4) * U
         assert bool((rel.abs() <= bound).all()), (lo, hi, float((rel.abs() - bound).max()) / U)
         assert abs(float(rel.mean())) <= 10 * U, (lo, hi, float(rel.mean()) / U)
+
+
+@gpu
+@pytest.mark.parametrize("rows", [1, 5, 300])
+@pytest.mark.parametrize("kind", ["silu", "gelu", "relu", "sigmoid"])
+def test_infinite_gates(kind, rows):
+    """g of -infinity and infinity beside a finite u: what the formulas give, in the forms for few rows and in tiles.  silu and gelu of -infinity are 0 times infinity, no number."""
+    import torch
+    x = torch.ones(rows, 1, dtype=torch.float64, device="cuda")
+    x[::2] = -1
+    g = x * math.inf
+    if kind == "relu":
+        a, d = g.clamp(min=0), (g > 0).double()
+    elif kind == "gelu":
+        cdf = 0.5 * torch.erfc(-g / math.sqrt(2))
+        a, d = g * cdf, cdf + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    else:
+        s = 1 / (1 + torch.exp(-g))
+        a, d = (s, s * (1 - s)) if kind == "sigmoid" else (g * s, s * (1 + g * (1 - s)))
+    want = dict(act=a, slope=x * d, h=a * x, y=a * x)
+    for dtype in (torch.bfloat16, torch.float16) + ((torch.float32,) if rows <= 16 else ()):
+        one = torch.ones(1, 1, dtype=dtype, device="cuda")
+        for save in (False, True) if dtype != torch.float32 else (False,):
+            r = pkg.gated_feed_forward(x.to(dtype), one * math.inf, one, one, activation=kind, save=save).check()
+            for name, w in want.items():
+                t = getattr(r, name)
+                if t is not None:
+                    assert torch.equal(t.double().nan_to_num(nan=7.0), w.nan_to_num(nan=7.0)), (name, dtype, save)
