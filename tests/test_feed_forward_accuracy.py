@@ -138,3 +138,34 @@ def test_infinite_gates(kind, rows):
                 t = getattr(r, name)
                 if t is not None:
                     assert torch.equal(t.double().nan_to_num(nan=7.0), w.nan_to_num(nan=7.0)), (name, dtype, save)
+
+
+@gpu
+@pytest.mark.parametrize("rows", [6, 40])
+def test_infinite_values_in_fp32(rows):
+    """Up to 16 rows as the formulas have them; where operands are taken in three parts, no numbers in all that they have a part in, and in nothing else."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    D, F = 72, 136
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    x, Wg, Wu, Wd, dy = r(rows, D), r(F, D) / 8, r(F, D) / 8, r(D, F) / 8, r(rows, D)
+    clean = pkg.gated_feed_forward(x, Wg, Wu, Wd, activation="sigmoid").y
+    saved = pkg.gated_feed_forward(x, Wg, Wu, Wd, activation="sigmoid", save=True)
+    others = torch.arange(rows, device="cuda") != 3
+    columns = torch.arange(D, device="cuda") != 5
+
+    xi, Wi = x.clone(), Wd.clone()
+    xi[3, 7], Wi[5, 9] = math.inf, -math.inf
+    y = pkg.gated_feed_forward(xi, Wg, Wu, Wd, activation="sigmoid").check().y
+    want = (torch.sigmoid(xi[3:4].double() @ Wg.double().t()) * (xi[3:4].double() @ Wu.double().t())) @ Wd.double().t()
+    assert torch.equal(y[others], clean[others]) and not bool(y[3].isfinite().any()) and (rows <= 16 or bool(y[3].isnan().all())) and not bool(want.isfinite().any())
+    y = pkg.gated_feed_forward(x, Wg, Wu, Wi, activation="sigmoid").check().y
+    want = -math.inf * saved.h[:, 9]
+    assert torch.equal(y[:, columns], clean[:, columns]) and (torch.equal(y[:, 5], want) if rows <= 16 else bool(y[:, 5].isnan().all()))
+    kept = pkg.gated_feed_forward(xi, Wg, Wu, Wd, activation="sigmoid", save=True).check()
+    assert all(bool(getattr(kept, k)[3].isnan().all()) and torch.equal(getattr(kept, k)[others], getattr(saved, k)[others]) for k in ("y", "act", "slope", "h"))
+    dyi = dy.clone()
+    dyi[3, 7] = math.inf
+    b = pkg.gated_feed_forward_backward(dyi, x, Wg, Wu, Wd, saved.act, saved.slope, saved.h).check()
+    assert bool(b.dx[3].isnan().all()) and bool(b.dx[others].isfinite().all())
+    assert bool(b.dWd[7].isnan().all()) and bool(b.dWd[torch.arange(D, device="cuda") != 7].isfinite().all())
