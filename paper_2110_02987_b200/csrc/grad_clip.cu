@@ -5,7 +5,7 @@
 // itself, in the same order (a ticket for the last block would have to be cleared beforehand: a launch more), and scales its chunks, the last first: those the L2 still holds.
 // Bound by HBM: the gradients are read twice, as far as the L2 does not hold them, and written once.
 //
-// Sums of squares are fp32 over the values of a chunk a thread has (two sums of about 64 at most), fp64 above.  A thread's sum outside 2^-80 .. 2^100 is taken again in fp64, so no
+// Sums of squares are fp32 over the values of a chunk a thread has (two sums of at most 64 each; of rows that start anywhere 34 each, however many rows a warp has), fp64 above.  A sum outside 2^-80 .. 2^100 is taken again in fp64, so no
 // square over- or underflows; whether a sum of zero is one of zeros shows in the values' bits.
 #include <algorithm>
 #include <cmath>
@@ -111,6 +111,7 @@ __device__ __forceinline__ double chunk_squares(const ClipEntry& e, const ClipCh
 // Rows that start anywhere: a warp has up to kRun values of a row at a time, single ones up to the first and from the last 16-byte boundary on, vectors between.  (A value a lane, with a
 // division for its place, took 92 us for the norm of clip-sized 60 million values of three types, half of them in such rows, and 177 us for scaling them into fp32; now 57 and 120.)
 constexpr int kRun = 2048, kLeastRun = 128;
+constexpr int kRunMost = 2 + kRun / 64;                  // values of a whole run in one of a lane's two sums: single ones in front and behind, and half of its vectors
 template <class F>
 __device__ __forceinline__ void each_run(const ClipChunk& k, F f) {
     const int per = (k.cols + kRun - 1) / kRun, n = per * k.rows;
@@ -126,13 +127,23 @@ __device__ __forceinline__ double run_squares(const ClipEntry& e, const ClipChun
     constexpr int VEC = 16 / sizeof(T), U = 4;
     const T* base = reinterpret_cast<const T*>(e.g) + k.row * e.ld + k.col;
     const int lane = threadIdx.x & 31;
+    double total = 0.0;
     float s[2] = {0.f, 0.f};
     uint32_t some = 0;                                   // any bit of a value but its sign
+    int held = 0;                                        // values that a lane may have in either sum
     const auto one = [&](const T* p) { const float v = to_float(*p); some |= __float_as_uint(v) & 0x7FFFFFFFu; s[0] = fmaf(v, v, s[0]); };
     each_run(k, [&](int r, int c, int len) {
         const T* p = base + r * e.ld + c;
         const int head = min(len, values_to_16(p)), nv = (len - head) / VEC, tail = head + nv * VEC;
         const uint4* q = reinterpret_cast<const uint4*>(p + head);
+        // short rows: their sums go on in fp64 before either has more than kRunMost values
+        const int more = 2 + ((nv + 31) / 32 + 1) / 2 * VEC;
+        if (held + more > kRunMost) {
+            total += s[0] + s[1];
+            s[0] = s[1] = 0.f;
+            held = 0;
+        }
+        held += more;
         if (lane < head) one(p + lane);
         if (tail + lane < len) one(p + tail + lane);
         for (int i = lane; i < nv; i += 32 * U) {
@@ -149,8 +160,8 @@ __device__ __forceinline__ double run_squares(const ClipEntry& e, const ClipChun
             }
         }
     });
-    const float both = s[0] + s[1];
-    if (both >= 0x1p-80f && both <= 0x1p100f) return both;
+    total += s[0] + s[1];
+    if (total >= 0x1p-80 && total <= 0x1p100) return total;
     if (some == 0) return 0.0;
     double d = 0.0;
     each_run(k, [&](int r, int c, int len) {

@@ -1,0 +1,32 @@
+"""Lists of gradients whose rows lie anywhere: many short rows in long chunks, single rows with their values apart, tensors in the gaps of others."""
+import ctypes
+import math
+
+import pytest
+
+import __graft_entry__ as entry
+import paper_2110_02987_b200 as pkg
+from paper_2110_02987_b200 import grads as gr
+
+U = 2.0 ** -24
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    entry.build()
+
+
+@gpu
+@pytest.mark.parametrize("rows", [4000, 1_190_000])
+def test_norm_of_many_short_rows(rows):
+    """Rows of 131 values that do not start on 16 bytes, in chunks of 8192 and of 32 768 values.  The value's square is one whose fp32 sums are all rounded to the same side: 320 of them would be off by 80 u.
+
+    A sum in fp32 has at most 34 values, two of them are added: 35 roundings of u, halved by the square root, and the result's: 18.5 u; counted as 20."""
+    import torch
+    value = 1.2773438
+    g = torch.full((rows, 132), math.nan, dtype=torch.float16, device="cuda")[:, :131]
+    g.fill_(value)
+    v = float(g[0, 0])
+    n = v * math.sqrt(rows * 131)
+    assert abs(pkg.grad_norm([g]).item() - n) <= 20 * U * n
