@@ -64,6 +64,9 @@ def _entry(t, o, device, types):
         raise GadError(-1, "out must have the gradients' shapes, and their types or float32, on their device")
     oorder, orows, ocols, old = _rows(o, "out")
     if order != oorder:
+        if t.dim() == 2 and t.shape[0] == 1:
+            # one row, whose values lie apart on one side: columns of one value
+            return t.data_ptr(), types[t.dtype], types[o.dtype], t.shape[1], 1, t.stride(1), o.data_ptr(), o.stride(1)
         # a dense matrix has contiguous rows too
         if order + oorder != 1:
             raise GadError(-1, "a gradient and its out must both have contiguous rows, or both contiguous columns")

@@ -30,3 +30,18 @@ def test_norm_of_many_short_rows(rows):
     v = float(g[0, 0])
     n = v * math.sqrt(rows * 131)
     assert abs(pkg.grad_norm([g]).item() - n) <= 20 * U * n
+
+
+@gpu
+def test_a_row_whose_values_lie_apart():
+    """[1 x n] with a column stride, into a dense one and back."""
+    import torch
+    wide = torch.randn(1, 60, device="cuda")
+    g, dense = wide[:, ::3], torch.randn(1, 20, device="cuda")
+    n = math.sqrt(float((g.double() ** 2).sum()))
+    out = torch.zeros(1, 20, device="cuda")
+    pkg.clip_grads([g], n / 2, out=[out])
+    assert bool(((out.double() - g.double() / 2).abs() <= 20 * U * g.double().abs()).all())
+    keep = wide.clone()
+    pkg.clip_grads([dense], math.inf, out=[wide[:, 1::3]])
+    assert torch.equal(wide[:, 1::3], dense) and torch.equal(wide[:, ::3], keep[:, ::3]) and torch.equal(wide[:, 2::3], keep[:, 2::3])
