@@ -510,7 +510,7 @@ int gad_gated_feed_forward_backward(const gad_gated_grad_args* args, void* works
  * A tensor is [rows x cols] with a row stride of ld elements (whatever lies one value behind the other is one row).  out: where g' goes, in g's type or GAD_F32; g itself: in place (nothing is
  * written where the norm is max_norm at most); NULL: the tensor only counts for the norm.  A norm that is not finite in fp32 leaves the gradients as they are (copied to out).
  * Sums are fp32 over at most 70 values and fp64 above; no square over- or underflows.  Equal calls give equal bits.
- * The list is read on the host before the call returns.  What is written must not overlap anything else in the list (GAD_ERR_ARG; columns of one matrix may be tensors of their own); a tensor that is only
+ * The list is read on the host before the call returns.  What is written must not overlap anything else in the list (GAD_ERR_ARG; columns of one matrix, of all rows or of every second, third .. one or of one, may be tensors of their own); a tensor that is only
  * read may be there twice, and counts twice.  count 0: the norm is 0.  Refused (GAD_ERR_RANGE): more than 2^20 tensors, 2^40 values in one. */
 typedef struct {
     const void* g;

@@ -353,12 +353,14 @@ int check_tensor(const gad_grad_tensor& t) {
     return GAD_OK;
 }
 
-// What is written must not be read or written elsewhere in the list.  Column ranges of the same matrix do not meet although their first to last bytes do.
+// What is written must not be read or written elsewhere in the list.  Column ranges of the same matrix do not meet although their first to last bytes do: of all of its rows, of every second
+// (third ..) one, of one (ld 0).
 struct Region { uintptr_t lo, hi; int64_t ld, width; bool written; };
-bool meet(const Region& a, const Region& b) {
-    if (a.ld && a.ld == b.ld) {
-        const int64_t d = (int64_t)((b.lo - a.lo) % (uintptr_t)a.ld);
-        if (d >= a.width && d + b.width <= a.ld) return false;
+bool meet(const Region& a, const Region& b) {                        // (a.lo <= b.lo < a.hi)
+    const int64_t least = std::min(a.ld, b.ld), period = least ? least : std::max(a.ld, b.ld);
+    if (period && a.ld % period == 0 && b.ld % period == 0) {
+        const int64_t d = (int64_t)((b.lo - a.lo) % (uintptr_t)period);
+        if (d >= a.width && d + b.width <= period) return false;
     }
     return true;
 }

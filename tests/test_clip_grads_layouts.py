@@ -45,3 +45,22 @@ def test_a_row_whose_values_lie_apart():
     keep = wide.clone()
     pkg.clip_grads([dense], math.inf, out=[wide[:, 1::3]])
     assert torch.equal(wide[:, 1::3], dense) and torch.equal(wide[:, ::3], keep[:, ::3]) and torch.equal(wide[:, 2::3], keep[:, 2::3])
+
+
+def test_tensors_in_the_gaps_of_others():
+    """On the host: what does not meet is let through (the call then lacks its workspace), what meets is refused."""
+    L = gr._load()
+
+    def call(*entries):
+        return L.gad_clip_grads(gr._packer(len(entries)).pack(*[v for e in entries for v in e]), len(entries), 1.0, 256, None, 0, None)
+
+    def part(row, col, rows, cols, ld):                         # of a matrix with 16 columns of fp32
+        at = 4096 + 4 * (16 * row + col)
+        return (at, 0, 0, rows, cols, ld, at, ld)
+    left = part(0, 0, 8, 6, 16)
+    for other in (part(3, 6, 1, 10, 16), part(3, 6, 1, 10, 10), part(0, 6, 1, 1, 1), part(1, 8, 3, 4, 32), part(0, 6, 4, 10, 48)):
+        assert call(left, other) == -5 and call(other, left) == -5, other
+    assert call(part(0, 0, 4, 16, 32), part(1, 3, 1, 9, 9)) == -5                               # every second row, and a piece of one between
+    for other in (part(3, 5, 1, 3, 3), part(3, 6, 1, 11, 11), part(1, 8, 3, 9, 32), part(1, 5, 3, 4, 32), part(3, 0, 1, 1, 1), part(2, 8, 2, 4, 24), part(0, 3, 1, 40, 40)):
+        assert call(left, other) == -1 and call(other, left) == -1, other
+    assert call(part(0, 0, 4, 17, 32), part(1, 0, 1, 1, 1)) == -1 and call(part(0, 0, 4, 16, 32), part(2, 3, 1, 9, 9)) == -1
