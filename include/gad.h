@@ -454,7 +454,7 @@ int gad_policy_loss(const gad_policy_loss_args* args, void* workspace, size_t wo
  * Sums are fp32.  fp32 matrices are multiplied to fp32 accuracy (24-bit operands in three parts); in fp16 and bfloat16 h is rounded to that type before the second product, so in fp16
  * an h above 65 504 is infinite.  The tensor core does not round its sums but cuts them, at most 2^-23 of a sum every 16 terms; longer ones than cost an eighth of the result's
  * rounding are added up in chunks (fp32: of 64 terms).  In fp32 an infinite value of a matrix makes no numbers of all results that it has a part in, as one of its three parts is none; calls of up to
- * 16 rows that keep nothing multiply fp32 as it is (x and h of up to 51 200 columns), and have what the formulas give.  Outputs must not overlap inputs or one another.  Equal calls give equal bits.  Refused (GAD_ERR_RANGE): more than 2^30 rows, 2^20 columns,
+ * 16 rows that keep nothing multiply fp32 as it is (x and h of up to 51 200 columns), and have what the formulas give.  Pointers are on the elements of their type (GAD_ERR_ARG).  Outputs must not overlap inputs or one another.  Equal calls give equal bits.  Refused (GAD_ERR_RANGE): more than 2^30 rows, 2^20 columns,
  * 2^20 inner columns. */
 #define GAD_SILU 0
 #define GAD_GELU 1

@@ -1404,6 +1404,7 @@ int run_loss(const gad_class_loss_args& a, const gad_policy_loss_args* policy, v
     if (a.rows == 0) return a.dtype == GAD_F32 ? run_empty<float>(a, s) : a.dtype == GAD_F16 ? run_empty<__half>(a, s) : run_empty<__nv_bfloat16>(a, s);
     if (!a.H || !a.row_loss || (a.k == 0 && !a.labels) || (a.k > 0 && (!a.target_classes || !a.teacher))) return GAD_ERR_ARG;
     if (policy && (!policy->old_logp || !policy->advantages || !policy->logp)) return GAD_ERR_ARG;
+    if (policy && (((uintptr_t)policy->old_logp | (uintptr_t)policy->advantages | (uintptr_t)policy->ref_logp | (uintptr_t)policy->logp) & 3) != 0) return GAD_ERR_ARG;   // (off their elements)
     if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < (size_t)plan_class(a, policy != nullptr).total) return GAD_ERR_OOM;
     try {
         uint8_t* ws = (uint8_t*)workspace;

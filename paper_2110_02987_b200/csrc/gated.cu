@@ -398,6 +398,12 @@ int run_no_rows(const gad_gated_grad_args& a, cudaStream_t s) {
 bool sizes_ok(int dtype, int64_t rows, int cols, int inner) { return dtype >= GAD_F32 && dtype <= GAD_BF16 && rows >= 0 && cols >= 1 && inner >= 1; }
 bool in_range(int64_t rows, int cols, int inner) { return rows <= (1 << 30) && cols <= (1 << 20) && inner <= (1 << 20); }
 
+// Any of them off the elements of its type (null is on).
+bool off_elements(int dtype, std::initializer_list<const void*> all, const int32_t* status) {
+    uintptr_t bits = 0;
+    for (const void* p : all) bits |= (uintptr_t)p;
+    return (bits & (dtype == GAD_F32 ? 3 : 1)) != 0 || ((uintptr_t)status & 3) != 0;
+}
 int check_forward(const gad_gated_args* a) {
     if (!a || !sizes_ok(a->dtype, a->rows, a->cols, a->inner)) return GAD_ERR_ARG;
     if (!in_range(a->rows, a->cols, a->inner)) return GAD_ERR_RANGE;
@@ -435,7 +441,7 @@ extern "C" int gad_gated_feed_forward(const gad_gated_args* args, void* workspac
     const int rc = check_forward(args);
     if (rc != GAD_OK) return rc;
     const gad_gated_args& a = *args;
-    if (!a.status) return GAD_ERR_ARG;
+    if (!a.status || off_elements(a.dtype, {a.x, a.w_gate, a.w_up, a.w_down, a.y, a.act, a.slope, a.h}, a.status)) return GAD_ERR_ARG;
     const cudaStream_t s = (cudaStream_t)stream;
     if (a.rows == 0) return empty(a.status, s);
     if (!a.x || !a.w_gate || !a.w_up || !a.w_down || !a.y) return GAD_ERR_ARG;
@@ -464,7 +470,7 @@ extern "C" int gad_gated_feed_forward_backward(const gad_gated_grad_args* args, 
     const int rc = check_backward(args);
     if (rc != GAD_OK) return rc;
     const gad_gated_grad_args& a = *args;
-    if (!a.status) return GAD_ERR_ARG;
+    if (!a.status || off_elements(a.dtype, {a.dy, a.x, a.w_gate, a.w_up, a.w_down, a.act, a.slope, a.h, a.dx, a.dw_gate, a.dw_up, a.dw_down}, a.status)) return GAD_ERR_ARG;
     const cudaStream_t s = (cudaStream_t)stream;
     if (a.rows == 0) return a.dtype == GAD_F32 ? run_no_rows<float>(a, s) : a.dtype == GAD_F16 ? run_no_rows<__half>(a, s) : run_no_rows<__nv_bfloat16>(a, s);
     if (!a.dy || !a.x || !a.w_gate || !a.w_up || !a.w_down || !a.act || !a.slope || !a.h) return GAD_ERR_ARG;
