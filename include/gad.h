@@ -443,7 +443,8 @@ typedef struct {
     float* logp;                   /* device [rows]: lp_i                                                   */
 } gad_policy_loss_args;
 
-/* Workspace as that of gad_class_loss, and half a byte a row. */
+/* The workspace is not that of gad_class_loss: the products are cut otherwise.  Ask for it; it is larger by 260 bytes a row and 1 MB at most, and in fp32 with gradients by 320 MB more (sums of tiles
+ * that are cut along their reduction). */
 int gad_policy_loss_workspace_bytes(const gad_policy_loss_args* args, size_t* bytes);
 int gad_policy_loss(const gad_policy_loss_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
