@@ -369,7 +369,7 @@ gated_gemm_kernel(const __grid_constant__ GatedGroup<G> gr) {
                 load_block32<T>(reinterpret_cast<const T*>(ga.slope) + (long long)row0 * ga.ldslope + col, ga.ldslope, rows, a.N - col, store(ga.slope, ga.ldslope) == 16, lane, slope);
                 load_block32<T>(reinterpret_cast<const T*>(ga.act) + (long long)row0 * ga.ldact + col, ga.ldact, rows, a.N - col, store(ga.act, ga.ldact) == 16, lane, act);
             };
-            if (USE == kHidden && !ADD_UP) load_factors(t.n * a.width + half * half_w);   // (beside the sums of chunks they would spill)
+            if (USE == kHidden && !ADD_UP) load_factors(t.n * a.width + half * half_w);   // (the sums of chunks leave no registers for them: those forms spill 0.6 KB a thread as it is, in fp32 1.2)
             bool ok = true;
             const auto wait_full = [&]() {
                 ok = __all_sync(0xffffffffu, mbar_wait(tfull(acc), acc_phase, abort_flag, err, 46));

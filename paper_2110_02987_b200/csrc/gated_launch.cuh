@@ -283,7 +283,6 @@ GatedArgs product(const Shape& s, const Cut& c, int dtype, bool a_mn, int group,
     g.t.tiles_m = c.tiles_m; g.t.tiles_n = c.tiles_n; g.t.width = c.width;
     g.t.nkb = c.nkb; g.t.whole = c.whole; g.t.shares = c.shares; g.t.kb_share = c.kb_share;
     g.t.group = group;
-    g.t.pairs = dtype == GAD_F32 ? 6 : 1;
     g.t.bf16 = dtype != GAD_F16;
     g.t.err = status;
     return g;
