@@ -126,6 +126,7 @@ def clip_grads(grads, max_norm, *, out=None, stream=None):
     (before clipping), float32 [1].
 
     float32, float16 or bfloat16 (each its own), contiguous or matrices with a row stride.  In place; with ``out``, a list of tensors of the same shapes, in the
-    gradients' types or float32, what is scaled goes there instead.  A norm that is not finite leaves the values as they are."""
+    gradients' types or float32, what is scaled goes there instead.  A norm that is not finite leaves the values as they are.  Autograd does not see the call: the version counters of
+    the tensors that it writes stay as they were, so a tensor that a graph has saved must not be among them."""
     grads = list(grads) if not isinstance(grads, head.torch.Tensor if head.torch else ()) else grads
     return _clip(grads, max_norm, grads if out is None else out, stream)

@@ -310,7 +310,7 @@ def policy_loss(H, W, actions, old_logp, advantages, *, ref_logp=None, clip=0.2,
     With lp the log-probability of a row's action and r = exp(lp - old_logp), row_loss = -min(r A, clip(r, 1 - low, 1 + high) A) + kl_weight (exp(ref_logp - lp) -
     (ref_logp - lp) - 1).  actions as ``class_loss``'s labels (below zero: the row does not count); old_logp, advantages and ref_logp float32 [rows] (without ref_logp there is no
     KL term); clip: one number, or (low, high) with high up to infinity.  Everything else as in ``class_loss``.  Returns a ``PolicyLoss``, whose ``logp`` a later call may be given as
-    ``old_logp``; for the log-probabilities alone: ``-class_loss(H, W, actions, grads=False).row_loss``."""
+    ``old_logp``; for the log-probabilities alone: ``-class_loss(H, W, actions, grads=False).row_loss`` (its sums are cut otherwise: the last bits may differ)."""
     if actions is None or old_logp is None or advantages is None:
         raise GadError(-1, "actions, old_logp and advantages are needed")
     if isinstance(clip, (tuple, list)) and len(clip) != 2:

@@ -50,9 +50,9 @@ def held(got, want, K, chunk):
 
 
 @gpu
-@pytest.mark.parametrize("rows", [1, 16, 200])
+@pytest.mark.parametrize("rows", [1, 16, 200, 300])
 def test_long_sums_of_few_rows(rows):
-    """Sums of one sign, which lose most.  First y: g is one value a unit and u is 1, so h is exact and the down projection alone rounds.  Then h: a down projection that hands it on."""
+    """In the forms for up to 256 rows, and in tiles.  Sums of one sign, which lose most.  First y: g is one value a unit and u is 1, so h is exact and the down projection alone rounds.  Then h: a down projection that hands it on."""
     import torch
     dt, chunk = torch.float16, 8192
     g = torch.Generator(device="cuda").manual_seed(rows)
@@ -68,6 +68,18 @@ def test_long_sums_of_few_rows(rows):
     y = pkg.gated_feed_forward(x, Wg, one_column(F, D, dt), torch.eye(D, F, dtype=dt, device="cuda"), activation="relu").check().y
     held(y[:, :F], x.double() @ Wg.double().t(), D, chunk)
     assert not y[:, F:].any()
+
+
+@gpu
+def test_long_sums_of_a_weights_gradient():
+    """Over 50 000 rows, in whole tiles."""
+    import torch
+    dt, N, D, F = torch.float16, 50_000, 2304, 2304
+    g = torch.Generator(device="cuda").manual_seed(7)
+    dy, h = positive(N, D, g, dt).div_(16), positive(N, F, g, dt)
+    W = torch.zeros(F, D, dtype=dt, device="cuda")
+    got = pkg.gated_feed_forward_backward(dy, dy, W, W, W, h, h, h, grads="d").check().dWd
+    held(got, dy.double().t() @ h.double(), N, 8192)
 
 
 @gpu
