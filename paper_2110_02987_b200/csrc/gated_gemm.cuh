@@ -86,7 +86,7 @@ __device__ __forceinline__ void activation(int kind, float x, float& a, float& d
 }
 
 // The same of N values, g becomes act(g), with the kind looked at once: value by value the steps of one wait for one another.  (One way through for calls that keep the slope and calls that
-// do not: with code for each a tile of gelu took 10 us longer than relu's, and 4 with this.)
+// do not: with code for each gelu took longer.)  4096 x 2048 x 5504 bf16, all kept: relu 187 us, silu and sigmoid 190, gelu 204.
 template <int KIND, int N>
 __device__ __forceinline__ void activations_of(float (&g)[N], float (&d)[N]) {
 #pragma unroll
